@@ -13,7 +13,9 @@ OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["host_math.cpp", "coarse_kernels.hip", "encode_kernels.hip", "list_kernels.hip",
            "search_kernels.hip", "batch_kernels.hip", "batch_scan_b2.hip", "batch_scan_b3.hip", "batch_scan_b4.hip",
-           "batch_scan_b5.hip", "batch_scan_b8.hip", "api.hip"]
+           "batch_scan_b5.hip", "batch_scan_b8.hip", "api.hip",
+           "kv_rows.hip", "kv_pages.hip", "kv_attend_d64.hip", "kv_attend_d96.hip", "kv_attend_d128.hip", "kv_attend_d192.hip",
+           "kv_attend_d256.hip", "kv_api.hip"]
 
 # packed-fp32 instruction selection is switched off for every device compile
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

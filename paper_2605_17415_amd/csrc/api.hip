@@ -19,6 +19,7 @@
 #include "../../include/ivftq.h"
 #include "host_math.h"
 #include "kernels.h"
+#include "kv_kernels.h"
 
 using namespace ivftq;
 
@@ -127,6 +128,12 @@ std::mutex g_scratch_mutex;
 void* g_scratch_ptr[kMaxDevices] = {};
 
 }  // namespace
+
+namespace ivftq {
+void set_last_error(const char* text) {
+    try { g_error = text; } catch (...) { g_error.clear(); }
+}
+}  // namespace ivftq
 
 static __device__ __align__(256) unsigned char scratch[kNoAllocBytes];
 

@@ -1,0 +1,6 @@
+// Attention over the paged cache for heads of 192 coordinates.
+#include "kv_many.h"
+
+namespace ivftq {
+template hipError_t kv_attend_d<192>(const KvAttend&, const KvWork&, int, hipStream_t);
+}

@@ -1,0 +1,487 @@
+// Attention over the paged cache for few new rows: up to kFewRows query rows a key-value head (one token of every
+// sequence, or a few), bound by the bytes of the cache.
+//
+// A workgroup walks tiles of 32 tokens; each of its four wavefronts takes every fourth tile and keeps everything in
+// registers.  Scores are computed transposed, S^T = K Q^T (v_mfma 16x16x32: 16 tokens x 16 query rows), so a lane holds
+// scores of one query row only; which token a row of the operand is can be chosen, and is chosen so that a lane's eight
+// scores are those that the second product O^T = V^T P^T wants from that lane: no value crosses lanes between the two
+// products.  Keys and values come straight from the pages in operand layout (that is why values stand in groups of eight
+// tokens).  Running maximum and sum per query row, float32.
+//
+// Work is cut by tiles, not by sequences: the tiles of all (sequence, head) pairs, one after the other, are dealt to the
+// workgroups in equal consecutive shares.  A pair that lies whole in a share is finished there; of the others each
+// workgroup leaves at most two parts (one at its start, one at its end), which k_kv_few_join puts together.
+#pragma once
+#include "kv_kernels.h"
+
+namespace ivftq {
+
+constexpr int kFewRows = 64;          // query rows a key-value head: four column tiles of 16
+constexpr int kFewTile = 32;          // tokens of a wavefront's step
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct FewArgs {
+    KvAttend a;
+    const uint16_t* z;                // codes: rotated unit queries, float16, eights in the order of kv_levels8
+    const float* zn;                  // codes: the queries' norms
+    float* whole;                     // codes: results of pairs that one workgroup finished, before they are rotated back
+    float* part;                      // [column tile][2 * workgroups][16][D] unnormalised sums
+    float* part_ml;                   // [column tile][2 * workgroups][16][2] maximum (in log2 units), sum
+    int32_t wgs, split;               // workgroups that share the tiles; split == 0: one workgroup a pair
+};
+
+// Tiles of a sequence: those of the first tokens, then those of the window.
+struct FewSeq {
+    int first, count;                 // first new row, new rows that are computed
+    int base, end;                    // position of the first new row, one past the last one's
+    int low;                          // first token that the window of the earliest new row shows
+    int sink_tiles, window_tile, tiles;
+};
+
+__device__ __forceinline__ FewSeq few_seq(const KvAttend& a, int b) {
+    FewSeq s;
+    const int len = kv_length(a.c, b);
+    kv_new_rows(a.c, b, s.first, s.count);
+    s.base = len - s.count;
+    if (s.count > a.max_new) s.count = a.max_new;
+    s.end = s.base + s.count > 0 ? s.base + s.count : 0;
+    const int64_t low = a.window ? (int64_t)s.base - a.window + 1 : 0;
+    s.low = low > 0 ? (int)low : 0;
+    const int end = (s.end + kFewTile - 1) / kFewTile, seen = a.sinks < s.end ? a.sinks : s.end;
+    s.window_tile = s.low / kFewTile;
+    if (s.window_tile > end) s.window_tile = end;
+    s.sink_tiles = (seen + kFewTile - 1) / kFewTile;
+    if (s.sink_tiles > s.window_tile) s.sink_tiles = s.window_tile;
+    const int n = s.sink_tiles + end - s.window_tile;
+    s.tiles = s.count ? (n ? n : 1) : 0;                    // an empty sequence keeps one tile, all of it masked
+    return s;
+}
+
+__device__ __forceinline__ int few_tiles(const KvAttend& a, int b) { return b < a.c.batch ? few_seq(a, b).tiles : 0; }
+
+// Sum of tiles over all sequences (of one head), by a wavefront.
+__device__ __forceinline__ int64_t few_total(const KvAttend& a) {
+    int64_t total = 0;
+    for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+        int v = few_tiles(a, b0 + (threadIdx.x & 63));
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+        total += v;
+    }
+    return total;
+}
+
+// Tiles a workgroup takes.  At least four: one for each wavefront.
+__device__ __forceinline__ int64_t few_share(int64_t total, int wgs) {
+    const int64_t s = (total + wgs - 1) / wgs;
+    return s < 4 ? 4 : (s + 3) & ~(int64_t)3;
+}
+
+// Position x in the order (sequence, head, tile): its sequence and that sequence's first position.
+__device__ __forceinline__ void few_find(const KvAttend& a, int64_t x, int& seq, int64_t& at) {
+    const int lane = threadIdx.x & 63;
+    int64_t base = 0;
+    for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+        const int v = few_tiles(a, b0 + lane);
+        int64_t incl = v;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int64_t u = __shfl_up(incl, o); if (lane >= o) incl += u; }
+        const int64_t end = (base + incl) * a.c.heads;
+        const uint64_t past = __ballot(end > x);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            seq = b0 + l;
+            at = (base + __shfl(incl - v, l)) * a.c.heads;
+            return;
+        }
+        base += __shfl(incl, 63);
+    }
+    seq = a.c.batch; at = 0;
+}
+
+template <int F>
+__device__ __forceinline__ floatx4 kv_mfma16(uintx4 x, uintx4 y, floatx4 acc) {
+    if constexpr (F == IVFTQ_KV_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, x), __builtin_bit_cast(halfx8, y), acc, 0, 0, 0);
+}
+
+// One wavefront's tiles [from, to) in steps of four of pair (b, h): running maximum m, sum l (of this lane's tokens),
+// sums o (transposed: o[blk][r] = coordinate 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).
+template <int F, int D>
+__device__ __forceinline__ void few_walk(const FewArgs& f, const FewSeq& s, int b, int h, int col0, int from, int to, float& m, float& l,
+                                         floatx4 (&o)[D / 16]) {
+    const KvAttend& a = f.a;
+    const KvView& c = a.c;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int col = col0 + n, cols = s.count * a.group;
+    const int pos = s.base + (col < cols ? col / a.group : s.count - 1);       // position of this column's row
+    uintx4 q[D / 32];
+    float gain = a.scale * kLog2e;
+    {
+        const int64_t row = s.first + (col < cols ? col / a.group : 0), head = h * a.group + (col < cols ? col % a.group : 0);
+        if constexpr (F == IVFTQ_KV_CODE4) {
+            const int64_t at = row * a.q.heads + head;
+            gain *= f.zn[at];
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) q[k] = *reinterpret_cast<const uintx4*>(f.z + at * D + g * (D / 4) + 8 * k);
+        } else {
+            const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) q[k] = *reinterpret_cast<const uintx4*>(p + 32 * k);
+        }
+    }
+    for (int i = from; i < to; i += 4) {
+        const int t0 = (i < s.sink_tiles ? i : i - s.sink_tiles + s.window_tile) * kFewTile;
+        const int64_t p0 = kv_page(c, b, t0), p1 = kv_page(c, b, t0 + 16);
+        const char* r0 = kv_record(c, p0 < 0 ? 0 : p0, h);
+        const char* r1 = kv_record(c, p1 < 0 ? 0 : p1, h);
+        const int i0 = t0 & (c.page - 1), i1 = (t0 + 16) & (c.page - 1);
+        // lane's token of the two key operands: t0 + 8 (n / 4) + (16 bits: 4 x + n % 4; codes: 2 (n % 4) + x)
+        const int kt = 8 * (n >> 2 & 1) + (F == IVFTQ_KV_CODE4 ? 2 * (n & 3) : n & 3);
+        const char* kr = (n >> 3 ? r1 : r0);
+        const int ki = (n >> 3 ? i1 : i0) + kt;
+        const char* vr = (g >> 1 ? r1 : r0);
+        const int vi = ((g >> 1 ? i1 : i0) >> 3) + (g & 1);           // group of eight tokens in the page
+        floatx4 st[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        float sc[8];
+        uint32_t vw[D / 16];
+        uintx4 vv[D / 16], vg;
+        if constexpr (F == IVFTQ_KV_CODE4) {
+            const int codes = c.page * (D / 2);
+            uint32_t kw[2][D / 32];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t* p = reinterpret_cast<const uint32_t*>(kr + (int64_t)(ki + x) * (D / 2)) + g * (D / 32);
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) kw[x][k] = p[k];
+            }
+            const uintx4 kg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + vi * 16);
+            vg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + 2 * c.page + vi * 16);
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(vr + codes) + (int64_t)vi * D + n * (D / 16);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) vw[k] = p[k];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) st[x] = kv_mfma16<F>(__builtin_bit_cast(uintx4, kv_levels8(kw[x][k], c)), q[k], st[x]);
+            const halfx8 kn = __builtin_bit_cast(halfx8, kg);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sc[e] = st[e & 1][e >> 1] * ((float)kn[e] * gain);       // token e of the eight
+        } else {
+            uintx4 kk[2][D / 32];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uintx4* p = reinterpret_cast<const uintx4*>(kr + (int64_t)(ki + 4 * x) * (D * 2)) + g;
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) kk[x][k] = p[4 * k];
+            }
+            const uintx4* p = reinterpret_cast<const uintx4*>(vr + (int64_t)c.page * (D * 2)) + (int64_t)vi * D + n;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) vv[k] = p[16 * k];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) st[x] = kv_mfma16<F>(kk[x][k], q[k], st[x]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3] * gain;
+        }
+        // every token of the tile visible to every row?
+        const bool full = p0 >= 0 && p1 >= 0 && t0 + kFewTile - 1 <= s.base &&
+                          (!a.window || (int64_t)t0 > (int64_t)s.end - 1 - a.window || t0 + kFewTile <= a.sinks);
+        uint32_t shown = 0xff;              // of the lane's eight tokens: those that any row sees
+        if (!full) {
+            const bool there = (g >> 1 ? p1 : p0) >= 0;
+            shown = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = t0 + 8 * g + e;
+                const bool any = there && t < s.end && (t >= s.low || t < a.sinks);
+                const bool mine = any && t <= pos && (!a.window || (int64_t)t > (int64_t)pos - a.window || t < a.sinks);
+                shown |= any ? 1u << e : 0u;
+                if (!mine) sc[e] = -INFINITY;
+            }
+        }
+        float top = sc[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__ballot(top > m)) {
+            const float now = fmaxf(m, top), turn = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= turn;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) o[k] *= turn;
+        }
+        float pr[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            pr[e] = sc[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sc[e] - m);
+            l += pr[e];
+        }
+        if constexpr (F == IVFTQ_KV_CODE4) {
+            const halfx8 vn = __builtin_bit_cast(halfx8, vg);
+            halfx8 p;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float w = pr[e] * (float)vn[e];
+                p[kv_slot(e)] = (_Float16)(shown >> e & 1 && sc[e] != -INFINITY ? w : 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                o[k] = kv_mfma16<F>(__builtin_bit_cast(uintx4, kv_levels8(vw[k], c)), __builtin_bit_cast(uintx4, p), o[k]);
+        } else {
+            constexpr bool bf = F == IVFTQ_KV_BF16;
+            const uintx4 p = {kv_pack2<bf>(pr[0], pr[1]), kv_pack2<bf>(pr[2], pr[3]), kv_pack2<bf>(pr[4], pr[5]), kv_pack2<bf>(pr[6], pr[7])};
+            uint32_t dirty = 0;             // of the lane's eight tokens: no finite value, and not the same to every row
+            if (!full) {                    // what nobody sees may be anything, and 0 * NaN is no zero
+                if (s.count > 1) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) dirty |= kv_not_finite<bf>(vv[k]);
+#pragma unroll
+                    for (int w = 1; w < 16; w <<= 1) dirty |= __shfl_xor(dirty, w);
+                    dirty &= shown;
+                    shown &= ~dirty;
+                }
+                uintx4 keep;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) keep[e] = (shown >> 2 * e & 1 ? 0xffffu : 0u) | (shown >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) vv[k] &= keep;
+            }
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) o[k] = kv_mfma16<F>(vv[k], p, o[k]);
+            if (__ballot(dirty != 0)) {     // such tokens one by one, for the rows that see them
+                for (int t = 0; t < kFewTile; ++t) {
+                    const int from = t >> 3, e = t & 7;
+                    if (!(__shfl(dirty, 16 * from) >> e & 1)) continue;
+                    float v = sc[0], w = pr[0];
+#pragma unroll
+                    for (int i2 = 1; i2 < 8; ++i2) { v = e == i2 ? sc[i2] : v; w = e == i2 ? pr[i2] : w; }
+                    v = __shfl(v, 16 * from + n);
+                    w = __shfl(w, 16 * from + n);
+                    const uint16_t* y = reinterpret_cast<const uint16_t*>((from >> 1 ? r1 : r0) + (int64_t)c.page * (D * 2)) +
+                                        (int64_t)(((from >> 1 ? i1 : i0) >> 3) + (from & 1)) * D * 8 + e;
+                    if (v == -INFINITY) continue;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[k][r] += w * kv_to_float<bf>(y[(16 * k + 4 * g + r) * 8]);
+                }
+            }
+        }
+    }
+}
+
+template <int F>
+__device__ __forceinline__ int few_coord(int D, int k, int g, int r) { return F == IVFTQ_KV_CODE4 ? (4 * g + r) * (D / 16) + k : 16 * k + 4 * g + r; }
+
+template <int F, int D>
+__global__ __launch_bounds__(256) void k_kv_few(FewArgs f) {
+    constexpr int kPass = D > 128 ? D / 2 : D;                 // coordinates that pass through LDS at a time
+    __shared__ float sum[4][16][kPass + 1];
+    __shared__ float ml[4][16][2];
+    const KvAttend& a = f.a;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int col0 = blockIdx.y * 16;
+    int64_t x = 0, end = 0, at = 0;
+    int b = 0;
+    if (f.split) {
+        const int64_t total = few_total(a) * a.c.heads, share = few_share(total, f.wgs);
+        x = blockIdx.x * share;
+        end = x + share < total ? x + share : total;
+        if (x >= end) return;
+        few_find(a, x, b, at);
+    } else {
+        b = blockIdx.x / a.c.heads;
+    }
+    const int64_t begin = x;
+    FewSeq s = few_seq(a, b);
+    while (true) {
+        int h, from, to;
+        if (f.split) {
+            while (b < a.c.batch && x >= at + (int64_t)s.tiles * a.c.heads) {        // the next sequence that has tiles
+                at += (int64_t)s.tiles * a.c.heads;
+                if (++b < a.c.batch) s = few_seq(a, b);
+            }
+            if (b >= a.c.batch) return;
+            h = (int)((x - at) / s.tiles);
+            const int64_t pair = at + (int64_t)h * s.tiles;
+            from = (int)(x - pair);
+            to = (int)(end - pair < s.tiles ? end - pair : s.tiles);
+        } else {
+            h = blockIdx.x % a.c.heads;
+            from = 0;
+            to = s.tiles;
+            if (!s.tiles) return;
+        }
+        const int cols = s.count * a.group;
+        const bool whole = from == 0 && to == s.tiles;
+        if (col0 < cols) {
+            float m = -INFINITY, l = 0.f;
+            floatx4 o[D / 16];
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) o[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+            few_walk<F, D>(f, s, b, h, col0, from + wave, to, m, l, o);
+            l = kv_sum4(l);
+            if (g == 0) { ml[wave][n][0] = m; ml[wave][n][1] = l; }
+            __syncthreads();
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][n][0]);
+            const float turn = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+            for (int pass = 0; pass < D / kPass; ++pass) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = few_coord<F>(D, k, g, r) - pass * kPass;
+                        if (j >= 0 && j < kPass) sum[wave][n][j] = o[k][r] * turn;
+                    }
+                __syncthreads();
+                for (int i = threadIdx.x; i < 16 * (kPass / 2); i += 256) {
+                    const int row = i / (kPass / 2), j = i % (kPass / 2) * 2, col = col0 + row;
+                    if (col >= cols) break;
+                    float tm = -INFINITY, tl = 0.f, u = 0.f, v = 0.f;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) tm = fmaxf(tm, ml[w][row][0]);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        tl += ml[w][row][0] == -INFINITY ? ml[w][row][1] * 0.f : ml[w][row][1] * __builtin_amdgcn_exp2f(ml[w][row][0] - tm);
+                        u += sum[w][row][j];
+                        v += sum[w][row][j + 1];
+                    }
+                    const int64_t qrow = s.first + col / a.group;
+                    const int qhead = h * a.group + col % a.group, jj = pass * kPass + j;
+                    if (whole) {
+                        const float inv = tm == -INFINITY && tl == 0.f ? 0.f : 1.f / tl;
+                        if (F == IVFTQ_KV_CODE4) {
+                            *reinterpret_cast<float2*>(f.whole + (qrow * a.q.heads + qhead) * D + jj) = make_float2(u * inv, v * inv);
+                        } else {
+                            uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride + jj;
+                            *reinterpret_cast<uint32_t*>(p) = kv_pack2<F == IVFTQ_KV_BF16>(u * inv, v * inv);
+                        }
+                        if (a.lse && jj == 0) a.lse[qrow * a.q.heads + qhead] = tl > 0.f ? (tm + __builtin_amdgcn_logf(tl)) / kLog2e : (tl == 0.f ? -INFINITY : tl);
+                    } else {
+                        // a share's first part belongs to a pair that began before it, its last part to one that goes on
+                        const int64_t slot = (int64_t)blockIdx.y * 2 * f.wgs + 2 * blockIdx.x + (x == begin && from != 0 ? 0 : 1);
+                        *reinterpret_cast<float2*>(f.part + (slot * 16 + row) * D + jj) = make_float2(u, v);
+                        if (jj == 0) *reinterpret_cast<float2*>(f.part_ml + (slot * 16 + row) * 2) = make_float2(tm, tl);
+                    }
+                }
+                __syncthreads();
+            }
+        }
+        if (!f.split) return;
+        x += to - from;
+        if (x >= end) return;
+    }
+}
+
+// Pairs whose tiles lie in more than one share: their parts put together.  One workgroup a pair and column tile; a
+// wavefront takes a row at a time.  Codes: every pair, whose 16 rows are then rotated back by the first wavefront.
+template <int F, int D>
+__global__ __launch_bounds__(256) void k_kv_few_join(FewArgs f) {
+    __shared__ float row_sum[16][D + 4];
+    const KvAttend& a = f.a;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int b = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, col0 = blockIdx.y * 16;
+    const FewSeq s = few_seq(a, b);
+    const int cols = s.count * a.group;
+    if (col0 >= cols) return;
+    int64_t w0 = 0, w1 = 0, lo = 0, share = 1;
+    if (f.split) {
+        int64_t total = 0, before = 0;
+        for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+            const int i = b0 + lane;
+            int v = few_tiles(a, i), u = i < b ? v : 0;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) { v += __shfl_xor(v, o); u += __shfl_xor(u, o); }
+            total += v;
+            before += u;
+        }
+        share = few_share(total * a.c.heads, f.wgs);
+        lo = before * a.c.heads + (int64_t)h * s.tiles;
+        w0 = lo / share;
+        w1 = (lo + s.tiles - 1) / share;
+    }
+    const bool joined = w0 != w1;
+    if (!joined && F != IVFTQ_KV_CODE4) return;
+    for (int row = wave; row < 16 && col0 + row < cols; row += 4) {
+        const int col = col0 + row;
+        const int64_t qrow = s.first + col / a.group;
+        const int qhead = h * a.group + col % a.group;
+        float acc[(D + 63) / 64] = {};
+        if (joined) {
+            float top = -INFINITY, l = 0.f;
+            for (int64_t w = w0 + lane; w <= w1; w += 64) {
+                const int64_t slot = (int64_t)blockIdx.y * 2 * f.wgs + 2 * w + (w * share > lo ? 0 : 1);
+                top = fmaxf(top, f.part_ml[(slot * 16 + row) * 2]);
+            }
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+            for (int64_t w = w0; w <= w1; ++w) {
+                const int64_t slot = (int64_t)blockIdx.y * 2 * f.wgs + 2 * w + (w * share > lo ? 0 : 1);
+                const float2 u = *reinterpret_cast<const float2*>(f.part_ml + (slot * 16 + row) * 2);
+                const float turn = u.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u.x - top);
+                l += u.y * turn;
+#pragma unroll
+                for (int k = 0; k < (D + 63) / 64; ++k)
+                    if (64 * k + lane < D) acc[k] += f.part[(slot * 16 + row) * D + 64 * k + lane] * turn;
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+            for (int k = 0; k < (D + 63) / 64; ++k) acc[k] *= inv;
+            if (a.lse && lane == 0) a.lse[qrow * a.q.heads + qhead] = l > 0.f ? (top + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
+        } else if constexpr (F == IVFTQ_KV_CODE4) {
+#pragma unroll
+            for (int k = 0; k < (D + 63) / 64; ++k)
+                if (64 * k + lane < D) acc[k] = f.whole[(qrow * a.q.heads + qhead) * D + 64 * k + lane];
+        }
+        if constexpr (F == IVFTQ_KV_CODE4) {
+#pragma unroll
+            for (int k = 0; k < (D + 63) / 64; ++k)
+                if (64 * k + lane < D) row_sum[row][64 * k + lane] = acc[k];
+        } else {
+            uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride;
+#pragma unroll
+            for (int k = 0; k < (D + 63) / 64; ++k)
+                if (64 * k + lane < D) p[64 * k + lane] = kv_from_float<F == IVFTQ_KV_BF16>(acc[k]);
+        }
+    }
+    if constexpr (F == IVFTQ_KV_CODE4) {
+        __syncthreads();
+        if (wave) return;
+        const int n = lane & 15, g = lane >> 4;
+        const bool in = col0 + n < cols;
+        float x[D / 32][8], y[D / 32][8], n2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f; n2 += x[k][e] * x[k][e]; }
+        const float norm = sqrtf(kv_sum4(n2)), scale = norm > 0.f ? 1.f / norm : 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[k][e] *= scale;
+        kv_rotate16<D, true>(a.c.rotation, x, y);
+        if (!in) return;
+        const int col = col0 + n;
+        const int64_t qrow = s.first + col / a.group;
+        const int qhead = h * a.group + col % a.group;
+        uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride + g * (D / 4);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            uintx4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = a.out.type == IVFTQ_KV_BF16 ? kv_pack2<true>(y[k][2 * e] * norm, y[k][2 * e + 1] * norm) : kv_pack2<false>(y[k][2 * e] * norm, y[k][2 * e + 1] * norm);
+            *reinterpret_cast<uintx4*>(p + 8 * k) = w;
+        }
+    }
+}
+
+}  // namespace ivftq

@@ -1,0 +1,225 @@
+// What the translation units of the paged key-value cache share: the cache as kernels see it, the page look-up, the
+// 4-bit levels, 16-row products with the rotation.  The public side is include/ivftq_kv.h.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/ivftq_kv.h"
+#include "kernels.h"
+
+namespace ivftq {
+
+void set_last_error(const char* text);      // api.hip: the message of ivftq_last_error()
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// One layer's cache.  magnitudes: the eight positive levels as float16, low bytes in tab_lo, high bytes in tab_hi.
+struct KvView {
+    char* pool;
+    const int32_t* table;
+    const int32_t* lengths;
+    const int32_t* starts;       // null: one row per sequence
+    const float* rotation;
+    int64_t pages, table_stride, head_bytes, page_bytes;
+    int32_t batch, columns, page, page_log2, heads, rows;
+    uint32_t tab_lo[2], tab_hi[2];
+    float level[8], bound[7];    // positive levels and the boundaries between them
+};
+
+struct KvRows {
+    char* data;
+    int64_t row_stride, head_stride;      // elements
+    int32_t rows, heads, type;
+};
+
+struct KvAttend {
+    KvView c;
+    KvRows q, out;
+    float* lse;
+    int32_t group, max_new, window, sinks;
+    float scale;
+    char* work;
+};
+
+hipError_t launch_kv_append(const KvView& c, const KvRows& k, const KvRows& v, int d, int format, hipStream_t st);
+hipError_t launch_kv_read(const KvView& c, const KvRows& k, const KvRows& v, int d, int format, hipStream_t st);
+hipError_t launch_kv_reserve(const ivftq_kv_pages& s, const int32_t* counts, int32_t* granted, int32_t* scratch, hipStream_t st);
+hipError_t launch_kv_fork(const ivftq_kv_pages& s, const ivftq_kv_pools& p, const int32_t* parents, const int32_t* children, int n, int32_t* done,
+                          int32_t* scratch, hipStream_t st);
+hipError_t launch_kv_free(const ivftq_kv_pages& s, const int32_t* rows, int n, hipStream_t st);
+hipError_t launch_kv_trim(const ivftq_kv_pages& s, int window, int sinks, hipStream_t st);
+hipError_t launch_kv_compact(const ivftq_kv_pages& s, const ivftq_kv_pools& p, int32_t* used, int32_t* scratch, hipStream_t st);
+hipError_t launch_kv_copy(const ivftq_kv_pools& p, const int32_t* src, const int32_t* dst, const int32_t* count, int n, hipStream_t st);
+
+inline int64_t kv_head_bytes(int format, int page, int d) {
+    return format == IVFTQ_KV_CODE4 ? (int64_t)page * (d + 4) : (int64_t)page * d * 4;
+}
+
+#ifdef __HIPCC__
+
+// ---- sequences and pages -------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ int kv_length(const KvView& c, int b) {
+    const int64_t cap = (int64_t)c.columns << c.page_log2;
+    const int n = c.lengths[b];
+    return n < 0 ? 0 : (int)(n < cap ? n : (cap < 0x7fffff00 ? cap : 0x7fffff00));
+}
+
+// First row and number of rows of sequence b; what `starts` says is held inside the rows that there are.
+__device__ __forceinline__ void kv_new_rows(const KvView& c, int b, int& first, int& count) {
+    if (!c.starts) { first = b; count = b < c.rows ? 1 : 0; return; }
+    const int s = c.starts[b], e = c.starts[b + 1];
+    first = s < 0 ? 0 : (s < c.rows ? s : c.rows);
+    const int end = e < first ? first : (e < c.rows ? e : c.rows);
+    count = end - first;
+}
+
+// The sequence that row r belongs to: the last b with starts[b] <= r (a search of bounded length whatever starts holds).
+__device__ __forceinline__ int kv_sequence_of(const KvView& c, int r) {
+    if (!c.starts) return r;
+    int lo = 0, hi = c.batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (c.starts[mid] <= r) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// Number of the page that holds token t of sequence b, -1 where there is none.
+__device__ __forceinline__ int64_t kv_page(const KvView& c, int b, int t) {
+    const int col = t >> c.page_log2;
+    if ((unsigned)col >= (unsigned)c.columns) return -1;
+    const int32_t id = c.table[(int64_t)b * c.table_stride + col];
+    return id >= 0 && id < c.pages ? id : -1;
+}
+
+__device__ __forceinline__ char* kv_record(const KvView& c, int64_t page, int head) {
+    return c.pool + page * c.page_bytes + (int64_t)head * c.head_bytes;
+}
+
+// ---- 4-bit levels --------------------------------------------------------------------------------------------------
+
+// Eight half bytes as eight float16 levels, in the order 0 2 4 6 1 3 5 7: the eight magnitudes' high and low bytes are
+// each a table of eight bytes, which one byte permutation looks up for four codes at a time, and the sign bit goes into
+// the high byte.  14 operations for eight values.
+__device__ __forceinline__ halfx8 kv_levels8(uint32_t w, const KvView& c) {
+    const uint32_t even = w & 0x07070707u, odd = (w >> 4) & 0x07070707u;
+    const uint32_t even_hi = __builtin_amdgcn_perm(c.tab_hi[1], c.tab_hi[0], even) | ((w << 4) & 0x80808080u);
+    const uint32_t odd_hi = __builtin_amdgcn_perm(c.tab_hi[1], c.tab_hi[0], odd) | (w & 0x80808080u);
+    const uint32_t even_lo = __builtin_amdgcn_perm(c.tab_lo[1], c.tab_lo[0], even);
+    const uint32_t odd_lo = __builtin_amdgcn_perm(c.tab_lo[1], c.tab_lo[0], odd);
+    uintx4 r;
+    r[0] = __builtin_amdgcn_perm(even_hi, even_lo, 0x05010400u);
+    r[1] = __builtin_amdgcn_perm(even_hi, even_lo, 0x07030602u);
+    r[2] = __builtin_amdgcn_perm(odd_hi, odd_lo, 0x05010400u);
+    r[3] = __builtin_amdgcn_perm(odd_hi, odd_lo, 0x07030602u);
+    return __builtin_bit_cast(halfx8, r);
+}
+// Place of half byte i in that order.
+__device__ __forceinline__ constexpr int kv_slot(int i) { return (i & 1) * 4 + (i >> 1); }
+
+__device__ __forceinline__ float kv_level(uint32_t nibble, const KvView& c) {
+    const int m = nibble & 7;
+    const float v = m < 4 ? (m < 2 ? (m ? c.level[1] : c.level[0]) : (m == 2 ? c.level[2] : c.level[3]))
+                          : (m < 6 ? (m == 4 ? c.level[4] : c.level[5]) : (m == 6 ? c.level[6] : c.level[7]));
+    return nibble & 8 ? -v : v;
+}
+
+// Sign and magnitude of the level next to v: bins [tau_i, tau_i+1), so a negative value on a boundary belongs to the
+// smaller magnitude.  No number: magnitude 0.
+__device__ __forceinline__ uint32_t kv_nibble(float v, const KvView& c) {
+    const float a = __builtin_fabsf(v);
+    const bool neg = v < 0.f;
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 7; ++i) m += neg ? a > c.bound[i] : a >= c.bound[i];
+    return m | (neg ? 8u : 0u);
+}
+
+// ---- 16-bit rows ---------------------------------------------------------------------------------------------------
+
+template <bool BF>
+__device__ __forceinline__ float kv_to_float(uint32_t bits) {
+    if constexpr (BF) return __builtin_bit_cast(float, bits << 16);
+    else return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+}
+template <bool BF>
+__device__ __forceinline__ uint16_t kv_from_float(float v) {
+    if constexpr (BF) return __builtin_bit_cast(uint16_t, (__bf16)v);
+    else return __builtin_bit_cast(uint16_t, (_Float16)v);
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t kv_pack2(float a, float b) {
+    return (uint32_t)kv_from_float<BF>(a) | (uint32_t)kv_from_float<BF>(b) << 16;
+}
+
+// Which of the eight 16-bit values of w are no finite numbers, a bit each.
+template <bool BF>
+__device__ __forceinline__ uint32_t kv_not_finite(uintx4 w) {
+    constexpr uint32_t top = BF ? 0x7f80u : 0x7c00u;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bad |= ((w[e >> 1] >> 16 * (e & 1)) & top) == top ? 1u << e : 0u;
+    return bad;
+}
+
+__device__ __forceinline__ float kv_sum4(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+
+// ---- products with the rotation ------------------------------------------------------------------------------------
+
+// y = Pi x (or Pi^T x) for 16 rows.  Lane l holds row l % 16, coordinates 32 s + 8 (l / 16) + e in x[s][e], and gets
+// coordinates (l / 16) * D / 4 + 8 s + e in y[s][e]: which coordinate a row of the matrix operand is can be chosen freely,
+// and this choice leaves every lane with neighbouring ones.  Rows should be of length about one (the caller scales them):
+// both sides go in as sums of two float16 numbers, three products, so y is good to about 2^-21 of the row's length, far
+// under the distance of two levels; one product alone would move one code in two thousand.
+template <int D, bool TRANSPOSED>
+__device__ __forceinline__ void kv_rotate16(const float* __restrict__ pi, const float (&x)[D / 32][8], float (&y)[D / 32][8]) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    halfx8 bh[D / 32], bl[D / 32];
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = x[s][e] * kSplitScale;
+            bh[s][e] = (_Float16)v;
+            bl[s][e] = (_Float16)(v - (float)bh[s][e]);
+        }
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = (m >> 2) * (D / 4) + 8 * t + 4 * half + (m & 3);
+            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) {
+                float p[8];
+                if constexpr (TRANSPOSED) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = pi[(32 * s + 8 * g + e) * D + i];
+                } else {
+                    const float4* r = reinterpret_cast<const float4*>(pi + i * D + 32 * s + 8 * g);
+                    const float4 u = r[0], w = r[1];
+                    p[0] = u.x; p[1] = u.y; p[2] = u.z; p[3] = u.w; p[4] = w.x; p[5] = w.y; p[6] = w.z; p[7] = w.w;
+                }
+                halfx8 ah, al;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = p[e] * kSplitScale;
+                    ah[e] = (_Float16)v;
+                    al[e] = (_Float16)(v - (float)ah[e]);
+                }
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh[s], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl[s], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh[s], acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[t][4 * half + r] = acc[r] * (1.f / (kSplitScale * kSplitScale));
+        }
+}
+
+#endif
+}  // namespace ivftq

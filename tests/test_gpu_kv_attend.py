@@ -1,0 +1,272 @@
+"""Attention over the paged cache against float64, row by row: both kernels (few and many new rows), every format and head size, lengths
+from nothing to several shares, windows, first tokens, missing pages, what is no number in places that nobody sees."""
+import math
+
+import numpy as np
+import pytest
+
+import kv_reference as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _pkg():
+    import paper_2605_17415_amd as pkg
+    return pkg
+
+
+def starts_of(news):
+    return torch.tensor([0] + list(np.cumsum(news)), dtype=torch.int32, device=DEV)
+
+
+def queries(seed, rows, heads, d, dtype):
+    return (torch.randn(rows, heads, d, generator=torch.Generator().manual_seed(seed)) * 1.5).to(dtype).to(DEV)
+
+
+def run(c, q, news=None, want_lse=True, **mask):
+    t, codec = c.device()
+    lse = torch.full(q.shape[:2], 5.0, device=DEV) if want_lse else None
+    where = {} if news is None else {"starts": starts_of(news), "max_new": max(news)}
+    out = _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], lse=lse, **where, **mask, **codec)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+FORMS = [("f16", "f16"), ("bf16", "bf16"), ("code4", "bf16"), ("code4", "f16")]
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 32), (128, 64), (192, 16), (256, 128)])
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("lens", ([1], [0, 33, 7], [513, 16, 1200, 0, 1]))
+def test_one_token(form, kind, d, page, lens):
+    heads, group = (2, 3) if d < 192 else (1, 4)
+    c = ref.Cache(d + len(lens), form, heads, d, page, lens)
+    q = queries(d, len(lens), heads * group, d, ref.TYPES[kind])
+    print(f"one token {form} d={d} page={page} lens={lens}", flush=True)
+    out, lse = run(c, q)
+    ref.check_attention(c, q.cpu(), out, [1] * len(lens), lse=lse)
+
+
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (7, 3), (64, 4), (100, 40), (31, 600), (5000, 2)])
+def test_one_token_with_a_window(form, kind, window, sinks):
+    lens = [700, 20, 65, 0, 300]
+    c = ref.Cache(window, form, 2, 64, 16, lens)
+    q = queries(window, len(lens), 4, 64, ref.TYPES[kind])
+    out, lse = run(c, q, window=window, sinks=sinks)
+    ref.check_attention(c, q.cpu(), out, [1] * len(lens), lse=lse, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("group", (1, 8, 16, 17, 64))
+def test_heads_of_a_group(form, kind, group):
+    c = ref.Cache(group, form, 2, 128, 32, [130, 700])
+    q = queries(group, 2, 2 * group, 128, ref.TYPES[kind])
+    out, lse = run(c, q)
+    ref.check_attention(c, q.cpu(), out, [1, 1], lse=lse)
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 16), (128, 64), (192, 32), (256, 16)])
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 5)])
+def test_several_tokens(form, kind, d, page, window, sinks):
+    """Few rows: a handful of new tokens a sequence, among them sequences without any and with fewer tokens than rows."""
+    lens, news = [90, 3, 40, 600, 0], [3, 5, 0, 4, 1]
+    c = ref.Cache(d, form, 2, d, page, lens)
+    q = queries(d, sum(news), 4, d, ref.TYPES[kind])
+    out, lse = run(c, q, news, window=window, sinks=sinks)
+    ref.check_attention(c, q.cpu(), out, news, lse=lse, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 16), (128, 64), (192, 32), (256, 16)])
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 5), (1, 0), (70, 130)])
+def test_many_tokens(form, kind, d, page, window, sinks):
+    lens, news = [150, 260, 40, 0, 1], [150, 67, 41, 2, 1]
+    c = ref.Cache(d + window, form, 1, d, page, lens)
+    q = queries(d, sum(news), 3, d, ref.TYPES[kind])
+    print(f"many tokens {form} d={d} page={page} window={window}", flush=True)
+    out, lse = run(c, q, news, window=window, sinks=sinks)
+    ref.check_attention(c, q.cpu(), out, news, lse=lse, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("new", (1, 65))
+def test_missing_pages(form, kind, new):
+    """Entries that name no page hold no visible token; a sequence without any page sees nothing."""
+    lens, news = [200, 150, 100], [new, new, new]
+    c = ref.Cache(1, form, 2, 64, 16, lens)
+    c.table[0, 2], c.table[0, 5], c.table[1, 0] = -1, c.pages, -2 ** 31
+    c.table[2] = -1
+    q = queries(1, 3 * new, 4, 64, ref.TYPES[kind])
+    out, lse = run(c, q, news)
+    ref.check_attention(c, q.cpu(), out, news, lse=lse)
+    assert (out[2 * new:] == 0).all()
+
+
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("new,window,sinks", [(1, 0, 0), (1, 40, 3), (70, 0, 0), (70, 40, 3), (3, 0, 0), (3, 40, 3)])
+def test_no_numbers_where_nobody_looks(form, kind, new, window, sinks):
+    """Everything that no row of a sequence sees is NaN or infinite: the pages' ends, what lies before the window, free pages."""
+    lens = [133, 81]
+    c = ref.Cache(2, form, 2, 64, 16, lens)
+    q = queries(2, 2 * new, 4, 64, ref.TYPES[kind])
+    hidden = np.ones((c.pages, c.page), bool)
+    for b, n in enumerate(lens):
+        for t in range(n):
+            if not window or t > n - new - window or t < sinks:
+                hidden[c.table[b, t // c.page], t % c.page] = False
+    for p, t in zip(*np.nonzero(hidden)):
+        bad = (float("nan"), float("inf"), float("-inf"))[(p + t) % 3]
+        if form == "code4":
+            c.norms[:, p, :, t] = bad
+        else:
+            c.rows16[:, p, :, t] = bad
+    out, lse = run(c, q, [new, new], window=window, sinks=sinks)
+    shown = ref.Cache(2, form, 2, 64, 16, lens)
+    ref.check_attention(shown, q.cpu(), out, [new, new], lse=lse, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("form", ("f16", "bf16", "code4"))
+@pytest.mark.parametrize("bad", (float("nan"), float("inf")))
+@pytest.mark.parametrize("new", (6, 100))
+def test_no_number_in_a_later_token_leaves_earlier_rows_alone(form, bad, new):
+    """A token that only the later rows see: rows before it have the results that they have without it."""
+    c = ref.Cache(3, form, 1, 64, 16, [new + 40])
+    q = queries(3, new, 2, 64, ref.TYPES["bf16" if form == "code4" else form])
+    want, _ = run(c, q, [new])
+    at = new + 40 - 3                                       # seen by the last three rows
+    if form == "code4":
+        c.norms[:, c.table[0, at // 16], :, at % 16] = bad
+    else:
+        c.rows16[:, c.table[0, at // 16], :, at % 16, 5] = bad
+    got, _ = run(c, q, [new])
+    assert torch.equal(got[:-3], want[:-3])
+    assert not torch.isfinite(got[-3:]).all()
+
+
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+def test_long_sequences_in_many_shares(form, kind):
+    """Long enough that a pair is split over many workgroups, next to short ones; large scores at either end of the cache."""
+    lens = [20_011, 5, 4096, 777]
+    c = ref.Cache(4, form, 1, 64, 64, lens)
+    if form != "code4":
+        c.rows16[0, c.table[0, 0], 0, 3] *= 4
+        c.rows16[0, c.table[0, -1], 0, 1] *= 4
+    q = queries(4, 4, 4, 64, ref.TYPES[kind])
+    out, lse = run(c, q)
+    ref.check_attention(c, q.cpu(), out, [1] * 4, lse=lse)
+    again, _ = run(c, q)
+    assert torch.equal(out, again)                          # no order of atomics in it
+
+
+def test_many_sequences():
+    """More sequences than lanes: shares are found by scans over them."""
+    lens = [int(x) for x in np.random.default_rng(0).integers(0, 200, 150)] + [900]
+    c = ref.Cache(5, "bf16", 2, 64, 16, lens)
+    q = queries(5, len(lens), 2, 64, torch.bfloat16)
+    out, lse = run(c, q)
+    ref.check_attention(c, q.cpu(), out, [1] * len(lens), lse=lse)
+
+
+def test_far_offsets():
+    """A pool past 2^32 bytes, pages at its end."""
+    pkg = _pkg()
+    heads, d, page = 4, 128, 64
+    each = pkg.kv_page_bytes(1, page, heads, d)
+    pages = (5 << 30) // each
+    pool = torch.empty(pages, heads, 2, page, d, dtype=torch.bfloat16, device=DEV)
+    pool[-40:].normal_()
+    c = ref.Cache(6, "bf16", heads, d, page, [40 * page - 7], spare=0)
+    c.rows16 = torch.zeros(2, 40, heads, page, d, dtype=torch.bfloat16)
+    far = pool[-40:].cpu()
+    c.pages = 40
+    c.take(far)
+    q = queries(6, 1, 8, d, torch.bfloat16)
+    table = torch.from_numpy(c.table).to(DEV) + (pages - 40)
+    out = pkg.kv_attend(q, pool, table, torch.tensor(c.lens, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    ref.check_attention(c, q.cpu(), out, [1])
+
+
+@pytest.mark.parametrize("form", ("bf16", "code4"))
+@pytest.mark.parametrize("new", (1, 80))
+def test_strides_scale_and_an_own_output(form, new):
+    pkg = _pkg()
+    lens = [130, 90]
+    c = ref.Cache(8, form, 2, 64, 32, lens)
+    t, codec = c.device()
+    qkv = torch.randn(2 * new, 12, 64, device=DEV).bfloat16()
+    q = qkv[:, 4:8]                                         # heads inside a wider matrix
+    out = torch.full((2 * new, 6, 64), 9.0, dtype=torch.bfloat16, device=DEV)
+    got = pkg.kv_attend(q, t["pool"], t["table"], t["lengths"], starts=starts_of([new, new]), max_new=new, scale=0.3, out=out[:, 1:5], **codec)
+    torch.cuda.synchronize()
+    assert got.data_ptr() == out[:, 1:5].data_ptr() and (out[:, 0] == 9).all() and (out[:, 5] == 9).all()
+    ref.check_attention(c, q.cpu(), got, [new, new], scale=0.3)
+
+
+@pytest.mark.parametrize("form", ("f16", "code4"))
+def test_in_a_graph_and_on_another_stream(form):
+    """Captured once, replayed with other lengths, tables and queries in the same tensors; eager work between the replays."""
+    pkg = _pkg()
+    c = ref.Cache(10, form, 2, 64, 16, [300, 80])
+    t, codec = c.device()
+    kind = ref.TYPES["f16"]
+    q, k, v = queries(1, 2, 4, 64, kind), queries(2, 2, 2, 64, kind), queries(3, 2, 2, 64, kind)
+    out = torch.empty_like(q)
+
+    def step(pool):
+        pkg.kv_append(pool, k, v, t["table"], t["lengths"], **codec)
+        pkg.kv_attend(q, pool, t["table"], t["lengths"], out=out, **codec)
+
+    step(t["pool"])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            step(t["pool"])
+    torch.cuda.current_stream().wait_stream(s)
+    for n, lens in enumerate(([300, 80], [17, 1], [299, 64])):
+        t["lengths"].copy_(torch.tensor(lens, dtype=torch.int32))
+        q.copy_(queries(20 + n, 2, 4, 64, kind))
+        k.copy_(queries(30 + n, 2, 2, 64, kind))
+        torch.cuda.synchronize()
+        other = t["pool"].clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        step(other)
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(other, t["pool"])
+
+
+def test_refusals_with_tensors():
+    pkg = _pkg()
+    c = ref.Cache(11, "bf16", 2, 64, 16, [20])
+    t, _ = c.device()
+    q = queries(1, 1, 4, 64, torch.bfloat16)
+    good = (q, t["pool"], t["table"], t["lengths"])
+    pkg.kv_attend(*good)
+    for bad in ((q.half(), *good[1:]), (q[..., :32].contiguous(), *good[1:]), (q.float(), *good[1:]), (q[:, :3].contiguous(), *good[1:]),
+                (torch.cat([q, q]), *good[1:]), (q, t["pool"][:, :, :1], *good[2:]), (q, t["pool"].transpose(0, 1), *good[2:]),
+                (q, t["pool"], t["table"].long(), t["lengths"]), (q, t["pool"], t["table"], t["lengths"].repeat(2)), (q.cpu(), *good[1:]),
+                (torch.empty(1, 4, 128, dtype=q.dtype, device=DEV)[..., ::2], *good[1:])):
+        with pytest.raises((TypeError, ValueError, pkg.IvftqError)):
+            pkg.kv_attend(*bad)
+    with pytest.raises(pkg.IvftqError):
+        pkg.kv_attend(*good, window=-1)
+    with pytest.raises(ValueError):
+        pkg.kv_attend(*good, out=torch.empty(1, 2, 64, dtype=q.dtype, device=DEV))
+    with pytest.raises(ValueError):
+        pkg.kv_attend(*good, lse=torch.empty(4, device=DEV))
+    with pytest.raises((TypeError, ValueError)):
+        pkg.kv_attend(*good, starts=torch.zeros(3, dtype=torch.int32, device=DEV))
+    code = ref.Cache(11, "code4", 2, 64, 16, [20])
+    t2, codec = code.device()
+    for change in (dict(rotation=codec["rotation"][:32]), dict(rotation=codec["rotation"].double()), dict(levels=codec["levels"][:8]), dict(levels=codec["levels"] + 1)):
+        with pytest.raises((ValueError, pkg.IvftqError)):
+            pkg.kv_attend(q, t2["pool"], t2["table"], t2["lengths"], **{**codec, **change})
