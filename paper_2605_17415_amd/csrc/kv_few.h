@@ -22,7 +22,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 struct FewArgs {
     KvAttend a;
-    const uint16_t* z;                // codes: rotated unit queries, float16, eights in the order of kv_levels8
+    const uint16_t* z;                // codes: rotated unit queries, two float16 parts [2][rows][heads][D], eights in the order of kv_levels8
     const float* zn;                  // codes: the queries' norms
     float* whole;                     // codes: results of pairs that one workgroup finished, before they are rotated back
     float* part;                      // [column tile][2 * workgroups][16][D] unnormalised sums
@@ -68,7 +68,7 @@ __device__ __forceinline__ int64_t few_total(const KvAttend& a) {
         for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
         total += v;
     }
-    return total;
+    return kv_uniform(total);
 }
 
 // Tiles a workgroup takes.  At least four: one for each wavefront.
@@ -91,10 +91,10 @@ __device__ __forceinline__ void few_find(const KvAttend& a, int64_t x, int& seq,
         if (past) {
             const int l = __builtin_ctzll(past);
             seq = b0 + l;
-            at = (base + __shfl(incl - v, l)) * a.c.heads;
+            at = kv_uniform(base + (int64_t)__shfl(incl - v, l)) * a.c.heads;
             return;
         }
-        base += __shfl(incl, 63);
+        base += kv_uniform((int64_t)__shfl(incl, 63));
     }
     seq = a.c.batch; at = 0;
 }
@@ -107,170 +107,244 @@ __device__ __forceinline__ floatx4 kv_mfma16(uintx4 x, uintx4 y, floatx4 acc) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, x), __builtin_bit_cast(halfx8, y), acc, 0, 0, 0);
 }
 
-// One wavefront's tiles [from, to) in steps of four of pair (b, h): running maximum m, sum l (of this lane's tokens),
-// sums o (transposed: o[blk][r] = coordinate 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).
+// What a tile of 32 tokens is read into.  Codes: a lane's words of the two key operands, its words of the value operands,
+// the norms of its eight tokens; 16 bits: the operands themselves.
+template <int F, int D>
+struct FewTile {
+    static constexpr bool kCodes = F == IVFTQ_KV_CODE4;
+    uint32_t kw[2][kCodes ? D / 32 : 1], vw[kCodes ? D / 16 : 1];
+    uintx4 kg, vg;
+    uintx4 kk[2][kCodes ? 1 : D / 32], vv[kCodes ? 1 : D / 16];
+};
+struct FewPlace { int t0; int64_t p0, p1; };                // first token, pages of its two halves (-1: none)
+
+__device__ __forceinline__ FewPlace few_place(const KvView& c, const FewSeq& s, int b, int i) {
+    FewPlace p;
+    p.t0 = (i < s.sink_tiles ? i : i - s.sink_tiles + s.window_tile) * kFewTile;
+    p.p0 = kv_page(c, b, p.t0);
+    p.p1 = kv_page(c, b, p.t0 + 16);
+    return p;
+}
+
+template <int F, int D>
+__device__ __forceinline__ void few_load(const KvView& c, int h, const FewPlace& p, FewTile<F, D>& x) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const char* r0 = kv_record(c, p.p0 < 0 ? 0 : p.p0, h);
+    const char* r1 = kv_record(c, p.p1 < 0 ? 0 : p.p1, h);
+    const int i0 = p.t0 & (c.page - 1), i1 = (p.t0 + 16) & (c.page - 1);
+    // lane's token of the two key operands: t0 + 8 (n / 4) + (16 bits: 4 y + n % 4; codes: 2 (n % 4) + y)
+    const char* kr = n >> 3 ? r1 : r0;
+    const int ki = (n >> 3 ? i1 : i0) + 8 * (n >> 2 & 1) + (F == IVFTQ_KV_CODE4 ? 2 * (n & 3) : n & 3);
+    const char* vr = g >> 1 ? r1 : r0;
+    const int vi = ((g >> 1 ? i1 : i0) >> 3) + (g & 1);               // group of eight tokens in the page
+    if constexpr (F == IVFTQ_KV_CODE4) {
+        const int codes = c.page * (D / 2);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(kr + (ki + y) * (D / 2)) + g * (D / 32);
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) x.kw[y][k] = q[k];
+        }
+        x.kg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + vi * 16);
+        x.vg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + 2 * c.page + vi * 16);
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(vr + codes) + vi * D + n * (D / 16);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) x.vw[k] = q[k];
+    } else {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const uintx4* q = reinterpret_cast<const uintx4*>(kr + (ki + 4 * y) * (D * 2)) + g;
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) x.kk[y][k] = q[4 * k];
+        }
+        const uintx4* q = reinterpret_cast<const uintx4*>(vr + c.page * (D * 2)) + vi * D + n;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) x.vv[k] = q[16 * k];
+    }
+}
+
+// One query row a lane: its operands, what its scores are multiplied by, its position.
+template <int F, int D>
+struct FewQuery {
+    uintx4 q[D / 32], low[F == IVFTQ_KV_CODE4 ? D / 32 : 1];
+    float gain;
+    int pos;
+};
+
+template <int F, int D>
+__device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int h, int col0, FewQuery<F, D>& x) {
+    const KvAttend& a = f.a;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int cols = s.count * a.group, col = col0 + n < cols ? col0 + n : 0, tok = a.max_new == 1 ? 0 : col / a.group;
+    x.pos = col0 + n < cols ? s.base + tok : s.end - 1;
+    x.gain = a.scale * kLog2e;
+    const int64_t row = s.first + tok, head = h * a.group + col - tok * a.group;
+    if constexpr (F == IVFTQ_KV_CODE4) {
+        const int64_t at = row * a.q.heads + head, all = (int64_t)a.q.rows * a.q.heads;
+        x.gain *= f.zn[at] * (a.c.level_unit / kSplitScale);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            x.q[k] = *reinterpret_cast<const uintx4*>(f.z + at * D + g * (D / 4) + 8 * k);
+            x.low[k] = *reinterpret_cast<const uintx4*>(f.z + (all + at) * D + g * (D / 4) + 8 * k);
+        }
+    } else {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) x.q[k] = *reinterpret_cast<const uintx4*>(p + 32 * k);
+    }
+}
+
+// A tile into the running maximum m, sum l (of this lane's tokens) and sums o (transposed: o[blk][r] = coordinate
+// 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).
+template <int F, int D>
+__device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int h, const FewQuery<F, D>& q, const FewPlace& at, FewTile<F, D>& x, float& m,
+                                         float& l, floatx4 (&o)[D / 16]) {
+    const KvView& c = a.c;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, t0 = at.t0;
+    floatx4 st[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    float sc[8];                            // of the tokens t0 + 8 g + e
+    if constexpr (F == IVFTQ_KV_CODE4) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                const uintx4 w = __builtin_bit_cast(uintx4, kv_levels8(x.kw[y][k], c));
+                st[y] = kv_mfma16<F>(w, q.q[k], st[y]);
+                st[y] = kv_mfma16<F>(w, q.low[k], st[y]);
+            }
+        const halfx8 kn = __builtin_bit_cast(halfx8, x.kg);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sc[e] = st[e & 1][e >> 1] * ((float)kn[e] * q.gain);
+    } else {
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) st[y] = kv_mfma16<F>(x.kk[y][k], q.q[k], st[y]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3] * q.gain;
+    }
+    // every token of the tile visible to every row?
+    const bool full = at.p0 >= 0 && at.p1 >= 0 && t0 + kFewTile - 1 <= s.base &&
+                      (!a.window || (int64_t)t0 > (int64_t)s.end - 1 - a.window || t0 + kFewTile <= a.sinks);
+    uint32_t shown = 0xff;                  // of the lane's eight tokens: those that any row sees
+    if (!full) {
+        const bool there = (g >> 1 ? at.p1 : at.p0) >= 0;
+        shown = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int t = t0 + 8 * g + e;
+            const bool any = there && t < s.end && (t >= s.low || t < a.sinks);
+            const bool mine = any && t <= q.pos && (!a.window || (int64_t)t > (int64_t)q.pos - a.window || t < a.sinks);
+            shown |= any ? 1u << e : 0u;
+            if (!mine) sc[e] = -INFINITY;
+        }
+    }
+    float top = sc[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (__ballot(top > m)) {
+        const float now = fmaxf(m, top), turn = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= turn;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) o[k] *= turn;
+    }
+    float pr[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(sc[e] - m);
+    if (!full) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pr[e] = sc[e] == -INFINITY ? 0.f : pr[e];       // a row that has seen nothing has no maximum
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) l += pr[e];
+    if constexpr (F == IVFTQ_KV_CODE4) {
+        const halfx8 vn = __builtin_bit_cast(halfx8, x.vg);
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = pr[e] * (float)vn[e];
+        if (!full) {                        // what a row does not see may be anything, and 0 * NaN is no zero
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = shown >> e & 1 && sc[e] != -INFINITY ? w[e] : 0.f;
+        }
+        const uintx4 p = {kv_pack2<false>(w[0], w[2]), kv_pack2<false>(w[4], w[6]), kv_pack2<false>(w[1], w[3]), kv_pack2<false>(w[5], w[7])};
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) o[k] = kv_mfma16<F>(__builtin_bit_cast(uintx4, kv_levels8(x.vw[k], c)), p, o[k]);
+    } else {
+        constexpr bool bf = F == IVFTQ_KV_BF16;
+        const uintx4 p = {kv_pack2<bf>(pr[0], pr[1]), kv_pack2<bf>(pr[2], pr[3]), kv_pack2<bf>(pr[4], pr[5]), kv_pack2<bf>(pr[6], pr[7])};
+        uint32_t dirty = 0;                 // of the lane's eight tokens: no finite value, and not the same to every row
+        if (!full) {
+            if (s.count > 1) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) dirty |= kv_not_finite<bf>(x.vv[k]);
+#pragma unroll
+                for (int w = 1; w < 16; w <<= 1) dirty |= __shfl_xor(dirty, w);
+                dirty &= shown;
+                shown &= ~dirty;
+            }
+            uintx4 keep;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) keep[e] = (shown >> 2 * e & 1 ? 0xffffu : 0u) | (shown >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) x.vv[k] &= keep;
+        }
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) o[k] = kv_mfma16<F>(x.vv[k], p, o[k]);
+        if (!full && __ballot(dirty != 0)) {         // such tokens one by one, for the rows that see them
+            for (int t = 0; t < kFewTile; ++t) {
+                const int from = t >> 3, e = t & 7;
+                if (!(__shfl(dirty, 16 * from) >> e & 1)) continue;
+                float v = sc[0], w = pr[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) { v = e == i ? sc[i] : v; w = e == i ? pr[i] : w; }
+                v = __shfl(v, 16 * from + n);
+                w = __shfl(w, 16 * from + n);
+                const int64_t page = from >> 1 ? at.p1 : at.p0;
+                const int in = (t0 + t) & (c.page - 1);
+                const uint16_t* y = reinterpret_cast<const uint16_t*>(kv_record(c, page < 0 ? 0 : page, h) + c.page * (D * 2)) + (in >> 3) * D * 8 + e;
+                if (v == -INFINITY) continue;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[k][r] += w * kv_to_float<bf>(y[(16 * k + 4 * g + r) * 8]);
+            }
+        }
+    }
+}
+
+// One wavefront's tiles [from, to) in steps of four.  Codes: the next tile's words are on their way while this one is
+// worked on (a tile is 24 registers, its arithmetic as long as its loads), the pages of the one after are looked up.  16
+// bits: a tile's 16 KB in flight are enough, only the pages are looked up ahead.
 template <int F, int D>
 __device__ __forceinline__ void few_walk(const FewArgs& f, const FewSeq& s, int b, int h, int col0, int from, int to, float& m, float& l,
                                          floatx4 (&o)[D / 16]) {
-    const KvAttend& a = f.a;
-    const KvView& c = a.c;
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int col = col0 + n, cols = s.count * a.group;
-    const int pos = s.base + (col < cols ? col / a.group : s.count - 1);       // position of this column's row
-    uintx4 q[D / 32];
-    float gain = a.scale * kLog2e;
-    {
-        const int64_t row = s.first + (col < cols ? col / a.group : 0), head = h * a.group + (col < cols ? col % a.group : 0);
-        if constexpr (F == IVFTQ_KV_CODE4) {
-            const int64_t at = row * a.q.heads + head;
-            gain *= f.zn[at];
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) q[k] = *reinterpret_cast<const uintx4*>(f.z + at * D + g * (D / 4) + 8 * k);
-        } else {
-            const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) q[k] = *reinterpret_cast<const uintx4*>(p + 32 * k);
+    const KvView& c = f.a.c;
+    if (from >= to) return;
+    FewQuery<F, D> q;
+    few_query<F, D>(f, s, h, col0, q);
+    FewPlace at = few_place(c, s, b, from);
+    if constexpr (F == IVFTQ_KV_CODE4) {
+        FewTile<F, D> x, y;
+        few_load<F, D>(c, h, at, x);
+        FewPlace next = few_place(c, s, b, from + 4 < to ? from + 4 : from);
+        for (int i = from; i < to; i += 4) {
+            const FewPlace then = few_place(c, s, b, i + 8 < to ? i + 8 : i);
+            few_load<F, D>(c, h, next, y);                    // past the end: a tile that is there, read and not used
+            few_step<F, D>(f.a, s, h, q, at, x, m, l, o);
+            x = y;
+            at = next;
+            next = then;
         }
-    }
-    for (int i = from; i < to; i += 4) {
-        const int t0 = (i < s.sink_tiles ? i : i - s.sink_tiles + s.window_tile) * kFewTile;
-        const int64_t p0 = kv_page(c, b, t0), p1 = kv_page(c, b, t0 + 16);
-        const char* r0 = kv_record(c, p0 < 0 ? 0 : p0, h);
-        const char* r1 = kv_record(c, p1 < 0 ? 0 : p1, h);
-        const int i0 = t0 & (c.page - 1), i1 = (t0 + 16) & (c.page - 1);
-        // lane's token of the two key operands: t0 + 8 (n / 4) + (16 bits: 4 x + n % 4; codes: 2 (n % 4) + x)
-        const int kt = 8 * (n >> 2 & 1) + (F == IVFTQ_KV_CODE4 ? 2 * (n & 3) : n & 3);
-        const char* kr = (n >> 3 ? r1 : r0);
-        const int ki = (n >> 3 ? i1 : i0) + kt;
-        const char* vr = (g >> 1 ? r1 : r0);
-        const int vi = ((g >> 1 ? i1 : i0) >> 3) + (g & 1);           // group of eight tokens in the page
-        floatx4 st[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-        float sc[8];
-        uint32_t vw[D / 16];
-        uintx4 vv[D / 16], vg;
-        if constexpr (F == IVFTQ_KV_CODE4) {
-            const int codes = c.page * (D / 2);
-            uint32_t kw[2][D / 32];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const uint32_t* p = reinterpret_cast<const uint32_t*>(kr + (int64_t)(ki + x) * (D / 2)) + g * (D / 32);
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) kw[x][k] = p[k];
-            }
-            const uintx4 kg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + vi * 16);
-            vg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + 2 * c.page + vi * 16);
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(vr + codes) + (int64_t)vi * D + n * (D / 16);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) vw[k] = p[k];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) st[x] = kv_mfma16<F>(__builtin_bit_cast(uintx4, kv_levels8(kw[x][k], c)), q[k], st[x]);
-            const halfx8 kn = __builtin_bit_cast(halfx8, kg);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sc[e] = st[e & 1][e >> 1] * ((float)kn[e] * gain);       // token e of the eight
-        } else {
-            uintx4 kk[2][D / 32];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const uintx4* p = reinterpret_cast<const uintx4*>(kr + (int64_t)(ki + 4 * x) * (D * 2)) + g;
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) kk[x][k] = p[4 * k];
-            }
-            const uintx4* p = reinterpret_cast<const uintx4*>(vr + (int64_t)c.page * (D * 2)) + (int64_t)vi * D + n;
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) vv[k] = p[16 * k];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) st[x] = kv_mfma16<F>(kk[x][k], q[k], st[x]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3] * gain;
-        }
-        // every token of the tile visible to every row?
-        const bool full = p0 >= 0 && p1 >= 0 && t0 + kFewTile - 1 <= s.base &&
-                          (!a.window || (int64_t)t0 > (int64_t)s.end - 1 - a.window || t0 + kFewTile <= a.sinks);
-        uint32_t shown = 0xff;              // of the lane's eight tokens: those that any row sees
-        if (!full) {
-            const bool there = (g >> 1 ? p1 : p0) >= 0;
-            shown = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int t = t0 + 8 * g + e;
-                const bool any = there && t < s.end && (t >= s.low || t < a.sinks);
-                const bool mine = any && t <= pos && (!a.window || (int64_t)t > (int64_t)pos - a.window || t < a.sinks);
-                shown |= any ? 1u << e : 0u;
-                if (!mine) sc[e] = -INFINITY;
-            }
-        }
-        float top = sc[0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__ballot(top > m)) {
-            const float now = fmaxf(m, top), turn = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
-            m = now;
-            l *= turn;
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) o[k] *= turn;
-        }
-        float pr[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            pr[e] = sc[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sc[e] - m);
-            l += pr[e];
-        }
-        if constexpr (F == IVFTQ_KV_CODE4) {
-            const halfx8 vn = __builtin_bit_cast(halfx8, vg);
-            halfx8 p;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float w = pr[e] * (float)vn[e];
-                p[kv_slot(e)] = (_Float16)(shown >> e & 1 && sc[e] != -INFINITY ? w : 0.f);
-            }
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                o[k] = kv_mfma16<F>(__builtin_bit_cast(uintx4, kv_levels8(vw[k], c)), __builtin_bit_cast(uintx4, p), o[k]);
-        } else {
-            constexpr bool bf = F == IVFTQ_KV_BF16;
-            const uintx4 p = {kv_pack2<bf>(pr[0], pr[1]), kv_pack2<bf>(pr[2], pr[3]), kv_pack2<bf>(pr[4], pr[5]), kv_pack2<bf>(pr[6], pr[7])};
-            uint32_t dirty = 0;             // of the lane's eight tokens: no finite value, and not the same to every row
-            if (!full) {                    // what nobody sees may be anything, and 0 * NaN is no zero
-                if (s.count > 1) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) dirty |= kv_not_finite<bf>(vv[k]);
-#pragma unroll
-                    for (int w = 1; w < 16; w <<= 1) dirty |= __shfl_xor(dirty, w);
-                    dirty &= shown;
-                    shown &= ~dirty;
-                }
-                uintx4 keep;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) keep[e] = (shown >> 2 * e & 1 ? 0xffffu : 0u) | (shown >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) vv[k] &= keep;
-            }
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) o[k] = kv_mfma16<F>(vv[k], p, o[k]);
-            if (__ballot(dirty != 0)) {     // such tokens one by one, for the rows that see them
-                for (int t = 0; t < kFewTile; ++t) {
-                    const int from = t >> 3, e = t & 7;
-                    if (!(__shfl(dirty, 16 * from) >> e & 1)) continue;
-                    float v = sc[0], w = pr[0];
-#pragma unroll
-                    for (int i2 = 1; i2 < 8; ++i2) { v = e == i2 ? sc[i2] : v; w = e == i2 ? pr[i2] : w; }
-                    v = __shfl(v, 16 * from + n);
-                    w = __shfl(w, 16 * from + n);
-                    const uint16_t* y = reinterpret_cast<const uint16_t*>((from >> 1 ? r1 : r0) + (int64_t)c.page * (D * 2)) +
-                                        (int64_t)(((from >> 1 ? i1 : i0) >> 3) + (from & 1)) * D * 8 + e;
-                    if (v == -INFINITY) continue;
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[k][r] += w * kv_to_float<bf>(y[(16 * k + 4 * g + r) * 8]);
-                }
-            }
+    } else {
+        for (int i = from; i < to; i += 4) {
+            FewTile<F, D> x;
+            few_load<F, D>(c, h, at, x);
+            const FewPlace next = few_place(c, s, b, i + 4 < to ? i + 4 : i);
+            few_step<F, D>(f.a, s, h, q, at, x, m, l, o);
+            at = next;
         }
     }
 }
@@ -284,7 +358,7 @@ __global__ __launch_bounds__(256) void k_kv_few(FewArgs f) {
     __shared__ float sum[4][16][kPass + 1];
     __shared__ float ml[4][16][2];
     const KvAttend& a = f.a;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int col0 = blockIdx.y * 16;
     int64_t x = 0, end = 0, at = 0;
     int b = 0;
@@ -382,17 +456,21 @@ __global__ __launch_bounds__(256) void k_kv_few(FewArgs f) {
 }
 
 // Pairs whose tiles lie in more than one share: their parts put together.  One workgroup a pair and column tile; a
-// wavefront takes a row at a time.  Codes: every pair, whose 16 rows are then rotated back by the first wavefront.
+// wavefront takes a row at a time, its lanes the parts' weights first, then coordinates.  Codes: every pair; its 16 rows are
+// then rotated back, each wavefront computing every fourth block of 32 coordinates.
 template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_few_join(FewArgs f) {
-    __shared__ float row_sum[16][D + 4];
+    constexpr int kLanes = (D + 63) / 64;
+    __shared__ float row_sum[F == IVFTQ_KV_CODE4 ? 16 : 1][D + 4];
+    __shared__ float weight[4][64];
     const KvAttend& a = f.a;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = kv_wave(), lane = threadIdx.x & 63;
     const int b = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, col0 = blockIdx.y * 16;
     const FewSeq s = few_seq(a, b);
     const int cols = s.count * a.group;
     if (col0 >= cols) return;
-    int64_t w0 = 0, w1 = 0, lo = 0, share = 1;
+    int64_t lo = 0, share = 1;
+    int w0 = 0, w1 = 0;
     if (f.split) {
         int64_t total = 0, before = 0;
         for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
@@ -403,10 +481,12 @@ __global__ __launch_bounds__(256) void k_kv_few_join(FewArgs f) {
             total += v;
             before += u;
         }
+        total = kv_uniform(total);
+        before = kv_uniform(before);
         share = few_share(total * a.c.heads, f.wgs);
         lo = before * a.c.heads + (int64_t)h * s.tiles;
-        w0 = lo / share;
-        w1 = (lo + s.tiles - 1) / share;
+        w0 = (int)(lo / share);
+        w1 = (int)((lo + s.tiles - 1) / share);
     }
     const bool joined = w0 != w1;
     if (!joined && F != IVFTQ_KV_CODE4) return;
@@ -414,72 +494,74 @@ __global__ __launch_bounds__(256) void k_kv_few_join(FewArgs f) {
         const int col = col0 + row;
         const int64_t qrow = s.first + col / a.group;
         const int qhead = h * a.group + col % a.group;
-        float acc[(D + 63) / 64] = {};
+        float acc[kLanes] = {};
         if (joined) {
             float top = -INFINITY, l = 0.f;
-            for (int64_t w = w0 + lane; w <= w1; w += 64) {
-                const int64_t slot = (int64_t)blockIdx.y * 2 * f.wgs + 2 * w + (w * share > lo ? 0 : 1);
-                top = fmaxf(top, f.part_ml[(slot * 16 + row) * 2]);
-            }
+            // of the pair's first share the pair has the last part, of the others the first
+            const int64_t base = (int64_t)blockIdx.y * 2 * f.wgs;
+            const bool begins = (int64_t)w0 * share <= lo;
+            for (int w = w0 + lane; w <= w1; w += 64)
+                top = fmaxf(top, f.part_ml[((base + 2 * w + (w == w0 && begins ? 1 : 0)) * 16 + row) * 2]);
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-            for (int64_t w = w0; w <= w1; ++w) {
-                const int64_t slot = (int64_t)blockIdx.y * 2 * f.wgs + 2 * w + (w * share > lo ? 0 : 1);
-                const float2 u = *reinterpret_cast<const float2*>(f.part_ml + (slot * 16 + row) * 2);
-                const float turn = u.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u.x - top);
-                l += u.y * turn;
+            for (int v0 = w0; v0 <= w1; v0 += 64) {
+                const int w = v0 + lane;
+                float turn = 0.f;
+                if (w <= w1) {
+                    const float2 u = *reinterpret_cast<const float2*>(f.part_ml + ((base + 2 * w + (w == w0 && begins ? 1 : 0)) * 16 + row) * 2);
+                    turn = u.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u.x - top);
+                    l += u.y * turn;
+                }
+                weight[wave][lane] = turn;
+                const int many = w1 - v0 + 1 < 64 ? w1 - v0 + 1 : 64;
+#pragma unroll 8
+                for (int i = 0; i < many; ++i) {
+                    const int64_t slot = base + 2 * (v0 + i) + (v0 + i == w0 && begins ? 1 : 0);
+                    const float t = weight[wave][i];
 #pragma unroll
-                for (int k = 0; k < (D + 63) / 64; ++k)
-                    if (64 * k + lane < D) acc[k] += f.part[(slot * 16 + row) * D + 64 * k + lane] * turn;
+                    for (int k = 0; k < kLanes; ++k)
+                        if (D % 64 == 0 || 64 * k + lane < D) acc[k] += f.part[(slot * 16 + row) * D + 64 * k + lane] * t;
+                }
             }
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
             const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-            for (int k = 0; k < (D + 63) / 64; ++k) acc[k] *= inv;
+            for (int k = 0; k < kLanes; ++k) acc[k] *= inv;
             if (a.lse && lane == 0) a.lse[qrow * a.q.heads + qhead] = l > 0.f ? (top + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
         } else if constexpr (F == IVFTQ_KV_CODE4) {
 #pragma unroll
-            for (int k = 0; k < (D + 63) / 64; ++k)
-                if (64 * k + lane < D) acc[k] = f.whole[(qrow * a.q.heads + qhead) * D + 64 * k + lane];
+            for (int k = 0; k < kLanes; ++k)
+                if (D % 64 == 0 || 64 * k + lane < D) acc[k] = f.whole[(qrow * a.q.heads + qhead) * D + 64 * k + lane];
         }
         if constexpr (F == IVFTQ_KV_CODE4) {
 #pragma unroll
-            for (int k = 0; k < (D + 63) / 64; ++k)
-                if (64 * k + lane < D) row_sum[row][64 * k + lane] = acc[k];
+            for (int k = 0; k < kLanes; ++k)
+                if (D % 64 == 0 || 64 * k + lane < D) row_sum[row][64 * k + lane] = acc[k];
         } else {
             uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride;
 #pragma unroll
-            for (int k = 0; k < (D + 63) / 64; ++k)
-                if (64 * k + lane < D) p[64 * k + lane] = kv_from_float<F == IVFTQ_KV_BF16>(acc[k]);
+            for (int k = 0; k < kLanes; ++k)
+                if (D % 64 == 0 || 64 * k + lane < D) p[64 * k + lane] = kv_from_float<F == IVFTQ_KV_BF16>(acc[k]);
         }
     }
     if constexpr (F == IVFTQ_KV_CODE4) {
         __syncthreads();
-        if (wave) return;
-        const int n = lane & 15, g = lane >> 4;
-        const bool in = col0 + n < cols;
-        float x[D / 32][8], y[D / 32][8], n2 = 0.f;
+        const int n = lane & 15, g = lane >> 4, col = col0 + n;
+        const bool in = col < cols;
+        float x[D / 32][8];
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f; n2 += x[k][e] * x[k][e]; }
-        const float norm = sqrtf(kv_sum4(n2)), scale = norm > 0.f ? 1.f / norm : 0.f;
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[k][e] *= scale;
-        kv_rotate16<D, true>(a.c.rotation, x, y);
-        if (!in) return;
-        const int col = col0 + n;
-        const int64_t qrow = s.first + col / a.group;
-        const int qhead = h * a.group + col % a.group;
-        uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride + g * (D / 4);
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            uintx4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                w[e] = a.out.type == IVFTQ_KV_BF16 ? kv_pack2<true>(y[k][2 * e] * norm, y[k][2 * e + 1] * norm) : kv_pack2<false>(y[k][2 * e] * norm, y[k][2 * e + 1] * norm);
-            *reinterpret_cast<uintx4*>(p + 8 * k) = w;
+            for (int e = 0; e < 8; ++e) x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f;
+        const float norm = kv_unit_row<D>(x) * a.c.level_unit;
+#pragma unroll 1
+        for (int t = wave; t < D / 32; t += 4) {
+            float y[1][8];
+            kv_rotate16<D, true>(a.c.rotation, t, x, y);
+            if (!in) continue;
+            const int64_t qrow = s.first + col / a.group;
+            kv_store_turned(a.out, qrow, h * a.group + col % a.group, t, y[0], norm);
         }
     }
 }

@@ -17,7 +17,7 @@ typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// One layer's cache.  magnitudes: the eight positive levels as float16, low bytes in tab_lo, high bytes in tab_hi.
+// One layer's cache.  Magnitudes: the eight positive levels, scaled, as float16; low bytes in tab_lo, high bytes in tab_hi.
 struct KvView {
     char* pool;
     const int32_t* table;
@@ -28,6 +28,7 @@ struct KvView {
     int32_t batch, columns, page, page_log2, heads, rows;
     uint32_t tab_lo[2], tab_hi[2];
     float level[8], bound[7];    // positive levels and the boundaries between them
+    float level_unit;            // level[m] = level_unit * magnitude m, but for the magnitudes' rounding
 };
 
 struct KvRows {
@@ -61,6 +62,13 @@ inline int64_t kv_head_bytes(int format, int page, int d) {
 
 #ifdef __HIPCC__
 
+// A value that all lanes hold, as a scalar.
+__device__ __forceinline__ int kv_uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t kv_uniform(int64_t v) {
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) | (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
+}
+__device__ __forceinline__ int kv_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 // ---- sequences and pages -------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int kv_length(const KvView& c, int b) {
@@ -76,17 +84,6 @@ __device__ __forceinline__ void kv_new_rows(const KvView& c, int b, int& first, 
     first = s < 0 ? 0 : (s < c.rows ? s : c.rows);
     const int end = e < first ? first : (e < c.rows ? e : c.rows);
     count = end - first;
-}
-
-// The sequence that row r belongs to: the last b with starts[b] <= r (a search of bounded length whatever starts holds).
-__device__ __forceinline__ int kv_sequence_of(const KvView& c, int r) {
-    if (!c.starts) return r;
-    int lo = 0, hi = c.batch - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (c.starts[mid] <= r) lo = mid; else hi = mid - 1;
-    }
-    return lo;
 }
 
 // Number of the page that holds token t of sequence b, -1 where there is none.
@@ -129,15 +126,20 @@ __device__ __forceinline__ float kv_level(uint32_t nibble, const KvView& c) {
     return nibble & 8 ? -v : v;
 }
 
-// Sign and magnitude of the level next to v: bins [tau_i, tau_i+1), so a negative value on a boundary belongs to the
-// smaller magnitude.  No number: magnitude 0.
+// Sign and magnitude of the level next to v (no number: magnitude 0): three comparisons, each against the boundary that the
+// one before leaves.
 __device__ __forceinline__ uint32_t kv_nibble(float v, const KvView& c) {
     const float a = __builtin_fabsf(v);
-    const bool neg = v < 0.f;
-    uint32_t m = 0;
+    const bool b2 = a >= c.bound[3];
+    const bool b1 = a >= (b2 ? c.bound[5] : c.bound[1]);
+    const bool b0 = a >= (b2 ? (b1 ? c.bound[6] : c.bound[4]) : (b1 ? c.bound[2] : c.bound[0]));
+    return (b2 ? 4u : 0u) | (b1 ? 2u : 0u) | (b0 ? 1u : 0u) | (__builtin_bit_cast(uint32_t, v) >> 28 & 8u);
+}
+__device__ __forceinline__ uint32_t kv_nibbles8(const float (&y)[8], const KvView& c) {
+    uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 7; ++i) m += neg ? a > c.bound[i] : a >= c.bound[i];
-    return m | (neg ? 8u : 0u);
+    for (int e = 0; e < 8; ++e) w |= kv_nibble(y[e], c) << 4 * e;
+    return w;
 }
 
 // ---- 16-bit rows ---------------------------------------------------------------------------------------------------
@@ -171,13 +173,31 @@ __device__ __forceinline__ float kv_sum4(float v) { v += __shfl_xor(v, 16); retu
 
 // ---- products with the rotation ------------------------------------------------------------------------------------
 
-// y = Pi x (or Pi^T x) for 16 rows.  Lane l holds row l % 16, coordinates 32 s + 8 (l / 16) + e in x[s][e], and gets
-// coordinates (l / 16) * D / 4 + 8 s + e in y[s][e]: which coordinate a row of the matrix operand is can be chosen freely,
-// and this choice leaves every lane with neighbouring ones.  Rows should be of length about one (the caller scales them):
-// both sides go in as sums of two float16 numbers, three products, so y is good to about 2^-21 of the row's length, far
-// under the distance of two levels; one product alone would move one code in two thousand.
-template <int D, bool TRANSPOSED>
-__device__ __forceinline__ void kv_rotate16(const float* __restrict__ pi, const float (&x)[D / 32][8], float (&y)[D / 32][8]) {
+// A row in the operand layout, x[s][e] = coordinate 32 s + 8 (lane / 16) + e of row lane % 16, scaled to length one; returns
+// its norm.  What is zero (or shorter than float32 can say) stays zero.
+template <int D>
+__device__ __forceinline__ float kv_unit_row(float (&x)[D / 32][8]) {
+    float n2 = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) n2 += x[s][e] * x[s][e];
+    const float norm = sqrtf(kv_sum4(n2)), inv = norm > 0.f ? 1.f / norm : 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[s][e] *= inv;
+    return norm;
+}
+
+// 32 coordinates (block `first`, and N - 1 blocks after it) of y = Pi x, or of Pi^T x, for 16 unit rows.  A lane gets in
+// y[t][e] of its row, for Pi, coordinate 32 (first + t) + 8 (lane / 16) + e: which coordinate a row of the matrix operand
+// is can be chosen, and this choice leaves a lane with a whole word of codes; for Pi^T coordinate 32 (first + t) +
+// 16 (e / 4) + 4 (lane / 16) + e % 4, so that the sixteen lanes' reads down a column of Pi are neighbours.  Both sides go in
+// as sums of two float16 numbers, three products: y is good to about 2^-21 of the row's length, far under the distance of
+// two levels; one product alone would move one code in two thousand.
+template <int D, bool TRANSPOSED, int N>
+__device__ __forceinline__ void kv_rotate16(const float* __restrict__ pi, int first, const float (&x)[D / 32][8], float (&y)[N][8]) {
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     halfx8 bh[D / 32], bl[D / 32];
 #pragma unroll
@@ -189,10 +209,10 @@ __device__ __forceinline__ void kv_rotate16(const float* __restrict__ pi, const 
             bl[s][e] = (_Float16)(v - (float)bh[s][e]);
         }
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int i = (m >> 2) * (D / 4) + 8 * t + 4 * half + (m & 3);
+            const int i = 32 * (first + t) + (TRANSPOSED ? 16 * half + m : 8 * (m >> 2) + 4 * half + (m & 3));
             floatx4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < D / 32; ++s) {
@@ -219,6 +239,17 @@ __device__ __forceinline__ void kv_rotate16(const float* __restrict__ pi, const 
 #pragma unroll
             for (int r = 0; r < 4; ++r) y[t][4 * half + r] = acc[r] * (1.f / (kSplitScale * kSplitScale));
         }
+}
+
+// A lane's eight coordinates of block t of Pi^T x into a 16-bit row.
+__device__ __forceinline__ void kv_store_turned(const KvRows& out, int64_t row, int64_t head, int t, const float (&y)[8], float norm) {
+    uint16_t* p = reinterpret_cast<uint16_t*>(out.data) + row * out.row_stride + head * out.head_stride + 32 * t + 4 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const float a = y[4 * half] * norm, b = y[4 * half + 1] * norm, c = y[4 * half + 2] * norm, d = y[4 * half + 3] * norm;
+        *reinterpret_cast<uint2*>(p + 16 * half) = out.type == IVFTQ_KV_BF16 ? make_uint2(kv_pack2<true>(a, b), kv_pack2<true>(c, d))
+                                                                             : make_uint2(kv_pack2<false>(a, b), kv_pack2<false>(c, d));
+    }
 }
 
 #endif

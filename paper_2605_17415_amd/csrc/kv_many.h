@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void k_kv_many(ManyArgs f) {
     float gain = a.scale * kLog2e;
     if constexpr (F == IVFTQ_KV_CODE4) {
         const int64_t at = qrow * a.q.heads + qhead;
-        gain *= f.zn[at];
+        gain *= f.zn[at] * (c.level_unit / kSplitScale);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) q[k] = *reinterpret_cast<const uintx4*>(f.z + at * D + 16 * k + 8 * half);
     } else {
@@ -261,16 +261,16 @@ __global__ __launch_bounds__(256) void k_kv_many(ManyArgs f) {
     if (a.lse && half == 0) a.lse[qrow * a.q.heads + qhead] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
 }
 
-// Queries into the rotated frame: unit rows in float16 (one rounding of 2^-11 a coordinate, a score's error stays under
-// 2^-11 of |q| |k|; the levels it meets are float16 too) and their norms.  permuted: eights in the order of kv_levels8.
+// Queries into the rotated frame: unit rows in float16, a second part with what the first rounds away, and their norms.
+// permuted: eights in the order of kv_levels8.  One wavefront takes 16 rows and 32 coordinates (blockIdx.y).
 template <int D>
-__global__ __launch_bounds__(256) void k_kv_rotate_queries(KvRows q, const float* __restrict__ pi, uint16_t* __restrict__ z, float* __restrict__ zn, int permuted) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int64_t i = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 16 + n, all = (int64_t)q.rows * q.heads;
+__global__ __launch_bounds__(64) void k_kv_rotate_queries(KvRows q, const float* __restrict__ pi, uint16_t* __restrict__ z, float* __restrict__ zn, int permuted) {
+    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, block = blockIdx.y;
+    const int64_t i = (int64_t)blockIdx.x * 16 + n, all = (int64_t)q.rows * q.heads;
     const bool in = i < all;
     const int64_t row = in ? i / q.heads : 0, head = in ? i % q.heads : 0;
     const uint16_t* p = reinterpret_cast<const uint16_t*>(q.data) + row * q.row_stride + head * q.head_stride + 8 * g;
-    float x[D / 32][8], y[D / 32][8], n2 = 0.f;
+    float x[D / 32][8], y[1][8];
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
         const uintx4 w = *reinterpret_cast<const uintx4*>(p + 32 * s);
@@ -278,54 +278,39 @@ __global__ __launch_bounds__(256) void k_kv_rotate_queries(KvRows q, const float
         for (int e = 0; e < 8; ++e) {
             const uint32_t bits = w[e >> 1] >> 16 * (e & 1) & 0xffff;
             x[s][e] = q.type == IVFTQ_KV_BF16 ? kv_to_float<true>(bits) : kv_to_float<false>(bits);
-            n2 += x[s][e] * x[s][e];
         }
     }
-    const float norm = sqrtf(kv_sum4(n2)), inv = norm > 0.f ? 1.f / norm : 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] *= inv;
-    kv_rotate16<D, false>(pi, x, y);
+    const float norm = kv_unit_row<D>(x);
+    kv_rotate16<D, false>(pi, block, x, y);
     if (!in) return;
-    if (g == 0) zn[i] = norm;
+    if (g == 0 && block == 0) zn[i] = norm;
+    halfx8 hi, lo;
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-        halfx8 w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[permuted ? kv_slot(e) : e] = (_Float16)y[s][e];
-        *reinterpret_cast<halfx8*>(z + i * D + g * (D / 4) + 8 * s) = w;
+    for (int e = 0; e < 8; ++e) {
+        const int at = permuted ? kv_slot(e) : e;
+        const float v = y[0][e] * kSplitScale;
+        hi[at] = (_Float16)v;
+        lo[at] = (_Float16)(v - (float)hi[at]);
     }
+    *reinterpret_cast<halfx8*>(z + i * D + 32 * block + 8 * g) = hi;
+    *reinterpret_cast<halfx8*>(z + (all + i) * D + 32 * block + 8 * g) = lo;
 }
 
-// Results back into the rows' own frame.
+// Results back into the rows' own frame, split the same way.
 template <int D>
-__global__ __launch_bounds__(256) void k_kv_rotate_back(KvRows out, const float* __restrict__ pi, const float* __restrict__ whole) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int64_t i = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 16 + n, all = (int64_t)out.rows * out.heads;
+__global__ __launch_bounds__(64) void k_kv_rotate_back(KvRows out, const float* __restrict__ pi, const float* __restrict__ whole, float unit) {
+    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+    const int64_t i = (int64_t)blockIdx.x * 16 + n, all = (int64_t)out.rows * out.heads;
     const bool in = i < all;
     const float* p = whole + (in ? i : 0) * D + 8 * g;
-    float x[D / 32][8], y[D / 32][8], n2 = 0.f;
+    float x[D / 32][8], y[1][8];
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { x[s][e] = p[32 * s + e]; n2 += x[s][e] * x[s][e]; }
-    const float norm = sqrtf(kv_sum4(n2)), inv = norm > 0.f ? 1.f / norm : 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] *= inv;
-    kv_rotate16<D, true>(pi, x, y);
-    if (!in) return;
-    uint16_t* r = reinterpret_cast<uint16_t*>(out.data) + i / out.heads * out.row_stride + i % out.heads * out.head_stride + g * (D / 4);
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-        uintx4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = out.type == IVFTQ_KV_BF16 ? kv_pack2<true>(y[s][2 * e] * norm, y[s][2 * e + 1] * norm) : kv_pack2<false>(y[s][2 * e] * norm, y[s][2 * e + 1] * norm);
-        *reinterpret_cast<uintx4*>(r + 8 * s) = w;
-    }
+        for (int e = 0; e < 8; ++e) x[s][e] = p[32 * s + e];
+    const float norm = kv_unit_row<D>(x) * unit;
+    kv_rotate16<D, true>(pi, blockIdx.y, x, y);
+    if (in) kv_store_turned(out, i / out.heads, i % out.heads, blockIdx.y, y[0], norm);
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -341,8 +326,8 @@ template <int F, int D>
 hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) {
     uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
     float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole);
-    const unsigned rot = (unsigned)(((int64_t)a.q.rows * a.q.heads + 63) / 64);
-    if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, 256, 0, st>>>(a.q, a.c.rotation, z, zn, w.few);
+    const dim3 rot((unsigned)(((int64_t)a.q.rows * a.q.heads + 15) / 16), D / 32);
+    if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, 64, 0, st>>>(a.q, a.c.rotation, z, zn, w.few);
     const unsigned pairs = (unsigned)(a.c.batch * a.c.heads);
     if (w.few) {
         FewArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), reinterpret_cast<float*>(a.work + w.ml), w.wgs, w.split};
@@ -352,7 +337,7 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
         const int row_tiles = (int)(((int64_t)a.max_new * a.group + kManyRows - 1) / kManyRows);
         ManyArgs f{a, z, zn, whole, row_tiles};
         k_kv_many<F, D><<<pairs * (unsigned)row_tiles, 256, 0, st>>>(f);
-        if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D><<<rot, 256, 0, st>>>(a.out, a.c.rotation, whole);
+        if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D><<<rot, 64, 0, st>>>(a.out, a.c.rotation, whole, a.c.level_unit);
     }
     return hipGetLastError();
 }

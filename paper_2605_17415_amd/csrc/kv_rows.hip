@@ -4,32 +4,102 @@
 namespace ivftq {
 namespace {
 
-// Where row r's token lives: its page's record part of head h and its place in the page; null where there is none.
+// One row per sequence: where row r's token lives, its page's record part of head h and its place in the page; null where
+// there is none.
 __device__ __forceinline__ char* place_of(const KvView& c, int r, int h, int& t) {
-    const int b = kv_sequence_of(c, r);
-    int first, count;
-    kv_new_rows(c, b, first, count);
-    const int pos = kv_length(c, b) - count + (r - first);
-    if (r < first || r >= first + count || pos < 0) return nullptr;
-    const int64_t page = kv_page(c, b, pos);
+    const int pos = kv_length(c, r) - 1;
+    if (pos < 0) return nullptr;
+    const int64_t page = kv_page(c, r, pos);
     t = pos & (c.page - 1);
     return page < 0 ? nullptr : kv_record(c, page, h);
 }
 
-// ---- 16 bits: a thread moves eight coordinates of one row's key and value ------------------------------------------
+// ---- tiles of a sequence's new rows ---------------------------------------------------------------------------------
+// Where a sequence has several new rows the work is cut into tiles of 32 positions of a sequence, aligned, so that a group
+// of eight tokens (whose values share words) is written by one wavefront.  The tiles of all sequences stand one after the
+// other; a wavefront takes a consecutive share of (tile, head) items.
 
+struct NewTiles { int first_row, pos0, end, tile0, tiles; };      // pos0: position of the first new row (may be under zero)
+
+__device__ __forceinline__ NewTiles new_tiles(const KvView& c, int b) {
+    NewTiles t{0, 0, 0, 0, 0};
+    if (b >= c.batch) return t;
+    int count;
+    kv_new_rows(c, b, t.first_row, count);
+    t.end = kv_length(c, b);
+    t.pos0 = t.end - count;
+    const int lo = t.pos0 > 0 ? t.pos0 : 0;
+    t.tile0 = lo / 32;
+    t.tiles = count > 0 && t.end > lo ? (t.end + 31) / 32 - t.tile0 : 0;
+    return t;
+}
+
+struct NewItem { int64_t left; int b, tile, sub; NewTiles s; };   // items left; sub: number inside a tile
+
+// This wavefront's share of total * per_tile items.
+__device__ __forceinline__ NewItem first_item(const KvView& c, int per_tile) {
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0;
+    for (int b0 = 0; b0 < c.batch; b0 += 64) {
+        int v = new_tiles(c, b0 + lane).tiles;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+        total += v;
+    }
+    total = kv_uniform(total);
+    const int64_t waves = (int64_t)gridDim.x * (blockDim.x / 64), items = total * per_tile, share = (items + waves - 1) / waves;
+    const int64_t x = ((int64_t)blockIdx.x * (blockDim.x / 64) + kv_wave()) * share;
+    NewItem it{items - x < share ? items - x : share, 0, 0, 0, {}};
+    if (it.left <= 0) { it.left = 0; return it; }
+    const int64_t tile = x / per_tile;
+    it.sub = (int)(x % per_tile);
+    int64_t base = 0;
+    for (int b0 = 0; b0 < c.batch; b0 += 64) {
+        const int v = new_tiles(c, b0 + lane).tiles;
+        int64_t incl = v;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int64_t u = __shfl_up(incl, o); if (lane >= o) incl += u; }
+        const uint64_t past = __ballot(base + incl > tile);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            it.b = b0 + l;
+            it.tile = kv_uniform((int)(tile - base - __shfl(incl - v, l)));
+            break;
+        }
+        base += kv_uniform((int64_t)__shfl(incl, 63));
+    }
+    it.s = new_tiles(c, it.b);
+    return it;
+}
+__device__ __forceinline__ void next_item(const KvView& c, int per_tile, NewItem& it) {
+    if (--it.left <= 0) return;
+    if (++it.sub < per_tile) return;
+    it.sub = 0;
+    if (++it.tile < it.s.tiles) return;
+    it.tile = 0;
+    do { it.s = new_tiles(c, ++it.b); } while (!it.s.tiles && it.b < c.batch);      // there is one: items are left
+}
+
+// Reading: new rows that stand before position zero (a sequence has more rows than tokens) have no place and give zeros.
+__device__ __forceinline__ void no_place(const KvView& c, const KvRows& k, const KvRows& v, int d) {
+    for (int b = blockIdx.x; b < c.batch; b += gridDim.x) {
+        int first, count;
+        kv_new_rows(c, b, first, count);
+        const int64_t lost = count - kv_length(c, b);
+        for (int64_t i = threadIdx.x; i < lost * c.heads * (d / 8); i += blockDim.x) {
+            const int j = (int)(i % (d / 8)) * 8, h = (int)(i / (d / 8) % c.heads);
+            const int64_t r = first + i / (d / 8) / c.heads;
+            *reinterpret_cast<uintx4*>(reinterpret_cast<uint16_t*>(k.data) + r * k.row_stride + h * k.head_stride + j) = uintx4{0, 0, 0, 0};
+            *reinterpret_cast<uintx4*>(reinterpret_cast<uint16_t*>(v.data) + r * v.row_stride + h * v.head_stride + j) = uintx4{0, 0, 0, 0};
+        }
+    }
+}
+
+// ---- 16 bits ---------------------------------------------------------------------------------------------------------
+
+// One row per sequence (or a tile's ragged ends): eight coordinates of one row's key and value.
 template <bool READ>
-__global__ __launch_bounds__(256) void k_kv_move16(KvView c, KvRows k, KvRows v, int d) {
-    const int chunks = d / 8;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row_head = i / chunks;
-    const int j = (int)(i % chunks) * 8;
-    const int r = (int)(row_head / c.heads), h = (int)(row_head % c.heads);
-    if (r >= c.rows) return;
-    int t = 0;
-    char* rec = place_of(c, r, h, t);
-    uint16_t* kr = reinterpret_cast<uint16_t*>(k.data) + r * k.row_stride + h * k.head_stride + j;
-    uint16_t* vr = reinterpret_cast<uint16_t*>(v.data) + r * v.row_stride + h * v.head_stride + j;
+__device__ __forceinline__ void move16(const KvView& c, char* rec, int t, int d, int j, uint16_t* kr, uint16_t* vr) {
     uint16_t* kp = reinterpret_cast<uint16_t*>(rec) + (int64_t)t * d + j;
     uint16_t* vp = reinterpret_cast<uint16_t*>(rec) + (int64_t)c.page * d + ((int64_t)(t >> 3) * d + j) * 8 + (t & 7);
     if constexpr (READ) {
@@ -49,9 +119,76 @@ __global__ __launch_bounds__(256) void k_kv_move16(KvView c, KvRows k, KvRows v,
     }
 }
 
+template <bool READ>
+__global__ __launch_bounds__(256) void k_kv_move16(KvView c, KvRows k, KvRows v, int d) {
+    const int chunks = d / 8, i = blockIdx.x * 256 + threadIdx.x;              // rows * heads * d / 8 is under 2^31 here
+    const int row_head = i / chunks, j = i % chunks * 8, r = row_head / c.heads, h = row_head % c.heads;
+    if (r >= c.rows) return;
+    int t = 0;
+    char* rec = place_of(c, r, h, t);
+    move16<READ>(c, rec, t, d, j, reinterpret_cast<uint16_t*>(k.data) + r * k.row_stride + h * k.head_stride + j,
+                 reinterpret_cast<uint16_t*>(v.data) + r * v.row_stride + h * v.head_stride + j);
+}
+
+// 8 x 8 16-bit numbers, rows in a[0..7], turned: three rounds of exchanges of halves, 24 byte permutations and moves.
+__device__ __forceinline__ void turn8x8(uintx4 (&a)[8]) {
+    uintx4 r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)              // row i of the result: value i of rows 2 e and 2 e + 1
+            r[i][e] = __builtin_amdgcn_perm(a[2 * e + 1][i / 2], a[2 * e][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = r[i];
+}
+
+// Several rows a sequence: a lane moves eight tokens' eight coordinates, values turned in registers, so that both sides of
+// the copy are whole 16-byte pieces.
+template <bool READ>
+__global__ __launch_bounds__(256) void k_kv_tiles16(KvView c, KvRows k, KvRows v, int d) {
+    const int lane = threadIdx.x & 63, chunks = d / 8;
+    if constexpr (READ) no_place(c, k, v, d);
+    NewItem it = first_item(c, c.heads);
+    for (; it.left > 0; next_item(c, c.heads, it)) {
+        const int h = it.sub, t0 = (it.s.tile0 + it.tile) * 32;
+        for (int u = lane; u < 4 * chunks; u += 64) {
+            const int og = u / chunks, j = u % chunks * 8, t = t0 + 8 * og;
+            const int64_t page = kv_page(c, it.b, t);
+            char* rec = page < 0 ? nullptr : kv_record(c, page, h);
+            const int in = t & (c.page - 1), row = it.s.first_row + t - it.s.pos0;
+            uint16_t* kr = reinterpret_cast<uint16_t*>(k.data) + row * k.row_stride + h * k.head_stride + j;
+            uint16_t* vr = reinterpret_cast<uint16_t*>(v.data) + row * v.row_stride + h * v.head_stride + j;
+            if (rec && t >= it.s.pos0 && t + 8 <= it.s.end) {
+                uintx4* kp = reinterpret_cast<uintx4*>(reinterpret_cast<uint16_t*>(rec) + (int64_t)in * d + j);
+                uintx4* vp = reinterpret_cast<uintx4*>(reinterpret_cast<uint16_t*>(rec) + (int64_t)c.page * d + ((int64_t)(in >> 3) * d + j) * 8);
+                uintx4 x[8], y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = READ ? kp[e * chunks] : *reinterpret_cast<const uintx4*>(kr + e * k.row_stride);
+                    y[e] = READ ? vp[e] : *reinterpret_cast<const uintx4*>(vr + e * v.row_stride);
+                }
+                turn8x8(y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (READ) {
+                        *reinterpret_cast<uintx4*>(kr + e * k.row_stride) = x[e];
+                        *reinterpret_cast<uintx4*>(vr + e * v.row_stride) = y[e];
+                    } else {
+                        kp[e * chunks] = x[e];
+                        vp[e] = y[e];
+                    }
+                }
+            } else {
+                for (int e = 0; e < 8; ++e)
+                    if (t + e >= it.s.pos0 && t + e < it.s.end) move16<READ>(c, rec, in + e, d, j, kr + e * k.row_stride, vr + e * v.row_stride);
+            }
+        }
+    }
+}
+
 // ---- codes ---------------------------------------------------------------------------------------------------------
 
-// Loads the 16-bit row in the layout of kv_rotate16.
+// A 16-bit row in the operand layout: x[s][e] = coordinate 32 s + 8 (lane / 16) + e.
 template <int D, bool BF>
 __device__ __forceinline__ void load_row(const KvRows& x, int64_t row, int64_t head, bool valid, float (&v)[D / 32][8]) {
     const int g = (threadIdx.x & 63) >> 4;
@@ -65,66 +202,53 @@ __device__ __forceinline__ void load_row(const KvRows& x, int64_t row, int64_t h
     }
 }
 
-// A wavefront takes 16 (row, head) pairs of keys or of values (blockIdx.y): norm, rotation, levels.  A key's codes are
-// whole words of its lane.  A value's code is one half byte in each of d words that it shares with the seven other tokens
-// of its group: those words are changed with atomic operations on the own half byte alone, whose order does not matter.
+// One row per sequence: a wavefront takes 16 (row, head) pairs of keys or of values and 32 of the d codes (blockIdx.y), so
+// that even a single row's rotation is spread over several wavefronts: such calls are bound by the latency of their chain
+// of loads.  A key's codes are whole words; a value's code is one half byte in each of d words, which nothing else writes
+// in this call.
 template <int D, bool BF>
-__global__ __launch_bounds__(256) void k_kv_append_codes(KvView c, KvRows k, KvRows v) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const bool value = blockIdx.y;
-    const int64_t i = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 16 + n;
+__global__ __launch_bounds__(64) void k_kv_append_row_codes(KvView c, KvRows k, KvRows v) {
+    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+    const bool value = blockIdx.y >= D / 32;
+    const int block = blockIdx.y % (D / 32);
+    const int64_t i = (int64_t)blockIdx.x * 16 + n;
     const bool in = i < (int64_t)c.rows * c.heads;
     const int r = in ? (int)(i / c.heads) : 0, h = in ? (int)(i % c.heads) : 0;
-    float x[D / 32][8], y[D / 32][8];
+    float x[D / 32][8], y[1][8];
     load_row<D, BF>(value ? v : k, r, h, in, x);
-    float n2 = 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) n2 += x[s][e] * x[s][e];
-    const float norm = sqrtf(kv_sum4(n2)), inv = norm > 0.f ? 1.f / norm : 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] *= inv;
-    kv_rotate16<D, false>(c.rotation, x, y);
+    const float norm = kv_unit_row<D>(x);
+    kv_rotate16<D, false>(c.rotation, block, x, y);
     int t = 0;
     char* rec = in ? place_of(c, r, h, t) : nullptr;
     if (!rec) return;
-    const int codes = c.page * (D / 2);
-    if (g == 0) reinterpret_cast<_Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t] = (_Float16)norm;
+    const int codes = c.page * (D / 2), j = 32 * block + 8 * g;
+    if (g == 0 && block == 0) reinterpret_cast<_Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t] = (_Float16)norm;
+    const uint32_t w = kv_nibbles8(y[0], c);
+    if (!value) {
+        reinterpret_cast<uint32_t*>(rec + (int64_t)t * (D / 2))[j / 8] = w;
+    } else {
+        uint8_t* p = reinterpret_cast<uint8_t*>(rec + codes) + ((int64_t)(t >> 3) * D + j) * 4 + (t & 7) / 2;
+        uint32_t was[8];
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-        uint32_t w = 0, nib[8];
+        for (int e = 0; e < 8; ++e) was[e] = p[4 * e];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { nib[e] = kv_nibble(y[s][e], c); w |= nib[e] << 4 * e; }
-        const int j = g * (D / 4) + 8 * s;
-        if (!value) {
-            reinterpret_cast<uint32_t*>(rec + (int64_t)t * (D / 2))[j / 8] = w;
-        } else {
-            uint32_t* p = reinterpret_cast<uint32_t*>(rec + codes) + (int64_t)(t >> 3) * D + j;
-            const int shift = 4 * (t & 7);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                atomicAnd(p + e, ~(15u << shift));
-                atomicOr(p + e, nib[e] << shift);
-            }
-        }
+        for (int e = 0; e < 8; ++e) p[4 * e] = (uint8_t)(t & 1 ? (was[e] & 15) | (w >> 4 * e & 15) << 4 : (was[e] & 240) | (w >> 4 * e & 15));
     }
 }
 
-// The rows that the codes stand for: levels, rotated back, times the norm.
+// The rows that the codes stand for: levels, rotated back, times the norm.  Split the same way.
 template <int D, bool BF>
-__global__ __launch_bounds__(256) void k_kv_read_codes(KvView c, KvRows k, KvRows v) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const bool value = blockIdx.y;
-    const int64_t i = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 16 + n;
+__global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, KvRows v) {
+    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+    const bool value = blockIdx.y >= D / 32;
+    const int block = blockIdx.y % (D / 32);
+    const int64_t i = (int64_t)blockIdx.x * 16 + n;
     const bool in = i < (int64_t)c.rows * c.heads;
     const int r = in ? (int)(i / c.heads) : 0, h = in ? (int)(i % c.heads) : 0;
     int t = 0;
     const char* rec = in ? place_of(c, r, h, t) : nullptr;
     const int codes = c.page * (D / 2);
-    float x[D / 32][8], y[D / 32][8], norm = 0.f;
+    float x[D / 32][8], y[1][8], norm = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
         const int j = 32 * s + 8 * g;
@@ -139,30 +263,203 @@ __global__ __launch_bounds__(256) void k_kv_read_codes(KvView c, KvRows k, KvRow
         for (int e = 0; e < 8; ++e) x[s][e] = kv_level(w >> 4 * e & 15, c);
     }
     if (rec) norm = (float)reinterpret_cast<const _Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t];
-    kv_rotate16<D, true>(c.rotation, x, y);
+    kv_rotate16<D, true>(c.rotation, block, x, y);
     if (!in) return;
     const KvRows& o = value ? v : k;
-    uint16_t* out = reinterpret_cast<uint16_t*>(o.data) + r * o.row_stride + h * o.head_stride + g * (D / 4);
+    uint16_t* out = reinterpret_cast<uint16_t*>(o.data) + r * o.row_stride + h * o.head_stride + 32 * block + 4 * g;
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-        uintx4 w = {0, 0, 0, 0};
-        if (rec)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = kv_pack2<BF>(y[s][2 * e] * norm, y[s][2 * e + 1] * norm);
-        *reinterpret_cast<uintx4*>(out + 8 * s) = w;
+    for (int half = 0; half < 2; ++half) {
+        uint2 w = make_uint2(0, 0);
+        if (rec) w = make_uint2(kv_pack2<BF>(y[0][4 * half] * norm, y[0][4 * half + 1] * norm), kv_pack2<BF>(y[0][4 * half + 2] * norm, y[0][4 * half + 3] * norm));
+        *reinterpret_cast<uint2*>(out + 16 * half) = w;
     }
 }
 
-template <int D>
-hipError_t codes(const KvView& c, const KvRows& k, const KvRows& v, bool read, hipStream_t st) {
-    const int64_t tiles = ((int64_t)c.rows * c.heads + 63) / 64;
-    const dim3 grid((unsigned)tiles, 2);
-    const bool bf = k.type == IVFTQ_KV_BF16;
-    if (read) {
-        if (bf) k_kv_read_codes<D, true><<<grid, 256, 0, st>>>(c, k, v); else k_kv_read_codes<D, false><<<grid, 256, 0, st>>>(c, k, v);
-    } else {
-        if (bf) k_kv_append_codes<D, true><<<grid, 256, 0, st>>>(c, k, v); else k_kv_append_codes<D, false><<<grid, 256, 0, st>>>(c, k, v);
+// 8 x 8 half bytes over eight neighbouring lanes, turned: lane i's half byte e becomes lane e's half byte i.
+__device__ __forceinline__ uint32_t turn_nibbles(uint32_t w, int lane) {
+    uint32_t p = __shfl_xor(w, 4);
+    w = lane & 4 ? (w & 0xffff0000u) | p >> 16 : (w & 0xffffu) | p << 16;
+    p = __shfl_xor(w, 2);
+    w = lane & 2 ? (w & 0xff00ff00u) | (p >> 8 & 0x00ff00ffu) : (w & 0x00ff00ffu) | (p << 8 & 0xff00ff00u);
+    p = __shfl_xor(w, 1);
+    return lane & 1 ? (w & 0xf0f0f0f0u) | (p >> 4 & 0x0f0f0f0fu) : (w & 0x0f0f0f0fu) | (p << 4 & 0xf0f0f0f0u);
+}
+
+// Several rows a sequence.  The rotation stands in LDS as two float16 parts in operand order, so that reading it costs 64
+// KB of LDS traffic per 32 rows and none of L2 (at d = 256 and 192 a workgroup computes one half of the coordinates:
+// 128 and 72 KB).  A wavefront takes a tile of 32 tokens of one head's keys or values: two column tiles, three products.
+template <int D> constexpr int kOutputs = D > 128 ? D / 2 : D;             // coordinates that a workgroup computes
+template <int D> constexpr int kTurnBytes = kOutputs<D> * D * 4;
+
+template <int D, bool BF, bool READ>
+__global__ __launch_bounds__(256) void k_kv_tiles_codes(KvView c, KvRows k, KvRows v) {
+    constexpr int NS = D / 32, NT = kOutputs<D> / 32;
+    extern __shared__ __align__(16) char turn[];                           // [NT][2][NS][hi, lo][64 lanes] of 16 bytes
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int out0 = blockIdx.y * kOutputs<D>;
+    if (READ && out0 == 0) no_place(c, k, v, D);
+    for (int u = threadIdx.x; u < NT * 2 * NS * 64; u += 256) {
+        const int l = u & 63, s = u / 64 % NS, half = u / 64 / NS & 1, t = u / 64 / NS / 2, m = l & 15;
+        // a lane's results: coordinates out0 + g * outputs / 4 + 8 t + 4 half + (0 .. 3)
+        const int i = out0 + (m >> 2) * (kOutputs<D> / 4) + 8 * t + 4 * half + (m & 3), k0 = 32 * s + 8 * (l >> 4);
+        halfx8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p = (READ ? c.rotation[(k0 + e) * D + i] : c.rotation[i * D + k0 + e]) * kSplitScale;
+            hi[e] = (_Float16)p;
+            lo[e] = (_Float16)(p - (float)hi[e]);
+        }
+        halfx8* to = reinterpret_cast<halfx8*>(turn) + (u / 64) * 128 + l;
+        to[0] = hi;
+        to[64] = lo;
     }
+    __syncthreads();
+    const int codes = c.page * (D / 2), per_tile = 2 * c.heads;
+    NewItem it = first_item(c, per_tile);
+    for (; it.left > 0; next_item(c, per_tile, it)) {
+        const bool value = it.sub >= c.heads;
+        const int h = value ? it.sub - c.heads : it.sub, t0 = (it.s.tile0 + it.tile) * 32;
+        const KvRows& rows = value ? v : k;
+        halfx8 xh[2][NS], xl[2][NS];
+        float norm[2];
+        char* rec[2];
+        int at[2];
+        bool mine[2];
+#pragma unroll
+        for (int ct = 0; ct < 2; ++ct) {
+            const int t = t0 + 16 * ct + n;
+            const int64_t page = kv_page(c, it.b, t);
+            mine[ct] = t >= it.s.pos0 && t < it.s.end;
+            rec[ct] = page < 0 ? nullptr : kv_record(c, page, h);
+            at[ct] = t & (c.page - 1);
+            float x[NS][8];
+            if constexpr (READ) {
+                norm[ct] = rec[ct] && mine[ct] ? (float)reinterpret_cast<const _Float16*>(rec[ct] + 2 * codes)[(value ? c.page : 0) + at[ct]] : 0.f;
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    uint32_t w = 0;
+                    if (rec[ct]) {
+                        if (value) w = reinterpret_cast<const uint32_t*>(rec[ct] + codes)[(int64_t)(at[ct] >> 3) * D + 32 * s + 8 * g + (n & 7)];
+                        else w = reinterpret_cast<const uint32_t*>(rec[ct] + (int64_t)at[ct] * (D / 2))[4 * s + g];
+                    }
+                    if (value) w = turn_nibbles(w, lane);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[s][e] = kv_level(w >> 4 * e & 15, c);
+                }
+            } else {
+                load_row<D, BF>(rows, it.s.first_row + t - it.s.pos0, h, mine[ct], x);
+                norm[ct] = kv_unit_row<D>(x);
+            }
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float w = x[s][e] * kSplitScale;
+                    xh[ct][s][e] = (_Float16)w;
+                    xl[ct][s][e] = (_Float16)(w - (float)xh[ct][s][e]);
+                }
+        }
+#pragma unroll 1
+        for (int t = 0; t < NT; ++t) {
+            float y[2][8];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                floatx4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+                const halfx8* from = reinterpret_cast<const halfx8*>(turn) + (t * 2 + half) * NS * 128 + lane;
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const halfx8 ah = from[s * 128], al = from[s * 128 + 64];
+#pragma unroll
+                    for (int ct = 0; ct < 2; ++ct) {
+                        acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, xh[ct][s], acc[ct], 0, 0, 0);
+                        acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, xl[ct][s], acc[ct], 0, 0, 0);
+                        acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, xh[ct][s], acc[ct], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int ct = 0; ct < 2; ++ct)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[ct][4 * half + r] = acc[ct][r] * (1.f / (kSplitScale * kSplitScale));
+            }
+            const int j = out0 + g * (kOutputs<D> / 4) + 8 * t;
+#pragma unroll
+            for (int ct = 0; ct < 2; ++ct) {
+                if constexpr (READ) {
+                    if (!mine[ct]) continue;
+                    uintx4 w = {0, 0, 0, 0};
+                    if (rec[ct])
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = kv_pack2<BF>(y[ct][2 * e] * norm[ct], y[ct][2 * e + 1] * norm[ct]);
+                    *reinterpret_cast<uintx4*>(reinterpret_cast<uint16_t*>(rows.data) + (int64_t)(it.s.first_row + t0 + 16 * ct + n - it.s.pos0) * rows.row_stride +
+                                               h * rows.head_stride + j) = w;
+                } else {
+                    uint32_t w = kv_nibbles8(y[ct], c);
+                    if (!value) {
+                        if (mine[ct] && rec[ct]) reinterpret_cast<uint32_t*>(rec[ct] + (int64_t)at[ct] * (D / 2))[j / 8] = w;
+                    } else {
+                        w = turn_nibbles(w, lane);           // this lane: coordinate j + n % 8, tokens of its group of eight
+                        const uint32_t given = (uint32_t)(__ballot(mine[ct]) >> (lane & 56)) & 0xff;
+                        uint32_t keep = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) keep |= given >> e & 1 ? 0 : 15u << 4 * e;
+                        if (given && rec[ct]) {
+                            uint32_t* p = reinterpret_cast<uint32_t*>(rec[ct] + codes) + (int64_t)(at[ct] >> 3) * D + j + (n & 7);
+                            *p = keep ? (*p & keep) | (w & ~keep) : w;
+                        }
+                    }
+                }
+            }
+        }
+        if constexpr (!READ) {
+#pragma unroll
+            for (int ct = 0; ct < 2; ++ct)
+                if (g == 0 && out0 == 0 && mine[ct] && rec[ct]) reinterpret_cast<_Float16*>(rec[ct] + 2 * codes)[(value ? c.page : 0) + at[ct]] = (_Float16)norm[ct];
+        }
+    }
+}
+
+// Workgroups for the tiles: as many as the chip holds at once, or fewer where there cannot be that many items.
+hipError_t tile_grid(ChipFill& fill, const void* kernel, size_t lds, const KvView& c, int per_tile, int slices, unsigned* wgs) {
+    if (hipError_t e = fill.get(kernel, 256, lds, wgs)) return e;
+    const int64_t most = (((int64_t)c.rows / 32 + 2 * (int64_t)c.batch) * per_tile + 3) / 4;
+    *wgs = *wgs / slices ? *wgs / slices : 1;
+    if (most < *wgs) *wgs = (unsigned)most;
+    return hipSuccess;
+}
+
+template <int D, bool BF, bool READ>
+hipError_t tiles_codes(const KvView& c, const KvRows& k, const KvRows& v, hipStream_t st) {
+    static ChipFill fill;
+    constexpr int slices = D / kOutputs<D>;
+    const void* kernel = reinterpret_cast<const void*>(&k_kv_tiles_codes<D, BF, READ>);
+    unsigned wgs;
+    if (hipError_t e = tile_grid(fill, kernel, kTurnBytes<D>, c, 2 * c.heads, slices, &wgs)) return e;
+    k_kv_tiles_codes<D, BF, READ><<<dim3(wgs, slices), 256, kTurnBytes<D>, st>>>(c, k, v);
+    return hipGetLastError();
+}
+
+template <int D, bool BF>
+hipError_t codes(const KvView& c, const KvRows& k, const KvRows& v, bool read, hipStream_t st) {
+    if (c.starts) {
+        if (read) return tiles_codes<D, BF, true>(c, k, v, st);
+        return tiles_codes<D, BF, false>(c, k, v, st);
+    }
+    const dim3 grid((unsigned)(((int64_t)c.rows * c.heads + 15) / 16), 2 * (D / 32));
+    if (read) k_kv_read_row_codes<D, BF><<<grid, 64, 0, st>>>(c, k, v); else k_kv_append_row_codes<D, BF><<<grid, 64, 0, st>>>(c, k, v);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t codes_d(const KvView& c, const KvRows& k, const KvRows& v, bool read, hipStream_t st) {
+    return k.type == IVFTQ_KV_BF16 ? codes<D, true>(c, k, v, read, st) : codes<D, false>(c, k, v, read, st);
+}
+
+template <bool READ>
+hipError_t tiles16(const KvView& c, const KvRows& k, const KvRows& v, int d, hipStream_t st) {
+    static ChipFill fill;
+    unsigned wgs;
+    if (hipError_t e = tile_grid(fill, reinterpret_cast<const void*>(&k_kv_tiles16<READ>), 0, c, c.heads, 1, &wgs)) return e;
+    k_kv_tiles16<READ><<<wgs, 256, 0, st>>>(c, k, v, d);
     return hipGetLastError();
 }
 
@@ -170,15 +467,15 @@ hipError_t move(const KvView& c, const KvRows& k, const KvRows& v, int d, int fo
     if (!c.rows) return hipSuccess;
     if (format == IVFTQ_KV_CODE4) {
         switch (d) {
-            case 64: return codes<64>(c, k, v, read, st);
-            case 96: return codes<96>(c, k, v, read, st);
-            case 128: return codes<128>(c, k, v, read, st);
-            case 192: return codes<192>(c, k, v, read, st);
-            default: return codes<256>(c, k, v, read, st);
+            case 64: return codes_d<64>(c, k, v, read, st);
+            case 96: return codes_d<96>(c, k, v, read, st);
+            case 128: return codes_d<128>(c, k, v, read, st);
+            case 192: return codes_d<192>(c, k, v, read, st);
+            default: return codes_d<256>(c, k, v, read, st);
         }
     }
-    const int64_t threads = (int64_t)c.rows * c.heads * (d / 8);
-    const unsigned grid = (unsigned)((threads + 255) / 256);
+    if (c.starts) return read ? tiles16<true>(c, k, v, d, st) : tiles16<false>(c, k, v, d, st);
+    const unsigned grid = (unsigned)(((int64_t)c.rows * c.heads * (d / 8) + 255) / 256);
     if (read) k_kv_move16<true><<<grid, 256, 0, st>>>(c, k, v, d); else k_kv_move16<false><<<grid, 256, 0, st>>>(c, k, v, d);
     return hipGetLastError();
 }
