@@ -126,40 +126,60 @@ __device__ __forceinline__ FewPlace few_place(const KvView& c, const FewSeq& s, 
     return p;
 }
 
+// Byte offsets of a lane's reads inside a tile of one page.
 template <int F, int D>
-__device__ __forceinline__ void few_load(const KvView& c, int h, const FewPlace& p, FewTile<F, D>& x) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const char* r0 = kv_record(c, p.p0 < 0 ? 0 : p.p0, h);
-    const char* r1 = kv_record(c, p.p1 < 0 ? 0 : p.p1, h);
-    const int i0 = p.t0 & (c.page - 1), i1 = (p.t0 + 16) & (c.page - 1);
-    // lane's token of the two key operands: t0 + 8 (n / 4) + (16 bits: 4 y + n % 4; codes: 2 (n % 4) + y)
-    const char* kr = n >> 3 ? r1 : r0;
-    const int ki = (n >> 3 ? i1 : i0) + 8 * (n >> 2 & 1) + (F == IVFTQ_KV_CODE4 ? 2 * (n & 3) : n & 3);
-    const char* vr = g >> 1 ? r1 : r0;
-    const int vi = ((g >> 1 ? i1 : i0) >> 3) + (g & 1);               // group of eight tokens in the page
-    if constexpr (F == IVFTQ_KV_CODE4) {
-        const int codes = c.page * (D / 2);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const uint32_t* q = reinterpret_cast<const uint32_t*>(kr + (ki + y) * (D / 2)) + g * (D / 32);
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) x.kw[y][k] = q[k];
+struct FewLane {
+    uint32_t key, value, norm;
+    __device__ __forceinline__ explicit FewLane(const KvView& c) {
+        const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+        // lane's token of the two key operands: 8 (n / 4) + (16 bits: 4 y + n % 4; codes: 2 (n % 4) + y)
+        if constexpr (F == IVFTQ_KV_CODE4) {
+            key = (8 * (n >> 2) + 2 * (n & 3)) * (D / 2) + g * (D / 8);
+            value = c.page * (D / 2) + g * (D * 4) + n * (D / 4);
+            norm = c.page * D + g * 16;
+        } else {
+            key = (8 * (n >> 2) + (n & 3)) * (D * 2) + g * 16;
+            value = c.page * (D * 2) + (g * D + n) * 16;
+            norm = 0;
         }
-        x.kg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + vi * 16);
-        x.vg = *reinterpret_cast<const uintx4*>(vr + 2 * codes + 2 * c.page + vi * 16);
-        const uint32_t* q = reinterpret_cast<const uint32_t*>(vr + codes) + vi * D + n * (D / 16);
+    }
+};
+
+template <int F, int D>
+__device__ __forceinline__ void few_load(const KvView& c, int h, const FewPlace& p, const FewLane<F, D>& at, FewTile<F, D>& x) {
+    constexpr bool codes = F == IVFTQ_KV_CODE4;
+    constexpr int row = codes ? D / 2 : D * 2;                        // bytes of a token's row
+    const int in = p.t0 & (c.page - 1);
+    const char* base = kv_record(c, p.p0 < 0 ? 0 : p.p0, h);
+    auto read = [&](const char* keys, const char* values, const char* norms) {
+        // every address is a scalar base and a lane's offset (pages of 32 and more), or a lane's own pointer
+        if constexpr (codes) {
+            const uint32_t *q = reinterpret_cast<const uint32_t*>(keys), *v = reinterpret_cast<const uint32_t*>(values);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) x.vw[k] = q[k];
-    } else {
+            for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const uintx4* q = reinterpret_cast<const uintx4*>(kr + (ki + 4 * y) * (D * 2)) + g;
+                for (int k = 0; k < D / 32; ++k) x.kw[y][k] = q[y * (D / 8) + k];
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) x.kk[y][k] = q[4 * k];
+            for (int k = 0; k < D / 16; ++k) x.vw[k] = v[k];
+            x.kg = *reinterpret_cast<const uintx4*>(norms);
+            x.vg = *reinterpret_cast<const uintx4*>(norms + 2 * c.page);
+        } else {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) x.kk[y][k] = *reinterpret_cast<const uintx4*>(keys + y * 4 * row + k * 64);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) x.vv[k] = *reinterpret_cast<const uintx4*>(values + k * 256);
         }
-        const uintx4* q = reinterpret_cast<const uintx4*>(vr + c.page * (D * 2)) + vi * D + n;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) x.vv[k] = q[16 * k];
+    };
+    if (c.page >= kFewTile) {
+        const char* here = base + in * row;
+        read(here + at.key, here + at.value, base + 2 * in + at.norm);
+    } else {                                                          // pages of 16: the tile's halves lie in two pages
+        const char* other = kv_record(c, p.p1 < 0 ? 0 : p.p1, h);
+        const int lane = threadIdx.x & 63;
+        const bool k1 = lane & 8, v1 = lane & 32;                     // second half: n / 8, g / 2
+        read((k1 ? other - 16 * row : base) + at.key, (v1 ? other - 16 * row : base) + at.value, (v1 ? other - 32 : base) + at.norm);
     }
 }
 
@@ -177,7 +197,10 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int cols = s.count * a.group, col = col0 + n < cols ? col0 + n : 0, tok = a.max_new == 1 ? 0 : col / a.group;
     x.pos = col0 + n < cols ? s.base + tok : s.end - 1;
-    x.gain = a.scale * kLog2e;
+    // scores are multiplied by a factor above zero, so that their maximum is that of the products: a negative scale turns the
+    // queries' signs, and none at all is taken as next to none
+    x.gain = fabsf(a.scale) * kLog2e;
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
     const int64_t row = s.first + tok, head = h * a.group + col - tok * a.group;
     if constexpr (F == IVFTQ_KV_CODE4) {
         const int64_t at = row * a.q.heads + head, all = (int64_t)a.q.rows * a.q.heads;
@@ -186,12 +209,15 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
         for (int k = 0; k < D / 32; ++k) {
             x.q[k] = *reinterpret_cast<const uintx4*>(f.z + at * D + g * (D / 4) + 8 * k);
             x.low[k] = *reinterpret_cast<const uintx4*>(f.z + (all + at) * D + g * (D / 4) + 8 * k);
+            x.low[k] ^= sign;
+            x.q[k] ^= sign;
         }
     } else {
         const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) x.q[k] = *reinterpret_cast<const uintx4*>(p + 32 * k);
+        for (int k = 0; k < D / 32; ++k) { x.q[k] = *reinterpret_cast<const uintx4*>(p + 32 * k); x.q[k] ^= sign; }
     }
+    x.gain = fmaxf(x.gain, 1e-30f);
 }
 
 // A tile into the running maximum m, sum l (of this lane's tokens) and sums o (transposed: o[blk][r] = coordinate
@@ -214,14 +240,14 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int
             }
         const halfx8 kn = __builtin_bit_cast(halfx8, x.kg);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e] = st[e & 1][e >> 1] * ((float)kn[e] * q.gain);
+        for (int e = 0; e < 8; ++e) sc[e] = st[e & 1][e >> 1] * (float)kn[e];
     } else {
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) st[y] = kv_mfma16<F>(x.kk[y][k], q.q[k], st[y]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3] * q.gain;
+        for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3];
     }
     // every token of the tile visible to every row?
     const bool full = at.p0 >= 0 && at.p1 >= 0 && t0 + kFewTile - 1 <= s.base &&
@@ -242,8 +268,7 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int
     float top = sc[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = kv_max4(top) * q.gain;
     if (__ballot(top > m)) {
         const float now = fmaxf(m, top), turn = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
         m = now;
@@ -251,13 +276,10 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) o[k] *= turn;
     }
+    const float less = m == -INFINITY ? 0.f : m;           // a row that has seen nothing: every score is -infinity
     float pr[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(sc[e] - m);
-    if (!full) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) pr[e] = sc[e] == -INFINITY ? 0.f : pr[e];       // a row that has seen nothing has no maximum
-    }
+    for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], q.gain, -less));
 #pragma unroll
     for (int e = 0; e < 8; ++e) l += pr[e];
     if constexpr (F == IVFTQ_KV_CODE4) {
@@ -325,23 +347,32 @@ __device__ __forceinline__ void few_walk(const FewArgs& f, const FewSeq& s, int 
     if (from >= to) return;
     FewQuery<F, D> q;
     few_query<F, D>(f, s, h, col0, q);
+    const FewLane<F, D> lane(c);
     FewPlace at = few_place(c, s, b, from);
     if constexpr (F == IVFTQ_KV_CODE4) {
         FewTile<F, D> x, y;
-        few_load<F, D>(c, h, at, x);
+        few_load<F, D>(c, h, at, lane, x);
         FewPlace next = few_place(c, s, b, from + 4 < to ? from + 4 : from);
-        for (int i = from; i < to; i += 4) {
-            const FewPlace then = few_place(c, s, b, i + 8 < to ? i + 8 : i);
-            few_load<F, D>(c, h, next, y);                    // past the end: a tile that is there, read and not used
-            few_step<F, D>(f.a, s, h, q, at, x, m, l, o);
-            x = y;
+        int i = from;
+        // past the end: a tile that is there, read and not used
+        auto step = [&](FewTile<F, D>& now, FewTile<F, D>& then) {
+            const FewPlace after = few_place(c, s, b, i + 8 < to ? i + 8 : i);
+            few_load<F, D>(c, h, next, lane, then);
+            few_step<F, D>(f.a, s, h, q, at, now, m, l, o);
             at = next;
-            next = then;
+            next = after;
+            i += 4;
+        };
+        while (true) {
+            step(x, y);
+            if (i >= to) break;
+            step(y, x);
+            if (i >= to) break;
         }
     } else {
         for (int i = from; i < to; i += 4) {
             FewTile<F, D> x;
-            few_load<F, D>(c, h, at, x);
+            few_load<F, D>(c, h, at, lane, x);
             const FewPlace next = few_place(c, s, b, i + 4 < to ? i + 4 : i);
             few_step<F, D>(f.a, s, h, q, at, x, m, l, o);
             at = next;
@@ -353,7 +384,7 @@ template <int F>
 __device__ __forceinline__ int few_coord(int D, int k, int g, int r) { return F == IVFTQ_KV_CODE4 ? (4 * g + r) * (D / 16) + k : 16 * k + 4 * g + r; }
 
 template <int F, int D>
-__global__ __launch_bounds__(256) void k_kv_few(FewArgs f) {
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_few(FewArgs f) {
     constexpr int kPass = D > 128 ? D / 2 : D;                 // coordinates that pass through LDS at a time
     __shared__ float sum[4][16][kPass + 1];
     __shared__ float ml[4][16][2];

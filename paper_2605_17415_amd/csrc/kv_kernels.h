@@ -69,18 +69,23 @@ __device__ __forceinline__ int64_t kv_uniform(int64_t v) {
 }
 __device__ __forceinline__ int kv_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
+// Tables and lengths are read-only while a kernel runs: read through the constant address space, a uniform index gives a
+// scalar load.
+typedef const __attribute__((address_space(4))) int32_t* KvInts;
+__device__ __forceinline__ int32_t kv_int(const int32_t* p, int64_t i) { return ((KvInts)(uintptr_t)p)[i]; }
+
 // ---- sequences and pages -------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int kv_length(const KvView& c, int b) {
     const int64_t cap = (int64_t)c.columns << c.page_log2;
-    const int n = c.lengths[b];
+    const int n = kv_int(c.lengths, b);
     return n < 0 ? 0 : (int)(n < cap ? n : (cap < 0x7fffff00 ? cap : 0x7fffff00));
 }
 
 // First row and number of rows of sequence b; what `starts` says is held inside the rows that there are.
 __device__ __forceinline__ void kv_new_rows(const KvView& c, int b, int& first, int& count) {
     if (!c.starts) { first = b; count = b < c.rows ? 1 : 0; return; }
-    const int s = c.starts[b], e = c.starts[b + 1];
+    const int s = kv_int(c.starts, b), e = kv_int(c.starts, b + 1);
     first = s < 0 ? 0 : (s < c.rows ? s : c.rows);
     const int end = e < first ? first : (e < c.rows ? e : c.rows);
     count = end - first;
@@ -90,7 +95,7 @@ __device__ __forceinline__ void kv_new_rows(const KvView& c, int b, int& first, 
 __device__ __forceinline__ int64_t kv_page(const KvView& c, int b, int t) {
     const int col = t >> c.page_log2;
     if ((unsigned)col >= (unsigned)c.columns) return -1;
-    const int32_t id = c.table[(int64_t)b * c.table_stride + col];
+    const int32_t id = kv_int(c.table, (int64_t)b * c.table_stride + col);
     return id >= 0 && id < c.pages ? id : -1;
 }
 
@@ -156,7 +161,11 @@ __device__ __forceinline__ uint16_t kv_from_float(float v) {
 }
 template <bool BF>
 __device__ __forceinline__ uint32_t kv_pack2(float a, float b) {
-    return (uint32_t)kv_from_float<BF>(a) | (uint32_t)kv_from_float<BF>(b) << 16;
+    typedef float two __attribute__((ext_vector_type(2)));
+    typedef _Float16 two_f16 __attribute__((ext_vector_type(2)));
+    typedef __bf16 two_bf16 __attribute__((ext_vector_type(2)));
+    if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector((two{a, b}), two_bf16));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector((two{a, b}), two_f16));
 }
 
 // Which of the eight 16-bit values of w are no finite numbers, a bit each.
@@ -169,7 +178,25 @@ __device__ __forceinline__ uint32_t kv_not_finite(uintx4 w) {
     return bad;
 }
 
-__device__ __forceinline__ float kv_sum4(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+// A value of the lane 16, or 32, lanes away (of the other half of a pair), without the LDS unit: swapping the odd rows of
+// one copy with the even rows of another leaves own and other value in two registers.
+__device__ __forceinline__ void kv_pair16(float v, float& a, float& b) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned x = r[0], y = r[1];
+    a = __builtin_bit_cast(float, x); b = __builtin_bit_cast(float, y);
+}
+__device__ __forceinline__ void kv_pair32(float v, float& a, float& b) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned x = r[0], y = r[1];
+    a = __builtin_bit_cast(float, x); b = __builtin_bit_cast(float, y);
+}
+__device__ __forceinline__ float kv_max32(float v) { float a, b; kv_pair32(v, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float kv_sum32(float v) { float a, b; kv_pair32(v, a, b); return a + b; }
+// Over the four lanes of one column (16 apart).
+__device__ __forceinline__ float kv_max4(float v) { float a, b; kv_pair16(v, a, b); return kv_max32(fmaxf(a, b)); }
+__device__ __forceinline__ float kv_sum4(float v) { float a, b; kv_pair16(v, a, b); return kv_sum32(a + b); }
 
 // ---- products with the rotation ------------------------------------------------------------------------------------
 

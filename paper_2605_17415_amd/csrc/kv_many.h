@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, st[x][r]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * gain;
+        top = kv_max32(top) * gain;
         // 16 bits: a row's maximum may lag by 2^8, weights of up to 256 lose nothing; with codes they meet the norms in float16
         const bool grows = top > m + (codes || m == -INFINITY ? 0.f : 8.f);
         if (__ballot(grows)) {
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         }
         __syncthreads();
     }
-    l += __shfl_xor(l, 32);
+    l = kv_sum32(l);
     if (col >= cols) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     // register r of o[k]: coordinate 32 k + 8 (r / 4) + 4 half + r % 4
