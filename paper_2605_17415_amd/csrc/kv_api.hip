@@ -14,14 +14,12 @@ extern template hipError_t kv_attend_d<128>(const KvAttend&, const KvWork&, int,
 extern template hipError_t kv_attend_d<192>(const KvAttend&, const KvWork&, int, hipStream_t);
 extern template hipError_t kv_attend_d<256>(const KvAttend&, const KvWork&, int, hipStream_t);
 
-KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity) {
+KvWork kv_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity) {
     KvWork w{};
     const int64_t cols = (int64_t)max_new * (q_heads / kv_heads);
     w.few = cols <= kFewRows;
     w.col_tiles = w.few ? (int)((cols + 15) / 16) : 0;
-    const int64_t pairs = (int64_t)batch * kv_heads;
     w.split = w.few && capacity > 512;
-    w.wgs = w.split ? 1024 : 0;
     int64_t at = 0;
     auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
     if (format == IVFTQ_KV_CODE4) {
@@ -30,10 +28,9 @@ KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_h
         w.whole = room(rows * q_heads * d * 4);
     }
     if (w.split) {
-        w.part = room((int64_t)w.col_tiles * 2 * w.wgs * 16 * d * 4);
-        w.ml = room((int64_t)w.col_tiles * 2 * w.wgs * 16 * 2 * 4);
+        w.part = room((int64_t)w.col_tiles * 2 * kFewMaxWgs * 16 * d * 4);
+        w.ml = room((int64_t)w.col_tiles * 2 * kFewMaxWgs * 16 * 2 * 4);
     }
-    (void)pairs;
     w.bytes = at;
     return w;
 }
@@ -226,7 +223,7 @@ int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int
         return -1;
     }
     if (max_new > rows) max_new = rows > 1 ? (int32_t)rows : 1;
-    return kv_work(cache->format, cache->d, cache->batch, cache->heads, rows, q_heads, max_new, (int64_t)cache->columns * cache->page).bytes;
+    return kv_work(cache->format, cache->d, cache->heads, rows, q_heads, max_new, (int64_t)cache->columns * cache->page).bytes;
 }
 
 ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse, const int32_t* starts,
@@ -242,7 +239,7 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     if (!q->rows || !cache->batch) return IVFTQ_OK;
     if (!starts) max_new = 1;
     if (max_new > q->rows) max_new = (int32_t)q->rows;
-    const KvWork w = kv_work(cache->format, cache->d, cache->batch, cache->heads, q->rows, q->heads, max_new, (int64_t)cache->columns * cache->page);
+    const KvWork w = kv_work(cache->format, cache->d, cache->heads, q->rows, q->heads, max_new, (int64_t)cache->columns * cache->page);
     if (w.bytes && (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)))
         return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)workspace_bytes, (long long)w.bytes);
     KvAttend a{};

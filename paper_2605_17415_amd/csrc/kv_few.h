@@ -18,6 +18,7 @@ namespace ivftq {
 
 constexpr int kFewRows = 64;          // query rows a key-value head: four column tiles of 16
 constexpr int kFewTile = 32;          // tokens of a wavefront's step
+constexpr int kFewMaxWgs = 1024;      // workgroups that share the tiles, at most: as many as the chip holds at once
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct FewArgs {
@@ -486,14 +487,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_few(FewArgs f) {
     }
 }
 
-// Pairs whose tiles lie in more than one share: their parts put together.  One workgroup a pair and column tile; a
-// wavefront takes a row at a time, its lanes the parts' weights first, then coordinates.  Codes: every pair; its 16 rows are
-// then rotated back, each wavefront computing every fourth block of 32 coordinates.
+// Pairs whose tiles lie in more than one share: their parts put together.  One workgroup a pair and column tile, a wavefront a
+// row: D / 4 lanes read a part, the others the parts beside it, eight at a time.  Codes: every pair; its 16 rows are then
+// rotated back, each wavefront computing a block of 32 coordinates.
 template <int F, int D>
-__global__ __launch_bounds__(256) void k_kv_few_join(FewArgs f) {
-    constexpr int kLanes = (D + 63) / 64;
-    __shared__ float row_sum[F == IVFTQ_KV_CODE4 ? 16 : 1][D + 4];
-    __shared__ float weight[4][64];
+__global__ __launch_bounds__(512) void k_kv_few_join(FewArgs f) {
+    constexpr int kPart = D / 4, kBeside = 64 / kPart > 0 ? 64 / kPart : 1;          // lanes of a part, parts side by side
+    static_assert(kPart <= 64);
+    __shared__ __align__(16) float row_sum[F == IVFTQ_KV_CODE4 ? 16 : 1][D + 4];
+    __shared__ float weight[8][64];
     const KvAttend& a = f.a;
     const int wave = kv_wave(), lane = threadIdx.x & 63;
     const int b = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, col0 = blockIdx.y * 16;
@@ -521,11 +523,12 @@ __global__ __launch_bounds__(256) void k_kv_few_join(FewArgs f) {
     }
     const bool joined = w0 != w1;
     if (!joined && F != IVFTQ_KV_CODE4) return;
-    for (int row = wave; row < 16 && col0 + row < cols; row += 4) {
+    const int beside = lane / kPart, j = lane % kPart * 4;
+    for (int row = wave; row < 16 && col0 + row < cols; row += 8) {
         const int col = col0 + row;
         const int64_t qrow = s.first + col / a.group;
         const int qhead = h * a.group + col % a.group;
-        float acc[kLanes] = {};
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         if (joined) {
             float top = -INFINITY, l = 0.f;
             // of the pair's first share the pair has the last part, of the others the first
@@ -546,54 +549,48 @@ __global__ __launch_bounds__(256) void k_kv_few_join(FewArgs f) {
                 weight[wave][lane] = turn;
                 const int many = w1 - v0 + 1 < 64 ? w1 - v0 + 1 : 64;
 #pragma unroll 8
-                for (int i = 0; i < many; ++i) {
+                for (int i = beside; i < many; i += kBeside) {
+                    if (kBeside * kPart < 64 && beside >= kBeside) break;
                     const int64_t slot = base + 2 * (v0 + i) + (v0 + i == w0 && begins ? 1 : 0);
                     const float t = weight[wave][i];
-#pragma unroll
-                    for (int k = 0; k < kLanes; ++k)
-                        if (D % 64 == 0 || 64 * k + lane < D) acc[k] += f.part[(slot * 16 + row) * D + 64 * k + lane] * t;
+                    const float4 u = *reinterpret_cast<const float4*>(f.part + (slot * 16 + row) * D + j);
+                    acc.x += u.x * t; acc.y += u.y * t; acc.z += u.z * t; acc.w += u.w * t;
                 }
+            }
+#pragma unroll
+            for (int o = kPart; o < kPart * kBeside; o <<= 1) {
+                acc.x += __shfl(acc.x, lane + o); acc.y += __shfl(acc.y, lane + o); acc.z += __shfl(acc.z, lane + o); acc.w += __shfl(acc.w, lane + o);
             }
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
             const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-            for (int k = 0; k < kLanes; ++k) acc[k] *= inv;
+            acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
             if (a.lse && lane == 0) a.lse[qrow * a.q.heads + qhead] = l > 0.f ? (top + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
-        } else if constexpr (F == IVFTQ_KV_CODE4) {
-#pragma unroll
-            for (int k = 0; k < kLanes; ++k)
-                if (D % 64 == 0 || 64 * k + lane < D) acc[k] = f.whole[(qrow * a.q.heads + qhead) * D + 64 * k + lane];
+        } else if (F == IVFTQ_KV_CODE4 && beside == 0) {
+            acc = *reinterpret_cast<const float4*>(f.whole + (qrow * a.q.heads + qhead) * D + j);
         }
+        if (beside) continue;
         if constexpr (F == IVFTQ_KV_CODE4) {
-#pragma unroll
-            for (int k = 0; k < kLanes; ++k)
-                if (D % 64 == 0 || 64 * k + lane < D) row_sum[row][64 * k + lane] = acc[k];
+            *reinterpret_cast<float4*>(&row_sum[row][j]) = acc;
         } else {
-            uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride;
-#pragma unroll
-            for (int k = 0; k < kLanes; ++k)
-                if (D % 64 == 0 || 64 * k + lane < D) p[64 * k + lane] = kv_from_float<F == IVFTQ_KV_BF16>(acc[k]);
+            constexpr bool bf = F == IVFTQ_KV_BF16;
+            uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride + j;
+            *reinterpret_cast<uint2*>(p) = make_uint2(kv_pack2<bf>(acc.x, acc.y), kv_pack2<bf>(acc.z, acc.w));
         }
     }
     if constexpr (F == IVFTQ_KV_CODE4) {
         __syncthreads();
+        if (wave >= D / 32) return;
         const int n = lane & 15, g = lane >> 4, col = col0 + n;
         const bool in = col < cols;
-        float x[D / 32][8];
+        float x[D / 32][8], y[1][8];
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f;
         const float norm = kv_unit_row<D>(x) * a.c.level_unit;
-#pragma unroll 1
-        for (int t = wave; t < D / 32; t += 4) {
-            float y[1][8];
-            kv_rotate16<D, true>(a.c.rotation, t, x, y);
-            if (!in) continue;
-            const int64_t qrow = s.first + col / a.group;
-            kv_store_turned(a.out, qrow, h * a.group + col % a.group, t, y[0], norm);
-        }
+        kv_rotate16<D, true>(a.c.rotation, wave, x, y);
+        if (in) kv_store_turned(a.out, s.first + col / a.group, h * a.group + col % a.group, wave, y[0], norm);
     }
 }
 

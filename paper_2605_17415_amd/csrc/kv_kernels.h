@@ -131,19 +131,21 @@ __device__ __forceinline__ float kv_level(uint32_t nibble, const KvView& c) {
     return nibble & 8 ? -v : v;
 }
 
-// Sign and magnitude of the level next to v (no number: magnitude 0): three comparisons, each against the boundary that the
-// one before leaves.
-__device__ __forceinline__ uint32_t kv_nibble(float v, const KvView& c) {
-    const float a = __builtin_fabsf(v);
-    const bool b2 = a >= c.bound[3];
-    const bool b1 = a >= (b2 ? c.bound[5] : c.bound[1]);
-    const bool b0 = a >= (b2 ? (b1 ? c.bound[6] : c.bound[4]) : (b1 ? c.bound[2] : c.bound[0]));
-    return (b2 ? 4u : 0u) | (b1 ? 2u : 0u) | (b0 ? 1u : 0u) | (__builtin_bit_cast(uint32_t, v) >> 28 & 8u);
-}
+// Signs and magnitudes of the levels next to eight values (no number: magnitude 0): three comparisons each, every one against
+// the boundary that the one before leaves; a word's bits are shifted in from its top by additions with carry.
 __device__ __forceinline__ uint32_t kv_nibbles8(const float (&y)[8], const KvView& c) {
     uint32_t w = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w |= kv_nibble(y[e], c) << 4 * e;
+    for (int e = 7; e >= 0; --e) {
+        const float a = __builtin_fabsf(y[e]);
+        const bool b2 = a >= c.bound[3];
+        const bool b1 = a >= (b2 ? c.bound[5] : c.bound[1]);
+        const bool b0 = a >= (b2 ? (b1 ? c.bound[6] : c.bound[4]) : (b1 ? c.bound[2] : c.bound[0]));
+        w = w + w + (y[e] < 0.f);
+        w = w + w + b2;
+        w = w + w + b1;
+        w = w + w + b0;
+    }
     return w;
 }
 

@@ -375,9 +375,9 @@ __global__ __launch_bounds__(64) void k_kv_rotate_back(KvRows out, const float* 
 // Sizes of the workspace's parts, as the launch and the caller's question see them.
 struct KvWork {
     int64_t z, zn, whole, part, ml, bytes;
-    int32_t few, col_tiles, wgs, split;
+    int32_t few, col_tiles, split;
 };
-KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity);
+KvWork kv_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity);
 
 template <int F, int D>
 hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) {
@@ -387,9 +387,15 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
     if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, 64, 0, st>>>(a.q, a.c.rotation, z, zn);
     const unsigned pairs = (unsigned)(a.c.batch * a.c.heads);
     if (w.few) {
-        FewArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), reinterpret_cast<float*>(a.work + w.ml), w.wgs, w.split};
-        k_kv_few<F, D><<<dim3(w.split ? (unsigned)w.wgs : pairs, (unsigned)w.col_tiles), 256, 0, st>>>(f);
-        if (w.split || F == IVFTQ_KV_CODE4) k_kv_few_join<F, D><<<dim3(pairs, (unsigned)w.col_tiles), 256, 0, st>>>(f);
+        static ChipFill fill;
+        unsigned wgs = 0;
+        if (w.split) {
+            if (hipError_t e = fill.get(reinterpret_cast<const void*>(&k_kv_few<F, D>), 256, 0, &wgs)) return e;
+            if (wgs > (unsigned)kFewMaxWgs) wgs = kFewMaxWgs;
+        }
+        FewArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), reinterpret_cast<float*>(a.work + w.ml), (int32_t)wgs, w.split};
+        k_kv_few<F, D><<<dim3(w.split ? wgs : pairs, (unsigned)w.col_tiles), 256, 0, st>>>(f);
+        if (w.split || F == IVFTQ_KV_CODE4) k_kv_few_join<F, D><<<dim3(pairs, (unsigned)w.col_tiles), 512, 0, st>>>(f);
     } else {
         const int row_tiles = (int)(((int64_t)a.max_new * a.group + kManyRows - 1) / kManyRows);
         ManyArgs f{a, z, zn, whole, row_tiles};

@@ -1,4 +1,7 @@
 // Rows of the paged key-value cache: written to their pages (rotated and quantised where the cache holds codes) and read back.
+#include <cstring>
+#include <type_traits>
+
 #include "kv_kernels.h"
 
 namespace ivftq {
@@ -285,20 +288,139 @@ __device__ __forceinline__ uint32_t turn_nibbles(uint32_t w, int lane) {
     return lane & 1 ? (w & 0xf0f0f0f0u) | (p >> 4 & 0x0f0f0f0fu) : (w & 0x0f0f0f0fu) | (p << 4 & 0xf0f0f0f0u);
 }
 
+// The eight levels, times 2^10, as two float16 parts that keep them to 2^-22: byte tables like those of kv_levels8, the second
+// part with a sign of its own.
+struct KvExact { uint32_t hi[4], lo[4]; };          // of each part: low bytes, then high bytes
+
+KvExact kv_exact(const KvView& c) {
+    KvExact x{};
+    for (int m = 0; m < 8; ++m) {
+        const float v = c.level[m] * kSplitScale;
+        const _Float16 part[2] = {(_Float16)v, (_Float16)(v - (float)(_Float16)v)};
+        for (int p = 0; p < 2; ++p) {
+            uint16_t bits;
+            memcpy(&bits, &part[p], 2);
+            uint32_t* to = p ? x.lo : x.hi;
+            to[m / 4] |= (uint32_t)(bits & 0xff) << 8 * (m % 4);
+            to[2 + m / 4] |= (uint32_t)(bits >> 8) << 8 * (m % 4);
+        }
+    }
+    return x;
+}
+
+__device__ __forceinline__ void kv_exact8(uint32_t w, const KvExact& x, halfx8& hi, halfx8& lo) {
+    const uint32_t even = w & 0x07070707u, odd = (w >> 4) & 0x07070707u, even_sign = (w << 4) & 0x80808080u, odd_sign = w & 0x80808080u;
+    uintx4 r[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const uint32_t* t = p ? x.lo : x.hi;
+        const uint32_t el = __builtin_amdgcn_perm(t[1], t[0], even), eh = __builtin_amdgcn_perm(t[3], t[2], even) ^ even_sign;
+        const uint32_t ol = __builtin_amdgcn_perm(t[1], t[0], odd), oh = __builtin_amdgcn_perm(t[3], t[2], odd) ^ odd_sign;
+        r[p][0] = __builtin_amdgcn_perm(eh, el, 0x05010400u);
+        r[p][1] = __builtin_amdgcn_perm(eh, el, 0x07030602u);
+        r[p][2] = __builtin_amdgcn_perm(oh, ol, 0x05010400u);
+        r[p][3] = __builtin_amdgcn_perm(oh, ol, 0x07030602u);
+    }
+    hi = __builtin_bit_cast(halfx8, r[0]);
+    lo = __builtin_bit_cast(halfx8, r[1]);
+}
+
 // Several rows a sequence.  The rotation stands in LDS as two float16 parts in operand order, so that reading it costs 64
-// KB of LDS traffic per 32 rows and none of L2 (at d = 256 and 192 a workgroup computes one half of the coordinates:
-// 128 and 72 KB).  A wavefront takes a tile of 32 tokens of one head's keys or values: two column tiles, three products.
+// KB of LDS traffic per 32 rows and none of L2 (at d = 256 and 192 a workgroup computes one half of the coordinates: 128
+// and 72 KB).  A wavefront takes a tile of 32 tokens of one head's keys or values, two column tiles, and has the next
+// tile's rows on their way meanwhile.  Writing: a row's values are float16 numbers as they are, or become such by a power of
+// two that puts the row's length between 2^8 and 2^9 (what that loses lies 2^-25 under the row's largest value), so two
+// products do, and the results are divided by the row's length afterwards.  Reading: the levels as two parts as well, three
+// products.  Bound by the vector unit: of about 1700 operations a tile of 64 x 32 values 800 look for the levels.
 template <int D> constexpr int kOutputs = D > 128 ? D / 2 : D;             // coordinates that a workgroup computes
 template <int D> constexpr int kTurnBytes = kOutputs<D> * D * 4;
+constexpr int kTileThreads = 512;
+
+template <int D, bool READ>
+struct TileRows {                                                          // a tile as it is read from memory
+    static constexpr int NS = D / 32;
+    typename std::conditional<READ, uint32_t, uintx4>::type w[2][NS];
+    uint32_t norm[2];
+    char* rec[2];
+};
+
+template <int D, bool READ>
+__device__ __forceinline__ void load_tile(const KvView& c, const KvRows& rows, const NewItem& it, int h, bool value, TileRows<D, READ>& x) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, codes = c.page * (D / 2);
+    const int t0 = (it.s.tile0 + it.tile) * 32;
+#pragma unroll
+    for (int ct = 0; ct < 2; ++ct) {
+        const int64_t page = kv_uniform((int)kv_page(c, it.b, t0 + 16 * ct));          // 16 tokens lie in one page
+        const int t = t0 + 16 * ct + n, at = t & (c.page - 1);
+        const bool mine = t >= it.s.pos0 && t < it.s.end;
+        x.rec[ct] = page < 0 ? nullptr : kv_record(c, page, h);
+        x.norm[ct] = 0;
+        if constexpr (READ) {
+            const char* rec = page < 0 ? kv_record(c, 0, h) : x.rec[ct];
+            x.norm[ct] = reinterpret_cast<const uint16_t*>(rec + 2 * codes)[(value ? c.page : 0) + at];
+            const uint32_t* p = value ? reinterpret_cast<const uint32_t*>(rec + codes) + (at >> 3) * D + 8 * g + (n & 7)
+                                      : reinterpret_cast<const uint32_t*>(rec + at * (D / 2)) + g;
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) x.w[ct][s] = p[s * (value ? 32 : 4)];
+        } else {
+            const uint16_t* p = reinterpret_cast<const uint16_t*>(rows.data) + (mine ? it.s.first_row + t - it.s.pos0 : 0) * rows.row_stride + h * rows.head_stride + 8 * g;
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) x.w[ct][s] = *reinterpret_cast<const uintx4*>(p + 32 * s);
+        }
+    }
+}
+
+// Operands of a column tile: float16 values `hi` (writing) or levels in two parts (reading, in the order of kv_levels8);
+// returns what the products are multiplied by, and the row's norm.
+template <int D, bool BF>
+__device__ __forceinline__ float row_operand(const uintx4 (&w)[D / 32], halfx8 (&x)[D / 32], float& norm) {
+    float n2 = 0.f;
+    if constexpr (BF) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float lo = kv_to_float<true>(w[s][e] & 0xffff), hi = __builtin_bit_cast(float, w[s][e] & 0xffff0000u);
+                n2 += lo * lo;
+                n2 += hi * hi;
+            }
+        norm = sqrtf(kv_sum4(n2));
+        // the power of two next under 2^9 / norm; norms of zero, none and infinity: any
+        const int up = 8 + 127 - (int)(__builtin_bit_cast(uint32_t, norm) >> 23);
+        const float scale = __builtin_bit_cast(float, (uint32_t)(up + 127 < 1 ? 1 : (up + 127 > 254 ? 254 : up + 127)) << 23);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            uintx4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = kv_pack2<false>(kv_to_float<true>(w[s][e] & 0xffff) * scale, __builtin_bit_cast(float, w[s][e] & 0xffff0000u) * scale);
+            x[s] = __builtin_bit_cast(halfx8, y);
+        }
+        return norm > 0.f ? 1.f / (norm * scale * kSplitScale) : 0.f;
+    } else {
+        typedef _Float16 two __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            x[s] = __builtin_bit_cast(halfx8, w[s]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t u = w[s][e];          // (a bit cast of an element of a vector casts the first one, whichever is named)
+                const two p = __builtin_bit_cast(two, u);
+                n2 = __builtin_amdgcn_fdot2(p, p, n2, false);
+            }
+        }
+        norm = sqrtf(kv_sum4(n2));
+        return norm > 0.f ? 1.f / (norm * kSplitScale) : 0.f;
+    }
+}
 
 template <int D, bool BF, bool READ>
-__global__ __launch_bounds__(256) void k_kv_tiles_codes(KvView c, KvRows k, KvRows v) {
+__global__ __launch_bounds__(kTileThreads, D <= 128 ? 4 : 2) void k_kv_tiles_codes(KvView c, KvRows k, KvRows v, KvExact exact) {
     constexpr int NS = D / 32, NT = kOutputs<D> / 32;
     extern __shared__ __align__(16) char turn[];                           // [NT][2][NS][hi, lo][64 lanes] of 16 bytes
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int out0 = blockIdx.y * kOutputs<D>;
     if (READ && out0 == 0) no_place(c, k, v, D);
-    for (int u = threadIdx.x; u < NT * 2 * NS * 64; u += 256) {
+    for (int u = threadIdx.x; u < NT * 2 * NS * 64; u += kTileThreads) {
         const int l = u & 63, s = u / 64 % NS, half = u / 64 / NS & 1, t = u / 64 / NS / 2, m = l & 15;
         // a lane's results: coordinates out0 + g * outputs / 4 + 8 t + 4 half + (0 .. 3)
         const int i = out0 + (m >> 2) * (kOutputs<D> / 4) + 8 * t + 4 * half + (m & 3), k0 = 32 * s + 8 * (l >> 4);
@@ -306,8 +428,9 @@ __global__ __launch_bounds__(256) void k_kv_tiles_codes(KvView c, KvRows k, KvRo
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float p = (READ ? c.rotation[(k0 + e) * D + i] : c.rotation[i * D + k0 + e]) * kSplitScale;
-            hi[e] = (_Float16)p;
-            lo[e] = (_Float16)(p - (float)hi[e]);
+            const int at = READ ? kv_slot(e) : e;
+            hi[at] = (_Float16)p;
+            lo[at] = (_Float16)(p - (float)hi[at]);
         }
         halfx8* to = reinterpret_cast<halfx8*>(turn) + (u / 64) * 128 + l;
         to[0] = hi;
@@ -316,49 +439,37 @@ __global__ __launch_bounds__(256) void k_kv_tiles_codes(KvView c, KvRows k, KvRo
     __syncthreads();
     const int codes = c.page * (D / 2), per_tile = 2 * c.heads;
     NewItem it = first_item(c, per_tile);
-    for (; it.left > 0; next_item(c, per_tile, it)) {
+    if (it.left <= 0) return;
+    TileRows<D, READ> next;
+    load_tile<D, READ>(c, it.sub >= c.heads ? v : k, it, it.sub >= c.heads ? it.sub - c.heads : it.sub, it.sub >= c.heads, next);
+    while (it.left > 0) {
         const bool value = it.sub >= c.heads;
         const int h = value ? it.sub - c.heads : it.sub, t0 = (it.s.tile0 + it.tile) * 32;
+        const NewTiles seq = it.s;
         const KvRows& rows = value ? v : k;
-        halfx8 xh[2][NS], xl[2][NS];
-        float norm[2];
+        halfx8 xh[2][NS], xl[2][READ ? NS : 1];
+        float norm[2], gain[2];
         char* rec[2];
-        int at[2];
         bool mine[2];
 #pragma unroll
         for (int ct = 0; ct < 2; ++ct) {
             const int t = t0 + 16 * ct + n;
-            const int64_t page = kv_page(c, it.b, t);
-            mine[ct] = t >= it.s.pos0 && t < it.s.end;
-            rec[ct] = page < 0 ? nullptr : kv_record(c, page, h);
-            at[ct] = t & (c.page - 1);
-            float x[NS][8];
+            mine[ct] = t >= seq.pos0 && t < seq.end;
+            rec[ct] = next.rec[ct];
             if constexpr (READ) {
-                norm[ct] = rec[ct] && mine[ct] ? (float)reinterpret_cast<const _Float16*>(rec[ct] + 2 * codes)[(value ? c.page : 0) + at[ct]] : 0.f;
+                norm[ct] = (float)__builtin_bit_cast(_Float16, (uint16_t)next.norm[ct]);
+                gain[ct] = norm[ct] * (1.f / (kSplitScale * kSplitScale));
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
-                    uint32_t w = 0;
-                    if (rec[ct]) {
-                        if (value) w = reinterpret_cast<const uint32_t*>(rec[ct] + codes)[(int64_t)(at[ct] >> 3) * D + 32 * s + 8 * g + (n & 7)];
-                        else w = reinterpret_cast<const uint32_t*>(rec[ct] + (int64_t)at[ct] * (D / 2))[4 * s + g];
-                    }
-                    if (value) w = turn_nibbles(w, lane);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[s][e] = kv_level(w >> 4 * e & 15, c);
+                    const uint32_t w = value ? turn_nibbles(next.w[ct][s], lane) : next.w[ct][s];
+                    kv_exact8(w, exact, xh[ct][s], xl[ct][s]);
                 }
             } else {
-                load_row<D, BF>(rows, it.s.first_row + t - it.s.pos0, h, mine[ct], x);
-                norm[ct] = kv_unit_row<D>(x);
+                gain[ct] = row_operand<D, BF>(next.w[ct], xh[ct], norm[ct]);
             }
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float w = x[s][e] * kSplitScale;
-                    xh[ct][s][e] = (_Float16)w;
-                    xl[ct][s][e] = (_Float16)(w - (float)xh[ct][s][e]);
-                }
         }
+        next_item(c, per_tile, it);
+        if (it.left > 0) load_tile<D, READ>(c, it.sub >= c.heads ? v : k, it, it.sub >= c.heads ? it.sub - c.heads : it.sub, it.sub >= c.heads, next);
 #pragma unroll 1
         for (int t = 0; t < NT; ++t) {
             float y[2][8];
@@ -372,39 +483,42 @@ __global__ __launch_bounds__(256) void k_kv_tiles_codes(KvView c, KvRows k, KvRo
 #pragma unroll
                     for (int ct = 0; ct < 2; ++ct) {
                         acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, xh[ct][s], acc[ct], 0, 0, 0);
-                        acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, xl[ct][s], acc[ct], 0, 0, 0);
                         acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, xh[ct][s], acc[ct], 0, 0, 0);
+                        if constexpr (READ) acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, xl[ct][s], acc[ct], 0, 0, 0);
                     }
                 }
 #pragma unroll
                 for (int ct = 0; ct < 2; ++ct)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) y[ct][4 * half + r] = acc[ct][r] * (1.f / (kSplitScale * kSplitScale));
+                    for (int r = 0; r < 4; ++r) y[ct][4 * half + r] = acc[ct][r] * gain[ct];
             }
             const int j = out0 + g * (kOutputs<D> / 4) + 8 * t;
 #pragma unroll
             for (int ct = 0; ct < 2; ++ct) {
+                const int at = (t0 + 16 * ct + n) & (c.page - 1);
                 if constexpr (READ) {
                     if (!mine[ct]) continue;
                     uintx4 w = {0, 0, 0, 0};
                     if (rec[ct])
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = kv_pack2<BF>(y[ct][2 * e] * norm[ct], y[ct][2 * e + 1] * norm[ct]);
-                    *reinterpret_cast<uintx4*>(reinterpret_cast<uint16_t*>(rows.data) + (int64_t)(it.s.first_row + t0 + 16 * ct + n - it.s.pos0) * rows.row_stride +
+                        for (int e = 0; e < 4; ++e) w[e] = kv_pack2<BF>(y[ct][2 * e], y[ct][2 * e + 1]);
+                    *reinterpret_cast<uintx4*>(reinterpret_cast<uint16_t*>(rows.data) + (int64_t)(seq.first_row + t0 + 16 * ct + n - seq.pos0) * rows.row_stride +
                                                h * rows.head_stride + j) = w;
-                } else {
+                } else if (rec[ct]) {
                     uint32_t w = kv_nibbles8(y[ct], c);
                     if (!value) {
-                        if (mine[ct] && rec[ct]) reinterpret_cast<uint32_t*>(rec[ct] + (int64_t)at[ct] * (D / 2))[j / 8] = w;
+                        if (mine[ct]) reinterpret_cast<uint32_t*>(rec[ct] + at * (D / 2))[j / 8] = w;
                     } else {
                         w = turn_nibbles(w, lane);           // this lane: coordinate j + n % 8, tokens of its group of eight
                         const uint32_t given = (uint32_t)(__ballot(mine[ct]) >> (lane & 56)) & 0xff;
-                        uint32_t keep = 0;
+                        uint32_t* p = reinterpret_cast<uint32_t*>(rec[ct] + codes) + (at >> 3) * D + j + (n & 7);
+                        if (given == 0xff) {
+                            *p = w;
+                        } else if (given) {                  // the other tokens' half bytes stay
+                            uint32_t keep = 0;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) keep |= given >> e & 1 ? 0 : 15u << 4 * e;
-                        if (given && rec[ct]) {
-                            uint32_t* p = reinterpret_cast<uint32_t*>(rec[ct] + codes) + (int64_t)(at[ct] >> 3) * D + j + (n & 7);
-                            *p = keep ? (*p & keep) | (w & ~keep) : w;
+                            for (int e = 0; e < 8; ++e) keep |= given >> e & 1 ? 0 : 15u << 4 * e;
+                            *p = (*p & keep) | (w & ~keep);
                         }
                     }
                 }
@@ -413,15 +527,16 @@ __global__ __launch_bounds__(256) void k_kv_tiles_codes(KvView c, KvRows k, KvRo
         if constexpr (!READ) {
 #pragma unroll
             for (int ct = 0; ct < 2; ++ct)
-                if (g == 0 && out0 == 0 && mine[ct] && rec[ct]) reinterpret_cast<_Float16*>(rec[ct] + 2 * codes)[(value ? c.page : 0) + at[ct]] = (_Float16)norm[ct];
+                if (g == 0 && out0 == 0 && mine[ct] && rec[ct])
+                    reinterpret_cast<_Float16*>(rec[ct] + 2 * codes)[(value ? c.page : 0) + ((t0 + 16 * ct + n) & (c.page - 1))] = (_Float16)norm[ct];
         }
     }
 }
 
 // Workgroups for the tiles: as many as the chip holds at once, or fewer where there cannot be that many items.
-hipError_t tile_grid(ChipFill& fill, const void* kernel, size_t lds, const KvView& c, int per_tile, int slices, unsigned* wgs) {
-    if (hipError_t e = fill.get(kernel, 256, lds, wgs)) return e;
-    const int64_t most = (((int64_t)c.rows / 32 + 2 * (int64_t)c.batch) * per_tile + 3) / 4;
+hipError_t tile_grid(ChipFill& fill, const void* kernel, int threads, size_t lds, const KvView& c, int per_tile, int slices, unsigned* wgs) {
+    if (hipError_t e = fill.get(kernel, threads, lds, wgs)) return e;
+    const int64_t waves = threads / 64, most = (((int64_t)c.rows / 32 + 2 * (int64_t)c.batch) * per_tile + waves - 1) / waves;
     *wgs = *wgs / slices ? *wgs / slices : 1;
     if (most < *wgs) *wgs = (unsigned)most;
     return hipSuccess;
@@ -433,8 +548,8 @@ hipError_t tiles_codes(const KvView& c, const KvRows& k, const KvRows& v, hipStr
     constexpr int slices = D / kOutputs<D>;
     const void* kernel = reinterpret_cast<const void*>(&k_kv_tiles_codes<D, BF, READ>);
     unsigned wgs;
-    if (hipError_t e = tile_grid(fill, kernel, kTurnBytes<D>, c, 2 * c.heads, slices, &wgs)) return e;
-    k_kv_tiles_codes<D, BF, READ><<<dim3(wgs, slices), 256, kTurnBytes<D>, st>>>(c, k, v);
+    if (hipError_t e = tile_grid(fill, kernel, kTileThreads, kTurnBytes<D>, c, 2 * c.heads, slices, &wgs)) return e;
+    k_kv_tiles_codes<D, BF, READ><<<dim3(wgs, slices), kTileThreads, kTurnBytes<D>, st>>>(c, k, v, READ ? kv_exact(c) : KvExact{});
     return hipGetLastError();
 }
 
@@ -458,7 +573,7 @@ template <bool READ>
 hipError_t tiles16(const KvView& c, const KvRows& k, const KvRows& v, int d, hipStream_t st) {
     static ChipFill fill;
     unsigned wgs;
-    if (hipError_t e = tile_grid(fill, reinterpret_cast<const void*>(&k_kv_tiles16<READ>), 0, c, c.heads, 1, &wgs)) return e;
+    if (hipError_t e = tile_grid(fill, reinterpret_cast<const void*>(&k_kv_tiles16<READ>), 256, 0, c, c.heads, 1, &wgs)) return e;
     k_kv_tiles16<READ><<<wgs, 256, 0, st>>>(c, k, v, d);
     return hipGetLastError();
 }

@@ -182,3 +182,34 @@ def test_other_stream_and_strides():
     pkg.kv_append(two, kv[:, 0], kv[:, 1], wide[:, : c.columns], t["lengths"], stream=s, **codec)
     torch.cuda.synchronize()
     assert torch.equal(one, two)
+
+
+@pytest.mark.parametrize("kind,scale", [("f16", 2.0 ** -17), ("f16", 1000.0), ("bf16", 2.0 ** -100), ("bf16", 2.0 ** 9), ("bf16", 2.0 ** -17)])
+@pytest.mark.parametrize("single", (False, True))
+def test_codes_of_short_and_long_rows(kind, scale, single):
+    """Codes depend on a row's direction alone: rows of subnormal float16 numbers, rows near the largest norm, rows far under it."""
+    pkg = _pkg()
+    d, n = 128, 40
+    lens = [1] * n if single else [n]
+    c = ref.Cache(12, "code4", 1, d, 16, lens)
+    t, codec = c.device()
+    x = (torch.randn(n, 2, 1, d, generator=torch.Generator().manual_seed(9)) * scale).to(ref.TYPES[kind])
+    where = {} if single else {"starts": starts_of([n])}
+    pkg.kv_append(t["pool"], x[:, 0].to(DEV), x[:, 1].to(DEV), t["table"], t["lengths"], **where, **codec)
+    torch.cuda.synchronize()
+    c.take(t["pool"].cpu())
+    level = c.levels.astype(np.float64)
+    border = (level[1:] + level[:-1]) / 2
+    seq, pos = (range(n), [0] * n) if single else ([0] * n, range(n))
+    pages, inside = [c.table[b, p // 16] for b, p in zip(seq, pos)], [p % 16 for p in pos]
+    for i in range(2):
+        rows = x[:, i, 0].double().numpy()
+        norm = np.linalg.norm(rows, axis=-1)
+        if norm.max() < 2.0 ** -63:                          # shorter than float32 can square: zeros
+            assert (c.norms[i, pages, 0, inside] == 0).all()
+            continue
+        rho = rows @ c.rotation.astype(np.float64).T / norm[:, None]
+        far = np.abs(rho[..., None] - border).min(axis=-1) > 2.0 ** -19
+        assert np.array_equal(c.codes[i, pages, 0, inside][far], np.searchsorted(border, rho, side="right")[far])
+        got = c.norms[i, pages, 0, inside].astype(np.float64)
+        assert (np.abs(got - norm) <= norm * (2.0 ** -11 + 2.0 ** -18) + 2.0 ** -25).all()
