@@ -14,19 +14,32 @@ extern template hipError_t kv_attend_d<128>(const KvAttend&, const KvWork&, int,
 extern template hipError_t kv_attend_d<192>(const KvAttend&, const KvWork&, int, hipStream_t);
 extern template hipError_t kv_attend_d<256>(const KvAttend&, const KvWork&, int, hipStream_t);
 
-KvWork kv_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity) {
+KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity) {
     KvWork w{};
-    const int64_t cols = (int64_t)max_new * (q_heads / kv_heads);
+    const int64_t cols = (int64_t)max_new * (q_heads / kv_heads), all = rows * q_heads;
     w.few = cols <= kFewRows;
-    w.col_tiles = w.few ? (int)((cols + 15) / 16) : 0;
-    w.split = w.few && capacity > 512;
+    w.parts = 1;
+    if (w.few) {
+        w.col_tiles = (int)((cols + 15) / 16);
+        w.split = capacity > 512;
+    } else {
+        // Where the row tiles leave workgroups that a compute unit could hold without one, a tile's keys are shared out: over as
+        // many parts as fill them, at most eight, none under eight tiles of keys.  (200 row tiles of 128 rows over 20,000
+        // tokens in codes: 737 us in one part.)
+        w.row_tiles = (int)((cols + kManyRows - 1) / kManyRows);
+        const int64_t wgs = (int64_t)batch * kv_heads * w.row_tiles, room = 256 * (d <= 128 ? 2 : 1);
+        const int64_t fill = wgs ? (room + wgs - 1) / wgs : 1, longest = capacity / (8 * kManyTile);
+        w.parts = (int)(fill < longest ? fill : longest);
+        w.parts = w.parts < 1 ? 1 : (w.parts > 8 ? 8 : w.parts);
+    }
     int64_t at = 0;
     auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
     if (format == IVFTQ_KV_CODE4) {
-        w.z = room(rows * q_heads * d * 4);
-        w.zn = room(rows * q_heads * 4);
-        w.whole = room(rows * q_heads * d * 4);
+        w.z = room(all * d * 4);
+        w.zn = room(all * 4);
     }
+    if (format == IVFTQ_KV_CODE4 || w.parts > 1) w.whole = room(all * d * 4 * w.parts);
+    if (w.parts > 1) w.ml = room(all * 8 * w.parts);
     if (w.split) {
         w.part = room((int64_t)w.col_tiles * 2 * kFewMaxWgs * 16 * d * 4);
         w.ml = room((int64_t)w.col_tiles * 2 * kFewMaxWgs * 16 * 2 * 4);
@@ -223,7 +236,7 @@ int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int
         return -1;
     }
     if (max_new > rows) max_new = rows > 1 ? (int32_t)rows : 1;
-    return kv_work(cache->format, cache->d, cache->heads, rows, q_heads, max_new, (int64_t)cache->columns * cache->page).bytes;
+    return kv_work(cache->format, cache->d, cache->batch, cache->heads, rows, q_heads, max_new, (int64_t)cache->columns * cache->page).bytes;
 }
 
 ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse, const int32_t* starts,
@@ -239,7 +252,7 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     if (!q->rows || !cache->batch) return IVFTQ_OK;
     if (!starts) max_new = 1;
     if (max_new > q->rows) max_new = (int32_t)q->rows;
-    const KvWork w = kv_work(cache->format, cache->d, cache->heads, q->rows, q->heads, max_new, (int64_t)cache->columns * cache->page);
+    const KvWork w = kv_work(cache->format, cache->d, cache->batch, cache->heads, q->rows, q->heads, max_new, (int64_t)cache->columns * cache->page);
     if (w.bytes && (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)))
         return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)workspace_bytes, (long long)w.bytes);
     KvAttend a{};
@@ -253,8 +266,7 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     a.sinks = sinks;
     a.scale = scale;
     a.work = static_cast<char*>(workspace);
-    const int64_t tiles = ((int64_t)max_new * a.group + kManyRows - 1) / kManyRows;
-    if ((int64_t)cache->batch * cache->heads * tiles > INT32_MAX) return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups");
+    if ((int64_t)cache->batch * cache->heads * (w.few ? 1 : (int64_t)w.row_tiles * w.parts) > INT32_MAX) return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups");
     return done(launch_kv_attend(a, w, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_attend");
 }
 

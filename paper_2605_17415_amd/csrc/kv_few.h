@@ -583,14 +583,14 @@ __global__ __launch_bounds__(512) void k_kv_few_join(FewArgs f) {
         if (wave >= D / 32) return;
         const int n = lane & 15, g = lane >> 4, col = col0 + n;
         const bool in = col < cols;
-        float x[D / 32][8], y[1][8];
+        float x[D / 32][8], y[8];
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f;
         const float norm = kv_unit_row<D>(x) * a.c.level_unit;
-        kv_rotate16<D, true>(a.c.rotation, wave, x, y);
-        if (in) kv_store_turned(a.out, s.first + col / a.group, h * a.group + col % a.group, wave, y[0], norm);
+        KvTurn<D, true>(a.c.rotation, wave)(x, y);
+        if (in) kv_store_turned(a.out, s.first + col / a.group, h * a.group + col % a.group, wave, y, norm);
     }
 }
 

@@ -219,30 +219,20 @@ __device__ __forceinline__ float kv_unit_row(float (&x)[D / 32][8]) {
     return norm;
 }
 
-// 32 coordinates (block `first`, and N - 1 blocks after it) of y = Pi x, or of Pi^T x, for 16 unit rows.  A lane gets in
-// y[t][e] of its row, for Pi, coordinate 32 (first + t) + 8 (lane / 16) + e: which coordinate a row of the matrix operand
-// is can be chosen, and this choice leaves a lane with a whole word of codes; for Pi^T coordinate 32 (first + t) +
-// 16 (e / 4) + 4 (lane / 16) + e % 4, so that the sixteen lanes' reads down a column of Pi are neighbours.  Both sides go in
-// as sums of two float16 numbers, three products: y is good to about 2^-21 of the row's length, far under the distance of
-// two levels; one product alone would move one code in two thousand.
-template <int D, bool TRANSPOSED, int N>
-__device__ __forceinline__ void kv_rotate16(const float* __restrict__ pi, int first, const float (&x)[D / 32][8], float (&y)[N][8]) {
-    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    halfx8 bh[D / 32], bl[D / 32];
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = x[s][e] * kSplitScale;
-            bh[s][e] = (_Float16)v;
-            bl[s][e] = (_Float16)(v - (float)bh[s][e]);
-        }
-#pragma unroll
-    for (int t = 0; t < N; ++t)
+// 32 coordinates (a block) of y = Pi x, or of Pi^T x, for 16 unit rows at a time.  A lane gets in y[e] of its row, for Pi,
+// coordinate 32 block + 8 (lane / 16) + e: which coordinate a row of the matrix operand is can be chosen, and this choice
+// leaves a lane with a whole word of codes; for Pi^T coordinate 32 block + 16 (e / 4) + 4 (lane / 16) + e % 4, so that the
+// sixteen lanes' reads down a column of Pi are neighbours.  Both sides go in as sums of two float16 numbers, three products:
+// y is good to about 2^-21 of the row's length, far under the distance of two levels; one product alone would move one code
+// in two thousand.
+template <int D, bool TRANSPOSED>
+struct KvTurn {
+    halfx8 hi[2][D / 32], lo[2][D / 32];
+    __device__ __forceinline__ KvTurn(const float* __restrict__ pi, int block) {
+        const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int i = 32 * (first + t) + (TRANSPOSED ? 16 * half + m : 8 * (m >> 2) + 4 * half + (m & 3));
-            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+            const int i = 32 * block + (TRANSPOSED ? 16 * half + m : 8 * (m >> 2) + 4 * half + (m & 3));
 #pragma unroll
             for (int s = 0; s < D / 32; ++s) {
                 float p[8];
@@ -254,21 +244,39 @@ __device__ __forceinline__ void kv_rotate16(const float* __restrict__ pi, int fi
                     const float4 u = r[0], w = r[1];
                     p[0] = u.x; p[1] = u.y; p[2] = u.z; p[3] = u.w; p[4] = w.x; p[5] = w.y; p[6] = w.z; p[7] = w.w;
                 }
-                halfx8 ah, al;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float v = p[e] * kSplitScale;
-                    ah[e] = (_Float16)v;
-                    al[e] = (_Float16)(v - (float)ah[e]);
+                    hi[half][s][e] = (_Float16)v;
+                    lo[half][s][e] = (_Float16)(v - (float)hi[half][s][e]);
                 }
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh[s], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl[s], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh[s], acc, 0, 0, 0);
+            }
+        }
+    }
+    __device__ __forceinline__ void operator()(const float (&x)[D / 32][8], float (&y)[8]) const {
+        floatx4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            halfx8 h, l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = x[s][e] * kSplitScale;
+                h[e] = (_Float16)v;
+                l[e] = (_Float16)(v - (float)h[e]);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[t][4 * half + r] = acc[r] * (1.f / (kSplitScale * kSplitScale));
+            for (int half = 0; half < 2; ++half) {
+                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], h, acc[half], 0, 0, 0);
+                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], l, acc[half], 0, 0, 0);
+                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[half][s], h, acc[half], 0, 0, 0);
+            }
         }
-}
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[4 * half + r] = acc[half][r] * (1.f / (kSplitScale * kSplitScale));
+    }
+};
 
 // A lane's eight coordinates of block t of Pi^T x into a 16-bit row.
 __device__ __forceinline__ void kv_store_turned(const KvRows& out, int64_t row, int64_t head, int t, const float (&y)[8], float norm) {

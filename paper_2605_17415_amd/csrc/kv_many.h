@@ -24,8 +24,9 @@ struct ManyArgs {
     KvAttend a;
     const uint16_t* z;                // codes: rotated unit queries, two float16 parts, eights in the order of kv_levels8
     const float* zn;                  // codes: the queries' norms
-    float* whole;                     // codes: results before they are rotated back
-    int32_t row_tiles;                // row tiles a (sequence, head): those of max_new
+    float* whole;                     // codes: results before they are rotated back; several parts: their sums [parts][rows][heads][D]
+    float* part_ml;                   // several parts: maximum (in log2 units) and sum of weights
+    int32_t row_tiles, parts;         // row tiles a (sequence, head): those of max_new; shares of a row tile's keys
 };
 
 template <int F>
@@ -105,8 +106,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     const KvAttend& a = f.a;
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
-    // heads fastest: with eight heads each XCD reads one head's pages; long row tiles (the last ones) first
-    const int h = blockIdx.x % c.heads, rt = f.row_tiles - 1 - (int)(blockIdx.x / c.heads) % f.row_tiles, b = blockIdx.x / c.heads / f.row_tiles;
+    // heads fastest: with eight heads each XCD reads one head's pages; then a row tile's shares, then sequences; the row tiles
+    // with the longest reach first
+    const int h = blockIdx.x % c.heads, part = blockIdx.x / c.heads % f.parts, b = blockIdx.x / c.heads / f.parts % c.batch;
+    const int rt = f.row_tiles - 1 - (int)(blockIdx.x / c.heads / f.parts / c.batch);
     const FewSeq s = few_seq(a, b);
     const int cols = s.count * a.group;
     if (rt * kManyRows >= cols) return;
@@ -117,6 +120,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     const int last_col = (rt + 1) * kManyRows < cols ? (rt + 1) * kManyRows - 1 : cols - 1;
     const int pos0 = s.base + rt * kManyRows / a.group, pos1 = s.base + last_col / a.group;
     const ManySpan span = many_span(a, pos0, pos1);
+    const int from = (int)((int64_t)span.tiles * part / f.parts), to = (int)((int64_t)span.tiles * (part + 1) / f.parts);
 
     // scores are multiplied by a factor above zero, so that their maximum is that of the products: a negative scale turns the
     // queries' signs, and none at all is taken as next to none
@@ -148,22 +152,22 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     const int tok = 16 * (n >> 4) + 8 * (n >> 2 & 1) + 4 * (n >> 3 & 1) + (n & 3);
 
     Stage stage;
-    auto page_of = [&](int i) { return i < span.tiles ? kv_page(c, b, span.first_token(i) + 16 * wave) : -1; };
-    auto load = [&](int i, int64_t page) { if (i < span.tiles) stage.load(c, h, page, span.first_token(i) + 16 * wave); };
-    int64_t ahead = page_of(0);
-    load(0, ahead);
-    ahead = page_of(1);
-    if (span.tiles) stage.store(c, lds[0], wave);
-    load(1, ahead);
-    ahead = page_of(2);
+    auto page_of = [&](int i) { return i < to ? kv_page(c, b, span.first_token(i) + 16 * wave) : -1; };
+    auto load = [&](int i, int64_t page) { if (i < to) stage.load(c, h, page, span.first_token(i) + 16 * wave); };
+    int64_t ahead = page_of(from);
+    load(from, ahead);
+    ahead = page_of(from + 1);
+    if (from < to) stage.store(c, lds[0], wave);
+    load(from + 1, ahead);
+    ahead = page_of(from + 2);
     __syncthreads();
 
-    for (int i = 0; i < span.tiles; ++i) {
-        const char* keys = lds[i & 1];
+    for (int i = from; i < to; ++i) {
+        const char* keys = lds[(i - from) & 1];
         const char* vals = keys + Stage::kKeyBytes;
         const float* gains = reinterpret_cast<const float*>(vals + kManyTile * D * 2);
         const int t0 = span.first_token(i);
-        if (i + 1 < span.tiles) stage.store(c, lds[(i + 1) & 1], wave);
+        if (i + 1 < to) stage.store(c, lds[(i - from + 1) & 1], wave);
         load(i + 2, ahead);
         ahead = page_of(i + 3);
 
@@ -300,74 +304,144 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     }
     l = kv_sum32(l);
     if (col >= cols) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = f.parts > 1 ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+    const int64_t row_head = qrow * a.q.heads + qhead, all = (int64_t)a.q.rows * a.q.heads;
     // register r of o[k]: coordinate 32 k + 8 (r / 4) + 4 half + r % 4
 #pragma unroll
     for (int k = 0; k < D / 32; ++k)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int j = 32 * k + 2 * r + 4 * half;
-            if constexpr (codes) {
-                *reinterpret_cast<float4*>(f.whole + (qrow * a.q.heads + qhead) * D + j) =
+            if (codes || f.parts > 1) {
+                *reinterpret_cast<float4*>(f.whole + (part * all + row_head) * D + j) =
                     make_float4(o[k][r] * inv, o[k][r + 1] * inv, o[k][r + 2] * inv, o[k][r + 3] * inv);
             } else {
                 uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride + j;
                 *reinterpret_cast<uint2*>(p) = make_uint2(kv_pack2<bf>(o[k][r] * inv, o[k][r + 1] * inv), kv_pack2<bf>(o[k][r + 2] * inv, o[k][r + 3] * inv));
             }
         }
-    if (a.lse && half == 0) a.lse[qrow * a.q.heads + qhead] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
+    if (half) return;
+    if (f.parts > 1) *reinterpret_cast<float2*>(f.part_ml + (part * all + row_head) * 2) = make_float2(m, l);
+    else if (a.lse) a.lse[row_head] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
 }
 
 // Queries into the rotated frame: unit rows in float16, a second part with what the first rounds away, and their norms.
-// Eights stand in the order of kv_levels8.  One wavefront takes 16 rows and 32 coordinates (blockIdx.y).
+// Eights stand in the order of kv_levels8.  A wavefront takes 32 coordinates (blockIdx.y) of `tiles` times 16 rows: few
+// rows are spread over many wavefronts (a chain of loads is what they cost), many share a block of Pi.
 template <int D>
-__global__ __launch_bounds__(64) void k_kv_rotate_queries(KvRows q, const float* __restrict__ pi, uint16_t* __restrict__ z, float* __restrict__ zn) {
+__global__ __launch_bounds__(64) void k_kv_rotate_queries(KvRows q, const float* __restrict__ pi, uint16_t* __restrict__ z, float* __restrict__ zn, int tiles) {
     const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, block = blockIdx.y;
-    const int64_t i = (int64_t)blockIdx.x * 16 + n, all = (int64_t)q.rows * q.heads;
-    const bool in = i < all;
-    const int64_t row = in ? i / q.heads : 0, head = in ? i % q.heads : 0;
-    const uint16_t* p = reinterpret_cast<const uint16_t*>(q.data) + row * q.row_stride + head * q.head_stride + 8 * g;
-    float x[D / 32][8], y[1][8];
+    const int64_t all = (int64_t)q.rows * q.heads;
+    const KvTurn<D, false> turn(pi, block);
+    for (int64_t tile = (int64_t)blockIdx.x * tiles; tile < ((int64_t)blockIdx.x + 1) * tiles && tile * 16 < all; ++tile) {
+        const int64_t i = tile * 16 + n;
+        const bool in = i < all;
+        const int64_t row = in ? i / q.heads : 0, head = in ? i % q.heads : 0;
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(q.data) + row * q.row_stride + head * q.head_stride + 8 * g;
+        float x[D / 32][8], y[8];
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-        const uintx4 w = *reinterpret_cast<const uintx4*>(p + 32 * s);
+        for (int s = 0; s < D / 32; ++s) {
+            const uintx4 w = *reinterpret_cast<const uintx4*>(p + 32 * s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t bits = w[e >> 1] >> 16 * (e & 1) & 0xffff;
+                x[s][e] = q.type == IVFTQ_KV_BF16 ? kv_to_float<true>(bits) : kv_to_float<false>(bits);
+            }
+        }
+        const float norm = kv_unit_row<D>(x);
+        turn(x, y);
+        if (!in) continue;
+        if (g == 0 && block == 0) zn[i] = norm;
+        halfx8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t bits = w[e >> 1] >> 16 * (e & 1) & 0xffff;
-            x[s][e] = q.type == IVFTQ_KV_BF16 ? kv_to_float<true>(bits) : kv_to_float<false>(bits);
+            const int at = kv_slot(e);
+            const float v = y[e] * kSplitScale;
+            hi[at] = (_Float16)v;
+            lo[at] = (_Float16)(v - (float)hi[at]);
         }
+        *reinterpret_cast<halfx8*>(z + i * D + 32 * block + 8 * g) = hi;
+        *reinterpret_cast<halfx8*>(z + (all + i) * D + 32 * block + 8 * g) = lo;
     }
-    const float norm = kv_unit_row<D>(x);
-    kv_rotate16<D, false>(pi, block, x, y);
-    if (!in) return;
-    if (g == 0 && block == 0) zn[i] = norm;
-    halfx8 hi, lo;
+}
+
+// Parts of a row's result (one for each share of its keys) put together: eight coordinates from j on, divided by the sum of
+// weights; lse where it is asked for.
+template <int D>
+__device__ __forceinline__ void many_join(const ManyArgs& f, int64_t i, int64_t all, int j, float (&x)[8], bool lse) {
+    float top = -INFINITY, l = 0.f;
+    for (int p = 0; p < f.parts; ++p) top = fmaxf(top, f.part_ml[(p * all + i) * 2]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int at = kv_slot(e);
-        const float v = y[0][e] * kSplitScale;
-        hi[at] = (_Float16)v;
-        lo[at] = (_Float16)(v - (float)hi[at]);
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    for (int p = 0; p < f.parts; ++p) {
+        const float2 u = *reinterpret_cast<const float2*>(f.part_ml + (p * all + i) * 2);
+        const float turn = u.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u.x - top);
+        const float4* w = reinterpret_cast<const float4*>(f.whole + (p * all + i) * D + j);
+        const float4 a = w[0], b = w[1];
+        l += u.y * turn;
+        x[0] += a.x * turn; x[1] += a.y * turn; x[2] += a.z * turn; x[3] += a.w * turn;
+        x[4] += b.x * turn; x[5] += b.y * turn; x[6] += b.z * turn; x[7] += b.w * turn;
     }
-    *reinterpret_cast<halfx8*>(z + i * D + 32 * block + 8 * g) = hi;
-    *reinterpret_cast<halfx8*>(z + (all + i) * D + 32 * block + 8 * g) = lo;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    if (lse && f.a.lse) f.a.lse[i] = l > 0.f ? (top + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
+}
+
+// Rows that have a result: of a sequence, and not past max_new.
+__device__ __forceinline__ bool many_has(const KvAttend& a, int64_t row) {
+    if (!a.c.starts) return row < a.c.batch;
+    int lo = 0, hi = a.c.batch;                     // first sequence that begins after the row, minus one
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (kv_int(a.c.starts, mid) <= row) lo = mid; else hi = mid;
+    }
+    int first, count;
+    kv_new_rows(a.c, lo, first, count);
+    return row >= first && row < first + (count < a.max_new ? count : a.max_new);
+}
+
+template <int F, int D>
+__global__ __launch_bounds__(256) void k_kv_many_join(ManyArgs f) {
+    const KvRows& out = f.a.out;
+    const int64_t all = (int64_t)out.rows * out.heads, u = (int64_t)blockIdx.x * 256 + threadIdx.x, i = u / (D / 8);
+    const int j = (int)(u % (D / 8)) * 8;
+    if (i >= all || !many_has(f.a, i / out.heads)) return;
+    float x[8];
+    many_join<D>(f, i, all, j, x, j == 0);
+    constexpr bool bf = F == IVFTQ_KV_BF16;
+    uint16_t* p = reinterpret_cast<uint16_t*>(out.data) + i / out.heads * out.row_stride + i % out.heads * out.head_stride + j;
+    *reinterpret_cast<uintx4*>(p) = uintx4{kv_pack2<bf>(x[0], x[1]), kv_pack2<bf>(x[2], x[3]), kv_pack2<bf>(x[4], x[5]), kv_pack2<bf>(x[6], x[7])};
 }
 
 // Results back into the rows' own frame, split the same way.
 template <int D>
-__global__ __launch_bounds__(64) void k_kv_rotate_back(KvRows out, const float* __restrict__ pi, const float* __restrict__ whole, float unit) {
+__global__ __launch_bounds__(64) void k_kv_rotate_back(ManyArgs f, int tiles) {
+    const KvRows& out = f.a.out;
     const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
-    const int64_t i = (int64_t)blockIdx.x * 16 + n, all = (int64_t)out.rows * out.heads;
-    const bool in = i < all;
-    const float* p = whole + (in ? i : 0) * D + 8 * g;
-    float x[D / 32][8], y[1][8];
+    const int64_t all = (int64_t)out.rows * out.heads;
+    const KvTurn<D, true> turn(f.a.c.rotation, blockIdx.y);
+    for (int64_t tile = (int64_t)blockIdx.x * tiles; tile < ((int64_t)blockIdx.x + 1) * tiles && tile * 16 < all; ++tile) {
+        const int64_t i = tile * 16 + n;
+        const bool in = i < all && many_has(f.a, i / out.heads);
+        float x[D / 32][8], y[8];
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s)
+        for (int s = 0; s < D / 32; ++s) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] = p[32 * s + e];
-    const float norm = kv_unit_row<D>(x) * unit;
-    kv_rotate16<D, true>(pi, blockIdx.y, x, y);
-    if (in) kv_store_turned(out, i / out.heads, i % out.heads, blockIdx.y, y[0], norm);
+            for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
+            if (!in) continue;
+            if (f.parts > 1) {
+                many_join<D>(f, i, all, 32 * s + 8 * g, x[s], s == 0 && g == 0 && blockIdx.y == 0);
+            } else {
+                const float4* w = reinterpret_cast<const float4*>(f.whole + i * D + 32 * s + 8 * g);
+                const float4 a = w[0], b = w[1];
+                x[s][0] = a.x; x[s][1] = a.y; x[s][2] = a.z; x[s][3] = a.w; x[s][4] = b.x; x[s][5] = b.y; x[s][6] = b.z; x[s][7] = b.w;
+            }
+        }
+        const float norm = kv_unit_row<D>(x) * f.a.c.level_unit;
+        turn(x, y);
+        if (in) kv_store_turned(out, i / out.heads, i % out.heads, blockIdx.y, y, norm);
+    }
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -375,16 +449,18 @@ __global__ __launch_bounds__(64) void k_kv_rotate_back(KvRows out, const float* 
 // Sizes of the workspace's parts, as the launch and the caller's question see them.
 struct KvWork {
     int64_t z, zn, whole, part, ml, bytes;
-    int32_t few, col_tiles, split;
+    int32_t few, col_tiles, split, row_tiles, parts;
 };
-KvWork kv_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity);
+KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity);
 
 template <int F, int D>
 hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) {
     uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
-    float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole);
-    const dim3 rot((unsigned)(((int64_t)a.q.rows * a.q.heads + 15) / 16), D / 32);
-    if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, 64, 0, st>>>(a.q, a.c.rotation, z, zn);
+    float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole), *ml = reinterpret_cast<float*>(a.work + w.ml);
+    const int64_t all = (int64_t)a.q.rows * a.q.heads;
+    const int tiles = all >= 16384 ? 8 : 1;              // 16-row tiles a wavefront rotates
+    const dim3 rot((unsigned)((all + 16 * tiles - 1) / (16 * tiles)), D / 32);
+    if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, 64, 0, st>>>(a.q, a.c.rotation, z, zn, tiles);
     const unsigned pairs = (unsigned)(a.c.batch * a.c.heads);
     if (w.few) {
         static ChipFill fill;
@@ -393,16 +469,17 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
             if (hipError_t e = fill.get(reinterpret_cast<const void*>(&k_kv_few<F, D>), 256, 0, &wgs)) return e;
             if (wgs > (unsigned)kFewMaxWgs) wgs = kFewMaxWgs;
         }
-        FewArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), reinterpret_cast<float*>(a.work + w.ml), (int32_t)wgs, w.split};
+        FewArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), ml, (int32_t)wgs, w.split};
         k_kv_few<F, D><<<dim3(w.split ? wgs : pairs, (unsigned)w.col_tiles), 256, 0, st>>>(f);
         if (w.split || F == IVFTQ_KV_CODE4) k_kv_few_join<F, D><<<dim3(pairs, (unsigned)w.col_tiles), 512, 0, st>>>(f);
     } else {
-        const int row_tiles = (int)(((int64_t)a.max_new * a.group + kManyRows - 1) / kManyRows);
-        ManyArgs f{a, z, zn, whole, row_tiles};
+        ManyArgs f{a, z, zn, whole, ml, w.row_tiles, w.parts};
+        const unsigned wgs = pairs * (unsigned)w.row_tiles * (unsigned)w.parts;
         // float16 results: the queries' second part matters beside the rounding of the result
-        if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4><<<pairs * (unsigned)row_tiles, 256, 0, st>>>(f);
-        else k_kv_many<F, D, false><<<pairs * (unsigned)row_tiles, 256, 0, st>>>(f);
-        if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D><<<rot, 64, 0, st>>>(a.out, a.c.rotation, whole, a.c.level_unit);
+        if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4><<<wgs, 256, 0, st>>>(f);
+        else k_kv_many<F, D, false><<<wgs, 256, 0, st>>>(f);
+        if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D><<<rot, 64, 0, st>>>(f, tiles);
+        else if (w.parts > 1) k_kv_many_join<F, D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, st>>>(f);
     }
     return hipGetLastError();
 }

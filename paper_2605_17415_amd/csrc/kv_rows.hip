@@ -217,16 +217,16 @@ __global__ __launch_bounds__(64) void k_kv_append_row_codes(KvView c, KvRows k, 
     const int64_t i = (int64_t)blockIdx.x * 16 + n;
     const bool in = i < (int64_t)c.rows * c.heads;
     const int r = in ? (int)(i / c.heads) : 0, h = in ? (int)(i % c.heads) : 0;
-    float x[D / 32][8], y[1][8];
+    float x[D / 32][8], y[8];
     load_row<D, BF>(value ? v : k, r, h, in, x);
     const float norm = kv_unit_row<D>(x);
-    kv_rotate16<D, false>(c.rotation, block, x, y);
+    KvTurn<D, false>(c.rotation, block)(x, y);
     int t = 0;
     char* rec = in ? place_of(c, r, h, t) : nullptr;
     if (!rec) return;
     const int codes = c.page * (D / 2), j = 32 * block + 8 * g;
     if (g == 0 && block == 0) reinterpret_cast<_Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t] = (_Float16)norm;
-    const uint32_t w = kv_nibbles8(y[0], c);
+    const uint32_t w = kv_nibbles8(y, c);
     if (!value) {
         reinterpret_cast<uint32_t*>(rec + (int64_t)t * (D / 2))[j / 8] = w;
     } else {
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, Kv
     int t = 0;
     const char* rec = in ? place_of(c, r, h, t) : nullptr;
     const int codes = c.page * (D / 2);
-    float x[D / 32][8], y[1][8], norm = 0.f;
+    float x[D / 32][8], y[8], norm = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
         const int j = 32 * s + 8 * g;
@@ -266,16 +266,9 @@ __global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, Kv
         for (int e = 0; e < 8; ++e) x[s][e] = kv_level(w >> 4 * e & 15, c);
     }
     if (rec) norm = (float)reinterpret_cast<const _Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t];
-    kv_rotate16<D, true>(c.rotation, block, x, y);
+    KvTurn<D, true>(c.rotation, block)(x, y);
     if (!in) return;
-    const KvRows& o = value ? v : k;
-    uint16_t* out = reinterpret_cast<uint16_t*>(o.data) + r * o.row_stride + h * o.head_stride + 32 * block + 4 * g;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        uint2 w = make_uint2(0, 0);
-        if (rec) w = make_uint2(kv_pack2<BF>(y[0][4 * half] * norm, y[0][4 * half + 1] * norm), kv_pack2<BF>(y[0][4 * half + 2] * norm, y[0][4 * half + 3] * norm));
-        *reinterpret_cast<uint2*>(out + 16 * half) = w;
-    }
+    kv_store_turned(value ? v : k, r, h, block, y, norm);
 }
 
 // 8 x 8 half bytes over eight neighbouring lanes, turned: lane i's half byte e becomes lane e's half byte i.

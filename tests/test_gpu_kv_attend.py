@@ -162,6 +162,45 @@ def test_long_sequences_in_many_shares(form, kind):
     assert torch.equal(out, again)                          # no order of atomics in it
 
 
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 32), (128, 64), (256, 16)])
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (900, 5)])
+def test_a_chunk_after_a_long_beginning(form, kind, d, page, window, sinks):
+    """Many new rows whose keys are shared out over several workgroups, next to a sequence without any and to a short one."""
+    lens, news = [2300, 70, 9, 1500], [70, 66, 0, 40]
+    c = ref.Cache(d, form, 1, d, page, lens)
+    q = queries(d, sum(news), 2, d, ref.TYPES[kind])
+    out, lse = run(c, q, news, window=window, sinks=sinks)
+    ref.check_attention(c, q.cpu(), out, news, lse=lse, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("lens", ([40, 0, 5], [1800, 700]))
+def test_more_heads_than_few_rows(form, kind, lens):
+    """One token of a group of 72 heads: the kernel of many rows, without starts."""
+    c = ref.Cache(14, form, 1, 64, 16, lens)
+    q = queries(14, len(lens), 72, 64, ref.TYPES[kind])
+    out, lse = run(c, q)
+    ref.check_attention(c, q.cpu(), out, [1] * len(lens), lse=lse)
+
+
+@pytest.mark.parametrize("form", ("bf16", "code4"))
+def test_rows_without_a_result(form):
+    """Rows past max_new and rows of no sequence get none; the others' results do not change."""
+    lens, news = [1200, 90], [100, 90]
+    c = ref.Cache(15, form, 1, 64, 16, lens)
+    q = queries(15, sum(news) + 6, 2, 64, torch.bfloat16)
+    t, codec = c.device()
+    starts = starts_of(news) + 3                            # rows 0 .. 2 and the last three belong to nobody
+    want = _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], starts=starts, max_new=100, **codec)
+    ref.check_attention(c, q[3:-3].cpu(), want[3:-3], news)
+    out = torch.full_like(q, 3.0)
+    _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], starts=starts, max_new=95, out=out, **codec)
+    torch.cuda.synchronize()
+    assert torch.equal(out[3:98], want[3:98]) and torch.equal(out[103:-3], want[103:-3])
+    assert (out[:3] == 3).all() and (out[98:103] == 3).all() and (out[-3:] == 3).all()
+
+
 def test_many_sequences():
     """More sequences than lanes: shares are found by scans over them."""
     lens = [int(x) for x in np.random.default_rng(0).integers(0, 200, 150)] + [900]
