@@ -74,6 +74,16 @@ __device__ __forceinline__ int kv_wave() { return __builtin_amdgcn_readfirstlane
 typedef const __attribute__((address_space(4))) int32_t* KvInts;
 __device__ __forceinline__ int32_t kv_int(const int32_t* p, int64_t i) { return ((KvInts)(uintptr_t)p)[i]; }
 
+// 16 bytes a lane from memory to LDS, without registers: lane l's go to `to` + 16 l (the same `to` in every lane).
+__device__ __forceinline__ void kv_load_lds16(const char* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+// Before the barrier behind which others read what this wavefront has loaded.
+__device__ __forceinline__ void kv_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A value that is computed here and not further down, where it is used.
+__device__ __forceinline__ uint32_t kv_here(uint32_t v) { asm volatile("" : "+v"(v)); return v; }
+
 // ---- sequences and pages -------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int kv_length(const KvView& c, int b) {
@@ -271,6 +281,26 @@ struct KvTurn {
                 acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[half][s], h, acc[half], 0, 0, 0);
             }
         }
+        finish(acc, y);
+    }
+    // Rows that stand in LDS as two parts already (rows.hi[block][lane], rows.lo).
+    template <class Rows>
+    __device__ __forceinline__ void operator()(const Rows& rows, float (&y)[8]) const {
+        const int lane = threadIdx.x & 63;
+        floatx4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            const halfx8 h = rows.hi[s][lane], l = rows.lo[s][lane];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], h, acc[half], 0, 0, 0);
+                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], l, acc[half], 0, 0, 0);
+                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[half][s], h, acc[half], 0, 0, 0);
+            }
+        }
+        finish(acc, y);
+    }
+    __device__ __forceinline__ void finish(const floatx4 (&acc)[2], float (&y)[8]) const {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll

@@ -6,8 +6,8 @@
 // tokens, staged in LDS (16-bit pages are copied, codes become float16 levels on the way).  As in kv_few.h the products
 // are transposed, S^T = K Q^T and O^T = V^T P^T (v_mfma 32x32x16), and the token order of the key operand is chosen so
 // that the scores a lane gets are those it puts into the second product: nothing goes through LDS but keys and values.
-// Two workgroups a compute unit, which are not in step, so that one's exponentials run beside the other's products; each
-// loads a tile into registers two steps before it is used and stores it to the second LDS buffer one step before.
+// Two workgroups a compute unit, which are not in step; inside a wavefront the products of one half tile stand between the
+// exponentials of another.
 #pragma once
 #include <type_traits>
 
@@ -19,6 +19,7 @@ typedef float floatx16_ __attribute__((ext_vector_type(16)));
 
 constexpr int kManyRows = 128;        // query rows of a workgroup
 constexpr int kManyTile = 64;         // tokens of a step
+constexpr int kTurnTiles = 8;         // tiles of 16 rows that a workgroup rotates where there are many
 
 struct ManyArgs {
     KvAttend a;
@@ -56,41 +57,83 @@ __device__ __forceinline__ ManySpan many_span(const KvAttend& a, int pos0, int p
     return s;
 }
 
-// One wavefront's quarter of a tile on its way to LDS: 16 tokens, which lie in one page.
+// A tile in LDS.  Keys: rows of kRow 16-byte chunks, chunk w of token t in place w ^ turn(t), so that sixteen lanes that read one
+// chunk of sixteen tokens use all banks; values: groups of eight tokens as they stand in a page; codes: the norms behind.
+// A wavefront brings a quarter, 16 tokens, which lie in one page: 16 bits by loads that go to LDS directly (64 lanes write 1 KB
+// in order, which is why keys are turned by choosing what a lane reads), codes through registers, where they become levels.
+template <int F, int D>
+struct ManyTile {
+    static constexpr bool kCodes = F == IVFTQ_KV_CODE4;
+    static constexpr int kRow = D <= 64 ? 8 : (D <= 128 ? 16 : 32);
+    static constexpr int kKeyBytes = kManyTile * kRow * 16, kValueBytes = kManyTile * D * 2;
+    char keys[2][kKeyBytes];
+    char values[2][kValueBytes];
+    float key_gain[kCodes ? 2 : 1][kCodes ? kManyTile : 1], value_gain[kCodes ? 2 : 1][kCodes ? kManyTile : 1];
+    uint32_t odd[2][2];
+
+    static __device__ __forceinline__ int turn(int t) { return kRow == 8 ? t >> 1 & 7 : t & 15; }
+};
+
 template <int F, int D>
 struct ManyStage {
+    using Tile = ManyTile<F, D>;
     static constexpr bool kCodes = F == IVFTQ_KV_CODE4;
-    static constexpr int kKeyPitch = D * 2 + 16;                // bytes of a key row in LDS: rows 4 banks apart
-    static constexpr int kKeyBytes = kManyTile * kKeyPitch, kBytes = kKeyBytes + kManyTile * D * 2 + (kCodes ? kManyTile * 8 : 0);
-    using W = typename std::conditional<kCodes, uint32_t, uintx4>::type;      // eight coordinates of a key, eight tokens of a value
-    W k[D / 32], v[D / 32];
-    uint32_t norm;
+    uint32_t k[kCodes ? D / 32 : 1], v[kCodes ? D / 32 : 1];      // eight coordinates of a key, eight tokens of a value
+    uint32_t key_norm, value_norm;
 
-    __device__ __forceinline__ void load(const KvView& c, int h, int64_t page, int t) {
-        const int lane = threadIdx.x & 63, in = t & (c.page - 1);
-        const char* rec = kv_record(c, page < 0 ? 0 : page, h);
-        const int row = kCodes ? D / 2 : D * 2;
-        const W* x = reinterpret_cast<const W*>(rec + in * row);
-        const W* y = reinterpret_cast<const W*>(rec + c.page * row + in * row);
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) { k[j] = x[lane + 64 * j]; v[j] = y[lane + 64 * j]; }
-        if constexpr (kCodes)
-            norm = reinterpret_cast<const uint16_t*>(rec + 2 * c.page * row)[(lane & 16 ? c.page : 0) + in + (lane & 15)];
-    }
-    // quarter: of the tile; a key chunk of eight coordinates goes to its row, a value chunk of eight tokens stays in order
-    __device__ __forceinline__ void store(const KvView& c, char* to, int quarter) const {
+    // keys (values) of a tile's quarter, which begins with token `in` of record `rec`, to buffer `to` of LDS
+    __device__ __forceinline__ void bring_keys(const KvView& c, const char* rec, int in, Tile& lds, int to, int quarter) {
         const int lane = threadIdx.x & 63;
+        if constexpr (kCodes) {
+            const uint32_t* x = reinterpret_cast<const uint32_t*>(rec + in * (D / 2));
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-            const int u = lane + 64 * j, t = 16 * quarter + u / (D / 8), w = u % (D / 8);
-            uintx4 x, y;
-            if constexpr (kCodes) { x = __builtin_bit_cast(uintx4, kv_levels8(k[j], c)); y = __builtin_bit_cast(uintx4, kv_levels8(v[j], c)); }
-            else { x = k[j]; y = v[j]; }
-            *reinterpret_cast<uintx4*>(to + t * kKeyPitch + w * 16) = x;
-            *reinterpret_cast<uintx4*>(to + kKeyBytes + (quarter * 2 * D + u) * 16) = y;
+            for (int j = 0; j < D / 32; ++j) k[j] = x[lane + 64 * j];
+            key_norm = reinterpret_cast<const uint16_t*>(rec + c.page * D)[in + (lane & 15)];
+        } else {
+            // lane's place in the first 64 chunks; the next 64 are kRows rows on, where chunks are turned by a further xor
+            constexpr int kRows = 64 / Tile::kRow, kTurn = Tile::kRow == 8 ? kRows / 2 : kRows;
+            const char* from = rec + in * (D * 2);
+            const uint32_t row = lane / Tile::kRow, chunk = (lane % Tile::kRow) ^ (Tile::kRow == 8 ? row / 2 : row);
+#pragma unroll
+            for (int j = 0; j < Tile::kRow / 4; ++j) {
+                uint32_t w = chunk ^ (kTurn * j);
+                if (D / 8 < Tile::kRow) w = w < D / 8 ? w : 0;                       // rows of 96 and 192: chunks that nobody reads
+                kv_load_lds16(from + (row * (D * 2) + w * 16 + j * kRows * D * 2), lds.keys[to] + (quarter * 16 * Tile::kRow + 64 * j) * 16);
+            }
         }
-        if (kCodes && lane < 32)
-            reinterpret_cast<float*>(to + kKeyBytes + kManyTile * D * 2)[(lane & 16) * 4 + 16 * quarter + (lane & 15)] = (float)__builtin_bit_cast(_Float16, (uint16_t)norm);
+    }
+    __device__ __forceinline__ void bring_values(const KvView& c, const char* rec, int in, Tile& lds, int to, int quarter) {
+        const int lane = threadIdx.x & 63;
+        if constexpr (kCodes) {
+            const uint32_t* x = reinterpret_cast<const uint32_t*>(rec + (c.page + in) * (D / 2));
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) v[j] = x[lane + 64 * j];
+            value_norm = reinterpret_cast<const uint16_t*>(rec + c.page * D)[c.page + in + (lane & 15)];
+        } else {
+            const char* from = rec + (c.page + in) * (D * 2);
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) kv_load_lds16(from + (uint32_t)(lane * 16 + j * 1024), lds.values[to] + (quarter * 2 * D + 64 * j) * 16);
+        }
+    }
+    // codes: what has been brought, into LDS
+    __device__ __forceinline__ void store_keys(const KvView& c, Tile& lds, int to, int quarter) const {
+        if constexpr (kCodes) {
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                const int u = lane + 64 * j, row = u / (D / 8), w = u % (D / 8);
+                *reinterpret_cast<halfx8*>(lds.keys[to] + ((16 * quarter + row) * Tile::kRow + (w ^ Tile::turn(row))) * 16) = kv_levels8(k[j], c);
+            }
+            if (lane < 16) lds.key_gain[to][16 * quarter + lane] = (float)__builtin_bit_cast(_Float16, (uint16_t)key_norm);
+        }
+    }
+    __device__ __forceinline__ void store_values(const KvView& c, Tile& lds, int to, int quarter) const {
+        if constexpr (kCodes) {
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) *reinterpret_cast<halfx8*>(lds.values[to] + (quarter * 2 * D + lane + 64 * j) * 16) = kv_levels8(v[j], c);
+            if (lane < 16) lds.value_gain[to][16 * quarter + lane] = (float)__builtin_bit_cast(_Float16, (uint16_t)value_norm);
+        }
     }
 };
 
@@ -99,10 +142,11 @@ __device__ __forceinline__ uint64_t many_below(int64_t n) { return n <= 0 ? 0 : 
 
 template <int F, int D, bool LOW>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
-    using Stage = ManyStage<F, D>;
+    using Tile = ManyTile<F, D>;
+    constexpr int kSteps = D / 16;               // matrix instructions of a half tile's scores, and of its values
+    constexpr int kLead = 3;                     // operands that are read ahead
     constexpr bool codes = F == IVFTQ_KV_CODE4, bf = F == IVFTQ_KV_BF16;
-    __shared__ __align__(16) char lds[2][Stage::kBytes];
-    __shared__ uint32_t odd[2];
+    __shared__ __align__(1024) Tile lds;
     const KvAttend& a = f.a;
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
@@ -151,99 +195,85 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     // the token (of 32) that this lane's operand row stands for
     const int tok = 16 * (n >> 4) + 8 * (n >> 2 & 1) + 4 * (n >> 3 & 1) + (n & 3);
 
-    Stage stage;
-    auto page_of = [&](int i) { return i < to ? kv_page(c, b, span.first_token(i) + 16 * wave) : -1; };
-    auto load = [&](int i, int64_t page) { if (i < to) stage.load(c, h, page, span.first_token(i) + 16 * wave); };
-    int64_t ahead = page_of(from);
-    load(from, ahead);
-    ahead = page_of(from + 1);
-    if (from < to) stage.store(c, lds[0], wave);
-    load(from + 1, ahead);
-    ahead = page_of(from + 2);
-    __syncthreads();
-
-    for (int i = from; i < to; ++i) {
-        const char* keys = lds[(i - from) & 1];
-        const char* vals = keys + Stage::kKeyBytes;
-        const float* gains = reinterpret_cast<const float*>(vals + kManyTile * D * 2);
-        const int t0 = span.first_token(i);
-        if (i + 1 < to) stage.store(c, lds[(i - from + 1) & 1], wave);
-        load(i + 2, ahead);
-        ahead = page_of(i + 3);
-
-        floatx16_ st[2];
+    ManyStage<F, D> stage;
+    // What is known of a tile ahead of its turn: its first token, the record with this wavefront's quarter, quarters without a page.
+    struct Ahead { int t; const char* rec; uint32_t absent; };
+    const int32_t* const row = c.table + (int64_t)b * c.table_stride;
+    const char* const head = c.pool + (int64_t)h * c.head_bytes;
+    const int32_t pages = (int32_t)c.pages;
+    // lane u % 4 asks for the page of quarter u % 4; the answer is taken up one tile later
+    auto ask = [&](int i) __attribute__((always_inline)) {
+        const int col = (span.first_token(i < to ? i : from) + 16 * (lane & 3)) >> c.page_log2;
+        return col < c.columns ? row[col] : -1;
+    };
+    auto answer = [&](int i, int32_t id) __attribute__((always_inline)) {
+        const bool none = (uint32_t)id >= (uint32_t)pages;
+        const int32_t mine = __builtin_amdgcn_readlane(none ? 0 : id, wave);
+        return Ahead{span.first_token(i < to ? i : from), head + (int64_t)mine * c.page_bytes, (uint32_t)__ballot(none) & 15u};
+    };
+    auto bring_keys = [&](int i, const Ahead& at, int buffer) __attribute__((always_inline)) {
+        if (i < to) stage.bring_keys(c, at.rec, (at.t + 16 * wave) & (c.page - 1), lds, buffer, wave);
+    };
+    auto bring_values = [&](int i, const Ahead& at, int buffer) __attribute__((always_inline)) {
+        if (i < to) stage.bring_values(c, at.rec, (at.t + 16 * wave) & (c.page - 1), lds, buffer, wave);
+    };
+    // S^T of tokens 32 x .. of a tile; register r: token 32 x + 16 (r / 8) + 8 half + r % 8
+    const int key_at = tok * (Tile::kRow * 16) + ((half ^ Tile::turn(tok)) << 4);
+    auto key_chunk = [&](int buffer, int x, int k) __attribute__((always_inline)) {
+        return *reinterpret_cast<const uintx4*>(lds.keys[buffer] + 32 * x * (Tile::kRow * 16) + (key_at ^ (k << 5)));
+    };
+    auto value_chunk = [&](int buffer, int x, int j) __attribute__((always_inline)) {       // j: (16 tokens, block of 32 coordinates)
+        return *reinterpret_cast<const uintx4*>(lds.values[buffer] + ((4 * x + 2 * (j / (D / 32)) + half) * D + 32 * (j % (D / 32)) + n) * 16);
+    };
+    auto score = [&](const uintx4& w, int k, floatx16_& st) __attribute__((always_inline)) {
+        st = kv_mfma32<F>(w, q[k], st);
+        if constexpr (LOW) st = kv_mfma32<F>(w, ql[k], st);
+    };
+    auto scores = [&](int buffer, int x, floatx16_& st) __attribute__((always_inline)) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int r = 0; r < 16; ++r) st[r] = 0.f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) st[x][r] = 0.f;
-            const char* p = keys + (32 * x + tok) * Stage::kKeyPitch + 16 * half;
+        for (int k = 0; k < kSteps; ++k) score(key_chunk(buffer, x, k), k, st);
+    };
+    auto product = [&](int buffer, int x, const uintx4 (&p)[2]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uintx4 w = *reinterpret_cast<const uintx4*>(p + 32 * k);
-                st[x] = kv_mfma32<F>(w, q[k], st[x]);
-                if constexpr (LOW) st[x] = kv_mfma32<F>(w, ql[k], st[x]);
-            }
-        }
-        // register r of st[x]: token 32 x + 16 (r / 8) + 8 half + r % 8
+        for (int j = 0; j < kSteps; ++j) o[j % (D / 32)] = kv_mfma32<F>(value_chunk(buffer, x, j), p[j / (D / 32)], o[j % (D / 32)]);
+    };
+    // Each matrix instruction is followed by the vector instructions of a part of the sixteen scores, and the LDS read of the
+    // one kLead further on stands before it; the compiler may not move anything from one such group to another (left alone it puts the
+    // matrix instructions first, and the wavefront stands still behind them).
+    //
+    // O^T += V^T P^T of tokens 32 x .. of buffer `from`; the maximum of the scores st of half `y` of buffer `at` (codes: times the
+    // keys' norms; mine: the tokens that this lane's row sees, a bit each, from this lane's half on).
+    auto product_and_maximum = [&](int from, int x, const uintx4 (&p)[2], int at, int y, bool full, uint32_t mine, floatx16_& st) __attribute__((always_inline)) {
+        uintx4 w[kSteps];
+#pragma unroll
+        for (int j = 0; j < kLead; ++j) w[j] = value_chunk(from, x, j);
+        float gains[16];
         if constexpr (codes) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) st[x][r] *= gains[32 * x + 16 * (r >> 3) + 8 * half + (r & 7)];
+            for (int r = 0; r < 16; ++r) gains[r] = lds.key_gain[at][32 * y + 8 * half + 16 * (r >> 3) + (r & 7)];
         }
-        uint32_t absent = 0;                        // quarters of 16 tokens whose page is missing
+        if (!full) {                                // (a norm that is no number: the product comes before the mask)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) absent |= kv_page(c, b, t0 + 16 * u) < 0 ? 1u << u : 0u;
-        const bool full = !absent && t0 + kManyTile - 1 <= pos0 &&
-                          (!a.window || (int64_t)t0 > (int64_t)pos1 - a.window || t0 + kManyTile <= a.sinks);
-        uint64_t dirty = 0;                         // tokens with a value that is no finite number, seen by some rows and not by others
-        if (!full) {
-            uint64_t none = 0;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) none |= absent >> u & 1 ? 0xffffull << 16 * u : 0;
-            const uint64_t sinks = many_below(a.sinks - (int64_t)t0);
-            const uint64_t mine = (many_below((int64_t)pos - t0 + 1) & ~none & (a.window ? ~many_below((int64_t)pos - a.window + 1 - t0) | sinks : ~0ull)) >> 8 * half;
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!(mine >> (32 * x + 16 * (r >> 3) + (r & 7)) & 1)) st[x][r] = -INFINITY;
-            // What no row of the workgroup sees may be anything, and 0 * NaN is no zero: such values are set to zero in LDS.  So are
-            // values of no finite number that only some rows see; those rows get them one by one below.
-            if constexpr (!codes) {
-                const uint64_t shown = many_below((int64_t)span.end - t0) & ~none & (~many_below((int64_t)span.low - t0) | sinks);
-                if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-                __syncthreads();
-#pragma unroll
-                for (int j = 0; j < D / 32; ++j) {
-                    const int u = threadIdx.x + 256 * j;
-                    const uint32_t bad = kv_not_finite<bf>(*reinterpret_cast<const uintx4*>(vals + u * 16)) << 8 * (u / D & 3);
-                    if (bad) atomicOr(odd + u / D / 4, bad);
-                }
-                __syncthreads();
-                const uint64_t found = (uint64_t)(uint32_t)kv_uniform((int)odd[0]) | (uint64_t)(uint32_t)kv_uniform((int)odd[1]) << 32;
-                dirty = found & shown;
-                const uint64_t keep = shown & ~found;
-                if (~keep) {
-#pragma unroll
-                    for (int j = 0; j < D / 32; ++j) {
-                        const int u = threadIdx.x + 256 * j;
-                        const uint32_t bits = (uint32_t)(keep >> 8 * (u / D));
-                        uintx4* p = reinterpret_cast<uintx4*>(const_cast<char*>(vals) + u * 16);
-                        uintx4 w = *p;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] &= (bits >> 2 * e & 1 ? 0xffffu : 0u) | (bits >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
-                        *p = w;
-                    }
-                }
-                __syncthreads();
+            for (int r = 0; r < 16; ++r) {
+                if constexpr (codes) { st[r] *= gains[r]; gains[r] = 1.f; }
+                st[r] = mine >> (16 * (r >> 3) + (r & 7)) & 1 ? st[r] : -INFINITY;
             }
         }
-        float top = st[0][0];
+        float top = -INFINITY;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int j = 0; j < kSteps; ++j) {
+            if (j + kLead < kSteps) w[j + kLead] = value_chunk(from, x, j + kLead);
+            o[j % (D / 32)] = kv_mfma32<F>(w[j], p[j / (D / 32)], o[j % (D / 32)]);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, st[x][r]);
+            for (int r = 16 * j / kSteps; r < 16 * (j + 1) / kSteps; ++r) {
+                if constexpr (codes) st[r] *= gains[r];
+                top = fmaxf(top, st[r]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
         top = kv_max32(top) * gain;
         // 16 bits: a row's maximum may lag by 2^8, weights of up to 256 lose nothing; with codes they meet the norms in float16
         const bool grows = top > m + (codes || m == -INFINITY ? 0.f : 8.f);
@@ -254,44 +284,55 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) o[k] *= turn;
         }
+    };
+    // S^T of tokens 32 x .. of buffer `from` into `next`; the weights of the scores st of half `y` of buffer `at`.
+    auto scores_and_weights = [&](int from, int x, floatx16_& next, int at, int y, bool full, uint32_t mine, const floatx16_& st, uintx4 (&p)[2]) __attribute__((always_inline)) {
+        uintx4 w[kSteps];
+#pragma unroll
+        for (int k = 0; k < kLead; ++k) w[k] = key_chunk(from, x, k);
         const float less = m == -INFINITY ? 0.f : m;              // a row that has seen nothing: every score is -infinity
+        float gains[16], pr[16];
+        if constexpr (codes) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+            for (int r = 0; r < 16; ++r) gains[r] = lds.value_gain[at][32 * y + 8 * half + 16 * (r >> 3) + (r & 7)];
+            if (!full) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {           // 16 tokens: this lane's half of them in registers 8 u ..
-                float pr[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    pr[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[x][8 * u + e], gain, -less));
-                    l += pr[e];
-                }
-                const int og = 4 * x + 2 * u + half;             // group of eight tokens in the tile
-                uintx4 p;
-                if constexpr (codes) {
-                    float w[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = pr[e] * gains[kManyTile + 8 * og + e];
-                    if (!full) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = st[x][8 * u + e] == -INFINITY ? 0.f : w[e];
-                    }
-                    p = uintx4{kv_pack2<bf>(w[0], w[2]), kv_pack2<bf>(w[4], w[6]), kv_pack2<bf>(w[1], w[3]), kv_pack2<bf>(w[5], w[7])};
-                } else {
-                    p = uintx4{kv_pack2<bf>(pr[0], pr[1]), kv_pack2<bf>(pr[2], pr[3]), kv_pack2<bf>(pr[4], pr[5]), kv_pack2<bf>(pr[6], pr[7])};
-                }
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) o[k] = kv_mfma32<F>(*reinterpret_cast<const uintx4*>(vals + (og * D + 32 * k + n) * 16), p, o[k]);
+                for (int r = 0; r < 16; ++r) gains[r] = mine >> (16 * (r >> 3) + (r & 7)) & 1 ? gains[r] : 0.f;
             }
-        for (uint64_t left = dirty; left; left &= left - 1) {           // such tokens one by one, for the rows that see them
-            const int t = __builtin_ctzll(left);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) next[r] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            if (k + kLead < kSteps) w[k + kLead] = key_chunk(from, x, k + kLead);
+            score(w[k], k, next);
+#pragma unroll
+            for (int r = 16 * k / kSteps; r < 16 * (k + 1) / kSteps; ++r) {
+                pr[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r], gain, -less));
+                l += pr[r];
+                const int e = r & 7, u = r >> 3;
+                if constexpr (codes) {                            // in the order of kv_levels8
+                    pr[r] *= gains[r];
+                    if (e & 2) p[u][(e & 1) * 2 + (e >> 2)] = kv_here(kv_pack2<false>(pr[r - 2], pr[r]));
+                } else if (e & 1) {
+                    p[u][e >> 1] = kv_here(kv_pack2<bf>(pr[r - 1], pr[r]));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // Values that are no finite numbers, of tokens that some rows see and others do not: for the rows that see them, one by one.
+    auto singly = [&](int t0, int x, uint32_t dirty, const floatx16_& st) __attribute__((always_inline)) {
+        const float less = m == -INFINITY ? 0.f : m;
+        for (uint32_t left = dirty; left; left &= left - 1) {
+            const int t = __builtin_ctz(left);
             float v = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) v = 32 * x + 16 * (r >> 3) + (r & 7) == (t & ~8) ? st[x][r] : v;
+            for (int r = 0; r < 16; ++r) v = 16 * (r >> 3) + (r & 7) == (t & ~8) ? st[r] : v;
             v = __shfl(v, n + 32 * (t >> 3 & 1));
-            const int64_t page = kv_page(c, b, t0 + t);
-            const int in = (t0 + t) & (c.page - 1);
+            const int64_t page = kv_page(c, b, t0 + 32 * x + t);
+            const int in = (t0 + 32 * x + t) & (c.page - 1);
             const uint16_t* y = reinterpret_cast<const uint16_t*>(kv_record(c, page < 0 ? 0 : page, h) + c.page * (D * 2)) + (in >> 3) * D * 8 + (in & 7);
             if (v == -INFINITY) continue;
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(v, gain, -less));
@@ -300,8 +341,102 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[k][r] += w * kv_to_float<bf>(y[(32 * k + 8 * (r >> 2) + 4 * half + (r & 3)) * 8]);
         }
+    };
+
+    // The order of things: keys of tile i + 1 and values of tile i are there when tile i's second half begins, half way through
+    // tile i (one barrier a tile); what the buffers are then free for, keys of tile i + 2 and values of tile i + 1, is on its
+    // way from there on.
+    Ahead now = answer(from, ask(from)), next = answer(from + 1, ask(from + 1));
+    bring_keys(from, now, 0);
+    if constexpr (codes) { if (from < to) stage.store_keys(c, lds, 0, wave); }
+    bring_keys(from + 1, next, 1);
+    bring_values(from, now, 0);
+    int32_t asked = ask(from + 2);
+    if (threadIdx.x < 4) lds.odd[threadIdx.x >> 1][threadIdx.x & 1] = 0;
+    // the first tile's step begins with the product of weights of zero and the other buffer's values: those have to be numbers
+    for (int u = threadIdx.x; u < kManyTile * D / 8; u += 256) *reinterpret_cast<uintx4*>(lds.values[1] + u * 16) = uintx4{0, 0, 0, 0};
+    kv_loads_done();
+    __syncthreads();
+    floatx16_ s0, s1;
+    uintx4 p0[2], p1[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (from < to) scores(0, 0, s0);
+
+    // A tile.  While a half tile's scores become weights (vector unit), the weights of the half before meet their values and the
+    // next half's scores are made (matrix cores): no product waits for the weights beside it.
+    const int beyond = a.window && (int64_t)pos1 - a.window > 0 ? (int)((int64_t)pos1 - a.window) : -1;       // tokens up to this one are not in every row's window
+    auto step = [&](int i, auto buffer) __attribute__((always_inline)) {
+        constexpr int here = decltype(buffer)::value, other = here ^ 1;
+        const int t0 = now.t;
+        const uint32_t absent = now.absent;
+        const bool full = !absent && t0 + kManyTile - 1 <= pos0 && (t0 > beyond || t0 + kManyTile <= a.sinks);       // every row sees every token
+        const Ahead then = answer(i + 2, asked);
+        asked = ask(i + 3);
+        uint64_t mine = ~0ull;
+        [[maybe_unused]] uint64_t shown = ~0ull, dirty = 0;
+        if constexpr (codes) {
+            if (i + 1 < to) stage.store_keys(c, lds, other, wave);
+            stage.store_values(c, lds, here, wave);
+            bring_keys(i + 2, then, here);
+            bring_values(i + 1, next, other);
+        }
+        if (!full) {
+            uint64_t none = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) none |= absent >> u & 1 ? 0xffffull << 16 * u : 0;
+            const uint64_t sinks = many_below(a.sinks - (int64_t)t0);
+            mine = (many_below((int64_t)pos - t0 + 1) & ~none & (a.window ? ~many_below((int64_t)pos - a.window + 1 - t0) | sinks : ~0ull)) >> 8 * half;
+            shown = many_below((int64_t)span.end - t0) & ~none & (~many_below((int64_t)span.low - t0) | sinks);
+        }
+        product_and_maximum(other, 1, p1, here, 0, full, (uint32_t)mine, s0);
+        scores_and_weights(here, 1, s1, here, 0, full, (uint32_t)mine, s0, p0);
+        kv_loads_done();
         __syncthreads();
+        if (!codes && !full) {
+            // What no row of the workgroup sees may be anything, and 0 * NaN is no zero: such values are set to zero in LDS.  So are
+            // values of no finite number that only some rows see; those rows get them one by one.
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                const int u = threadIdx.x + 256 * j;
+                const uint32_t bad = kv_not_finite<bf>(*reinterpret_cast<const uintx4*>(lds.values[here] + u * 16)) << 8 * (u / D & 3);
+                if (bad) atomicOr(&lds.odd[here][u / D / 4], bad);
+            }
+            __syncthreads();
+            const uint64_t found = (uint64_t)(uint32_t)kv_uniform((int)lds.odd[here][0]) | (uint64_t)(uint32_t)kv_uniform((int)lds.odd[here][1]) << 32;
+            dirty = found & shown;
+            const uint64_t keep = shown & ~found;
+            if (~keep) {
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) {
+                    const int u = threadIdx.x + 256 * j;
+                    const uint32_t bits = (uint32_t)(keep >> 8 * (u / D));
+                    uintx4* p = reinterpret_cast<uintx4*>(lds.values[here] + u * 16);
+                    uintx4 w = *p;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] &= (bits >> 2 * e & 1 ? 0xffffu : 0u) | (bits >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+                    *p = w;
+                }
+            }
+            if (threadIdx.x < 2) lds.odd[other][threadIdx.x] = 0;
+            __syncthreads();
+            if ((uint32_t)dirty) singly(t0, 0, (uint32_t)dirty, s0);
+        }
+        if constexpr (!codes) {
+            bring_keys(i + 2, then, here);
+            bring_values(i + 1, next, other);
+        }
+        now = next;
+        next = then;
+        product_and_maximum(here, 0, p0, here, 1, full, (uint32_t)(mine >> 32), s1);
+        scores_and_weights(other, 0, s0, here, 1, full, (uint32_t)(mine >> 32), s1, p1);       // past the last tile: of what LDS holds, not used
+        if constexpr (!codes) {
+            if (dirty >> 32) singly(t0, 1, (uint32_t)(dirty >> 32), s1);
+        }
+    };
+    for (int i = from; i < to; i += 2) {
+        step(i, std::integral_constant<int, 0>{});
+        if (i + 1 < to) step(i + 1, std::integral_constant<int, 1>{});
     }
+    if (from < to) product((to - from - 1) & 1, 1, p1);
     l = kv_sum32(l);
     if (col >= cols) return;
     const float inv = f.parts > 1 ? 1.f : (l == 0.f ? 0.f : 1.f / l);
@@ -325,33 +460,64 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     else if (a.lse) a.lse[row_head] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
 }
 
-// Queries into the rotated frame: unit rows in float16, a second part with what the first rounds away, and their norms.
-// Eights stand in the order of kv_levels8.  A wavefront takes 32 coordinates (blockIdx.y) of `tiles` times 16 rows: few
-// rows are spread over many wavefronts (a chain of loads is what they cost), many share a block of Pi.
+// 16 unit rows in LDS as operands of the rotation: each of the workgroup's D / 32 wavefronts brings 32 coordinates of them
+// (x[e] = coordinate 32 wave + 8 (lane / 16) + e of row lane % 16, any length) and gets all; returns the rows' lengths.
 template <int D>
-__global__ __launch_bounds__(64) void k_kv_rotate_queries(KvRows q, const float* __restrict__ pi, uint16_t* __restrict__ z, float* __restrict__ zn, int tiles) {
-    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, block = blockIdx.y;
+struct UnitRows {
+    halfx8 hi[D / 32][64], lo[D / 32][64];
+    float square[D / 32][16];
+
+    __device__ __forceinline__ float bring(const float (&x)[8]) {
+        const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15;
+        float n2 = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) n2 += x[e] * x[e];
+        n2 = kv_sum4(n2);
+        __syncthreads();                            // the rows before are no longer read
+        if (lane < 16) square[wave][n] = n2;
+        __syncthreads();
+        float sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) sum += square[s][n];
+        const float norm = sqrtf(sum), scale = norm > 0.f ? kSplitScale / norm : 0.f;
+        halfx8 h, l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = x[e] * scale;
+            h[e] = (_Float16)v;
+            l[e] = (_Float16)(v - (float)h[e]);
+        }
+        hi[wave][lane] = h;
+        lo[wave][lane] = l;
+        __syncthreads();
+        return norm;
+    }
+};
+
+// Queries into the rotated frame: unit rows in float16, a second part with what the first rounds away, and their norms.
+// Eights stand in the order of kv_levels8.  A workgroup takes `tiles` times 16 rows, each of its wavefronts a block of 32
+// coordinates of the result (and of the rows that it reads).
+template <int D>
+__global__ __launch_bounds__(D * 2) void k_kv_rotate_queries(KvRows q, const float* __restrict__ pi, uint16_t* __restrict__ z, float* __restrict__ zn, int tiles) {
+    __shared__ UnitRows<D> unit;
+    const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int64_t all = (int64_t)q.rows * q.heads;
-    const KvTurn<D, false> turn(pi, block);
+    const KvTurn<D, false> turn(pi, wave);
     for (int64_t tile = (int64_t)blockIdx.x * tiles; tile < ((int64_t)blockIdx.x + 1) * tiles && tile * 16 < all; ++tile) {
         const int64_t i = tile * 16 + n;
         const bool in = i < all;
         const int64_t row = in ? i / q.heads : 0, head = in ? i % q.heads : 0;
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(q.data) + row * q.row_stride + head * q.head_stride + 8 * g;
-        float x[D / 32][8], y[8];
+        const uintx4 w = *reinterpret_cast<const uintx4*>(reinterpret_cast<const uint16_t*>(q.data) + row * q.row_stride + head * q.head_stride + 32 * wave + 8 * g);
+        float x[8], y[8];
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const uintx4 w = *reinterpret_cast<const uintx4*>(p + 32 * s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t bits = w[e >> 1] >> 16 * (e & 1) & 0xffff;
-                x[s][e] = q.type == IVFTQ_KV_BF16 ? kv_to_float<true>(bits) : kv_to_float<false>(bits);
-            }
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t bits = w[e >> 1] >> 16 * (e & 1) & 0xffff;
+            x[e] = q.type == IVFTQ_KV_BF16 ? kv_to_float<true>(bits) : kv_to_float<false>(bits);
         }
-        const float norm = kv_unit_row<D>(x);
-        turn(x, y);
+        const float norm = unit.bring(x);
+        turn(unit, y);
         if (!in) continue;
-        if (g == 0 && block == 0) zn[i] = norm;
+        if (g == 0 && wave == 0) zn[i] = norm;
         halfx8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -360,8 +526,8 @@ __global__ __launch_bounds__(64) void k_kv_rotate_queries(KvRows q, const float*
             hi[at] = (_Float16)v;
             lo[at] = (_Float16)(v - (float)hi[at]);
         }
-        *reinterpret_cast<halfx8*>(z + i * D + 32 * block + 8 * g) = hi;
-        *reinterpret_cast<halfx8*>(z + (all + i) * D + 32 * block + 8 * g) = lo;
+        *reinterpret_cast<halfx8*>(z + i * D + 32 * wave + 8 * g) = hi;
+        *reinterpret_cast<halfx8*>(z + (all + i) * D + 32 * wave + 8 * g) = lo;
     }
 }
 
@@ -416,31 +582,32 @@ __global__ __launch_bounds__(256) void k_kv_many_join(ManyArgs f) {
 
 // Results back into the rows' own frame, split the same way.
 template <int D>
-__global__ __launch_bounds__(64) void k_kv_rotate_back(ManyArgs f, int tiles) {
+__global__ __launch_bounds__(D * 2) void k_kv_rotate_back(ManyArgs f, int tiles) {
+    __shared__ UnitRows<D> unit;
+    __shared__ bool has[16 * kTurnTiles];
     const KvRows& out = f.a.out;
-    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
-    const int64_t all = (int64_t)out.rows * out.heads;
-    const KvTurn<D, true> turn(f.a.c.rotation, blockIdx.y);
-    for (int64_t tile = (int64_t)blockIdx.x * tiles; tile < ((int64_t)blockIdx.x + 1) * tiles && tile * 16 < all; ++tile) {
-        const int64_t i = tile * 16 + n;
-        const bool in = i < all && many_has(f.a, i / out.heads);
-        float x[D / 32][8], y[8];
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
-            if (!in) continue;
+    const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int64_t all = (int64_t)out.rows * out.heads, first = (int64_t)blockIdx.x * tiles * 16;
+    for (int u = threadIdx.x; u < 16 * tiles; u += D * 2) has[u] = first + u < all && many_has(f.a, (first + u) / out.heads);
+    const KvTurn<D, true> turn(f.a.c.rotation, wave);
+    __syncthreads();
+    for (int tile = 0; tile < tiles && first + tile * 16 < all; ++tile) {
+        const int64_t i = first + tile * 16 + n;
+        const bool in = has[tile * 16 + n];
+        float x[8] = {}, y[8];
+        if (in) {
+            const int j = 32 * wave + 8 * g;
             if (f.parts > 1) {
-                many_join<D>(f, i, all, 32 * s + 8 * g, x[s], s == 0 && g == 0 && blockIdx.y == 0);
+                many_join<D>(f, i, all, j, x, j == 0);
             } else {
-                const float4* w = reinterpret_cast<const float4*>(f.whole + i * D + 32 * s + 8 * g);
+                const float4* w = reinterpret_cast<const float4*>(f.whole + i * D + j);
                 const float4 a = w[0], b = w[1];
-                x[s][0] = a.x; x[s][1] = a.y; x[s][2] = a.z; x[s][3] = a.w; x[s][4] = b.x; x[s][5] = b.y; x[s][6] = b.z; x[s][7] = b.w;
+                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
             }
         }
-        const float norm = kv_unit_row<D>(x) * f.a.c.level_unit;
-        turn(x, y);
-        if (in) kv_store_turned(out, i / out.heads, i % out.heads, blockIdx.y, y, norm);
+        const float norm = unit.bring(x) * f.a.c.level_unit;
+        turn(unit, y);
+        if (in) kv_store_turned(out, i / out.heads, i % out.heads, wave, y, norm);
     }
 }
 
@@ -458,9 +625,9 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
     uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
     float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole), *ml = reinterpret_cast<float*>(a.work + w.ml);
     const int64_t all = (int64_t)a.q.rows * a.q.heads;
-    const int tiles = all >= 16384 ? 8 : 1;              // 16-row tiles a wavefront rotates
-    const dim3 rot((unsigned)((all + 16 * tiles - 1) / (16 * tiles)), D / 32);
-    if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, 64, 0, st>>>(a.q, a.c.rotation, z, zn, tiles);
+    const int tiles = all >= 16384 ? kTurnTiles : 1;     // a workgroup's 16-row tiles: few rows are spread, many share the rotation's operands
+    const unsigned rot = (unsigned)((all + 16 * tiles - 1) / (16 * tiles));
+    if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, D * 2, 0, st>>>(a.q, a.c.rotation, z, zn, tiles);
     const unsigned pairs = (unsigned)(a.c.batch * a.c.heads);
     if (w.few) {
         static ChipFill fill;
@@ -478,7 +645,7 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
         // float16 results: the queries' second part matters beside the rounding of the result
         if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4><<<wgs, 256, 0, st>>>(f);
         else k_kv_many<F, D, false><<<wgs, 256, 0, st>>>(f);
-        if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D><<<rot, 64, 0, st>>>(f, tiles);
+        if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D><<<rot, D * 2, 0, st>>>(f, tiles);
         else if (w.parts > 1) k_kv_many_join<F, D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, st>>>(f);
     }
     return hipGetLastError();
