@@ -35,7 +35,7 @@ struct FewArgs {
 struct FewSeq {
     int first, count;                 // first new row, new rows that are computed
     int base, end;                    // position of the first new row, one past the last one's
-    int low;                          // first token that the window of the earliest new row shows
+    int low, beyond;                  // first token that the window of the earliest new row shows; last one outside that of the latest
     int sink_tiles, window_tile, tiles;
 };
 
@@ -48,6 +48,7 @@ __device__ __forceinline__ FewSeq few_seq(const KvAttend& a, int b) {
     s.end = s.base + s.count > 0 ? s.base + s.count : 0;
     const int64_t low = a.window ? (int64_t)s.base - a.window + 1 : 0;
     s.low = low > 0 ? (int)low : 0;
+    s.beyond = a.window && (int64_t)s.end - 1 - a.window > 0 ? (int)((int64_t)s.end - 1 - a.window) : -1;
     const int end = (s.end + kFewTile - 1) / kFewTile, seen = a.sinks < s.end ? a.sinks : s.end;
     s.window_tile = s.low / kFewTile;
     if (s.window_tile > end) s.window_tile = end;
@@ -60,44 +61,44 @@ __device__ __forceinline__ FewSeq few_seq(const KvAttend& a, int b) {
 
 __device__ __forceinline__ int few_tiles(const KvAttend& a, int b) { return b < a.c.batch ? few_seq(a, b).tiles : 0; }
 
-// Sum of tiles over all sequences (of one head), by a wavefront.
-__device__ __forceinline__ int64_t few_total(const KvAttend& a) {
-    int64_t total = 0;
-    for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-        int v = few_tiles(a, b0 + (threadIdx.x & 63));
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-        total += v;
-    }
-    return kv_uniform(total);
-}
-
 // Tiles a workgroup takes.  At least four: one for each wavefront.
 __device__ __forceinline__ int64_t few_share(int64_t total, int wgs) {
     const int64_t s = (total + wgs - 1) / wgs;
     return s < 4 ? 4 : (s + 3) & ~(int64_t)3;
 }
 
-// Position x in the order (sequence, head, tile): its sequence and that sequence's first position.
-__device__ __forceinline__ void few_find(const KvAttend& a, int64_t x, int& seq, int64_t& at) {
+// The share of workgroup `wg`, positions [x, end) in the order (sequence, head, tile): the sequence of x and that sequence's
+// first position.  By a wavefront: a lane a sequence, scans over them; up to 64 sequences are looked at once.
+__device__ __forceinline__ void few_find(const KvAttend& a, int wg, int wgs, int64_t& x, int64_t& end, int& seq, int64_t& at) {
     const int lane = threadIdx.x & 63;
-    int64_t base = 0;
-    for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-        const int v = few_tiles(a, b0 + lane);
-        int64_t incl = v;
+    int tiles = 0;
+    int64_t incl = 0, total = 0;
+    auto scan = [&](int b0) __attribute__((always_inline)) {
+        tiles = few_tiles(a, b0 + lane);
+        incl = tiles;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) { const int64_t u = __shfl_up(incl, o); if (lane >= o) incl += u; }
-        const int64_t end = (base + incl) * a.c.heads;
-        const uint64_t past = __ballot(end > x);
+        return kv_uniform((int64_t)__shfl(incl, 63));
+    };
+    for (int b0 = 0; b0 < a.c.batch; b0 += 64) total += scan(b0);
+    total *= a.c.heads;
+    const int64_t share = few_share(total, wgs);
+    x = wg * share;
+    end = x + share < total ? x + share : total;
+    seq = a.c.batch;
+    at = 0;
+    int64_t base = 0;
+    for (int b0 = 0; x < end && b0 < a.c.batch; b0 += 64) {
+        const int64_t all = a.c.batch <= 64 ? total / a.c.heads : scan(b0);
+        const uint64_t past = __ballot((base + incl) * a.c.heads > x);
         if (past) {
             const int l = __builtin_ctzll(past);
             seq = b0 + l;
-            at = kv_uniform(base + (int64_t)__shfl(incl - v, l)) * a.c.heads;
+            at = kv_uniform(base + (int64_t)__shfl(incl - tiles, l)) * a.c.heads;
             return;
         }
-        base += kv_uniform((int64_t)__shfl(incl, 63));
+        base += all;
     }
-    seq = a.c.batch; at = 0;
 }
 
 template <int F>
@@ -117,15 +118,31 @@ struct FewTile {
     uintx4 kg, vg;
     uintx4 kk[2][kCodes ? 1 : D / 32], vv[kCodes ? 1 : D / 16];
 };
-struct FewPlace { int t0; int64_t p0, p1; };                // first token, pages of its two halves (-1: none)
-
-__device__ __forceinline__ FewPlace few_place(const KvView& c, const FewSeq& s, int b, int i) {
-    FewPlace p;
-    p.t0 = (i < s.sink_tiles ? i : i - s.sink_tiles + s.window_tile) * kFewTile;
-    p.p0 = kv_page(c, b, p.t0);
-    p.p1 = kv_page(c, b, p.t0 + 16);
-    return p;
-}
+// A tile's first token and the records of its page (pages of 16: of its two pages); page 0 where there is none.
+struct FewPlace {
+    int t0;
+    const char *r0, *r1;
+    bool there0, there1;
+};
+struct FewTable {                     // one pair's way into the cache
+    const int32_t* row;
+    const char* head;
+    __device__ __forceinline__ FewTable(const KvView& c, int b, int h) : row(c.table + (int64_t)b * c.table_stride), head(c.pool + (int64_t)h * c.head_bytes) {}
+    __device__ __forceinline__ const char* find(const KvView& c, int t, bool& there) const {
+        const int col = t >> c.page_log2;
+        const int32_t id = col < c.columns ? kv_int(row, col) : -1;
+        there = (uint32_t)id < (uint32_t)c.pages;
+        return head + (int64_t)(there ? id : 0) * c.page_bytes;
+    }
+    __device__ __forceinline__ FewPlace operator()(const KvView& c, const FewSeq& s, int i) const {
+        FewPlace p;
+        p.t0 = (i < s.sink_tiles ? i : i - s.sink_tiles + s.window_tile) * kFewTile;
+        p.r0 = p.r1 = find(c, p.t0, p.there0);
+        p.there1 = p.there0;
+        if (c.page < kFewTile) p.r1 = find(c, p.t0 + 16, p.there1);
+        return p;
+    }
+};
 
 // Byte offsets of a lane's reads inside a tile of one page.
 template <int F, int D>
@@ -147,11 +164,11 @@ struct FewLane {
 };
 
 template <int F, int D>
-__device__ __forceinline__ void few_load(const KvView& c, int h, const FewPlace& p, const FewLane<F, D>& at, FewTile<F, D>& x) {
+__device__ __forceinline__ void few_load(const KvView& c, const FewPlace& p, const FewLane<F, D>& at, FewTile<F, D>& x) {
     constexpr bool codes = F == IVFTQ_KV_CODE4;
     constexpr int row = codes ? D / 2 : D * 2;                        // bytes of a token's row
     const int in = p.t0 & (c.page - 1);
-    const char* base = kv_record(c, p.p0 < 0 ? 0 : p.p0, h);
+    const char* base = p.r0;
     auto read = [&](const char* keys, const char* values, const char* norms) {
         // every address is a scalar base and a lane's offset (pages of 32 and more), or a lane's own pointer
         if constexpr (codes) {
@@ -177,7 +194,7 @@ __device__ __forceinline__ void few_load(const KvView& c, int h, const FewPlace&
         const char* here = base + in * row;
         read(here + at.key, here + at.value, base + 2 * in + at.norm);
     } else {                                                          // pages of 16: the tile's halves lie in two pages
-        const char* other = kv_record(c, p.p1 < 0 ? 0 : p.p1, h);
+        const char* other = p.r1;
         const int lane = threadIdx.x & 63;
         const bool k1 = lane & 8, v1 = lane & 32;                     // second half: n / 8, g / 2
         read((k1 ? other - 16 * row : base) + at.key, (v1 ? other - 16 * row : base) + at.value, (v1 ? other - 32 : base) + at.norm);
@@ -185,15 +202,15 @@ __device__ __forceinline__ void few_load(const KvView& c, int h, const FewPlace&
 }
 
 // One query row a lane: its operands, what its scores are multiplied by, its position.
-template <int F, int D>
+template <int F, int D, bool LOW>
 struct FewQuery {
-    uintx4 q[D / 32], low[F == IVFTQ_KV_CODE4 ? D / 32 : 1];
+    uintx4 q[D / 32], low[LOW ? D / 32 : 1];
     float gain;
     int pos;
 };
 
-template <int F, int D>
-__device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int h, int col0, FewQuery<F, D>& x) {
+template <int F, int D, bool LOW>
+__device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int h, int col0, FewQuery<F, D, LOW>& x) {
     const KvAttend& a = f.a;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int cols = s.count * a.group, col = col0 + n < cols ? col0 + n : 0, tok = a.max_new == 1 ? 0 : col / a.group;
@@ -209,9 +226,8 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
             x.q[k] = *reinterpret_cast<const uintx4*>(f.z + at * D + g * (D / 4) + 8 * k);
-            x.low[k] = *reinterpret_cast<const uintx4*>(f.z + (all + at) * D + g * (D / 4) + 8 * k);
-            x.low[k] ^= sign;
             x.q[k] ^= sign;
+            if constexpr (LOW) { x.low[k] = *reinterpret_cast<const uintx4*>(f.z + (all + at) * D + g * (D / 4) + 8 * k); x.low[k] ^= sign; }
         }
     } else {
         const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
@@ -223,8 +239,8 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
 
 // A tile into the running maximum m, sum l (of this lane's tokens) and sums o (transposed: o[blk][r] = coordinate
 // 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).
-template <int F, int D>
-__device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int h, const FewQuery<F, D>& q, const FewPlace& at, FewTile<F, D>& x, float& m,
+template <int F, int D, bool LOW>
+__device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, const FewQuery<F, D, LOW>& q, const FewPlace& at, FewTile<F, D>& x, float& m,
                                          float& l, floatx4 (&o)[D / 16]) {
     const KvView& c = a.c;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, t0 = at.t0;
@@ -237,7 +253,7 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int
             for (int k = 0; k < D / 32; ++k) {
                 const uintx4 w = __builtin_bit_cast(uintx4, kv_levels8(x.kw[y][k], c));
                 st[y] = kv_mfma16<F>(w, q.q[k], st[y]);
-                st[y] = kv_mfma16<F>(w, q.low[k], st[y]);
+                if constexpr (LOW) st[y] = kv_mfma16<F>(w, q.low[k], st[y]);
             }
         const halfx8 kn = __builtin_bit_cast(halfx8, x.kg);
 #pragma unroll
@@ -251,11 +267,10 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int
         for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3];
     }
     // every token of the tile visible to every row?
-    const bool full = at.p0 >= 0 && at.p1 >= 0 && t0 + kFewTile - 1 <= s.base &&
-                      (!a.window || (int64_t)t0 > (int64_t)s.end - 1 - a.window || t0 + kFewTile <= a.sinks);
+    const bool full = at.there0 && at.there1 && t0 + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks);
     uint32_t shown = 0xff;                  // of the lane's eight tokens: those that any row sees
     if (!full) {
-        const bool there = (g >> 1 ? at.p1 : at.p0) >= 0;
+        const bool there = g >> 1 ? at.there1 : at.there0;
         shown = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -325,9 +340,8 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int
                 for (int i = 1; i < 8; ++i) { v = e == i ? sc[i] : v; w = e == i ? pr[i] : w; }
                 v = __shfl(v, 16 * from + n);
                 w = __shfl(w, 16 * from + n);
-                const int64_t page = from >> 1 ? at.p1 : at.p0;
                 const int in = (t0 + t) & (c.page - 1);
-                const uint16_t* y = reinterpret_cast<const uint16_t*>(kv_record(c, page < 0 ? 0 : page, h) + c.page * (D * 2)) + (in >> 3) * D * 8 + e;
+                const uint16_t* y = reinterpret_cast<const uint16_t*>((from >> 1 ? at.r1 : at.r0) + c.page * (D * 2)) + (in >> 3) * D * 8 + e;
                 if (v == -INFINITY) continue;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
@@ -341,25 +355,26 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, int
 // One wavefront's tiles [from, to) in steps of four.  Codes: the next tile's words are on their way while this one is
 // worked on (a tile is 24 registers, its arithmetic as long as its loads), the pages of the one after are looked up.  16
 // bits: a tile's 16 KB in flight are enough, only the pages are looked up ahead.
-template <int F, int D>
+template <int F, int D, bool LOW>
 __device__ __forceinline__ void few_walk(const FewArgs& f, const FewSeq& s, int b, int h, int col0, int from, int to, float& m, float& l,
                                          floatx4 (&o)[D / 16]) {
     const KvView& c = f.a.c;
     if (from >= to) return;
-    FewQuery<F, D> q;
-    few_query<F, D>(f, s, h, col0, q);
+    FewQuery<F, D, LOW> q;
+    const FewTable table(c, b, h);
+    FewPlace at = table(c, s, from);
+    few_query<F, D, LOW>(f, s, h, col0, q);
     const FewLane<F, D> lane(c);
-    FewPlace at = few_place(c, s, b, from);
     if constexpr (F == IVFTQ_KV_CODE4) {
         FewTile<F, D> x, y;
-        few_load<F, D>(c, h, at, lane, x);
-        FewPlace next = few_place(c, s, b, from + 4 < to ? from + 4 : from);
+        few_load<F, D>(c, at, lane, x);
+        FewPlace next = table(c, s, from + 4 < to ? from + 4 : from);
         int i = from;
         // past the end: a tile that is there, read and not used
         auto step = [&](FewTile<F, D>& now, FewTile<F, D>& then) {
-            const FewPlace after = few_place(c, s, b, i + 8 < to ? i + 8 : i);
-            few_load<F, D>(c, h, next, lane, then);
-            few_step<F, D>(f.a, s, h, q, at, now, m, l, o);
+            const FewPlace after = table(c, s, i + 8 < to ? i + 8 : i);
+            few_load<F, D>(c, next, lane, then);
+            few_step<F, D, LOW>(f.a, s, q, at, now, m, l, o);
             at = next;
             next = after;
             i += 4;
@@ -373,9 +388,9 @@ __device__ __forceinline__ void few_walk(const FewArgs& f, const FewSeq& s, int 
     } else {
         for (int i = from; i < to; i += 4) {
             FewTile<F, D> x;
-            few_load<F, D>(c, h, at, lane, x);
-            const FewPlace next = few_place(c, s, b, i + 4 < to ? i + 4 : i);
-            few_step<F, D>(f.a, s, h, q, at, x, m, l, o);
+            few_load<F, D>(c, at, lane, x);
+            const FewPlace next = table(c, s, i + 4 < to ? i + 4 : i);
+            few_step<F, D, LOW>(f.a, s, q, at, x, m, l, o);
             at = next;
         }
     }
@@ -384,8 +399,8 @@ __device__ __forceinline__ void few_walk(const FewArgs& f, const FewSeq& s, int 
 template <int F>
 __device__ __forceinline__ int few_coord(int D, int k, int g, int r) { return F == IVFTQ_KV_CODE4 ? (4 * g + r) * (D / 16) + k : 16 * k + 4 * g + r; }
 
-template <int F, int D>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_few(FewArgs f) {
+template <int F, int D, bool LOW>
+__global__ __launch_bounds__(256, D <= 128 ? 3 : 1) void k_kv_few(FewArgs f) {
     constexpr int kPass = D > 128 ? D / 2 : D;                 // coordinates that pass through LDS at a time
     __shared__ float sum[4][16][kPass + 1];
     __shared__ float ml[4][16][2];
@@ -395,11 +410,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_few(FewArgs f) {
     int64_t x = 0, end = 0, at = 0;
     int b = 0;
     if (f.split) {
-        const int64_t total = few_total(a) * a.c.heads, share = few_share(total, f.wgs);
-        x = blockIdx.x * share;
-        end = x + share < total ? x + share : total;
+        few_find(a, blockIdx.x, f.wgs, x, end, b, at);
         if (x >= end) return;
-        few_find(a, x, b, at);
     } else {
         b = blockIdx.x / a.c.heads;
     }
@@ -430,7 +442,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_few(FewArgs f) {
             floatx4 o[D / 16];
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) o[k] = floatx4{0.f, 0.f, 0.f, 0.f};
-            few_walk<F, D>(f, s, b, h, col0, from + wave, to, m, l, o);
+            few_walk<F, D, LOW>(f, s, b, h, col0, from + wave, to, m, l, o);
             l = kv_sum4(l);
             if (g == 0) { ml[wave][n][0] = m; ml[wave][n][1] = l; }
             __syncthreads();

@@ -630,14 +630,22 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
     if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, D * 2, 0, st>>>(a.q, a.c.rotation, z, zn, tiles);
     const unsigned pairs = (unsigned)(a.c.batch * a.c.heads);
     if (w.few) {
-        static ChipFill fill;
-        unsigned wgs = 0;
-        if (w.split) {
-            if (hipError_t e = fill.get(reinterpret_cast<const void*>(&k_kv_few<F, D>), 256, 0, &wgs)) return e;
-            if (wgs > (unsigned)kFewMaxWgs) wgs = kFewMaxWgs;
-        }
-        FewArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), ml, (int32_t)wgs, w.split};
-        k_kv_few<F, D><<<dim3(w.split ? wgs : pairs, (unsigned)w.col_tiles), 256, 0, st>>>(f);
+        FewArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), ml, 0, w.split};
+        // float16 results: the queries' second part matters beside the rounding of the result
+        constexpr bool codes = F == IVFTQ_KV_CODE4;
+        const bool low = codes && a.q.type == IVFTQ_KV_F16;
+        auto launch = [&](auto kernel, ChipFill& fill) {
+            unsigned wgs = pairs;
+            if (w.split) {
+                if (hipError_t e = fill.get(reinterpret_cast<const void*>(kernel), 256, 0, &wgs)) return e;
+                if (wgs > (unsigned)kFewMaxWgs) wgs = kFewMaxWgs;
+                f.wgs = (int32_t)wgs;
+            }
+            kernel<<<dim3(wgs, (unsigned)w.col_tiles), 256, 0, st>>>(f);
+            return hipGetLastError();
+        };
+        static ChipFill fill, fill_low;
+        if (hipError_t e = low ? launch(&k_kv_few<F, D, codes>, fill_low) : launch(&k_kv_few<F, D, false>, fill)) return e;
         if (w.split || F == IVFTQ_KV_CODE4) k_kv_few_join<F, D><<<dim3(pairs, (unsigned)w.col_tiles), 512, 0, st>>>(f);
     } else {
         ManyArgs f{a, z, zn, whole, ml, w.row_tiles, w.parts};
