@@ -243,6 +243,7 @@ template <int F, int D, bool LOW>
 __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, const FewQuery<F, D, LOW>& q, const FewPlace& at, FewTile<F, D>& x, float& m,
                                          float& l, floatx4 (&o)[D / 16]) {
     const KvView& c = a.c;
+    constexpr bool codes = F == IVFTQ_KV_CODE4;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, t0 = at.t0;
     floatx4 st[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     float sc[8];                            // of the tokens t0 + 8 g + e
@@ -257,7 +258,7 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
             }
         const halfx8 kn = __builtin_bit_cast(halfx8, x.kg);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e] = st[e & 1][e >> 1] * (float)kn[e];
+        for (int e = 0; e < 8; ++e) sc[e] = __builtin_fmaf((float)kn[e], st[e & 1][e >> 1], 0.f);        // one v_fma_mix
     } else {
 #pragma unroll
         for (int y = 0; y < 2; ++y)
@@ -284,9 +285,12 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
     float top = sc[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
-    top = kv_max4(top) * q.gain;
-    if (__ballot(top > m)) {
-        const float now = fmaxf(m, top), turn = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
+    // The reference m is no maximum: sums are only turned when a score passes it.  16 bits: it may lie 2^8 under a row's scores,
+    // weights of up to 256 lose nothing.  Codes: weights meet the norms in float16, so it is set 2^4 above the maximum, weights
+    // stay under one.
+    if (__ballot(top * q.gain > m + (codes || m == -INFINITY ? 0.f : 8.f))) {
+        const float all = kv_max4(top) * q.gain, now = all > m + (codes || m == -INFINITY ? 0.f : 8.f) ? all + (codes ? 4.f : 0.f) : m;
+        const float turn = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
         m = now;
         l *= turn;
 #pragma unroll
@@ -302,7 +306,7 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
         const halfx8 vn = __builtin_bit_cast(halfx8, x.vg);
         float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = pr[e] * (float)vn[e];
+        for (int e = 0; e < 8; ++e) w[e] = __builtin_fmaf((float)vn[e], pr[e], 0.f);
         if (!full) {                        // what a row does not see may be anything, and 0 * NaN is no zero
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = shown >> e & 1 && sc[e] != -INFINITY ? w[e] : 0.f;

@@ -275,8 +275,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
             __builtin_amdgcn_sched_barrier(0);
         }
         top = kv_max32(top) * gain;
-        // 16 bits: a row's maximum may lag by 2^8, weights of up to 256 lose nothing; with codes they meet the norms in float16
+        // m is no maximum, but near it (see kv_few.h)
         const bool grows = top > m + (codes || m == -INFINITY ? 0.f : 8.f);
+        if constexpr (codes) top += 4.f;
         if (__ballot(grows)) {
             const float turn = grows ? __builtin_amdgcn_exp2f(m - top) : 1.f;
             m = grows ? top : m;
