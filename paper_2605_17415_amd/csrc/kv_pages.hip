@@ -28,15 +28,28 @@ __device__ __forceinline__ int scan_before(int v, int& total) {
     return before + incl - v;
 }
 
+// Pages are looked at four a thread, so that some thousands take one pass and one scan (a pass is a chain of loads and
+// barriers, about 2 us).
+constexpr int kPages = 4;
+__device__ __forceinline__ void four_refs(const ivftq_kv_pages& s, int64_t p, int32_t (&refs)[kPages], int32_t past) {
+#pragma unroll
+    for (int e = 0; e < kPages; ++e) refs[e] = p + e < s.pages ? s.refs[p + e] : past;
+}
+
 // The lowest `want` free pages into list; returns how many there are (at most `want`).
 __device__ __forceinline__ int lowest_free(const ivftq_kv_pages& s, int want, int32_t* list) {
     int found = 0;
-    for (int64_t p0 = 0; p0 < s.pages && found < want; p0 += kThreads) {
-        const int64_t p = p0 + threadIdx.x;
-        const int free = p < s.pages && s.refs[p] <= 0;
-        int total;
-        const int rank = found + scan_before(free, total);
-        if (free && rank < want) list[rank] = (int32_t)p;
+    for (int64_t p0 = 0; p0 < s.pages && found < want; p0 += kThreads * kPages) {
+        const int64_t p = p0 + threadIdx.x * kPages;
+        int32_t refs[kPages];
+        four_refs(s, p, refs, 1);
+        int free = 0, total;
+#pragma unroll
+        for (int e = 0; e < kPages; ++e) free += refs[e] <= 0;
+        int rank = found + scan_before(free, total);
+#pragma unroll
+        for (int e = 0; e < kPages; ++e)
+            if (refs[e] <= 0 && rank < want) list[rank++] = (int32_t)(p + e);
         found += total;
     }
     __syncthreads();
@@ -50,7 +63,6 @@ __device__ __forceinline__ int length_of(const ivftq_kv_pages& s, int r) {
 }
 
 __global__ __launch_bounds__(kThreads) void k_kv_reserve(ivftq_kv_pages s, const int32_t* counts, int32_t* granted, int32_t* list) {
-    int want = 0;
     auto need_of = [&](int r, int& have, bool& fits) {
         const int n = length_of(s, r), more = counts[r] > 0 ? counts[r] : 0;
         have = (n + s.page - 1) / s.page;
@@ -58,15 +70,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_reserve(ivftq_kv_pages s, const
         fits = all <= s.columns;
         return fits ? (int)all - have : 0;
     };
-    for (int r0 = 0; r0 < s.rows; r0 += kThreads) {
-        const int r = r0 + threadIdx.x;
-        int have = 0, total;
-        bool fits = false;
-        const int need = r < s.rows ? need_of(r, have, fits) : 0;
-        scan_before(need, total);
-        want = want + total < s.pages ? want + total : (int)s.pages;      // a sum of two numbers of pages fits 32 bits
-    }
-    const int found = lowest_free(s, want, list);
+    // granted[r] first holds the number of pages that the rows before r need (as far as there can be pages)
     int64_t before = 0;
     for (int r0 = 0; r0 < s.rows; r0 += kThreads) {
         const int r = r0 + threadIdx.x;
@@ -74,17 +78,24 @@ __global__ __launch_bounds__(kThreads) void k_kv_reserve(ivftq_kv_pages s, const
         bool fits = false;
         const int need = r < s.rows ? need_of(r, have, fits) : 0;
         const int64_t at = before + scan_before(need, total);
+        if (r < s.rows) granted[r] = (int32_t)(at < s.pages ? at : s.pages);
         before += total;
-        if (r >= s.rows) continue;
-        fits = fits && (!need || at + need <= found);
-        granted[r] = fits && counts[r] > 0 ? counts[r] : 0;
+    }
+    const int found = lowest_free(s, (int)(before < s.pages ? before : s.pages), list);
+    for (int r = threadIdx.x; r < s.rows; r += kThreads) {
+        int have = 0;
+        bool fits = false;
+        const int need = need_of(r, have, fits), at = granted[r];
+        fits = fits && (!need || (int64_t)at + need <= found);
+        const int more = fits && counts[r] > 0 ? counts[r] : 0;
+        granted[r] = more;
         if (!fits) continue;
         for (int i = 0; i < need; ++i) {
             const int32_t p = list[at + i];
             s.table[(int64_t)r * s.table_stride + have + i] = p;
             s.refs[p] = 1;
         }
-        s.lengths[r] = length_of(s, r) + granted[r];
+        s.lengths[r] = length_of(s, r) + more;
     }
 }
 
@@ -105,24 +116,20 @@ __global__ __launch_bounds__(kThreads) void k_kv_fork(ivftq_kv_pages s, const in
         return (unsigned)p < (unsigned)s.rows && (unsigned)c < (unsigned)s.rows && __hip_atomic_load(claim + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i &&
                !__hip_atomic_load(parent + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) && s.lengths[c] <= 0;
     };
+    // src[i] first holds how many pages the entries before i take, dst[i] whether this one takes one
     int want = 0;
     for (int i0 = 0; i0 < n; i0 += kThreads) {
         const int i = i0 + threadIdx.x;
         int total;
-        scan_before(i < n && ready(i) && length_of(s, parents[i]) % s.page, total);
+        const bool ok = i < n && ready(i), part = ok && length_of(s, parents[i]) % s.page;
+        const int at = want + scan_before(part, total);
         want += total;
+        if (i < n) { done[i] = ok; src[i] = at; dst[i] = part; }
     }
     const int found = lowest_free(s, want < s.pages ? want : (int)s.pages, list);
-    int before = 0;
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
-        const int i = i0 + threadIdx.x;
-        int total;
-        const bool ok = i < n && ready(i);
-        const bool part = ok && length_of(s, parents[i]) % s.page;
-        const int at = before + scan_before(part, total);
-        before += total;
-        if (i >= n) continue;
-        done[i] = ok && (!part || at < found);
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const int at = src[i], part = dst[i];
+        done[i] = done[i] && (!part || at < found);
         src[i] = dst[i] = -1;
         if (done[i] && part) {
             const int32_t from = s.table[(int64_t)parents[i] * s.table_stride + length_of(s, parents[i]) / s.page];
@@ -131,19 +138,22 @@ __global__ __launch_bounds__(kThreads) void k_kv_fork(ivftq_kv_pages s, const in
         }
     }
     __syncthreads();
-    for (int64_t u = threadIdx.x; u < (int64_t)n * s.columns; u += kThreads) {
-        const int i = (int)(u / s.columns), col = (int)(u % s.columns);
+    for (int i = threadIdx.x >> 6; i < n; i += kWaves) {         // a wavefront a row
         if (!done[i]) continue;
-        const int whole = length_of(s, parents[i]) / s.page;
-        int32_t p = -1;
-        if (col < whole) {
-            p = s.table[(int64_t)parents[i] * s.table_stride + col];
-            if (p >= 0 && p < s.pages) atomicAdd(s.refs + p, 1); else p = -1;
-        } else if (col == whole && dst[i] >= 0) {
-            p = dst[i];
-            s.refs[p] = 1;
+        const int whole = length_of(s, parents[i]) / s.page, last = dst[i];
+        const int32_t* from = s.table + (int64_t)parents[i] * s.table_stride;
+        int32_t* row = s.table + (int64_t)children[i] * s.table_stride;
+        for (int col = threadIdx.x & 63; col < s.columns; col += 64) {
+            int32_t p = -1;
+            if (col < whole) {
+                p = from[col];
+                if (p >= 0 && p < s.pages) atomicAdd(s.refs + p, 1); else p = -1;
+            } else if (col == whole && last >= 0) {
+                p = last;
+                s.refs[p] = 1;
+            }
+            row[col] = p;
         }
-        s.table[(int64_t)children[i] * s.table_stride + col] = p;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads)
@@ -175,25 +185,34 @@ __global__ __launch_bounds__(256) void k_kv_trim(ivftq_kv_pages s, int window, i
 __global__ __launch_bounds__(kThreads) void k_kv_compact(ivftq_kv_pages s, int32_t* used_out, int32_t* scratch) {
     int32_t *to = scratch, *src = to + s.pages, *dst = src + s.pages;
     int used = 0;
-    for (int64_t p0 = 0; p0 < s.pages; p0 += kThreads) {
-        const int64_t p = p0 + threadIdx.x;
-        int total;
-        scan_before(p < s.pages && s.refs[p] > 0, total);
+    for (int64_t p0 = 0; p0 < s.pages; p0 += kThreads * kPages) {
+        int32_t refs[kPages];
+        four_refs(s, p0 + threadIdx.x * kPages, refs, 0);
+        int busy = 0, total;
+#pragma unroll
+        for (int e = 0; e < kPages; ++e) busy += refs[e] > 0;
+        scan_before(busy, total);
         used += total;
     }
     int moves = 0, holes = 0;
-    for (int64_t p0 = 0; p0 < s.pages; p0 += kThreads) {
-        const int64_t p = p0 + threadIdx.x;
-        const bool in = p < s.pages, busy = in && s.refs[p] > 0;
-        const bool move = busy && p >= used, hole = in && !busy && p < used;
-        int total;
-        const int rank = scan_before(move, total) + moves;
-        moves += total;
-        const int place = scan_before(hole, total) + holes;
-        holes += total;
-        if (in) to[p] = (int32_t)p;
-        if (move) src[rank] = (int32_t)p;
-        if (hole) dst[place] = (int32_t)p;
+    for (int64_t p0 = 0; p0 < s.pages; p0 += kThreads * kPages) {
+        const int64_t p = p0 + threadIdx.x * kPages;
+        int32_t refs[kPages];
+        four_refs(s, p, refs, 0);
+        int both = 0, total;                             // moves in the low half, holes in the high half: 4096 at most
+#pragma unroll
+        for (int e = 0; e < kPages; ++e) both += refs[e] > 0 ? p + e >= used : (p + e < s.pages && p + e < used ? 1 << 16 : 0);
+        const int at = scan_before(both, total);
+        int move = moves + (at & 0xffff), hole = holes + (at >> 16);
+        moves += total & 0xffff;
+        holes += total >> 16;
+#pragma unroll
+        for (int e = 0; e < kPages; ++e) {
+            if (p + e >= s.pages) break;
+            to[p + e] = (int32_t)(p + e);
+            if (refs[e] > 0 && p + e >= used) src[move++] = (int32_t)(p + e);
+            if (refs[e] <= 0 && p + e < used) dst[hole++] = (int32_t)(p + e);
+        }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < moves; i += kThreads) {

@@ -173,7 +173,7 @@ def _stream(stream, like):
 
 def _scratch(count, dtype, like, stream):
     """Device memory from the caching allocator, marked as used by the call's stream where that is not the current one."""
-    t = torch.empty(count, dtype=dtype, device=like.device)
+    t = like.new_empty(count, dtype=dtype)
     if stream is not None:
         t.record_stream(stream)
     return t
@@ -239,7 +239,7 @@ def _pages(table, lengths, refs, page):
 def _pools(pools, like):
     """[layers, pages, ...]: contiguous records, layers any distance apart."""
     _on_device(pools, "pools", like)
-    if pools.dim() < 3 or not pools.numel() or not pools[0].is_contiguous():
+    if pools.dim() < 3 or not pools.numel() or not (pools.is_contiguous() or pools[0].is_contiguous()):
         raise ValueError("pools must be layers x pages x record with contiguous layers")
     size, (layers, pages) = pools.element_size(), pools.shape[:2]
     return _pack_pools(pools.data_ptr(), pools.stride(0) * size, pools.numel() // (layers * pages) * size, pages, layers)
