@@ -4,7 +4,8 @@ from .binding import (ALLOC_FN, FREE_FN, Index, IvftqError, declared_symbols, iv
                       ivftq_haar_from_gaussian, ivftq_haar_rotation, ivftq_measure_mfma_rate, ivftq_quantiser_grid, ivftq_rerank, ivftq_version,
                       load_library)
 
-_KV = ("declared_kv_symbols", "kv_append", "kv_attend", "kv_compact", "kv_copy", "kv_fork", "kv_free", "kv_page_bytes", "kv_read", "kv_reserve", "kv_trim")
+_KV = ("KVCache", "declared_kv_symbols", "kv_append", "kv_attend", "kv_compact", "kv_copy", "kv_fork", "kv_free", "kv_page_bytes", "kv_read",
+       "kv_reserve", "kv_trim")
 
 
 def __getattr__(name):

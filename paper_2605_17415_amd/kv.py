@@ -15,7 +15,7 @@ import struct
 import numpy as np
 import torch
 
-from .binding import _check, load_library
+from .binding import _check, ivftq_build_codebook, ivftq_haar_rotation, load_library
 
 F16, BF16, CODE4 = range(3)
 HEAD_SIZES = (64, 96, 128, 192, 256)
@@ -285,3 +285,56 @@ def kv_copy(pools, src, dst, stream=None):
     """Record of page src[i] to page dst[i] in every layer of pools; no page both source and destination."""
     where = _pools(pools, pools)
     _check(_library().ivftq_kv_copy(where, _ints(src, "src", pools), _ints(dst, "dst", pools, src.numel()), src.numel(), _stream(stream, pools)))
+
+
+# ---- a model's cache -----------------------------------------------------------------------------
+
+
+class KVCache:
+    """Keys and values of a model's layers for up to `sequences` rows of up to `tokens` tokens, in a pool of `pages` pages that all
+    layers number alike.  codes=True keeps them in the 4-bit codes of the library's quantiser: `rotation_seed` and d fix the
+    codec, nothing is trained.  Tensors: pools [layers, pages, ...], table, lengths, refs; methods carry the C names minus the
+    prefix and queue their work on the current stream (or `stream`).
+
+    A step of a model: `reserve` room for the new tokens, then for every layer `append` its keys and values and `attend`.  Rows
+    without new tokens have none between their `starts`."""
+
+    def __init__(self, layers: int, heads: int, d: int, pages: int, sequences: int, tokens: int, page: int = 64, dtype=torch.bfloat16, codes: bool = False,
+                 rotation_seed: int = 0, device="cuda"):
+        if kv_page_bytes(CODE4 if codes else _TYPES.get(dtype, -1), page, heads, d) == 0:
+            raise ValueError(f"no cache of pages of {page} tokens, {heads} heads and {d} coordinates in {'codes' if codes else dtype}")
+        if layers < 1 or pages < 1 or sequences < 1 or tokens < 1:
+            raise ValueError("a cache has at least one layer, page, sequence and token")
+        self.d, self.heads, self.page, self.codes = d, heads, page, codes
+        record = (heads, page * (d + 4)) if codes else (heads, 2, page, d)
+        self.pools = torch.empty((layers, pages, *record), dtype=torch.uint8 if codes else dtype, device=device)
+        self.table = torch.full((sequences, -(-tokens // page)), -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        self.refs = torch.zeros(pages, dtype=torch.int32, device=device)
+        self._codec = {}
+        if codes:
+            self._codec = {"rotation": torch.from_numpy(ivftq_haar_rotation(d, rotation_seed)).to(device), "levels": ivftq_build_codebook(4, d)[0]}
+
+    def reserve(self, counts, stream=None):
+        return kv_reserve(self.table, self.lengths, self.refs, counts, self.page, stream)
+
+    def append(self, layer: int, k, v, starts=None, stream=None):
+        kv_append(self.pools[layer], k, v, self.table, self.lengths, starts, stream=stream, **self._codec)
+
+    def attend(self, layer: int, q, starts=None, max_new: int = 1, window: int = 0, sinks: int = 0, scale=None, out=None, lse=None, stream=None):
+        return kv_attend(q, self.pools[layer], self.table, self.lengths, starts, max_new, window, sinks, scale, out=out, lse=lse, stream=stream, **self._codec)
+
+    def read(self, layer: int, k_out, v_out, starts=None, stream=None):
+        kv_read(self.pools[layer], self.table, self.lengths, k_out, v_out, starts, stream=stream, **self._codec)
+
+    def fork(self, parents, children, stream=None):
+        return kv_fork(self.pools, self.table, self.lengths, self.refs, parents, children, self.page, stream)
+
+    def free(self, rows, stream=None):
+        kv_free(self.table, self.lengths, self.refs, rows, stream)
+
+    def trim(self, window: int, sinks: int = 0, stream=None):
+        kv_trim(self.table, self.lengths, self.refs, self.page, window, sinks, stream)
+
+    def compact(self, stream=None):
+        return kv_compact(self.pools, self.table, self.refs, stream)
