@@ -119,40 +119,46 @@ ivftq_status check_rows(const ivftq_kv_rows* r, const char* name, int heads, int
 }
 
 // The magnitudes' float16 table.  A table's common scale is free (scores and results are multiplied by it in float32), and the
-// rounding of eight numbers to float16 depends on it: of 512 scales in [1, 5/4) the one with the smallest sum of squares
-// leaves 2 to 3 times less than a scale taken blindly (a result's error in float16 was 6.8e-4 without this and without
-// the queries' second part, 2.1e-4 is the rounding of the result itself).  About a microsecond.
-void level_table(KvView& v) {
-    float ulp[8], inv[8], best = 1e30f, scale = 1.f;
+// rounding of eight numbers to float16 depends on it: of 128 scales in [1, 2) the one that leaves the smallest mean square,
+// levels weighted by how often a coordinate of variance 1 / d meets them and what a common factor mends left out, 4e-5 to 8e-5
+// of a row where a scale taken blindly leaves 2e-4 (the rounding of a float16 result itself is 2.1e-4).  About a microsecond.
+void level_table(KvView& v, int d) {
+    constexpr int kScales = 128;
+    float square[kScales] = {}, along[kScales] = {}, weight[8], energy = 0.f;
     for (int i = 0; i < 8; ++i) {
         int e;
-        frexpf(v.level[i], &e);
-        ulp[i] = ldexpf(1.f, e - 11);
-        inv[i] = v.level[i] * ldexpf(1.f, 11 - e);
-    }
-    for (int k = 0; k < 512; ++k) {
-        const float s = 1.f + (float)k * (0.25f / 512);
-        float sum = 0.f;
-        for (int i = 0; i < 8; ++i) {
-            const float x = inv[i] * s, r = (x + 12582912.f) - 12582912.f, off = (x - r) * ulp[i];     // 1.5 * 2^23: to the next whole number
-            sum += off * off;
+        const float mantissa = ldexpf(frexpf(v.level[i], &e), 11), ulp = ldexpf(1.f, e - 11);          // [1024, 2048)
+        const float low = i ? v.bound[i - 1] : 0.f, high = i < 7 ? v.bound[i] : 2.f * v.level[7] - v.bound[6];
+        const float w = expf(-0.5f * v.level[i] * v.level[i] * (float)d) * (high - low);
+        weight[i] = w;
+        energy += w * v.level[i] * v.level[i];
+        for (int k = 0; k < kScales; ++k) {
+            const float x = mantissa * (1.f + (float)k * (1.f / kScales)), down = x >= 2048.f ? 0.5f : 1.f, up = x >= 2048.f ? 2.f : 1.f;
+            const float y = x * down, off = (y - ((y + 12582912.f) - 12582912.f)) * (ulp * up);         // 1.5 * 2^23: to the next whole number
+            square[k] += w * off * off;
+            along[k] += w * off * v.level[i];
         }
-        if (sum < best) { best = sum; scale = s; }
     }
-    double dot = 0, square = 0;
+    float best = 1e30f, scale = 1.f;
+    for (int k = 0; k < kScales; ++k) {
+        const float s = 1.f + (float)k * (1.f / kScales), left = (square[k] - along[k] * along[k] / energy) / (s * s);
+        if (left < best) { best = left; scale = s; }
+    }
+    double dot = 0, sum = 0;
     for (int i = 0; i < 8; ++i) {
         const _Float16 h = (_Float16)(v.level[i] * scale);
         uint16_t bits;
         memcpy(&bits, &h, 2);
         v.tab_lo[i / 4] |= (uint32_t)(bits & 0xff) << 8 * (i % 4);
         v.tab_hi[i / 4] |= (uint32_t)(bits >> 8) << 8 * (i % 4);
-        dot += (double)v.level[i] * (double)(float)h;
-        square += (double)(float)h * (double)(float)h;
+        dot += (double)weight[i] * (double)v.level[i] * (double)(float)h;
+        sum += (double)weight[i] * (double)(float)h * (double)(float)h;
     }
-    v.level_unit = (float)(dot / square);
+    v.level_unit = sum > 0 ? (float)(dot / sum) : 1.f / scale;
 }
 
-KvView view_of(const ivftq_kv_cache& c, const int32_t* starts, int64_t rows) {
+// attends: the table of magnitudes is needed (rows are written and read with the levels themselves)
+KvView view_of(const ivftq_kv_cache& c, const int32_t* starts, int64_t rows, bool attends) {
     KvView v{};
     v.pool = static_cast<char*>(c.pool);
     v.table = c.table;
@@ -174,7 +180,7 @@ KvView view_of(const ivftq_kv_cache& c, const int32_t* starts, int64_t rows) {
             v.level[i] = c.levels[8 + i];
             if (i) v.bound[i - 1] = (float)(((double)c.levels[7 + i] + c.levels[8 + i]) / 2);
         }
-        level_table(v);
+        if (attends) level_table(v, c.d);
     }
     return v;
 }
@@ -189,7 +195,7 @@ ivftq_status move_rows(const ivftq_kv_cache* cache, const ivftq_kv_rows* k, cons
     if (ivftq_status e = check_rows(v, read ? "v_out" : "v", cache->heads, cache->d, cache, starts)) return e;
     if (k->rows != v->rows || k->type != v->type) return refuse(IVFTQ_INVALID_ARG, "keys and values have one number of rows and one type");
     if (!k->rows || !cache->batch) return IVFTQ_OK;
-    const KvView c = view_of(*cache, starts, k->rows);
+    const KvView c = view_of(*cache, starts, k->rows, false);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const hipError_t e = read ? launch_kv_read(c, rows_of(*k), rows_of(*v), cache->d, cache->format, st) : launch_kv_append(c, rows_of(*k), rows_of(*v), cache->d, cache->format, st);
     return done(e, read ? "ivftq_kv_read" : "ivftq_kv_append");
@@ -256,7 +262,7 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     if (w.bytes && (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)))
         return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)workspace_bytes, (long long)w.bytes);
     KvAttend a{};
-    a.c = view_of(*cache, starts, q->rows);
+    a.c = view_of(*cache, starts, q->rows, true);
     a.q = rows_of(*q);
     a.out = rows_of(*out);
     a.lse = lse;

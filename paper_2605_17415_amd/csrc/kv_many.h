@@ -68,7 +68,8 @@ struct ManyTile {
     static constexpr int kKeyBytes = kManyTile * kRow * 16, kValueBytes = kManyTile * D * 2;
     char keys[2][kKeyBytes];
     char values[2][kValueBytes];
-    float key_gain[kCodes ? 2 : 1][kCodes ? kManyTile : 1], value_gain[kCodes ? 2 : 1][kCodes ? kManyTile : 1];
+    // norms have four places: a tile's are written, a tile ahead, while others may still be at the tile before and read its own
+    float key_gain[kCodes ? 4 : 1][kCodes ? kManyTile : 1], value_gain[kCodes ? 4 : 1][kCodes ? kManyTile : 1];
     uint32_t odd[2][2];
 
     static __device__ __forceinline__ int turn(int t) { return kRow == 8 ? t >> 1 & 7 : t & 15; }
@@ -79,7 +80,7 @@ struct ManyStage {
     using Tile = ManyTile<F, D>;
     static constexpr bool kCodes = F == IVFTQ_KV_CODE4;
     uint32_t k[kCodes ? D / 32 : 1], v[kCodes ? D / 32 : 1];      // eight coordinates of a key, eight tokens of a value
-    uint32_t key_norm, value_norm;
+    uint32_t norm;                // lanes 0 .. 15: of the quarter's keys, 16 .. 31: of its values
 
     // keys (values) of a tile's quarter, which begins with token `in` of record `rec`, to buffer `to` of LDS
     __device__ __forceinline__ void bring_keys(const KvView& c, const char* rec, int in, Tile& lds, int to, int quarter) {
@@ -88,7 +89,7 @@ struct ManyStage {
             const uint32_t* x = reinterpret_cast<const uint32_t*>(rec + in * (D / 2));
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) k[j] = x[lane + 64 * j];
-            key_norm = reinterpret_cast<const uint16_t*>(rec + c.page * D)[in + (lane & 15)];
+            norm = reinterpret_cast<const uint16_t*>(rec + c.page * D)[(lane & 16 ? c.page : 0) + in + (lane & 15)];
         } else {
             // lane's place in the first 64 chunks; the next 64 are kRows rows on, where chunks are turned by a further xor
             constexpr int kRows = 64 / Tile::kRow, kTurn = Tile::kRow == 8 ? kRows / 2 : kRows;
@@ -108,7 +109,6 @@ struct ManyStage {
             const uint32_t* x = reinterpret_cast<const uint32_t*>(rec + (c.page + in) * (D / 2));
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) v[j] = x[lane + 64 * j];
-            value_norm = reinterpret_cast<const uint16_t*>(rec + c.page * D)[c.page + in + (lane & 15)];
         } else {
             const char* from = rec + (c.page + in) * (D * 2);
 #pragma unroll
@@ -116,7 +116,7 @@ struct ManyStage {
         }
     }
     // codes: what has been brought, into LDS
-    __device__ __forceinline__ void store_keys(const KvView& c, Tile& lds, int to, int quarter) const {
+    __device__ __forceinline__ void store_keys(const KvView& c, Tile& lds, int to, int gain_to, int quarter) const {
         if constexpr (kCodes) {
             const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -124,7 +124,7 @@ struct ManyStage {
                 const int u = lane + 64 * j, row = u / (D / 8), w = u % (D / 8);
                 *reinterpret_cast<halfx8*>(lds.keys[to] + ((16 * quarter + row) * Tile::kRow + (w ^ Tile::turn(row))) * 16) = kv_levels8(k[j], c);
             }
-            if (lane < 16) lds.key_gain[to][16 * quarter + lane] = (float)__builtin_bit_cast(_Float16, (uint16_t)key_norm);
+            if (lane < 32) (lane < 16 ? lds.key_gain : lds.value_gain)[gain_to][16 * quarter + (lane & 15)] = (float)__builtin_bit_cast(_Float16, (uint16_t)norm);
         }
     }
     __device__ __forceinline__ void store_values(const KvView& c, Tile& lds, int to, int quarter) const {
@@ -132,7 +132,6 @@ struct ManyStage {
             const int lane = threadIdx.x & 63;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) *reinterpret_cast<halfx8*>(lds.values[to] + (quarter * 2 * D + lane + 64 * j) * 16) = kv_levels8(v[j], c);
-            if (lane < 16) lds.value_gain[to][16 * quarter + lane] = (float)__builtin_bit_cast(_Float16, (uint16_t)value_norm);
         }
     }
 };
@@ -243,16 +242,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     // one kLead further on stands before it; the compiler may not move anything from one such group to another (left alone it puts the
     // matrix instructions first, and the wavefront stands still behind them).
     //
-    // O^T += V^T P^T of tokens 32 x .. of buffer `from`; the maximum of the scores st of half `y` of buffer `at` (codes: times the
+    // O^T += V^T P^T of tokens 32 x .. of `buffer`; the maximum of the scores st of half `y` of tile `tile` (codes: times the
     // keys' norms; mine: the tokens that this lane's row sees, a bit each, from this lane's half on).
-    auto product_and_maximum = [&](int from, int x, const uintx4 (&p)[2], int at, int y, bool full, uint32_t mine, floatx16_& st) __attribute__((always_inline)) {
+    auto product_and_maximum = [&](int buffer, int x, const uintx4 (&p)[2], int tile, int y, bool full, uint32_t mine, floatx16_& st) __attribute__((always_inline)) {
         uintx4 w[kSteps];
 #pragma unroll
-        for (int j = 0; j < kLead; ++j) w[j] = value_chunk(from, x, j);
+        for (int j = 0; j < kLead; ++j) w[j] = value_chunk(buffer, x, j);
         float gains[16];
         if constexpr (codes) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) gains[r] = lds.key_gain[at][32 * y + 8 * half + 16 * (r >> 3) + (r & 7)];
+            for (int r = 0; r < 16; ++r) gains[r] = lds.key_gain[(tile - from) & 3][32 * y + 8 * half + 16 * (r >> 3) + (r & 7)];
         }
         if (!full) {                                // (a norm that is no number: the product comes before the mask)
 #pragma unroll
@@ -265,7 +264,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-            if (j + kLead < kSteps) w[j + kLead] = value_chunk(from, x, j + kLead);
+            if (j + kLead < kSteps) w[j + kLead] = value_chunk(buffer, x, j + kLead);
             o[j % (D / 32)] = kv_mfma32<F>(w[j], p[j / (D / 32)], o[j % (D / 32)]);
 #pragma unroll
             for (int r = 16 * j / kSteps; r < 16 * (j + 1) / kSteps; ++r) {
@@ -286,16 +285,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
             for (int k = 0; k < D / 32; ++k) o[k] *= turn;
         }
     };
-    // S^T of tokens 32 x .. of buffer `from` into `next`; the weights of the scores st of half `y` of buffer `at`.
-    auto scores_and_weights = [&](int from, int x, floatx16_& next, int at, int y, bool full, uint32_t mine, const floatx16_& st, uintx4 (&p)[2]) __attribute__((always_inline)) {
+    // S^T of tokens 32 x .. of `buffer` into `next`; the weights of the scores st of half `y` of tile `tile`.
+    auto scores_and_weights = [&](int buffer, int x, floatx16_& next, int tile, int y, bool full, uint32_t mine, const floatx16_& st, uintx4 (&p)[2]) __attribute__((always_inline)) {
         uintx4 w[kSteps];
 #pragma unroll
-        for (int k = 0; k < kLead; ++k) w[k] = key_chunk(from, x, k);
+        for (int k = 0; k < kLead; ++k) w[k] = key_chunk(buffer, x, k);
         const float less = m == -INFINITY ? 0.f : m;              // a row that has seen nothing: every score is -infinity
         float gains[16], pr[16];
         if constexpr (codes) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) gains[r] = lds.value_gain[at][32 * y + 8 * half + 16 * (r >> 3) + (r & 7)];
+            for (int r = 0; r < 16; ++r) gains[r] = lds.value_gain[(tile - from) & 3][32 * y + 8 * half + 16 * (r >> 3) + (r & 7)];
             if (!full) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) gains[r] = mine >> (16 * (r >> 3) + (r & 7)) & 1 ? gains[r] : 0.f;
@@ -306,7 +305,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-            if (k + kLead < kSteps) w[k + kLead] = key_chunk(from, x, k + kLead);
+            if (k + kLead < kSteps) w[k + kLead] = key_chunk(buffer, x, k + kLead);
             score(w[k], k, next);
 #pragma unroll
             for (int r = 16 * k / kSteps; r < 16 * (k + 1) / kSteps; ++r) {
@@ -344,12 +343,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         }
     };
 
-    // The order of things: keys of tile i + 1 and values of tile i are there when tile i's second half begins, half way through
-    // tile i (one barrier a tile); what the buffers are then free for, keys of tile i + 2 and values of tile i + 1, is on its
+    // The order of things: keys and norms of tile i + 1 and values of tile i are there when tile i's second half begins, half way
+    // through tile i (one barrier a tile); what the buffers are then free for, keys of tile i + 2 and values of tile i + 1, is on its
     // way from there on.
     Ahead now = answer(from, ask(from)), next = answer(from + 1, ask(from + 1));
     bring_keys(from, now, 0);
-    if constexpr (codes) { if (from < to) stage.store_keys(c, lds, 0, wave); }
+    if constexpr (codes) { if (from < to) stage.store_keys(c, lds, 0, 0, wave); }
     bring_keys(from + 1, next, 1);
     bring_values(from, now, 0);
     int32_t asked = ask(from + 2);
@@ -375,7 +374,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         uint64_t mine = ~0ull;
         [[maybe_unused]] uint64_t shown = ~0ull, dirty = 0;
         if constexpr (codes) {
-            if (i + 1 < to) stage.store_keys(c, lds, other, wave);
+            if (i + 1 < to) stage.store_keys(c, lds, other, (i + 1 - from) & 3, wave);
             stage.store_values(c, lds, here, wave);
             bring_keys(i + 2, then, here);
             bring_values(i + 1, next, other);
@@ -388,8 +387,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
             mine = (many_below((int64_t)pos - t0 + 1) & ~none & (a.window ? ~many_below((int64_t)pos - a.window + 1 - t0) | sinks : ~0ull)) >> 8 * half;
             shown = many_below((int64_t)span.end - t0) & ~none & (~many_below((int64_t)span.low - t0) | sinks);
         }
-        product_and_maximum(other, 1, p1, here, 0, full, (uint32_t)mine, s0);
-        scores_and_weights(here, 1, s1, here, 0, full, (uint32_t)mine, s0, p0);
+        product_and_maximum(other, 1, p1, i, 0, full, (uint32_t)mine, s0);
+        scores_and_weights(here, 1, s1, i, 0, full, (uint32_t)mine, s0, p0);
         kv_loads_done();
         __syncthreads();
         if (!codes && !full) {
@@ -417,8 +416,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
                     *p = w;
                 }
             }
-            if (threadIdx.x < 2) lds.odd[other][threadIdx.x] = 0;
             __syncthreads();
+            if (threadIdx.x < 2) lds.odd[here][threadIdx.x] = 0;          // for the tile after the next
             if ((uint32_t)dirty) singly(t0, 0, (uint32_t)dirty, s0);
         }
         if constexpr (!codes) {
@@ -427,8 +426,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         }
         now = next;
         next = then;
-        product_and_maximum(here, 0, p0, here, 1, full, (uint32_t)(mine >> 32), s1);
-        scores_and_weights(other, 0, s0, here, 1, full, (uint32_t)(mine >> 32), s1, p1);       // past the last tile: of what LDS holds, not used
+        product_and_maximum(here, 0, p0, i, 1, full, (uint32_t)(mine >> 32), s1);
+        scores_and_weights(other, 0, s0, i, 1, full, (uint32_t)(mine >> 32), s1, p1);       // past the last tile: of what LDS holds, not used
         if constexpr (!codes) {
             if (dirty >> 32) singly(t0, 1, (uint32_t)(dirty >> 32), s1);
         }

@@ -174,6 +174,32 @@ def test_a_chunk_after_a_long_beginning(form, kind, d, page, window, sinks):
     ref.check_attention(c, q.cpu(), out, news, lse=lse, window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 64), (128, 128), (192, 32), (256, 64)])
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2199, 4)])
+def test_both_kernels_agree(form, kind, d, page, window, sinks):
+    """The last rows of long chunks, as rows of the chunk and as few rows: the same operands, so only the weights' rounding (2^-11, 2^-8;
+    a few 2^-24 for each token's score and sum) and the result's own may differ.  Many workgroups and many tiles, several times."""
+    pkg = _pkg()
+    heads, group, lens, news = 4, 4, [5000, 3100, 900], [500, 756, 300]
+    c = ref.Cache(17, form, heads, d, page, lens)
+    t, codec = c.device()
+    q = queries(17, sum(news), heads * group, d, ref.TYPES[kind])
+    last = 3
+    rows = torch.cat([torch.arange(e - last, e) for e in np.cumsum(news)]).to(DEV)
+    few = pkg.kv_attend(q[rows], t["pool"], t["table"], t["lengths"], starts=starts_of([last] * 3), max_new=last, window=window, sinks=sinks, **codec)
+    for _ in range(3):
+        many = pkg.kv_attend(q, t["pool"], t["table"], t["lengths"], starts=starts_of(news), max_new=max(news), window=window, sinks=sinks, **codec)
+        torch.cuda.synchronize()
+        far = (many[rows].double() - few.double()).norm(dim=-1)
+        # the values are independent rows, so the result's length is about |w|_2 |v|, and roundings of at most `step` of each weight, independent
+        # in the two kernels, move it by at most that times sqrt(2) step in the mean square: five times step leaves three standard
+        # deviations and a result a third shorter than the mean
+        step = 2.0 ** -11 if form == "code4" else ref.HALF[few.dtype]
+        size = few.double().norm(dim=-1)
+        assert (far <= (2 * ref.HALF[few.dtype] + 5 * step) * size + 2.0 ** -18 * math.sqrt(d)).all(), float((far / size).max())
+
+
 @pytest.mark.parametrize("form,kind", FORMS[:3])
 @pytest.mark.parametrize("lens", ([40, 0, 5], [1800, 700]))
 def test_more_heads_than_few_rows(form, kind, lens):
