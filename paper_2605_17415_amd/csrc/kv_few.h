@@ -21,6 +21,17 @@ constexpr int kFewTile = 32;          // tokens of a wavefront's step
 constexpr int kFewMaxWgs = 1024;      // workgroups that share the tiles, at most: as many as the chip holds at once
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// Weights are powers e^(score - reference) rounded to 16 bits; the reference is no maximum, and sums are only turned to another one
+// when a score passes it by kWeightRoom (powers of two).  It is set kWeightLift under the maximum: float16 weights then keep their 11
+// bits down to 2^-26 of the largest one, which counts where the heaviest token (a first token that most heads look at) has next to no
+// value and the result is made of the others; bfloat16 has range enough.  Codes: weights meet the values' norms before they are rounded,
+// so what is compared is the score plus the norm's exponent.
+template <int F> constexpr float kWeightLift = F == IVFTQ_KV_BF16 ? 0.f : 12.f;
+template <int F> constexpr float kWeightRoom = F == IVFTQ_KV_BF16 ? 8.f : 15.f;
+
+// The exponent of a float16 norm, as a power of two that is above it (zero and what is under 2^-14: as 2^-14; no number: 2^17).
+__device__ __forceinline__ float kv_norm_power(uint32_t bits) { return (float)(int)(__builtin_amdgcn_ubfe(bits, 10, 5)) - 14.f; }
+
 struct FewArgs {
     KvAttend a;
     const uint16_t* z;                // codes: rotated unit queries, two float16 parts [2][rows][heads][D], eights in the order of kv_levels8
@@ -206,8 +217,11 @@ template <int F, int D, bool LOW>
 struct FewQuery {
     uintx4 q[D / 32], low[LOW ? D / 32 : 1];
     float gain;
-    int pos;
+    int pos, begin;                   // its position, the first token of its window
 };
+
+// The lowest n of eight bits.
+__device__ __forceinline__ uint32_t few_below(int n) { return 0xffu >> (n <= 0 ? 8 : (n >= 8 ? 0 : 8 - n)); }
 
 template <int F, int D, bool LOW>
 __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int h, int col0, FewQuery<F, D, LOW>& x) {
@@ -215,6 +229,8 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int cols = s.count * a.group, col = col0 + n < cols ? col0 + n : 0, tok = a.max_new == 1 ? 0 : col / a.group;
     x.pos = col0 + n < cols ? s.base + tok : s.end - 1;
+    const int64_t low = a.window ? (int64_t)x.pos - a.window + 1 : 0;
+    x.begin = low > 0 ? (int)low : 0;
     // scores are multiplied by a factor above zero, so that their maximum is that of the products: a negative scale turns the
     // queries' signs, and none at all is taken as next to none
     x.gain = fabsf(a.scale) * kLog2e;
@@ -271,25 +287,31 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
     const bool full = at.there0 && at.there1 && t0 + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks);
     uint32_t shown = 0xff;                  // of the lane's eight tokens: those that any row sees
     if (!full) {
-        const bool there = g >> 1 ? at.there1 : at.there0;
-        shown = 0;
+        // bits and selects only: what the compiler makes of conditions here was found to be wrong
+        const int tb = t0 + 8 * g;
+        const uint32_t there = (g >> 1 ? at.there1 : at.there0) ? 0xffu : 0u, sinks = few_below(a.sinks - tb);
+        shown = few_below(s.end - tb) & (~few_below(s.low - tb) | sinks) & there;
+        const uint32_t mine = few_below(q.pos + 1 - tb) & (~few_below(q.begin - tb) | sinks) & shown;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int t = t0 + 8 * g + e;
-            const bool any = there && t < s.end && (t >= s.low || t < a.sinks);
-            const bool mine = any && t <= q.pos && (!a.window || (int64_t)t > (int64_t)q.pos - a.window || t < a.sinks);
-            shown |= any ? 1u << e : 0u;
-            if (!mine) sc[e] = -INFINITY;
+        for (int e = 0; e < 8; ++e) sc[e] = mine >> e & 1 ? sc[e] : -INFINITY;
+        if constexpr (codes) {                // norms of others may be anything, and 0 * NaN is no zero
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.vg[e] &= (mine >> 2 * e & 1 ? 0xffffu : 0u) | (mine >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
         }
     }
     float top = sc[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
-    // The reference m is no maximum: sums are only turned when a score passes it.  16 bits: it may lie 2^8 under a row's scores,
-    // weights of up to 256 lose nothing.  Codes: weights meet the norms in float16, so it is set 2^4 above the maximum, weights
-    // stay under one.
-    if (__ballot(top * q.gain > m + (codes || m == -INFINITY ? 0.f : 8.f))) {
-        const float all = kv_max4(top) * q.gain, now = all > m + (codes || m == -INFINITY ? 0.f : 8.f) ? all + (codes ? 4.f : 0.f) : m;
+    top *= q.gain;
+    if constexpr (codes) {                  // norms are not negative: the largest is that of the largest bits
+        typedef uint16_t two __attribute__((ext_vector_type(2)));
+        const uint32_t w0 = x.vg[0], w1 = x.vg[1], w2 = x.vg[2], w3 = x.vg[3];
+        const two u = __builtin_elementwise_max(__builtin_elementwise_max(__builtin_bit_cast(two, w0), __builtin_bit_cast(two, w1)),
+                                                __builtin_elementwise_max(__builtin_bit_cast(two, w2), __builtin_bit_cast(two, w3)));
+        top += kv_norm_power(u[0] > u[1] ? u[0] : u[1]);
+    }
+    if (__ballot(top > m + kWeightRoom<F>)) {
+        const float all = kv_max4(top), now = all > m + kWeightRoom<F> ? all - kWeightLift<F> : m;
         const float turn = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
         m = now;
         l *= turn;
@@ -307,10 +329,6 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = __builtin_fmaf((float)vn[e], pr[e], 0.f);
-        if (!full) {                        // what a row does not see may be anything, and 0 * NaN is no zero
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = shown >> e & 1 && sc[e] != -INFINITY ? w[e] : 0.f;
-        }
         const uintx4 p = {kv_pack2<false>(w[0], w[2]), kv_pack2<false>(w[4], w[6]), kv_pack2<false>(w[1], w[3]), kv_pack2<false>(w[5], w[7])};
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) o[k] = kv_mfma16<F>(__builtin_bit_cast(uintx4, kv_levels8(x.vw[k], c)), p, o[k]);
@@ -404,7 +422,7 @@ template <int F>
 __device__ __forceinline__ int few_coord(int D, int k, int g, int r) { return F == IVFTQ_KV_CODE4 ? (4 * g + r) * (D / 16) + k : 16 * k + 4 * g + r; }
 
 template <int F, int D, bool LOW>
-__global__ __launch_bounds__(256, D <= 128 ? 3 : 1) void k_kv_few(FewArgs f) {
+__global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_few(FewArgs f) {
     constexpr int kPass = D > 128 ? D / 2 : D;                 // coordinates that pass through LDS at a time
     __shared__ float sum[4][16][kPass + 1];
     __shared__ float ml[4][16][2];

@@ -70,6 +70,7 @@ struct ManyTile {
     char values[2][kValueBytes];
     // norms have four places: a tile's are written, a tile ahead, while others may still be at the tile before and read its own
     float key_gain[kCodes ? 4 : 1][kCodes ? kManyTile : 1], value_gain[kCodes ? 4 : 1][kCodes ? kManyTile : 1];
+    float value_power[kCodes ? 4 : 1][4];      // of the quarters' largest norms
     uint32_t odd[2][2];
 
     static __device__ __forceinline__ int turn(int t) { return kRow == 8 ? t >> 1 & 7 : t & 15; }
@@ -124,6 +125,10 @@ struct ManyStage {
                 const int u = lane + 64 * j, row = u / (D / 8), w = u % (D / 8);
                 *reinterpret_cast<halfx8*>(lds.keys[to] + ((16 * quarter + row) * Tile::kRow + (w ^ Tile::turn(row))) * 16) = kv_levels8(k[j], c);
             }
+            uint32_t most = norm;
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) { const uint32_t other = __shfl_xor(most, o); most = most > other ? most : other; }
+            if (lane == 16) lds.value_power[gain_to][quarter] = kv_norm_power(most);
             if (lane < 32) (lane < 16 ? lds.key_gain : lds.value_gain)[gain_to][16 * quarter + (lane & 15)] = (float)__builtin_bit_cast(_Float16, (uint16_t)norm);
         }
     }
@@ -260,6 +265,20 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
                 st[r] = mine >> (16 * (r >> 3) + (r & 7)) & 1 ? st[r] : -INFINITY;
             }
         }
+        float power = 0.f;
+        if constexpr (codes) {
+            power = fmaxf(lds.value_power[(tile - from) & 3][2 * y], lds.value_power[(tile - from) & 3][2 * y + 1]);
+            if (!full) {                            // of the tokens that the row sees: others' norms may be anything
+                float most = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float v = lds.value_gain[(tile - from) & 3][32 * y + 8 * half + 16 * (r >> 3) + (r & 7)];
+                    most = fmaxf(most, mine >> (16 * (r >> 3) + (r & 7)) & 1 ? v : 0.f);
+                }
+                const int e = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 126;
+                power = (float)(e < -14 ? -14 : (e > 17 ? 17 : e));
+            }
+        }
         float top = -INFINITY;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -273,10 +292,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        top = kv_max32(top) * gain;
-        // m is no maximum, but near it (see kv_few.h)
-        const bool grows = top > m + (codes || m == -INFINITY ? 0.f : 8.f);
-        if constexpr (codes) top += 4.f;
+        top = codes && !full ? kv_max32(__builtin_fmaf(top, gain, power)) : __builtin_fmaf(kv_max32(top), gain, power);
+        const bool grows = top > m + kWeightRoom<F>;
+        top -= kWeightLift<F>;
         if (__ballot(grows)) {
             const float turn = grows ? __builtin_amdgcn_exp2f(m - top) : 1.f;
             m = grows ? top : m;

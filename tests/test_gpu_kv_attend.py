@@ -335,3 +335,56 @@ def test_refusals_with_tensors():
     for change in (dict(rotation=codec["rotation"][:32]), dict(rotation=codec["rotation"].double()), dict(levels=codec["levels"][:8]), dict(levels=codec["levels"] + 1)):
         with pytest.raises((ValueError, pkg.IvftqError)):
             pkg.kv_attend(q, t2["pool"], t2["table"], t2["lengths"], **{**codec, **change})
+
+
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("new", (1, 70))
+def test_a_heavy_token_without_a_value(form, kind, new):
+    """A first token that takes all of the weight but a millionth and has next to no value: the result is made of the others.  Their
+    roundings (a score's operands, the weight, for codes the value's levels: a few times `step` of each token's part) are independent, so
+    they add up as squares: eight steps of the parts' root of squares, and the result's own rounding."""
+    d, n = 64, 2000
+    rng = np.random.default_rng(new)
+    u = rng.standard_normal(d)
+    u /= np.linalg.norm(u)
+    c = ref.Cache(21, form, 1, d, 64, [n])
+    p0 = c.table[0, 0]
+    if form == "code4":
+        z = c.rotation.astype(np.float64) @ u
+        c.codes[0, p0, 0, 0] = np.abs(z[:, None] - c.levels[None].astype(np.float64)).argmin(1)
+        c.norms[0] = math.sqrt(d)
+        c.norms[0, p0, 0, 0], c.norms[1, p0, 0, 0] = 15.0, 2.0 ** -12
+    else:
+        c.rows16[0, p0, 0, 0] = torch.from_numpy(15 * u).to(c.rows16.dtype)
+        c.rows16[1] *= 64
+        c.rows16[1, p0, 0, 0] = 2.0 ** -12
+    q = torch.from_numpy(8 * u + 0.3 * rng.standard_normal((new, 2, d))).to(ref.TYPES[kind]).to(DEV)
+    got, _ = run(c, q, [new])
+    k, v = c.rows(0, 0, 0, n), c.rows(1, 0, 0, n)
+    size, step, out_step = np.linalg.norm(v, axis=1), 2.0 ** -11 if form == "code4" else ref.HALF[ref.TYPES[kind]], ref.HALF[ref.TYPES[kind]]
+    for i in range(new):
+        seen = n - new + i + 1
+        for h in range(2):
+            s = k[:seen] @ q[i, h].double().cpu().numpy() / math.sqrt(d)
+            w = np.exp(s - s.max())
+            assert s.argmax() == 0 and np.sort(w)[-2] < 0.01
+            w /= w.sum()
+            exact = w @ v[:seen]
+            far = np.linalg.norm(got[i, h].double().cpu().numpy() - exact)
+            may = 8 * step * math.sqrt(((w * size[:seen]) ** 2).sum()) + out_step * np.linalg.norm(exact) + 2.0 ** -25 * math.sqrt(d)
+            assert far <= may, (i, h, far / may)
+
+
+@pytest.mark.parametrize("kind", ("f16", "bf16"))
+@pytest.mark.parametrize("new", (1, 70))
+@pytest.mark.parametrize("power", (-12, 7))
+def test_norms_of_any_size(kind, new, power):
+    """Values' norms far from one, and from each other: float16 weights take no harm."""
+    c = ref.Cache(22, "code4", 2, 64, 16, [900, 130])
+    c.norms[1] = (c.norms[1].astype(np.float64) * 2.0 ** power * np.where(c.rng.random(c.norms[1].shape) < 0.1, 2.0 ** 4, 1)).astype(np.float16)
+    q = queries(22, 2 * new, 4, 64, ref.TYPES[kind])
+    if kind == "f16" and power < 0:
+        kind = "bf16"                                       # such results are under what float16 holds well
+        q = q.bfloat16()
+    out, lse = run(c, q, [new, new])
+    ref.check_attention(c, q.cpu(), out, [new, new], lse=lse)
