@@ -18,19 +18,13 @@ KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_h
     KvWork w{};
     const int64_t cols = (int64_t)max_new * (q_heads / kv_heads), all = rows * q_heads;
     w.few = cols <= kFewRows;
-    w.parts = 1;
     if (w.few) {
         w.col_tiles = (int)((cols + 15) / 16);
         w.split = capacity > 512;
     } else {
-        // Where the row tiles leave workgroups that a compute unit could hold without one, a tile's keys are shared out: over as
-        // many parts as fill them, at most eight, none under eight tiles of keys.  (200 row tiles of 128 rows over 20,000
-        // tokens in codes: 737 us in one part.)
         w.row_tiles = (int)((cols + kManyRows - 1) / kManyRows);
-        const int64_t wgs = (int64_t)batch * kv_heads * w.row_tiles, room = 256 * (d <= 128 ? 2 : 1);
-        const int64_t fill = wgs ? (room + wgs - 1) / wgs : 1, longest = capacity / (8 * kManyTile);
-        w.parts = (int)(fill < longest ? fill : longest);
-        w.parts = w.parts < 1 ? 1 : (w.parts > 8 ? 8 : w.parts);
+        const int64_t wgs = (int64_t)batch * kv_heads * w.row_tiles, room = 256 * (d <= 128 ? 2 : 1);       // the chip's compute units hold two each
+        if (wgs < 2 * room && kv_heads <= room && capacity > 512) w.shared = (int)(room / kv_heads);
     }
     int64_t at = 0;
     auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
@@ -38,8 +32,13 @@ KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_h
         w.z = room(all * d * 4);
         w.zn = room(all * 4);
     }
-    if (format == IVFTQ_KV_CODE4 || w.parts > 1) w.whole = room(all * d * 4 * w.parts);
-    if (w.parts > 1) w.ml = room(all * 8 * w.parts);
+    if (format == IVFTQ_KV_CODE4) w.whole = room(all * d * 4);
+    if (w.shared) {
+        const int64_t slots = (int64_t)2 * kv_heads * w.shared * kManyRows;
+        w.part = room(slots * d * 4);
+        w.ml = room(slots * 8);
+        w.begin = room(8 * (1 + (int64_t)batch * w.row_tiles));
+    }
     if (w.split) {
         w.part = room((int64_t)w.col_tiles * 2 * kFewMaxWgs * 16 * d * 4);
         w.ml = room((int64_t)w.col_tiles * 2 * kFewMaxWgs * 16 * 2 * 4);
@@ -272,7 +271,7 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     a.sinks = sinks;
     a.scale = scale;
     a.work = static_cast<char*>(workspace);
-    if ((int64_t)cache->batch * cache->heads * (w.few ? 1 : (int64_t)w.row_tiles * w.parts) > INT32_MAX) return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups");
+    if ((int64_t)cache->batch * cache->heads * (w.few ? 1 : (int64_t)w.row_tiles) > INT32_MAX) return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups");
     return done(launch_kv_attend(a, w, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_attend");
 }
 

@@ -25,9 +25,11 @@ struct ManyArgs {
     KvAttend a;
     const uint16_t* z;                // codes: rotated unit queries, two float16 parts, eights in the order of kv_levels8
     const float* zn;                  // codes: the queries' norms
-    float* whole;                     // codes: results before they are rotated back; several parts: their sums [parts][rows][heads][D]
-    float* part_ml;                   // several parts: maximum (in log2 units) and sum of weights
-    int32_t row_tiles, parts;         // row tiles a (sequence, head): those of max_new; shares of a row tile's keys
+    float* whole;                     // codes: results before they are rotated back
+    float* part;                      // shared tiles: [2 * workgroups][kManyRows][D] unnormalised sums
+    float* part_ml;                   // [2 * workgroups][kManyRows][2] reference (in log2 units), sum of weights
+    int64_t* begin;                   // a share's tiles, then [sequence][row tile] where a row tile begins among its head's tiles
+    int32_t row_tiles, wgs;           // row tiles a (sequence, head): those of max_new; workgroups a head that share the tiles
 };
 
 template <int F>
@@ -54,6 +56,63 @@ __device__ __forceinline__ ManySpan many_span(const KvAttend& a, int pos0, int p
     s.sink_tiles = (seen + kManyTile - 1) / kManyTile;
     if (s.sink_tiles > s.window_tile) s.sink_tiles = s.window_tile;
     s.tiles = s.sink_tiles + end_tile - s.window_tile;
+    return s;
+}
+
+// What a workgroup works on: one row tile (of 128 query rows) of a sequence.
+struct ManyRowTile {
+    FewSeq s;
+    int cols, pos0, pos1;             // query rows of the sequence, positions of the first and the last row
+    ManySpan span;
+    __device__ __forceinline__ ManyRowTile(const KvAttend& a, int b, int rt) : s(few_seq(a, b)), cols(s.count * a.group) {
+        const int last = (rt + 1) * kManyRows < cols ? (rt + 1) * kManyRows - 1 : cols - 1;
+        pos0 = s.base + rt * kManyRows / a.group;
+        pos1 = s.base + last / a.group;
+        span = many_span(a, pos0, pos1);
+        if (rt * kManyRows >= cols) span.tiles = 0;
+        else if (!span.tiles) span.tiles = 1;             // rows that see nothing keep one tile, all of it masked
+    }
+};
+
+// Where there are fewer row tiles than workgroups that keep the chip busy, or not many more, the key tiles of a head's row tiles, one
+// after the other, are dealt out in equal consecutive shares, as in kv_few.h: a row tile that lies whole in a share is finished there, of
+// the others each workgroup leaves at most two parts.  (27 row tiles a head of 20,256 and 11,900 tokens in codes, 8 heads: 437 us of the
+// kernel with every row tile's keys cut in two, and half of the compute units waiting for the longer sequence's.)
+struct ManyShare { int64_t size; int b, rt, from, to; int64_t begin; };       // from, to: tiles of the row tile; begin: its first one's place
+
+// The part of share `w` from its tile `x` on (x < size); to == from where there is none.
+__device__ __forceinline__ ManyShare many_share(const KvAttend& a, int row_tiles, int wgs, int w, int64_t x) {
+    const int lane = threadIdx.x & 63, items = a.c.batch * row_tiles;
+    int tiles = 0;
+    int64_t incl = 0;
+    auto scan = [&](int e0) __attribute__((always_inline)) {
+        const int e = e0 + lane;
+        tiles = e < items ? ManyRowTile(a, e / row_tiles, e % row_tiles).span.tiles : 0;
+        incl = tiles;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int64_t u = __shfl_up(incl, o); if (lane >= o) incl += u; }
+        return kv_uniform((int64_t)__shfl(incl, 63));
+    };
+    int64_t total = 0;
+    for (int e0 = 0; e0 < items; e0 += 64) total += scan(e0);
+    ManyShare s{(total + wgs - 1) / wgs, 0, 0, 0, 0, 0};
+    if (s.size < 8) s.size = 8;
+    const int64_t at = w * s.size + x, end = (w + 1) * s.size < total ? (w + 1) * s.size : total;
+    int64_t base = 0;
+    for (int e0 = 0; at < end && e0 < items; e0 += 64) {
+        const int64_t all = items <= 64 ? total : scan(e0);
+        const uint64_t past = __ballot(base + incl > at);
+        if (past) {
+            const int l = __builtin_ctzll(past), e = e0 + l, n = kv_uniform(__shfl(tiles, l));
+            s.b = e / row_tiles;
+            s.rt = e % row_tiles;
+            s.begin = base + kv_uniform((int64_t)__shfl(incl - tiles, l));
+            s.from = (int)(at - s.begin);
+            s.to = (int)(end - s.begin < n ? end - s.begin : n);
+            break;
+        }
+        base += all;
+    }
     return s;
 }
 
@@ -144,7 +203,7 @@ struct ManyStage {
 // The lowest n bits.
 __device__ __forceinline__ uint64_t many_below(int64_t n) { return n <= 0 ? 0 : (n >= 64 ? ~0ull : (1ull << n) - 1); }
 
-template <int F, int D, bool LOW>
+template <int F, int D, bool LOW, bool SHARED>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     using Tile = ManyTile<F, D>;
     constexpr int kSteps = D / 16;               // matrix instructions of a half tile's scores, and of its values
@@ -154,21 +213,37 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     const KvAttend& a = f.a;
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
-    // heads fastest: with eight heads each XCD reads one head's pages; then a row tile's shares, then sequences; the row tiles
-    // with the longest reach first
-    const int h = blockIdx.x % c.heads, part = blockIdx.x / c.heads % f.parts, b = blockIdx.x / c.heads / f.parts % c.batch;
-    const int rt = f.row_tiles - 1 - (int)(blockIdx.x / c.heads / f.parts / c.batch);
-    const FewSeq s = few_seq(a, b);
-    const int cols = s.count * a.group;
-    if (rt * kManyRows >= cols) return;
+    // heads fastest: with eight heads each XCD reads one head's pages; then shares, or sequences and the row tiles with the longest
+    // reach first
+    const int h = blockIdx.x % c.heads, share = blockIdx.x / c.heads;
+    int64_t x = 0;                               // the share's tiles that are done
+  while (true) {                                 // a row tile, or what of it lies in the share
+    int b, rt, from = 0, to = 0;
+    bool last_part = true;
+    if constexpr (SHARED) {
+        const ManyShare now = many_share(a, f.row_tiles, f.wgs, share, x);
+        if (now.from >= now.to) return;
+        b = now.b; rt = now.rt; from = now.from; to = now.to;
+        if (threadIdx.x == 0 && h == 0 && from == 0) f.begin[1 + b * f.row_tiles + rt] = now.begin;
+        if (threadIdx.x == 0 && blockIdx.x == 0) f.begin[0] = now.size;
+        last_part = x + (to - from) >= now.size;
+        if (x) __syncthreads();                  // LDS is no longer read
+    } else {
+        b = share % c.batch;
+        rt = f.row_tiles - 1 - share / c.batch;
+    }
+    const ManyRowTile tile(a, b, rt);
+    const FewSeq& s = tile.s;
+    const ManySpan& span = tile.span;
+    const int cols = tile.cols, pos0 = tile.pos0, pos1 = tile.pos1;
+    if (!SHARED) {
+        if (rt * kManyRows >= cols) return;
+        to = span.tiles;
+    }
     const int col = rt * kManyRows + wave * 32 + n, used = col < cols ? col : cols - 1;
     const int pos = s.base + used / a.group;
     const int64_t qrow = s.first + used / a.group;
     const int qhead = h * a.group + used % a.group;
-    const int last_col = (rt + 1) * kManyRows < cols ? (rt + 1) * kManyRows - 1 : cols - 1;
-    const int pos0 = s.base + rt * kManyRows / a.group, pos1 = s.base + last_col / a.group;
-    const ManySpan span = many_span(a, pos0, pos1);
-    const int from = (int)((int64_t)span.tiles * part / f.parts), to = (int)((int64_t)span.tiles * (part + 1) / f.parts);
 
     // scores are multiplied by a factor above zero, so that their maximum is that of the products: a negative scale turns the
     // queries' signs, and none at all is taken as next to none
@@ -456,26 +531,33 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     }
     if (from < to) product((to - from - 1) & 1, 1, p1);
     l = kv_sum32(l);
-    if (col >= cols) return;
-    const float inv = f.parts > 1 ? 1.f : (l == 0.f ? 0.f : 1.f / l);
-    const int64_t row_head = qrow * a.q.heads + qhead, all = (int64_t)a.q.rows * a.q.heads;
     // register r of o[k]: coordinate 32 k + 8 (r / 4) + 4 half + r % 4
+    const bool whole = !SHARED || (from == 0 && to == span.tiles);
+    const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+    const int64_t row_head = qrow * a.q.heads + qhead, slot = (((int64_t)h * f.wgs + share) * 2 + (from == 0)) * kManyRows + wave * 32 + n;
+    if (col < cols) {
+        float* to_float = whole ? f.whole + row_head * D : f.part + slot * D;
 #pragma unroll
-    for (int k = 0; k < D / 32; ++k)
+        for (int k = 0; k < D / 32; ++k)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int j = 32 * k + 2 * r + 4 * half;
-            if (codes || f.parts > 1) {
-                *reinterpret_cast<float4*>(f.whole + (part * all + row_head) * D + j) =
-                    make_float4(o[k][r] * inv, o[k][r + 1] * inv, o[k][r + 2] * inv, o[k][r + 3] * inv);
-            } else {
-                uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride + j;
-                *reinterpret_cast<uint2*>(p) = make_uint2(kv_pack2<bf>(o[k][r] * inv, o[k][r + 1] * inv), kv_pack2<bf>(o[k][r + 2] * inv, o[k][r + 3] * inv));
+            for (int r = 0; r < 16; r += 4) {
+                const int j = 32 * k + 2 * r + 4 * half;
+                const float4 v = make_float4(o[k][r] * inv, o[k][r + 1] * inv, o[k][r + 2] * inv, o[k][r + 3] * inv);
+                if (codes || !whole) {
+                    *reinterpret_cast<float4*>(to_float + j) = v;
+                } else {
+                    uint16_t* p = reinterpret_cast<uint16_t*>(a.out.data) + qrow * a.out.row_stride + qhead * a.out.head_stride + j;
+                    *reinterpret_cast<uint2*>(p) = make_uint2(kv_pack2<bf>(v.x, v.y), kv_pack2<bf>(v.z, v.w));
+                }
             }
+        if (half == 0) {
+            if (!whole) *reinterpret_cast<float2*>(f.part_ml + slot * 2) = make_float2(m, l);
+            else if (a.lse) a.lse[row_head] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
         }
-    if (half) return;
-    if (f.parts > 1) *reinterpret_cast<float2*>(f.part_ml + (part * all + row_head) * 2) = make_float2(m, l);
-    else if (a.lse) a.lse[row_head] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
+    }
+    if (!SHARED || last_part) return;
+    x += to - from;
+  }
 }
 
 // 16 unit rows in LDS as operands of the rotation: each of the workgroup's D / 32 wavefronts brings 32 coordinates of them
@@ -549,19 +631,45 @@ __global__ __launch_bounds__(D * 2) void k_kv_rotate_queries(KvRows q, const flo
     }
 }
 
-// Parts of a row's result (one for each share of its keys) put together: eight coordinates from j on, divided by the sum of
-// weights; lse where it is asked for.
+// Where a row's result is: parts in the shares first .. last of its head (one share: finished), row `row` of each part; last < 0: none,
+// because the row is of no sequence or past max_new.
+struct ManyPlace { int first, last, row; };
+template <bool SHARED>
+__device__ __forceinline__ ManyPlace many_place(const ManyArgs& f, int64_t row, int qhead) {
+    const KvAttend& a = f.a;
+    int lo = 0, hi = a.c.batch;                     // first sequence that begins after the row, minus one
+    if (a.c.starts) {
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (kv_int(a.c.starts, mid) <= row) lo = mid; else hi = mid;
+        }
+    } else {
+        lo = row < a.c.batch ? (int)row : 0;
+    }
+    int first, count;
+    kv_new_rows(a.c, lo, first, count);
+    const int64_t i = row - first;
+    if (i < 0 || i >= (count < a.max_new ? count : a.max_new)) return {0, -1, 0};
+    if constexpr (!SHARED) return {0, 0, 0};
+    const int col = (int)i * a.group + qhead % a.group, rt = col / kManyRows;
+    const int64_t size = f.begin[0], begin = f.begin[1 + lo * f.row_tiles + rt];
+    return {(int)(begin / size), (int)((begin + ManyRowTile(a, lo, rt).span.tiles - 1) / size), col % kManyRows};
+}
+
+// Parts of a row's result put together: eight coordinates from j on, divided by the sum of weights; lse where it is asked for.
 template <int D>
-__device__ __forceinline__ void many_join(const ManyArgs& f, int64_t i, int64_t all, int j, float (&x)[8], bool lse) {
+__device__ __forceinline__ void many_join(const ManyArgs& f, const ManyPlace& at, int64_t i, int j, float (&x)[8], bool lse) {
+    const int64_t h = i % f.a.q.heads / f.a.group;
+    auto slot = [&](int w) { return ((h * f.wgs + w) * 2 + (w == at.first)) * kManyRows + at.row; };
     float top = -INFINITY, l = 0.f;
-    for (int p = 0; p < f.parts; ++p) top = fmaxf(top, f.part_ml[(p * all + i) * 2]);
+    for (int w = at.first; w <= at.last; ++w) top = fmaxf(top, f.part_ml[slot(w) * 2]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    for (int p = 0; p < f.parts; ++p) {
-        const float2 u = *reinterpret_cast<const float2*>(f.part_ml + (p * all + i) * 2);
+    for (int w = at.first; w <= at.last; ++w) {
+        const float2 u = *reinterpret_cast<const float2*>(f.part_ml + slot(w) * 2);
         const float turn = u.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u.x - top);
-        const float4* w = reinterpret_cast<const float4*>(f.whole + (p * all + i) * D + j);
-        const float4 a = w[0], b = w[1];
+        const float4* p = reinterpret_cast<const float4*>(f.part + slot(w) * D + j);
+        const float4 a = p[0], b = p[1];
         l += u.y * turn;
         x[0] += a.x * turn; x[1] += a.y * turn; x[2] += a.z * turn; x[3] += a.w * turn;
         x[4] += b.x * turn; x[5] += b.y * turn; x[6] += b.z * turn; x[7] += b.w * turn;
@@ -572,51 +680,43 @@ __device__ __forceinline__ void many_join(const ManyArgs& f, int64_t i, int64_t 
     if (lse && f.a.lse) f.a.lse[i] = l > 0.f ? (top + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
 }
 
-// Rows that have a result: of a sequence, and not past max_new.
-__device__ __forceinline__ bool many_has(const KvAttend& a, int64_t row) {
-    if (!a.c.starts) return row < a.c.batch;
-    int lo = 0, hi = a.c.batch;                     // first sequence that begins after the row, minus one
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (kv_int(a.c.starts, mid) <= row) lo = mid; else hi = mid;
-    }
-    int first, count;
-    kv_new_rows(a.c, lo, first, count);
-    return row >= first && row < first + (count < a.max_new ? count : a.max_new);
-}
-
+// Rows whose tiles lie in more than one share.
 template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_many_join(ManyArgs f) {
     const KvRows& out = f.a.out;
     const int64_t all = (int64_t)out.rows * out.heads, u = (int64_t)blockIdx.x * 256 + threadIdx.x, i = u / (D / 8);
     const int j = (int)(u % (D / 8)) * 8;
-    if (i >= all || !many_has(f.a, i / out.heads)) return;
+    if (i >= all) return;
+    const ManyPlace at = many_place<true>(f, i / out.heads, (int)(i % out.heads));
+    if (at.last <= at.first) return;
     float x[8];
-    many_join<D>(f, i, all, j, x, j == 0);
+    many_join<D>(f, at, i, j, x, j == 0);
     constexpr bool bf = F == IVFTQ_KV_BF16;
     uint16_t* p = reinterpret_cast<uint16_t*>(out.data) + i / out.heads * out.row_stride + i % out.heads * out.head_stride + j;
     *reinterpret_cast<uintx4*>(p) = uintx4{kv_pack2<bf>(x[0], x[1]), kv_pack2<bf>(x[2], x[3]), kv_pack2<bf>(x[4], x[5]), kv_pack2<bf>(x[6], x[7])};
 }
 
 // Results back into the rows' own frame, split the same way.
-template <int D>
+template <int D, bool SHARED>
 __global__ __launch_bounds__(D * 2) void k_kv_rotate_back(ManyArgs f, int tiles) {
     __shared__ UnitRows<D> unit;
-    __shared__ bool has[16 * kTurnTiles];
+    __shared__ ManyPlace places[16 * kTurnTiles];
     const KvRows& out = f.a.out;
     const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int64_t all = (int64_t)out.rows * out.heads, first = (int64_t)blockIdx.x * tiles * 16;
-    for (int u = threadIdx.x; u < 16 * tiles; u += D * 2) has[u] = first + u < all && many_has(f.a, (first + u) / out.heads);
+    for (int u = threadIdx.x; u < 16 * tiles; u += D * 2)
+        places[u] = first + u < all ? many_place<SHARED>(f, (first + u) / out.heads, (int)((first + u) % out.heads)) : ManyPlace{0, -1, 0};
     const KvTurn<D, true> turn(f.a.c.rotation, wave);
     __syncthreads();
     for (int tile = 0; tile < tiles && first + tile * 16 < all; ++tile) {
         const int64_t i = first + tile * 16 + n;
-        const bool in = has[tile * 16 + n];
+        const ManyPlace at = places[tile * 16 + n];
+        const bool in = at.last >= 0;
         float x[8] = {}, y[8];
         if (in) {
             const int j = 32 * wave + 8 * g;
-            if (f.parts > 1) {
-                many_join<D>(f, i, all, j, x, j == 0);
+            if (SHARED && at.last > at.first) {
+                many_join<D>(f, at, i, j, x, j == 0);
             } else {
                 const float4* w = reinterpret_cast<const float4*>(f.whole + i * D + j);
                 const float4 a = w[0], b = w[1];
@@ -633,8 +733,8 @@ __global__ __launch_bounds__(D * 2) void k_kv_rotate_back(ManyArgs f, int tiles)
 
 // Sizes of the workspace's parts, as the launch and the caller's question see them.
 struct KvWork {
-    int64_t z, zn, whole, part, ml, bytes;
-    int32_t few, col_tiles, split, row_tiles, parts;
+    int64_t z, zn, whole, part, ml, begin, bytes;
+    int32_t few, col_tiles, split, row_tiles, shared;        // shared: workgroups a head that share its tiles, 0: one a row tile
 };
 KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity);
 
@@ -666,13 +766,17 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
         if (hipError_t e = low ? launch(&k_kv_few<F, D, codes>, fill_low) : launch(&k_kv_few<F, D, false>, fill)) return e;
         if (w.split || F == IVFTQ_KV_CODE4) k_kv_few_join<F, D><<<dim3(pairs, (unsigned)w.col_tiles), 512, 0, st>>>(f);
     } else {
-        ManyArgs f{a, z, zn, whole, ml, w.row_tiles, w.parts};
-        const unsigned wgs = pairs * (unsigned)w.row_tiles * (unsigned)w.parts;
-        // float16 results: the queries' second part matters beside the rounding of the result
-        if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4><<<wgs, 256, 0, st>>>(f);
-        else k_kv_many<F, D, false><<<wgs, 256, 0, st>>>(f);
-        if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D><<<rot, D * 2, 0, st>>>(f, tiles);
-        else if (w.parts > 1) k_kv_many_join<F, D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, st>>>(f);
+        const ManyArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), ml, reinterpret_cast<int64_t*>(a.work + w.begin), w.row_tiles, w.shared};
+        auto launch = [&](auto shared) {
+            constexpr bool S = decltype(shared)::value;
+            const unsigned wgs = S ? (unsigned)(a.c.heads * w.shared) : pairs * (unsigned)w.row_tiles;
+            // float16 results: the queries' second part matters beside the rounding of the result
+            if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4, S><<<wgs, 256, 0, st>>>(f);
+            else k_kv_many<F, D, false, S><<<wgs, 256, 0, st>>>(f);
+            if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D, S><<<rot, D * 2, 0, st>>>(f, tiles);
+            else if constexpr (S) k_kv_many_join<F, D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, st>>>(f);
+        };
+        if (w.shared) launch(std::true_type{}); else launch(std::false_type{});
     }
     return hipGetLastError();
 }
