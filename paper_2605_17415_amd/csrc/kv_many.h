@@ -130,7 +130,7 @@ struct ManyTile {
     // norms have four places: a tile's are written, a tile ahead, while others may still be at the tile before and read its own
     float key_gain[kCodes ? 4 : 1][kCodes ? kManyTile : 1], value_gain[kCodes ? 4 : 1][kCodes ? kManyTile : 1];
     float value_power[kCodes ? 4 : 1][4];      // of the quarters' largest norms
-    uint32_t odd[2][2];
+    alignas(8) uint16_t odd[2][4];             // masked tiles: tokens of each quarter with a value that is no finite number
 
     static __device__ __forceinline__ int turn(int t) { return kRow == 8 ? t >> 1 & 7 : t & 15; }
 };
@@ -445,7 +445,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     bring_keys(from + 1, next, 1);
     bring_values(from, now, 0);
     int32_t asked = ask(from + 2);
-    if (threadIdx.x < 4) lds.odd[threadIdx.x >> 1][threadIdx.x & 1] = 0;
     // the first tile's step begins with the product of weights of zero and the other buffer's values: those have to be numbers
     for (int u = threadIdx.x; u < kManyTile * D / 8; u += 256) *reinterpret_cast<uintx4*>(lds.values[1] + u * 16) = uintx4{0, 0, 0, 0};
     kv_loads_done();
@@ -483,34 +482,37 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         product_and_maximum(other, 1, p1, i, 0, full, (uint32_t)mine, s0);
         scores_and_weights(here, 1, s1, i, 0, full, (uint32_t)mine, s0, p0);
         kv_loads_done();
-        __syncthreads();
         if (!codes && !full) {
-            // What no row of the workgroup sees may be anything, and 0 * NaN is no zero: such values are set to zero in LDS.  So are
-            // values of no finite number that only some rows see; those rows get them one by one.
+            // What no row of the workgroup sees may be anything, and 0 * NaN is no zero: such values are set to zero in LDS, each quarter
+            // by the wavefront that has brought it, before the others read it.  So are values of no finite number that only some rows
+            // see; those rows get them one by one.
+            uint32_t found = 0;
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-                const int u = threadIdx.x + 256 * j;
-                const uint32_t bad = kv_not_finite<bf>(*reinterpret_cast<const uintx4*>(lds.values[here] + u * 16)) << 8 * (u / D & 3);
-                if (bad) atomicOr(&lds.odd[here][u / D / 4], bad);
+            for (int j = 0; j < D / 32; ++j)
+                found |= kv_not_finite<bf>(*reinterpret_cast<const uintx4*>(lds.values[here] + (wave * 2 * D + lane + 64 * j) * 16)) << 8 * ((lane + 64 * j) / D);
+            if (__ballot(found != 0)) {
+#pragma unroll
+                for (int w = 1; w < 64; w <<= 1) found |= __shfl_xor(found, w);
             }
-            __syncthreads();
-            const uint64_t found = (uint64_t)(uint32_t)kv_uniform((int)lds.odd[here][0]) | (uint64_t)(uint32_t)kv_uniform((int)lds.odd[here][1]) << 32;
-            dirty = found & shown;
-            const uint64_t keep = shown & ~found;
-            if (~keep) {
+            found = kv_uniform((int)found);
+            if (lane == 0) lds.odd[here][wave] = (uint16_t)found;
+            const uint32_t keep = (uint32_t)(shown >> 16 * wave) & ~found;
+            if (~keep & 0xffffu) {
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) {
-                    const int u = threadIdx.x + 256 * j;
-                    const uint32_t bits = (uint32_t)(keep >> 8 * (u / D));
-                    uintx4* p = reinterpret_cast<uintx4*>(lds.values[here] + u * 16);
+                    const uint32_t bits = keep >> 8 * ((lane + 64 * j) / D);
+                    uintx4* p = reinterpret_cast<uintx4*>(lds.values[here] + (wave * 2 * D + lane + 64 * j) * 16);
                     uintx4 w = *p;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] &= (bits >> 2 * e & 1 ? 0xffffu : 0u) | (bits >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
                     *p = w;
                 }
             }
-            __syncthreads();
-            if (threadIdx.x < 2) lds.odd[here][threadIdx.x] = 0;          // for the tile after the next
+        }
+        __syncthreads();
+        if (!codes && !full) {
+            const uint32_t* odd = reinterpret_cast<const uint32_t*>(lds.odd[here]);
+            dirty = ((uint64_t)(uint32_t)kv_uniform((int)odd[0]) | (uint64_t)(uint32_t)kv_uniform((int)odd[1]) << 32) & shown;
             if ((uint32_t)dirty) singly(t0, 0, (uint32_t)dirty, s0);
         }
         if constexpr (!codes) {
@@ -743,7 +745,10 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
     uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
     float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole), *ml = reinterpret_cast<float*>(a.work + w.ml);
     const int64_t all = (int64_t)a.q.rows * a.q.heads;
-    const int tiles = all >= 16384 ? kTurnTiles : 1;     // a workgroup's 16-row tiles: few rows are spread, many share the rotation's operands
+    // a workgroup's 16-row tiles: many rows share the rotation's operands, where that leaves three workgroups a compute unit (27,000 rows
+    // of 128, eight tiles each: 18 us there and 33 us back)
+    const int64_t fill = all / (16 * 768);
+    const int tiles = fill < 1 ? 1 : (fill < kTurnTiles ? (int)fill : kTurnTiles);
     const unsigned rot = (unsigned)((all + 16 * tiles - 1) / (16 * tiles));
     if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_queries<D><<<rot, D * 2, 0, st>>>(a.q, a.c.rotation, z, zn, tiles);
     const unsigned pairs = (unsigned)(a.c.batch * a.c.heads);
