@@ -134,23 +134,18 @@ __device__ __forceinline__ halfx8 kv_levels8(uint32_t w, const KvView& c) {
 // Place of half byte i in that order.
 __device__ __forceinline__ constexpr int kv_slot(int i) { return (i & 1) * 4 + (i >> 1); }
 
-__device__ __forceinline__ float kv_level(uint32_t nibble, const KvView& c) {
-    const int m = nibble & 7;
-    const float v = m < 4 ? (m < 2 ? (m ? c.level[1] : c.level[0]) : (m == 2 ? c.level[2] : c.level[3]))
-                          : (m < 6 ? (m == 4 ? c.level[4] : c.level[5]) : (m == 6 ? c.level[6] : c.level[7]));
-    return nibble & 8 ? -v : v;
-}
-
 // Signs and magnitudes of the levels next to eight values (no number: magnitude 0): three comparisons each, every one against
 // the boundary that the one before leaves; a word's bits are shifted in from its top by additions with carry.
 __device__ __forceinline__ uint32_t kv_nibbles8(const float (&y)[8], const KvView& c) {
+    // (copies: a choice between elements of the argument would be branches around its reads)
+    const float t0 = c.bound[0], t1 = c.bound[1], t2 = c.bound[2], t3 = c.bound[3], t4 = c.bound[4], t5 = c.bound[5], t6 = c.bound[6];
     uint32_t w = 0;
 #pragma unroll
     for (int e = 7; e >= 0; --e) {
         const float a = __builtin_fabsf(y[e]);
-        const bool b2 = a >= c.bound[3];
-        const bool b1 = a >= (b2 ? c.bound[5] : c.bound[1]);
-        const bool b0 = a >= (b2 ? (b1 ? c.bound[6] : c.bound[4]) : (b1 ? c.bound[2] : c.bound[0]));
+        const bool b2 = a >= t3, b1 = a >= (b2 ? t5 : t1);
+        const float high = b1 ? t6 : t4, low = b1 ? t2 : t0;
+        const bool b0 = a >= (b2 ? high : low);
         w = w + w + (y[e] < 0.f);
         w = w + w + b2;
         w = w + w + b1;
@@ -235,33 +230,46 @@ __device__ __forceinline__ float kv_unit_row(float (&x)[D / 32][8]) {
 // sixteen lanes' reads down a column of Pi are neighbours.  Both sides go in as sums of two float16 numbers, three products:
 // y is good to about 2^-21 of the row's length, far under the distance of two levels; one product alone would move one code
 // in two thousand.
+// What it reads of Pi: asked for early where a chain of other loads comes first.
 template <int D, bool TRANSPOSED>
-struct KvTurn {
-    halfx8 hi[2][D / 32], lo[2][D / 32];
-    __device__ __forceinline__ KvTurn(const float* __restrict__ pi, int block) {
+struct KvTurnRows {
+    float p[2][D / 32][8];
+    __device__ __forceinline__ KvTurnRows(const float* __restrict__ pi, int block) {
         const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int i = 32 * block + (TRANSPOSED ? 16 * half + m : 8 * (m >> 2) + 4 * half + (m & 3));
 #pragma unroll
             for (int s = 0; s < D / 32; ++s) {
-                float p[8];
+                float(&x)[8] = p[half][s];
                 if constexpr (TRANSPOSED) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = pi[(32 * s + 8 * g + e) * D + i];
+                    for (int e = 0; e < 8; ++e) x[e] = pi[(32 * s + 8 * g + e) * D + i];
                 } else {
                     const float4* r = reinterpret_cast<const float4*>(pi + i * D + 32 * s + 8 * g);
                     const float4 u = r[0], w = r[1];
-                    p[0] = u.x; p[1] = u.y; p[2] = u.z; p[3] = u.w; p[4] = w.x; p[5] = w.y; p[6] = w.z; p[7] = w.w;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = p[e] * kSplitScale;
-                    hi[half][s][e] = (_Float16)v;
-                    lo[half][s][e] = (_Float16)(v - (float)hi[half][s][e]);
+                    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
                 }
             }
         }
+    }
+};
+
+template <int D, bool TRANSPOSED>
+struct KvTurn {
+    halfx8 hi[2][D / 32], lo[2][D / 32];
+    __device__ __forceinline__ KvTurn(const float* __restrict__ pi, int block) : KvTurn(KvTurnRows<D, TRANSPOSED>(pi, block)) {}
+    __device__ __forceinline__ explicit KvTurn(const KvTurnRows<D, TRANSPOSED>& rows) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = rows.p[half][s][e] * kSplitScale;
+                    hi[half][s][e] = (_Float16)v;
+                    lo[half][s][e] = (_Float16)(v - (float)hi[half][s][e]);
+                }
     }
     __device__ __forceinline__ void operator()(const float (&x)[D / 32][8], float (&y)[8]) const {
         floatx4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -274,13 +282,15 @@ struct KvTurn {
                 h[e] = (_Float16)v;
                 l[e] = (_Float16)(v - (float)h[e]);
             }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], h, acc[half], 0, 0, 0);
-                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], l, acc[half], 0, 0, 0);
-                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[half][s], h, acc[half], 0, 0, 0);
-            }
+            product(h, l, s, acc);
         }
+        finish(acc, y);
+    }
+    // Rows in two parts.
+    __device__ __forceinline__ void operator()(const halfx8 (&h)[D / 32], const halfx8 (&l)[D / 32], float (&y)[8]) const {
+        floatx4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) product(h[s], l[s], s, acc);
         finish(acc, y);
     }
     // Rows that stand in LDS as two parts already (rows.hi[block][lane], rows.lo).
@@ -290,15 +300,17 @@ struct KvTurn {
         floatx4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) {
-            const halfx8 h = rows.hi[s][lane], l = rows.lo[s][lane];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], h, acc[half], 0, 0, 0);
-                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], l, acc[half], 0, 0, 0);
-                acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[half][s], h, acc[half], 0, 0, 0);
-            }
+            product(rows.hi[s][lane], rows.lo[s][lane], s, acc);
         }
         finish(acc, y);
+    }
+    __device__ __forceinline__ void product(const halfx8& h, const halfx8& l, int s, floatx4 (&acc)[2]) const {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], h, acc[half], 0, 0, 0);
+            acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[half][s], l, acc[half], 0, 0, 0);
+            acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[half][s], h, acc[half], 0, 0, 0);
+        }
     }
     __device__ __forceinline__ void finish(const floatx4 (&acc)[2], float (&y)[8]) const {
 #pragma unroll

@@ -193,13 +193,12 @@ __global__ __launch_bounds__(256) void k_kv_tiles16(KvView c, KvRows k, KvRows v
 
 // A 16-bit row in the operand layout: x[s][e] = coordinate 32 s + 8 (lane / 16) + e.
 template <int D, bool BF>
-__device__ __forceinline__ void load_row(const KvRows& x, int64_t row, int64_t head, bool valid, float (&v)[D / 32][8]) {
+__device__ __forceinline__ void load_row(const KvRows& x, int64_t row, int64_t head, float (&v)[D / 32][8]) {
     const int g = (threadIdx.x & 63) >> 4;
     const uint16_t* p = reinterpret_cast<const uint16_t*>(x.data) + row * x.row_stride + head * x.head_stride + 8 * g;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
-        uintx4 w = {0, 0, 0, 0};
-        if (valid) w = *reinterpret_cast<const uintx4*>(p + 32 * s);
+        const uintx4 w = *reinterpret_cast<const uintx4*>(p + 32 * s);
 #pragma unroll
         for (int e = 0; e < 4; ++e) { v[s][2 * e] = kv_to_float<BF>(w[e] & 0xffff); v[s][2 * e + 1] = kv_to_float<BF>(w[e] >> 16); }
     }
@@ -214,15 +213,16 @@ __global__ __launch_bounds__(64) void k_kv_append_row_codes(KvView c, KvRows k, 
     const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
     const bool value = blockIdx.y >= D / 32;
     const int block = blockIdx.y % (D / 32);
-    const int64_t i = (int64_t)blockIdx.x * 16 + n;
-    const bool in = i < (int64_t)c.rows * c.heads;
-    const int r = in ? (int)(i / c.heads) : 0, h = in ? (int)(i % c.heads) : 0;
+    const uint32_t i = blockIdx.x * 16u + n;                 // rows * heads is under 2^31
+    const bool in = i < (uint32_t)c.rows * (uint32_t)c.heads;
+    const int r = in ? (int)(i / (uint32_t)c.heads) : 0, h = in ? (int)(i % (uint32_t)c.heads) : 0;
+    const KvTurnRows<D, false> pi(c.rotation, block);
     float x[D / 32][8], y[8];
-    load_row<D, BF>(value ? v : k, r, h, in, x);
+    load_row<D, BF>(value ? v : k, r, h, x);          // (of lanes past the end: the first row, not used)
     const float norm = kv_unit_row<D>(x);
-    KvTurn<D, false>(c.rotation, block)(x, y);
     int t = 0;
     char* rec = in ? place_of(c, r, h, t) : nullptr;
+    KvTurn<D, false>{pi}(x, y);
     if (!rec) return;
     const int codes = c.page * (D / 2), j = 32 * block + 8 * g;
     if (g == 0 && block == 0) reinterpret_cast<_Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t] = (_Float16)norm;
@@ -239,46 +239,17 @@ __global__ __launch_bounds__(64) void k_kv_append_row_codes(KvView c, KvRows k, 
     }
 }
 
-// The rows that the codes stand for: levels, rotated back, times the norm.  Split the same way.
-template <int D, bool BF>
-__global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, KvRows v) {
-    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
-    const bool value = blockIdx.y >= D / 32;
-    const int block = blockIdx.y % (D / 32);
-    const int64_t i = (int64_t)blockIdx.x * 16 + n;
-    const bool in = i < (int64_t)c.rows * c.heads;
-    const int r = in ? (int)(i / c.heads) : 0, h = in ? (int)(i % c.heads) : 0;
-    int t = 0;
-    const char* rec = in ? place_of(c, r, h, t) : nullptr;
-    const int codes = c.page * (D / 2);
-    float x[D / 32][8], y[8], norm = 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-        const int j = 32 * s + 8 * g;
-        uint32_t w = 0;
-        if (rec && !value) w = reinterpret_cast<const uint32_t*>(rec + (int64_t)t * (D / 2))[j / 8];
-        if (rec && value) {
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(rec + codes) + (int64_t)(t >> 3) * D + j;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w |= (p[e] >> 4 * (t & 7) & 15) << 4 * e;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] = kv_level(w >> 4 * e & 15, c);
-    }
-    if (rec) norm = (float)reinterpret_cast<const _Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t];
-    KvTurn<D, true>(c.rotation, block)(x, y);
-    if (!in) return;
-    kv_store_turned(value ? v : k, r, h, block, y, norm);
-}
-
-// 8 x 8 half bytes over eight neighbouring lanes, turned: lane i's half byte e becomes lane e's half byte i.
+// 8 x 8 half bytes over eight neighbouring lanes, turned: lane i's half byte e becomes lane e's half byte i.  Exchanges inside a row of lanes
+// (a lane 4 away: mirrored over eight, then over four), and byte permutations whose selectors depend on the lane.
+template <int CTRL>
+__device__ __forceinline__ uint32_t lanes_moved(uint32_t w) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)w, CTRL, 0xf, 0xf, true); }
 __device__ __forceinline__ uint32_t turn_nibbles(uint32_t w, int lane) {
-    uint32_t p = __shfl_xor(w, 4);
-    w = lane & 4 ? (w & 0xffff0000u) | p >> 16 : (w & 0xffffu) | p << 16;
-    p = __shfl_xor(w, 2);
-    w = lane & 2 ? (w & 0xff00ff00u) | (p >> 8 & 0x00ff00ffu) : (w & 0x00ff00ffu) | (p << 8 & 0xff00ff00u);
-    p = __shfl_xor(w, 1);
-    return lane & 1 ? (w & 0xf0f0f0f0u) | (p >> 4 & 0x0f0f0f0fu) : (w & 0x0f0f0f0fu) | (p << 4 & 0xf0f0f0f0u);
+    const uint32_t by4 = lane & 4 ? 0x03020706u : 0x05040100u, by2 = lane & 2 ? 0x03070105u : 0x06020400u;
+    const uint32_t keep = lane & 1 ? 0xf0f0f0f0u : 0x0f0f0f0fu, right = lane & 1 ? 4u : 28u;
+    w = __builtin_amdgcn_perm(lanes_moved<0x1b>(lanes_moved<0x141>(w)), w, by4);
+    w = __builtin_amdgcn_perm(lanes_moved<0x4e>(w), w, by2);
+    const uint32_t p = lanes_moved<0xb1>(w);
+    return (w & keep) | (__builtin_amdgcn_alignbit(p, p, right) & ~keep);
 }
 
 // The eight levels, times 2^10, as two float16 parts that keep them to 2^-22: byte tables like those of kv_levels8, the second
@@ -316,6 +287,52 @@ __device__ __forceinline__ void kv_exact8(uint32_t w, const KvExact& x, halfx8& 
     }
     hi = __builtin_bit_cast(halfx8, r[0]);
     lo = __builtin_bit_cast(halfx8, r[1]);
+}
+
+// The rows that the codes stand for, one per sequence: levels, rotated back, times the norm.  Split as k_kv_append_row_codes is; what the
+// rotation is read from is asked for before the chain length, table entry, words, and lanes without a page read page 0.
+template <int D, bool BF>
+__global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, KvRows v, KvExact exact) {
+    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+    const bool value = blockIdx.y >= D / 32;
+    const int block = blockIdx.y % (D / 32);
+    const uint32_t i = blockIdx.x * 16u + n;                 // rows * heads is under 2^31
+    const bool in = i < (uint32_t)c.rows * (uint32_t)c.heads;
+    const int r = in ? (int)(i / (uint32_t)c.heads) : 0, h = in ? (int)(i % (uint32_t)c.heads) : 0;
+    const KvTurnRows<D, true> pi(c.rotation, block);
+    int t = 0;
+    const char* const place = place_of(c, r, h, t);
+    const char* const rec = place ? place : kv_record(c, 0, h);
+    const int codes = c.page * (D / 2);
+    const _Float16 norm = reinterpret_cast<const _Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t];
+    uint32_t w[D / 32];
+    if (!value) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(rec + (int64_t)t * (D / 2)) + g;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) w[s] = p[4 * s];
+    } else {
+        const uintx4* p = reinterpret_cast<const uintx4*>(reinterpret_cast<const uint32_t*>(rec + codes) + (int64_t)(t >> 3) * D + 8 * g);
+        uintx4 u[D / 32][2];
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) { u[s][0] = p[8 * s]; u[s][1] = p[8 * s + 1]; }
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            w[s] = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[s] |= (u[s][e >> 2][e & 3] >> 4 * (t & 7) & 15) << 4 * e;
+        }
+    }
+    halfx8 hi[D / 32], lo[D / 32];
+    float y[8];
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+        kv_exact8(w[s], exact, hi[s], lo[s]);
+        hi[s] = __builtin_shufflevector(hi[s], hi[s], 0, 4, 1, 5, 2, 6, 3, 7);
+        lo[s] = __builtin_shufflevector(lo[s], lo[s], 0, 4, 1, 5, 2, 6, 3, 7);
+    }
+    KvTurn<D, true>{pi}(hi, lo, y);
+    if (!in) return;
+    kv_store_turned(value ? v : k, r, h, block, y, place ? (float)norm : 0.f);
 }
 
 // Several rows a sequence.  The rotation stands in LDS as two float16 parts in operand order, so that reading it costs 64
@@ -415,8 +432,8 @@ __global__ __launch_bounds__(kTileThreads, D <= 128 ? 4 : 2) void k_kv_tiles_cod
     if (READ && out0 == 0) no_place(c, k, v, D);
     for (int u = threadIdx.x; u < NT * 2 * NS * 64; u += kTileThreads) {
         const int l = u & 63, s = u / 64 % NS, half = u / 64 / NS & 1, t = u / 64 / NS / 2, m = l & 15;
-        // a lane's results: coordinates out0 + g * outputs / 4 + 8 t + 4 half + (0 .. 3)
-        const int i = out0 + (m >> 2) * (kOutputs<D> / 4) + 8 * t + 4 * half + (m & 3), k0 = 32 * s + 8 * (l >> 4);
+        // a lane's results: coordinates out0 + 32 t + 8 g + 4 half + (0 .. 3), so that the four lanes of a row write neighbouring pieces
+        const int i = out0 + 32 * t + 8 * (m >> 2) + 4 * half + (m & 3), k0 = 32 * s + 8 * (l >> 4);
         halfx8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -485,7 +502,7 @@ __global__ __launch_bounds__(kTileThreads, D <= 128 ? 4 : 2) void k_kv_tiles_cod
 #pragma unroll
                     for (int r = 0; r < 4; ++r) y[ct][4 * half + r] = acc[ct][r] * gain[ct];
             }
-            const int j = out0 + g * (kOutputs<D> / 4) + 8 * t;
+            const int j = out0 + 32 * t + 8 * g;
 #pragma unroll
             for (int ct = 0; ct < 2; ++ct) {
                 const int at = (t0 + 16 * ct + n) & (c.page - 1);
@@ -553,7 +570,7 @@ hipError_t codes(const KvView& c, const KvRows& k, const KvRows& v, bool read, h
         return tiles_codes<D, BF, false>(c, k, v, st);
     }
     const dim3 grid((unsigned)(((int64_t)c.rows * c.heads + 15) / 16), 2 * (D / 32));
-    if (read) k_kv_read_row_codes<D, BF><<<grid, 64, 0, st>>>(c, k, v); else k_kv_append_row_codes<D, BF><<<grid, 64, 0, st>>>(c, k, v);
+    if (read) k_kv_read_row_codes<D, BF><<<grid, 64, 0, st>>>(c, k, v, kv_exact(c)); else k_kv_append_row_codes<D, BF><<<grid, 64, 0, st>>>(c, k, v);
     return hipGetLastError();
 }
 
