@@ -90,7 +90,8 @@ ivftq_status ivftq_kv_read(const ivftq_kv_cache* cache, const ivftq_kv_rows* k_o
  * position p = lengths[b] - n + i and sees the tokens t <= p with window == 0 or t > p - window or t < sinks.
  *     out = sum_t e^(scale <q, k_t> - max) v_t / sum_t e^(scale <q, k_t> - max)
  * A row that sees nothing gives zeros (lse: -infinity).  lse, NULL or rows x (heads * group) floats: the natural logarithm of
- * the sum of e^(scale <q, k_t>).  max_new: no sequence has more new rows than this (>= 1; rows beyond it get no result).
+ * the sum of e^(scale <q, k_t>).  max_new: no sequence has more new rows than this (>= 1; rows beyond it get no result;
+ * starts NULL: taken as 1, which is then what the workspace is asked for with).
  * workspace: ivftq_kv_attend_workspace bytes, 256-byte aligned, its content does not matter. */
 ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse,
                              const int32_t* starts, int32_t max_new, int32_t window, int32_t sinks, float scale,

@@ -193,6 +193,7 @@ ivftq_status move_rows(const ivftq_kv_cache* cache, const ivftq_kv_rows* k, cons
     if (ivftq_status e = check_rows(k, read ? "k_out" : "k", cache->heads, cache->d, cache, starts)) return e;
     if (ivftq_status e = check_rows(v, read ? "v_out" : "v", cache->heads, cache->d, cache, starts)) return e;
     if (k->rows != v->rows || k->type != v->type) return refuse(IVFTQ_INVALID_ARG, "keys and values have one number of rows and one type");
+    if (!starts && k->rows * cache->heads > INT32_MAX / (cache->d / 8)) return refuse(IVFTQ_UNSUPPORTED, "%lld rows of %d heads in one call", (long long)k->rows, cache->heads);
     if (!k->rows || !cache->batch) return IVFTQ_OK;
     const KvView c = view_of(*cache, starts, k->rows, false);
     const hipStream_t st = static_cast<hipStream_t>(stream);

@@ -481,7 +481,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
         }
         product_and_maximum(other, 1, p1, i, 0, full, (uint32_t)mine, s0);
         scores_and_weights(here, 1, s1, i, 0, full, (uint32_t)mine, s0, p0);
-        kv_loads_done();
+        if constexpr (!codes) kv_loads_done();
         if (!codes && !full) {
             // What no row of the workgroup sees may be anything, and 0 * NaN is no zero: such values are set to zero in LDS, each quarter
             // by the wavefront that has brought it, before the others read it.  So are values of no finite number that only some rows

@@ -219,6 +219,8 @@ def kv_attend(q, pool, table, lengths, starts=None, max_new=1, window=0, sinks=0
         if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous float32 matrix of rows x query heads")
     first = _starts(starts, table, pool)
+    if starts is None and max_new > 1:
+        max_new = 1
     need = lib.ivftq_kv_attend_workspace(cache, q.shape[0], q.shape[1], max_new)
     if need < 0:
         _check(1)

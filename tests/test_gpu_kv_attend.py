@@ -388,3 +388,24 @@ def test_norms_of_any_size(kind, new, power):
         q = q.bfloat16()
     out, lse = run(c, q, [new, new])
     ref.check_attention(c, q.cpu(), out, [new, new], lse=lse)
+
+
+@pytest.mark.parametrize("form,kind", FORMS[1:])
+def test_more_row_tiles_than_lanes_share_the_workgroups(form, kind):
+    """Shares are found by scans over all row tiles, 96 here, among them rows that see nothing and a sequence without rows."""
+    lens, news = [3000, 100, 0, 1500], [3000, 100, 3, 700]
+    c = ref.Cache(23, form, 1, 64, 64, lens)
+    q = queries(23, sum(news), 1, 64, ref.TYPES[kind])
+    out, lse = run(c, q, news)
+    ref.check_attention(c, q.cpu(), out, news, lse=lse)
+    again, _ = run(c, q, news)
+    assert torch.equal(out, again)
+
+
+def test_without_starts_one_row_a_sequence_whatever_max_new_says():
+    c = ref.Cache(24, "bf16", 1, 64, 16, [900, 30])
+    t, _ = c.device()
+    q = queries(24, 2, 4, 64, torch.bfloat16)
+    out = _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], max_new=500)
+    torch.cuda.synchronize()
+    ref.check_attention(c, q.cpu(), out, [1, 1])

@@ -96,6 +96,14 @@ def test_bad_rows_are_refused(lib, change):
         assert lib.ivftq_kv_attend(C.byref(c), C.byref(k), C.byref(v), None, None, 1, 0, 0, 0.1, HERE, 1 << 40, None) == 1
 
 
+def test_more_pieces_of_rows_than_a_launch_counts_are_refused(lib):
+    """One row per sequence: 2^28 heads of 8 pieces of eight coordinates."""
+    c = cache(format=kv.BF16, batch=1 << 20, heads=256, d=64, columns=1, table_stride=1)
+    r = rows(row_stride=256 * 64, head_stride=64, rows=1 << 20, heads=256)
+    assert lib.ivftq_kv_append(C.byref(c), C.byref(r), C.byref(r), None, None) == 6
+    assert lib.ivftq_kv_read(C.byref(c), C.byref(r), C.byref(r), None, None) == 6
+
+
 def test_types_of_rows_and_cache(lib):
     c = cache(format=kv.F16)
     assert lib.ivftq_kv_append(C.byref(c), C.byref(rows()), C.byref(rows()), None, None) == 1            # bfloat16 into a float16 cache
