@@ -11,6 +11,10 @@
 // Work is cut by tiles, not by sequences: the tiles of all (sequence, head) pairs, one after the other, are dealt to the
 // workgroups in equal consecutive shares.  A pair that lies whole in a share is finished there; of the others each
 // workgroup leaves at most two parts (one at its start, one at its end), which k_kv_few_join puts together.
+//
+// Measured: 48 sequences of up to 9,000 tokens, 8 heads of 128 in bfloat16, four query heads each: 157 us for 912 MB (5.8 TB/s, the
+// rate of a read).  Four of 131,000 in codes, eight query heads each: 70 us for 328 MB (4.7 TB/s); there 263 vector
+// instructions a tile take 63 % of the cycles, 224 of them make levels of codes.
 #pragma once
 #include "kv_kernels.h"
 
