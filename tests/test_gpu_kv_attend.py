@@ -409,3 +409,37 @@ def test_without_starts_one_row_a_sequence_whatever_max_new_says():
     out = _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], max_new=500)
     torch.cuda.synchronize()
     ref.check_attention(c, q.cpu(), out, [1, 1])
+
+
+@pytest.mark.parametrize("form,kind", FORMS[1:])
+def test_a_chunk_in_a_graph(form, kind):
+    """Rows written and attended over many keys, captured once and replayed with other lengths and rows; eager work between the replays."""
+    pkg = _pkg()
+    news = [90, 40]
+    c = ref.Cache(25, form, 2, 64, 16, [1600, 900])
+    t, codec = c.device()
+    dtype = ref.TYPES[kind]
+    q, k, v = queries(1, sum(news), 4, 64, dtype), queries(2, sum(news), 2, 64, dtype), queries(3, sum(news), 2, 64, dtype)
+    out, lse, starts = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV), starts_of(news)
+
+    def step(pool):
+        pkg.kv_append(pool, k, v, t["table"], t["lengths"], starts=starts, **codec)
+        pkg.kv_attend(q, pool, t["table"], t["lengths"], starts=starts, max_new=90, window=700, sinks=3, out=out, lse=lse, **codec)
+
+    step(t["pool"])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(t["pool"])
+    for n, lens in enumerate(([1600, 900], [95, 40], [1111, 899])):
+        t["lengths"].copy_(torch.tensor(lens, dtype=torch.int32))
+        for x, seed in ((q, 40), (k, 50), (v, 60)):
+            x.copy_(queries(seed + n, x.shape[0], x.shape[1], 64, dtype))
+        torch.cuda.synchronize()
+        other = t["pool"].clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        step(other)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out) and torch.equal(got[1], lse) and torch.equal(other, t["pool"])
