@@ -9,9 +9,9 @@
 // Two workgroups a compute unit, which are not in step; inside a wavefront the products of one half tile stand between the
 // exponentials of another.
 //
-// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8, window 4,096, bfloat16: 437 us, 0.94 PFLOP/s (an 8192^3 library
-// product: 1.18), products 47 % of the cycles and vector instructions 41 %.  Chunks of 512 rows over 20,000 tokens in codes:
-// 0.6 PFLOP/s, vector instructions 51 %, a third of them for the levels, products 27 %.
+// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8, window 4,096, bfloat16: 435 us, 0.95 PFLOP/s (an 8192^3 library
+// product: 1.18), products 48 % of the cycles and vector instructions 42 %.  Chunks of 512 rows over 20,000 tokens in codes: 429 us,
+// 0.63 PFLOP/s, vector instructions 54 %, a third of them for the levels, products 28 %.
 #pragma once
 #include <type_traits>
 
