@@ -82,6 +82,9 @@ struct ManyRowTile {
 // after the other, are dealt out in equal consecutive shares, as in kv_few.h: a row tile that lies whole in a share is finished there, of
 // the others each workgroup leaves at most two parts.  (Chunks of two sequences over 20,000 and 12,000 tokens in codes: the call
 // 505 us with every row tile's keys cut in two, the longer sequence's workgroups last, and 474 us in equal shares; 737 us uncut.)
+// Shares of few tiles are not worth their search and their parts (a prompt of 3,000 tokens, 94 row tiles a head, 35 tiles a share: 187
+// us in shares, 102 us uncut); only the device knows the lengths, so it decides.
+constexpr int kLeastShare = 64;
 struct ManyShare { int64_t size; int b, rt, from, to; int64_t begin; };       // from, to: tiles of the row tile; begin: its first one's place
 
 // The part of share `w` from its tile `x` on (x < size); to == from where there is none.
@@ -100,7 +103,15 @@ __device__ __forceinline__ ManyShare many_share(const KvAttend& a, int row_tiles
     int64_t total = 0;
     for (int e0 = 0; e0 < items; e0 += 64) total += scan(e0);
     ManyShare s{(total + wgs - 1) / wgs, 0, 0, 0, 0, 0};
-    if (s.size < 8) s.size = 8;
+    if (s.size < kLeastShare) {                       // a row tile a workgroup, those with the longest reach first; all lie in one share
+        s.size = (int64_t)1 << 60;
+        if (x == 0 && w < items) {
+            s.b = w % a.c.batch;
+            s.rt = row_tiles - 1 - w / a.c.batch;
+            s.to = ManyRowTile(a, s.b, s.rt).span.tiles;
+        }
+        return s;
+    }
     const int64_t at = w * s.size + x, end = (w + 1) * s.size < total ? (w + 1) * s.size : total;
     int64_t base = 0;
     for (int e0 = 0; at < end && e0 < items; e0 += 64) {
@@ -232,11 +243,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     bool last_part = true;
     if constexpr (SHARED) {
         const ManyShare now = many_share(a, f.row_tiles, f.wgs, share, x);
+        if (threadIdx.x == 0 && blockIdx.x == 0 && x == 0) f.begin[0] = now.size;
         if (now.from >= now.to) return;
         b = now.b; rt = now.rt; from = now.from; to = now.to;
         if (threadIdx.x == 0 && h == 0 && from == 0) f.begin[1 + b * f.row_tiles + rt] = now.begin;
-        if (threadIdx.x == 0 && blockIdx.x == 0) f.begin[0] = now.size;
-        last_part = x + (to - from) >= now.size;
+        last_part = x + (to - from) >= now.size || now.size > (int64_t)1 << 59;
         if (x) __syncthreads();                  // LDS is no longer read
     } else {
         b = share % c.batch;
@@ -787,7 +798,8 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
         const ManyArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), ml, reinterpret_cast<int64_t*>(a.work + w.begin), w.row_tiles, w.shared};
         auto launch = [&](auto shared) {
             constexpr bool S = decltype(shared)::value;
-            const unsigned wgs = S ? (unsigned)(a.c.heads * w.shared) : pairs * (unsigned)w.row_tiles;
+            // shares: workgroups for either way
+            const unsigned one_each = pairs * (unsigned)w.row_tiles, wgs = S && one_each < (unsigned)(a.c.heads * w.shared) ? (unsigned)(a.c.heads * w.shared) : one_each;
             // float16 results: the queries' second part matters beside the rounding of the result
             if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4, S><<<wgs, 256, 0, st>>>(f);
             else k_kv_many<F, D, false, S><<<wgs, 256, 0, st>>>(f);

@@ -443,3 +443,37 @@ def test_a_chunk_in_a_graph(form, kind):
         step(other)
         torch.cuda.synchronize()
         assert torch.equal(got[0], out) and torch.equal(got[1], lse) and torch.equal(other, t["pool"])
+
+
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("d", (64, 128))
+def test_row_tiles_in_shares_agree_with_few_rows(form, kind, d):
+    """Enough keys a head that its row tiles are dealt out in shares of more than 64 tiles, most of them cut: the last rows against the
+    kernel of few rows, as in test_both_kernels_agree."""
+    pkg = _pkg()
+    heads, group, page, lens, news = 32, 4, 64, [20_000, 3000], [100, 40]
+    need = [-(-n // page) for n in lens]
+    g = torch.Generator(device=DEV).manual_seed(d)
+    table = torch.full((2, max(need)), -1, dtype=torch.int32, device=DEV)
+    order = torch.randperm(sum(need), generator=g, device=DEV).int()
+    table[0], table[1, :need[1]] = order[:need[0]], order[need[0]:]
+    codec = {}
+    if form == "code4":
+        pool = torch.randint(0, 256, (sum(need), heads, page * (d + 4)), generator=g, device=DEV, dtype=torch.uint8)
+        norms = ((torch.rand(sum(need), heads, 2 * page, generator=g, device=DEV) + 0.5) * math.sqrt(d)).half()
+        pool[..., page * d:] = norms.view(torch.uint8)
+        codec = {"rotation": torch.from_numpy(pkg.ivftq_haar_rotation(d, 3)).to(DEV), "levels": pkg.ivftq_build_codebook(4, d)[0]}
+    else:
+        pool = torch.randn(sum(need), heads, 2, page, d, generator=g, device=DEV).to(ref.TYPES[form])
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    q = queries(d, sum(news), heads * group, d, ref.TYPES[kind])
+    last = 3
+    rows = torch.cat([torch.arange(e - last, e) for e in np.cumsum(news)]).to(DEV)
+    logs, few_logs = torch.empty(q.shape[:2], device=DEV), torch.empty(2 * last, heads * group, device=DEV)
+    few = pkg.kv_attend(q[rows], pool, table, lengths, starts=starts_of([last] * 2), max_new=last, lse=few_logs, **codec)
+    many = pkg.kv_attend(q, pool, table, lengths, starts=starts_of(news), max_new=max(news), lse=logs, **codec)
+    torch.cuda.synchronize()
+    far, size = (many[rows].double() - few.double()).norm(dim=-1), few.double().norm(dim=-1)
+    step = 2.0 ** -11 if form == "code4" else ref.HALF[few.dtype]
+    assert (far <= (2 * ref.HALF[few.dtype] + 5 * step) * size + 2.0 ** -18 * math.sqrt(d)).all(), float((far / size).max())
+    assert (logs[rows] - few_logs).abs().max() <= 1e-4
