@@ -50,7 +50,7 @@ struct FewArgs {
 struct FewSeq {
     int first, count;                 // first new row, new rows that are computed
     int base, end;                    // position of the first new row, one past the last one's
-    int low, beyond;                  // first token that the window of the earliest new row shows; last one outside that of the latest
+    int low, beyond;                  // first token that the window of the earliest new row shows; last one outside that of the latest (-1: none)
     int sink_tiles, window_tile, tiles;
 };
 
@@ -63,7 +63,7 @@ __device__ __forceinline__ FewSeq few_seq(const KvAttend& a, int b) {
     s.end = s.base + s.count > 0 ? s.base + s.count : 0;
     const int64_t low = a.window ? (int64_t)s.base - a.window + 1 : 0;
     s.low = low > 0 ? (int)low : 0;
-    s.beyond = a.window && (int64_t)s.end - 1 - a.window > 0 ? (int)((int64_t)s.end - 1 - a.window) : -1;
+    s.beyond = a.window && (int64_t)s.end - 1 - a.window >= 0 ? (int)((int64_t)s.end - 1 - a.window) : -1;
     const int end = (s.end + kFewTile - 1) / kFewTile, seen = a.sinks < s.end ? a.sinks : s.end;
     s.window_tile = s.low / kFewTile;
     if (s.window_tile > end) s.window_tile = end;

@@ -479,7 +479,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
 
     // A tile.  While a half tile's scores become weights (vector unit), the weights of the half before meet their values and the
     // next half's scores are made (matrix cores): no product waits for the weights beside it.
-    const int beyond = a.window && (int64_t)pos1 - a.window > 0 ? (int)((int64_t)pos1 - a.window) : -1;       // tokens up to this one are not in every row's window
+    const int beyond = a.window && (int64_t)pos1 - a.window >= 0 ? (int)((int64_t)pos1 - a.window) : -1;       // tokens up to this one are not in every row's window
     auto step = [&](int i, auto buffer) __attribute__((always_inline)) {
         constexpr int here = decltype(buffer)::value, other = here ^ 1;
         const int t0 = now.t;
