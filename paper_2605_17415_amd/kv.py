@@ -5,6 +5,10 @@ Like `binding`, this module marshals arguments; every step runs in the library's
               the second block is really [page / 8][d][8]
     codes     uint8 [pages, heads, page * (d + 4)]            see ivftq_kv.h
 and tensors of several layers have one more dimension in front.
+
+`stream`: a call's kernels, its workspace and what it gives back belong to this stream (None: the current one).  As everywhere in
+PyTorch the caller has `stream` wait for the work that makes the inputs, and the reader of results wait for `stream`; inputs from
+another stream that are dropped while the call is queued are the caller's to record.
 """
 from __future__ import annotations
 
@@ -172,10 +176,17 @@ def _stream(stream, like):
 
 
 def _scratch(count, dtype, like, stream):
-    """Device memory from the caching allocator, marked as used by the call's stream where that is not the current one."""
-    t = like.new_empty(count, dtype=dtype)
+    """Device memory from the caching allocator's share of the stream that uses it: the current stream may still use what it has freed."""
+    if stream is None:
+        return like.new_empty(count, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(count, dtype=dtype)
+
+
+def _result(t, stream):
+    """A tensor that is given back, made for `stream`: the caller's current stream reads it, and its memory waits for that."""
     if stream is not None:
-        t.record_stream(stream)
+        t.record_stream(torch.cuda.current_stream(t.device))
     return t
 
 
@@ -208,9 +219,12 @@ def kv_attend(q, pool, table, lengths, starts=None, max_new=1, window=0, sinks=0
     d = q.shape[-1]
     cache, rows = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d)
     if out is None:
-        out = torch.empty_like(q)
-        if stream is not None:
-            out.record_stream(stream)
+        if stream is None:
+            out = torch.empty_like(q)
+        else:
+            with torch.cuda.stream(stream):
+                out = torch.empty_like(q)
+            _result(out, stream)
     elif out.shape != q.shape:
         raise ValueError(f"out has shape {tuple(out.shape)}, not {tuple(q.shape)}")
     result = _rows(out, "out", pool, d)
@@ -250,7 +264,7 @@ def _pools(pools, like):
 def kv_reserve(table, lengths, refs, counts, page, stream=None):
     """Pages for counts[r] more tokens in each row, lengths raised; returns what was granted (counts[r] or 0)."""
     state, rows = _pages(table, lengths, refs, page), table.shape[0]
-    granted, scratch = _scratch(rows, torch.int32, refs, stream), _scratch(refs.numel(), torch.int32, refs, stream)
+    granted, scratch = _result(_scratch(rows, torch.int32, refs, stream), stream), _scratch(refs.numel(), torch.int32, refs, stream)
     _check(_library().ivftq_kv_reserve(state, _ints(counts, "counts", refs, rows), granted.data_ptr(), scratch.data_ptr(), _stream(stream, refs)))
     return granted
 
@@ -259,7 +273,7 @@ def kv_fork(pools, table, lengths, refs, parents, children, page, stream=None):
     """Rows `children` become copies of rows `parents`: full pages shared, a last page that is not full copied in every layer
     of pools [layers, pages, ...].  Returns 1 for each entry that was done."""
     state, where, n = _pages(table, lengths, refs, page), _pools(pools, refs), parents.numel()
-    done, scratch = _scratch(n, torch.int32, refs, stream), _scratch(refs.numel() + 2 * n + 2 * table.shape[0], torch.int32, refs, stream)
+    done, scratch = _result(_scratch(n, torch.int32, refs, stream), stream), _scratch(refs.numel() + 2 * n + 2 * table.shape[0], torch.int32, refs, stream)
     _check(_library().ivftq_kv_fork(state, where, _ints(parents, "parents", refs), _ints(children, "children", refs, n), n, done.data_ptr(),
                                     scratch.data_ptr(), _stream(stream, refs)))
     return done
@@ -278,7 +292,7 @@ def kv_trim(table, lengths, refs, page, window, sinks=0, stream=None):
 def kv_compact(pools, table, refs, stream=None):
     """Pages in use move to the lowest numbers; returns how many there are (device, int32 [1])."""
     state, where = _pages(table, None, refs, 16), _pools(pools, refs)
-    used, scratch = _scratch(1, torch.int32, refs, stream), _scratch(3 * refs.numel() + 64, torch.int32, refs, stream)
+    used, scratch = _result(_scratch(1, torch.int32, refs, stream), stream), _scratch(3 * refs.numel() + 64, torch.int32, refs, stream)
     _check(_library().ivftq_kv_compact(state, where, used.data_ptr(), scratch.data_ptr(), _stream(stream, refs)))
     return used
 
