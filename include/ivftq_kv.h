@@ -12,7 +12,7 @@
  *   - The caller owns every buffer: pool, table, lengths, reference counts, workspace.  Device pointers unless stated.
  *     Nothing is kept from one call for the next.
  *   - Calls are asynchronous on `stream` (a hipStream_t passed as void*, NULL = the default stream), allocate nothing, issue
- *     kernel launches only and may be recorded into a HIP graph.
+ *     kernel launches only and may be recorded into a HIP graph.  Buffers and stream belong to the current device.
  *   - Arguments that the host can see are checked before any launch; every call returns an ivftq_status and
  *     ivftq_last_error() has the message.  What only the device sees (table entries, lengths, starts, rows of a list) is
  *     bounded by the kernels: an entry that names no page of the pool holds no visible token and takes no row, a length

@@ -172,7 +172,20 @@ def _starts(starts, table, like):
 
 
 def _stream(stream, like):
-    return torch._C._cuda_getCurrentRawStream(like.device.index) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(like.device.index)
+    if stream.device != like.device:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on {like.device}")
+    return stream.cuda_stream
+
+
+def _run(call, like, *args):
+    """The library launches on the current device, which has to be that of the tensors."""
+    if like.device.index == torch._C._cuda_getDevice():
+        _check(call(*args))
+    else:
+        with torch.cuda.device(like.device):
+            _check(call(*args))
 
 
 def _scratch(count, dtype, like, stream):
@@ -196,18 +209,16 @@ def _result(t, stream):
 def kv_append(pool, k, v, table, lengths, starts=None, rotation=None, levels=None, stream=None):
     """Write the new rows k, v [rows, heads, d] of every sequence to its pages: sequence b's rows are starts[b] ..
     starts[b + 1] - 1 and its last tokens (starts None: one row per sequence).  lengths count the new tokens already."""
-    lib = _library()
     d = k.shape[-1]
-    _check(lib.ivftq_kv_append(_cache(pool, table, lengths, d, rotation, levels), _rows(k, "k", pool, d),
-                               _rows(v, "v", pool, d), _starts(starts, table, pool), _stream(stream, pool)))
+    _run(_library().ivftq_kv_append, pool, _cache(pool, table, lengths, d, rotation, levels), _rows(k, "k", pool, d), _rows(v, "v", pool, d),
+         _starts(starts, table, pool), _stream(stream, pool))
 
 
 def kv_read(pool, table, lengths, k_out, v_out, starts=None, rotation=None, levels=None, stream=None):
     """The opposite of kv_append: the rows that the cache holds for these tokens."""
-    lib = _library()
     d = k_out.shape[-1]
-    _check(lib.ivftq_kv_read(_cache(pool, table, lengths, d, rotation, levels), _rows(k_out, "k_out", pool, d),
-                             _rows(v_out, "v_out", pool, d), _starts(starts, table, pool), _stream(stream, pool)))
+    _run(_library().ivftq_kv_read, pool, _cache(pool, table, lengths, d, rotation, levels), _rows(k_out, "k_out", pool, d), _rows(v_out, "v_out", pool, d),
+         _starts(starts, table, pool), _stream(stream, pool))
 
 
 def kv_attend(q, pool, table, lengths, starts=None, max_new=1, window=0, sinks=0, scale=None, rotation=None, levels=None, out=None,
@@ -217,7 +228,7 @@ def kv_attend(q, pool, table, lengths, starts=None, max_new=1, window=0, sinks=0
     max_new: no sequence has more new rows.  lse (float32 [rows, query heads], optional) receives the logarithm of the sums."""
     lib = _library()
     d = q.shape[-1]
-    cache, rows = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d)
+    cache, rows, where = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d), _stream(stream, pool)
     if out is None:
         if stream is None:
             out = torch.empty_like(q)
@@ -239,8 +250,8 @@ def kv_attend(q, pool, table, lengths, starts=None, max_new=1, window=0, sinks=0
     if need < 0:
         _check(1)
     work = _scratch(need, torch.uint8, q, stream) if need else None
-    _check(lib.ivftq_kv_attend(cache, rows, result, None if lse is None else lse.data_ptr(), first, max_new, window, sinks,
-                               1 / math.sqrt(d) if scale is None else scale, None if work is None else work.data_ptr(), need, _stream(stream, pool)))
+    _run(lib.ivftq_kv_attend, pool, cache, rows, result, None if lse is None else lse.data_ptr(), first, max_new, window, sinks,
+         1 / math.sqrt(d) if scale is None else scale, None if work is None else work.data_ptr(), need, where)
     return out
 
 
@@ -263,44 +274,44 @@ def _pools(pools, like):
 
 def kv_reserve(table, lengths, refs, counts, page, stream=None):
     """Pages for counts[r] more tokens in each row, lengths raised; returns what was granted (counts[r] or 0)."""
-    state, rows = _pages(table, lengths, refs, page), table.shape[0]
+    state, rows, where = _pages(table, lengths, refs, page), table.shape[0], _stream(stream, refs)
     granted, scratch = _result(_scratch(rows, torch.int32, refs, stream), stream), _scratch(refs.numel(), torch.int32, refs, stream)
-    _check(_library().ivftq_kv_reserve(state, _ints(counts, "counts", refs, rows), granted.data_ptr(), scratch.data_ptr(), _stream(stream, refs)))
+    _run(_library().ivftq_kv_reserve, refs, state, _ints(counts, "counts", refs, rows), granted.data_ptr(), scratch.data_ptr(), where)
     return granted
 
 
 def kv_fork(pools, table, lengths, refs, parents, children, page, stream=None):
     """Rows `children` become copies of rows `parents`: full pages shared, a last page that is not full copied in every layer
     of pools [layers, pages, ...].  Returns 1 for each entry that was done."""
-    state, where, n = _pages(table, lengths, refs, page), _pools(pools, refs), parents.numel()
+    state, records, n, where = _pages(table, lengths, refs, page), _pools(pools, refs), parents.numel(), _stream(stream, refs)
     done, scratch = _result(_scratch(n, torch.int32, refs, stream), stream), _scratch(refs.numel() + 2 * n + 2 * table.shape[0], torch.int32, refs, stream)
-    _check(_library().ivftq_kv_fork(state, where, _ints(parents, "parents", refs), _ints(children, "children", refs, n), n, done.data_ptr(),
-                                    scratch.data_ptr(), _stream(stream, refs)))
+    _run(_library().ivftq_kv_fork, refs, state, records, _ints(parents, "parents", refs), _ints(children, "children", refs, n), n, done.data_ptr(),
+         scratch.data_ptr(), where)
     return done
 
 
 def kv_free(table, lengths, refs, rows, stream=None):
     """Rows give their pages back and become empty."""
-    _check(_library().ivftq_kv_free(_pages(table, lengths, refs, 16), _ints(rows, "rows", refs), rows.numel(), _stream(stream, refs)))
+    _run(_library().ivftq_kv_free, refs, _pages(table, lengths, refs, 16), _ints(rows, "rows", refs), rows.numel(), _stream(stream, refs))
 
 
 def kv_trim(table, lengths, refs, page, window, sinks=0, stream=None):
     """Every row gives back the pages that no later token sees with this window and these first tokens."""
-    _check(_library().ivftq_kv_trim(_pages(table, lengths, refs, page), window, sinks, _stream(stream, refs)))
+    _run(_library().ivftq_kv_trim, refs, _pages(table, lengths, refs, page), window, sinks, _stream(stream, refs))
 
 
 def kv_compact(pools, table, refs, stream=None):
     """Pages in use move to the lowest numbers; returns how many there are (device, int32 [1])."""
-    state, where = _pages(table, None, refs, 16), _pools(pools, refs)
+    state, records, where = _pages(table, None, refs, 16), _pools(pools, refs), _stream(stream, refs)
     used, scratch = _result(_scratch(1, torch.int32, refs, stream), stream), _scratch(3 * refs.numel() + 64, torch.int32, refs, stream)
-    _check(_library().ivftq_kv_compact(state, where, used.data_ptr(), scratch.data_ptr(), _stream(stream, refs)))
+    _run(_library().ivftq_kv_compact, refs, state, records, used.data_ptr(), scratch.data_ptr(), where)
     return used
 
 
 def kv_copy(pools, src, dst, stream=None):
     """Record of page src[i] to page dst[i] in every layer of pools; no page both source and destination."""
-    where = _pools(pools, pools)
-    _check(_library().ivftq_kv_copy(where, _ints(src, "src", pools), _ints(dst, "dst", pools, src.numel()), src.numel(), _stream(stream, pools)))
+    records = _pools(pools, pools)
+    _run(_library().ivftq_kv_copy, pools, records, _ints(src, "src", pools), _ints(dst, "dst", pools, src.numel()), src.numel(), _stream(stream, pools))
 
 
 # ---- a model's cache -----------------------------------------------------------------------------

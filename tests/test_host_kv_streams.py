@@ -121,3 +121,25 @@ def test_without_a_stream_the_current_one_is_used(world, name):
     call()
     assert [x[2] for x in world.launched] == [1000]
     assert all(x == (0, "caller") for x in world.allocated) and not world.recorded
+
+
+@pytest.mark.parametrize("name", ALL)
+def test_a_cache_on_another_device_than_the_current_one(world, name):
+    """The library launches on the current device: it is the cache's for the length of the call."""
+    call, _ = calls(world, device=1)[name]
+    call()
+    assert [x[1:] for x in world.launched] == [(1, 1001)]
+    assert all(x[0] == 1 for x in world.allocated)
+    assert world.device == 0
+    world.launched.clear()
+    call(stream=side(1))
+    assert [x[1:] for x in world.launched] == [(1, 77)]
+    assert (world.device, world.stream) == (0, "caller")
+
+
+@pytest.mark.parametrize("name", ALL)
+def test_a_stream_of_another_device_is_refused(world, name):
+    call, _ = calls(world)[name]
+    with pytest.raises(ValueError):
+        call(stream=side(1))
+    assert not world.launched
