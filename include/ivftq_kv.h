@@ -41,7 +41,10 @@ enum { IVFTQ_KV_F16 = 0, IVFTQ_KV_BF16 = 1, IVFTQ_KV_CODE4 = 2 };
  * heads, 1 to 1024.  Sequence b's token t is token t % page of page table[b * table_stride + t / page].  lengths[b]: tokens
  * of the sequence, those of the present step included.  rotation (device, d x d, 16-byte aligned) and levels (16 values,
  * ascending, levels[15 - i] == -levels[i], as ivftq_build_codebook(4, d, ...) gives them) are read for IVFTQ_KV_CODE4 only.
- * pool is 16-byte aligned. */
+ * pool is 16-byte aligned.
+ * asked and granted (device, batch numbers each, or both NULL): counts and results of the present step's ivftq_kv_reserve.
+ * ivftq_kv_append writes no row of a sequence with granted[b] < asked[b]: its length does not count them, so that they would
+ * fall on the tokens before them.  No other call reads the two. */
 typedef struct ivftq_kv_cache {
     void* pool;
     const int32_t* table;
@@ -56,6 +59,8 @@ typedef struct ivftq_kv_cache {
     int32_t heads;
     int32_t d;
     float levels[16];
+    const int32_t* asked;
+    const int32_t* granted;
 } ivftq_kv_cache;
 
 /* Rows of the present step: row r, head h, coordinate j at data[r * row_stride + h * head_stride + j] (strides in elements,
@@ -124,7 +129,8 @@ typedef struct ivftq_kv_pools {
 } ivftq_kv_pools;
 
 /* Room for counts[r] more tokens (device, negative counts as 0) in each row: pages taken, lengths raised; granted[r] = counts[r].
- * Where the table's columns or the free pages do not reach, granted[r] = 0 and the row stays as it is; once the pages have not
+ * Where the table's columns or the free pages do not reach, granted[r] = 0 and the row stays as it is (new rows must not be
+ * appended to it: see asked and granted above); once the pages have not
  * reached for one row, no later row that needs a page gets one.  scratch: pages int32. */
 ivftq_status ivftq_kv_reserve(const ivftq_kv_pages* state, const int32_t* counts, int32_t* granted, int32_t* scratch,
                               void* stream);

@@ -103,6 +103,8 @@ ivftq_status check_cache(const ivftq_kv_cache* c) {
             if (!(c->levels[8 + i] > (i ? c->levels[7 + i] : 0.f)) || c->levels[7 - i] != -c->levels[8 + i] || !(c->levels[8 + i] < 1e4f))
                 return refuse(IVFTQ_INVALID_ARG, "levels have to ascend and be symmetric about zero (level %d: %g)", 8 + i, (double)c->levels[8 + i]);
     }
+    if (!c->asked != !c->granted || !aligned(c->asked, 4) || !aligned(c->granted, 4))
+        return refuse(IVFTQ_INVALID_ARG, "asked and granted go together, 4-byte aligned");
     return IVFTQ_OK;
 }
 
@@ -197,7 +199,8 @@ ivftq_status move_rows(const ivftq_kv_cache* cache, const ivftq_kv_rows* k, cons
     if (k->rows != v->rows || k->type != v->type) return refuse(IVFTQ_INVALID_ARG, "keys and values have one number of rows and one type");
     if (!starts && k->rows * cache->heads > INT32_MAX / (cache->d / 8)) return refuse(IVFTQ_UNSUPPORTED, "%lld rows of %d heads in one call", (long long)k->rows, cache->heads);
     if (!k->rows || !cache->batch) return IVFTQ_OK;
-    const KvView c = view_of(*cache, starts, k->rows, false);
+    KvView c = view_of(*cache, starts, k->rows, false);
+    if (!read) { c.asked = cache->asked; c.granted = cache->granted; }
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const hipError_t e = read ? launch_kv_read(c, rows_of(*k), rows_of(*v), cache->d, cache->format, st) : launch_kv_append(c, rows_of(*k), rows_of(*v), cache->d, cache->format, st);
     return done(e, read ? "ivftq_kv_read" : "ivftq_kv_append");

@@ -23,6 +23,7 @@ struct KvView {
     const int32_t* table;
     const int32_t* lengths;
     const int32_t* starts;       // null: one row per sequence
+    const int32_t *asked, *granted;      // append: null, or what the step's reservation was asked for and gave
     const float* rotation;
     int64_t pages, table_stride, head_bytes, page_bytes;
     int32_t batch, columns, page, page_log2, heads, rows;
@@ -100,6 +101,9 @@ __device__ __forceinline__ void kv_new_rows(const KvView& c, int b, int& first, 
     const int end = e < first ? first : (e < c.rows ? e : c.rows);
     count = end - first;
 }
+
+// Whether sequence b's reservation was refused: its length does not count the new rows.
+__device__ __forceinline__ bool kv_refused(const KvView& c, int b) { return c.asked && kv_int(c.granted, b) < kv_int(c.asked, b); }
 
 // Number of the page that holds token t of sequence b, -1 where there is none.
 __device__ __forceinline__ int64_t kv_page(const KvView& c, int b, int t) {

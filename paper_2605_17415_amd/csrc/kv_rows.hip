@@ -11,7 +11,7 @@ namespace {
 // there is none.
 __device__ __forceinline__ char* place_of(const KvView& c, int r, int h, int& t) {
     const int pos = kv_length(c, r) - 1;
-    if (pos < 0) return nullptr;
+    if (pos < 0 || kv_refused(c, r)) return nullptr;
     const int64_t page = kv_page(c, r, pos);
     t = pos & (c.page - 1);
     return page < 0 ? nullptr : kv_record(c, page, h);
@@ -26,7 +26,7 @@ struct NewTiles { int first_row, pos0, end, tile0, tiles; };      // pos0: posit
 
 __device__ __forceinline__ NewTiles new_tiles(const KvView& c, int b) {
     NewTiles t{0, 0, 0, 0, 0};
-    if (b >= c.batch) return t;
+    if (b >= c.batch || kv_refused(c, b)) return t;
     int count;
     kv_new_rows(c, b, t.first_row, count);
     t.end = kv_length(c, b);

@@ -12,6 +12,7 @@ another stream that are dropped while the call is queued are the caller's to rec
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import math
 import struct
@@ -29,7 +30,7 @@ _TYPES = {torch.float16: F16, torch.bfloat16: BF16}
 class _Cache(C.Structure):
     _fields_ = [("pool", C.c_void_p), ("table", C.c_void_p), ("lengths", C.c_void_p), ("rotation", C.c_void_p), ("pages", C.c_int64),
                 ("table_stride", C.c_int64), ("batch", C.c_int32), ("columns", C.c_int32), ("format", C.c_int32), ("page", C.c_int32),
-                ("heads", C.c_int32), ("d", C.c_int32), ("levels", C.c_float * 16)]
+                ("heads", C.c_int32), ("d", C.c_int32), ("levels", C.c_float * 16), ("asked", C.c_void_p), ("granted", C.c_void_p)]
 
 
 class _Rows(C.Structure):
@@ -144,7 +145,7 @@ def _rows(t, name, like, d):
     return _pack_rows(t.data_ptr(), row, head, rows, heads, _type_of(t, name))
 
 
-def _cache(pool, table, lengths, d, rotation, levels):
+def _cache(pool, table, lengths, d, rotation, levels, asked=None, granted=None):
     _on_device(pool, "pool")
     if not pool.is_contiguous():
         raise ValueError("pool must be contiguous")
@@ -164,7 +165,8 @@ def _cache(pool, table, lengths, d, rotation, levels):
             raise ValueError(f"a 16-bit pool is pages x heads x 2 x page x {d}, got {tuple(shape)}")
         form, page = _type_of(pool, "pool"), shape[3]
     where, stride, batch, columns = _table(table, pool)
-    return _pack_cache(pool.data_ptr(), where, _ints(lengths, "lengths", pool, batch), turn, shape[0], stride, batch, columns, form, page, shape[1], d, values)
+    return _pack_cache(pool.data_ptr(), where, _ints(lengths, "lengths", pool, batch), turn, shape[0], stride, batch, columns, form, page, shape[1], d, values,
+                       _ints(asked, "asked", pool, batch) or 0, _ints(granted, "granted", pool, batch) or 0)
 
 
 def _starts(starts, table, like):
@@ -206,11 +208,13 @@ def _result(t, stream):
 # ---- rows and attention --------------------------------------------------------------------------
 
 
-def kv_append(pool, k, v, table, lengths, starts=None, rotation=None, levels=None, stream=None):
+def kv_append(pool, k, v, table, lengths, starts=None, rotation=None, levels=None, stream=None, asked=None, granted=None):
     """Write the new rows k, v [rows, heads, d] of every sequence to its pages: sequence b's rows are starts[b] ..
-    starts[b + 1] - 1 and its last tokens (starts None: one row per sequence).  lengths count the new tokens already."""
+    starts[b + 1] - 1 and its last tokens (starts None: one row per sequence).  lengths count the new tokens already, unless
+    kv_reserve refused them: with its counts as `asked` and its result as `granted`, such sequences' rows are not written (without
+    the two they fall on the tokens before them)."""
     d = k.shape[-1]
-    _run(_library().ivftq_kv_append, pool, _cache(pool, table, lengths, d, rotation, levels), _rows(k, "k", pool, d), _rows(v, "v", pool, d),
+    _run(_library().ivftq_kv_append, pool, _cache(pool, table, lengths, d, rotation, levels, asked, granted), _rows(k, "k", pool, d), _rows(v, "v", pool, d),
          _starts(starts, table, pool), _stream(stream, pool))
 
 
@@ -273,7 +277,8 @@ def _pools(pools, like):
 
 
 def kv_reserve(table, lengths, refs, counts, page, stream=None):
-    """Pages for counts[r] more tokens in each row, lengths raised; returns what was granted (counts[r] or 0)."""
+    """Pages for counts[r] more tokens in each row, lengths raised; returns what was granted (counts[r], or 0 where there is no
+    room: the row stays as it is, and new rows must not be appended to it)."""
     state, rows, where = _pages(table, lengths, refs, page), table.shape[0], _stream(stream, refs)
     granted, scratch = _result(_scratch(rows, torch.int32, refs, stream), stream), _scratch(refs.numel(), torch.int32, refs, stream)
     _run(_library().ivftq_kv_reserve, refs, state, _ints(counts, "counts", refs, rows), granted.data_ptr(), scratch.data_ptr(), where)
@@ -324,7 +329,8 @@ class KVCache:
     prefix and queue their work on the current stream (or `stream`).
 
     A step of a model: `reserve` room for the new tokens, then for every layer `append` its keys and values and `attend`.  Rows
-    without new tokens have none between their `starts`."""
+    without new tokens have none between their `starts`.  A row whose reservation was refused keeps its tokens: `append` leaves it
+    out until a `reserve` grants it what it asks for, and what `attend` gives for its new rows means nothing."""
 
     def __init__(self, layers: int, heads: int, d: int, pages: int, sequences: int, tokens: int, page: int = 64, dtype=torch.bfloat16, codes: bool = False,
                  rotation_seed: int = 0, device="cuda"):
@@ -338,15 +344,20 @@ class KVCache:
         self.table = torch.full((sequences, -(-tokens // page)), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self.refs = torch.zeros(pages, dtype=torch.int32, device=device)
+        self._asked, self._granted = (torch.zeros(sequences, dtype=torch.int32, device=device) for _ in range(2))      # of the last reserve
         self._codec = {}
         if codes:
             self._codec = {"rotation": torch.from_numpy(ivftq_haar_rotation(d, rotation_seed)).to(device), "levels": ivftq_build_codebook(4, d)[0]}
 
     def reserve(self, counts, stream=None):
-        return kv_reserve(self.table, self.lengths, self.refs, counts, self.page, stream)
+        granted = kv_reserve(self.table, self.lengths, self.refs, counts, self.page, stream)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            self._asked.copy_(counts)
+            self._granted.copy_(granted)
+        return granted
 
     def append(self, layer: int, k, v, starts=None, stream=None):
-        kv_append(self.pools[layer], k, v, self.table, self.lengths, starts, stream=stream, **self._codec)
+        kv_append(self.pools[layer], k, v, self.table, self.lengths, starts, stream=stream, asked=self._asked, granted=self._granted, **self._codec)
 
     def attend(self, layer: int, q, starts=None, max_new: int = 1, window: int = 0, sinks: int = 0, scale=None, out=None, lse=None, stream=None):
         return kv_attend(q, self.pools[layer], self.table, self.lengths, starts, max_new, window, sinks, scale, out=out, lse=lse, stream=stream, **self._codec)

@@ -179,3 +179,11 @@ def test_tensors_that_are_no_device_tensors_are_refused():
         pkg.kv_append(pool, q, q, table, lengths)
     with pytest.raises(TypeError):
         pkg.kv_copy(pool, table, table)
+
+
+@pytest.mark.parametrize("one", ("asked", "granted"))
+def test_half_of_a_reservation_is_refused(lib, one):
+    c, r = cache(**{one: HERE}), rows()
+    assert lib.ivftq_kv_append(C.byref(c), C.byref(r), C.byref(r), None, None) == 1
+    c = cache(asked=HERE, granted=C.c_void_p((1 << 20) + 2))
+    assert lib.ivftq_kv_append(C.byref(c), C.byref(r), C.byref(r), None, None) == 1
