@@ -121,6 +121,11 @@ ivftq_status check_rows(const ivftq_kv_rows* r, const char* name, int heads, int
     return IVFTQ_OK;
 }
 
+ivftq_status check_workgroups(const ivftq_kv_cache& c, const KvWork& w) {
+    if ((int64_t)c.batch * c.heads * (w.few ? 1 : (int64_t)w.row_tiles) <= INT32_MAX) return IVFTQ_OK;
+    return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups: %d sequences of %d heads and up to %d row tiles", c.batch, c.heads, w.row_tiles);
+}
+
 // The magnitudes' float16 table.  A table's common scale is free (scores and results are multiplied by it in float32), and the
 // rounding of eight numbers to float16 depends on it: of 128 scales in [1, 2) the one that leaves the smallest mean square,
 // levels weighted by how often a coordinate of variance 1 / d meets them and what a common factor mends left out, 4e-5 to 8e-5
@@ -247,7 +252,8 @@ int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int
         return -1;
     }
     if (max_new > rows) max_new = rows > 1 ? (int32_t)rows : 1;
-    return kv_work(cache->format, cache->d, cache->batch, cache->heads, rows, q_heads, max_new, (int64_t)cache->columns * cache->page).bytes;
+    const KvWork w = kv_work(cache->format, cache->d, cache->batch, cache->heads, rows, q_heads, max_new, (int64_t)cache->columns * cache->page);
+    return check_workgroups(*cache, w) ? -1 : w.bytes;
 }
 
 ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse, const int32_t* starts,
@@ -264,6 +270,7 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     if (!starts) max_new = 1;
     if (max_new > q->rows) max_new = (int32_t)q->rows;
     const KvWork w = kv_work(cache->format, cache->d, cache->batch, cache->heads, q->rows, q->heads, max_new, (int64_t)cache->columns * cache->page);
+    if (ivftq_status e = check_workgroups(*cache, w)) return e;
     if (w.bytes && (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)))
         return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)workspace_bytes, (long long)w.bytes);
     KvAttend a{};
@@ -277,7 +284,6 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     a.sinks = sinks;
     a.scale = scale;
     a.work = static_cast<char*>(workspace);
-    if ((int64_t)cache->batch * cache->heads * (w.few ? 1 : (int64_t)w.row_tiles) > INT32_MAX) return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups");
     return done(launch_kv_attend(a, w, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_attend");
 }
 

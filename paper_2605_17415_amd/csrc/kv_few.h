@@ -439,7 +439,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_fe
         few_find(a, blockIdx.x, f.wgs, x, end, b, at);
         if (x >= end) return;
     } else {
-        b = blockIdx.x / a.c.heads;
+        b = (int)(kv_workgroup() / (uint32_t)a.c.heads);
+        if (b >= a.c.batch) return;
     }
     const int64_t begin = x;
     FewSeq s = few_seq(a, b);
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_fe
             from = (int)(x - pair);
             to = (int)(end - pair < s.tiles ? end - pair : s.tiles);
         } else {
-            h = blockIdx.x % a.c.heads;
+            h = (int)(kv_workgroup() % (uint32_t)a.c.heads);
             from = 0;
             to = s.tiles;
             if (!s.tiles) return;
@@ -536,7 +537,8 @@ __global__ __launch_bounds__(512) void k_kv_few_join(FewArgs f) {
     __shared__ float weight[8][64];
     const KvAttend& a = f.a;
     const int wave = kv_wave(), lane = threadIdx.x & 63;
-    const int b = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, col0 = blockIdx.y * 16;
+    const int b = (int)(kv_workgroup() / (uint32_t)a.c.heads), h = (int)(kv_workgroup() % (uint32_t)a.c.heads), col0 = blockIdx.y * 16;
+    if (b >= a.c.batch) return;
     const FewSeq s = few_seq(a, b);
     const int cols = s.count * a.group;
     if (col0 >= cols) return;

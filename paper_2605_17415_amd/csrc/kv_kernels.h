@@ -63,6 +63,14 @@ inline int64_t kv_head_bytes(int format, int page, int d) {
 
 #ifdef __HIPCC__
 
+// Workgroups in one row, as the kernel numbers them.  A dimension of a grid counts threads in 32 bits, and a launch of more takes what
+// is left of the count without an error; so the row goes on in the third dimension (and a kernel passes over what lies past its end).
+inline dim3 kv_grid(int64_t wgs, int threads, unsigned columns = 1) {
+    const int64_t most = 0xffffffffll / threads, rows = (wgs + most - 1) / most;
+    return dim3((unsigned)((wgs + rows - 1) / rows), columns, (unsigned)rows);
+}
+__device__ __forceinline__ uint32_t kv_workgroup() { return blockIdx.z * gridDim.x + blockIdx.x; }
+
 // A value that all lanes hold, as a scalar.
 __device__ __forceinline__ int kv_uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int64_t kv_uniform(int64_t v) {

@@ -236,14 +236,14 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
     // heads fastest: with eight heads each XCD reads one head's pages; then shares, or sequences and the row tiles with the longest
     // reach first
-    const int h = blockIdx.x % c.heads, share = blockIdx.x / c.heads;
+    const int h = (int)(kv_workgroup() % (uint32_t)c.heads), share = (int)(kv_workgroup() / (uint32_t)c.heads);
     int64_t x = 0;                               // the share's tiles that are done
   while (true) {                                 // a row tile, or what of it lies in the share
     int b, rt, from = 0, to = 0;
     bool last_part = true;
     if constexpr (SHARED) {
         const ManyShare now = many_share(a, f.row_tiles, f.wgs, share, x);
-        if (threadIdx.x == 0 && blockIdx.x == 0 && x == 0) f.begin[0] = now.size;
+        if (threadIdx.x == 0 && share == 0 && h == 0 && x == 0) f.begin[0] = now.size;
         if (now.from >= now.to) return;
         b = now.b; rt = now.rt; from = now.from; to = now.to;
         if (threadIdx.x == 0 && h == 0 && from == 0) f.begin[1 + b * f.row_tiles + rt] = now.begin;
@@ -252,6 +252,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_kv_many(ManyArgs f) {
     } else {
         b = share % c.batch;
         rt = f.row_tiles - 1 - share / c.batch;
+        if (rt < 0) return;
     }
     const ManyRowTile tile(a, b, rt);
     const FewSeq& s = tile.s;
@@ -710,7 +711,7 @@ __device__ __forceinline__ void many_join(const ManyArgs& f, const ManyPlace& at
 template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_many_join(ManyArgs f) {
     const KvRows& out = f.a.out;
-    const int64_t all = (int64_t)out.rows * out.heads, u = (int64_t)blockIdx.x * 256 + threadIdx.x, i = u / (D / 8);
+    const int64_t all = (int64_t)out.rows * out.heads, u = (int64_t)kv_workgroup() * 256 + threadIdx.x, i = u / (D / 8);
     const int j = (int)(u % (D / 8)) * 8;
     if (i >= all) return;
     const ManyPlace at = many_place<true>(f, i / out.heads, (int)(i % out.heads));
@@ -770,7 +771,7 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
     float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole), *ml = reinterpret_cast<float*>(a.work + w.ml);
     const int64_t all = (int64_t)a.q.rows * a.q.heads;
     // a workgroup's 16-row tiles: many rows share the rotation's operands, where that leaves three workgroups a compute unit (27,000 rows
-    // of 128: eight tiles each 18 us there and 33 us back, two 16 and 20)
+    // of 128: eight tiles each 18 us there and 33 us back, two 16 and 20); rows whose workspace fits a card are far from 2^32 threads
     const int64_t fill = all / (16 * 768);
     const int tiles = fill < 1 ? 1 : (fill < kTurnTiles ? (int)fill : kTurnTiles);
     const unsigned rot = (unsigned)((all + 16 * tiles - 1) / (16 * tiles));
@@ -788,12 +789,12 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
                 if (wgs > (unsigned)kFewMaxWgs) wgs = kFewMaxWgs;
                 f.wgs = (int32_t)wgs;
             }
-            kernel<<<dim3(wgs, (unsigned)w.col_tiles), 256, 0, st>>>(f);
+            kernel<<<kv_grid(wgs, 256, (unsigned)w.col_tiles), 256, 0, st>>>(f);
             return hipGetLastError();
         };
         static ChipFill fill, fill_low;
         if (hipError_t e = low ? launch(&k_kv_few<F, D, codes>, fill_low) : launch(&k_kv_few<F, D, false>, fill)) return e;
-        if (w.split || F == IVFTQ_KV_CODE4) k_kv_few_join<F, D><<<dim3(pairs, (unsigned)w.col_tiles), 512, 0, st>>>(f);
+        if (w.split || F == IVFTQ_KV_CODE4) k_kv_few_join<F, D><<<kv_grid(pairs, 512, (unsigned)w.col_tiles), 512, 0, st>>>(f);
     } else {
         const ManyArgs f{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), ml, reinterpret_cast<int64_t*>(a.work + w.begin), w.row_tiles, w.shared};
         auto launch = [&](auto shared) {
@@ -801,10 +802,10 @@ hipError_t kv_attend_launch(const KvAttend& a, const KvWork& w, hipStream_t st) 
             // shares: workgroups for either way
             const unsigned one_each = pairs * (unsigned)w.row_tiles, wgs = S && one_each < (unsigned)(a.c.heads * w.shared) ? (unsigned)(a.c.heads * w.shared) : one_each;
             // float16 results: the queries' second part matters beside the rounding of the result
-            if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4, S><<<wgs, 256, 0, st>>>(f);
-            else k_kv_many<F, D, false, S><<<wgs, 256, 0, st>>>(f);
+            if (F == IVFTQ_KV_CODE4 && a.q.type == IVFTQ_KV_F16) k_kv_many<F, D, F == IVFTQ_KV_CODE4, S><<<kv_grid(wgs, 256), 256, 0, st>>>(f);
+            else k_kv_many<F, D, false, S><<<kv_grid(wgs, 256), 256, 0, st>>>(f);
             if constexpr (F == IVFTQ_KV_CODE4) k_kv_rotate_back<D, S><<<rot, D * 2, 0, st>>>(f, tiles);
-            else if constexpr (S) k_kv_many_join<F, D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, st>>>(f);
+            else if constexpr (S) k_kv_many_join<F, D><<<kv_grid((all * (D / 8) + 255) / 256, 256), 256, 0, st>>>(f);
         };
         if (w.shared) launch(std::true_type{}); else launch(std::false_type{});
     }

@@ -168,8 +168,9 @@ __device__ __forceinline__ void give_back(const ivftq_kv_pages& s, int r, int fr
         if (p >= 0 && p < s.pages) atomicSub(s.refs + p, 1);
     }
 }
-__global__ __launch_bounds__(256) void k_kv_free(ivftq_kv_pages s, const int32_t* rows) {
-    const int r = rows[blockIdx.x];
+__global__ __launch_bounds__(256) void k_kv_free(ivftq_kv_pages s, const int32_t* rows, int n) {
+    if (kv_workgroup() >= (uint32_t)n) return;
+    const int r = rows[kv_workgroup()];
     if ((unsigned)r >= (unsigned)s.rows) return;
     give_back(s, r, 0, s.columns);
     if (threadIdx.x == 0) s.lengths[r] = 0;
@@ -271,7 +272,7 @@ hipError_t launch_kv_fork(const ivftq_kv_pages& s, const ivftq_kv_pools& p, cons
 }
 hipError_t launch_kv_free(const ivftq_kv_pages& s, const int32_t* rows, int n, hipStream_t st) {
     if (!n) return hipSuccess;
-    k_kv_free<<<(unsigned)n, 256, 0, st>>>(s, rows);
+    k_kv_free<<<kv_grid(n, 256), 256, 0, st>>>(s, rows, n);
     return hipGetLastError();
 }
 hipError_t launch_kv_trim(const ivftq_kv_pages& s, int window, int sinks, hipStream_t st) {

@@ -187,3 +187,12 @@ def test_half_of_a_reservation_is_refused(lib, one):
     assert lib.ivftq_kv_append(C.byref(c), C.byref(r), C.byref(r), None, None) == 1
     c = cache(asked=HERE, granted=C.c_void_p((1 << 20) + 2))
     assert lib.ivftq_kv_append(C.byref(c), C.byref(r), C.byref(r), None, None) == 1
+
+
+def test_a_workspace_for_more_workgroups_than_a_call_takes_is_refused(lib):
+    """What the call refuses, the question for its workspace refuses too: 2^20 sequences of up to 2^19 row tiles."""
+    c = cache(format=kv.BF16, batch=1 << 20, heads=8, d=64)
+    r = rows(rows=1 << 23, heads=64, row_stride=64 * 64, head_stride=64)
+    assert lib.ivftq_kv_attend(C.byref(c), C.byref(r), C.byref(r), None, HERE, 1 << 23, 0, 0, 0.1, HERE, 1 << 40, None) == 6
+    assert lib.ivftq_kv_attend_workspace(C.byref(c), 1 << 23, 64, 1 << 23) == -1
+    assert b"workgroups" in lib.ivftq_last_error()
