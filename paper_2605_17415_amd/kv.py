@@ -103,7 +103,7 @@ def kv_page_bytes(format: int, page: int, heads: int, d: int) -> int:
 def _on_device(t, name, like=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a torch tensor in device memory")
-    if like is not None and t.device != like.device:
+    if like is not None and t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
 
 
