@@ -252,14 +252,19 @@ __device__ __forceinline__ uint32_t turn_nibbles(uint32_t w, int lane) {
     return (w & keep) | (__builtin_amdgcn_alignbit(p, p, right) & ~keep);
 }
 
-// The eight levels, times 2^10, as two float16 parts that keep them to 2^-22: byte tables like those of kv_levels8, the second
-// part with a sign of its own.
-struct KvExact { uint32_t hi[4], lo[4]; };          // of each part: low bytes, then high bytes
+// The eight levels, times 2^10 (levels from 32 on: a lower power of two, so that float16 holds the largest), as two float16 parts that
+// keep them to 2^-22: byte tables like those of kv_levels8, the second part with a sign of its own.
+struct KvExact {
+    uint32_t hi[4], lo[4];          // of each part: low bytes, then high bytes
+    float unit;                     // 2^10 over that power of two
+};
 
 KvExact kv_exact(const KvView& c) {
     KvExact x{};
+    x.unit = 1.f;
+    while (c.level[7] * kSplitScale >= 32768.f * x.unit) x.unit *= 2.f;          // levels are under 10^4
     for (int m = 0; m < 8; ++m) {
-        const float v = c.level[m] * kSplitScale;
+        const float v = c.level[m] * kSplitScale / x.unit;
         const _Float16 part[2] = {(_Float16)v, (_Float16)(v - (float)(_Float16)v)};
         for (int p = 0; p < 2; ++p) {
             uint16_t bits;
@@ -332,7 +337,7 @@ __global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, Kv
     }
     KvTurn<D, true>{pi}(hi, lo, y);
     if (!in) return;
-    kv_store_turned(value ? v : k, r, h, block, y, place ? (float)norm : 0.f);
+    kv_store_turned(value ? v : k, r, h, block, y, place ? (float)norm * exact.unit : 0.f);
 }
 
 // Several rows a sequence.  The rotation stands in LDS as two float16 parts in operand order, so that reading it costs 64
@@ -470,7 +475,7 @@ __global__ __launch_bounds__(kTileThreads, D <= 128 ? 4 : 2) void k_kv_tiles_cod
             rec[ct] = next.rec[ct];
             if constexpr (READ) {
                 norm[ct] = (float)__builtin_bit_cast(_Float16, (uint16_t)next.norm[ct]);
-                gain[ct] = norm[ct] * (1.f / (kSplitScale * kSplitScale));
+                gain[ct] = norm[ct] * exact.unit * (1.f / (kSplitScale * kSplitScale));
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const uint32_t w = value ? turn_nibbles(next.w[ct][s], lane) : next.w[ct][s];
