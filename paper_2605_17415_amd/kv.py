@@ -225,11 +225,12 @@ def kv_read(pool, table, lengths, k_out, v_out, starts=None, rotation=None, leve
          _starts(starts, table, pool), _stream(stream, pool))
 
 
-def kv_attend(q, pool, table, lengths, starts=None, max_new=1, window=0, sinks=0, scale=None, rotation=None, levels=None, out=None,
+def kv_attend(q, pool, table, lengths, starts=None, max_new=None, window=0, sinks=0, scale=None, rotation=None, levels=None, out=None,
               lse=None, stream=None):
     """Attention of the new rows q [rows, query heads, d] over the cache; returns out (like q).  The last rows of a sequence are
     its last tokens; a token sees itself and those before it, with a window the last `window` of them and the first `sinks`.
-    max_new: no sequence has more new rows.  lse (float32 [rows, query heads], optional) receives the logarithm of the sums."""
+    max_new: no sequence has more new rows (None: whatever number; a call that is told prepares for fewer).  Rows past it and rows of no
+    sequence keep what `out` holds, which is nothing in particular where it is not given.  lse (float32 [rows, query heads], optional) receives the logarithm of the sums."""
     lib = _library()
     d = q.shape[-1]
     cache, rows, where = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d), _stream(stream, pool)
@@ -248,8 +249,10 @@ def kv_attend(q, pool, table, lengths, starts=None, max_new=1, window=0, sinks=0
         if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous float32 matrix of rows x query heads")
     first = _starts(starts, table, pool)
-    if starts is None and max_new > 1:
+    if starts is None and (max_new is None or max_new > 1):
         max_new = 1
+    elif max_new is None:
+        max_new = max(q.shape[0], 1)
     need = lib.ivftq_kv_attend_workspace(cache, q.shape[0], q.shape[1], max_new)
     if need < 0:
         _check(1)
@@ -359,7 +362,7 @@ class KVCache:
     def append(self, layer: int, k, v, starts=None, stream=None):
         kv_append(self.pools[layer], k, v, self.table, self.lengths, starts, stream=stream, asked=self._asked, granted=self._granted, **self._codec)
 
-    def attend(self, layer: int, q, starts=None, max_new: int = 1, window: int = 0, sinks: int = 0, scale=None, out=None, lse=None, stream=None):
+    def attend(self, layer: int, q, starts=None, max_new: int | None = None, window: int = 0, sinks: int = 0, scale=None, out=None, lse=None, stream=None):
         return kv_attend(q, self.pools[layer], self.table, self.lengths, starts, max_new, window, sinks, scale, out=out, lse=lse, stream=stream, **self._codec)
 
     def read(self, layer: int, k_out, v_out, starts=None, stream=None):

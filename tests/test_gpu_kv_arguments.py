@@ -1,0 +1,54 @@
+"""Arguments that are left out, and calls that the arguments alone show to be wrong."""
+import numpy as np
+import pytest
+
+import kv_reference as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _pkg():
+    import paper_2605_17415_amd as pkg
+    return pkg
+
+
+def queries(seed, rows, heads, d, dtype):
+    return (torch.randn(rows, heads, d, generator=torch.Generator().manual_seed(seed)) * 1.5).to(dtype).to(DEV)
+
+
+@pytest.mark.parametrize("form", ("f16", "code4"))
+@pytest.mark.parametrize("news", ([3, 0, 2], [70, 0, 33]))
+def test_every_row_has_a_result_where_max_new_is_not_given(form, news):
+    lens = [200, 30, 75]
+    c = ref.Cache(51, form, 2, 64, 16, lens)
+    t, codec = c.device()
+    q = queries(51, sum(news), 4, 64, torch.float16)
+    starts = torch.tensor([0] + list(np.cumsum(news)), dtype=torch.int32, device=DEV)
+    out = torch.full_like(q, float("nan"))
+    assert _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], starts=starts, out=out, **codec) is out
+    torch.cuda.synchronize()
+    ref.check_attention(c, q.cpu(), out, news)
+
+
+def test_every_row_has_a_result_where_max_new_is_not_given_to_the_object():
+    cache = _pkg().KVCache(1, 2, 64, pages=20, sequences=2, tokens=100, page=16, dtype=torch.float16, device=DEV)
+    news = [9, 5]
+    cache.reserve(torch.tensor(news, dtype=torch.int32, device=DEV))
+    q, k, v = queries(1, 14, 4, 64, torch.float16), queries(2, 14, 2, 64, torch.float16), queries(3, 14, 2, 64, torch.float16)
+    starts = torch.tensor([0, 9, 14], dtype=torch.int32, device=DEV)
+    cache.append(0, k, v, starts)
+    out = torch.full_like(q, float("nan"))
+    cache.attend(0, q, starts, out=out)
+    want = cache.attend(0, q, starts, max_new=9)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_no_rows_and_no_max_new():
+    c = ref.Cache(52, "f16", 2, 64, 16, [20])
+    t, _ = c.device()
+    none = torch.empty(0, 4, 64, dtype=torch.float16, device=DEV)
+    out = _pkg().kv_attend(none, t["pool"], t["table"], t["lengths"], starts=torch.zeros(2, dtype=torch.int32, device=DEV))
+    assert out.shape == none.shape
