@@ -9,6 +9,8 @@ and tensors of several layers have one more dimension in front.
 `stream`: a call's kernels, its workspace and what it gives back belong to this stream (None: the current one).  As everywhere in
 PyTorch the caller has `stream` wait for the work that makes the inputs, and the reader of results wait for `stream`; inputs from
 another stream that are dropped while the call is queued are the caller's to record.
+
+The cache serves: there is no backward pass, and rows that ask for a gradient are refused unless gradients are off.
 """
 from __future__ import annotations
 
@@ -134,8 +136,14 @@ def _type_of(t, name):
     return kind
 
 
+def _no_gradient(t, name):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} asks for a gradient, and the cache's calls have none: call them under torch.no_grad()")
+
+
 def _rows(t, name, like, d):
     _on_device(t, name, like)
+    _no_gradient(t, name)
     if t.dim() != 3 or t.shape[2] != d:
         raise ValueError(f"{name} must be rows x heads x {d}, got {tuple(t.shape)}")
     row, head, one = t.stride()
@@ -147,6 +155,7 @@ def _rows(t, name, like, d):
 
 def _cache(pool, table, lengths, d, rotation, levels, asked=None, granted=None):
     _on_device(pool, "pool")
+    _no_gradient(pool, "pool")
     if not pool.is_contiguous():
         raise ValueError("pool must be contiguous")
     shape, turn, values = pool.shape, 0, _NO_LEVELS

@@ -143,3 +143,24 @@ def test_a_stream_of_another_device_is_refused(world, name):
     with pytest.raises(ValueError):
         call(stream=side(1))
     assert not world.launched
+
+
+@pytest.mark.parametrize("which", ("k", "v", "q", "out", "pool"))
+def test_a_gradient_that_would_be_lost_is_refused(world, which):
+    """There is no backward pass: what asks for one is refused, unless gradients are off."""
+    pool, table, lengths = world.tensor(4, 2, 2, 16, 64, dtype=torch.float16), world.tensor(3, 4), world.tensor(3)
+    q, k, v, out = (world.tensor(3, 2, 64, dtype=torch.float16) for _ in range(4))
+    {"k": k, "v": v, "q": q, "out": out, "pool": pool}[which].requires_grad_()
+
+    def call():
+        if which in "kv":
+            pkg.kv_append(pool, k, v, table, lengths)
+        else:
+            pkg.kv_attend(q, pool, table, lengths, out=out)
+
+    with pytest.raises(ValueError, match="gradient"):
+        call()
+    assert not world.launched
+    with torch.no_grad():
+        call()
+    assert len(world.launched) == 1
