@@ -135,7 +135,7 @@ typedef struct ivftq_kv_pools {
 ivftq_status ivftq_kv_reserve(const ivftq_kv_pages* state, const int32_t* counts, int32_t* granted, int32_t* scratch,
                               void* stream);
 /* children[i] becomes a copy of parents[i] (device, n row numbers each, n <= 65536): full pages are shared, a last page that is
- * not full is copied in every layer to a free one.  done[i] = 1, or 0 where nothing was done: a number out of range, a child
+ * not full is copied in every layer to a free one (entries that name no page become -1).  done[i] = 1, or 0 where nothing was done: a number out of range, a child
  * that is not empty, that an earlier entry names or that is any entry's parent, or no free page left.  scratch:
  * pages + 2 n + 2 rows int32. */
 ivftq_status ivftq_kv_fork(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, const int32_t* parents,

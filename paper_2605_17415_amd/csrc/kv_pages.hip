@@ -117,12 +117,19 @@ __global__ __launch_bounds__(kThreads) void k_kv_fork(ivftq_kv_pages s, const in
         return (unsigned)p < (unsigned)s.rows && (unsigned)c < (unsigned)s.rows && __hip_atomic_load(claim + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i &&
                !__hip_atomic_load(parent + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) && s.lengths[c] <= 0;
     };
+    // the parent's last page where it is not full, -1 where there is none (full, or the entry names no page: nothing to copy, and what
+    // a page held before is not shown as the child's)
+    auto last_part = [&](int i) {
+        const int n = length_of(s, parents[i]);
+        const int32_t p = n % s.page ? s.table[(int64_t)parents[i] * s.table_stride + n / s.page] : -1;
+        return p >= 0 && p < s.pages ? p : -1;
+    };
     // src[i] first holds how many pages the entries before i take, dst[i] whether this one takes one
     int want = 0;
     for (int i0 = 0; i0 < n; i0 += kThreads) {
         const int i = i0 + threadIdx.x;
         int total;
-        const bool ok = i < n && ready(i), part = ok && length_of(s, parents[i]) % s.page;
+        const bool ok = i < n && ready(i), part = ok && last_part(i) >= 0;
         const int at = want + scan_before(part, total);
         want += total;
         if (i < n) { done[i] = ok; src[i] = at; dst[i] = part; }
@@ -133,8 +140,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_fork(ivftq_kv_pages s, const in
         done[i] = done[i] && (!part || at < found);
         src[i] = dst[i] = -1;
         if (done[i] && part) {
-            const int32_t from = s.table[(int64_t)parents[i] * s.table_stride + length_of(s, parents[i]) / s.page];
-            src[i] = from >= 0 && from < s.pages ? from : -1;
+            src[i] = last_part(i);
             dst[i] = list[at];
         }
     }

@@ -52,3 +52,21 @@ def test_no_rows_and_no_max_new():
     none = torch.empty(0, 4, 64, dtype=torch.float16, device=DEV)
     out = _pkg().kv_attend(none, t["pool"], t["table"], t["lengths"], starts=torch.zeros(2, dtype=torch.int32, device=DEV))
     assert out.shape == none.shape
+
+
+@pytest.mark.parametrize("missing", (-1, 60))
+def test_a_fork_of_a_missing_last_page_shows_nothing(missing):
+    """The parent's last page is none of the pool: the child's is none either, and no page is taken (its content would be someone's)."""
+    pkg = _pkg()
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    table, lengths, refs = torch.full((4, 3), -1, dtype=torch.int32, device=DEV), ints(20, 20, 0, 0), ints(1, 1, 1, 0, 0, 0)
+    table[0, 0], table[0, 1] = 0, missing
+    table[1, 0], table[1, 1] = 1, 2
+    pools = torch.randn(1, 6, 2, 2, 16, 64, device=DEV).half()
+    before = pools.clone()
+    done = pkg.kv_fork(pools, table, lengths, refs, ints(0, 1), ints(2, 3), page=16)
+    torch.cuda.synchronize()
+    assert done.tolist() == [1, 1] and lengths.tolist() == [20] * 4
+    assert table[2].tolist() == [0, -1, -1] and table[3].tolist() == [1, 3, -1]
+    assert refs.tolist() == [2, 2, 1, 1, 0, 0]
+    assert torch.equal(pools[:, 3], before[:, 2]) and torch.equal(pools[:, :3], before[:, :3]) and torch.equal(pools[:, 4:], before[:, 4:])
