@@ -91,7 +91,7 @@ ivftq_status ivftq_kv_read(const ivftq_kv_cache* cache, const ivftq_kv_rows* k_o
                            const int32_t* starts, void* stream);
 
 /* Attention of the new rows over the cache.  q and out: rows x (heads * group), the group consecutive query heads h * group ..
- * of key-value head h share its keys; out has q's rows, heads and type.  The i-th of sequence b's n new rows stands at
+ * of key-value head h share its keys; out has q's rows, heads and type, and does not overlap it (codes: may be the same rows).  The i-th of sequence b's n new rows stands at
  * position p = lengths[b] - n + i and sees the tokens t <= p with window == 0 or t > p - window or t < sinks.
  *     out = sum_t e^(scale <q, k_t> - max) v_t / sum_t e^(scale <q, k_t> - max)
  * A row that sees nothing gives zeros (lse: -infinity).  lse, NULL or rows x (heads * group) floats: the natural logarithm of

@@ -271,6 +271,7 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     if (max_new > q->rows) max_new = (int32_t)q->rows;
     const KvWork w = kv_work(cache->format, cache->d, cache->batch, cache->heads, q->rows, q->heads, max_new, (int64_t)cache->columns * cache->page);
     if (ivftq_status e = check_workgroups(*cache, w)) return e;
+    if (cache->format != IVFTQ_KV_CODE4 && q->data == out->data) return refuse(IVFTQ_INVALID_ARG, "out stands where q does: only a cache of codes allows that");
     if (w.bytes && (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)))
         return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)workspace_bytes, (long long)w.bytes);
     KvAttend a{};

@@ -70,3 +70,17 @@ def test_a_fork_of_a_missing_last_page_shows_nothing(missing):
     assert table[2].tolist() == [0, -1, -1] and table[3].tolist() == [1, 3, -1]
     assert refs.tolist() == [2, 2, 1, 1, 0, 0]
     assert torch.equal(pools[:, 3], before[:, 2]) and torch.equal(pools[:, :3], before[:, :3]) and torch.equal(pools[:, 4:], before[:, 4:])
+
+
+@pytest.mark.parametrize("new", (1, 70))
+def test_results_may_take_the_queries_place_over_codes(new):
+    """The queries are rotated into the workspace first, nothing reads them afterwards."""
+    lens, news = [1300, 90], [new, new]
+    c = ref.Cache(53, "code4", 2, 64, 16, lens)
+    t, codec = c.device()
+    q = queries(53, 2 * new, 4, 64, torch.bfloat16)
+    starts = torch.tensor([0, new, 2 * new], dtype=torch.int32, device=DEV)
+    want = _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], starts=starts, **codec)
+    assert _pkg().kv_attend(q, t["pool"], t["table"], t["lengths"], starts=starts, out=q, **codec) is q
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)

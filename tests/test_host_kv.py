@@ -196,3 +196,13 @@ def test_a_workspace_for_more_workgroups_than_a_call_takes_is_refused(lib):
     assert lib.ivftq_kv_attend(C.byref(c), C.byref(r), C.byref(r), None, HERE, 1 << 23, 0, 0, 0.1, HERE, 1 << 40, None) == 6
     assert lib.ivftq_kv_attend_workspace(C.byref(c), 1 << 23, 64, 1 << 23) == -1
     assert b"workgroups" in lib.ivftq_last_error()
+
+
+@pytest.mark.parametrize("form", (kv.F16, kv.BF16))
+def test_results_over_the_queries_are_refused_in_16_bits(lib, form):
+    """Other workgroups still read the queries when a result is written."""
+    c, q = cache(format=form), rows(type=form)
+    for columns in (4, 400):
+        c.columns = c.table_stride = columns
+        assert lib.ivftq_kv_attend(C.byref(c), C.byref(q), C.byref(q), None, None, 1, 0, 0, 0.1, HERE, 1 << 40, None) == 1
+        assert b"out" in lib.ivftq_last_error()
