@@ -9,9 +9,10 @@ namespace {
 
 // One row per sequence: where row r's token lives, its page's record part of head h and its place in the page; null where
 // there is none.
+template <bool READ>
 __device__ __forceinline__ char* place_of(const KvView& c, int r, int h, int& t) {
     const int pos = kv_length(c, r) - 1;
-    if (pos < 0 || kv_refused(c, r)) return nullptr;
+    if (pos < 0 || (!READ && kv_refused(c, r))) return nullptr;
     const int64_t page = kv_page(c, r, pos);
     t = pos & (c.page - 1);
     return page < 0 ? nullptr : kv_record(c, page, h);
@@ -24,9 +25,10 @@ __device__ __forceinline__ char* place_of(const KvView& c, int r, int h, int& t)
 
 struct NewTiles { int first_row, pos0, end, tile0, tiles; };      // pos0: position of the first new row (may be under zero)
 
+template <bool READ>
 __device__ __forceinline__ NewTiles new_tiles(const KvView& c, int b) {
     NewTiles t{0, 0, 0, 0, 0};
-    if (b >= c.batch || kv_refused(c, b)) return t;
+    if (b >= c.batch || (!READ && kv_refused(c, b))) return t;
     int count;
     kv_new_rows(c, b, t.first_row, count);
     t.end = kv_length(c, b);
@@ -40,11 +42,12 @@ __device__ __forceinline__ NewTiles new_tiles(const KvView& c, int b) {
 struct NewItem { int64_t left; int b, tile, sub; NewTiles s; };   // items left; sub: number inside a tile
 
 // This wavefront's share of total * per_tile items.
+template <bool READ>
 __device__ __forceinline__ NewItem first_item(const KvView& c, int per_tile) {
     const int lane = threadIdx.x & 63;
     int64_t total = 0;
     for (int b0 = 0; b0 < c.batch; b0 += 64) {
-        int v = new_tiles(c, b0 + lane).tiles;
+        int v = new_tiles<READ>(c, b0 + lane).tiles;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
         total += v;
@@ -58,7 +61,7 @@ __device__ __forceinline__ NewItem first_item(const KvView& c, int per_tile) {
     it.sub = (int)(x % per_tile);
     int64_t base = 0;
     for (int b0 = 0; b0 < c.batch; b0 += 64) {
-        const int v = new_tiles(c, b0 + lane).tiles;
+        const int v = new_tiles<READ>(c, b0 + lane).tiles;
         int64_t incl = v;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) { const int64_t u = __shfl_up(incl, o); if (lane >= o) incl += u; }
@@ -71,16 +74,17 @@ __device__ __forceinline__ NewItem first_item(const KvView& c, int per_tile) {
         }
         base += kv_uniform((int64_t)__shfl(incl, 63));
     }
-    it.s = new_tiles(c, it.b);
+    it.s = new_tiles<READ>(c, it.b);
     return it;
 }
+template <bool READ>
 __device__ __forceinline__ void next_item(const KvView& c, int per_tile, NewItem& it) {
     if (--it.left <= 0) return;
     if (++it.sub < per_tile) return;
     it.sub = 0;
     if (++it.tile < it.s.tiles) return;
     it.tile = 0;
-    do { it.s = new_tiles(c, ++it.b); } while (!it.s.tiles && it.b < c.batch);      // there is one: items are left
+    do { it.s = new_tiles<READ>(c, ++it.b); } while (!it.s.tiles && it.b < c.batch);      // there is one: items are left
 }
 
 // Reading: new rows that stand before position zero (a sequence has more rows than tokens) have no place and give zeros.
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(256) void k_kv_move16(KvView c, KvRows k, KvRows v,
     const int row_head = i / chunks, j = i % chunks * 8, r = row_head / c.heads, h = row_head % c.heads;
     if (r >= c.rows) return;
     int t = 0;
-    char* rec = place_of(c, r, h, t);
+    char* rec = place_of<READ>(c, r, h, t);
     move16<READ>(c, rec, t, d, j, reinterpret_cast<uint16_t*>(k.data) + r * k.row_stride + h * k.head_stride + j,
                  reinterpret_cast<uint16_t*>(v.data) + r * v.row_stride + h * v.head_stride + j);
 }
@@ -151,8 +155,8 @@ template <bool READ>
 __global__ __launch_bounds__(256) void k_kv_tiles16(KvView c, KvRows k, KvRows v, int d) {
     const int lane = threadIdx.x & 63, chunks = d / 8;
     if constexpr (READ) no_place(c, k, v, d);
-    NewItem it = first_item(c, c.heads);
-    for (; it.left > 0; next_item(c, c.heads, it)) {
+    NewItem it = first_item<READ>(c, c.heads);
+    for (; it.left > 0; next_item<READ>(c, c.heads, it)) {
         const int h = it.sub, t0 = (it.s.tile0 + it.tile) * 32;
         for (int u = lane; u < 4 * chunks; u += 64) {
             const int og = u / chunks, j = u % chunks * 8, t = t0 + 8 * og;
@@ -221,7 +225,7 @@ __global__ __launch_bounds__(64) void k_kv_append_row_codes(KvView c, KvRows k, 
     load_row<D, BF>(value ? v : k, r, h, x);          // (of lanes past the end: the first row, not used)
     const float norm = kv_unit_row<D>(x);
     int t = 0;
-    char* rec = in ? place_of(c, r, h, t) : nullptr;
+    char* rec = in ? place_of<false>(c, r, h, t) : nullptr;
     KvTurn<D, false>{pi}(x, y);
     if (!rec) return;
     const int codes = c.page * (D / 2), j = 32 * block + 8 * g;
@@ -306,7 +310,7 @@ __global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, Kv
     const int r = in ? (int)(i / (uint32_t)c.heads) : 0, h = in ? (int)(i % (uint32_t)c.heads) : 0;
     const KvTurnRows<D, true> pi(c.rotation, block);
     int t = 0;
-    const char* const place = place_of(c, r, h, t);
+    const char* const place = place_of<true>(c, r, h, t);
     const char* const rec = place ? place : kv_record(c, 0, h);
     const int codes = c.page * (D / 2);
     const _Float16 norm = reinterpret_cast<const _Float16*>(rec + 2 * codes)[(value ? c.page : 0) + t];
@@ -455,7 +459,7 @@ __global__ __launch_bounds__(kTileThreads, D <= 128 ? 4 : 2) void k_kv_tiles_cod
     }
     __syncthreads();
     const int codes = c.page * (D / 2), per_tile = 2 * c.heads;
-    NewItem it = first_item(c, per_tile);
+    NewItem it = first_item<READ>(c, per_tile);
     if (it.left <= 0) return;
     TileRows<D, READ> next;
     load_tile<D, READ>(c, it.sub >= c.heads ? v : k, it, it.sub >= c.heads ? it.sub - c.heads : it.sub, it.sub >= c.heads, next);
@@ -485,7 +489,7 @@ __global__ __launch_bounds__(kTileThreads, D <= 128 ? 4 : 2) void k_kv_tiles_cod
                 gain[ct] = row_operand<D, BF>(next.w[ct], xh[ct], norm[ct]);
             }
         }
-        next_item(c, per_tile, it);
+        next_item<READ>(c, per_tile, it);
         if (it.left > 0) load_tile<D, READ>(c, it.sub >= c.heads ? v : k, it, it.sub >= c.heads ? it.sub - c.heads : it.sub, it.sub >= c.heads, next);
 #pragma unroll 1
         for (int t = 0; t < NT; ++t) {

@@ -137,13 +137,14 @@ def _type_of(t, name):
 
 
 def _no_gradient(t, name):
-    if t.requires_grad and torch.is_grad_enabled():
+    if torch.is_grad_enabled():
         raise ValueError(f"{name} asks for a gradient, and the cache's calls have none: call them under torch.no_grad()")
 
 
 def _rows(t, name, like, d):
     _on_device(t, name, like)
-    _no_gradient(t, name)
+    if t.requires_grad:
+        _no_gradient(t, name)
     if t.dim() != 3 or t.shape[2] != d:
         raise ValueError(f"{name} must be rows x heads x {d}, got {tuple(t.shape)}")
     row, head, one = t.stride()
@@ -155,7 +156,8 @@ def _rows(t, name, like, d):
 
 def _cache(pool, table, lengths, d, rotation, levels, asked=None, granted=None):
     _on_device(pool, "pool")
-    _no_gradient(pool, "pool")
+    if pool.requires_grad:
+        _no_gradient(pool, "pool")
     if not pool.is_contiguous():
         raise ValueError("pool must be contiguous")
     shape, turn, values = pool.shape, 0, _NO_LEVELS
@@ -175,7 +177,7 @@ def _cache(pool, table, lengths, d, rotation, levels, asked=None, granted=None):
         form, page = _type_of(pool, "pool"), shape[3]
     where, stride, batch, columns = _table(table, pool)
     return _pack_cache(pool.data_ptr(), where, _ints(lengths, "lengths", pool, batch), turn, shape[0], stride, batch, columns, form, page, shape[1], d, values,
-                       _ints(asked, "asked", pool, batch) or 0, _ints(granted, "granted", pool, batch) or 0)
+                       0 if asked is None else _ints(asked, "asked", pool, batch), 0 if granted is None else _ints(granted, "granted", pool, batch))
 
 
 def _starts(starts, table, like):
