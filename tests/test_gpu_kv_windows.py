@@ -65,3 +65,40 @@ def test_row_tiles_that_end_where_the_first_token_is_left_behind(form, kind, d, 
     c, q = heavy_beginning(window, form, d, page, lens, sum(news), 2, kind)
     out, lse = run(c, q, news, window=window)
     ref.check_attention(c, q.cpu(), out, news, lse=lse, window=window)
+
+
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("window,sinks", [(5999, 0), (3000, 0), (2000, 70)])
+def test_row_tiles_in_shares_with_a_window_agree_with_few_rows(form, kind, window, sinks):
+    """128 heads leave four workgroups a head, whose shares are then of more than 64 tiles and cut row tiles: every sequence's last rows
+    against the kernel of few rows.  Roundings of at most `step` of each weight, independent in the two kernels, move a result of about
+    |w|_2 |v| by sqrt(2) step of it in the mean square: five times step; the result's own rounding twice."""
+    import paper_2605_17415_amd as pkg
+    heads, group, d, page, lens, news, last = 128, 2, 64, 64, [6000, 4100], [200, 130], 3
+    need = [-(-n // page) for n in lens]
+    g = torch.Generator(device=DEV).manual_seed(window)
+    table = torch.full((2, max(need)), -1, dtype=torch.int32, device=DEV)
+    order = torch.randperm(sum(need), generator=g, device=DEV).int()
+    table[0], table[1, :need[1]] = order[:need[0]], order[need[0]:]
+    codec = {}
+    if form == "code4":
+        pool = torch.randint(0, 256, (sum(need), heads, page * (d + 4)), generator=g, device=DEV, dtype=torch.uint8)
+        norms = ((torch.rand(sum(need), heads, 2 * page, generator=g, device=DEV) + 0.5) * math.sqrt(d)).half()
+        norms[table[:, 0].long(), :, 0] *= 4
+        pool[..., page * d:] = norms.view(torch.uint8)
+        codec = {"rotation": torch.from_numpy(pkg.ivftq_haar_rotation(d, 3)).to(DEV), "levels": pkg.ivftq_build_codebook(4, d)[0]}
+    else:
+        pool = torch.randn(sum(need), heads, 2, page, d, generator=g, device=DEV).to(ref.TYPES[form])
+        pool[table[:, 0].long(), :, 0, 0] *= 4
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    q = (torch.randn(sum(news), heads * group, d, generator=g, device=DEV) * 1.5).to(ref.TYPES[kind])
+    rows = torch.cat([torch.arange(e - last, e) for e in np.cumsum(news)]).to(DEV)
+    starts, few_starts = (torch.tensor([0] + list(np.cumsum(x)), dtype=torch.int32, device=DEV) for x in (news, [last] * 2))
+    logs, few_logs = torch.empty(q.shape[:2], device=DEV), torch.empty(2 * last, heads * group, device=DEV)
+    few = pkg.kv_attend(q[rows], pool, table, lengths, starts=few_starts, max_new=last, window=window, sinks=sinks, lse=few_logs, **codec)
+    many = pkg.kv_attend(q, pool, table, lengths, starts=starts, max_new=max(news), window=window, sinks=sinks, lse=logs, **codec)
+    torch.cuda.synchronize()
+    far, size = (many[rows].double() - few.double()).norm(dim=-1), few.double().norm(dim=-1)
+    step = 2.0 ** -11 if form == "code4" else ref.HALF[few.dtype]
+    assert (far <= (2 * ref.HALF[few.dtype] + 5 * step) * size + 2.0 ** -18 * math.sqrt(d)).all(), float((far / size).max())
+    assert (logs[rows] - few_logs).abs().max() <= 1e-4
