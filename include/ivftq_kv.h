@@ -106,7 +106,9 @@ int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int
 
 /* ---- pages ------------------------------------------------------------------------------
  * refs[p]: how many table entries name page p, 0 = free.  Free pages are taken lowest first, rows are served in the order
- * given, so equal states give equal results.  table: rows x columns with stride table_stride, -1 = no page; lengths: rows. */
+ * given, so equal states give equal results.  table: rows x columns with stride table_stride, -1 = no page; lengths: rows.
+ * Once a row holds pages, these calls alone change the three.  In particular a row is not cut back by a lower length: the entries
+ * past it would be written over and their pages lost, and a page that a fork shares would be appended to. */
 typedef struct ivftq_kv_pages {
     int32_t* table;
     int32_t* lengths;

@@ -12,15 +12,20 @@
 // workgroups in equal consecutive shares.  A pair that lies whole in a share is finished there; of the others each
 // workgroup leaves at most two parts (one at its start, one at its end), which k_kv_few_join puts together.
 //
-// Measured: 48 sequences of up to 9,000 tokens, 8 heads of 128 in bfloat16, four query heads each: 157 us for 912 MB (5.8 TB/s, the
-// rate of a read).  Four of 131,000 in codes, eight query heads each: 70 us for 328 MB (4.7 TB/s); there 263 vector
+// Measured (medians): 48 sequences of up to 9,000 tokens, 8 heads of 128 in bfloat16, four query heads each: 159 us for 912 MB (5.7
+// TB/s, the rate of a read).  Four of 131,000 in codes, eight query heads each: 72 us for 328 MB (4.6 TB/s); there 263 vector
 // instructions a tile take 63 % of the cycles, 224 of them make levels of codes.
 #pragma once
 #include "kv_kernels.h"
 
 namespace ivftq {
 
-constexpr int kFewRows = 64;          // query rows a key-value head: four column tiles of 16
+// Query rows a key-value head: four column tiles of 16, each of which walks the cache.  Against the kernel of many rows (8 heads of 128,
+// bfloat16, us): 16 sequences of 4,000 tokens 77 and 93 at 64 rows, 106 and 94 at 96; four of 20,000, which leave that kernel's row tiles
+// few, 129 and 410, 182 and 410.  Codes gain more (70 and 165 at 64 rows of the first).  Where the sequences alone fill the chip and are
+// short the other kernel is ahead from about 16 rows on (64 of 1,000 tokens: 40 and 35 at 16 rows, 101 and 36 at 64), but the host, which
+// chooses, knows no lengths.
+constexpr int kFewRows = 64;
 constexpr int kFewTile = 32;          // tokens of a wavefront's step
 constexpr int kFewMaxWgs = 1024;      // workgroups that share the tiles, at most: as many as the chip holds at once
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -573,16 +578,15 @@ __global__ __launch_bounds__(512) void k_kv_few_join(FewArgs f) {
             float top = -INFINITY, l = 0.f;
             // of the pair's first share the pair has the last part, of the others the first
             const int64_t base = (int64_t)blockIdx.y * 2 * f.wgs;
-            const bool begins = (int64_t)w0 * share <= lo;
             for (int w = w0 + lane; w <= w1; w += 64)
-                top = fmaxf(top, f.part_ml[((base + 2 * w + (w == w0 && begins ? 1 : 0)) * 16 + row) * 2]);
+                top = fmaxf(top, f.part_ml[((base + 2 * w + (w == w0)) * 16 + row) * 2]);
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
             for (int v0 = w0; v0 <= w1; v0 += 64) {
                 const int w = v0 + lane;
                 float turn = 0.f;
                 if (w <= w1) {
-                    const float2 u = *reinterpret_cast<const float2*>(f.part_ml + ((base + 2 * w + (w == w0 && begins ? 1 : 0)) * 16 + row) * 2);
+                    const float2 u = *reinterpret_cast<const float2*>(f.part_ml + ((base + 2 * w + (w == w0)) * 16 + row) * 2);
                     turn = u.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u.x - top);
                     l += u.y * turn;
                 }
@@ -591,7 +595,7 @@ __global__ __launch_bounds__(512) void k_kv_few_join(FewArgs f) {
 #pragma unroll 8
                 for (int i = beside; i < many; i += kBeside) {
                     if (kBeside * kPart < 64 && beside >= kBeside) break;
-                    const int64_t slot = base + 2 * (v0 + i) + (v0 + i == w0 && begins ? 1 : 0);
+                    const int64_t slot = base + 2 * (v0 + i) + (v0 + i == w0);
                     const float t = weight[wave][i];
                     const float4 u = *reinterpret_cast<const float4*>(f.part + (slot * 16 + row) * D + j);
                     acc.x += u.x * t; acc.y += u.y * t; acc.z += u.z * t; acc.w += u.w * t;

@@ -351,8 +351,8 @@ __global__ __launch_bounds__(64) void k_kv_read_row_codes(KvView c, KvRows k, Kv
 // two that puts the row's length between 2^8 and 2^9 (what that loses lies 2^-25 under the row's largest value), so two
 // products do, and the results are divided by the row's length afterwards.  Reading: the levels as two parts as well, three
 // products.  Writing is bound by the vector unit, half of whose operations look for levels; 363,000 rows of keys and as many of values
-// (float16, d = 128) take 104 us to write and 74 us to read back, where neighbouring lanes write neighbouring pieces (95 us where a
-// lane's pieces of a row lay 64 bytes apart).
+// (float16, d = 128) take 125 us to write and 82 us to read back (medians; 114 and 75 at the least), where neighbouring lanes write
+// neighbouring pieces (20 us more where a lane's pieces of a row lay 64 bytes apart).
 template <int D> constexpr int kOutputs = D > 128 ? D / 2 : D;             // coordinates that a workgroup computes
 template <int D> constexpr int kTurnBytes = kOutputs<D> * D * 4;
 constexpr int kTileThreads = 512;

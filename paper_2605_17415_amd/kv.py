@@ -344,7 +344,8 @@ class KVCache:
 
     A step of a model: `reserve` room for the new tokens, then for every layer `append` its keys and values and `attend`.  Rows
     without new tokens have none between their `starts`.  A row whose reservation was refused keeps its tokens: `append` leaves it
-    out until a `reserve` grants it what it asks for, and what `attend` gives for its new rows means nothing."""
+    out until a `reserve` grants it what it asks for, and what `attend` gives for its new rows means nothing.  lengths are not to be
+    lowered by hand (a row is emptied by `free`)."""
 
     def __init__(self, layers: int, heads: int, d: int, pages: int, sequences: int, tokens: int, page: int = 64, dtype=torch.bfloat16, codes: bool = False,
                  rotation_seed: int = 0, device="cuda"):
