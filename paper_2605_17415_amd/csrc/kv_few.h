@@ -12,7 +12,7 @@
 // workgroups in equal consecutive shares.  A pair that lies whole in a share is finished there; of the others each
 // workgroup leaves at most two parts (one at its start, one at its end), which k_kv_few_join puts together.
 //
-// Measured (medians): 48 sequences of up to 9,000 tokens, 8 heads of 128 in bfloat16, four query heads each: 159 us for 912 MB (5.7
+// Measured (medians): 48 sequences of up to 9,000 tokens, 8 heads of 128 in bfloat16, four query heads each: 161 us for 912 MB (5.7
 // TB/s, the rate of a read).  Four of 131,000 in codes, eight query heads each: 72 us for 328 MB (4.6 TB/s); there 263 vector
 // instructions a tile take 63 % of the cycles, 224 of them make levels of codes.
 #pragma once
