@@ -87,3 +87,48 @@ def test_with_the_calls_themselves():
     for one in (dict(asked=ints([1] * 4)), dict(granted=ints([1] * 4)), dict(asked=ints([1] * 3), granted=ints([1] * 4)), dict(asked=ints([1] * 4).long(), granted=ints([1] * 4))):
         with pytest.raises((TypeError, ValueError, pkg.IvftqError)):
             pkg.kv_append(pool, k, v, table, lengths, **one)
+
+
+@pytest.mark.parametrize("codes", (False, True))
+def test_a_recorded_step_leaves_refused_rows_out(codes):
+    """Reserve, append and attend recorded once; replayed until the pages run out and past that, with eager reads between."""
+    cache = _pkg().KVCache(1, 2, 64, pages=3, sequences=2, tokens=400, page=16, codes=codes, device=DEV)
+    cache.reserve(ints([14, 15]))
+    k, v = rows(1, 29)
+    starts = ints([0, 14, 29])
+    cache.append(0, k, v, starts)
+    one, two = rows(2, 2)
+    q, counts, out = torch.randn(2, 4, 64, device=DEV).bfloat16(), ints([1, 1]), torch.empty(2, 4, 64, dtype=torch.bfloat16, device=DEV)
+
+    def step():
+        granted = cache.reserve(counts)
+        cache.append(0, one, two)
+        cache.attend(0, q, out=out)
+        return granted
+
+    state = [x.clone() for x in (cache.table, cache.lengths, cache.refs, cache.pools)]
+    step()                                                  # (what a first call sets up is not recorded)
+    for x, y in zip((cache.table, cache.lengths, cache.refs, cache.pools), state):
+        x.copy_(y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        granted = step()
+    lengths = [14, 15]
+    for n in range(8):                                      # row 1 takes the third page for its 17th token, row 0 ends at its 16th
+        before = [content(cache, r, lengths[r]) for r in range(2)]
+        for x, seed in ((one, 10 + n), (two, 30 + n)):
+            x.copy_(rows(seed, 2)[0])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = [1 if lengths[0] < 16 else 0, 1]
+        assert granted.tolist() == want
+        for r in range(2):
+            assert torch.equal(content(cache, r, lengths[r]), before[r]), (n, r)
+            lengths[r] += want[r]
+            if want[r]:
+                now = content(cache, r, lengths[r])[:, -1]
+                assert (now[0] - one[r]).float().norm() < 0.2 * one[r].float().norm() and (now[1] - two[r]).float().norm() < 0.2 * two[r].float().norm()
+        assert cache.lengths.tolist() == lengths
+    assert lengths == [16, 23]
