@@ -23,7 +23,7 @@ KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_h
         w.split = capacity > 512;
     } else {
         w.row_tiles = (int)((cols + kManyRows - 1) / kManyRows);
-        const int64_t wgs = (int64_t)batch * kv_heads * w.row_tiles, room = 256 * (d <= 128 ? 2 : 1);       // workgroups that the compute units hold (of d = 64: three each would fit)
+        const int64_t wgs = (int64_t)batch * kv_heads * w.row_tiles, room = 256 * (d <= 128 ? 2 : 1);       // workgroups that the compute units hold (of d = 64 more would fit)
         // Up to twice as many, codes gain by sharing (752 workgroups of 16,000 keys: 1291 us, 1398 uncut), 16 bits do not (920
         // and 900).
         if (wgs < (format == IVFTQ_KV_CODE4 ? 2 : 1) * room && kv_heads <= room && capacity > 512) w.shared = (int)(room / kv_heads);
