@@ -104,6 +104,42 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
 /* -1 for arguments that ivftq_kv_attend refuses. */
 int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads, int32_t max_new);
 
+/* ---- attention over chosen pages ---------------------------------------------------------
+ * Over a long cache a row needs few pages.  A page's digest bounds its keys,
+ *     low[j] = min_t k_t[j]     high[j] = max_t k_t[j]     (codes: of the rotated keys, norm * level)
+ * and a row's queries with it the products that they can have with any key of the page,
+ *     score = sum_g sum_j max(q_g[j] low[j], q_g[j] high[j])  >=  sum_g max_t <q_g, k_t>     (g: the key-value head's query heads).
+ * Each row and key-value head attends to the pages of the highest scores.  A step of a model: ivftq_kv_append, ivftq_kv_digest,
+ * ivftq_kv_score, ivftq_kv_select, ivftq_kv_attend_pages.
+ * digests: for each page, one after the other, heads x (low[d], high[d]) in the cache's type (codes: float16), 16-byte aligned; an
+ * array like a pool, whose pages ivftq_kv_fork_pools and ivftq_kv_compact_pools move with the pool's. */
+
+/* Digests of the pages that hold the new rows, from the rows that ivftq_kv_append has written (same starts, asked and granted): a page
+ * whose first token is new gets the digest of its new tokens, one that goes on has them added to the digest that it has.  With every
+ * token of a sequence as a new row its digests are made afresh.  Coordinates that are no number count for nothing. */
+ivftq_status ivftq_kv_digest(const ivftq_kv_cache* cache, void* digests, const int32_t* starts, void* stream);
+
+/* scores: rows x heads x columns floats; -infinity where a page holds no token that the row sees (behind its position, no page).
+ * q, starts, max_new as in ivftq_kv_attend; rows that it gives no result keep their scores.  workspace: ivftq_kv_score_workspace
+ * bytes, 256-byte aligned (0 for the 16-bit formats). */
+ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts,
+                            int32_t max_new, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t ivftq_kv_score_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads);
+
+/* chosen: rows x heads x count numbers: of the columns that a row's position p reaches (column c: c * page <= p) the first `first` and
+ * the last `last`, and those of the highest scores (ties: the lowest column; -infinity and what is no number: never), ascending, -1
+ * behind them.  first + last <= count <= 4096.  Rows of no sequence get -1 throughout. */
+ivftq_status ivftq_kv_select(const float* scores, const int32_t* lengths, const int32_t* starts, int64_t rows, int32_t batch, int32_t heads,
+                             int32_t columns, int32_t page, int32_t count, int32_t first, int32_t last, int32_t* chosen, void* stream);
+
+/* ivftq_kv_attend where a row and key-value head sees, of the tokens up to its own, those of the columns chosen[row][head][0 .. count - 1]
+ * (count: 1 to 4096).  Columns ascend; an entry that is not above every one before it, or names no page, is passed over. */
+ivftq_status ivftq_kv_attend_pages(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse,
+                                   const int32_t* starts, int32_t max_new, const int32_t* chosen, int32_t count, float scale,
+                                   void* workspace, int64_t workspace_bytes, void* stream);
+/* -1 for arguments that ivftq_kv_attend_pages refuses. */
+int64_t ivftq_kv_attend_pages_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads, int32_t max_new, int32_t count);
+
 /* ---- pages ------------------------------------------------------------------------------
  * refs[p]: how many table entries name page p, 0 = free.  Free pages are taken lowest first, rows are served in the order
  * given, so equal states give equal results.  table: rows x columns with stride table_stride, -1 = no page; lengths: rows.
@@ -153,6 +189,11 @@ ivftq_status ivftq_kv_trim(const ivftq_kv_pages* state, int32_t window, int32_t 
  * int32.  The lengths and the page size of the state are not read (page: any that is allowed). */
 ivftq_status ivftq_kv_compact(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, int32_t* used_out, int32_t* scratch,
                               void* stream);
+/* The two for `groups` arrays (1 to 8) of records whose pages are numbered alike: a cache's pools and its digests. */
+ivftq_status ivftq_kv_fork_pools(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, int32_t groups, const int32_t* parents,
+                                 const int32_t* children, int32_t n, int32_t* done, int32_t* scratch, void* stream);
+ivftq_status ivftq_kv_compact_pools(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, int32_t groups, int32_t* used_out,
+                                    int32_t* scratch, void* stream);
 /* Record of page src[i] to page dst[i] in every layer (device, n numbers each; a pair with a number out of range is passed
  * over).  No page may be both source and destination, or destination twice. */
 ivftq_status ivftq_kv_copy(const ivftq_kv_pools* pools, const int32_t* src, const int32_t* dst, int32_t n, void* stream);

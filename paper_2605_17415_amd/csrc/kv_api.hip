@@ -4,7 +4,7 @@
 #include <cstdio>
 #include <cstring>
 
-#include "kv_many.h"
+#include "kv_pick.h"
 
 namespace ivftq {
 
@@ -13,6 +13,16 @@ extern template hipError_t kv_attend_d<96>(const KvAttend&, const KvWork&, int, 
 extern template hipError_t kv_attend_d<128>(const KvAttend&, const KvWork&, int, hipStream_t);
 extern template hipError_t kv_attend_d<192>(const KvAttend&, const KvWork&, int, hipStream_t);
 extern template hipError_t kv_attend_d<256>(const KvAttend&, const KvWork&, int, hipStream_t);
+extern template hipError_t kv_score_d<64>(const KvAttend&, const void*, float*, int, hipStream_t);
+extern template hipError_t kv_picked_d<64>(const KvAttend&, const PickWork&, const int32_t*, int, int, hipStream_t);
+extern template hipError_t kv_score_d<96>(const KvAttend&, const void*, float*, int, hipStream_t);
+extern template hipError_t kv_picked_d<96>(const KvAttend&, const PickWork&, const int32_t*, int, int, hipStream_t);
+extern template hipError_t kv_score_d<128>(const KvAttend&, const void*, float*, int, hipStream_t);
+extern template hipError_t kv_picked_d<128>(const KvAttend&, const PickWork&, const int32_t*, int, int, hipStream_t);
+extern template hipError_t kv_score_d<192>(const KvAttend&, const void*, float*, int, hipStream_t);
+extern template hipError_t kv_picked_d<192>(const KvAttend&, const PickWork&, const int32_t*, int, int, hipStream_t);
+extern template hipError_t kv_score_d<256>(const KvAttend&, const void*, float*, int, hipStream_t);
+extern template hipError_t kv_picked_d<256>(const KvAttend&, const PickWork&, const int32_t*, int, int, hipStream_t);
 
 KvWork kv_work(int format, int d, int batch, int kv_heads, int64_t rows, int q_heads, int max_new, int64_t capacity) {
     KvWork w{};
@@ -56,6 +66,54 @@ hipError_t launch_kv_attend(const KvAttend& a, const KvWork& w, int d, int forma
         case 128: return kv_attend_d<128>(a, w, format, st);
         case 192: return kv_attend_d<192>(a, w, format, st);
         default: return kv_attend_d<256>(a, w, format, st);
+    }
+}
+
+PickWork pick_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int page, int columns, int count) {
+    PickWork w{};
+    const int64_t all = rows * q_heads;
+    w.col_tiles = (q_heads / kv_heads + 15) / 16;
+    // as many workgroups as the chip holds, but four tiles for each: one for each of its wavefronts
+    const int64_t pairs = rows * kv_heads * w.col_tiles, most = (int64_t)(count < columns ? count : columns) * page / kFewTile / 4;
+    int64_t splits = pairs ? 256 * (d <= 64 ? 4 : (d <= 128 ? 3 : 1)) / pairs : 1;
+    splits = splits < most ? splits : most;
+    w.splits = (int)(splits < 1 ? 1 : (splits < 64 ? splits : 64));
+    int64_t at = 0;
+    auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
+    if (format == IVFTQ_KV_CODE4) {
+        w.z = room(all * d * 4);
+        w.zn = room(all * 4);
+        if (w.splits == 1) w.whole = room(all * d * 4);
+    }
+    if (w.splits > 1) {
+        w.part = room(pairs * w.splits * 16 * d * 4);
+        w.ml = room(pairs * w.splits * 16 * 8);
+    }
+    w.bytes = at;
+    return w;
+}
+
+int64_t score_work(int format, int d, int64_t all, int64_t* zn) {
+    *zn = round_up64(all * d * 4, 256);
+    return format == IVFTQ_KV_CODE4 ? *zn + round_up64(all * 4, 256) : 0;
+}
+
+hipError_t launch_kv_score(const KvAttend& a, const void* digests, float* scores, int d, int format, hipStream_t st) {
+    switch (d) {
+        case 64: return kv_score_d<64>(a, digests, scores, format, st);
+        case 96: return kv_score_d<96>(a, digests, scores, format, st);
+        case 128: return kv_score_d<128>(a, digests, scores, format, st);
+        case 192: return kv_score_d<192>(a, digests, scores, format, st);
+        default: return kv_score_d<256>(a, digests, scores, format, st);
+    }
+}
+hipError_t launch_kv_picked(const KvAttend& a, const PickWork& w, const int32_t* chosen, int count, int d, int format, hipStream_t st) {
+    switch (d) {
+        case 64: return kv_picked_d<64>(a, w, chosen, count, format, st);
+        case 96: return kv_picked_d<96>(a, w, chosen, count, format, st);
+        case 128: return kv_picked_d<128>(a, w, chosen, count, format, st);
+        case 192: return kv_picked_d<192>(a, w, chosen, count, format, st);
+        default: return kv_picked_d<256>(a, w, chosen, count, format, st);
     }
 }
 
@@ -211,6 +269,34 @@ ivftq_status move_rows(const ivftq_kv_cache* cache, const ivftq_kv_rows* k, cons
     return done(e, read ? "ivftq_kv_read" : "ivftq_kv_append");
 }
 
+// Queries of a call on chosen pages, or of scores.
+ivftq_status check_queries(const ivftq_kv_cache* c, const ivftq_kv_rows* q, const int32_t* starts, int32_t max_new) {
+    if (ivftq_status e = check_cache(c)) return e;
+    if (!q) return refuse(IVFTQ_INVALID_ARG, "q is NULL");
+    if (q->heads < 1 || q->heads % c->heads) return refuse(IVFTQ_INVALID_ARG, "%d query heads over %d key-value heads", q->heads, c->heads);
+    if (ivftq_status e = check_rows(q, "q", q->heads, c->d, c, starts)) return e;
+    if (max_new < 1) return refuse(IVFTQ_INVALID_ARG, "max_new = %d", max_new);
+    return IVFTQ_OK;
+}
+bool known_sizes(const ivftq_kv_cache* c, int64_t rows, int32_t q_heads) {
+    if (rows >= 0 && rows <= INT32_MAX / 2 && q_heads >= 1 && q_heads % c->heads == 0 && rows * q_heads <= INT32_MAX) return true;
+    refuse(IVFTQ_INVALID_ARG, "%lld rows of %d query heads over %d", (long long)rows, q_heads, c->heads);
+    return false;
+}
+KvAttend attend_of(const ivftq_kv_cache& c, const ivftq_kv_rows& q, const int32_t* starts, int32_t max_new, void* workspace) {
+    KvAttend a{};
+    a.c = view_of(c, starts, q.rows, true);
+    a.q = rows_of(q);
+    a.group = q.heads / c.heads;
+    a.max_new = !starts ? 1 : (max_new < q.rows ? max_new : (int32_t)q.rows);
+    a.work = static_cast<char*>(workspace);
+    return a;
+}
+ivftq_status check_work(const void* workspace, int64_t bytes, int64_t need) {
+    if (!need || (workspace && bytes >= need && aligned(workspace, 256))) return IVFTQ_OK;
+    return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)bytes, (long long)need);
+}
+
 ivftq_status check_pages(const ivftq_kv_pages* s, bool lengths = true) {
     if (!s) return refuse(IVFTQ_INVALID_ARG, "state is NULL");
     if (!known_page(s->page)) return refuse(IVFTQ_UNSUPPORTED, "page = %d: a power of two from 16 to 1024", s->page);
@@ -226,6 +312,16 @@ ivftq_status check_pools(const ivftq_kv_pools* p) {
         (p->layers > 1 && p->layer_stride < p->pages * p->page_bytes))
         return refuse(IVFTQ_INVALID_ARG, "pools: %d layers, %lld bytes apart, of %lld records of %lld bytes (multiples of 16)", p->layers, (long long)p->layer_stride,
                       (long long)p->pages, (long long)p->page_bytes);
+    return IVFTQ_OK;
+}
+
+ivftq_status check_groups(const ivftq_kv_pages& state, const ivftq_kv_pools* p, int32_t groups) {
+    if (groups < 1 || groups > 8) return refuse(IVFTQ_INVALID_ARG, "groups = %d: 1 to 8", groups);
+    if (!p) return refuse(IVFTQ_INVALID_ARG, "pools is NULL");
+    for (int i = 0; i < groups; ++i) {
+        if (ivftq_status e = check_pools(p + i)) return e;
+        if (p[i].pages != state.pages) return refuse(IVFTQ_INVALID_ARG, "pools of %lld pages, counts of %lld", (long long)p[i].pages, (long long)state.pages);
+    }
     return IVFTQ_OK;
 }
 
@@ -288,21 +384,106 @@ ivftq_status ivftq_kv_attend(const ivftq_kv_cache* cache, const ivftq_kv_rows* q
     return done(launch_kv_attend(a, w, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_attend");
 }
 
+ivftq_status ivftq_kv_digest(const ivftq_kv_cache* cache, void* digests, const int32_t* starts, void* stream) {
+    if (ivftq_status e = check_cache(cache)) return e;
+    if (!digests || !aligned(digests, 16)) return refuse(IVFTQ_INVALID_ARG, "digests is NULL or not 16-byte aligned");
+    if (!cache->batch) return IVFTQ_OK;
+    // the number of rows is not asked for: with starts it is what the last of them says
+    KvView c = view_of(*cache, starts, starts ? INT32_MAX : cache->batch, false);
+    c.asked = cache->asked;
+    c.granted = cache->granted;
+    return done(launch_kv_digest(c, digests, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_digest");
+}
+
+int64_t ivftq_kv_score_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads) {
+    if (check_cache(cache) || !known_sizes(cache, rows, q_heads)) return -1;
+    int64_t zn;
+    return score_work(cache->format, cache->d, rows * q_heads, &zn);
+}
+ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts, int32_t max_new,
+                            void* workspace, int64_t workspace_bytes, void* stream) {
+    if (ivftq_status e = check_queries(cache, q, starts, max_new)) return e;
+    if (!digests || !aligned(digests, 16)) return refuse(IVFTQ_INVALID_ARG, "digests is NULL or not 16-byte aligned");
+    if (!q->rows || !cache->batch) return IVFTQ_OK;
+    if (!scores || !aligned(scores, 4)) return refuse(IVFTQ_INVALID_ARG, "scores is NULL or not 4-byte aligned");
+    const KvAttend a = attend_of(*cache, *q, starts, max_new, workspace);
+    if ((int64_t)cache->batch * cache->heads * ((a.max_new + 15) / 16) > INT32_MAX)
+        return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups: %d sequences of %d heads and up to %d rows", cache->batch, cache->heads, a.max_new);
+    int64_t zn;
+    if (ivftq_status e = check_work(workspace, workspace_bytes, score_work(cache->format, cache->d, q->rows * q->heads, &zn))) return e;
+    return done(launch_kv_score(a, digests, scores, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_score");
+}
+
+ivftq_status ivftq_kv_select(const float* scores, const int32_t* lengths, const int32_t* starts, int64_t rows, int32_t batch, int32_t heads, int32_t columns,
+                             int32_t page, int32_t count, int32_t first, int32_t last, int32_t* chosen, void* stream) {
+    if (!known_page(page)) return refuse(IVFTQ_UNSUPPORTED, "page = %d: a power of two from 16 to 1024", page);
+    if (heads < 1 || heads > kMaxHeads) return refuse(IVFTQ_UNSUPPORTED, "heads = %d: 1 to %d", heads, kMaxHeads);
+    if (batch < 0 || batch > kMaxBatch || columns < 1 || columns > kMaxColumns) return refuse(IVFTQ_INVALID_ARG, "%d sequences of %d columns", batch, columns);
+    if (rows < 0 || rows * heads > INT32_MAX) return refuse(IVFTQ_INVALID_ARG, "%lld rows of %d heads", (long long)rows, heads);
+    if (!starts && rows != batch) return refuse(IVFTQ_INVALID_ARG, "%lld rows for %d sequences without starts", (long long)rows, batch);
+    if (count < 1 || count > kMostPicks) return refuse(IVFTQ_UNSUPPORTED, "count = %d: 1 to %d", count, kMostPicks);
+    if (first < 0 || last < 0 || (int64_t)first + last > count) return refuse(IVFTQ_INVALID_ARG, "first = %d and last = %d of %d", first, last, count);
+    if (!rows) return IVFTQ_OK;
+    if (!scores || !chosen || (batch && !lengths)) return refuse(IVFTQ_INVALID_ARG, "scores, lengths or chosen is NULL");
+    if (!aligned(scores, 4) || !aligned(chosen, 4) || !aligned(lengths, 4)) return refuse(IVFTQ_INVALID_ARG, "scores, lengths and chosen are 4-byte aligned");
+    KvSelect s{scores, chosen, {}, count, first, last};
+    s.c.lengths = lengths;
+    s.c.starts = starts;
+    s.c.batch = batch;
+    s.c.columns = columns;
+    s.c.page = page;
+    s.c.page_log2 = __builtin_ctz((unsigned)page);
+    s.c.heads = heads;
+    s.c.rows = (int32_t)rows;
+    return done(launch_kv_select(s, static_cast<hipStream_t>(stream)), "ivftq_kv_select");
+}
+
+int64_t ivftq_kv_attend_pages_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads, int32_t max_new, int32_t count) {
+    if (check_cache(cache) || !known_sizes(cache, rows, q_heads)) return -1;
+    if (max_new < 1 || count < 1 || count > kMostPicks) {
+        refuse(IVFTQ_INVALID_ARG, "max_new = %d, count = %d: 1 to %d", max_new, count, kMostPicks);
+        return -1;
+    }
+    return pick_work(cache->format, cache->d, cache->heads, rows, q_heads, cache->page, cache->columns, count).bytes;
+}
+ivftq_status ivftq_kv_attend_pages(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse, const int32_t* starts,
+                                   int32_t max_new, const int32_t* chosen, int32_t count, float scale, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (ivftq_status e = check_queries(cache, q, starts, max_new)) return e;
+    if (!out) return refuse(IVFTQ_INVALID_ARG, "out is NULL");
+    if (ivftq_status e = check_rows(out, "out", q->heads, cache->d, cache, starts)) return e;
+    if (q->rows != out->rows || q->type != out->type) return refuse(IVFTQ_INVALID_ARG, "out has the rows and the type of q");
+    if (count < 1 || count > kMostPicks) return refuse(IVFTQ_UNSUPPORTED, "count = %d: 1 to %d", count, kMostPicks);
+    if (!std::isfinite(scale)) return refuse(IVFTQ_INVALID_ARG, "scale is no number");
+    if (!q->rows || !cache->batch) return IVFTQ_OK;
+    if (!chosen || !aligned(chosen, 4)) return refuse(IVFTQ_INVALID_ARG, "chosen is NULL or not 4-byte aligned");
+    if (cache->format != IVFTQ_KV_CODE4 && q->data == out->data) return refuse(IVFTQ_INVALID_ARG, "out stands where q does: only a cache of codes allows that");
+    const PickWork w = pick_work(cache->format, cache->d, cache->heads, q->rows, q->heads, cache->page, cache->columns, count);
+    if (ivftq_status e = check_work(workspace, workspace_bytes, w.bytes)) return e;
+    KvAttend a = attend_of(*cache, *q, starts, max_new, workspace);
+    a.out = rows_of(*out);
+    a.lse = lse;
+    a.scale = scale;
+    return done(launch_kv_picked(a, w, chosen, count, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_attend_pages");
+}
+
 ivftq_status ivftq_kv_reserve(const ivftq_kv_pages* state, const int32_t* counts, int32_t* granted, int32_t* scratch, void* stream) {
     if (ivftq_status e = check_pages(state)) return e;
     if (!counts || !granted || !scratch) return refuse(IVFTQ_INVALID_ARG, "counts, granted or scratch is NULL");
     if (!state->rows) return IVFTQ_OK;
     return done(launch_kv_reserve(*state, counts, granted, scratch, static_cast<hipStream_t>(stream)), "ivftq_kv_reserve");
 }
-ivftq_status ivftq_kv_fork(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, const int32_t* parents, const int32_t* children, int32_t n,
-                           int32_t* done_out, int32_t* scratch, void* stream) {
+ivftq_status ivftq_kv_fork_pools(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, int32_t groups, const int32_t* parents, const int32_t* children,
+                                 int32_t n, int32_t* done_out, int32_t* scratch, void* stream) {
     if (ivftq_status e = check_pages(state)) return e;
-    if (ivftq_status e = check_pools(pools)) return e;
-    if (pools->pages != state->pages) return refuse(IVFTQ_INVALID_ARG, "pools of %lld pages, counts of %lld", (long long)pools->pages, (long long)state->pages);
+    if (ivftq_status e = check_groups(*state, pools, groups)) return e;
     if (n < 0 || n > 65536) return refuse(IVFTQ_INVALID_ARG, "n = %d: 0 to 65536", n);
     if (!n) return IVFTQ_OK;
     if (!parents || !children || !done_out || !scratch) return refuse(IVFTQ_INVALID_ARG, "parents, children, done or scratch is NULL");
-    return done(launch_kv_fork(*state, *pools, parents, children, n, done_out, scratch, static_cast<hipStream_t>(stream)), "ivftq_kv_fork");
+    return done(launch_kv_fork(*state, pools, groups, parents, children, n, done_out, scratch, static_cast<hipStream_t>(stream)), "ivftq_kv_fork");
+}
+ivftq_status ivftq_kv_fork(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, const int32_t* parents, const int32_t* children, int32_t n,
+                           int32_t* done_out, int32_t* scratch, void* stream) {
+    return ivftq_kv_fork_pools(state, pools, 1, parents, children, n, done_out, scratch, stream);
 }
 ivftq_status ivftq_kv_free(const ivftq_kv_pages* state, const int32_t* rows, int32_t n, void* stream) {
     if (ivftq_status e = check_pages(state)) return e;
@@ -314,12 +495,14 @@ ivftq_status ivftq_kv_trim(const ivftq_kv_pages* state, int32_t window, int32_t 
     if (window < 1 || sinks < 0) return refuse(IVFTQ_INVALID_ARG, "window = %d, sinks = %d", window, sinks);
     return done(launch_kv_trim(*state, window, sinks, static_cast<hipStream_t>(stream)), "ivftq_kv_trim");
 }
-ivftq_status ivftq_kv_compact(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, int32_t* used_out, int32_t* scratch, void* stream) {
+ivftq_status ivftq_kv_compact_pools(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, int32_t groups, int32_t* used_out, int32_t* scratch, void* stream) {
     if (ivftq_status e = check_pages(state, false)) return e;
-    if (ivftq_status e = check_pools(pools)) return e;
-    if (pools->pages != state->pages) return refuse(IVFTQ_INVALID_ARG, "pools of %lld pages, counts of %lld", (long long)pools->pages, (long long)state->pages);
+    if (ivftq_status e = check_groups(*state, pools, groups)) return e;
     if (!used_out || !scratch) return refuse(IVFTQ_INVALID_ARG, "used_out or scratch is NULL");
-    return done(launch_kv_compact(*state, *pools, used_out, scratch, static_cast<hipStream_t>(stream)), "ivftq_kv_compact");
+    return done(launch_kv_compact(*state, pools, groups, used_out, scratch, static_cast<hipStream_t>(stream)), "ivftq_kv_compact");
+}
+ivftq_status ivftq_kv_compact(const ivftq_kv_pages* state, const ivftq_kv_pools* pools, int32_t* used_out, int32_t* scratch, void* stream) {
+    return ivftq_kv_compact_pools(state, pools, 1, used_out, scratch, stream);
 }
 ivftq_status ivftq_kv_copy(const ivftq_kv_pools* pools, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
     if (ivftq_status e = check_pools(pools)) return e;

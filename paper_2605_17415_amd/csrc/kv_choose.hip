@@ -1,0 +1,282 @@
+// Digests of the key-value cache's pages, and the pages that a row is given for their scores.
+#include "kv_kernels.h"
+
+namespace ivftq {
+namespace {
+
+// ---- digests ---------------------------------------------------------------------------------------------------------
+// The smallest and the largest value of each key coordinate: comparisons only, so a digest is exact and the order of its tokens does not
+// matter.  Bound by the bytes of the new keys.
+
+// Pages of a sequence that hold new rows.
+struct NewPages { int lo, end, col0, count; };          // positions of the new rows, first column, number of pages
+__device__ __forceinline__ NewPages new_pages(const KvView& c, int b) {
+    NewPages p{0, 0, 0, 0};
+    if (b >= c.batch || kv_refused(c, b)) return p;
+    int first, count;
+    kv_new_rows(c, b, first, count);
+    p.end = kv_length(c, b);
+    p.lo = p.end > count ? p.end - count : 0;
+    p.col0 = p.lo >> c.page_log2;
+    p.count = count > 0 && p.end > p.lo ? ((p.end - 1) >> c.page_log2) - p.col0 + 1 : 0;
+    return p;
+}
+
+// Eight coordinates of a key: 16 bits each, or codes and the row's norm.
+template <int F>
+struct KeyPiece {
+    uintx4 w;
+    uint32_t codes;
+    float norm;
+    __device__ __forceinline__ void load(const KvView& c, const char* rec, int t, int d, int j) {
+        if constexpr (F == IVFTQ_KV_CODE4) {
+            codes = *reinterpret_cast<const uint32_t*>(rec + (int64_t)t * (d / 2) + j / 2);
+            norm = (float)reinterpret_cast<const _Float16*>(rec + (int64_t)c.page * d)[t];
+        } else {
+            w = *reinterpret_cast<const uintx4*>(rec + ((int64_t)t * d + j) * 2);
+        }
+    }
+    // level: the sixteen levels by half byte, in LDS
+    __device__ __forceinline__ float value(int e, const float* level) const {
+        if constexpr (F == IVFTQ_KV_CODE4) return norm * level[codes >> 4 * e & 15];
+        else return kv_to_float<F == IVFTQ_KV_BF16>(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffff);
+    }
+};
+
+struct Box {
+    float low[8], high[8];
+    __device__ __forceinline__ Box() {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { low[e] = INFINITY; high[e] = -INFINITY; }
+    }
+    template <int F>
+    __device__ __forceinline__ void add(const KeyPiece<F>& k, const float* level) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = k.value(e, level);
+            low[e] = fminf(low[e], v);
+            high[e] = fmaxf(high[e], v);
+        }
+    }
+    // into the digest of a page (at: its eight lowest values, D values before its eight highest), with what stands there
+    template <bool BF>
+    __device__ __forceinline__ void store(uint16_t* at, int d, bool goes_on) {
+        if (goes_on) {
+            const uintx4 l = *reinterpret_cast<const uintx4*>(at), h = *reinterpret_cast<const uintx4*>(at + d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                low[e] = fminf(low[e], kv_to_float<BF>(l[e >> 1] >> 16 * (e & 1) & 0xffff));
+                high[e] = fmaxf(high[e], kv_to_float<BF>(h[e >> 1] >> 16 * (e & 1) & 0xffff));
+            }
+        }
+        uintx4 l, h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { l[e] = kv_pack2<BF>(low[2 * e], low[2 * e + 1]); h[e] = kv_pack2<BF>(high[2 * e], high[2 * e + 1]); }
+        *reinterpret_cast<uintx4*>(at) = l;
+        *reinterpret_cast<uintx4*>(at + d) = h;
+    }
+};
+
+__device__ __forceinline__ void level_table(const KvView& c, float* level) {
+    if (threadIdx.x < 16) level[threadIdx.x] = threadIdx.x & 8 ? -c.level[threadIdx.x & 7] : c.level[threadIdx.x & 7];
+    __syncthreads();
+}
+
+// One new row a sequence: a thread eight coordinates of a head.
+template <int F>
+__global__ __launch_bounds__(256) void k_kv_digest_row(KvView c, uint16_t* digests, int d) {
+    __shared__ float level[16];
+    if constexpr (F == IVFTQ_KV_CODE4) level_table(c, level);
+    const int chunks = d / 8;
+    const int64_t i = (int64_t)kv_workgroup() * 256 + threadIdx.x, row_head = i / chunks;
+    const int j = (int)(i % chunks) * 8, r = (int)(row_head / c.heads), h = (int)(row_head % c.heads);
+    if (row_head >= (int64_t)c.rows * c.heads || kv_refused(c, r)) return;
+    const int pos = kv_length(c, r) - 1;
+    const int64_t page = pos < 0 ? -1 : kv_page(c, r, pos);
+    if (page < 0) return;
+    const int t = pos & (c.page - 1);
+    KeyPiece<F> k;
+    k.load(c, kv_record(c, page, h), t, d, j);
+    Box box;
+    box.add<F>(k, level);
+    box.store<F == IVFTQ_KV_BF16>(digests + (page * c.heads + h) * 2 * d + j, d, t > 0);
+}
+
+// Several: the (page, head) pairs of all sequences, one after the other, are dealt to the wavefronts in equal consecutive shares.  A
+// wavefront's lanes are 64 / (D / 8) tokens of D / 8 pieces of eight coordinates.
+template <int F, int D>
+__global__ __launch_bounds__(256) void k_kv_digest(KvView c, uint16_t* digests) {
+    constexpr int kPieces = D / 8, kTokens = 64 / kPieces, kAhead = 4;
+    __shared__ float level[16];
+    if constexpr (F == IVFTQ_KV_CODE4) level_table(c, level);
+    const int lane = threadIdx.x & 63, token = lane / kPieces, j = lane % kPieces * 8;
+    int64_t total = 0;
+    for (int b0 = 0; b0 < c.batch; b0 += 64) {
+        int v = new_pages(c, b0 + lane).count;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+        total += v;
+    }
+    const int64_t items = kv_uniform(total) * c.heads, waves = (int64_t)gridDim.x * 4, share = (items + waves - 1) / waves;
+    const int64_t begin = ((int64_t)blockIdx.x * 4 + kv_wave()) * share, end = begin + share < items ? begin + share : items;
+    int64_t base = 0;                                     // pages before the sequences of this round
+    for (int b0 = 0; b0 < c.batch && base * c.heads < end; b0 += 64) {
+        const int mine = new_pages(c, b0 + lane).count;
+        int64_t incl = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int64_t u = __shfl_up(incl, o); if (lane >= o) incl += u; }
+        for (uint64_t left = __ballot(mine && (base + incl) * c.heads > begin && (base + incl - mine) * c.heads < end); left; left &= left - 1) {
+            const int l = __builtin_ctzll(left), b = b0 + l;
+            const int64_t before = kv_uniform(base + (int64_t)__shfl(incl - mine, l));
+            const NewPages p = new_pages(c, b);
+            const int64_t to = before + p.count < (end + c.heads - 1) / c.heads ? (before + p.count) * c.heads : end;
+            for (int64_t x = begin > before * c.heads ? begin : before * c.heads; x < to && x < end; ++x) {
+                const int col = p.col0 + (int)(x / c.heads - before), h = (int)(x % c.heads), t_first = col << c.page_log2;
+                const int64_t page = kv_page(c, b, t_first);
+                if (page < 0) continue;
+                const int from = p.lo > t_first ? p.lo - t_first : 0, past = p.end - t_first < c.page ? p.end - t_first : c.page;
+                const char* rec = kv_record(c, page, h);
+                Box box;
+                if (token < kTokens) {
+                    for (int t = from + token; t < past; t += kTokens * kAhead) {
+                        KeyPiece<F> k[kAhead];
+#pragma unroll
+                        for (int u = 0; u < kAhead; ++u) k[u].load(c, rec, t + u * kTokens < past ? t + u * kTokens : t, D, j);       // past the end: once more
+#pragma unroll
+                        for (int u = 0; u < kAhead; ++u) box.add<F>(k[u], level);
+                    }
+                }
+                // over the lanes of one piece
+                if constexpr ((kTokens & (kTokens - 1)) == 0 && kTokens * kPieces == 64) {
+#pragma unroll
+                    for (int o = kPieces; o < 64; o <<= 1)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            box.low[e] = fminf(box.low[e], __shfl_xor(box.low[e], o));
+                            box.high[e] = fmaxf(box.high[e], __shfl_xor(box.high[e], o));
+                        }
+                } else {
+                    const Box own = box;
+#pragma unroll
+                    for (int u = 1; u < kTokens; ++u)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            box.low[e] = fminf(box.low[e], __shfl(own.low[e], (lane + u * kPieces) & 63));
+                            box.high[e] = fmaxf(box.high[e], __shfl(own.high[e], (lane + u * kPieces) & 63));
+                        }
+                }
+                if (lane < kPieces) box.store<F == IVFTQ_KV_BF16>(digests + (page * c.heads + h) * 2 * D + j, D, from > 0);
+            }
+        }
+        base += kv_uniform((int64_t)__shfl(incl, 63));
+    }
+}
+
+template <int F>
+hipError_t digest(const KvView& c, uint16_t* digests, int d, hipStream_t st) {
+    if (!c.starts) {
+        k_kv_digest_row<F><<<kv_grid(((int64_t)c.rows * c.heads * (d / 8) + 255) / 256, 256), 256, 0, st>>>(c, digests, d);
+        return hipGetLastError();
+    }
+    // no more pages than the table has, a wavefront each where the chip holds so many
+    const int64_t most = (int64_t)c.batch * c.columns * c.heads;
+    const unsigned wgs = (unsigned)(most < 4 * 2048 ? (most + 3) / 4 : 2048);
+    switch (d) {
+        case 64: k_kv_digest<F, 64><<<wgs, 256, 0, st>>>(c, digests); break;
+        case 96: k_kv_digest<F, 96><<<wgs, 256, 0, st>>>(c, digests); break;
+        case 128: k_kv_digest<F, 128><<<wgs, 256, 0, st>>>(c, digests); break;
+        case 192: k_kv_digest<F, 192><<<wgs, 256, 0, st>>>(c, digests); break;
+        default: k_kv_digest<F, 256><<<wgs, 256, 0, st>>>(c, digests); break;
+    }
+    return hipGetLastError();
+}
+
+// ---- pages of the highest scores --------------------------------------------------------------------------------------
+
+// Scores as numbers whose order is theirs; 0: never chosen, the largest: always.
+__device__ __forceinline__ uint32_t order_of(float v) {
+    if (!(v > -INFINITY)) return 0;
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v + 0.f);                 // no negative zero
+    return bits >> 31 ? ~bits : bits | 0x80000000u;
+}
+
+// Sum of v over the threads before this one, and over all of the 256.
+__device__ __forceinline__ uint32_t before256(uint32_t v, uint32_t* sums, uint32_t& all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t incl = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const uint32_t u = __shfl_up(incl, o); if (lane >= o) incl += u; }
+    __syncthreads();
+    if (lane == 63) sums[wave] = incl;
+    __syncthreads();
+    uint32_t before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) { before += w < wave ? sums[w] : 0; all += sums[w]; }
+    return before + incl - v;
+}
+
+// A workgroup a row and head: the order of the count-th highest score is found eight bits at a time by counting, then what is above it, and
+// of its equals the lowest columns, is written in order.
+__global__ __launch_bounds__(256) void k_kv_select(KvSelect s) {
+    __shared__ uint32_t counts[256], sums[4], found[2];
+    const KvView& c = s.c;
+    const int64_t unit = kv_workgroup();
+    if (unit >= (int64_t)c.rows * c.heads) return;
+    const int row = (int)(unit / c.heads);
+    int32_t* out = s.chosen + unit * s.count;
+    const int pos = kv_position(c, row);
+    const int reach = pos < 0 ? 0 : (pos >> c.page_log2) + 1, n = reach < c.columns ? reach : c.columns;
+    const float* scores = s.scores + unit * c.columns;
+    auto key = [&](int col) { return col < s.first || col >= n - s.last ? 0xffffffffu : order_of(scores[col]); };
+    uint32_t prefix = 0, want = (uint32_t)s.count;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        counts[threadIdx.x] = 0;
+        if (threadIdx.x == 0) found[0] = 0xffffffffu;
+        __syncthreads();
+        for (int col = threadIdx.x; col < n; col += 256) {
+            const uint32_t k = key(col);
+            if (k && (shift == 24 || k >> (shift + 8) == prefix)) atomicAdd(&counts[k >> shift & 255], 1u);
+        }
+        __syncthreads();
+        uint32_t all;
+        const uint32_t mine = counts[255 - threadIdx.x], above = before256(mine, sums, all);
+        if (above < want && above + mine >= want) { found[0] = 255 - threadIdx.x; found[1] = want - above; }
+        __syncthreads();
+        if (found[0] == 0xffffffffu) { prefix = 0; want = 0; break; }            // fewer than count: all of them
+        prefix = prefix << 8 | found[0];
+        want = found[1];
+        __syncthreads();
+    }
+    // above `prefix` all, of its equals the first `want`
+    uint32_t above = 0, equal = 0;
+    for (int col0 = 0; col0 < n; col0 += 256) {
+        const int col = col0 + threadIdx.x;
+        const uint32_t k = col < n ? key(col) : 0;
+        const uint32_t flags = k > prefix ? 1 : (k && k == prefix ? 1u << 16 : 0);
+        uint32_t all;
+        const uint32_t before = before256(flags, sums, all);
+        const uint32_t a = above + (before & 0xffff), e = equal + (before >> 16);
+        if (flags == 1 || (flags && e < want)) out[a + (e < want ? e : want)] = col;
+        above += all & 0xffff;
+        equal += all >> 16;
+    }
+    for (int i = (int)(above + (equal < want ? equal : want)) + threadIdx.x; i < s.count; i += 256) out[i] = -1;
+}
+
+}  // namespace
+
+hipError_t launch_kv_digest(const KvView& c, void* digests, int d, int format, hipStream_t st) {
+    uint16_t* p = static_cast<uint16_t*>(digests);
+    switch (format) {
+        case IVFTQ_KV_F16: return digest<IVFTQ_KV_F16>(c, p, d, st);
+        case IVFTQ_KV_BF16: return digest<IVFTQ_KV_BF16>(c, p, d, st);
+        default: return digest<IVFTQ_KV_CODE4>(c, p, d, st);
+    }
+}
+hipError_t launch_kv_select(const KvSelect& s, hipStream_t st) {
+    k_kv_select<<<kv_grid((int64_t)s.c.rows * s.c.heads, 256), 256, 0, st>>>(s);
+    return hipGetLastError();
+}
+
+}  // namespace ivftq

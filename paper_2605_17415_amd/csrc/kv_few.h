@@ -143,6 +143,7 @@ struct FewPlace {
     int t0;
     const char *r0, *r1;
     bool there0, there1;
+    int apart;                        // chosen pages of 16: tokens between the tile's halves
 };
 struct FewTable {                     // one pair's way into the cache
     const int32_t* row;
@@ -263,8 +264,8 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
 }
 
 // A tile into the running maximum m, sum l (of this lane's tokens) and sums o (transposed: o[blk][r] = coordinate
-// 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).
-template <int F, int D, bool LOW>
+// 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).  APART: the tile's halves need not follow one another.
+template <int F, int D, bool LOW, bool APART = false>
 __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, const FewQuery<F, D, LOW>& q, const FewPlace& at, FewTile<F, D>& x, float& m,
                                          float& l, floatx4 (&o)[D / 16]) {
     const KvView& c = a.c;
@@ -293,11 +294,11 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
         for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3];
     }
     // every token of the tile visible to every row?
-    const bool full = at.there0 && at.there1 && t0 + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks);
+    const bool full = at.there0 && at.there1 && t0 + (APART ? at.apart : 0) + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks);
     uint32_t shown = 0xff;                  // of the lane's eight tokens: those that any row sees
     if (!full) {
         // bits and selects only: what the compiler makes of conditions here was found to be wrong
-        const int tb = t0 + 8 * g;
+        const int tb = t0 + 8 * g + (APART && g >> 1 ? at.apart : 0);
         const uint32_t there = (g >> 1 ? at.there1 : at.there0) ? 0xffu : 0u, sinks = few_below(a.sinks - tb);
         shown = few_below(s.end - tb) & (~few_below(s.low - tb) | sinks) & there;
         const uint32_t mine = few_below(q.pos + 1 - tb) & (~few_below(q.begin - tb) | sinks) & shown;

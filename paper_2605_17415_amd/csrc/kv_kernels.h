@@ -47,14 +47,24 @@ struct KvAttend {
     char* work;
 };
 
+// Scores of a row's pages, and the pages that it is given.
+struct KvSelect {
+    const float* scores;         // [rows][heads][c.columns]
+    int32_t* chosen;             // [rows][heads][count]
+    KvView c;                    // of it: lengths, starts, batch, columns, page, heads, rows
+    int32_t count, first, last;
+};
+
 hipError_t launch_kv_append(const KvView& c, const KvRows& k, const KvRows& v, int d, int format, hipStream_t st);
 hipError_t launch_kv_read(const KvView& c, const KvRows& k, const KvRows& v, int d, int format, hipStream_t st);
 hipError_t launch_kv_reserve(const ivftq_kv_pages& s, const int32_t* counts, int32_t* granted, int32_t* scratch, hipStream_t st);
-hipError_t launch_kv_fork(const ivftq_kv_pages& s, const ivftq_kv_pools& p, const int32_t* parents, const int32_t* children, int n, int32_t* done,
+hipError_t launch_kv_digest(const KvView& c, void* digests, int d, int format, hipStream_t st);
+hipError_t launch_kv_select(const KvSelect& s, hipStream_t st);
+hipError_t launch_kv_fork(const ivftq_kv_pages& s, const ivftq_kv_pools* p, int groups, const int32_t* parents, const int32_t* children, int n, int32_t* done,
                           int32_t* scratch, hipStream_t st);
 hipError_t launch_kv_free(const ivftq_kv_pages& s, const int32_t* rows, int n, hipStream_t st);
 hipError_t launch_kv_trim(const ivftq_kv_pages& s, int window, int sinks, hipStream_t st);
-hipError_t launch_kv_compact(const ivftq_kv_pages& s, const ivftq_kv_pools& p, int32_t* used, int32_t* scratch, hipStream_t st);
+hipError_t launch_kv_compact(const ivftq_kv_pages& s, const ivftq_kv_pools* p, int groups, int32_t* used, int32_t* scratch, hipStream_t st);
 hipError_t launch_kv_copy(const ivftq_kv_pools& p, const int32_t* src, const int32_t* dst, const int32_t* count, int n, hipStream_t st);
 
 inline int64_t kv_head_bytes(int format, int page, int d) {
@@ -108,6 +118,28 @@ __device__ __forceinline__ void kv_new_rows(const KvView& c, int b, int& first, 
     first = s < 0 ? 0 : (s < c.rows ? s : c.rows);
     const int end = e < first ? first : (e < c.rows ? e : c.rows);
     count = end - first;
+}
+
+// The sequence of a new row, -1 for rows of none; its position (of none: -1).  Looked for between the starts.
+__device__ __forceinline__ int kv_sequence(const KvView& c, int64_t row, int& first, int& count) {
+    int lo = 0, hi = c.batch;                       // first sequence that begins after the row, minus one
+    first = count = 0;
+    if (hi <= 0) return -1;
+    if (c.starts) {
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (kv_int(c.starts, mid) <= row) lo = mid; else hi = mid;
+        }
+    } else {
+        lo = row < c.batch ? (int)row : 0;
+    }
+    kv_new_rows(c, lo, first, count);
+    return row >= first && row < (int64_t)first + count ? lo : -1;
+}
+__device__ __forceinline__ int kv_position(const KvView& c, int64_t row) {
+    int first, count;
+    const int b = kv_sequence(c, row, first, count);
+    return b < 0 ? -1 : kv_length(c, b) - count + (int)(row - first);
 }
 
 // Whether sequence b's reservation was refused: its length does not count the new rows.

@@ -269,12 +269,13 @@ hipError_t launch_kv_reserve(const ivftq_kv_pages& s, const int32_t* counts, int
     k_kv_reserve<<<1, kThreads, 0, st>>>(s, counts, granted, scratch);
     return hipGetLastError();
 }
-hipError_t launch_kv_fork(const ivftq_kv_pages& s, const ivftq_kv_pools& p, const int32_t* parents, const int32_t* children, int n, int32_t* done,
+hipError_t launch_kv_fork(const ivftq_kv_pages& s, const ivftq_kv_pools* p, int groups, const int32_t* parents, const int32_t* children, int n, int32_t* done,
                           int32_t* scratch, hipStream_t st) {
     if (!n) return hipSuccess;
     k_kv_fork<<<1, kThreads, 0, st>>>(s, parents, children, n, done, scratch);
-    const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_kv_copy(p, scratch + s.pages, scratch + s.pages + n, nullptr, n, st);
+    hipError_t e = hipGetLastError();
+    for (int i = 0; i < groups && e == hipSuccess; ++i) e = launch_kv_copy(p[i], scratch + s.pages, scratch + s.pages + n, nullptr, n, st);
+    return e;
 }
 hipError_t launch_kv_free(const ivftq_kv_pages& s, const int32_t* rows, int n, hipStream_t st) {
     if (!n) return hipSuccess;
@@ -286,7 +287,7 @@ hipError_t launch_kv_trim(const ivftq_kv_pages& s, int window, int sinks, hipStr
     k_kv_trim<<<(unsigned)s.rows, 256, 0, st>>>(s, window, sinks);
     return hipGetLastError();
 }
-hipError_t launch_kv_compact(const ivftq_kv_pages& s, const ivftq_kv_pools& p, int32_t* used, int32_t* scratch, hipStream_t st) {
+hipError_t launch_kv_compact(const ivftq_kv_pages& s, const ivftq_kv_pools* p, int groups, int32_t* used, int32_t* scratch, hipStream_t st) {
     k_kv_compact<<<1, kThreads, 0, st>>>(s, used, scratch);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && s.rows) {
@@ -294,7 +295,8 @@ hipError_t launch_kv_compact(const ivftq_kv_pages& s, const ivftq_kv_pools& p, i
         e = hipGetLastError();
     }
     const int most = (int)(s.pages / 2);              // every move has a hole
-    return e != hipSuccess ? e : launch_kv_copy(p, scratch + s.pages, scratch + 2 * s.pages, scratch + 3 * s.pages, most, st);
+    for (int i = 0; i < groups && e == hipSuccess; ++i) e = launch_kv_copy(p[i], scratch + s.pages, scratch + 2 * s.pages, scratch + 3 * s.pages, most, st);
+    return e;
 }
 
 }  // namespace ivftq

@@ -1,0 +1,435 @@
+// Scores of pages by their digests, and attention over chosen pages.
+//
+// Scores are products of queries and digests (v_mfma 16x16x32: 16 pages x 16 new rows), the negative coordinates of a query with the lowest
+// values and the others with the highest; the group's heads add up in the accumulators.  Codes: rotated unit queries in two float16 parts.
+//
+// Attention: every new row has pages of its own for each key-value head, so a (row, head) pair is what kv_few.h calls a sequence: a
+// workgroup's wavefronts take every fourth tile of 32 tokens of the chosen pages, the query rows are the group's heads.  Where
+// the pairs are few several workgroups share a pair's tiles, and a second kernel joins their parts.
+#pragma once
+#include "kv_many.h"
+
+namespace ivftq {
+
+struct ScoreArgs {
+    KvAttend a;                       // c, q, group, max_new
+    const uint16_t* digests;
+    float* scores;
+    const uint16_t* z;                // codes: rotated unit queries, two float16 parts, eights in the order of kv_levels8
+    const float* zn;                  // codes: the queries' norms
+    int32_t row_tiles;
+};
+
+// The coordinates of w that are negative; the others are w & ~mask.
+__device__ __forceinline__ uintx4 kv_negative(uintx4 w) {
+    uintx4 m;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        typedef int16_t two __attribute__((ext_vector_type(2)));
+        const uint32_t u = w[e];
+        m[e] = __builtin_bit_cast(uint32_t, (two)(__builtin_bit_cast(two, u) >> (two)(15)));
+    }
+    return m;
+}
+// Eight values from the order of kv_levels8 into their own.
+__device__ __forceinline__ uintx4 kv_in_order(uintx4 w) {
+    return uintx4{__builtin_amdgcn_perm(w[2], w[0], 0x05040100u), __builtin_amdgcn_perm(w[2], w[0], 0x07060302u),
+                  __builtin_amdgcn_perm(w[3], w[1], 0x05040100u), __builtin_amdgcn_perm(w[3], w[1], 0x07060302u)};
+}
+
+template <int F, int D>
+__global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
+    constexpr bool codes = F == IVFTQ_KV_CODE4;
+    const KvAttend& a = f.a;
+    const KvView& c = a.c;
+    const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const uint32_t wg = kv_workgroup();
+    const int h = (int)(wg % (uint32_t)c.heads), rt = (int)(wg / (uint32_t)c.heads % (uint32_t)f.row_tiles), b = (int)(wg / (uint32_t)c.heads / (uint32_t)f.row_tiles);
+    if (b >= c.batch) return;
+    int first, count;
+    kv_new_rows(c, b, first, count);
+    const int base = kv_length(c, b) - count;
+    if (count > a.max_new) count = a.max_new;
+    if (16 * rt >= count) return;
+    const int col0 = ((int)blockIdx.y * 4 + wave) * 16;
+    if (col0 >= c.columns) return;
+    const int rows = count - 16 * rt < 16 ? count - 16 * rt : 16, row = first + 16 * rt + (n < rows ? n : 0);
+    // page of column col0 + n
+    const int32_t id = col0 + n < c.columns ? c.table[(int64_t)b * c.table_stride + col0 + n] : -1;
+    const bool there = (uint32_t)id < (uint32_t)c.pages;
+    const uint32_t known = (uint32_t)__ballot(there) & 0xffffu;
+    floatx4 total = {0.f, 0.f, 0.f, 0.f};
+    if (col0 <= (base + 16 * rt + rows - 1) >> c.page_log2) {           // any of the rows reaches these pages
+        const uint16_t* box = f.digests + ((int64_t)(there ? id : 0) * c.heads + h) * (2 * D) + 8 * g;
+        uintx4 low[D / 32], high[D / 32];
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            low[k] = *reinterpret_cast<const uintx4*>(box + 32 * k);
+            high[k] = *reinterpret_cast<const uintx4*>(box + D + 32 * k);
+        }
+        for (int i = 0; i < a.group; ++i) {
+            const int head = h * a.group + i;
+            if constexpr (codes) {
+                const int64_t at = (int64_t)row * a.q.heads + head, all = (int64_t)a.q.rows * a.q.heads;
+                floatx4 part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) {
+                    const uintx4 w = kv_in_order(*reinterpret_cast<const uintx4*>(f.z + at * D + 32 * k + 8 * g)), m = kv_negative(w);
+                    const uintx4 v = kv_in_order(*reinterpret_cast<const uintx4*>(f.z + (all + at) * D + 32 * k + 8 * g));
+                    part = kv_mfma16<F>(low[k], w & m, part);
+                    part = kv_mfma16<F>(high[k], w & ~m, part);
+                    part = kv_mfma16<F>(low[k], v & m, part);
+                    part = kv_mfma16<F>(high[k], v & ~m, part);
+                }
+                total += part * (f.zn[at] * (1.f / kSplitScale));
+            } else {
+                const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) {
+                    const uintx4 w = *reinterpret_cast<const uintx4*>(q + 32 * k), m = kv_negative(w);
+                    total = kv_mfma16<F>(low[k], w & m, total);
+                    total = kv_mfma16<F>(high[k], w & ~m, total);
+                }
+            }
+        }
+    }
+    if (n >= rows) return;
+    const int reach = (base + 16 * rt + n) >> c.page_log2, col = col0 + 4 * g;         // a position under zero reaches column -1
+    float* out = f.scores + ((int64_t)row * c.heads + h) * c.columns + col;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (col + r < c.columns) out[r] = col + r <= reach && (known >> (4 * g + r) & 1) ? total[r] : -INFINITY;
+}
+
+// ---- attention ----------------------------------------------------------------------------------------------------
+
+constexpr int kMostPicks = 4096;      // pages of a row and head
+
+struct PickArgs {
+    FewArgs f;                        // its KvAttend with max_new = 1: a pair has one new row
+    const int32_t* chosen;            // [rows][heads][count]
+    int32_t count, splits, max_new;   // splits: workgroups that share a pair's tiles
+};
+
+// A pair's pages: columns and page numbers in LDS, ascending, without what does not count.
+struct Picked { int n, tiles; };
+__device__ __forceinline__ Picked pick_list(const PickArgs& p, int b, int64_t pair, int pos, int2* list) {
+    const KvView& c = p.f.a.c;
+    __shared__ int many;
+    if (kv_wave() == 0) {
+        const int lane = threadIdx.x;
+        int top = -1, n = 0;
+        for (int i0 = 0; i0 < p.count; i0 += 64) {
+            const int col = i0 + lane < p.count ? p.chosen[pair * p.count + i0 + lane] : -1;
+            int most = col;                          // of the entries up to this one
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(most, o); if (lane >= o) most = most > u ? most : u; }
+            const int prev = __shfl_up(most, 1), before = lane && prev > top ? prev : top;
+            bool in = col > before && col < c.columns && (int64_t)col << c.page_log2 <= pos;
+            const int32_t id = in ? c.table[(int64_t)b * c.table_stride + col] : -1;
+            in = (uint32_t)id < (uint32_t)c.pages;
+            const uint64_t all = __ballot(in);
+            if (in) list[n + __popcll(all & ((1ull << lane) - 1))] = make_int2(col, id);
+            n += __popcll(all);
+            const int last = __shfl(most, 63);
+            top = top > last ? top : last;
+        }
+        if (lane == 0) many = n;
+    }
+    __syncthreads();
+    Picked x;
+    x.n = kv_uniform(many);
+    if (c.page < kFewTile) {
+        x.tiles = (x.n + 1) / 2;
+    } else {                                         // of the last page, the only one that may end behind the row, what it reaches
+        const int each = c.page / kFewTile;
+        const int left = x.n ? (pos - (kv_uniform(list[x.n - 1].x) << c.page_log2)) / kFewTile + 1 : 0;
+        x.tiles = x.n ? (x.n - 1) * each + (left < each ? left : each) : 0;
+    }
+    return x;
+}
+
+struct PickTable {
+    const int2* list;
+    const char* head;
+    int n, each_log2;                                // pages of 32 and more: log2 of a page's tiles
+    __device__ __forceinline__ FewPlace operator()(const KvView& c, const FewSeq&, int i) const {
+        FewPlace p;
+        p.apart = 0;
+        p.there0 = p.there1 = true;
+        if (c.page < kFewTile) {
+            const int2 x = list[2 * i], y = list[2 * i + 1 < n ? 2 * i + 1 : 2 * i];
+            const int xc = kv_uniform(x.x), yc = kv_uniform(y.x);
+            p.t0 = xc * 16;
+            p.there1 = 2 * i + 1 < n;
+            p.apart = p.there1 ? (yc - xc - 1) * 16 : 0;
+            p.r0 = head + (int64_t)kv_uniform(x.y) * c.page_bytes;
+            p.r1 = head + (int64_t)kv_uniform(y.y) * c.page_bytes;
+        } else {
+            const int2 x = list[i >> each_log2];
+            p.t0 = (kv_uniform(x.x) << c.page_log2) + (i & ((1 << each_log2) - 1)) * kFewTile;
+            p.r0 = p.r1 = head + (int64_t)kv_uniform(x.y) * c.page_bytes;
+        }
+        return p;
+    }
+};
+
+// One wavefront's tiles [from, to) in steps of four, as few_walk.
+template <int F, int D, bool LOW>
+__device__ __forceinline__ void pick_walk(const FewArgs& f, const FewSeq& s, const PickTable& table, int h, int col0, int from, int to, float& m, float& l,
+                                          floatx4 (&o)[D / 16]) {
+    const KvView& c = f.a.c;
+    if (from >= to) return;
+    FewQuery<F, D, LOW> q;
+    FewPlace at = table(c, s, from);
+    few_query<F, D, LOW>(f, s, h, col0, q);
+    const FewLane<F, D> lane(c);
+    if constexpr (F == IVFTQ_KV_CODE4) {
+        FewTile<F, D> x, y;
+        few_load<F, D>(c, at, lane, x);
+        int i = from;
+        auto step = [&](FewTile<F, D>& now, FewTile<F, D>& then) __attribute__((always_inline)) {      // past the end: a tile that is there, read and not used
+            const FewPlace next = table(c, s, i + 4 < to ? i + 4 : i);
+            few_load<F, D>(c, next, lane, then);
+            few_step<F, D, LOW, true>(f.a, s, q, at, now, m, l, o);
+            at = next;
+            i += 4;
+        };
+        while (true) {
+            step(x, y);
+            if (i >= to) break;
+            step(y, x);
+            if (i >= to) break;
+        }
+    } else {
+        for (int i = from; i < to; i += 4) {
+            FewTile<F, D> x;
+            few_load<F, D>(c, at, lane, x);
+            const FewPlace next = table(c, s, i + 4 < to ? i + 4 : i);
+            few_step<F, D, LOW, true>(f.a, s, q, at, x, m, l, o);
+            at = next;
+        }
+    }
+}
+
+template <int F, int D, bool LOW>
+__global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_picked(PickArgs p) {
+    constexpr int kPass = D > 128 ? D / 2 : D;                 // coordinates that pass through LDS at a time
+    __shared__ float ml[4][16][2];
+    extern __shared__ int2 list[];                             // the pages; when they have been walked, the wavefronts' sums
+    float(*sum)[16][kPass + 1] = reinterpret_cast<float(*)[16][kPass + 1]>(list);
+    const FewArgs& f = p.f;
+    const KvAttend& a = f.a;
+    const KvView& c = a.c;
+    const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, col0 = blockIdx.y * 16;
+    const uint32_t wg = kv_workgroup();
+    const int h = (int)(wg % (uint32_t)c.heads), row = (int)(wg / (uint32_t)c.heads % (uint32_t)c.rows), share = (int)(wg / (uint32_t)c.heads / (uint32_t)c.rows);
+    if (share >= p.splits) return;
+    int first, count;
+    const int b = kv_sequence(c, row, first, count);
+    if (b < 0 || row - first >= p.max_new) return;
+    const int pos = kv_length(c, b) - count + row - first;
+    const int64_t pair = (int64_t)row * c.heads + h;
+    const Picked picked = pick_list(p, b, pair, pos, list);
+    FewSeq s{};
+    s.first = row;
+    s.count = 1;
+    s.base = pos;
+    s.end = pos + 1 > 0 ? pos + 1 : 0;
+    s.beyond = -1;
+    int from = 0, to = picked.tiles;
+    if (p.splits > 1) {
+        const int each = ((picked.tiles + p.splits - 1) / p.splits + 3) & ~3;
+        from = share * each;
+        to = from + each < to ? from + each : to;
+    }
+    float m = -INFINITY, l = 0.f;
+    floatx4 o[D / 16];
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) o[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const PickTable table{list, c.pool + (int64_t)h * c.head_bytes, picked.n, c.page_log2 - 5};
+    pick_walk<F, D, LOW>(f, s, table, h, col0, from + wave, to, m, l, o);
+    l = kv_sum4(l);
+    if (g == 0) { ml[wave][n][0] = m; ml[wave][n][1] = l; }
+    __syncthreads();
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][n][0]);
+    const float turn = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+    for (int pass = 0; pass < D / kPass; ++pass) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int j = few_coord<F>(D, k, g, r) - pass * kPass;
+                if (j >= 0 && j < kPass) sum[wave][n][j] = o[k][r] * turn;
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * (kPass / 2); i += 256) {
+            const int q = i / (kPass / 2), j = i % (kPass / 2) * 2, col = col0 + q;
+            if (col >= a.group) break;
+            float tm = -INFINITY, tl = 0.f, u = 0.f, v = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) tm = fmaxf(tm, ml[w][q][0]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                tl += ml[w][q][0] == -INFINITY ? ml[w][q][1] * 0.f : ml[w][q][1] * __builtin_amdgcn_exp2f(ml[w][q][0] - tm);
+                u += sum[w][q][j];
+                v += sum[w][q][j + 1];
+            }
+            const int head = h * a.group + col, jj = pass * kPass + j;
+            if (p.splits == 1) {
+                const float inv = tm == -INFINITY && tl == 0.f ? 0.f : 1.f / tl;
+                if (F == IVFTQ_KV_CODE4) {
+                    *reinterpret_cast<float2*>(f.whole + ((int64_t)row * a.q.heads + head) * D + jj) = make_float2(u * inv, v * inv);
+                } else {
+                    uint16_t* to16 = reinterpret_cast<uint16_t*>(a.out.data) + row * a.out.row_stride + head * a.out.head_stride + jj;
+                    *reinterpret_cast<uint32_t*>(to16) = kv_pack2<F == IVFTQ_KV_BF16>(u * inv, v * inv);
+                }
+                if (a.lse && jj == 0) a.lse[(int64_t)row * a.q.heads + head] = tl > 0.f ? (tm + __builtin_amdgcn_logf(tl)) / kLog2e : (tl == 0.f ? -INFINITY : tl);
+            } else {
+                const int64_t slot = (((int64_t)blockIdx.y * c.rows * c.heads + pair) * p.splits + share) * 16 + q;
+                *reinterpret_cast<float2*>(f.part + slot * D + jj) = make_float2(u, v);
+                if (jj == 0) *reinterpret_cast<float2*>(f.part_ml + slot * 2) = make_float2(tm, tl);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The parts of a pair put together, a workgroup a pair and column tile, a wavefront a row; codes: rotated back, each wavefront a block
+// of 32 coordinates.
+template <int F, int D>
+__global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
+    constexpr int kPart = D / 4;
+    __shared__ __align__(16) float row_sum[F == IVFTQ_KV_CODE4 ? 16 : 1][D + 4];
+    const FewArgs& f = p.f;
+    const KvAttend& a = f.a;
+    const KvView& c = a.c;
+    const int wave = kv_wave(), lane = threadIdx.x & 63, col0 = blockIdx.y * 16;
+    const uint32_t wg = kv_workgroup();
+    const int h = (int)(wg % (uint32_t)c.heads), row = (int)(wg / (uint32_t)c.heads);
+    if (row >= c.rows) return;
+    int first, count;
+    if (kv_sequence(c, row, first, count) < 0 || row - first >= p.max_new) return;
+    for (int q = wave; q < 16 && col0 + q < a.group; q += 8) {
+        const int head = h * a.group + col0 + q;
+        const int64_t slot0 = (((int64_t)blockIdx.y * c.rows * c.heads + (int64_t)row * c.heads + h) * p.splits) * 16 + q;
+        // a lane a part's maximum and sum (at most 64 parts)
+        float2 u = make_float2(-INFINITY, 0.f);
+        if (lane < p.splits) u = *reinterpret_cast<const float2*>(f.part_ml + (slot0 + lane * 16) * 2);
+        float top = u.x;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+        const float turn = u.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u.x - top);
+        float l = u.x == -INFINITY ? u.y * 0.f : u.y * turn;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int j = lane < kPart ? lane * 4 : 0;
+#pragma unroll 4
+        for (int w = 0; w < p.splits; ++w) {
+            const float t = __shfl(turn, w);
+            const float4 x = *reinterpret_cast<const float4*>(f.part + (slot0 + w * 16) * D + j);
+            acc.x += x.x * t; acc.y += x.y * t; acc.z += x.z * t; acc.w += x.w * t;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+        if (a.lse && lane == 0) a.lse[(int64_t)row * a.q.heads + head] = l > 0.f ? (top + __builtin_amdgcn_logf(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
+        if (lane >= kPart) continue;
+        if constexpr (F == IVFTQ_KV_CODE4) {
+            *reinterpret_cast<float4*>(&row_sum[q][j]) = acc;
+        } else {
+            constexpr bool bf = F == IVFTQ_KV_BF16;
+            uint16_t* to16 = reinterpret_cast<uint16_t*>(a.out.data) + row * a.out.row_stride + head * a.out.head_stride + j;
+            *reinterpret_cast<uint2*>(to16) = make_uint2(kv_pack2<bf>(acc.x, acc.y), kv_pack2<bf>(acc.z, acc.w));
+        }
+    }
+    if constexpr (F == IVFTQ_KV_CODE4) {
+        __syncthreads();
+        if (wave >= D / 32) return;
+        const int n = lane & 15, g = lane >> 4;
+        const bool in = col0 + n < a.group;
+        float x[D / 32][8], y[8];
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f;
+        const float norm = kv_unit_row<D>(x) * c.level_unit;
+        KvTurn<D, true>(c.rotation, wave)(x, y);
+        if (in) kv_store_turned(a.out, row, h * a.group + col0 + n, wave, y, norm);
+    }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+
+// Sizes of the workspaces' parts, as the launches and the caller's questions see them.
+struct PickWork {
+    int64_t z, zn, whole, part, ml, bytes;
+    int32_t col_tiles, splits;
+};
+PickWork pick_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int page, int columns, int count);
+int64_t score_work(int format, int d, int64_t all, int64_t* zn);
+
+// 16-row tiles that a workgroup rotates, and workgroups (as kv_attend_launch).
+template <int D>
+void rotate_queries(const KvAttend& a, uint16_t* z, float* zn, hipStream_t st) {
+    const int64_t all = (int64_t)a.q.rows * a.q.heads, fill = all / (16 * 768);
+    const int tiles = fill < 1 ? 1 : (fill < kTurnTiles ? (int)fill : kTurnTiles);
+    k_kv_rotate_queries<D><<<(unsigned)((all + 16 * tiles - 1) / (16 * tiles)), D * 2, 0, st>>>(a.q, a.c.rotation, z, zn, tiles);
+}
+
+template <int F, int D>
+hipError_t kv_score_launch(const KvAttend& a, const void* digests, float* scores, hipStream_t st) {
+    int64_t zn;
+    score_work(F, D, (int64_t)a.q.rows * a.q.heads, &zn);
+    ScoreArgs f{a, static_cast<const uint16_t*>(digests), scores, reinterpret_cast<const uint16_t*>(a.work), reinterpret_cast<const float*>(a.work + zn), (a.max_new + 15) / 16};
+    if constexpr (F == IVFTQ_KV_CODE4) rotate_queries<D>(a, reinterpret_cast<uint16_t*>(a.work), reinterpret_cast<float*>(a.work + zn), st);
+    k_kv_score<F, D><<<kv_grid((int64_t)a.c.batch * a.c.heads * f.row_tiles, 256, (unsigned)((a.c.columns + 63) / 64)), 256, 0, st>>>(f);
+    return hipGetLastError();
+}
+template <int D>
+hipError_t kv_score_d(const KvAttend& a, const void* digests, float* scores, int format, hipStream_t st) {
+    switch (format) {
+        case IVFTQ_KV_F16: return kv_score_launch<IVFTQ_KV_F16, D>(a, digests, scores, st);
+        case IVFTQ_KV_BF16: return kv_score_launch<IVFTQ_KV_BF16, D>(a, digests, scores, st);
+        default: return kv_score_launch<IVFTQ_KV_CODE4, D>(a, digests, scores, st);
+    }
+}
+
+template <int F, int D>
+hipError_t kv_picked_launch(const KvAttend& a, const PickWork& w, const int32_t* chosen, int count, hipStream_t st) {
+    uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
+    float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole);
+    if constexpr (F == IVFTQ_KV_CODE4) rotate_queries<D>(a, z, zn, st);
+    PickArgs p{FewArgs{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), reinterpret_cast<float*>(a.work + w.ml), 0, 0}, chosen, count, w.splits, a.max_new};
+    p.f.a.max_new = 1;
+    const int64_t pairs = (int64_t)a.q.rows * a.c.heads;
+    const dim3 grid = kv_grid(pairs * w.splits, 256, (unsigned)w.col_tiles);
+    // float16 results: the queries' second part matters beside the rounding of the result
+    constexpr bool codes = F == IVFTQ_KV_CODE4;
+    constexpr int sums = 4 * 16 * ((D > 128 ? D / 2 : D) + 1) * 4;
+    const unsigned lds = (unsigned)(count * 8 > sums ? count * 8 : sums);
+    if (codes && a.q.type == IVFTQ_KV_F16) k_kv_picked<F, D, codes><<<grid, 256, lds, st>>>(p);
+    else k_kv_picked<F, D, false><<<grid, 256, lds, st>>>(p);
+    if (w.splits > 1) {
+        k_kv_picked_join<F, D><<<kv_grid(pairs, 512, (unsigned)w.col_tiles), 512, 0, st>>>(p);
+    } else if constexpr (codes) {
+        const ManyArgs f{a, z, zn, whole, nullptr, nullptr, nullptr, 0, 0};
+        const int64_t all = (int64_t)a.q.rows * a.q.heads, fill = all / (16 * 768);
+        const int tiles = fill < 1 ? 1 : (fill < kTurnTiles ? (int)fill : kTurnTiles);
+        k_kv_rotate_back<D, false><<<(unsigned)((all + 16 * tiles - 1) / (16 * tiles)), D * 2, 0, st>>>(f, tiles);
+    }
+    return hipGetLastError();
+}
+template <int D>
+hipError_t kv_picked_d(const KvAttend& a, const PickWork& w, const int32_t* chosen, int count, int format, hipStream_t st) {
+    switch (format) {
+        case IVFTQ_KV_F16: return kv_picked_launch<IVFTQ_KV_F16, D>(a, w, chosen, count, st);
+        case IVFTQ_KV_BF16: return kv_picked_launch<IVFTQ_KV_BF16, D>(a, w, chosen, count, st);
+        default: return kv_picked_launch<IVFTQ_KV_CODE4, D>(a, w, chosen, count, st);
+    }
+}
+
+}  // namespace ivftq

@@ -4,6 +4,8 @@ Like `binding`, this module marshals arguments; every step runs in the library's
     16 bits   float16 / bfloat16 [pages, heads, 2, page, d]   keys [page][d], then values in groups of eight tokens:
               the second block is really [page / 8][d][8]
     codes     uint8 [pages, heads, page * (d + 4)]            see ivftq_kv.h
+and its digests, the lowest and the highest value of a page's key coordinates, by which pages are chosen for attention over a long cache:
+    digests   [pages, heads, 2, d] of the pool's type (codes: float16, of the rotated keys)
 and tensors of several layers have one more dimension in front.
 
 `stream`: a call's kernels, its workspace and what it gives back belong to this stream (None: the current one).  As everywhere in
@@ -68,8 +70,16 @@ _SIGNATURES = {
     "ivftq_kv_attend": (C.c_int, [_P, _P, _P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_float,
                                   _P, C.c_int64, _P]),
     "ivftq_kv_attend_workspace": (C.c_int64, [_P, C.c_int64, C.c_int32, C.c_int32]),
+    "ivftq_kv_digest": (C.c_int, [_P, _P, _P, _P]),
+    "ivftq_kv_score": (C.c_int, [_P, _P, _P, _P, _P, C.c_int32, _P, C.c_int64, _P]),
+    "ivftq_kv_score_workspace": (C.c_int64, [_P, C.c_int64, C.c_int32]),
+    "ivftq_kv_select": (C.c_int, [_P, _P, _P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P]),
+    "ivftq_kv_attend_pages": (C.c_int, [_P, _P, _P, _P, _P, C.c_int32, _P, C.c_int32, C.c_float, _P, C.c_int64, _P]),
+    "ivftq_kv_attend_pages_workspace": (C.c_int64, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32]),
     "ivftq_kv_reserve": (C.c_int, [_P, _P, _P, _P, _P]),
     "ivftq_kv_fork": (C.c_int, [_P, _P, _P, _P, C.c_int32, _P, _P, _P]),
+    "ivftq_kv_fork_pools": (C.c_int, [_P, _P, C.c_int32, _P, _P, C.c_int32, _P, _P, _P]),
+    "ivftq_kv_compact_pools": (C.c_int, [_P, _P, C.c_int32, _P, _P, _P]),
     "ivftq_kv_free": (C.c_int, [_P, _P, C.c_int32, _P]),
     "ivftq_kv_trim": (C.c_int, [_P, C.c_int32, C.c_int32, _P]),
     "ivftq_kv_compact": (C.c_int, [_P, _P, _P, _P, _P]),
@@ -273,6 +283,118 @@ def kv_attend(q, pool, table, lengths, starts=None, max_new=None, window=0, sink
     return out
 
 
+# ---- attention over chosen pages ------------------------------------------------------------------
+
+
+def _digests(digests, pool, d):
+    _on_device(digests, "digests", pool)
+    if digests.requires_grad:
+        _no_gradient(digests, "digests")
+    kind = torch.float16 if pool.dtype == torch.uint8 else pool.dtype
+    if digests.dtype != kind or tuple(digests.shape) != (pool.shape[0], pool.shape[1], 2, d) or not digests.is_contiguous():
+        raise ValueError(f"digests must be a contiguous tensor of pages x heads x 2 x {d} in {kind}, got {tuple(digests.shape)} in {digests.dtype}")
+    return digests.data_ptr()
+
+
+def _floats(t, name, like, shape):
+    _on_device(t, name, like)
+    if t.requires_grad:
+        _no_gradient(t, name)
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {tuple(shape)}, got {tuple(t.shape)} in {t.dtype}")
+    return t.data_ptr()
+
+
+def _most_new(max_new, starts, rows):
+    if starts is None and (max_new is None or max_new > 1):
+        return 1
+    return max(rows, 1) if max_new is None else max_new
+
+
+def _blank(shape, dtype, like, stream):
+    """A tensor that is given back."""
+    return _result(_scratch(shape, dtype, like, stream), stream)
+
+
+def kv_digest(pool, digests, table, lengths, starts=None, rotation=None, levels=None, stream=None, asked=None, granted=None):
+    """Digests of the pages that hold the new rows, after kv_append has written them (and with its starts, asked and granted): a page that
+    begins with a new row gets the digest of its new rows, one that goes on has them added.  With all of a sequence's tokens between
+    its starts its digests are made afresh."""
+    d = digests.shape[-1]
+    where = _digests(digests, pool, d)
+    _run(_library().ivftq_kv_digest, pool, _cache(pool, table, lengths, d, rotation, levels, asked, granted), where, _starts(starts, table, pool), _stream(stream, pool))
+
+
+def kv_score(q, digests, pool, table, lengths, starts=None, max_new=None, rotation=None, levels=None, out=None, stream=None):
+    """Scores of every page for the new rows q [rows, query heads, d]: float32 [rows, heads, columns], for each key-value head the most that
+    the products of its query heads with a key of the page can add up to (-inf: the row sees nothing of it).  max_new and rows past it as
+    in kv_attend."""
+    d = q.shape[-1]
+    cache, rows, where = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d), _stream(stream, pool)
+    box, shape = _digests(digests, pool, d), (q.shape[0], pool.shape[1], table.shape[1])
+    if out is None:
+        out = _blank(shape, torch.float32, q, stream)
+    result, first, max_new = _floats(out, "out", pool, shape), _starts(starts, table, pool), _most_new(max_new, starts, q.shape[0])
+    lib = _library()
+    need = 0
+    if pool.dtype == torch.uint8:
+        need = lib.ivftq_kv_score_workspace(cache, q.shape[0], q.shape[1])
+        if need < 0:
+            _check(1)
+    work = _scratch(need, torch.uint8, q, stream) if need else None
+    _run(lib.ivftq_kv_score, pool, cache, rows, box, result, first, max_new, None if work is None else work.data_ptr(), need, where)
+    return out
+
+
+def kv_select(scores, lengths, page, count, starts=None, first=1, last=1, out=None, stream=None):
+    """The pages of each row and key-value head: int32 [rows, heads, count], of the columns that the row's position reaches the first `first`
+    and the last `last` ones and those of the highest scores (ties: the lowest column; -inf and what is no number: none), ascending, -1
+    behind them."""
+    _on_device(scores, "scores")
+    if scores.dim() != 3:
+        raise ValueError(f"scores must be rows x heads x columns, got {tuple(scores.shape)}")
+    rows, heads, columns = scores.shape
+    data, where = _floats(scores, "scores", scores, scores.shape), _stream(stream, scores)
+    lens, batch = _ints(lengths, "lengths", scores), lengths.shape[0]
+    if out is None:
+        out = _blank((rows, heads, count), torch.int32, scores, stream)
+    _run(_library().ivftq_kv_select, scores, data, lens, None if starts is None else _ints(starts, "starts", scores, batch + 1), rows, batch, heads, columns, page, count,
+         first, last, _columns(out, "out", scores, (rows, heads, count)), where)
+    return out
+
+
+def _columns(t, name, like, shape):
+    _on_device(t, name, like)
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {tuple(shape)}, got {tuple(t.shape)} in {t.dtype}")
+    return t.data_ptr()
+
+
+def kv_attend_pages(q, pool, table, lengths, chosen, starts=None, max_new=None, scale=None, rotation=None, levels=None, out=None, lse=None, stream=None):
+    """kv_attend where a row and key-value head sees, of the tokens up to its own, those of the columns `chosen` [rows, heads, count] (as
+    kv_select gives them: ascending; an entry that is not above those before it, or names no page, is passed over)."""
+    lib = _library()
+    d = q.shape[-1]
+    cache, rows, where = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d), _stream(stream, pool)
+    if chosen.dim() != 3:
+        raise ValueError(f"chosen must be rows x heads x count, got {tuple(chosen.shape)}")
+    count = chosen.shape[2]
+    pages = _columns(chosen, "chosen", pool, (q.shape[0], pool.shape[1], count))
+    if out is None:
+        out = _blank(q.shape, q.dtype, q, stream)
+    elif out.shape != q.shape:
+        raise ValueError(f"out has shape {tuple(out.shape)}, not {tuple(q.shape)}")
+    result, sums = _rows(out, "out", pool, d), None if lse is None else _floats(lse, "lse", pool, q.shape[:2])
+    first, max_new = _starts(starts, table, pool), _most_new(max_new, starts, q.shape[0])
+    need = lib.ivftq_kv_attend_pages_workspace(cache, q.shape[0], q.shape[1], max_new, count)
+    if need < 0:
+        _check(1)
+    work = _scratch(need, torch.uint8, q, stream) if need else None
+    _run(lib.ivftq_kv_attend_pages, pool, cache, rows, result, sums, first, max_new, pages, count, 1 / math.sqrt(d) if scale is None else scale,
+         None if work is None else work.data_ptr(), need, where)
+    return out
+
+
 # ---- pages ---------------------------------------------------------------------------------------
 
 
@@ -290,6 +412,13 @@ def _pools(pools, like):
     return _pack_pools(pools.data_ptr(), pools.stride(0) * size, pools.numel() // (layers * pages) * size, pages, layers)
 
 
+def _groups(pools, like):
+    """(structures of all tensors, their number)"""
+    if isinstance(pools, torch.Tensor):
+        return _pools(pools, like), 1
+    return b"".join(_pools(p, like) for p in pools), len(pools)
+
+
 def kv_reserve(table, lengths, refs, counts, page, stream=None):
     """Pages for counts[r] more tokens in each row, lengths raised; returns what was granted (counts[r], or 0 where there is no
     room: the row stays as it is, and new rows must not be appended to it)."""
@@ -301,10 +430,10 @@ def kv_reserve(table, lengths, refs, counts, page, stream=None):
 
 def kv_fork(pools, table, lengths, refs, parents, children, page, stream=None):
     """Rows `children` become copies of rows `parents`: full pages shared, a last page that is not full copied in every layer
-    of pools [layers, pages, ...].  Returns 1 for each entry that was done."""
-    state, records, n, where = _pages(table, lengths, refs, page), _pools(pools, refs), parents.numel(), _stream(stream, refs)
+    of pools [layers, pages, ...] (several such tensors: a list of them).  Returns 1 for each entry that was done."""
+    state, records, n, where = _pages(table, lengths, refs, page), _groups(pools, refs), parents.numel(), _stream(stream, refs)
     done, scratch = _result(_scratch(n, torch.int32, refs, stream), stream), _scratch(refs.numel() + 2 * n + 2 * table.shape[0], torch.int32, refs, stream)
-    _run(_library().ivftq_kv_fork, refs, state, records, _ints(parents, "parents", refs), _ints(children, "children", refs, n), n, done.data_ptr(),
+    _run(_library().ivftq_kv_fork_pools, refs, state, *records, _ints(parents, "parents", refs), _ints(children, "children", refs, n), n, done.data_ptr(),
          scratch.data_ptr(), where)
     return done
 
@@ -320,10 +449,11 @@ def kv_trim(table, lengths, refs, page, window, sinks=0, stream=None):
 
 
 def kv_compact(pools, table, refs, stream=None):
-    """Pages in use move to the lowest numbers; returns how many there are (device, int32 [1])."""
-    state, records, where = _pages(table, None, refs, 16), _pools(pools, refs), _stream(stream, refs)
+    """Pages in use move to the lowest numbers, in every layer of pools (several such tensors: a list of them); returns how many there
+    are (device, int32 [1])."""
+    state, records, where = _pages(table, None, refs, 16), _groups(pools, refs), _stream(stream, refs)
     used, scratch = _result(_scratch(1, torch.int32, refs, stream), stream), _scratch(3 * refs.numel() + 64, torch.int32, refs, stream)
-    _run(_library().ivftq_kv_compact, refs, state, records, used.data_ptr(), scratch.data_ptr(), where)
+    _run(_library().ivftq_kv_compact_pools, refs, state, *records, used.data_ptr(), scratch.data_ptr(), where)
     return used
 
 
@@ -345,10 +475,13 @@ class KVCache:
     A step of a model: `reserve` room for the new tokens, then for every layer `append` its keys and values and `attend`.  Rows
     without new tokens have none between their `starts`.  A row whose reservation was refused keeps its tokens: `append` leaves it
     out until a `reserve` grants it what it asks for, and what `attend` gives for its new rows means nothing.  lengths are not to be
-    lowered by hand (a row is emptied by `free`)."""
+    lowered by hand (a row is emptied by `free`).
+
+    digests=True keeps a digest beside every page: `append` brings them up to date, `select` chooses each row's pages by them, and `attend`
+    with those pages reads nothing else, which is what a long cache is read with."""
 
     def __init__(self, layers: int, heads: int, d: int, pages: int, sequences: int, tokens: int, page: int = 64, dtype=torch.bfloat16, codes: bool = False,
-                 rotation_seed: int = 0, device="cuda"):
+                 rotation_seed: int = 0, device="cuda", digests: bool = False):
         if kv_page_bytes(CODE4 if codes else _TYPES.get(dtype, -1), page, heads, d) == 0:
             raise ValueError(f"no cache of pages of {page} tokens, {heads} heads and {d} coordinates in {'codes' if codes else dtype}")
         if layers < 1 or pages < 1 or sequences < 1 or tokens < 1:
@@ -356,6 +489,7 @@ class KVCache:
         self.d, self.heads, self.page, self.codes = d, heads, page, codes
         record = (heads, page * (d + 4)) if codes else (heads, 2, page, d)
         self.pools = torch.empty((layers, pages, *record), dtype=torch.uint8 if codes else dtype, device=device)
+        self.digests = torch.empty((layers, pages, heads, 2, d), dtype=torch.float16 if codes else dtype, device=device) if digests else None
         self.table = torch.full((sequences, -(-tokens // page)), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self.refs = torch.zeros(pages, dtype=torch.int32, device=device)
@@ -373,15 +507,31 @@ class KVCache:
 
     def append(self, layer: int, k, v, starts=None, stream=None):
         kv_append(self.pools[layer], k, v, self.table, self.lengths, starts, stream=stream, asked=self._asked, granted=self._granted, **self._codec)
+        if self.digests is not None:
+            kv_digest(self.pools[layer], self.digests[layer], self.table, self.lengths, starts, stream=stream, asked=self._asked, granted=self._granted, **self._codec)
 
-    def attend(self, layer: int, q, starts=None, max_new: int | None = None, window: int = 0, sinks: int = 0, scale=None, out=None, lse=None, stream=None):
+    def select(self, layer: int, q, count: int, starts=None, max_new: int | None = None, first: int = 1, last: int = 1, stream=None):
+        """The `count` pages of each row and key-value head, for `attend`."""
+        if self.digests is None:
+            raise ValueError("pages are chosen by their digests: make the cache with digests=True")
+        scores = kv_score(q, self.digests[layer], self.pools[layer], self.table, self.lengths, starts, max_new, stream=stream, **self._codec)
+        return kv_select(scores, self.lengths, self.page, count, starts, first, last, stream=stream)
+
+    def attend(self, layer: int, q, starts=None, max_new: int | None = None, window: int = 0, sinks: int = 0, scale=None, out=None, lse=None, stream=None, pages=None):
+        if pages is not None:
+            if window:
+                raise ValueError("attention over chosen pages has no window: the pages say what is seen")
+            return kv_attend_pages(q, self.pools[layer], self.table, self.lengths, pages, starts, max_new, scale, out=out, lse=lse, stream=stream, **self._codec)
         return kv_attend(q, self.pools[layer], self.table, self.lengths, starts, max_new, window, sinks, scale, out=out, lse=lse, stream=stream, **self._codec)
 
     def read(self, layer: int, k_out, v_out, starts=None, stream=None):
         kv_read(self.pools[layer], self.table, self.lengths, k_out, v_out, starts, stream=stream, **self._codec)
 
+    def _records(self):
+        return self.pools if self.digests is None else [self.pools, self.digests]
+
     def fork(self, parents, children, stream=None):
-        return kv_fork(self.pools, self.table, self.lengths, self.refs, parents, children, self.page, stream)
+        return kv_fork(self._records(), self.table, self.lengths, self.refs, parents, children, self.page, stream)
 
     def free(self, rows, stream=None):
         kv_free(self.table, self.lengths, self.refs, rows, stream)
@@ -390,4 +540,4 @@ class KVCache:
         kv_trim(self.table, self.lengths, self.refs, self.page, window, sinks, stream)
 
     def compact(self, stream=None):
-        return kv_compact(self.pools, self.table, self.refs, stream)
+        return kv_compact(self._records(), self.table, self.refs, stream)
