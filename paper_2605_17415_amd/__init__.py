@@ -6,12 +6,17 @@ from .binding import (ALLOC_FN, FREE_FN, Index, IvftqError, declared_symbols, iv
 
 _KV = ("KVCache", "declared_kv_symbols", "kv_append", "kv_attend", "kv_attend_pages", "kv_compact", "kv_copy", "kv_digest", "kv_fork", "kv_free",
        "kv_page_bytes", "kv_read", "kv_reserve", "kv_score", "kv_select", "kv_trim")
+_SAMPLE = ("declared_sample_symbols", "sample_tokens")
 
 
 def __getattr__(name):
-    """The key-value cache's calls take torch tensors and nothing else: torch is imported with the first of them."""
+    """The calls of the key-value cache and of sampling take torch tensors and nothing else: torch is imported with the first of them."""
     if name in _KV:
         from . import kv
         globals().update({n: getattr(kv, n) for n in _KV})
+        return globals()[name]
+    if name in _SAMPLE:
+        from . import sample
+        globals().update({n: getattr(sample, n) for n in _SAMPLE})
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

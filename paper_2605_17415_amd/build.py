@@ -16,7 +16,7 @@ SOURCES = ["host_math.cpp", "coarse_kernels.hip", "encode_kernels.hip", "list_ke
            "batch_scan_b5.hip", "batch_scan_b8.hip", "api.hip",
            "kv_rows.hip", "kv_pages.hip", "kv_attend_d64.hip", "kv_attend_d96.hip", "kv_attend_d128.hip", "kv_attend_d192.hip",
            "kv_attend_d256.hip", "kv_choose.hip", "kv_pick_d64.hip", "kv_pick_d96.hip", "kv_pick_d128.hip", "kv_pick_d192.hip",
-           "kv_pick_d256.hip", "kv_api.hip"]
+           "kv_pick_d256.hip", "kv_api.hip", "sample.hip"]
 
 # packed-fp32 instruction selection is switched off for every device compile
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
