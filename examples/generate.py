@@ -2,9 +2,10 @@
 one prompt is forked into two answers, tokens are made one at a time, ended conversations give their pages back and the pool is
 brought together.
 
-    python examples/generate.py [--codes] [--window 64 --sinks 4] [--steps 24]
+    python examples/generate.py [--codes] [--window 64 --sinks 4 | --pages 4] [--temperature 0.8 --top-k 40 --top-p 0.9 --min-p 0.02] [--steps 24]
 
-With --check every step's logits are compared with a full recomputation in float32 that keeps no cache.
+--pages: each token attends to that many pages of its own choice.  With a temperature tokens are sampled, otherwise the likeliest is taken.
+With --check every step's logits are compared with a full recomputation in float32 that keeps no cache and sees every page.
 """
 from __future__ import annotations
 
@@ -61,13 +62,13 @@ def recompute(model, tokens, window, sinks):
     return wide(torch.tensor(tokens, device=at.device), at, attention)[-1]
 
 
-def generate(codes=False, window=0, sinks=0, steps=24, check=False, page=16, prompts=(37, 5, 90), seed=0):
+def generate(codes=False, window=0, sinks=0, steps=24, check=False, page=16, prompts=(37, 5, 90), seed=0, pages=0, temperature=0.0, top_k=0, top_p=1.0, min_p=0.0):
     """Returns (token lists, largest difference of logits from the recomputation relative to their spread, pages left in use)."""
     device = torch.device("cuda", torch.cuda.current_device())
     model = Model(seed=seed, device=device)
     rows = len(prompts) + 1                                                       # one more for the fork
     cache = ivftq.KVCache(model.layers, model.kv_heads, model.d, pages=rows * (max(prompts) + steps + page) // page + rows, sequences=rows,
-                          tokens=max(prompts) + steps + 1, page=page, codes=codes, device=device)
+                          tokens=max(prompts) + steps + 1, page=page, codes=codes, device=device, digests=pages > 0)
     g = torch.Generator().manual_seed(seed + 1)
     texts = [torch.randint(0, 256, (n,), generator=g).tolist() for n in prompts] + [[]]
     worst = 0.0
@@ -84,6 +85,9 @@ def generate(codes=False, window=0, sinks=0, steps=24, check=False, page=16, pro
 
         def attention(layer, q, k, v):
             cache.append(layer, k, v, starts)
+            if pages:
+                chosen = cache.select(layer, q, pages, starts, max_new=max(map(len, new)))
+                return cache.attend(layer, q, starts, max_new=max(map(len, new)), pages=chosen)
             return cache.attend(layer, q, starts, max_new=max(map(len, new)), window=window, sinks=sinks)
 
         return model(flat, positions, attention)[(starts[1:] - 1).long().clamp(min=0)]
@@ -94,10 +98,17 @@ def generate(codes=False, window=0, sinks=0, steps=24, check=False, page=16, pro
     logits[-1] = logits[0]
     live = list(range(rows))
     for n in range(steps):
-        best = logits.topk(2).indices.tolist()
+        if temperature > 0:
+            u = torch.rand(rows, generator=g).to(device)
+            tokens = ivftq.sample_tokens(logits, u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p).tolist()
+        else:
+            best = logits.topk(2).indices.tolist()
+            tokens = [b[0] for b in best]
+            if n == 0:
+                tokens[-1] = best[-1][1]                                           # the fork begins with the second best token
         new = [[] for _ in range(rows)]
         for r in live:
-            new[r] = [best[r][1] if n == 0 and r == rows - 1 else best[r][0]]      # the fork begins with the second best token
+            new[r] = [tokens[r]]
             texts[r] += new[r]
         logits = step(new)
         if check:
@@ -118,10 +129,15 @@ if __name__ == "__main__":
     parser.add_argument("--codes", action="store_true", help="keep keys and values in 4-bit codes")
     parser.add_argument("--window", type=int, default=0)
     parser.add_argument("--sinks", type=int, default=0)
+    parser.add_argument("--pages", type=int, default=0, help="pages that a token attends to (0: all)")
+    parser.add_argument("--temperature", type=float, default=0.0)
+    parser.add_argument("--top-k", type=int, default=0)
+    parser.add_argument("--top-p", type=float, default=1.0)
+    parser.add_argument("--min-p", type=float, default=0.0)
     parser.add_argument("--steps", type=int, default=24)
     parser.add_argument("--check", action="store_true")
     a = parser.parse_args()
-    got, off, used = generate(a.codes, a.window, a.sinks, a.steps, a.check)
+    got, off, used = generate(a.codes, a.window, a.sinks, a.steps, a.check, pages=a.pages, temperature=a.temperature, top_k=a.top_k, top_p=a.top_p, min_p=a.min_p)
     for r, text in enumerate(got):
         print(f"row {r}: {len(text)} tokens, the last {text[-8:]}")
     print(f"{used} pages in use" + (f", logits {off:.3g} from the recomputation" if a.check else ""))
