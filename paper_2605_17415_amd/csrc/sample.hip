@@ -1,5 +1,13 @@
-// The next token of each row from its logits: the k-th rank and the rank where the mass reaches p are found by counting (and adding up weights)
-// over the digits of the logits' order, most significant first; no row is sorted.
+// The next token of each row from its logits.  No row is sorted: what decides is always within a short list of tokens, whose ranks are counted.
+//   - k_sample_tops reads the logits once and leaves the largest one of every 4,096 tokens (a chunk) and of every 64 (a group).
+//   - Few ranks are kept (top_k up to 256): at least k tokens are not under the k-th largest group maximum, so the tokens not under it, a
+//     little more than k of them in as few groups, are the list (k_sample_rows).
+//   - Otherwise a second reading (k_sample_chunks) adds up the weights of every chunk, and where a rank is looked for by its number or its mass, of
+//     2,048 bins of logits.  k_sample_rows finds the bins in which the two ranks lie; a third reading (k_sample_bins) lists their tokens, and
+//     k_sample_cut counts ranks among them.
+//   - The token is looked for in the chunk in which the sum passes u times all of it.
+// Where a list would be too long (thousands of tokens within a bin) the row is worked through digit by digit of the logits' order by one
+// workgroup.
 //
 // Weights are whole numbers of 2^-42, so that partial sums of any split and order agree to the last bit, and e^x is computed in 64 bits:
 // a float32 weight is off by 2^-23, which over a hundred thousand tokens moves the drawn one in some of every thousand rows.
@@ -24,6 +32,19 @@ constexpr int kBlock = kThreads;                 // tokens whose mass is one num
 constexpr int kMostTokens = 1 << 20;
 constexpr double kUnit = 4398046511104.0;        // 2^42
 
+constexpr int kChunk = 4096, kGroup = 64, kGroups = kChunk / kGroup;
+constexpr int kFewRanks = 256;                   // top_k that goes by the groups
+constexpr int kList = 2048;                      // tokens of a list
+constexpr int kBins = 2048;
+constexpr int kSliceRows = 1024;                 // rows that share a workspace's places
+
+// What a row's search by bins has found.
+struct RowBins {
+    uint64_t before_k, before_p, total;          // mass of the bins before bin_k, before p0, of all
+    int32_t bin_k, p0, p1;                       // the bin of the last rank of top_k (kBins: none), the first and the last that the mass top_p can end in
+    uint32_t count_k;                            // tokens before bin_k
+};
+
 struct SampleArgs {
     const char* logits;
     int64_t row_stride;
@@ -31,22 +52,72 @@ struct SampleArgs {
     ivftq_sampling how;
     int32_t *tokens;
     float* logprobs;
-    int32_t vocabulary, rows;
+    int32_t vocabulary, rows, chunks;
+    // workspace, for each row: chunks' largest and lowest logit, the largest one's place, groups' largest ones, masses; bins, what they tell, the list
+    float *chunk_top, *chunk_low, *group_top;
+    int32_t* chunk_at;
+    uint64_t *chunk_mass, *bin_mass, *list;
+    uint32_t *bin_count, *list_count;
+    RowBins* found;
+};
+
+// How a row is sampled.
+enum Way { kTop, kFew, kBinned, kAll };
+struct Settings {
+    Way way;
+    int k;                                       // 0: all
+    float p, temperature;                        // p: 1: all
+    double least;                                // smallest weight
+    __device__ __forceinline__ Settings(const SampleArgs& a, int r) {
+        temperature = a.how.temperature ? a.how.temperature[r] : a.how.temperature_all;
+        const int top_k = a.how.top_k ? a.how.top_k[r] : a.how.top_k_all;
+        const float top_p = a.how.top_p ? a.how.top_p[r] : a.how.top_p_all, min_p = a.how.min_p ? a.how.min_p[r] : a.how.min_p_all;
+        k = top_k > 0 && top_k < a.vocabulary ? top_k : 0;
+        p = top_p < 1.f ? (top_p > 0.f ? top_p : 0.f) : 1.f;
+        least = min_p > 0.f ? (min_p < 1.f ? (double)min_p : 1.0) : 0.0;
+        // one rank is the largest logit
+        way = !(temperature > 0.f) || k == 1 || p == 0.f ? kTop : (k && k <= kFewRanks ? kFew : (k || p < 1.f ? kBinned : kAll));
+    }
 };
 
 // A logit and its order: larger numbers have larger keys, both zeros one, what is no number that of -infinity.
+template <int T> constexpr int kSize = T == IVFTQ_LOGITS_F32 ? 4 : 2;
+__device__ __forceinline__ float counted(float v) { return v == v ? v + 0.f : -INFINITY; }
 template <int T>
 __device__ __forceinline__ float logit(const char* row, int i) {
-    float v;
-    if constexpr (T == IVFTQ_LOGITS_F32) v = reinterpret_cast<const float*>(row)[i];
-    else if constexpr (T == IVFTQ_LOGITS_F16) v = (float)reinterpret_cast<const _Float16*>(row)[i];
-    else v = __builtin_bit_cast(float, (uint32_t)reinterpret_cast<const uint16_t*>(row)[i] << 16);
-    return v == v ? v + 0.f : -INFINITY;
+    if constexpr (T == IVFTQ_LOGITS_F32) return counted(reinterpret_cast<const float*>(row)[i]);
+    else if constexpr (T == IVFTQ_LOGITS_F16) return counted((float)reinterpret_cast<const _Float16*>(row)[i]);
+    else return counted(__builtin_bit_cast(float, (uint32_t)reinterpret_cast<const uint16_t*>(row)[i] << 16));
+}
+// N neighbouring ones from i on, in loads of 16 bytes wherever the row begins; behind the row's end -infinity.
+template <int T, int N>
+__device__ __forceinline__ void logits_of(const char* row, int i, int n, float (&v)[N]) {
+    if (i + N <= n) {
+        if constexpr (T == IVFTQ_LOGITS_F32) {
+            float w[N];
+            __builtin_memcpy(w, row + (int64_t)i * 4, N * 4);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = counted(w[e]);
+        } else {
+            uint32_t w[N / 2];
+            __builtin_memcpy(w, row + (int64_t)i * 2, N * 2);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const uint32_t bits = e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffff;
+                v[e] = counted(T == IVFTQ_LOGITS_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)bits) : __builtin_bit_cast(float, bits << 16));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = i + e < n ? logit<T>(row, i + e) : -INFINITY;
+    }
 }
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t bits = __builtin_bit_cast(uint32_t, v);
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
+// A token's rank as a number: larger ones first.
+__device__ __forceinline__ uint64_t rank_of(float v, int i) { return (uint64_t)key_of(v) << 20 | (uint32_t)(kMostTokens - 1 - i); }
 __device__ __forceinline__ float of_key(uint32_t k) { return __builtin_bit_cast(float, k >> 31 ? k & 0x7fffffffu : ~k); }
 
 // e^x for x <= 0 to about 2^-50: x = n ln 2 + r, |r| <= ln 2 / 2, the series of e^r up to r^12.
@@ -141,15 +212,29 @@ __device__ __forceinline__ uint32_t find_key(const char* row, int n, uint32_t le
     return prefix;
 }
 
-// A workgroup a row.
+// u of a whole number of masses: the token is the first up to which more than this has been added up.
+__device__ __forceinline__ uint64_t target_of(float u, uint64_t all) {
+    if (u >= 1.f) return all - 1;
+    const double want = (u > 0.f ? (double)u : 0.0) * (double)all;
+    return want < (double)all ? (uint64_t)want : all - 1;
+}
+__device__ __forceinline__ void drawn(const SampleArgs& a, int r, int token, double weight, uint64_t all) {
+    a.tokens[r] = token;
+    if (a.logprobs) a.logprobs[r] = (float)log(weight / ((double)all / kUnit));
+}
+__device__ __forceinline__ void top_token(const SampleArgs& a, int r, float top, int at) {
+    if (threadIdx.x) return;
+    const bool none = top == -INFINITY;
+    a.tokens[r] = none ? -1 : at;
+    if (a.logprobs) a.logprobs[r] = none ? -INFINITY : 0.f;
+}
+
+// A row by one workgroup, whatever it holds.
 template <int T>
-__global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
-    __shared__ Shared s;
-    const int r = blockIdx.x, n = a.vocabulary, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const char* row = a.logits + (int64_t)r * a.row_stride * (T == IVFTQ_LOGITS_F32 ? 4 : 2);
-    const float temperature = a.how.temperature ? a.how.temperature[r] : a.how.temperature_all;
-    int top_k = a.how.top_k ? a.how.top_k[r] : a.how.top_k_all;
-    const float top_p = a.how.top_p ? a.how.top_p[r] : a.how.top_p_all, min_p = a.how.min_p ? a.how.min_p[r] : a.how.min_p_all;
+__device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Shared& s) {
+    const int n = a.vocabulary, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
+    __syncthreads();
 
     // the largest logit and its first place
     uint32_t best = 0;
@@ -170,24 +255,20 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     for (int w = 0; w < kWaves; ++w)
         if (s.most[w] > best || (s.most[w] == best && (int)s.sums[w] < at)) { best = s.most[w]; at = (int)s.sums[w]; }
     __syncthreads();
-    const Weights weight{of_key(best), 1.0 / (double)temperature};
-    const bool none = weight.top == -INFINITY;
-    if (none || !(temperature > 0.f)) {
-        if (threadIdx.x == 0) {
-            a.tokens[r] = none ? -1 : at;
-            if (a.logprobs) a.logprobs[r] = none ? -INFINITY : 0.f;
-        }
+    const Weights weight{of_key(best), 1.0 / (double)how.temperature};
+    if (weight.top == -INFINITY || how.way == kTop) {
+        top_token(a, r, weight.top, at);
         return;
     }
 
     // kept: keys above `cut`, and of its equals the first `ties`
     uint32_t cut = 0;
     uint64_t ties = ~0ull, above = 0;
-    if (top_k > 0 && top_k < n) {
-        cut = find_key<T>(row, n, 0, (double)top_k, s, above, [](float) { return (uint64_t)1; });
-        ties = (uint64_t)top_k - above;
+    if (how.k) {
+        cut = find_key<T>(row, n, 0, (double)how.k, s, above, [](float) { return (uint64_t)1; });
+        ties = (uint64_t)how.k - above;
     }
-    if (top_p < 1.f) {
+    if (how.p < 1.f) {
         uint64_t mass = 0, all;
         for (int i = threadIdx.x; i < n; i += kThreads) {
             const float v = logit<T>(row, i);
@@ -195,20 +276,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
         }
         scan(mass, s.sums, all);
         if (ties != ~0ull) all += ties * weight.mass(of_key(cut));
-        const double want = (double)(top_p > 0.f ? top_p : 0.f) * (double)all;
-        if (want > 0.0) {
-            const uint32_t key = find_key<T>(row, n, cut, want, s, above, [&](float v) { return weight.mass(v); });
-            const uint64_t one = weight.mass(of_key(key));
-            // rank i of its equals is kept where above + i * one < want
-            uint64_t i = (uint64_t)((want - (double)above) / (double)one);
-            while (i > 0 && !((double)(above + (i - 1) * one) < want)) --i;
-            while ((double)(above + i * one) < want) ++i;
-            ties = key == cut && i > ties ? ties : i;
-            cut = key;
-        } else {
-            cut = best;
-            ties = 1;
-        }
+        const double want = (double)how.p * (double)all;             // above zero
+        const uint32_t key = find_key<T>(row, n, cut, want, s, above, [&](float v) { return weight.mass(v); });
+        const uint64_t one = weight.mass(of_key(key));
+        // rank i of its equals is kept where above + i * one < want
+        uint64_t i = (uint64_t)((want - (double)above) / (double)one);
+        while (i > 0 && !((double)(above + (i - 1) * one) < want)) --i;
+        while ((double)(above + i * one) < want) ++i;
+        ties = key == cut && i > ties ? ties : i;
+        cut = key;
     }
     // the place of the last of the equals that are kept
     int last = n;
@@ -237,12 +313,11 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
         }
         __syncthreads();
     }
-    const double least = min_p > 0.f ? (min_p < 1.f ? (double)min_p : 1.0) : 0.0;
     auto kept = [&](int i, double& w) {
         const float v = logit<T>(row, i);
         const uint32_t k = key_of(v);
         w = weight(v);
-        return (k > cut || (k == cut && i <= last)) && w >= least ? Weights::whole(w) : 0;
+        return (k > cut || (k == cut && i <= last)) && w >= how.least ? Weights::whole(w) : 0;
     };
     // masses of blocks, the block in which the sum passes u * all, the token in it
     for (int b = wave; b < blocks; b += kWaves) {
@@ -256,9 +331,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     __syncthreads();
     uint64_t all;
     const uint64_t mine = (int)threadIdx.x < blocks ? s.blocks[threadIdx.x] : 0, upto = scan(mine, s.sums, all);
-    const float u = a.u[r];
-    const double want = (u > 0.f ? (double)u : 0.0) * (double)all;
-    const uint64_t target = u < 1.f || !(u == u) ? (want < (double)all ? (uint64_t)want : all - 1) : all - 1;
+    const uint64_t target = target_of(a.u[r], all);
     if (upto > target && upto - mine <= target) { s.digit = threadIdx.x; s.above = upto - mine; }
     __syncthreads();
     const int i = (int)s.digit * kBlock + threadIdx.x;
@@ -267,10 +340,592 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     double w = 0.0;
     uint64_t total;
     const uint64_t one = i < n ? kept(i, w) : 0, sum = before + scan(one, s.sums, total);
-    if (sum > target && sum - one <= target) {
-        a.tokens[r] = i;
-        if (a.logprobs) a.logprobs[r] = (float)log(w / ((double)all / kUnit));
+    if (sum > target && sum - one <= target) drawn(a, r, i, w, all);
+}
+
+// ---- chunks ------------------------------------------------------------------------------------------------------------
+constexpr int kChunkThreads = 256;
+constexpr int kEach = kChunk / kChunkThreads / 8;         // a thread's pieces of eight tokens
+
+__device__ __forceinline__ float lane_max(float v, int width) {
+    for (int o = 1; o < width; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+__device__ __forceinline__ float lane_min(float v, int width) {
+    for (int o = 1; o < width; o <<= 1) v = fminf(v, __shfl_xor(v, o));
+    return v;
+}
+
+// The first reading: 4,096 tokens a workgroup, bound by memory.
+template <int T>
+__global__ __launch_bounds__(kChunkThreads) void k_sample_tops(SampleArgs a) {
+    __shared__ float tops[4], lows[4];
+    __shared__ int places[4];
+    const int r = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, n = a.vocabulary, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
+    const Settings how(a, r);
+    float v[kEach][8], top = -INFINITY, low = INFINITY;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) logits_of<T, 8>(row, chunk * kChunk + (j * kChunkThreads + threadIdx.x) * 8, n, v[j]);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            most = fmaxf(most, v[j][e]);
+            low = v[j][e] > -INFINITY ? fminf(low, v[j][e]) : low;
+        }
+        top = fmaxf(top, most);
+        if (how.way == kFew) {
+            most = lane_max(most, 8);
+            if ((lane & 7) == 0) a.group_top[((int64_t)r * a.chunks + chunk) * kGroups + (j * kChunkThreads + threadIdx.x) / 8] = most;
+        }
     }
+    top = lane_max(top, 64);
+    low = lane_min(low, 64);
+    if (lane == 0) { tops[wave] = top; lows[wave] = low; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) { top = fmaxf(top, tops[w]); low = fminf(low, lows[w]); }
+    int at = n;
+#pragma unroll
+    for (int j = kEach - 1; j >= 0; --j)
+#pragma unroll
+        for (int e = 7; e >= 0; --e) at = v[j][e] == top ? chunk * kChunk + (j * kChunkThreads + (int)threadIdx.x) * 8 + e : at;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int other = __shfl_xor(at, o); at = other < at ? other : at; }
+    if (lane == 0) places[wave] = at;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) at = places[w] < at ? places[w] : at;
+        const int64_t to = (int64_t)r * a.chunks + chunk;
+        a.chunk_top[to] = top;
+        a.chunk_low[to] = low;
+        a.chunk_at[to] = at;
+    }
+    if (how.way == kBinned) {                             // what the next readings add to
+        for (int i = chunk * kChunkThreads + threadIdx.x; i < kBins; i += a.chunks * kChunkThreads) {
+            a.bin_mass[(int64_t)r * kBins + i] = 0;
+            a.bin_count[(int64_t)r * kBins + i] = 0;
+        }
+        if (chunk == 0 && threadIdx.x == 0) a.list_count[r] = 0;
+    }
+}
+
+// A row's largest logit, its first place, the lowest one above -infinity, from those of its chunks; by the whole workgroup (W wavefronts).
+struct RowTop { float top, low; int at; };
+template <int W>
+__device__ __forceinline__ RowTop row_top(const SampleArgs& a, int r) {
+    __shared__ float tops[W], lows[W];
+    __shared__ int places[W];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    RowTop x{-INFINITY, INFINITY, kMostTokens};
+    for (int c = threadIdx.x; c < a.chunks; c += W * 64) {
+        const int64_t from = (int64_t)r * a.chunks + c;
+        const float top = a.chunk_top[from];
+        if (top > x.top || x.at == kMostTokens) { x.top = top; x.at = a.chunk_at[from]; }
+        x.low = fminf(x.low, a.chunk_low[from]);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const float top = __shfl_xor(x.top, o);
+        const int at = __shfl_xor(x.at, o);
+        if (top > x.top || (top == x.top && at < x.at)) { x.top = top; x.at = at; }
+        x.low = fminf(x.low, __shfl_xor(x.low, o));
+    }
+    if (lane == 0) { tops[wave] = x.top; lows[wave] = x.low; places[wave] = x.at; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (tops[w] > x.top || (tops[w] == x.top && places[w] < x.at)) { x.top = tops[w]; x.at = places[w]; }
+        x.low = fminf(x.low, lows[w]);
+    }
+    return x;
+}
+
+// Bins of logits: equally wide, from the largest logit down to the lowest one or 32 temperatures, the last one open; a bin's logits come before
+// the next one's.
+struct Bins {
+    float top, by;
+    int last;
+    __device__ __forceinline__ Bins(float top_, float low, float reach, int bins) : top(top_), last(bins - 1) {
+        const float wide = fminf(top - low, reach);
+        by = wide > 0.f ? (float)bins / wide : 0.f;
+        if (!(by < 1e30f)) by = 1e30f;
+    }
+    __device__ __forceinline__ int operator()(float v) const {      // v above -infinity
+        const float x = (top - v) * by;
+        return x < (float)last ? (int)x : last;
+    }
+};
+__device__ __forceinline__ Bins row_bins(const RowTop& x, const Settings& how) { return Bins(x.top, x.low, 32.f * how.temperature, kBins); }
+
+// The second reading: chunks' masses, or the masses and numbers of the bins.
+template <int T>
+__global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
+    __shared__ uint64_t mass[kBins], sums[4];
+    __shared__ uint32_t count[kBins];
+    const int r = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, n = a.vocabulary;
+    const Settings how(a, r);
+    if (how.way == kTop || how.way == kFew) return;
+    const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
+    float v[kEach][8];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) logits_of<T, 8>(row, chunk * kChunk + (j * kChunkThreads + threadIdx.x) * 8, n, v[j]);
+    const RowTop x = row_top<4>(a, r);
+    if (!(__builtin_fabsf(x.top) < INFINITY)) return;                  // one workgroup takes the row whole
+    const Weights weight{x.top, 1.0 / (double)how.temperature};
+    if (how.way == kAll) {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double w = weight(v[j][e]);
+                sum += w >= how.least ? Weights::whole(w) : 0;
+            }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) a.chunk_mass[(int64_t)r * a.chunks + chunk] = sums[0] + sums[1] + sums[2] + sums[3];
+        return;
+    }
+    for (int i = threadIdx.x; i < kBins; i += kChunkThreads) { mass[i] = 0; count[i] = 0; }
+    __syncthreads();
+    const Bins bins = row_bins(x, how);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (!(v[j][e] > -INFINITY)) continue;
+            const int bin = bins(v[j][e]);
+            if (how.p < 1.f) {
+                const uint64_t m = weight.mass(v[j][e]);
+                if (m) atomicAdd(reinterpret_cast<unsigned long long*>(&mass[bin]), (unsigned long long)m);
+            }
+            if (how.k) atomicAdd(&count[bin], 1u);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kChunkThreads) {
+        if (mass[i]) atomicAdd(reinterpret_cast<unsigned long long*>(&a.bin_mass[(int64_t)r * kBins + i]), (unsigned long long)mass[i]);
+        if (count[i]) atomicAdd(&a.bin_count[(int64_t)r * kBins + i], count[i]);
+    }
+}
+
+// The third reading: the masses of the chunks' tokens that are kept for certain, and the tokens whose ranks have to be counted.
+template <int T>
+__global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
+    __shared__ uint64_t sums[4];
+    __shared__ uint32_t many, begin;
+    const int r = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, n = a.vocabulary;
+    const Settings how(a, r);
+    if (how.way != kBinned) return;
+    const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
+    float v[kEach][8];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) logits_of<T, 8>(row, chunk * kChunk + (j * kChunkThreads + threadIdx.x) * 8, n, v[j]);
+    if (threadIdx.x == 0) many = 0;
+    const RowTop x = row_top<4>(a, r);
+    if (!(__builtin_fabsf(x.top) < INFINITY)) return;
+    const Weights weight{x.top, 1.0 / (double)how.temperature};
+    const Bins bins = row_bins(x, how);
+    const RowBins f = a.found[r];
+    uint64_t sum = 0;
+    uint32_t open = 0;                                     // of the thread's tokens: those of the list, a bit each
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int bin = v[j][e] > -INFINITY ? bins(v[j][e]) : kBins + 1;
+            if (bin < f.p0) {
+                const double w = weight(v[j][e]);
+                sum += w >= how.least ? Weights::whole(w) : 0;
+            } else if (bin <= f.p1 || bin == f.bin_k) {
+                open |= 1u << (8 * j + e);
+            }
+        }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+    uint32_t at = open ? atomicAdd(&many, (uint32_t)__popc(open)) : 0;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        a.chunk_mass[(int64_t)r * a.chunks + chunk] = sums[0] + sums[1] + sums[2] + sums[3];
+        begin = many ? atomicAdd(&a.list_count[r], many) : 0;
+    }
+    __syncthreads();
+    at += begin;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (open >> (8 * j + e) & 1) {
+                if (at < kList) a.list[(int64_t)r * kList + at] = rank_of(v[j][e], chunk * kChunk + (j * kChunkThreads + (int)threadIdx.x) * 8 + e);
+                ++at;
+            }
+}
+
+// ---- rows --------------------------------------------------------------------------------------------------------------
+
+struct ListShared {
+    uint64_t rank[kList], mass[kList];             // of the list's tokens
+    uint64_t sums[kWaves];
+    uint64_t value[4];
+    uint32_t many;
+    uint32_t bins[1024];
+    int groups[kList];
+};
+
+// Sum over all threads.
+__device__ __forceinline__ uint64_t sum_all(uint64_t v, uint64_t* sums) { uint64_t all; scan(v, sums, all); return all; }
+
+// The token among those of rank `cut` and better, by the masses of the chunks (in `mass`, a number a chunk).
+template <int T>
+__device__ __forceinline__ void locate(const SampleArgs& a, int r, const Weights& weight, double least, uint64_t cut, const uint64_t* mass, ListShared& s) {
+    __syncthreads();
+    uint64_t all;
+    const uint64_t mine = (int)threadIdx.x < a.chunks ? mass[threadIdx.x] : 0, upto = scan(mine, s.sums, all), target = target_of(a.u[r], all);
+    if (upto > target && upto - mine <= target) { s.value[0] = threadIdx.x; s.value[1] = upto - mine; }
+    __syncthreads();
+    const int i = (int)s.value[0] * kChunk + (int)threadIdx.x * 4;
+    const uint64_t before = s.value[1];
+    float v[4];
+    logits_of<T, 4>(a.logits + (int64_t)r * a.row_stride * kSize<T>, i, a.vocabulary, v);
+    double w[4];
+    uint64_t one[4], sum = 0, whole;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        w[e] = weight(v[e]);
+        one[e] = i + e < a.vocabulary && rank_of(v[e], i + e) >= cut && w[e] >= least ? Weights::whole(w[e]) : 0;
+        sum += one[e];
+    }
+    uint64_t at = before + scan(sum, s.sums, whole) - sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (at + one[e] > target && at <= target) drawn(a, r, i + e, w[e], all);
+        at += one[e];
+    }
+}
+
+// Few ranks: false where the list would be too long.
+template <int T>
+__device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Settings& how, const RowTop& x, const Weights& weight, ListShared& s) {
+    const int groups = a.chunks * kGroups, lane = threadIdx.x & 63;
+    const float* tops = a.group_top + (int64_t)r * groups;
+    const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
+    // the bin of the k-th largest group maximum
+    float low = INFINITY;
+    for (int g = threadIdx.x; g < groups; g += kThreads) { const float t = tops[g]; low = t > -INFINITY ? fminf(low, t) : low; }
+    low = lane_min(low, 64);
+    if (lane == 0) s.sums[threadIdx.x >> 6] = __builtin_bit_cast(uint32_t, low);
+    s.bins[threadIdx.x] = 0;
+    if (threadIdx.x == 0) { s.many = 0; s.value[0] = 1023; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) low = fminf(low, __builtin_bit_cast(float, (uint32_t)s.sums[w]));
+    const Bins bins(x.top, low, INFINITY, 1024);
+    for (int g = threadIdx.x; g < groups; g += kThreads) {
+        const float t = tops[g];
+        if (t > -INFINITY) atomicAdd(&s.bins[bins(t)], 1u);
+    }
+    __syncthreads();
+    uint64_t all;
+    const uint64_t mine = s.bins[threadIdx.x], upto = scan(mine, s.sums, all);
+    if (upto >= (uint64_t)how.k && upto - mine < (uint64_t)how.k) { s.value[0] = threadIdx.x; s.value[1] = upto; }
+    if (threadIdx.x == 1023 && upto < (uint64_t)how.k) s.value[1] = upto;
+    __syncthreads();
+    const int cut_bin = (int)s.value[0];
+    if (s.value[1] > (uint64_t)kList) return false;
+    __syncthreads();
+    for (int g = threadIdx.x; g < groups; g += kThreads) {
+        const float t = tops[g];
+        if (t > -INFINITY && bins(t) <= cut_bin) s.groups[atomicAdd(&s.many, 1u)] = g;
+    }
+    __syncthreads();
+    const int chosen = (int)s.many;
+    __syncthreads();
+    if (threadIdx.x == 0) s.many = 0;
+    __syncthreads();
+    for (int u = threadIdx.x >> 6; u < chosen; u += kWaves) {
+        const int i = s.groups[u] * kGroup + lane;
+        const float v = i < a.vocabulary ? logit<T>(row, i) : -INFINITY;
+        const bool in = v > -INFINITY && bins(v) <= cut_bin;
+        const uint64_t which = __ballot(in);
+        uint32_t begin = 0;
+        if (lane == 0) begin = atomicAdd(&s.many, (uint32_t)__popcll(which));
+        const uint32_t at = __shfl(begin, 0) + (uint32_t)__popcll(which & ((1ull << lane) - 1));
+        if (in && at < kList) { s.rank[at] = rank_of(v, i); s.mass[at] = weight.mass(v); }
+    }
+    __syncthreads();
+    const int n = (int)s.many;
+    if (n > kList) return false;
+    // ranks, and the mass before each, counted
+    uint64_t rank[2], mass[2], before[2] = {0, 0};
+    uint32_t ahead[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int i = threadIdx.x + e * kThreads;
+        rank[e] = i < n ? s.rank[i] : 0;
+        mass[e] = i < n ? s.mass[i] : 0;
+        if (i < n)
+            for (int j = 0; j < n; ++j) {
+                const bool better = s.rank[j] > rank[e];
+                ahead[e] += better;
+                before[e] += better ? s.mass[j] : 0;
+            }
+    }
+    const uint64_t total = sum_all((ahead[0] < (uint32_t)how.k ? mass[0] : 0) + (ahead[1] < (uint32_t)how.k ? mass[1] : 0), s.sums);
+    const double want = (double)how.p * (double)total;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int i = threadIdx.x + e * kThreads;
+        const bool in = i < n && ahead[e] < (uint32_t)how.k && (how.p == 1.f || (double)before[e] < want) && weight(of_key((uint32_t)(rank[e] >> 20))) >= how.least;
+        mass[e] = in ? mass[e] : 0;
+        if (i < n) s.mass[i] = mass[e];
+    }
+    const uint64_t kept = sum_all(mass[0] + mass[1], s.sums), target = target_of(a.u[r], kept);
+    // the first token up to which the masses pass the target: in the order of the tokens
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if (!mass[e]) continue;
+        const uint32_t place = (uint32_t)rank[e] & (kMostTokens - 1);
+        uint64_t earlier = 0;
+        for (int j = 0; j < n; ++j) earlier += ((uint32_t)s.rank[j] & (kMostTokens - 1)) > place ? s.mass[j] : 0;
+        if (earlier <= target && earlier + mass[e] > target) drawn(a, r, kMostTokens - 1 - (int)place, weight(of_key((uint32_t)(rank[e] >> 20))), kept);
+    }
+    return true;
+}
+
+// What the bins tell: a thread two of them.
+__device__ __forceinline__ RowBins look_up(const SampleArgs& a, int r, const Settings& how, ListShared& s) {
+    const uint64_t* masses = a.bin_mass + (int64_t)r * kBins + 2 * threadIdx.x;
+    const uint32_t* counts = a.bin_count + (int64_t)r * kBins + 2 * threadIdx.x;
+    const uint64_t m0 = masses[0], m1 = masses[1], c0 = counts[0], c1 = counts[1];
+    uint64_t all, many;
+    const uint64_t mass = scan(m0 + m1, s.sums, all) - m0 - m1;
+    __syncthreads();
+    const uint64_t count = scan(c0 + c1, s.sums, many) - c0 - c1;
+    RowBins f{all, 0, all, kBins, kBins, kBins, 0};
+    uint64_t in_k = 0;
+    if (how.k && many > (uint64_t)how.k) {             // (otherwise every token above -infinity)
+        const bool first = count < (uint64_t)how.k && count + c0 >= (uint64_t)how.k, second = count + c0 < (uint64_t)how.k && count + c0 + c1 >= (uint64_t)how.k;
+        if (first || second) {
+            s.value[0] = 2 * threadIdx.x + second;
+            s.value[1] = second ? count + c0 : count;
+            s.value[2] = second ? mass + m0 : mass;
+            s.value[3] = second ? m1 : m0;
+        }
+        __syncthreads();
+        f.bin_k = (int)s.value[0];
+        f.count_k = (uint32_t)s.value[1];
+        f.before_k = s.value[2];
+        in_k = s.value[3];
+        f.p0 = f.bin_k;
+        f.p1 = f.bin_k;
+        __syncthreads();
+    }
+    if (how.p < 1.f) {                                 // the mass of the ranks that top_k leaves is before_k to before_k + in_k
+        const double low = (double)how.p * (double)f.before_k, high = (double)how.p * (double)(f.before_k + in_k);
+        if (threadIdx.x == 0) { s.value[0] = 0; s.value[1] = 0; s.value[2] = f.bin_k < kBins ? f.bin_k : kBins - 1; }
+        __syncthreads();
+        const uint64_t m[2] = {m0, m1};
+        uint64_t before = mass;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if ((double)before < low && (double)(before + m[e]) >= low) { s.value[0] = 2 * threadIdx.x + e; s.value[1] = before; }
+            if ((double)before < high && (double)(before + m[e]) >= high) s.value[2] = 2 * threadIdx.x + e;
+            before += m[e];
+        }
+        __syncthreads();
+        f.p0 = (int)s.value[0];
+        f.before_p = s.value[1];
+        f.p1 = (int)s.value[2];
+    }
+    return f;
+}
+
+// After the first two readings: rows by their largest logit, by few ranks and by all chunks are done, of the others the bins are found.
+template <int T>
+__global__ __launch_bounds__(kThreads) void k_sample_rows(SampleArgs a) {
+    __shared__ union { ListShared list; Shared whole; } s;
+    const int r = blockIdx.x;
+    const Settings how(a, r);
+    const RowTop x = row_top<kWaves>(a, r);
+    if (x.top == -INFINITY || how.way == kTop) {
+        top_token(a, r, x.top, x.at);
+        return;
+    }
+    const Weights weight{x.top, 1.0 / (double)how.temperature};
+    bool done = x.top < INFINITY;
+    if (done && how.way == kFew) done = few_ranks<T>(a, r, how, x, weight, s.list);
+    else if (done && how.way == kAll) locate<T>(a, r, weight, how.least, 0, a.chunk_mass + (int64_t)r * a.chunks, s.list);
+    else if (done) {
+        const RowBins f = look_up(a, r, how, s.list);
+        if (threadIdx.x == 0) a.found[r] = f;
+    }
+    if (!done) whole_row<T>(a, r, how, s.whole);
+}
+
+// Ranks by bins: where exactly they end, and the token.
+template <int T>
+__global__ __launch_bounds__(kThreads) void k_sample_cut(SampleArgs a) {
+    __shared__ union { ListShared list; Shared whole; } shared;
+    ListShared& s = shared.list;
+    const int r = blockIdx.x;
+    const Settings how(a, r);
+    if (how.way != kBinned) return;
+    const RowTop x = row_top<kWaves>(a, r);
+    if (!(__builtin_fabsf(x.top) < INFINITY)) return;       // done by k_sample_rows
+    const int n = (int)a.list_count[r];
+    if (n > kList) {
+        whole_row<T>(a, r, how, shared.whole);
+        return;
+    }
+    const Weights weight{x.top, 1.0 / (double)how.temperature};
+    const Bins bins = row_bins(x, how);
+    const RowBins f = a.found[r];
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        s.rank[i] = a.list[(int64_t)r * kList + i];
+        s.mass[i] = weight.mass(of_key((uint32_t)(s.rank[i] >> 20)));
+    }
+    __syncthreads();
+    uint64_t rank[2], mass[2], kept_k = 0;
+    int bin[2];
+    bool in[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int i = threadIdx.x + e * kThreads;
+        in[e] = i < n;
+        rank[e] = in[e] ? s.rank[i] : 0;
+        mass[e] = in[e] ? s.mass[i] : 0;
+        bin[e] = in[e] ? bins(of_key((uint32_t)(rank[e] >> 20))) : kBins + 1;
+        if (f.bin_k < kBins && in[e] && bin[e] >= f.bin_k) {          // ranks within top_k's last bin
+            uint32_t ahead = f.count_k;
+            for (int j = 0; j < n; ++j) ahead += s.rank[j] > rank[e] && bins(of_key((uint32_t)(s.rank[j] >> 20))) == f.bin_k;
+            in[e] = ahead < (uint32_t)how.k;
+            kept_k += in[e] ? mass[e] : 0;
+        }
+    }
+    if (how.p < 1.f) {
+        const double want = (double)how.p * (double)(f.before_k + sum_all(kept_k, s.sums));
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int i = threadIdx.x + e * kThreads;
+            if (i < n) s.mass[i] = in[e] && bin[e] >= f.p0 && bin[e] <= f.p1 ? mass[e] : 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if (!in[e]) continue;
+            uint64_t before = f.before_p;
+            for (int j = 0; j < n; ++j) before += s.rank[j] > rank[e] ? s.mass[j] : 0;
+            in[e] = bin[e] <= f.p1 && (double)before < want;
+        }
+    }
+    // the last rank that is kept, and the masses of the chunks
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.chunks; c += kThreads) s.mass[c] = a.chunk_mass[(int64_t)r * a.chunks + c];
+    if (threadIdx.x == 0) s.value[2] = ~0ull;
+    __syncthreads();
+    uint64_t cut = ~0ull, beyond = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if (in[e]) {
+            cut = rank[e] < cut ? rank[e] : cut;
+            const int place = kMostTokens - 1 - (int)((uint32_t)rank[e] & (kMostTokens - 1));
+            if (weight(of_key((uint32_t)(rank[e] >> 20))) >= how.least) atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[place / kChunk]), (unsigned long long)mass[e]);
+        } else if (rank[e] > beyond) {
+            beyond = rank[e];                                           // the best rank that is not kept
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint64_t c = __shfl_xor(cut, o), b = __shfl_xor(beyond, o);
+        cut = c < cut ? c : cut;
+        beyond = b > beyond ? b : beyond;
+    }
+    if ((threadIdx.x & 63) == 0) s.sums[threadIdx.x >> 6] = beyond;
+    if ((threadIdx.x & 63) == 0) s.rank[threadIdx.x >> 6] = cut;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) { cut = s.rank[w] < cut ? s.rank[w] : cut; beyond = s.sums[w] > beyond ? s.sums[w] : beyond; }
+    locate<T>(a, r, weight, how.least, cut == ~0ull ? beyond + 1 : cut, s.mass, s);
+}
+
+// Rows of one chunk or less, and everything at once.
+template <int T>
+__global__ __launch_bounds__(kThreads) void k_sample_whole(SampleArgs a) {
+    __shared__ Shared s;
+    whole_row<T>(a, blockIdx.x, Settings(a, blockIdx.x), s);
+}
+
+struct SampleWork { int64_t chunk_top, chunk_low, chunk_at, group_top, chunk_mass, bin_mass, bin_count, list, list_count, found, bytes; };
+SampleWork sample_work(int64_t rows, int32_t vocabulary) {
+    SampleWork w{};
+    if (vocabulary <= kChunk) return w;
+    if (rows > kSliceRows) rows = kSliceRows;
+    const int64_t chunks = (vocabulary + kChunk - 1) / kChunk;
+    int64_t at = 0;
+    auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
+    w.chunk_top = room(rows * chunks * 4);
+    w.chunk_low = room(rows * chunks * 4);
+    w.chunk_at = room(rows * chunks * 4);
+    w.group_top = room(rows * chunks * kGroups * 4);
+    w.chunk_mass = room(rows * chunks * 8);
+    w.bin_mass = room(rows * kBins * 8);
+    w.bin_count = room(rows * kBins * 4);
+    w.list = room(rows * kList * 8);
+    w.list_count = room(rows * 4);
+    w.found = room(rows * (int64_t)sizeof(RowBins));
+    w.bytes = at;
+    return w;
+}
+
+template <int T>
+hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st) {
+    if (a.vocabulary <= kChunk) {
+        k_sample_whole<T><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    a.chunks = (a.vocabulary + kChunk - 1) / kChunk;
+    a.chunk_top = reinterpret_cast<float*>(work + w.chunk_top);
+    a.chunk_low = reinterpret_cast<float*>(work + w.chunk_low);
+    a.group_top = reinterpret_cast<float*>(work + w.group_top);
+    a.chunk_at = reinterpret_cast<int32_t*>(work + w.chunk_at);
+    a.chunk_mass = reinterpret_cast<uint64_t*>(work + w.chunk_mass);
+    a.bin_mass = reinterpret_cast<uint64_t*>(work + w.bin_mass);
+    a.bin_count = reinterpret_cast<uint32_t*>(work + w.bin_count);
+    a.list = reinterpret_cast<uint64_t*>(work + w.list);
+    a.list_count = reinterpret_cast<uint32_t*>(work + w.list_count);
+    a.found = reinterpret_cast<RowBins*>(work + w.found);
+    // what the settings of all rows rule out is not launched
+    const bool k = a.how.top_k || (a.how.top_k_all > 1 && a.how.top_k_all < a.vocabulary), few = !a.how.top_k && k && a.how.top_k_all <= kFewRanks;
+    const bool top = (!a.how.temperature && a.how.temperature_all == 0.f) || (!a.how.top_k && a.how.top_k_all == 1) || (!a.how.top_p && a.how.top_p_all == 0.f);
+    const bool again = !top && !few, binned = again && (k || a.how.top_p || a.how.top_p_all < 1.f);
+    for (int64_t left = a.rows; left > 0; left -= kSliceRows) {
+        const unsigned rows = (unsigned)(left < kSliceRows ? left : kSliceRows), wgs = rows * (unsigned)a.chunks;
+        k_sample_tops<T><<<wgs, kChunkThreads, 0, st>>>(a);
+        if (again) k_sample_chunks<T><<<wgs, kChunkThreads, 0, st>>>(a);
+        k_sample_rows<T><<<rows, kThreads, 0, st>>>(a);
+        if (binned) {
+            k_sample_bins<T><<<wgs, kChunkThreads, 0, st>>>(a);
+            k_sample_cut<T><<<rows, kThreads, 0, st>>>(a);
+        }
+        if (hipError_t e = hipGetLastError()) return e;
+        a.logits += (int64_t)rows * a.row_stride * kSize<T>;
+        a.u += rows;
+        a.tokens += rows;
+        if (a.logprobs) a.logprobs += rows;
+        if (a.how.temperature) a.how.temperature += rows;
+        if (a.how.top_k) a.how.top_k += rows;
+        if (a.how.top_p) a.how.top_p += rows;
+        if (a.how.min_p) a.how.min_p += rows;
+    }
+    return hipSuccess;
 }
 
 ivftq_status refuse(ivftq_status code, const char* fmt, ...) {
@@ -301,10 +956,10 @@ using namespace ivftq;
 
 extern "C" {
 
-int64_t ivftq_sample_workspace(const ivftq_logits* logits) { return check_logits(logits) ? -1 : 0; }
+int64_t ivftq_sample_workspace(const ivftq_logits* logits) { return check_logits(logits) ? -1 : sample_work(logits->rows, logits->vocabulary).bytes; }
 
-ivftq_status ivftq_sample_tokens(const ivftq_logits* logits, const float* u, const ivftq_sampling* how, int32_t* tokens, float* logprobs, void*, int64_t,
-                                 void* stream) {
+ivftq_status ivftq_sample_tokens(const ivftq_logits* logits, const float* u, const ivftq_sampling* how, int32_t* tokens, float* logprobs, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
     if (ivftq_status e = check_logits(logits)) return e;
     if (!how) return refuse(IVFTQ_INVALID_ARG, "how is NULL");
     if (!how->temperature && !(how->temperature_all >= 0.f)) return refuse(IVFTQ_INVALID_ARG, "temperature = %g: 0 and above", (double)how->temperature_all);
@@ -316,15 +971,23 @@ ivftq_status ivftq_sample_tokens(const ivftq_logits* logits, const float* u, con
     if (!aligned(u, 4) || !aligned(tokens, 4) || !aligned(logprobs, 4) || !aligned(how->temperature, 4) || !aligned(how->top_k, 4) || !aligned(how->top_p, 4) ||
         !aligned(how->min_p, 4))
         return refuse(IVFTQ_INVALID_ARG, "u, tokens, logprobs and the arrays of settings are 4-byte aligned");
-    const SampleArgs a{static_cast<const char*>(logits->data), logits->row_stride, u, *how, tokens, logprobs, logits->vocabulary, (int32_t)logits->rows};
+    const SampleWork w = sample_work(logits->rows, logits->vocabulary);
+    if (w.bytes && (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)))
+        return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)workspace_bytes, (long long)w.bytes);
+    SampleArgs a{};
+    a.logits = static_cast<const char*>(logits->data);
+    a.row_stride = logits->row_stride;
+    a.u = u;
+    a.how = *how;
+    a.tokens = tokens;
+    a.logprobs = logprobs;
+    a.vocabulary = logits->vocabulary;
+    a.rows = (int32_t)logits->rows;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const unsigned rows = (unsigned)logits->rows;
-    switch (logits->type) {
-        case IVFTQ_LOGITS_F16: k_sample<IVFTQ_LOGITS_F16><<<rows, kThreads, 0, st>>>(a); break;
-        case IVFTQ_LOGITS_BF16: k_sample<IVFTQ_LOGITS_BF16><<<rows, kThreads, 0, st>>>(a); break;
-        default: k_sample<IVFTQ_LOGITS_F32><<<rows, kThreads, 0, st>>>(a); break;
-    }
-    const hipError_t e = hipGetLastError();
+    char* work = static_cast<char*>(workspace);
+    const hipError_t e = logits->type == IVFTQ_LOGITS_F16    ? sample<IVFTQ_LOGITS_F16>(a, w, work, st)
+                         : logits->type == IVFTQ_LOGITS_BF16 ? sample<IVFTQ_LOGITS_BF16>(a, w, work, st)
+                                                             : sample<IVFTQ_LOGITS_F32>(a, w, work, st);
     return e == hipSuccess ? IVFTQ_OK : refuse(IVFTQ_HIP_ERROR, "ivftq_sample_tokens: %s", hipGetErrorString(e));
 }
 

@@ -153,3 +153,28 @@ def test_equal_calls_give_equal_tokens():
     s = _pkg().sample_tokens(x, u, top_p=0.97, logprobs=a)
     t = _pkg().sample_tokens(x, u, top_p=0.97, logprobs=b)
     assert torch.equal(s, t) and torch.equal(a, b) and math.isfinite(float(a.sum()))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("v", (4096, 4097, 9000, 70_001))
+def test_long_lists(kind, v):
+    """Logits so close together that thousands fall between two ranks that have to be told apart, ranks at the ends of lists, masked tokens."""
+    g = torch.Generator().manual_seed(v)
+    x = torch.stack([torch.rand(v, generator=g) * 1e-2, 5 + torch.rand(v, generator=g), torch.where(torch.rand(v, generator=g) < 0.01, torch.randn(v, generator=g), -torch.inf),
+                     torch.randn(v, generator=g) * 100, torch.cat([torch.full((1,), 30.0), torch.randn(v - 1, generator=g)]), torch.arange(v) * 1e-3]).to(TYPES[kind])
+    u = np.linspace(0.01, 0.99, 6).astype(np.float32)
+    for how in (dict(top_k=255), dict(top_k=256), dict(top_k=257), dict(top_k=3000), dict(top_k=v - 1), dict(top_p=0.3), dict(top_p=0.99), dict(top_k=2000, top_p=0.6),
+                dict(top_k=300, top_p=0.999, min_p=0.2), dict(temperature=100.0, top_p=0.5), dict(temperature=0.01, top_p=0.9, top_k=500), dict(min_p=0.9),
+                dict(temperature=1e6, top_k=1000), dict(temperature=1e-6, top_k=v // 2, top_p=0.5)):
+        check(x, u, **how)
+
+
+def test_more_rows_than_share_a_workspace():
+    rows, v = 2500, 5000
+    x = logits(12, rows, v, "bf16")
+    r = np.random.default_rng(1)
+    check(x, r.random(rows, np.float32), temperature=r.choice([0.0, 0.8, 1.0], rows), top_k=r.choice([0, 20, 600], rows), top_p=r.choice([0.9, 1.0], rows),
+          min_p=r.choice([0.0, 0.02], rows))
+    u = np.float32(0.4) * np.ones(rows, np.float32)
+    check(x, u, top_k=30)
+    check(x, u, top_p=0.8)
