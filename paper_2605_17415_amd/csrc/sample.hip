@@ -20,6 +20,7 @@
 
 #include "../../include/ivftq_sample.h"
 #include "kernels.h"
+#include "wave_ops.h"
 
 namespace ivftq {
 
@@ -141,30 +142,48 @@ __device__ __forceinline__ double exp64(double x) {
     return __builtin_ldexp(p, (int)n);
 }
 
-// Weights of a row.
+// Weights of a row: 2^(t / 64) for t = 64 log2(e) (x - top) / temperature, the whole 64ths from a table of 2^(j / 64) in LDS, the rest, at most half a
+// 64th, by the series up to its fifth power (2^-54).
+__device__ __forceinline__ void fill_table(double* table) {
+    if (threadIdx.x < 64) table[threadIdx.x] = threadIdx.x ? 2.0 * exp64((double)((int)threadIdx.x - 64) * (0.69314718055994530942 / 64)) : 1.0;
+    __syncthreads();
+}
 struct Weights {
     float top;
-    double by;                                   // 1 / temperature
+    double first, by;
+    const double* table;
+    __device__ __forceinline__ Weights(float top_, float temperature, const double* table_) : top(top_), first((double)top_), by(92.332482616893656 / (double)temperature), table(table_) {}
+    // top is finite.  -infinity: 2^-64, no mass
     __device__ __forceinline__ double operator()(float v) const {
-        if (v == top) return 1.0;                // both may be infinite
-        return v == -INFINITY || top == INFINITY ? 0.0 : exp64(((double)v - (double)top) * by);
+        constexpr double c = 0.69314718055994530942 / 64, shift = 6755399441055744.0;        // 1.5 * 2^52: sums with it end in a whole number's bits
+        const double t = __builtin_fmax(((double)v - first) * by, -4096.0), n = t + shift, r = t - (n - shift);
+        double p = c * c * c * c * c / 120;
+        p = __builtin_fma(p, r, c * c * c * c / 24);
+        p = __builtin_fma(p, r, c * c * c / 6);
+        p = __builtin_fma(p, r, c * c / 2);
+        p = __builtin_fma(p, r, c);
+        p = __builtin_fma(p, r, 1.0);
+        const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, n);
+        const uint64_t w = __builtin_bit_cast(uint64_t, table[k & 63] * p);
+        return __builtin_bit_cast(double, w + ((uint64_t)(uint32_t)(k >> 6) << 52));
     }
     __device__ __forceinline__ uint64_t mass(float v) const { return whole((*this)(v)); }
     // to a whole number of 2^-42: the last bits of a number of 2^52
     static __device__ __forceinline__ uint64_t whole(double w) { return __builtin_bit_cast(uint64_t, __builtin_fma(w, kUnit, 4503599627370496.0)) & ((1ull << 52) - 1); }
 };
+// The same where the largest logit may be infinite.
+struct AnyWeights : Weights {
+    using Weights::Weights;
+    __device__ __forceinline__ double operator()(float v) const { return v == top ? 1.0 : (top == INFINITY ? 0.0 : Weights::operator()(v)); }
+    __device__ __forceinline__ uint64_t mass(float v) const { return whole((*this)(v)); }
+};
+// A share of a mass: the tokens that less than it comes before are those that less than this whole number does.
+__device__ __forceinline__ uint64_t share_of(float p, uint64_t mass) { return (uint64_t)__builtin_ceil((double)p * (double)mass); }
 
-template <class T>
-__device__ __forceinline__ T wave_scan(T v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const T u = __shfl_up(v, o); if (lane >= o) v += u; }
-    return v;
-}
 // Sum over the threads up to this one; all: over all threads.  sums: kWaves numbers in LDS.
 template <class T>
 __device__ __forceinline__ T scan(T v, T* sums, T& all) {
-    const T incl = wave_scan(v);
+    const T incl = lanes_upto(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = incl;
     __syncthreads();
@@ -179,12 +198,13 @@ struct Shared {
     uint64_t sums[kWaves], bins[256], blocks[kMostTokens / kBlock];
     uint32_t most[kWaves], digit;
     uint64_t above;
+    double table[64];
 };
 
 // Digits of the keys, most significant first: the key at which sum(amount of larger keys) < want <= sum(amount of keys not smaller), and
 // the first of the two sums.  Keys under `least` are left out.
 template <int T, class Amount>
-__device__ __forceinline__ uint32_t find_key(const char* row, int n, uint32_t least, double want, Shared& s, uint64_t& above, Amount amount) {
+__device__ __forceinline__ uint32_t find_key(const char* row, int n, uint32_t least, uint64_t want, Shared& s, uint64_t& above, Amount amount) {
     uint32_t prefix = 0;
     above = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -203,7 +223,7 @@ __device__ __forceinline__ uint32_t find_key(const char* row, int n, uint32_t le
         const uint64_t mine = threadIdx.x < 256 ? s.bins[255 - threadIdx.x] : 0;
         uint64_t all;
         const uint64_t upto = above + scan(mine, s.sums, all), before = upto - mine;
-        if (mine && (double)before < want && (double)upto >= want) { s.digit = 255 - threadIdx.x; s.above = before; }
+        if (mine && before < want && upto >= want) { s.digit = 255 - threadIdx.x; s.above = before; }
         __syncthreads();
         prefix = prefix << 8 | s.digit;
         above = s.above;
@@ -235,6 +255,7 @@ __device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Share
     const int n = a.vocabulary, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
     __syncthreads();
+    fill_table(s.table);
 
     // the largest logit and its first place
     uint32_t best = 0;
@@ -243,19 +264,16 @@ __device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Share
         const uint32_t k = key_of(logit<T>(row, i));
         if (k > best) { best = k; at = i; }
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t k = __shfl_xor(best, o);
-        const int i = __shfl_xor(at, o);
-        if (k > best || (k == best && i < at)) { best = k; at = i; }
-    }
+    const uint32_t mine_best = best;
+    best = lanes64(best, Larger());
+    at = lanes64(mine_best == best ? at : n, Smaller());
     if (lane == 0) { s.most[wave] = best; s.sums[wave] = (uint64_t)at; }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
         if (s.most[w] > best || (s.most[w] == best && (int)s.sums[w] < at)) { best = s.most[w]; at = (int)s.sums[w]; }
     __syncthreads();
-    const Weights weight{of_key(best), 1.0 / (double)how.temperature};
+    const AnyWeights weight(of_key(best), how.temperature, s.table);
     if (weight.top == -INFINITY || how.way == kTop) {
         top_token(a, r, weight.top, at);
         return;
@@ -265,7 +283,7 @@ __device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Share
     uint32_t cut = 0;
     uint64_t ties = ~0ull, above = 0;
     if (how.k) {
-        cut = find_key<T>(row, n, 0, (double)how.k, s, above, [](float) { return (uint64_t)1; });
+        cut = find_key<T>(row, n, 0, (uint64_t)how.k, s, above, [](float) { return (uint64_t)1; });
         ties = (uint64_t)how.k - above;
     }
     if (how.p < 1.f) {
@@ -276,13 +294,11 @@ __device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Share
         }
         scan(mass, s.sums, all);
         if (ties != ~0ull) all += ties * weight.mass(of_key(cut));
-        const double want = (double)how.p * (double)all;             // above zero
+        const uint64_t want = share_of(how.p, all);
         const uint32_t key = find_key<T>(row, n, cut, want, s, above, [&](float v) { return weight.mass(v); });
         const uint64_t one = weight.mass(of_key(key));
         // rank i of its equals is kept where above + i * one < want
-        uint64_t i = (uint64_t)((want - (double)above) / (double)one);
-        while (i > 0 && !((double)(above + (i - 1) * one) < want)) --i;
-        while ((double)(above + i * one) < want) ++i;
+        const uint64_t i = (want - above + one - 1) / one;
         ties = key == cut && i > ties ? ties : i;
         cut = key;
     }
@@ -324,8 +340,7 @@ __device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Share
         uint64_t mass = 0;
         double w;
         for (int i = b * kBlock + lane; i < (b + 1) * kBlock && i < n; i += 64) mass += kept(i, w);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) mass += __shfl_xor(mass, o);
+        mass = lanes64(mass, Sum());
         if (lane == 0) s.blocks[b] = mass;
     }
     __syncthreads();
@@ -347,15 +362,6 @@ __device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Share
 constexpr int kChunkThreads = 256;
 constexpr int kEach = kChunk / kChunkThreads / 8;         // a thread's pieces of eight tokens
 
-__device__ __forceinline__ float lane_max(float v, int width) {
-    for (int o = 1; o < width; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ float lane_min(float v, int width) {
-    for (int o = 1; o < width; o <<= 1) v = fminf(v, __shfl_xor(v, o));
-    return v;
-}
-
 // The first reading: 4,096 tokens a workgroup, bound by memory.
 template <int T>
 __global__ __launch_bounds__(kChunkThreads) void k_sample_tops(SampleArgs a) {
@@ -369,40 +375,41 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_tops(SampleArgs a) {
     for (int j = 0; j < kEach; ++j) logits_of<T, 8>(row, chunk * kChunk + (j * kChunkThreads + threadIdx.x) * 8, n, v[j]);
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        float most = -INFINITY;
+        float most = v[j][0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            most = fmaxf(most, v[j][e]);
-            low = v[j][e] > -INFINITY ? fminf(low, v[j][e]) : low;
-        }
+        for (int e = 1; e < 8; ++e) most = fmaxf(most, v[j][e]);
         top = fmaxf(top, most);
         if (how.way == kFew) {
-            most = lane_max(most, 8);
+            most = lanes8(most, Larger());
             if ((lane & 7) == 0) a.group_top[((int64_t)r * a.chunks + chunk) * kGroups + (j * kChunkThreads + threadIdx.x) / 8] = most;
         }
     }
-    top = lane_max(top, 64);
-    low = lane_min(low, 64);
+    if (how.way == kBinned) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) low = v[j][e] > -INFINITY ? fminf(low, v[j][e]) : low;
+        low = lanes64(low, Smaller());
+    }
+    top = lanes64(top, Larger());
     if (lane == 0) { tops[wave] = top; lows[wave] = low; }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 4; ++w) { top = fmaxf(top, tops[w]); low = fminf(low, lows[w]); }
-    int at = n;
+    const int64_t to = (int64_t)r * a.chunks + chunk;
+    if (threadIdx.x == 0) { a.chunk_top[to] = top; a.chunk_low[to] = low; }
+    if (how.way == kTop) {
+        int at = n;
 #pragma unroll
-    for (int j = kEach - 1; j >= 0; --j)
+        for (int j = kEach - 1; j >= 0; --j)
 #pragma unroll
-        for (int e = 7; e >= 0; --e) at = v[j][e] == top ? chunk * kChunk + (j * kChunkThreads + (int)threadIdx.x) * 8 + e : at;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const int other = __shfl_xor(at, o); at = other < at ? other : at; }
-    if (lane == 0) places[wave] = at;
-    __syncthreads();
-    if (threadIdx.x == 0) {
+            for (int e = 7; e >= 0; --e) at = v[j][e] == top ? chunk * kChunk + (j * kChunkThreads + (int)threadIdx.x) * 8 + e : at;
+        at = lanes64(at, Smaller());
+        if (lane == 0) places[wave] = at;
+        __syncthreads();
 #pragma unroll
         for (int w = 0; w < 4; ++w) at = places[w] < at ? places[w] : at;
-        const int64_t to = (int64_t)r * a.chunks + chunk;
-        a.chunk_top[to] = top;
-        a.chunk_low[to] = low;
-        a.chunk_at[to] = at;
+        if (threadIdx.x == 0) a.chunk_at[to] = at;
     }
     if (how.way == kBinned) {                             // what the next readings add to
         for (int i = chunk * kChunkThreads + threadIdx.x; i < kBins; i += a.chunks * kChunkThreads) {
@@ -413,34 +420,23 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_tops(SampleArgs a) {
     }
 }
 
-// A row's largest logit, its first place, the lowest one above -infinity, from those of its chunks; by the whole workgroup (W wavefronts).
-struct RowTop { float top, low; int at; };
+// A row's largest logit and the lowest one above -infinity (ways that need it), from those of its chunks; by the whole workgroup (W wavefronts).
+struct RowTop { float top, low; };
 template <int W>
 __device__ __forceinline__ RowTop row_top(const SampleArgs& a, int r) {
     __shared__ float tops[W], lows[W];
-    __shared__ int places[W];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    RowTop x{-INFINITY, INFINITY, kMostTokens};
+    RowTop x{-INFINITY, INFINITY};
     for (int c = threadIdx.x; c < a.chunks; c += W * 64) {
-        const int64_t from = (int64_t)r * a.chunks + c;
-        const float top = a.chunk_top[from];
-        if (top > x.top || x.at == kMostTokens) { x.top = top; x.at = a.chunk_at[from]; }
-        x.low = fminf(x.low, a.chunk_low[from]);
+        x.top = fmaxf(x.top, a.chunk_top[(int64_t)r * a.chunks + c]);
+        x.low = fminf(x.low, a.chunk_low[(int64_t)r * a.chunks + c]);
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const float top = __shfl_xor(x.top, o);
-        const int at = __shfl_xor(x.at, o);
-        if (top > x.top || (top == x.top && at < x.at)) { x.top = top; x.at = at; }
-        x.low = fminf(x.low, __shfl_xor(x.low, o));
-    }
-    if (lane == 0) { tops[wave] = x.top; lows[wave] = x.low; places[wave] = x.at; }
+    x.top = lanes64(x.top, Larger());
+    x.low = lanes64(x.low, Smaller());
+    if (lane == 0) { tops[wave] = x.top; lows[wave] = x.low; }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        if (tops[w] > x.top || (tops[w] == x.top && places[w] < x.at)) { x.top = tops[w]; x.at = places[w]; }
-        x.low = fminf(x.low, lows[w]);
-    }
+    for (int w = 0; w < W; ++w) { x.top = fmaxf(x.top, tops[w]); x.low = fminf(x.low, lows[w]); }
     return x;
 }
 
@@ -464,6 +460,7 @@ __device__ __forceinline__ Bins row_bins(const RowTop& x, const Settings& how) {
 // The second reading: chunks' masses, or the masses and numbers of the bins.
 template <int T>
 __global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
+    __shared__ double table[64];
     __shared__ uint64_t mass[kBins], sums[4];
     __shared__ uint32_t count[kBins];
     const int r = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, n = a.vocabulary;
@@ -475,7 +472,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
     for (int j = 0; j < kEach; ++j) logits_of<T, 8>(row, chunk * kChunk + (j * kChunkThreads + threadIdx.x) * 8, n, v[j]);
     const RowTop x = row_top<4>(a, r);
     if (!(__builtin_fabsf(x.top) < INFINITY)) return;                  // one workgroup takes the row whole
-    const Weights weight{x.top, 1.0 / (double)how.temperature};
+    fill_table(table);
+    const Weights weight(x.top, how.temperature, table);
     if (how.way == kAll) {
         uint64_t sum = 0;
 #pragma unroll
@@ -485,8 +483,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
                 const double w = weight(v[j][e]);
                 sum += w >= how.least ? Weights::whole(w) : 0;
             }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        sum = lanes64(sum, Sum());
         if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
         __syncthreads();
         if (threadIdx.x == 0) a.chunk_mass[(int64_t)r * a.chunks + chunk] = sums[0] + sums[1] + sums[2] + sums[3];
@@ -517,6 +514,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
 // The third reading: the masses of the chunks' tokens that are kept for certain, and the tokens whose ranks have to be counted.
 template <int T>
 __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
+    __shared__ double table[64];
     __shared__ uint64_t sums[4];
     __shared__ uint32_t many, begin;
     const int r = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, n = a.vocabulary;
@@ -529,7 +527,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
     if (threadIdx.x == 0) many = 0;
     const RowTop x = row_top<4>(a, r);
     if (!(__builtin_fabsf(x.top) < INFINITY)) return;
-    const Weights weight{x.top, 1.0 / (double)how.temperature};
+    fill_table(table);
+    const Weights weight(x.top, how.temperature, table);
     const Bins bins = row_bins(x, how);
     const RowBins f = a.found[r];
     uint64_t sum = 0;
@@ -546,8 +545,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
                 open |= 1u << (8 * j + e);
             }
         }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    sum = lanes64(sum, Sum());
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
     uint32_t at = open ? atomicAdd(&many, (uint32_t)__popc(open)) : 0;
     __syncthreads();
@@ -570,16 +568,72 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
 // ---- rows --------------------------------------------------------------------------------------------------------------
 
 struct ListShared {
-    uint64_t rank[kList], mass[kList];             // of the list's tokens
-    uint64_t sums[kWaves];
-    uint64_t value[4];
-    uint32_t many;
-    uint32_t bins[1024];
+    uint64_t bins[1024], sums[kWaves], value[4];
+    uint64_t mass[kMostTokens / kChunk];           // of chunks
+    uint64_t rank[kList];                          // the list's tokens
+    uint32_t counts[1024], many;
     int groups[kList];
+    double table[64];
 };
 
-// Sum over all threads.
-__device__ __forceinline__ uint64_t sum_all(uint64_t v, uint64_t* sums) { uint64_t all; scan(v, sums, all); return all; }
+// Over all threads.
+template <class T, class Op>
+__device__ __forceinline__ T all_threads(T v, uint64_t* sums, Op op) {
+    T* at = reinterpret_cast<T*>(sums);
+    v = lanes64(v, op);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
+    __syncthreads();
+    T all = at[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = op(all, at[w]);
+    return all;
+}
+
+// Of the tokens that have an amount, ordered by `by` (all different, the largest first), the one at which the sum reaches `want`: ten bits of `by`
+// at a time, from bit `high` on, until one token is left.  Each thread holds two.
+constexpr int kHeld = kList / kThreads;
+__device__ __forceinline__ uint64_t find_rank(const uint64_t (&by)[kHeld], const uint64_t (&amount)[kHeld], int high, uint64_t before, uint64_t want, ListShared& s) {
+    uint32_t open = 0;
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e) open |= amount[e] ? 1u << e : 0;
+    int past = high + 1;                             // bits from this one on are alike
+    while (true) {
+        const int shift = past > 10 ? past - 10 : 0;
+        const uint32_t mask = (1u << (past - shift)) - 1;
+        __syncthreads();
+        s.bins[threadIdx.x] = 0;
+        s.counts[threadIdx.x] = 0;
+        if (threadIdx.x == 0) { s.value[0] = 0; s.value[1] = before; s.value[2] = 1; }
+        __syncthreads();
+        uint32_t digit[kHeld];
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) {
+            digit[e] = mask - ((uint32_t)(by[e] >> shift) & mask);           // the largest first
+            if (open >> e & 1) {
+                atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[digit[e]]), (unsigned long long)amount[e]);
+                atomicAdd(&s.counts[digit[e]], 1u);
+            }
+        }
+        __syncthreads();
+        uint64_t all;
+        const uint64_t mine = s.bins[threadIdx.x], upto = before + scan(mine, s.sums, all);
+        if (mine && upto >= want && upto - mine < want) { s.value[0] = threadIdx.x; s.value[1] = upto - mine; s.value[2] = s.counts[threadIdx.x]; }
+        __syncthreads();
+        const uint32_t found = (uint32_t)s.value[0];
+        before = s.value[1];
+        const bool last = s.value[2] <= 1 || shift == 0;
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) open &= digit[e] == found ? ~0u : ~(1u << e);
+        if (last) break;
+        past = shift;
+    }
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+        if (open >> e & 1) s.value[3] = by[e];
+    __syncthreads();
+    return s.value[3];
+}
 
 // The token among those of rank `cut` and better, by the masses of the chunks (in `mass`, a number a chunk).
 template <int T>
@@ -618,21 +672,17 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     // the bin of the k-th largest group maximum
     float low = INFINITY;
     for (int g = threadIdx.x; g < groups; g += kThreads) { const float t = tops[g]; low = t > -INFINITY ? fminf(low, t) : low; }
-    low = lane_min(low, 64);
-    if (lane == 0) s.sums[threadIdx.x >> 6] = __builtin_bit_cast(uint32_t, low);
-    s.bins[threadIdx.x] = 0;
+    s.counts[threadIdx.x] = 0;
     if (threadIdx.x == 0) { s.many = 0; s.value[0] = 1023; }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) low = fminf(low, __builtin_bit_cast(float, (uint32_t)s.sums[w]));
+    low = all_threads(low, s.sums, Smaller());
     const Bins bins(x.top, low, INFINITY, 1024);
     for (int g = threadIdx.x; g < groups; g += kThreads) {
         const float t = tops[g];
-        if (t > -INFINITY) atomicAdd(&s.bins[bins(t)], 1u);
+        if (t > -INFINITY) atomicAdd(&s.counts[bins(t)], 1u);
     }
     __syncthreads();
     uint64_t all;
-    const uint64_t mine = s.bins[threadIdx.x], upto = scan(mine, s.sums, all);
+    const uint64_t mine = s.counts[threadIdx.x], upto = scan(mine, s.sums, all);
     if (upto >= (uint64_t)how.k && upto - mine < (uint64_t)how.k) { s.value[0] = threadIdx.x; s.value[1] = upto; }
     if (threadIdx.x == 1023 && upto < (uint64_t)how.k) s.value[1] = upto;
     __syncthreads();
@@ -656,46 +706,37 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
         uint32_t begin = 0;
         if (lane == 0) begin = atomicAdd(&s.many, (uint32_t)__popcll(which));
         const uint32_t at = __shfl(begin, 0) + (uint32_t)__popcll(which & ((1ull << lane) - 1));
-        if (in && at < kList) { s.rank[at] = rank_of(v, i); s.mass[at] = weight.mass(v); }
+        if (in && at < kList) s.rank[at] = rank_of(v, i);
     }
     __syncthreads();
     const int n = (int)s.many;
     if (n > kList) return false;
-    // ranks, and the mass before each, counted
-    uint64_t rank[2], mass[2], before[2] = {0, 0};
-    uint32_t ahead[2] = {0, 0};
+    uint64_t rank[kHeld], amount[kHeld], place[kHeld], mixed = 0, sum = 0;
+    double w[kHeld];
+    const uint64_t any = s.rank[0];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < kHeld; ++e) {
         const int i = threadIdx.x + e * kThreads;
-        rank[e] = i < n ? s.rank[i] : 0;
-        mass[e] = i < n ? s.mass[i] : 0;
-        if (i < n)
-            for (int j = 0; j < n; ++j) {
-                const bool better = s.rank[j] > rank[e];
-                ahead[e] += better;
-                before[e] += better ? s.mass[j] : 0;
-            }
+        rank[e] = i < n ? s.rank[i] : any;
+        amount[e] = i < n;
+        w[e] = i < n ? weight(of_key((uint32_t)(rank[e] >> 20))) : 0.0;
+        place[e] = rank[e] & (kMostTokens - 1);
+        mixed |= rank[e] ^ any;
     }
-    const uint64_t total = sum_all((ahead[0] < (uint32_t)how.k ? mass[0] : 0) + (ahead[1] < (uint32_t)how.k ? mass[1] : 0), s.sums);
-    const double want = (double)how.p * (double)total;
-    __syncthreads();
+    mixed = all_threads(mixed, s.sums, Union());
+    const int high = 63 - __builtin_clzll(mixed | 1);
+    uint64_t cut = n > how.k ? find_rank(rank, amount, high, 0, (uint64_t)how.k, s) : 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int i = threadIdx.x + e * kThreads;
-        const bool in = i < n && ahead[e] < (uint32_t)how.k && (how.p == 1.f || (double)before[e] < want) && weight(of_key((uint32_t)(rank[e] >> 20))) >= how.least;
-        mass[e] = in ? mass[e] : 0;
-        if (i < n) s.mass[i] = mass[e];
-    }
-    const uint64_t kept = sum_all(mass[0] + mass[1], s.sums), target = target_of(a.u[r], kept);
-    // the first token up to which the masses pass the target: in the order of the tokens
+    for (int e = 0; e < kHeld; ++e) sum += amount[e] = amount[e] && rank[e] >= cut ? Weights::whole(w[e]) : 0;
+    if (how.p < 1.f) cut = find_rank(rank, amount, high, 0, share_of(how.p, all_threads(sum, s.sums, Sum())), s);
+    // of what is kept, in the order of the tokens, the first up to which the mass passes the target
+    sum = 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (!mass[e]) continue;
-        const uint32_t place = (uint32_t)rank[e] & (kMostTokens - 1);
-        uint64_t earlier = 0;
-        for (int j = 0; j < n; ++j) earlier += ((uint32_t)s.rank[j] & (kMostTokens - 1)) > place ? s.mass[j] : 0;
-        if (earlier <= target && earlier + mass[e] > target) drawn(a, r, kMostTokens - 1 - (int)place, weight(of_key((uint32_t)(rank[e] >> 20))), kept);
-    }
+    for (int e = 0; e < kHeld; ++e) sum += amount[e] = rank[e] >= cut && w[e] >= how.least ? amount[e] : 0;
+    const uint64_t kept = all_threads(sum, s.sums, Sum()), found = find_rank(place, amount, 19, 0, target_of(a.u[r], kept) + 1, s);
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+        if (amount[e] && place[e] == found) drawn(a, r, kMostTokens - 1 - (int)found, w[e], kept);
     return true;
 }
 
@@ -728,15 +769,15 @@ __device__ __forceinline__ RowBins look_up(const SampleArgs& a, int r, const Set
         __syncthreads();
     }
     if (how.p < 1.f) {                                 // the mass of the ranks that top_k leaves is before_k to before_k + in_k
-        const double low = (double)how.p * (double)f.before_k, high = (double)how.p * (double)(f.before_k + in_k);
+        const uint64_t low = share_of(how.p, f.before_k), high = share_of(how.p, f.before_k + in_k);
         if (threadIdx.x == 0) { s.value[0] = 0; s.value[1] = 0; s.value[2] = f.bin_k < kBins ? f.bin_k : kBins - 1; }
         __syncthreads();
         const uint64_t m[2] = {m0, m1};
         uint64_t before = mass;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            if ((double)before < low && (double)(before + m[e]) >= low) { s.value[0] = 2 * threadIdx.x + e; s.value[1] = before; }
-            if ((double)before < high && (double)(before + m[e]) >= high) s.value[2] = 2 * threadIdx.x + e;
+            if (before < low && before + m[e] >= low) { s.value[0] = 2 * threadIdx.x + e; s.value[1] = before; }
+            if (before < high && before + m[e] >= high) s.value[2] = 2 * threadIdx.x + e;
             before += m[e];
         }
         __syncthreads();
@@ -755,16 +796,23 @@ __global__ __launch_bounds__(kThreads) void k_sample_rows(SampleArgs a) {
     const Settings how(a, r);
     const RowTop x = row_top<kWaves>(a, r);
     if (x.top == -INFINITY || how.way == kTop) {
-        top_token(a, r, x.top, x.at);
+        int at = a.vocabulary;
+        if (how.way == kTop)
+            for (int c = threadIdx.x; c < a.chunks; c += kThreads)
+                if (a.chunk_top[(int64_t)r * a.chunks + c] == x.top) at = min(at, a.chunk_at[(int64_t)r * a.chunks + c]);
+        top_token(a, r, x.top, all_threads(at, s.list.sums, Smaller()));
         return;
     }
-    const Weights weight{x.top, 1.0 / (double)how.temperature};
     bool done = x.top < INFINITY;
-    if (done && how.way == kFew) done = few_ranks<T>(a, r, how, x, weight, s.list);
-    else if (done && how.way == kAll) locate<T>(a, r, weight, how.least, 0, a.chunk_mass + (int64_t)r * a.chunks, s.list);
-    else if (done) {
-        const RowBins f = look_up(a, r, how, s.list);
-        if (threadIdx.x == 0) a.found[r] = f;
+    if (done) {
+        fill_table(s.list.table);
+        const Weights weight(x.top, how.temperature, s.list.table);
+        if (how.way == kFew) done = few_ranks<T>(a, r, how, x, weight, s.list);
+        else if (how.way == kAll) locate<T>(a, r, weight, how.least, 0, a.chunk_mass + (int64_t)r * a.chunks, s.list);
+        else {
+            const RowBins f = look_up(a, r, how, s.list);
+            if (threadIdx.x == 0) a.found[r] = f;
+        }
     }
     if (!done) whole_row<T>(a, r, how, s.whole);
 }
@@ -784,76 +832,49 @@ __global__ __launch_bounds__(kThreads) void k_sample_cut(SampleArgs a) {
         whole_row<T>(a, r, how, shared.whole);
         return;
     }
-    const Weights weight{x.top, 1.0 / (double)how.temperature};
+    fill_table(s.table);
+    const Weights weight(x.top, how.temperature, s.table);
     const Bins bins = row_bins(x, how);
     const RowBins f = a.found[r];
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        s.rank[i] = a.list[(int64_t)r * kList + i];
-        s.mass[i] = weight.mass(of_key((uint32_t)(s.rank[i] >> 20)));
-    }
-    __syncthreads();
-    uint64_t rank[2], mass[2], kept_k = 0;
-    int bin[2];
-    bool in[2];
+    const uint64_t* list = a.list + (int64_t)r * kList;
+    const uint64_t any = n ? list[0] : 0;
+    uint64_t rank[kHeld], mass[kHeld], amount[kHeld], mixed = 0, cut = 0;
+    int bin[kHeld];
+    double w[kHeld];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < kHeld; ++e) {
         const int i = threadIdx.x + e * kThreads;
-        in[e] = i < n;
-        rank[e] = in[e] ? s.rank[i] : 0;
-        mass[e] = in[e] ? s.mass[i] : 0;
-        bin[e] = in[e] ? bins(of_key((uint32_t)(rank[e] >> 20))) : kBins + 1;
-        if (f.bin_k < kBins && in[e] && bin[e] >= f.bin_k) {          // ranks within top_k's last bin
-            uint32_t ahead = f.count_k;
-            for (int j = 0; j < n; ++j) ahead += s.rank[j] > rank[e] && bins(of_key((uint32_t)(s.rank[j] >> 20))) == f.bin_k;
-            in[e] = ahead < (uint32_t)how.k;
-            kept_k += in[e] ? mass[e] : 0;
-        }
+        rank[e] = i < n ? list[i] : any;
+        const float v = of_key((uint32_t)(rank[e] >> 20));
+        bin[e] = i < n ? bins(v) : kBins + 1;
+        w[e] = i < n ? weight(v) : 0.0;
+        mass[e] = i < n ? Weights::whole(w[e]) : 0;
+        mixed |= rank[e] ^ any;
+    }
+    for (int c = threadIdx.x; c < a.chunks; c += kThreads) s.mass[c] = a.chunk_mass[(int64_t)r * a.chunks + c];
+    mixed = all_threads(mixed, s.sums, Union());
+    const int high = 63 - __builtin_clzll(mixed | 1);
+    uint64_t in_k = 0;
+    if (f.bin_k < kBins) {
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) amount[e] = bin[e] == f.bin_k;
+        cut = find_rank(rank, amount, high, f.count_k, (uint64_t)how.k, s);
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) in_k += bin[e] == f.bin_k && rank[e] >= cut ? mass[e] : 0;
     }
     if (how.p < 1.f) {
-        const double want = (double)how.p * (double)(f.before_k + sum_all(kept_k, s.sums));
-        __syncthreads();
+        const uint64_t all = f.bin_k < kBins ? f.before_k + all_threads(in_k, s.sums, Sum()) : f.total;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int i = threadIdx.x + e * kThreads;
-            if (i < n) s.mass[i] = in[e] && bin[e] >= f.p0 && bin[e] <= f.p1 ? mass[e] : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if (!in[e]) continue;
-            uint64_t before = f.before_p;
-            for (int j = 0; j < n; ++j) before += s.rank[j] > rank[e] ? s.mass[j] : 0;
-            in[e] = bin[e] <= f.p1 && (double)before < want;
-        }
+        for (int e = 0; e < kHeld; ++e) amount[e] = bin[e] >= f.p0 && bin[e] <= f.p1 && rank[e] >= cut ? mass[e] : 0;
+        cut = find_rank(rank, amount, high, f.before_p, share_of(how.p, all), s);
     }
-    // the last rank that is kept, and the masses of the chunks
-    __syncthreads();
-    for (int c = threadIdx.x; c < a.chunks; c += kThreads) s.mass[c] = a.chunk_mass[(int64_t)r * a.chunks + c];
-    if (threadIdx.x == 0) s.value[2] = ~0ull;
-    __syncthreads();
-    uint64_t cut = ~0ull, beyond = 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (in[e]) {
-            cut = rank[e] < cut ? rank[e] : cut;
+    for (int e = 0; e < kHeld; ++e)
+        if (mass[e] && rank[e] >= cut && w[e] >= how.least) {
             const int place = kMostTokens - 1 - (int)((uint32_t)rank[e] & (kMostTokens - 1));
-            if (weight(of_key((uint32_t)(rank[e] >> 20))) >= how.least) atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[place / kChunk]), (unsigned long long)mass[e]);
-        } else if (rank[e] > beyond) {
-            beyond = rank[e];                                           // the best rank that is not kept
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[place / kChunk]), (unsigned long long)mass[e]);
         }
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t c = __shfl_xor(cut, o), b = __shfl_xor(beyond, o);
-        cut = c < cut ? c : cut;
-        beyond = b > beyond ? b : beyond;
-    }
-    if ((threadIdx.x & 63) == 0) s.sums[threadIdx.x >> 6] = beyond;
-    if ((threadIdx.x & 63) == 0) s.rank[threadIdx.x >> 6] = cut;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) { cut = s.rank[w] < cut ? s.rank[w] : cut; beyond = s.sums[w] > beyond ? s.sums[w] : beyond; }
-    locate<T>(a, r, weight, how.least, cut == ~0ull ? beyond + 1 : cut, s.mass, s);
+    locate<T>(a, r, weight, how.least, cut, s.mass, s);
 }
 
 // Rows of one chunk or less, and everything at once.
