@@ -121,10 +121,11 @@ ivftq_status ivftq_kv_digest(const ivftq_kv_cache* cache, void* digests, const i
 
 /* scores: rows x heads x columns floats; -infinity where a page holds no token that the row sees (behind its position, no page).
  * q, starts, max_new as in ivftq_kv_attend; rows that it gives no result keep their scores.  workspace: ivftq_kv_score_workspace
- * bytes, 256-byte aligned (0 for the 16-bit formats). */
+ * bytes (starts NULL: of max_new = 1), 256-byte aligned. */
 ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts,
                             int32_t max_new, void* workspace, int64_t workspace_bytes, void* stream);
-int64_t ivftq_kv_score_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads);
+/* -1 for arguments that ivftq_kv_score refuses. */
+int64_t ivftq_kv_score_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads, int32_t max_new);
 
 /* chosen: rows x heads x count numbers: of the columns that a row's position p reaches (column c: c * page <= p) the first `first` and
  * the last `last`, and those of the highest scores (ties: the lowest column; -infinity and what is no number: never), ascending, -1

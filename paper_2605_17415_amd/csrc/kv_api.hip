@@ -93,9 +93,20 @@ PickWork pick_work(int format, int d, int kv_heads, int64_t rows, int q_heads, i
     return w;
 }
 
-int64_t score_work(int format, int d, int64_t all, int64_t* zn) {
-    *zn = round_up64(all * d * 4, 256);
-    return format == IVFTQ_KV_CODE4 ? *zn + round_up64(all * 4, 256) : 0;
+ScoreWork score_work(int format, int d, int64_t rows, int q_heads, int kv_heads, bool one) {
+    ScoreWork w{};
+    int64_t at = 0;
+    auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
+    if (format == IVFTQ_KV_CODE4) {
+        w.z = room(rows * q_heads * d * 4);
+        w.zn = room(rows * q_heads * 4);
+    }
+    if (!one) {
+        w.sides = room(rows * kv_heads * (format == IVFTQ_KV_BF16 ? 3 : 2) * 2 * d * 2);
+        w.unit = room(rows * kv_heads * 4);
+    }
+    w.bytes = at;
+    return w;
 }
 
 hipError_t launch_kv_score(const KvAttend& a, const void* digests, float* scores, int d, int format, hipStream_t st) {
@@ -395,10 +406,13 @@ ivftq_status ivftq_kv_digest(const ivftq_kv_cache* cache, void* digests, const i
     return done(launch_kv_digest(c, digests, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_digest");
 }
 
-int64_t ivftq_kv_score_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads) {
+int64_t ivftq_kv_score_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads, int32_t max_new) {
     if (check_cache(cache) || !known_sizes(cache, rows, q_heads)) return -1;
-    int64_t zn;
-    return score_work(cache->format, cache->d, rows * q_heads, &zn);
+    if (max_new < 1) {
+        refuse(IVFTQ_INVALID_ARG, "max_new = %d", max_new);
+        return -1;
+    }
+    return score_work(cache->format, cache->d, rows, q_heads, cache->heads, max_new == 1 || rows <= 1).bytes;
 }
 ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts, int32_t max_new,
                             void* workspace, int64_t workspace_bytes, void* stream) {
@@ -409,8 +423,7 @@ ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q,
     const KvAttend a = attend_of(*cache, *q, starts, max_new, workspace);
     if ((int64_t)cache->batch * cache->heads * ((a.max_new + 15) / 16) > INT32_MAX)
         return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups: %d sequences of %d heads and up to %d rows", cache->batch, cache->heads, a.max_new);
-    int64_t zn;
-    if (ivftq_status e = check_work(workspace, workspace_bytes, score_work(cache->format, cache->d, q->rows * q->heads, &zn))) return e;
+    if (ivftq_status e = check_work(workspace, workspace_bytes, score_work(cache->format, cache->d, q->rows, q->heads, cache->heads, a.max_new == 1).bytes)) return e;
     return done(launch_kv_score(a, digests, scores, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_score");
 }
 

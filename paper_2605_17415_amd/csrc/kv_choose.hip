@@ -1,5 +1,8 @@
 // Digests of the key-value cache's pages, and the pages that a row is given for their scores.
+#include <type_traits>
+
 #include "kv_kernels.h"
+#include "wave_ops.h"
 
 namespace ivftq {
 namespace {
@@ -193,11 +196,10 @@ hipError_t digest(const KvView& c, uint16_t* digests, int d, hipStream_t st) {
 
 // ---- pages of the highest scores --------------------------------------------------------------------------------------
 
-// Scores as numbers whose order is theirs; 0: never chosen, the largest: always.
+// Scores as numbers whose order is theirs; 0: never chosen.  (Without branches: there are many of them.)
 __device__ __forceinline__ uint32_t order_of(float v) {
-    if (!(v > -INFINITY)) return 0;
     const uint32_t bits = __builtin_bit_cast(uint32_t, v + 0.f);                 // no negative zero
-    return bits >> 31 ? ~bits : bits | 0x80000000u;
+    return (bits ^ (uint32_t)((int32_t)bits >> 31 | (int32_t)0x80000000)) & (v > -INFINITY ? ~0u : 0u);
 }
 
 // Sum of v over the threads before this one, and over all of the 256.
@@ -216,7 +218,114 @@ __device__ __forceinline__ uint32_t before256(uint32_t v, uint32_t* sums, uint32
     return before + incl - v;
 }
 
-// A workgroup a row and head: the order of the count-th highest score is found eight bits at a time by counting, then what is above it, and
+// W wavefronts a row and head, its scores in registers (lane l of wavefront w: columns 64 R w + l, + 64, ..): the order of the last one that is
+// chosen is found by halving the range from the lowest to the highest, counting what is not under the middle, until the count is right
+// (about twelve times for a thousand scores) or the range is one number, whose lowest columns are taken.
+template <int R, int W>
+__global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void k_kv_select_held(KvSelect s) {
+    constexpr int kUnits = W < 4 ? 4 / W : 1;             // of a workgroup
+    __shared__ uint32_t shared[kUnits][2][W][2];
+    const KvView& c = s.c;
+    const int lane = threadIdx.x & 63, wave = kv_wave() % W, sub = kv_wave() / W;
+    const int64_t unit = (int64_t)kv_workgroup() * kUnits + sub, last_unit = (int64_t)c.rows * c.heads - 1;
+    const int64_t used = unit < last_unit ? unit : last_unit;                    // (past the end: the last one once more, for the barriers)
+    int turn = 0;
+    // two numbers of every wavefront
+    auto exchange = [&](uint32_t a, uint32_t b, uint32_t (&as)[W], uint32_t (&bs)[W]) __attribute__((always_inline)) {
+        if constexpr (W == 1) { as[0] = a; bs[0] = b; return; }
+        if (lane == 0) { shared[sub][turn][wave][0] = a; shared[sub][turn][wave][1] = b; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) { as[w] = shared[sub][turn][w][0]; bs[w] = shared[sub][turn][w][1]; }
+        turn ^= 1;
+    };
+    const int pos = kv_uniform(kv_position(c, used / c.heads));
+    const int reach = pos < 0 ? 0 : (pos >> c.page_log2) + 1, n = reach < c.columns ? reach : c.columns;
+    const float* scores = s.scores + used * c.columns;
+    int32_t* out = s.chosen + used * s.count;
+    float score[R];
+    uint32_t key[R], high = 0, low = 0xffffffffu, as[W], bs[W];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int col = 64 * (R * wave + j) + lane;
+        score[j] = scores[col < c.columns ? col : c.columns - 1];
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int col = 64 * (R * wave + j) + lane;
+        key[j] = order_of(score[j]) & (col >= s.first && col < n - s.last ? ~0u : 0u);
+        high = key[j] > high ? key[j] : high;
+        low = key[j] - 1 < low - 1 ? key[j] : low;        // of those above zero
+    }
+    exchange(lanes64(high, Larger()), lanes64(low - 1, Smaller()), as, bs);
+    high = as[0];
+    low = bs[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) { high = as[w] > high ? as[w] : high; low = bs[w] < low ? bs[w] : low; }
+    high = kv_uniform((int)high);
+    low = kv_uniform((int)low) + 1;
+    auto not_under = [&](uint32_t t) __attribute__((always_inline)) {
+        uint32_t count = 0;
+#pragma unroll
+        for (int j = 0; j < R; ++j) count += key[j] >= t;
+        exchange(lanes64(count, Sum()), 0, as, bs);
+        count = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) count += as[w];
+        return kv_uniform((int)count);
+    };
+    // always: the first and the last columns; of the others `want`: those not under `low` (all of them: low = 1), of low's equals `ties`
+    const int kept = (s.first < n ? s.first : n) + (s.last < n - s.first ? s.last : (n > s.first ? n - s.first : 0)), want = s.count - kept;
+    int ties = 1 << 30;
+    if (want <= 0) {
+        low = 0xffffffffu;
+    } else if (high == 0 || not_under(low) <= want) {
+        low = 1;
+    } else {
+        // not_under(low) > want; not_under(past) < want (past: none is as large, at first)
+        uint32_t past = high + 1;
+        int above = 0;
+        while (true) {
+            if (past - low == 1) { ties = want - above; break; }
+            const uint32_t mid = low + (past - low) / 2;
+            const int count = not_under(mid);
+            if (count >= want) low = mid; else { past = mid; above = count; }
+            if (count == want) break;
+        }
+    }
+    uint32_t better = 0, same = 0;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int col = 64 * (R * wave + j) + lane;
+        better += key[j] > low || (col < n && (col < s.first || col >= n - s.last));
+        same += key[j] == low;
+    }
+    exchange(lanes64(better, Sum()), lanes64(same, Sum()), as, bs);
+    int at = 0, equal = 0, total_better = 0, total_same = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        at += w < wave ? as[w] : 0;
+        equal += w < wave ? bs[w] : 0;
+        total_better += as[w];
+        total_same += bs[w];
+    }
+    if (unit > last_unit) return;
+    at += equal < ties ? equal : ties;
+    const uint64_t before = (1ull << lane) - 1;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int col = 64 * (R * wave + j) + lane;
+        const uint64_t all_same = __ballot(key[j] == low);
+        const bool always = col < n && (col < s.first || col >= n - s.last), tie = key[j] == low && equal + __popcll(all_same & before) < ties;
+        const uint64_t all_in = __ballot(always || key[j] > low || tie);
+        if (all_in >> lane & 1) out[at + __popcll(all_in & before)] = col;
+        at += __popcll(all_in);
+        equal += __popcll(all_same);
+    }
+    for (int i = total_better + (total_same < ties ? total_same : ties) + (int)(threadIdx.x % (64 * W)); i < s.count; i += 64 * W) out[i] = -1;
+}
+
+// Longer rows, a workgroup a row and head: the order of the count-th highest score is found eight bits at a time by counting, then what is above it, and
 // of its equals the lowest columns, is written in order.
 __global__ __launch_bounds__(256) void k_kv_select(KvSelect s) {
     __shared__ uint32_t counts[256], sums[4], found[2];
@@ -275,7 +384,29 @@ hipError_t launch_kv_digest(const KvView& c, void* digests, int d, int format, h
     }
 }
 hipError_t launch_kv_select(const KvSelect& s, hipStream_t st) {
-    k_kv_select<<<kv_grid((int64_t)s.c.rows * s.c.heads, 256), 256, 0, st>>>(s);
+    const int64_t units = (int64_t)s.c.rows * s.c.heads;
+    // Many pairs: a wavefront each, with as many registers as its row is long (6,432 rows of 1,251: 24 us, four wavefronts each 37); few: four
+    // wavefronts (32 rows of 2,048: 8.6 us, one each 14.3, sixteen 11.6).
+    const int n = s.c.columns, of_one = (n + 255) / 256, of_four = (n + 511) / 512;
+    auto one = [&](auto r) { k_kv_select_held<decltype(r)::value, 1><<<kv_grid((units + 3) / 4, 256), 256, 0, st>>>(s); };
+    auto four = [&](auto r) { k_kv_select_held<decltype(r)::value, 4><<<kv_grid(units, 256), 256, 0, st>>>(s); };
+    if (n > 4096) k_kv_select<<<kv_grid(units, 256), 256, 0, st>>>(s);
+    else if (units >= 1024 && n <= 2048)
+        switch (of_one) {
+            case 1: one(std::integral_constant<int, 4>{}); break;
+            case 2: one(std::integral_constant<int, 8>{}); break;
+            case 3: one(std::integral_constant<int, 12>{}); break;
+            case 4: one(std::integral_constant<int, 16>{}); break;
+            case 5: one(std::integral_constant<int, 20>{}); break;
+            case 6: one(std::integral_constant<int, 24>{}); break;
+            case 7: one(std::integral_constant<int, 28>{}); break;
+            default: one(std::integral_constant<int, 32>{}); break;
+        }
+    else if (of_four <= 1) four(std::integral_constant<int, 2>{});
+    else if (of_four <= 2) four(std::integral_constant<int, 4>{});
+    else if (of_four <= 4) four(std::integral_constant<int, 8>{});
+    else if (of_four <= 6) four(std::integral_constant<int, 12>{});
+    else four(std::integral_constant<int, 16>{});
     return hipGetLastError();
 }
 

@@ -1,13 +1,16 @@
 // Scores of pages by their digests, and attention over chosen pages.
 //
-// Scores are products of queries and digests (v_mfma 16x16x32: 16 pages x 16 new rows), the negative coordinates of a query with the lowest
-// values and the others with the highest; the group's heads add up in the accumulators.  Codes: rotated unit queries in two float16 parts.
+// A score is linear in two sums over the group's heads, those of the queries' negative coordinates (which meet the lowest values) and of the
+// others (the highest): sides[2][D].  One new row a sequence: sums and products in float32, a digest's sixteen-byte pieces over
+// the lanes, bound by the digests' bytes.  Several: the sides are made once, in two (bfloat16: three) 16-bit parts, and meet the
+// digests in v_mfma 16x16x32, 16 pages x 16 new rows.
 //
 // Attention: every new row has pages of its own for each key-value head, so a (row, head) pair is what kv_few.h calls a sequence: a
 // workgroup's wavefronts take every fourth tile of 32 tokens of the chosen pages, the query rows are the group's heads.  Where
 // the pairs are few several workgroups share a pair's tiles, and a second kernel joins their parts.
 #pragma once
 #include "kv_many.h"
+#include "wave_ops.h"
 
 namespace ivftq {
 
@@ -17,88 +20,206 @@ struct ScoreArgs {
     float* scores;
     const uint16_t* z;                // codes: rotated unit queries, two float16 parts, eights in the order of kv_levels8
     const float* zn;                  // codes: the queries' norms
-    int32_t row_tiles;
+    uint16_t* sides;                  // [rows][heads][parts][2 D]
+    float* unit;                      // [rows][heads] what the parts are multiplied by
+    int32_t row_tiles, each;          // row tiles of 16 a sequence, and a workgroup's
 };
+template <int F> constexpr int kSideParts = F == IVFTQ_KV_BF16 ? 3 : 2;
 
-// The coordinates of w that are negative; the others are w & ~mask.
-__device__ __forceinline__ uintx4 kv_negative(uintx4 w) {
-    uintx4 m;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        typedef int16_t two __attribute__((ext_vector_type(2)));
-        const uint32_t u = w[e];
-        m[e] = __builtin_bit_cast(uint32_t, (two)(__builtin_bit_cast(two, u) >> (two)(15)));
-    }
-    return m;
-}
 // Eight values from the order of kv_levels8 into their own.
 __device__ __forceinline__ uintx4 kv_in_order(uintx4 w) {
     return uintx4{__builtin_amdgcn_perm(w[2], w[0], 0x05040100u), __builtin_amdgcn_perm(w[2], w[0], 0x07060302u),
                   __builtin_amdgcn_perm(w[3], w[1], 0x05040100u), __builtin_amdgcn_perm(w[3], w[1], 0x07060302u)};
 }
 
+// Eight coordinates from j on of the sides of a row and head: sums of the negative ones, and of the others.
+template <int F, int D>
+__device__ __forceinline__ void score_sides(const ScoreArgs& f, int64_t row, int h, int j, float (&low)[8], float (&high)[8]) {
+    const KvAttend& a = f.a;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) low[e] = high[e] = 0.f;
+    auto add = [&](int e, float v) __attribute__((always_inline)) { low[e] += fminf(v, 0.f); high[e] += fmaxf(v, 0.f); };
+#pragma unroll 4
+    for (int i = 0; i < a.group; ++i) {
+        const int64_t head = (int64_t)h * a.group + i;
+        if constexpr (F == IVFTQ_KV_CODE4) {
+            const int64_t at = row * a.q.heads + head, all = (int64_t)a.q.rows * a.q.heads;
+            const halfx8 u = __builtin_bit_cast(halfx8, kv_in_order(*reinterpret_cast<const uintx4*>(f.z + at * D + j)));
+            const halfx8 v = __builtin_bit_cast(halfx8, kv_in_order(*reinterpret_cast<const uintx4*>(f.z + (all + at) * D + j)));
+            const float norm = f.zn[at] * (1.f / kSplitScale);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) add(e, ((float)u[e] + (float)v[e]) * norm);
+        } else {
+            const uintx4 w = *reinterpret_cast<const uintx4*>(reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + j);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) add(e, kv_to_float<F == IVFTQ_KV_BF16>(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffff));
+        }
+    }
+}
+
+// One new row a sequence.  A page's digest lies over kLanes lanes (a sixteen-byte piece each; 96 and 192 coordinates leave a quarter of them
+// idle), a wavefront's load has kPages of them, 16 loads are on their way at once.
+template <int F, int D>
+__global__ __launch_bounds__(256) void k_kv_score_one(ScoreArgs f) {
+    constexpr int kPieces = D / 4, kLanes = kPieces <= 16 ? 16 : (kPieces <= 32 ? 32 : 64), kPages = 64 / kLanes, kLoads = 32 / kPages < 16 ? 32 / kPages : 16;
+    constexpr int kAll = kPages * kLoads;                                 // pages of a wavefront
+    const KvAttend& a = f.a;
+    const KvView& c = a.c;
+    const int wave = kv_wave(), lane = threadIdx.x & 63, piece = lane % kLanes, sub = lane / kLanes;
+    const int64_t wg = kv_workgroup();
+    const int h = (int)(wg % c.heads);
+    const int64_t row = wg / c.heads;
+    const int col0 = ((int)blockIdx.y * 4 + wave) * kAll;
+    if (row >= c.rows || col0 >= c.columns) return;
+    int first, count;
+    const int b = kv_uniform(kv_sequence(c, row, first, count));
+    if (b < 0 || row - first >= a.max_new) return;
+    const int pos = kv_length(c, b) - count + (int)(row - first), reach = pos >> c.page_log2;      // a position under zero reaches column -1
+    const int mine = col0 + lane;                                          // the column that this lane writes
+    const int32_t id = lane < kAll && mine < c.columns && mine <= reach ? c.table[(int64_t)b * c.table_stride + mine] : -1;
+    const bool there = (uint32_t)id < (uint32_t)c.pages;
+    const int32_t page = there ? id : 0;
+    float score = 0.f;
+    if (col0 <= reach) {
+        const uint16_t* box = f.digests + (int64_t)h * (2 * D) + (piece < kPieces ? piece : 0) * 8;
+        uintx4 w[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) w[i] = *reinterpret_cast<const uintx4*>(box + (int64_t)__shfl(page, i * kPages + sub) * c.heads * (2 * D));
+        float low[8], high[8], side[8];
+        const int j = piece < kPieces ? piece * 8 % D : 0;
+        score_sides<F, D>(f, row, h, j, low, high);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) side[e] = piece * 8 < D ? low[e] : (piece < kPieces ? high[e] : 0.f);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            float v = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v = __builtin_fmaf(kv_to_float<F == IVFTQ_KV_BF16>(e & 1 ? w[i][e >> 1] >> 16 : w[i][e >> 1] & 0xffff), side[e], v);
+            if (kLanes > kPieces) v = piece < kPieces ? v : 0.f;
+            v = lanes8(v, Sum());
+            v += lane_moved<0x140>(v);
+            if (kLanes >= 32) v = lane_pair<false>(v, Sum());
+            if (kLanes == 64) v = lane_pair<true>(v, Sum());
+            // the lanes that write the pages of this load
+#pragma unroll
+            for (int u = 0; u < kPages; ++u) {
+                const float of = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), u * kLanes));
+                score = lane == i * kPages + u ? of : score;
+            }
+        }
+    }
+    if (lane < kAll && mine < c.columns) f.scores[(row * c.heads + h) * c.columns + mine] = there ? score : -INFINITY;
+}
+
+// Sides of several rows: 32 lanes a (row, head) pair, of which D / 8 work.
+template <int F, int D>
+__global__ __launch_bounds__(256) void k_kv_sides(ScoreArgs f) {
+    constexpr int kParts = kSideParts<F>;
+    constexpr bool bf = F == IVFTQ_KV_BF16;
+    const KvView& c = f.a.c;
+    const int64_t pair = (int64_t)kv_workgroup() * 8 + threadIdx.x / 32, pairs = (int64_t)c.rows * c.heads;
+    const int piece = threadIdx.x % 32, j = piece < D / 8 ? piece * 8 : 0;
+    const int64_t used = pair < pairs ? pair : pairs - 1;
+    float x[2][8], most = 0.f;
+    score_sides<F, D>(f, used / c.heads, (int)(used % c.heads), j, x[0], x[1]);
+    float by = 1.f;
+    if constexpr (!bf) {                                      // float16: the largest value to 2^14, so that the second part keeps its bits
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fmaxf(-x[0][e], x[1][e]));
+        most = lanes8(most, Larger());
+        most = fmaxf(most, lane_moved<0x140>(most));
+        most = lane_pair<false>(most, Larger());
+        const int e = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
+        by = most > 0.f && most < INFINITY ? ldexpf(1.f, e < -100 ? 114 : 14 - e) : 1.f;
+    }
+    if (pair >= pairs || piece >= D / 8) return;
+    if (piece == 0) f.unit[pair] = 1.f / by;
+    uint16_t* to = f.sides + pair * (kParts * 2 * D) + j;
+#pragma unroll
+    for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[side][e] *= by;
+#pragma unroll
+    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            uintx4 w;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                w[e / 2] = kv_pack2<bf>(x[side][e], x[side][e + 1]);
+                x[side][e] -= kv_to_float<bf>(w[e / 2] & 0xffff);
+                x[side][e + 1] -= kv_to_float<bf>(w[e / 2] >> 16);
+            }
+            *reinterpret_cast<uintx4*>(to + (part * 2 + side) * D) = w;
+        }
+}
+
+// Several new rows: a wavefront keeps the digests of its pages and walks the row tiles.
 template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
-    constexpr bool codes = F == IVFTQ_KV_CODE4;
+    constexpr int kSteps = 2 * D / 32, kTiles = D <= 128 ? 2 : 1, kParts = kSideParts<F>;
     const KvAttend& a = f.a;
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const uint32_t wg = kv_workgroup();
-    const int h = (int)(wg % (uint32_t)c.heads), rt = (int)(wg / (uint32_t)c.heads % (uint32_t)f.row_tiles), b = (int)(wg / (uint32_t)c.heads / (uint32_t)f.row_tiles);
+    const uint32_t wg = kv_workgroup(), groups = ((uint32_t)f.row_tiles + f.each - 1) / f.each;
+    const int h = (int)(wg % (uint32_t)c.heads), rt0 = (int)(wg / (uint32_t)c.heads % groups) * f.each, b = (int)(wg / (uint32_t)c.heads / groups);
     if (b >= c.batch) return;
     int first, count;
     kv_new_rows(c, b, first, count);
     const int base = kv_length(c, b) - count;
     if (count > a.max_new) count = a.max_new;
-    if (16 * rt >= count) return;
-    const int col0 = ((int)blockIdx.y * 4 + wave) * 16;
+    if (16 * rt0 >= count) return;
+    const int col0 = ((int)blockIdx.y * 4 + wave) * 16 * kTiles;
     if (col0 >= c.columns) return;
-    const int rows = count - 16 * rt < 16 ? count - 16 * rt : 16, row = first + 16 * rt + (n < rows ? n : 0);
-    // page of column col0 + n
-    const int32_t id = col0 + n < c.columns ? c.table[(int64_t)b * c.table_stride + col0 + n] : -1;
-    const bool there = (uint32_t)id < (uint32_t)c.pages;
-    const uint32_t known = (uint32_t)__ballot(there) & 0xffffu;
-    floatx4 total = {0.f, 0.f, 0.f, 0.f};
-    if (col0 <= (base + 16 * rt + rows - 1) >> c.page_log2) {           // any of the rows reaches these pages
-        const uint16_t* box = f.digests + ((int64_t)(there ? id : 0) * c.heads + h) * (2 * D) + 8 * g;
-        uintx4 low[D / 32], high[D / 32];
+    uint32_t known[kTiles];
+    uintx4 box[kTiles][kSteps];
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            low[k] = *reinterpret_cast<const uintx4*>(box + 32 * k);
-            high[k] = *reinterpret_cast<const uintx4*>(box + D + 32 * k);
+    for (int t = 0; t < kTiles; ++t) {
+        const int col = col0 + 16 * t + n;                                 // this lane's page
+        const int32_t id = col < c.columns && col <= (base + count - 1) >> c.page_log2 ? c.table[(int64_t)b * c.table_stride + col] : -1;
+        const bool there = (uint32_t)id < (uint32_t)c.pages;
+        known[t] = (uint32_t)__ballot(there) & 0xffffu;
+        const uint16_t* p = f.digests + ((int64_t)(there ? id : 0) * c.heads + h) * (2 * D) + 8 * g;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) box[t][k] = *reinterpret_cast<const uintx4*>(p + 32 * k);
+    }
+    const int last = rt0 + f.each < f.row_tiles ? rt0 + f.each : f.row_tiles;
+    for (int rt = rt0; rt < last && 16 * rt < count; ++rt) {
+        const int rows = count - 16 * rt < 16 ? count - 16 * rt : 16, row = first + 16 * rt + (n < rows ? n : 0);
+        const int64_t pair = (int64_t)row * c.heads + h;
+        floatx4 acc[kTiles];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (col0 <= (base + 16 * rt + rows - 1) >> c.page_log2) {          // any of the rows reaches these pages
+            const uint16_t* p = f.sides + pair * (kParts * 2 * D) + 8 * g;
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) {
+                    const uintx4 w = *reinterpret_cast<const uintx4*>(p + part * 2 * D + 32 * k);
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) acc[t] = kv_mfma16<F>(box[t][k], w, acc[t]);
+                }
         }
-        for (int i = 0; i < a.group; ++i) {
-            const int head = h * a.group + i;
-            if constexpr (codes) {
-                const int64_t at = (int64_t)row * a.q.heads + head, all = (int64_t)a.q.rows * a.q.heads;
-                floatx4 part = {0.f, 0.f, 0.f, 0.f};
+        if (n >= rows) continue;
+        const float unit = f.unit[pair];
+        const int reach = (base + 16 * rt + n) >> c.page_log2;             // a position under zero reaches column -1
 #pragma unroll
-                for (int k = 0; k < D / 32; ++k) {
-                    const uintx4 w = kv_in_order(*reinterpret_cast<const uintx4*>(f.z + at * D + 32 * k + 8 * g)), m = kv_negative(w);
-                    const uintx4 v = kv_in_order(*reinterpret_cast<const uintx4*>(f.z + (all + at) * D + 32 * k + 8 * g));
-                    part = kv_mfma16<F>(low[k], w & m, part);
-                    part = kv_mfma16<F>(high[k], w & ~m, part);
-                    part = kv_mfma16<F>(low[k], v & m, part);
-                    part = kv_mfma16<F>(high[k], v & ~m, part);
-                }
-                total += part * (f.zn[at] * (1.f / kSplitScale));
+        for (int t = 0; t < kTiles; ++t) {
+            const int col = col0 + 16 * t + 4 * g;
+            float* out = f.scores + pair * c.columns + col;
+            floatx4 v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = col + r <= reach && (known[t] >> (4 * g + r) & 1) ? acc[t][r] * unit : -INFINITY;
+            if (col + 3 < c.columns) {
+                __builtin_memcpy(out, &v, 16);
             } else {
-                const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
 #pragma unroll
-                for (int k = 0; k < D / 32; ++k) {
-                    const uintx4 w = *reinterpret_cast<const uintx4*>(q + 32 * k), m = kv_negative(w);
-                    total = kv_mfma16<F>(low[k], w & m, total);
-                    total = kv_mfma16<F>(high[k], w & ~m, total);
-                }
+                for (int r = 0; r < 3; ++r)
+                    if (col + r < c.columns) out[r] = v[r];
             }
         }
     }
-    if (n >= rows) return;
-    const int reach = (base + 16 * rt + n) >> c.page_log2, col = col0 + 4 * g;         // a position under zero reaches column -1
-    float* out = f.scores + ((int64_t)row * c.heads + h) * c.columns + col;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (col + r < c.columns) out[r] = col + r <= reach && (known >> (4 * g + r) & 1) ? total[r] : -INFINITY;
 }
 
 // ---- attention ----------------------------------------------------------------------------------------------------
@@ -370,7 +491,8 @@ struct PickWork {
     int32_t col_tiles, splits;
 };
 PickWork pick_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int page, int columns, int count);
-int64_t score_work(int format, int d, int64_t all, int64_t* zn);
+struct ScoreWork { int64_t z, zn, sides, unit, bytes; };
+ScoreWork score_work(int format, int d, int64_t rows, int q_heads, int kv_heads, bool one);
 
 // 16-row tiles that a workgroup rotates, and workgroups (as kv_attend_launch).
 template <int D>
@@ -382,11 +504,25 @@ void rotate_queries(const KvAttend& a, uint16_t* z, float* zn, hipStream_t st) {
 
 template <int F, int D>
 hipError_t kv_score_launch(const KvAttend& a, const void* digests, float* scores, hipStream_t st) {
-    int64_t zn;
-    score_work(F, D, (int64_t)a.q.rows * a.q.heads, &zn);
-    ScoreArgs f{a, static_cast<const uint16_t*>(digests), scores, reinterpret_cast<const uint16_t*>(a.work), reinterpret_cast<const float*>(a.work + zn), (a.max_new + 15) / 16};
-    if constexpr (F == IVFTQ_KV_CODE4) rotate_queries<D>(a, reinterpret_cast<uint16_t*>(a.work), reinterpret_cast<float*>(a.work + zn), st);
-    k_kv_score<F, D><<<kv_grid((int64_t)a.c.batch * a.c.heads * f.row_tiles, 256, (unsigned)((a.c.columns + 63) / 64)), 256, 0, st>>>(f);
+    const bool one = a.max_new == 1;
+    const ScoreWork w = score_work(F, D, a.q.rows, a.q.heads, a.c.heads, one);
+    uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
+    float* zn = reinterpret_cast<float*>(a.work + w.zn);
+    if constexpr (F == IVFTQ_KV_CODE4) rotate_queries<D>(a, z, zn, st);
+    ScoreArgs f{a, static_cast<const uint16_t*>(digests), scores, z, zn, reinterpret_cast<uint16_t*>(a.work + w.sides), reinterpret_cast<float*>(a.work + w.unit), (a.max_new + 15) / 16, 1};
+    const int64_t pairs = (int64_t)a.c.rows * a.c.heads;
+    if (one) {
+        constexpr int pages = 4 * (D <= 128 ? 32 : 16);
+        k_kv_score_one<F, D><<<kv_grid(pairs, 256, (unsigned)((a.c.columns + pages - 1) / pages)), 256, 0, st>>>(f);
+        return hipGetLastError();
+    }
+    k_kv_sides<F, D><<<kv_grid((pairs + 7) / 8, 256), 256, 0, st>>>(f);
+    constexpr int pages = 4 * 16 * (D <= 128 ? 2 : 1);
+    const unsigned blocks = (unsigned)((a.c.columns + pages - 1) / pages);
+    // row tiles of a workgroup, which reads its digests once for them: as many as leave four workgroups a compute unit
+    const int64_t wgs = (int64_t)a.c.batch * a.c.heads * f.row_tiles * blocks / 1024;
+    f.each = wgs < 1 ? 1 : (wgs < f.row_tiles ? (int)wgs : f.row_tiles);
+    k_kv_score<F, D><<<kv_grid((int64_t)a.c.batch * a.c.heads * ((f.row_tiles + f.each - 1) / f.each), 256, blocks), 256, 0, st>>>(f);
     return hipGetLastError();
 }
 template <int D>

@@ -72,7 +72,7 @@ _SIGNATURES = {
     "ivftq_kv_attend_workspace": (C.c_int64, [_P, C.c_int64, C.c_int32, C.c_int32]),
     "ivftq_kv_digest": (C.c_int, [_P, _P, _P, _P]),
     "ivftq_kv_score": (C.c_int, [_P, _P, _P, _P, _P, C.c_int32, _P, C.c_int64, _P]),
-    "ivftq_kv_score_workspace": (C.c_int64, [_P, C.c_int64, C.c_int32]),
+    "ivftq_kv_score_workspace": (C.c_int64, [_P, C.c_int64, C.c_int32, C.c_int32]),
     "ivftq_kv_select": (C.c_int, [_P, _P, _P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P]),
     "ivftq_kv_attend_pages": (C.c_int, [_P, _P, _P, _P, _P, C.c_int32, _P, C.c_int32, C.c_float, _P, C.c_int64, _P]),
     "ivftq_kv_attend_pages_workspace": (C.c_int64, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32]),
@@ -336,11 +336,9 @@ def kv_score(q, digests, pool, table, lengths, starts=None, max_new=None, rotati
         out = _blank(shape, torch.float32, q, stream)
     result, first, max_new = _floats(out, "out", pool, shape), _starts(starts, table, pool), _most_new(max_new, starts, q.shape[0])
     lib = _library()
-    need = 0
-    if pool.dtype == torch.uint8:
-        need = lib.ivftq_kv_score_workspace(cache, q.shape[0], q.shape[1])
-        if need < 0:
-            _check(1)
+    need = lib.ivftq_kv_score_workspace(cache, q.shape[0], q.shape[1], max_new)
+    if need < 0:
+        _check(1)
     work = _scratch(need, torch.uint8, q, stream) if need else None
     _run(lib.ivftq_kv_score, pool, cache, rows, box, result, first, max_new, None if work is None else work.data_ptr(), need, where)
     return out

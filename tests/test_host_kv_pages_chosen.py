@@ -41,7 +41,7 @@ def attend(lib, c=None, q=None, out=None, chosen=HERE, count=8, starts=None, max
 @pytest.mark.parametrize("change,status", BAD_CACHES)
 def test_caches_that_are_refused(lib, change, status):
     assert [f(lib, cache(**change)) for f in (digest, score, attend)] == [status] * 3
-    assert lib.ivftq_kv_score_workspace(C.byref(cache(**change)), 2, 16) == -1
+    assert lib.ivftq_kv_score_workspace(C.byref(cache(**change)), 2, 16, 1) == -1
     assert lib.ivftq_kv_attend_pages_workspace(C.byref(cache(**change)), 2, 16, 1, 8) == -1
 
 
@@ -62,10 +62,11 @@ def test_digests_that_are_refused(lib):
 def test_scores_that_are_refused(lib):
     assert score(lib, box=None) == score(lib, box=UNEVEN) == score(lib, out=None) == score(lib, max_new=0) == 1
     assert score(lib, work=None) == score(lib, size=100) == score(lib, work=UNEVEN) == 1
-    need = lib.ivftq_kv_score_workspace(C.byref(cache()), 2, 16)
+    need = lib.ivftq_kv_score_workspace(C.byref(cache()), 2, 16, 1)
     assert need >= 2 * 16 * 128 * 4 + 2 * 16 * 4 and need % 256 == 0 and score(lib, size=need - 1) == 1
-    assert lib.ivftq_kv_score_workspace(C.byref(cache(format=kv.BF16)), 2, 16) == 0
-    for bad in ((-1, 16), (2, 0), (2, 12), (1 << 30, 16)):
+    assert lib.ivftq_kv_score_workspace(C.byref(cache(format=kv.BF16)), 2, 16, 1) == 0
+    assert score(lib, cache(format=kv.BF16), starts=HERE, max_new=2, size=lib.ivftq_kv_score_workspace(C.byref(cache(format=kv.BF16)), 2, 16, 2) - 1) == 1
+    for bad in ((-1, 16, 1), (2, 0, 1), (2, 12, 1), (1 << 30, 16, 1), (2, 16, 0)):
         assert lib.ivftq_kv_score_workspace(C.byref(cache()), *bad) == -1
     assert score(lib, cache(batch=1 << 20, heads=1024), queries(rows=1 << 20, heads=1024, row_stride=1 << 17), starts=HERE, max_new=1 << 20) != 0
     assert score(lib, cache(batch=0), queries(rows=0)) == 0
