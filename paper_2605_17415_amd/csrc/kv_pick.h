@@ -3,7 +3,7 @@
 // A score is linear in two sums over the group's heads, those of the queries' negative coordinates (which meet the lowest values) and of the
 // others (the highest): sides[2][D].  One new row a sequence: sums and products in float32, a digest's sixteen-byte pieces over
 // the lanes, bound by the digests' bytes.  Several: the sides are made once, in two (bfloat16: three) 16-bit parts, and meet the
-// digests in v_mfma 16x16x32, 16 pages x 16 new rows.
+// digests in v_mfma 16x16x32, 16 new rows x 16 pages.
 //
 // Attention: every new row has pages of its own for each key-value head, so a (row, head) pair is what kv_few.h calls a sequence: a
 // workgroup's wavefronts take every fourth tile of 32 tokens of the chosen pages, the query rows are the group's heads.  Where
@@ -20,8 +20,9 @@ struct ScoreArgs {
     float* scores;
     const uint16_t* z;                // codes: rotated unit queries, two float16 parts, eights in the order of kv_levels8
     const float* zn;                  // codes: the queries' norms
-    uint16_t* sides;                  // [rows][heads][parts][2 D]
-    float* unit;                      // [rows][heads] what the parts are multiplied by
+    uint16_t* sides;                  // [heads][tiles][parts][2 D / 32][64 lanes][8]: operands as they are read
+    float* unit;                      // [heads][tiles][16] what the parts are multiplied by
+    int32_t tiles;                    // tiles of 16 rows, those of sequence b from score_tile on
     int32_t row_tiles, each;          // row tiles of 16 a sequence, and a workgroup's
 };
 template <int F> constexpr int kSideParts = F == IVFTQ_KV_BF16 ? 3 : 2;
@@ -111,7 +112,11 @@ __global__ __launch_bounds__(256) void k_kv_score_one(ScoreArgs f) {
     if (lane < kAll && mine < c.columns) f.scores[(row * c.heads + h) * c.columns + mine] = there ? score : -INFINITY;
 }
 
-// Sides of several rows: 32 lanes a (row, head) pair, of which D / 8 work.
+// The first tile of a sequence: no two sequences' tiles meet, however long they are.
+__device__ __forceinline__ int score_tile(int first, int b) { return first / 16 + b; }
+
+// Sides of several rows: 32 lanes a (row, head) pair, of which D / 8 work.  (Rows that lie one after the other, 8 KB apart, meet in one
+// channel of the L2: read that way the products took four times as long.)
 template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_sides(ScoreArgs f) {
     constexpr int kParts = kSideParts<F>;
@@ -133,8 +138,14 @@ __global__ __launch_bounds__(256) void k_kv_sides(ScoreArgs f) {
         by = most > 0.f && most < INFINITY ? ldexpf(1.f, e < -100 ? 114 : 14 - e) : 1.f;
     }
     if (pair >= pairs || piece >= D / 8) return;
-    if (piece == 0) f.unit[pair] = 1.f / by;
-    uint16_t* to = f.sides + pair * (kParts * 2 * D) + j;
+    const int row = (int)(pair / c.heads), h = (int)(pair % c.heads);
+    int first, count;
+    const int b = kv_sequence(c, row, first, count);
+    if (b < 0 || row - first >= f.a.max_new) return;
+    const int64_t tile = (int64_t)h * f.tiles + score_tile(first, b) + (row - first) / 16;
+    const int i = (row - first) % 16;
+    if (piece == 0) f.unit[tile * 16 + i] = 1.f / by;
+    uint16_t* to = f.sides + (tile * (kParts * 2 * D / 32) + j / 32) * 512 + (j % 32 / 8 * 16 + i) * 8;
 #pragma unroll
     for (int side = 0; side < 2; ++side)
 #pragma unroll
@@ -150,7 +161,7 @@ __global__ __launch_bounds__(256) void k_kv_sides(ScoreArgs f) {
                 x[side][e] -= kv_to_float<bf>(w[e / 2] & 0xffff);
                 x[side][e + 1] -= kv_to_float<bf>(w[e / 2] >> 16);
             }
-            *reinterpret_cast<uintx4*>(to + (part * 2 + side) * D) = w;
+            *reinterpret_cast<uintx4*>(to + (part * 2 + side) * (D / 32) * 512) = w;
         }
 }
 
@@ -172,51 +183,61 @@ __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
     const int col0 = ((int)blockIdx.y * 4 + wave) * 16 * kTiles;
     if (col0 >= c.columns) return;
     uint32_t known[kTiles];
+    int32_t id[kTiles];
     uintx4 box[kTiles][kSteps];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
         const int col = col0 + 16 * t + n;                                 // this lane's page
-        const int32_t id = col < c.columns && col <= (base + count - 1) >> c.page_log2 ? c.table[(int64_t)b * c.table_stride + col] : -1;
-        const bool there = (uint32_t)id < (uint32_t)c.pages;
+        id[t] = c.table[(int64_t)b * c.table_stride + (col < c.columns ? col : 0)];
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const bool there = (uint32_t)id[t] < (uint32_t)c.pages && col0 + 16 * t + n < c.columns;
         known[t] = (uint32_t)__ballot(there) & 0xffffu;
-        const uint16_t* p = f.digests + ((int64_t)(there ? id : 0) * c.heads + h) * (2 * D) + 8 * g;
+        const uint16_t* p = f.digests + ((int64_t)(there ? id[t] : 0) * c.heads + h) * (2 * D) + 8 * g;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) box[t][k] = *reinterpret_cast<const uintx4*>(p + 32 * k);
     }
-    const int last = rt0 + f.each < f.row_tiles ? rt0 + f.each : f.row_tiles;
-    for (int rt = rt0; rt < last && 16 * rt < count; ++rt) {
-        const int rows = count - 16 * rt < 16 ? count - 16 * rt : 16, row = first + 16 * rt + (n < rows ? n : 0);
-        const int64_t pair = (int64_t)row * c.heads + h;
+    int last = rt0 + f.each < f.row_tiles ? rt0 + f.each : f.row_tiles;
+    if (last > (count + 15) / 16) last = (count + 15) / 16;
+    // A tile's operands are asked for while the tile before is worked on, part by part (left alone the compiler asks for one ahead and waits).
+    const int64_t tile0 = (int64_t)h * f.tiles + score_tile(first, b);
+    uintx4 w[kParts][kSteps];
+    auto ask = [&](int part, int64_t tile) __attribute__((always_inline)) {
+        const uint16_t* p = f.sides + (tile * kParts + part) * (kSteps * 512) + lane * 8;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) w[part][k] = *reinterpret_cast<const uintx4*>(p + 512 * k);
+    };
+#pragma unroll
+    for (int part = 0; part < kParts; ++part) ask(part, tile0 + rt0);
+    for (int rt = rt0; rt < last; ++rt) {
+        const int rows = count - 16 * rt < 16 ? count - 16 * rt : 16;
+        const int64_t next = tile0 + (rt + 1 < last ? rt + 1 : rt);
+        const float mine = f.unit[(tile0 + rt) * 16 + n];
         floatx4 acc[kTiles];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-        if (col0 <= (base + 16 * rt + rows - 1) >> c.page_log2) {          // any of the rows reaches these pages
-            const uint16_t* p = f.sides + pair * (kParts * 2 * D) + 8 * g;
 #pragma unroll
-            for (int part = 0; part < kParts; ++part)
+        for (int part = 0; part < kParts; ++part) {
 #pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    const uintx4 w = *reinterpret_cast<const uintx4*>(p + part * 2 * D + 32 * k);
+            for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) acc[t] = kv_mfma16<F>(box[t][k], w, acc[t]);
-                }
+                for (int t = 0; t < kTiles; ++t) acc[t] = kv_mfma16<F>(w[part][k], box[t][k], acc[t]);
+            __builtin_amdgcn_sched_barrier(0);
+            ask(part, next);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (n >= rows) continue;
-        const float unit = f.unit[pair];
-        const int reach = (base + 16 * rt + n) >> c.page_log2;             // a position under zero reaches column -1
+        // register r: row 4 g + r, page n: sixteen neighbouring scores a row (four a lane, of one row, were stored at a third of the speed:
+        // rows begin at any multiple of four bytes)
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            const int col = col0 + 16 * t + 4 * g;
-            float* out = f.scores + pair * c.columns + col;
-            floatx4 v;
+        for (int r = 0; r < 4; ++r) {
+            const int i = 4 * g + r, reach = (base + 16 * rt + i) >> c.page_log2;          // a position under zero reaches column -1
+            const float unit = __shfl(mine, i);
+            float* out = f.scores + ((int64_t)(first + 16 * rt + i) * c.heads + h) * c.columns + col0 + n;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = col + r <= reach && (known[t] >> (4 * g + r) & 1) ? acc[t][r] * unit : -INFINITY;
-            if (col + 3 < c.columns) {
-                __builtin_memcpy(out, &v, 16);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 3; ++r)
-                    if (col + r < c.columns) out[r] = v[r];
+            for (int t = 0; t < kTiles; ++t) {
+                const int col = col0 + 16 * t + n;
+                if (i < rows && col < c.columns) out[16 * t] = col <= reach && (known[t] >> n & 1) ? acc[t][r] * unit : -INFINITY;
             }
         }
     }
@@ -491,8 +512,8 @@ struct PickWork {
     int32_t col_tiles, splits;
 };
 PickWork pick_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int page, int columns, int count);
-struct ScoreWork { int64_t z, zn, sides, unit, bytes; };
-ScoreWork score_work(int format, int d, int64_t rows, int q_heads, int kv_heads, bool one);
+struct ScoreWork { int64_t z, zn, sides, unit, bytes; int32_t tiles; };
+ScoreWork score_work(int format, int d, int batch, int64_t rows, int q_heads, int kv_heads, bool one);
 
 // 16-row tiles that a workgroup rotates, and workgroups (as kv_attend_launch).
 template <int D>
@@ -505,11 +526,11 @@ void rotate_queries(const KvAttend& a, uint16_t* z, float* zn, hipStream_t st) {
 template <int F, int D>
 hipError_t kv_score_launch(const KvAttend& a, const void* digests, float* scores, hipStream_t st) {
     const bool one = a.max_new == 1;
-    const ScoreWork w = score_work(F, D, a.q.rows, a.q.heads, a.c.heads, one);
+    const ScoreWork w = score_work(F, D, a.c.batch, a.q.rows, a.q.heads, a.c.heads, one);
     uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
     float* zn = reinterpret_cast<float*>(a.work + w.zn);
     if constexpr (F == IVFTQ_KV_CODE4) rotate_queries<D>(a, z, zn, st);
-    ScoreArgs f{a, static_cast<const uint16_t*>(digests), scores, z, zn, reinterpret_cast<uint16_t*>(a.work + w.sides), reinterpret_cast<float*>(a.work + w.unit), (a.max_new + 15) / 16, 1};
+    ScoreArgs f{a, static_cast<const uint16_t*>(digests), scores, z, zn, reinterpret_cast<uint16_t*>(a.work + w.sides), reinterpret_cast<float*>(a.work + w.unit), w.tiles, (a.max_new + 15) / 16, 1};
     const int64_t pairs = (int64_t)a.c.rows * a.c.heads;
     if (one) {
         constexpr int pages = 4 * (D <= 128 ? 32 : 16);
@@ -519,8 +540,8 @@ hipError_t kv_score_launch(const KvAttend& a, const void* digests, float* scores
     k_kv_sides<F, D><<<kv_grid((pairs + 7) / 8, 256), 256, 0, st>>>(f);
     constexpr int pages = 4 * 16 * (D <= 128 ? 2 : 1);
     const unsigned blocks = (unsigned)((a.c.columns + pages - 1) / pages);
-    // row tiles of a workgroup, which reads its digests once for them: as many as leave four workgroups a compute unit
-    const int64_t wgs = (int64_t)a.c.batch * a.c.heads * f.row_tiles * blocks / 1024;
+    // row tiles of a workgroup, which reads its digests once for them: as many as leave two workgroups a compute unit
+    const int64_t wgs = (int64_t)a.c.batch * a.c.heads * f.row_tiles * blocks / 512;
     f.each = wgs < 1 ? 1 : (wgs < f.row_tiles ? (int)wgs : f.row_tiles);
     k_kv_score<F, D><<<kv_grid((int64_t)a.c.batch * a.c.heads * ((f.row_tiles + f.each - 1) / f.each), 256, blocks), 256, 0, st>>>(f);
     return hipGetLastError();
