@@ -138,7 +138,7 @@ ivftq_status ivftq_kv_select(const float* scores, const int32_t* lengths, const 
 ivftq_status ivftq_kv_attend_pages(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse,
                                    const int32_t* starts, int32_t max_new, const int32_t* chosen, int32_t count, float scale,
                                    void* workspace, int64_t workspace_bytes, void* stream);
-/* -1 for arguments that ivftq_kv_attend_pages refuses. */
+/* -1 for arguments that ivftq_kv_attend_pages refuses.  (starts NULL: of max_new = 1) */
 int64_t ivftq_kv_attend_pages_workspace(const ivftq_kv_cache* cache, int64_t rows, int32_t q_heads, int32_t max_new, int32_t count);
 
 /* ---- pages ------------------------------------------------------------------------------

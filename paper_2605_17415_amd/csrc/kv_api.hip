@@ -69,12 +69,21 @@ hipError_t launch_kv_attend(const KvAttend& a, const KvWork& w, int d, int forma
     }
 }
 
-PickWork pick_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int page, int columns, int count) {
+PickWork pick_work(const ivftq_kv_cache& c, int64_t rows, int q_heads, int max_new, int count) {
     PickWork w{};
+    const int format = c.format, d = c.d, group = q_heads / c.heads;
     const int64_t all = rows * q_heads;
-    w.col_tiles = (q_heads / kv_heads + 15) / 16;
+    w.col_tiles = (group + 15) / 16;
+    // Rows of a unit: their heads fill a product's columns, their columns' bits and their lists 16 KB and 4,096 places.
+    w.words = (c.columns + 31) / 32;
+    w.tokens = group < 16 ? 16 / group : 1;
+    if (w.tokens > max_new) w.tokens = max_new;
+    while (w.tokens > 1 && ((int64_t)w.tokens * w.words > 4096 || (int64_t)w.tokens * count > kMostPicks)) --w.tokens;
+    if (w.tokens == 1) w.words = 0;
+    w.list = w.tokens * count < c.columns || w.tokens == 1 ? w.tokens * count : c.columns;
+    w.units = (int32_t)(w.tokens == 1 ? rows : rows / w.tokens + c.batch);
     // as many workgroups as the chip holds, but four tiles for each: one for each of its wavefronts
-    const int64_t pairs = rows * kv_heads * w.col_tiles, most = (int64_t)(count < columns ? count : columns) * page / kFewTile / 4;
+    const int64_t pairs = (int64_t)w.units * c.heads * w.col_tiles, most = (int64_t)(count < c.columns ? count : c.columns) * c.page / kFewTile / 4;
     int64_t splits = pairs ? 256 * (d <= 64 ? 4 : (d <= 128 ? 3 : 1)) / pairs : 1;
     splits = splits < most ? splits : most;
     w.splits = (int)(splits < 1 ? 1 : (splits < 64 ? splits : 64));
@@ -458,7 +467,7 @@ int64_t ivftq_kv_attend_pages_workspace(const ivftq_kv_cache* cache, int64_t row
         refuse(IVFTQ_INVALID_ARG, "max_new = %d, count = %d: 1 to %d", max_new, count, kMostPicks);
         return -1;
     }
-    return pick_work(cache->format, cache->d, cache->heads, rows, q_heads, cache->page, cache->columns, count).bytes;
+    return pick_work(*cache, rows, q_heads, max_new < rows ? max_new : (rows > 1 ? (int32_t)rows : 1), count).bytes;
 }
 ivftq_status ivftq_kv_attend_pages(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const ivftq_kv_rows* out, float* lse, const int32_t* starts,
                                    int32_t max_new, const int32_t* chosen, int32_t count, float scale, void* workspace, int64_t workspace_bytes, void* stream) {
@@ -471,9 +480,9 @@ ivftq_status ivftq_kv_attend_pages(const ivftq_kv_cache* cache, const ivftq_kv_r
     if (!q->rows || !cache->batch) return IVFTQ_OK;
     if (!chosen || !aligned(chosen, 4)) return refuse(IVFTQ_INVALID_ARG, "chosen is NULL or not 4-byte aligned");
     if (cache->format != IVFTQ_KV_CODE4 && q->data == out->data) return refuse(IVFTQ_INVALID_ARG, "out stands where q does: only a cache of codes allows that");
-    const PickWork w = pick_work(cache->format, cache->d, cache->heads, q->rows, q->heads, cache->page, cache->columns, count);
-    if (ivftq_status e = check_work(workspace, workspace_bytes, w.bytes)) return e;
     KvAttend a = attend_of(*cache, *q, starts, max_new, workspace);
+    const PickWork w = pick_work(*cache, q->rows, q->heads, a.max_new, count);
+    if (ivftq_status e = check_work(workspace, workspace_bytes, w.bytes)) return e;
     a.out = rows_of(*out);
     a.lse = lse;
     a.scale = scale;

@@ -144,6 +144,7 @@ struct FewPlace {
     const char *r0, *r1;
     bool there0, there1;
     int apart;                        // chosen pages of 16: tokens between the tile's halves
+    uint32_t by0, by1;                // chosen pages: the new rows that have chosen them, a bit each
 };
 struct FewTable {                     // one pair's way into the cache
     const int32_t* row;
@@ -228,6 +229,7 @@ struct FewQuery {
     uintx4 q[D / 32], low[LOW ? D / 32 : 1];
     float gain;
     int pos, begin;                   // its position, the first token of its window
+    uint32_t bit;                     // of its row among the new ones
 };
 
 // The lowest n of eight bits.
@@ -239,6 +241,7 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int cols = s.count * a.group, col = col0 + n < cols ? col0 + n : 0, tok = a.max_new == 1 ? 0 : col / a.group;
     x.pos = col0 + n < cols ? s.base + tok : s.end - 1;
+    x.bit = 1u << (tok & 31);
     const int64_t low = a.window ? (int64_t)x.pos - a.window + 1 : 0;
     x.begin = low > 0 ? (int)low : 0;
     // scores are multiplied by a factor above zero, so that their maximum is that of the products: a negative scale turns the
@@ -264,8 +267,9 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
 }
 
 // A tile into the running maximum m, sum l (of this lane's tokens) and sums o (transposed: o[blk][r] = coordinate
-// 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).  APART: the tile's halves need not follow one another.
-template <int F, int D, bool LOW, bool APART = false>
+// 16 blk + 4 g + r, or (4 g + r) * D / 16 + blk for codes).  CHOSEN: of chosen pages, halves that need
+// not follow one another and that not every row has chosen.
+template <int F, int D, bool LOW, bool CHOSEN = false>
 __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, const FewQuery<F, D, LOW>& q, const FewPlace& at, FewTile<F, D>& x, float& m,
                                          float& l, floatx4 (&o)[D / 16]) {
     const KvView& c = a.c;
@@ -294,14 +298,15 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
         for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3];
     }
     // every token of the tile visible to every row?
-    const bool full = at.there0 && at.there1 && t0 + (APART ? at.apart : 0) + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks);
+    const bool full = at.there0 && at.there1 && t0 + (CHOSEN ? at.apart : 0) + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks) &&
+                      (!CHOSEN || (at.by0 & at.by1) + 1 == 1u << s.count);
     uint32_t shown = 0xff;                  // of the lane's eight tokens: those that any row sees
     if (!full) {
         // bits and selects only: what the compiler makes of conditions here was found to be wrong
-        const int tb = t0 + 8 * g + (APART && g >> 1 ? at.apart : 0);
+        const int tb = t0 + 8 * g + (CHOSEN && g >> 1 ? at.apart : 0);
         const uint32_t there = (g >> 1 ? at.there1 : at.there0) ? 0xffu : 0u, sinks = few_below(a.sinks - tb);
         shown = few_below(s.end - tb) & (~few_below(s.low - tb) | sinks) & there;
-        const uint32_t mine = few_below(q.pos + 1 - tb) & (~few_below(q.begin - tb) | sinks) & shown;
+        const uint32_t mine = few_below(q.pos + 1 - tb) & (~few_below(q.begin - tb) | sinks) & shown & (CHOSEN ? ((g >> 1 ? at.by1 : at.by0) & q.bit ? 0xffu : 0u) : 0xffu);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sc[e] = mine >> e & 1 ? sc[e] : -INFINITY;
         if constexpr (codes) {                // norms of others may be anything, and 0 * NaN is no zero

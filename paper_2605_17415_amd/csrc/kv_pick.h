@@ -5,9 +5,10 @@
 // the lanes, bound by the digests' bytes.  Several: the sides are made once, in two (bfloat16: three) 16-bit parts, and meet the
 // digests in v_mfma 16x16x32, 16 new rows x 16 pages.
 //
-// Attention: every new row has pages of its own for each key-value head, so a (row, head) pair is what kv_few.h calls a sequence: a
-// workgroup's wavefronts take every fourth tile of 32 tokens of the chosen pages, the query rows are the group's heads.  Where
-// the pairs are few several workgroups share a pair's tiles, and a second kernel joins their parts.
+// Attention: every new row has pages of its own for each key-value head.  A unit is what kv_few.h calls a sequence: as many neighbouring rows
+// as their heads fill the sixteen columns of a product, and the pages that any of them has chosen (neighbours choose much alike).  A
+// workgroup's wavefronts take every fourth tile of 32 tokens of those; a row that has not chosen a page has it masked.  Where the units are few
+// several workgroups share a unit's tiles, and a second kernel joins their parts.
 #pragma once
 #include "kv_many.h"
 #include "wave_ops.h"
@@ -248,69 +249,148 @@ __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
 constexpr int kMostPicks = 4096;      // pages of a row and head
 
 struct PickArgs {
-    FewArgs f;                        // its KvAttend with max_new = 1: a pair has one new row
+    FewArgs f;                        // its KvAttend with max_new = tokens
     const int32_t* chosen;            // [rows][heads][count]
-    int32_t count, splits, max_new;   // splits: workgroups that share a pair's tiles
+    int32_t count, max_new;
+    int32_t tokens, units;            // new rows of a unit at most; units a head
+    int32_t splits;                   // workgroups that share a unit's tiles
+    int32_t list, words;              // several rows: places of the list, words of a row's bits
 };
 
-// A pair's pages: columns and page numbers in LDS, ascending, without what does not count.
+// What a workgroup works on: up to `tokens` neighbouring rows of a sequence, pos: the first one's position.
+struct PickUnit { int b, row, count, pos; };
+__device__ __forceinline__ PickUnit pick_unit(const PickArgs& p, int unit) {
+    const KvView& c = p.f.a.c;
+    int first, count;
+    if (p.tokens == 1) {
+        const int b = kv_sequence(c, unit, first, count);
+        const bool none = b < 0 || unit - first >= p.max_new;
+        return {none ? -1 : b, unit, 1, kv_length(c, b < 0 ? 0 : b) - count + unit - first};
+    }
+    int lo = 0, hi = c.batch;                        // units of sequence b: from starts[b] / tokens + b on, so that no two sequences' units meet
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1, s = kv_int(c.starts, mid);
+        if ((s < 0 ? 0 : s) / p.tokens + mid <= unit) lo = mid; else hi = mid;
+    }
+    kv_new_rows(c, lo, first, count);
+    const int base = kv_length(c, lo) - count, most = count < p.max_new ? count : p.max_new, at = (unit - first / p.tokens - lo) * p.tokens;
+    return {at < 0 || at >= most ? -1 : lo, first + at, most - at < p.tokens ? most - at : p.tokens, base + at};
+}
+
+// A unit's pages in LDS, ascending: columns and page numbers, and which rows have chosen them.
 struct Picked { int n, tiles; };
-__device__ __forceinline__ Picked pick_list(const PickArgs& p, int b, int64_t pair, int pos, int2* list) {
+struct PickList { int2* page; uint16_t* by; uint32_t* bits; };
+__device__ __forceinline__ PickList pick_lds(const PickArgs& p, int2* at) {
+    uint16_t* by = reinterpret_cast<uint16_t*>(at + p.list);
+    return {at, by, reinterpret_cast<uint32_t*>(by + ((p.list + 1) & ~1))};
+}
+// The entries of a row's list that count, 64 at a time, by a wavefront: f(column, whether the lane has one).
+template <class Each>
+__device__ __forceinline__ void pick_entries(const PickArgs& p, int64_t pair, int pos, Each&& f) {
+    const KvView& c = p.f.a.c;
+    const int lane = threadIdx.x & 63;
+    int top = -1;
+    for (int i0 = 0; i0 < p.count; i0 += 64) {
+        const int col = i0 + lane < p.count ? p.chosen[pair * p.count + i0 + lane] : -1;
+        int most = col;                              // of the entries up to this one
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(most, o); if (lane >= o) most = most > u ? most : u; }
+        const int prev = __shfl_up(most, 1), before = lane && prev > top ? prev : top;
+        f(col, col > before && col < c.columns && (int64_t)col << c.page_log2 <= pos);
+        const int last = __shfl(most, 63);
+        top = top > last ? top : last;
+    }
+}
+__device__ __forceinline__ Picked pick_list(const PickArgs& p, const PickUnit& unit, int h, const PickList& list) {
     const KvView& c = p.f.a.c;
     __shared__ int many;
-    if (kv_wave() == 0) {
-        const int lane = threadIdx.x;
-        int top = -1, n = 0;
-        for (int i0 = 0; i0 < p.count; i0 += 64) {
-            const int col = i0 + lane < p.count ? p.chosen[pair * p.count + i0 + lane] : -1;
-            int most = col;                          // of the entries up to this one
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(most, o); if (lane >= o) most = most > u ? most : u; }
-            const int prev = __shfl_up(most, 1), before = lane && prev > top ? prev : top;
-            bool in = col > before && col < c.columns && (int64_t)col << c.page_log2 <= pos;
-            const int32_t id = in ? c.table[(int64_t)b * c.table_stride + col] : -1;
-            in = (uint32_t)id < (uint32_t)c.pages;
-            const uint64_t all = __ballot(in);
-            if (in) list[n + __popcll(all & ((1ull << lane) - 1))] = make_int2(col, id);
-            n += __popcll(all);
-            const int last = __shfl(most, 63);
-            top = top > last ? top : last;
+    const int lane = threadIdx.x & 63, wave = kv_wave();
+    const int32_t* table = c.table + (int64_t)unit.b * c.table_stride;
+    int n = 0;
+    if (p.tokens == 1) {                             // one row: what names no page is left out too
+        if (wave == 0) {
+            pick_entries(p, (int64_t)unit.row * c.heads + h, unit.pos, [&](int col, bool in) __attribute__((always_inline)) {
+                const int32_t id = in ? table[col] : -1;
+                in = (uint32_t)id < (uint32_t)c.pages;
+                const uint64_t all = __ballot(in);
+                if (in) list.page[n + __popcll(all & ((1ull << lane) - 1))] = make_int2(col, id);
+                n += __popcll(all);
+            });
+            if (lane == 0) many = n;
         }
-        if (lane == 0) many = n;
+        __syncthreads();
+    } else {                                         // several: their columns as bits, put together
+        for (int i = threadIdx.x; i < p.tokens * p.words; i += 256) list.bits[i] = 0;
+        __syncthreads();
+        for (int t = wave; t < unit.count; t += 4)
+            pick_entries(p, (int64_t)(unit.row + t) * c.heads + h, unit.pos + t, [&](int col, bool in) __attribute__((always_inline)) {
+                if (in) atomicOr(&list.bits[t * p.words + (col >> 5)], 1u << (col & 31));
+            });
+        __syncthreads();
+        if (wave == 0) {
+            for (int w0 = 0; w0 < p.words; w0 += 64) {
+                const int w = w0 + lane;
+                uint32_t any = 0;
+                for (int t = 0; t < unit.count; ++t) any |= w < p.words ? list.bits[t * p.words + w] : 0;
+                const int mine = __popc(any), upto = lanes_upto(mine);
+                int at = n + upto - mine;
+                for (; any; any &= any - 1) list.page[at++].x = w * 32 + __builtin_ctz(any);
+                n += __builtin_amdgcn_readlane(upto, 63);
+            }
+            if (lane == 0) many = n;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < many; i += 256) {
+            const int col = list.page[i].x;
+            const int32_t id = table[col];
+            uint32_t by = 0;
+            for (int t = 0; t < unit.count; ++t) by |= (list.bits[t * p.words + (col >> 5)] >> (col & 31) & 1) << t;
+            list.page[i].y = id;
+            list.by[i] = (uint16_t)by;
+        }
+        __syncthreads();
     }
-    __syncthreads();
     Picked x;
     x.n = kv_uniform(many);
     if (c.page < kFewTile) {
         x.tiles = (x.n + 1) / 2;
-    } else {                                         // of the last page, the only one that may end behind the row, what it reaches
+    } else {                                         // of the last page, the only one that may end behind the rows, what they reach
         const int each = c.page / kFewTile;
-        const int left = x.n ? (pos - (kv_uniform(list[x.n - 1].x) << c.page_log2)) / kFewTile + 1 : 0;
+        const int left = x.n ? (unit.pos + unit.count - 1 - (kv_uniform(list.page[x.n - 1].x) << c.page_log2)) / kFewTile + 1 : 0;
         x.tiles = x.n ? (x.n - 1) * each + (left < each ? left : each) : 0;
     }
     return x;
 }
 
 struct PickTable {
-    const int2* list;
+    PickList list;
     const char* head;
     int n, each_log2;                                // pages of 32 and more: log2 of a page's tiles
+    bool several;
+    __device__ __forceinline__ const char* record(const KvView& c, int id, bool& there) const {
+        there = (uint32_t)id < (uint32_t)c.pages;
+        return head + (int64_t)(there ? id : 0) * c.page_bytes;
+    }
     __device__ __forceinline__ FewPlace operator()(const KvView& c, const FewSeq&, int i) const {
         FewPlace p;
         p.apart = 0;
-        p.there0 = p.there1 = true;
+        p.by0 = p.by1 = 1;
         if (c.page < kFewTile) {
-            const int2 x = list[2 * i], y = list[2 * i + 1 < n ? 2 * i + 1 : 2 * i];
+            const int e0 = 2 * i, e1 = 2 * i + 1 < n ? 2 * i + 1 : 2 * i;
+            const int2 x = list.page[e0], y = list.page[e1];
             const int xc = kv_uniform(x.x), yc = kv_uniform(y.x);
             p.t0 = xc * 16;
-            p.there1 = 2 * i + 1 < n;
-            p.apart = p.there1 ? (yc - xc - 1) * 16 : 0;
-            p.r0 = head + (int64_t)kv_uniform(x.y) * c.page_bytes;
-            p.r1 = head + (int64_t)kv_uniform(y.y) * c.page_bytes;
+            p.apart = e1 > e0 ? (yc - xc - 1) * 16 : 0;
+            p.r0 = record(c, kv_uniform(x.y), p.there0);
+            p.r1 = record(c, kv_uniform(y.y), p.there1);
+            p.there1 = p.there1 && e1 > e0;
+            if (several) { p.by0 = (uint32_t)kv_uniform((int)list.by[e0]); p.by1 = (uint32_t)kv_uniform((int)list.by[e1]); }
         } else {
-            const int2 x = list[i >> each_log2];
+            const int2 x = list.page[i >> each_log2];
             p.t0 = (kv_uniform(x.x) << c.page_log2) + (i & ((1 << each_log2) - 1)) * kFewTile;
-            p.r0 = p.r1 = head + (int64_t)kv_uniform(x.y) * c.page_bytes;
+            p.r0 = p.r1 = record(c, kv_uniform(x.y), p.there0);
+            p.there1 = p.there0;
+            if (several) p.by0 = p.by1 = (uint32_t)kv_uniform((int)list.by[i >> each_log2]);
         }
         return p;
     }
@@ -358,27 +438,26 @@ template <int F, int D, bool LOW>
 __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_picked(PickArgs p) {
     constexpr int kPass = D > 128 ? D / 2 : D;                 // coordinates that pass through LDS at a time
     __shared__ float ml[4][16][2];
-    extern __shared__ int2 list[];                             // the pages; when they have been walked, the wavefronts' sums
-    float(*sum)[16][kPass + 1] = reinterpret_cast<float(*)[16][kPass + 1]>(list);
+    extern __shared__ int2 room[];                             // the list of pages; when they have been walked, the wavefronts' sums
+    float(*sum)[16][kPass + 1] = reinterpret_cast<float(*)[16][kPass + 1]>(room);
     const FewArgs& f = p.f;
     const KvAttend& a = f.a;
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, col0 = blockIdx.y * 16;
     const uint32_t wg = kv_workgroup();
-    const int h = (int)(wg % (uint32_t)c.heads), row = (int)(wg / (uint32_t)c.heads % (uint32_t)c.rows), share = (int)(wg / (uint32_t)c.heads / (uint32_t)c.rows);
+    const int h = (int)(wg % (uint32_t)c.heads), at = (int)(wg / (uint32_t)c.heads % (uint32_t)p.units), share = (int)(wg / (uint32_t)c.heads / (uint32_t)p.units);
     if (share >= p.splits) return;
-    int first, count;
-    const int b = kv_sequence(c, row, first, count);
-    if (b < 0 || row - first >= p.max_new) return;
-    const int pos = kv_length(c, b) - count + row - first;
-    const int64_t pair = (int64_t)row * c.heads + h;
-    const Picked picked = pick_list(p, b, pair, pos, list);
+    const PickUnit unit = pick_unit(p, at);
+    if (unit.b < 0) return;
+    const PickList list = pick_lds(p, room);
+    const Picked picked = pick_list(p, unit, h, list);
     FewSeq s{};
-    s.first = row;
-    s.count = 1;
-    s.base = pos;
-    s.end = pos + 1 > 0 ? pos + 1 : 0;
+    s.first = unit.row;
+    s.count = unit.count;
+    s.base = unit.pos;
+    s.end = unit.pos + unit.count > 0 ? unit.pos + unit.count : 0;
     s.beyond = -1;
+    const int cols = unit.count * a.group;
     int from = 0, to = picked.tiles;
     if (p.splits > 1) {
         const int each = ((picked.tiles + p.splits - 1) / p.splits + 3) & ~3;
@@ -389,7 +468,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_pi
     floatx4 o[D / 16];
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) o[k] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const PickTable table{list, c.pool + (int64_t)h * c.head_bytes, picked.n, c.page_log2 - 5};
+    const PickTable table{list, c.pool + (int64_t)h * c.head_bytes, picked.n, c.page_log2 - 5, p.tokens > 1};
     pick_walk<F, D, LOW>(f, s, table, h, col0, from + wave, to, m, l, o);
     l = kv_sum4(l);
     if (g == 0) { ml[wave][n][0] = m; ml[wave][n][1] = l; }
@@ -410,7 +489,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_pi
         __syncthreads();
         for (int i = threadIdx.x; i < 16 * (kPass / 2); i += 256) {
             const int q = i / (kPass / 2), j = i % (kPass / 2) * 2, col = col0 + q;
-            if (col >= a.group) break;
+            if (col >= cols) break;
             float tm = -INFINITY, tl = 0.f, u = 0.f, v = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) tm = fmaxf(tm, ml[w][q][0]);
@@ -420,7 +499,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_pi
                 u += sum[w][q][j];
                 v += sum[w][q][j + 1];
             }
-            const int head = h * a.group + col, jj = pass * kPass + j;
+            const int tok = p.tokens == 1 ? 0 : col / a.group, row = unit.row + tok, head = h * a.group + col - tok * a.group, jj = pass * kPass + j;
             if (p.splits == 1) {
                 const float inv = tm == -INFINITY && tl == 0.f ? 0.f : 1.f / tl;
                 if (F == IVFTQ_KV_CODE4) {
@@ -431,7 +510,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_pi
                 }
                 if (a.lse && jj == 0) a.lse[(int64_t)row * a.q.heads + head] = tl > 0.f ? (tm + __builtin_amdgcn_logf(tl)) / kLog2e : (tl == 0.f ? -INFINITY : tl);
             } else {
-                const int64_t slot = (((int64_t)blockIdx.y * c.rows * c.heads + pair) * p.splits + share) * 16 + q;
+                const int64_t slot = ((((int64_t)blockIdx.y * p.units + at) * c.heads + h) * p.splits + share) * 16 + q;
                 *reinterpret_cast<float2*>(f.part + slot * D + jj) = make_float2(u, v);
                 if (jj == 0) *reinterpret_cast<float2*>(f.part_ml + slot * 2) = make_float2(tm, tl);
             }
@@ -440,7 +519,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_pi
     }
 }
 
-// The parts of a pair put together, a workgroup a pair and column tile, a wavefront a row; codes: rotated back, each wavefront a block
+// The parts of a unit put together, a workgroup a unit and column tile, a wavefront a row; codes: rotated back, each wavefront a block
 // of 32 coordinates.
 template <int F, int D>
 __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
@@ -451,13 +530,20 @@ __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, col0 = blockIdx.y * 16;
     const uint32_t wg = kv_workgroup();
-    const int h = (int)(wg % (uint32_t)c.heads), row = (int)(wg / (uint32_t)c.heads);
-    if (row >= c.rows) return;
-    int first, count;
-    if (kv_sequence(c, row, first, count) < 0 || row - first >= p.max_new) return;
-    for (int q = wave; q < 16 && col0 + q < a.group; q += 8) {
-        const int head = h * a.group + col0 + q;
-        const int64_t slot0 = (((int64_t)blockIdx.y * c.rows * c.heads + (int64_t)row * c.heads + h) * p.splits) * 16 + q;
+    const int h = (int)(wg % (uint32_t)c.heads), at = (int)(wg / (uint32_t)c.heads);
+    if (at >= p.units) return;
+    const PickUnit unit = pick_unit(p, at);
+    if (unit.b < 0) return;
+    const int cols = unit.count * a.group;
+    auto place = [&](int col, int& row, int& head) __attribute__((always_inline)) {
+        const int tok = p.tokens == 1 ? 0 : col / a.group;
+        row = unit.row + tok;
+        head = h * a.group + col - tok * a.group;
+    };
+    for (int q = wave; q < 16 && col0 + q < cols; q += 8) {
+        int row, head;
+        place(col0 + q, row, head);
+        const int64_t slot0 = ((((int64_t)blockIdx.y * p.units + at) * c.heads + h) * p.splits) * 16 + q;
         // a lane a part's maximum and sum (at most 64 parts)
         float2 u = make_float2(-INFINITY, 0.f);
         if (lane < p.splits) u = *reinterpret_cast<const float2*>(f.part_ml + (slot0 + lane * 16) * 2);
@@ -492,7 +578,7 @@ __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
         __syncthreads();
         if (wave >= D / 32) return;
         const int n = lane & 15, g = lane >> 4;
-        const bool in = col0 + n < a.group;
+        const bool in = col0 + n < cols;
         float x[D / 32][8], y[8];
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
@@ -500,7 +586,9 @@ __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
             for (int e = 0; e < 8; ++e) x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f;
         const float norm = kv_unit_row<D>(x) * c.level_unit;
         KvTurn<D, true>(c.rotation, wave)(x, y);
-        if (in) kv_store_turned(a.out, row, h * a.group + col0 + n, wave, y, norm);
+        int row, head;
+        place(in ? col0 + n : 0, row, head);
+        if (in) kv_store_turned(a.out, row, head, wave, y, norm);
     }
 }
 
@@ -509,9 +597,9 @@ __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
 // Sizes of the workspaces' parts, as the launches and the caller's questions see them.
 struct PickWork {
     int64_t z, zn, whole, part, ml, bytes;
-    int32_t col_tiles, splits;
+    int32_t col_tiles, splits, tokens, units, list, words;
 };
-PickWork pick_work(int format, int d, int kv_heads, int64_t rows, int q_heads, int page, int columns, int count);
+PickWork pick_work(const ivftq_kv_cache& c, int64_t rows, int q_heads, int max_new, int count);
 struct ScoreWork { int64_t z, zn, sides, unit, bytes; int32_t tiles; };
 ScoreWork score_work(int format, int d, int batch, int64_t rows, int q_heads, int kv_heads, bool one);
 
@@ -560,18 +648,20 @@ hipError_t kv_picked_launch(const KvAttend& a, const PickWork& w, const int32_t*
     uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
     float *zn = reinterpret_cast<float*>(a.work + w.zn), *whole = reinterpret_cast<float*>(a.work + w.whole);
     if constexpr (F == IVFTQ_KV_CODE4) rotate_queries<D>(a, z, zn, st);
-    PickArgs p{FewArgs{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), reinterpret_cast<float*>(a.work + w.ml), 0, 0}, chosen, count, w.splits, a.max_new};
-    p.f.a.max_new = 1;
-    const int64_t pairs = (int64_t)a.q.rows * a.c.heads;
-    const dim3 grid = kv_grid(pairs * w.splits, 256, (unsigned)w.col_tiles);
+    PickArgs p{FewArgs{a, z, zn, whole, reinterpret_cast<float*>(a.work + w.part), reinterpret_cast<float*>(a.work + w.ml), 0, 0}, chosen, count, a.max_new, w.tokens, w.units,
+               w.splits, w.list, w.words};
+    p.f.a.max_new = w.tokens;
+    const int64_t units = (int64_t)w.units * a.c.heads;
+    const dim3 grid = kv_grid(units * w.splits, 256, (unsigned)w.col_tiles);
     // float16 results: the queries' second part matters beside the rounding of the result
     constexpr bool codes = F == IVFTQ_KV_CODE4;
     constexpr int sums = 4 * 16 * ((D > 128 ? D / 2 : D) + 1) * 4;
-    const unsigned lds = (unsigned)(count * 8 > sums ? count * 8 : sums);
+    const int pages = w.list * 8 + (w.list + 1) / 2 * 4 + w.tokens * w.words * 4;
+    const unsigned lds = (unsigned)(pages > sums ? pages : sums);
     if (codes && a.q.type == IVFTQ_KV_F16) k_kv_picked<F, D, codes><<<grid, 256, lds, st>>>(p);
     else k_kv_picked<F, D, false><<<grid, 256, lds, st>>>(p);
     if (w.splits > 1) {
-        k_kv_picked_join<F, D><<<kv_grid(pairs, 512, (unsigned)w.col_tiles), 512, 0, st>>>(p);
+        k_kv_picked_join<F, D><<<kv_grid(units, 512, (unsigned)w.col_tiles), 512, 0, st>>>(p);
     } else if constexpr (codes) {
         const ManyArgs f{a, z, zn, whole, nullptr, nullptr, nullptr, 0, 0};
         const int64_t all = (int64_t)a.q.rows * a.q.heads, fill = all / (16 * 768);

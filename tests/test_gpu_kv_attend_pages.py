@@ -151,6 +151,51 @@ def test_no_numbers_where_nobody_looks(form, kind):
 
 
 @pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("page", (16, 32))
+def test_no_numbers_in_a_neighbours_page(form, kind, page):
+    """Neighbouring rows are worked on together: what one of them has chosen may be anything to the others."""
+    n, new = 9 * page, 8
+    c = ref.Cache(7, form, 1, 64, page, [n], spare=2)
+    q = queries(7, new, 2, 64, ref.TYPES[kind])
+    chosen = np.full((new, 1, 5), -1, np.int32)
+    for r in range(new):
+        chosen[r, 0, :4] = [0, 2 + r % 3, 5, 8]
+    chosen[3, 0] = [0, 1, 2, 7, 8]                          # page 1 and page 7 are row 3's alone, page 6 is nobody's
+    want, _ = run(c, q, chosen, [new])
+    t, codec = c.device()
+    for col in (1, 6, 7):
+        p = int(c.table[0, col])
+        t["pool"][p] = 255 if form == "code4" else torch.nan
+    got = _pkg().kv_attend_pages(q, t["pool"], t["table"], t["lengths"], torch.from_numpy(chosen).to(DEV), starts=starts_of([new]), max_new=new, **codec)
+    others = [r for r in range(new) if r != 3]
+    assert torch.equal(got[others], want[others]) and not torch.isfinite(got[3].float()).all()
+    if form != "code4":                                     # infinite values, that only row 3 sees
+        clean, _ = c.device()
+        p = int(c.table[0, 7])
+        clean["pool"][p, 0, 1] = torch.inf
+        got = _pkg().kv_attend_pages(q, clean["pool"], t["table"], t["lengths"], torch.from_numpy(chosen).to(DEV), starts=starts_of([new]), max_new=new, **codec)
+        assert torch.equal(got[others], want[others]) and torch.isinf(got[3].float()).all()
+
+
+@pytest.mark.parametrize("form,kind", FORMS[:3])
+@pytest.mark.parametrize("group", (1, 2, 5, 9))
+def test_neighbours_that_choose_alike_and_not(form, kind, group):
+    """Units of 16, 8, 3 and 1 rows; sequences that begin and end inside one, more rows than tokens, columns past a word of bits."""
+    lens, news = [1300, 40, 700, 5], [37, 1, 20, 9]
+    c = ref.Cache(group, form, 2, 64, 16, lens, columns=90)
+    rows = sum(news)
+    q = queries(group, rows, 2 * group, 64, ref.TYPES[kind])
+    rng = np.random.default_rng(group)
+    chosen = np.full((rows, 2, 9), -1, np.int32)
+    for r in range(rows):
+        for h in range(2):
+            own = {0, int(rng.integers(0, 80)), int(rng.integers(0, 80)), 3 + (r + h) // 4, 40 + r % 3, 79}
+            chosen[r, h, : len(own)] = sorted(own)
+    out, lse = run(c, q, chosen, news)
+    pick.check_attention(c, q.cpu(), out, news, chosen, lse)
+
+
+@pytest.mark.parametrize("form,kind", FORMS[:3])
 @pytest.mark.parametrize("scale", (0.0, -0.3, 2.0))
 def test_scale(form, kind, scale):
     c = ref.Cache(4, form, 1, 64, 16, [200, 77])
