@@ -271,7 +271,7 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
 // not follow one another and that not every row has chosen.
 template <int F, int D, bool LOW, bool CHOSEN = false>
 __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, const FewQuery<F, D, LOW>& q, const FewPlace& at, FewTile<F, D>& x, float& m,
-                                         float& l, floatx4 (&o)[D / 16]) {
+                                         float& l, floatx4 (&o)[D / 16], bool careful = true) {
     const KvView& c = a.c;
     constexpr bool codes = F == IVFTQ_KV_CODE4;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, t0 = at.t0;
@@ -298,10 +298,18 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
         for (int e = 0; e < 8; ++e) sc[e] = st[e >> 2][e & 3];
     }
     // every token of the tile visible to every row?
-    const bool full = at.there0 && at.there1 && t0 + (CHOSEN ? at.apart : 0) + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks) &&
-                      (!CHOSEN || (at.by0 & at.by1) + 1 == 1u << s.count);
+    const bool inside = at.there0 && at.there1 && t0 + (CHOSEN ? at.apart : 0) + kFewTile - 1 <= s.base && (t0 > s.beyond || t0 + kFewTile <= a.sinks);
+    const bool full = inside && (!CHOSEN || (at.by0 & at.by1) + 1 == 1u << s.count);
     uint32_t shown = 0xff;                  // of the lane's eight tokens: those that any row sees
-    if (!full) {
+    if (CHOSEN && inside && !full) {        // a row sees all of a half or nothing
+        const bool mine = (g >> 1 ? at.by1 : at.by0) & q.bit;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sc[e] = mine ? sc[e] : -INFINITY;
+        if constexpr (codes) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.vg[e] &= mine ? ~0u : 0u;
+        }
+    } else if (!full) {
         // bits and selects only: what the compiler makes of conditions here was found to be wrong
         const int tb = t0 + 8 * g + (CHOSEN && g >> 1 ? at.apart : 0);
         const uint32_t there = (g >> 1 ? at.there1 : at.there0) ? 0xffu : 0u, sinks = few_below(a.sinks - tb);
@@ -352,7 +360,7 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
         const uintx4 p = {kv_pack2<bf>(pr[0], pr[1]), kv_pack2<bf>(pr[2], pr[3]), kv_pack2<bf>(pr[4], pr[5]), kv_pack2<bf>(pr[6], pr[7])};
         uint32_t dirty = 0;                 // of the lane's eight tokens: no finite value, and not the same to every row
         if (!full) {
-            if (s.count > 1) {
+            if (s.count > 1 && careful && __ballot(kv_any_not_finite<bf>(x.vv))) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) dirty |= kv_not_finite<bf>(x.vv[k]);
 #pragma unroll
@@ -360,11 +368,13 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
                 dirty &= shown;
                 shown &= ~dirty;
             }
-            uintx4 keep;
+            if (__ballot(shown != 0xff)) {
+                uintx4 keep;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) keep[e] = (shown >> 2 * e & 1 ? 0xffffu : 0u) | (shown >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+                for (int e = 0; e < 4; ++e) keep[e] = (shown >> 2 * e & 1 ? 0xffffu : 0u) | (shown >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) x.vv[k] &= keep;
+                for (int k = 0; k < D / 16; ++k) x.vv[k] &= keep;
+            }
         }
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) o[k] = kv_mfma16<F>(x.vv[k], p, o[k]);

@@ -229,6 +229,22 @@ __device__ __forceinline__ uint32_t kv_not_finite(uintx4 w) {
     return bad;
 }
 
+// Whether any of N times eight is none: the largest exponent tells.
+template <bool BF, int N>
+__device__ __forceinline__ bool kv_any_not_finite(const uintx4 (&w)[N]) {
+    typedef uint16_t two __attribute__((ext_vector_type(2)));
+    constexpr uint32_t top = BF ? 0x7f80u : 0x7c00u;
+    two most = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = w[i][e] & (top << 16 | top);
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(two, bits));
+        }
+    return (most[0] > most[1] ? most[0] : most[1]) == top;
+}
+
 // A value of the lane 16, or 32, lanes away (of the other half of a pair), without the LDS unit: swapping the odd rows of
 // one copy with the even rows of another leaves own and other value in two registers.
 __device__ __forceinline__ void kv_pair16(float v, float& a, float& b) {

@@ -396,11 +396,16 @@ struct PickTable {
     }
 };
 
-// One wavefront's tiles [from, to) in steps of four, as few_walk.
+// One wavefront's tiles [from, to) in steps of four, as few_walk.  careful: values that are no finite numbers, of pages that only some rows have
+// chosen, are looked for in every tile.
 template <int F, int D, bool LOW>
-__device__ __forceinline__ void pick_walk(const FewArgs& f, const FewSeq& s, const PickTable& table, int h, int col0, int from, int to, float& m, float& l,
+__device__ __forceinline__ void pick_walk(const FewArgs& f, const FewSeq& s, const PickTable& table, int h, int col0, int from, int to, bool careful, float& m, float& l,
                                           floatx4 (&o)[D / 16]) {
     const KvView& c = f.a.c;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) o[k] = floatx4{0.f, 0.f, 0.f, 0.f};
     if (from >= to) return;
     FewQuery<F, D, LOW> q;
     FewPlace at = table(c, s, from);
@@ -413,7 +418,7 @@ __device__ __forceinline__ void pick_walk(const FewArgs& f, const FewSeq& s, con
         auto step = [&](FewTile<F, D>& now, FewTile<F, D>& then) __attribute__((always_inline)) {      // past the end: a tile that is there, read and not used
             const FewPlace next = table(c, s, i + 4 < to ? i + 4 : i);
             few_load<F, D>(c, next, lane, then);
-            few_step<F, D, LOW, true>(f.a, s, q, at, now, m, l, o);
+            few_step<F, D, LOW, true>(f.a, s, q, at, now, m, l, o, careful);
             at = next;
             i += 4;
         };
@@ -428,7 +433,7 @@ __device__ __forceinline__ void pick_walk(const FewArgs& f, const FewSeq& s, con
             FewTile<F, D> x;
             few_load<F, D>(c, at, lane, x);
             const FewPlace next = table(c, s, i + 4 < to ? i + 4 : i);
-            few_step<F, D, LOW, true>(f.a, s, q, at, x, m, l, o);
+            few_step<F, D, LOW, true>(f.a, s, q, at, x, m, l, o, careful);
             at = next;
         }
     }
@@ -464,12 +469,21 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_pi
         from = share * each;
         to = from + each < to ? from + each : to;
     }
-    float m = -INFINITY, l = 0.f;
+    float m, l;
     floatx4 o[D / 16];
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) o[k] = floatx4{0.f, 0.f, 0.f, 0.f};
     const PickTable table{list, c.pool + (int64_t)h * c.head_bytes, picked.n, c.page_log2 - 5, p.tokens > 1};
-    pick_walk<F, D, LOW>(f, s, table, h, col0, from + wave, to, m, l, o);
+    // The weight of a value that a row does not see is zero, and zero times no finite number is none: only where a sum has become none
+    // are such values looked for, by walking once more (looking in every tile: 64 of some 200 vector instructions).
+    for (bool careful = F == IVFTQ_KV_CODE4 || unit.count == 1;; careful = true) {
+        pick_walk<F, D, LOW>(f, s, table, h, col0, from + wave, to, careful, m, l, o);
+        if (careful) break;
+        float far = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) far = fmaxf(far, __builtin_fabsf(o[k][r])), far = o[k][r] == o[k][r] ? far : INFINITY;
+        if (!__ballot(!(far < INFINITY))) break;
+    }
     l = kv_sum4(l);
     if (g == 0) { ml[wave][n][0] = m; ml[wave][n][1] = l; }
     __syncthreads();
