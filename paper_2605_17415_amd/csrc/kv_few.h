@@ -166,8 +166,13 @@ struct FewTable {                     // one pair's way into the cache
     }
 };
 
+// Key operands in 16 bits as they are read by default: sixteen lanes side by side read sixteen rows, which is a cache access a lane.
+// QUADS (heads of 128 and 256): four lanes read 64 neighbouring bytes of a row and exchange what they have read, a quarter of the accesses for 64
+// or 128 vector instructions a tile; worth it where pages come from the L2.
+template <int F, int D> constexpr bool kQuads = F != IVFTQ_KV_CODE4 && D % 128 == 0;
+
 // Byte offsets of a lane's reads inside a tile of one page.
-template <int F, int D>
+template <int F, int D, bool QUADS = false>
 struct FewLane {
     uint32_t key, value, norm;
     __device__ __forceinline__ explicit FewLane(const KvView& c) {
@@ -178,15 +183,15 @@ struct FewLane {
             value = c.page * (D / 2) + g * (D * 4) + n * (D / 4);
             norm = c.page * D + g * 16;
         } else {
-            key = (8 * (n >> 2) + (n & 3)) * (D * 2) + g * 16;
+            key = QUADS ? 8 * (n >> 2) * (D * 2) + (g * (D / 32) + (n & 3)) * 16 : (8 * (n >> 2) + (n & 3)) * (D * 2) + g * 16;
             value = c.page * (D * 2) + (g * D + n) * 16;
             norm = 0;
         }
     }
 };
 
-template <int F, int D>
-__device__ __forceinline__ void few_load(const KvView& c, const FewPlace& p, const FewLane<F, D>& at, FewTile<F, D>& x) {
+template <int F, int D, bool QUADS = false>
+__device__ __forceinline__ void few_load(const KvView& c, const FewPlace& p, const FewLane<F, D, QUADS>& at, FewTile<F, D>& x) {
     constexpr bool codes = F == IVFTQ_KV_CODE4;
     constexpr int row = codes ? D / 2 : D * 2;                        // bytes of a token's row
     const int in = p.t0 & (c.page - 1);
@@ -207,7 +212,7 @@ __device__ __forceinline__ void few_load(const KvView& c, const FewPlace& p, con
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int k = 0; k < D / 32; ++k) x.kk[y][k] = *reinterpret_cast<const uintx4*>(keys + y * 4 * row + k * 64);
+                for (int k = 0; k < D / 32; ++k) x.kk[y][k] = *reinterpret_cast<const uintx4*>(keys + (QUADS ? (4 * y + k % 4) * row + k / 4 * 64 : y * 4 * row + k * 64));
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) x.vv[k] = *reinterpret_cast<const uintx4*>(values + k * 256);
         }
@@ -223,6 +228,24 @@ __device__ __forceinline__ void few_load(const KvView& c, const FewPlace& p, con
     }
 }
 
+// Four lanes side by side: lane b's i-th piece for lane i's b-th.
+__device__ __forceinline__ void few_exchange(uintx4& x0, uintx4& x1, uintx4& x2, uintx4& x3) {
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    auto near = [](uint32_t v) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true); };
+    auto far = [](uint32_t v) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true); };
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        // (every lane takes part in every move: none may stand in a branch)
+        const uint32_t a0 = x0[e], a1 = x1[e], a2 = x2[e], a3 = x3[e], m0 = near(a0), m1 = near(a1), m2 = near(a2), m3 = near(a3);
+        const uint32_t b0 = odd ? m1 : a0, b1 = odd ? a1 : m0, b2 = odd ? m3 : a2, b3 = odd ? a3 : m2;
+        const uint32_t f0 = far(b0), f1 = far(b1), f2 = far(b2), f3 = far(b3);
+        x0[e] = high ? f2 : b0;
+        x1[e] = high ? f3 : b1;
+        x2[e] = high ? b2 : f0;
+        x3[e] = high ? b3 : f1;
+    }
+}
+
 // One query row a lane: its operands, what its scores are multiplied by, its position.
 template <int F, int D, bool LOW>
 struct FewQuery {
@@ -235,7 +258,7 @@ struct FewQuery {
 // The lowest n of eight bits.
 __device__ __forceinline__ uint32_t few_below(int n) { return 0xffu >> (n <= 0 ? 8 : (n >= 8 ? 0 : 8 - n)); }
 
-template <int F, int D, bool LOW>
+template <int F, int D, bool LOW, bool QUADS = false>
 __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int h, int col0, FewQuery<F, D, LOW>& x) {
     const KvAttend& a = f.a;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -259,9 +282,9 @@ __device__ __forceinline__ void few_query(const FewArgs& f, const FewSeq& s, int
             if constexpr (LOW) { x.low[k] = *reinterpret_cast<const uintx4*>(f.z + (all + at) * D + g * (D / 4) + 8 * k); x.low[k] ^= sign; }
         }
     } else {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + 8 * g;
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q.data) + row * a.q.row_stride + head * a.q.head_stride + (QUADS ? g * (D / 4) : 8 * g);
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) { x.q[k] = *reinterpret_cast<const uintx4*>(p + 32 * k); x.q[k] ^= sign; }
+        for (int k = 0; k < D / 32; ++k) { x.q[k] = *reinterpret_cast<const uintx4*>(p + (QUADS ? 8 * k : 32 * k)); x.q[k] ^= sign; }
     }
     x.gain = fmaxf(x.gain, 1e-30f);
 }
@@ -290,6 +313,12 @@ __device__ __forceinline__ void few_step(const KvAttend& a, const FewSeq& s, con
 #pragma unroll
         for (int e = 0; e < 8; ++e) sc[e] = __builtin_fmaf((float)kn[e], st[e & 1][e >> 1], 0.f);        // one v_fma_mix
     } else {
+        if constexpr (CHOSEN && kQuads<F, D>) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int k = 0; k < D / 32; k += 4) few_exchange(x.kk[y][k], x.kk[y][k + 1], x.kk[y][k + 2], x.kk[y][k + 3]);
+        }
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll

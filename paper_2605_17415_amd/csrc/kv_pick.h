@@ -409,15 +409,15 @@ __device__ __forceinline__ void pick_walk(const FewArgs& f, const FewSeq& s, con
     if (from >= to) return;
     FewQuery<F, D, LOW> q;
     FewPlace at = table(c, s, from);
-    few_query<F, D, LOW>(f, s, h, col0, q);
-    const FewLane<F, D> lane(c);
+    few_query<F, D, LOW, kQuads<F, D>>(f, s, h, col0, q);
+    const FewLane<F, D, kQuads<F, D>> lane(c);
     if constexpr (F == IVFTQ_KV_CODE4) {
         FewTile<F, D> x, y;
-        few_load<F, D>(c, at, lane, x);
+        few_load<F, D, kQuads<F, D>>(c, at, lane, x);
         int i = from;
         auto step = [&](FewTile<F, D>& now, FewTile<F, D>& then) __attribute__((always_inline)) {      // past the end: a tile that is there, read and not used
             const FewPlace next = table(c, s, i + 4 < to ? i + 4 : i);
-            few_load<F, D>(c, next, lane, then);
+            few_load<F, D, kQuads<F, D>>(c, next, lane, then);
             few_step<F, D, LOW, true>(f.a, s, q, at, now, m, l, o, careful);
             at = next;
             i += 4;
@@ -431,7 +431,7 @@ __device__ __forceinline__ void pick_walk(const FewArgs& f, const FewSeq& s, con
     } else {
         for (int i = from; i < to; i += 4) {
             FewTile<F, D> x;
-            few_load<F, D>(c, at, lane, x);
+            few_load<F, D, kQuads<F, D>>(c, at, lane, x);
             const FewPlace next = table(c, s, i + 4 < to ? i + 4 : i);
             few_step<F, D, LOW, true>(f.a, s, q, at, x, m, l, o, careful);
             at = next;
