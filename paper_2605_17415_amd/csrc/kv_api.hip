@@ -82,8 +82,8 @@ PickWork pick_work(const ivftq_kv_cache& c, int64_t rows, int q_heads, int max_n
     if (w.tokens == 1) w.words = 0;
     w.list = w.tokens * count < c.columns || w.tokens == 1 ? w.tokens * count : c.columns;
     w.units = (int32_t)(w.tokens == 1 ? rows : rows / w.tokens + c.batch);
-    // as many workgroups as the chip holds, but four tiles for each: one for each of its wavefronts
-    const int64_t pairs = (int64_t)w.units * c.heads * w.col_tiles, most = (int64_t)(count < c.columns ? count : c.columns) * c.page / kFewTile / 4;
+    // as many workgroups as the chip holds, but eight tiles for each, two for each of its wavefronts: the second kernel costs what those do
+    const int64_t pairs = (int64_t)w.units * c.heads * w.col_tiles, most = (int64_t)(count < c.columns ? count : c.columns) * c.page / kFewTile / 8;
     int64_t splits = pairs ? 256 * (d <= 64 ? 4 : (d <= 128 ? 3 : 1)) / pairs : 1;
     splits = splits < most ? splits : most;
     w.splits = (int)(splits < 1 ? 1 : (splits < 64 ? splits : 64));

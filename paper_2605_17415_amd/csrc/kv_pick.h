@@ -289,15 +289,13 @@ template <class Each>
 __device__ __forceinline__ void pick_entries(const PickArgs& p, int64_t pair, int pos, Each&& f) {
     const KvView& c = p.f.a.c;
     const int lane = threadIdx.x & 63;
-    int top = -1;
+    uint32_t top = 0;                                // columns + 1: of the entries before these
     for (int i0 = 0; i0 < p.count; i0 += 64) {
         const int col = i0 + lane < p.count ? p.chosen[pair * p.count + i0 + lane] : -1;
-        int most = col;                              // of the entries up to this one
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(most, o); if (lane >= o) most = most > u ? most : u; }
-        const int prev = __shfl_up(most, 1), before = lane && prev > top ? prev : top;
-        f(col, col > before && col < c.columns && (int64_t)col << c.page_log2 <= pos);
-        const int last = __shfl(most, 63);
+        const uint32_t mine = col < 0 ? 0u : (uint32_t)col + 1, most = lanes_most_upto(mine);
+        const uint32_t prev = __shfl_up(most, 1), before = lane && prev > top ? prev : top;
+        f(col, mine > before && col < c.columns && (int64_t)col << c.page_log2 <= pos);
+        const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)most, 63);
         top = top > last ? top : last;
     }
 }

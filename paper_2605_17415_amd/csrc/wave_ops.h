@@ -65,6 +65,17 @@ __device__ __forceinline__ T lanes_upto(T v) {
     return v;
 }
 
+// The largest of the lanes up to this one (not negative).
+__device__ __forceinline__ uint32_t lanes_most_upto(uint32_t v) {
+    auto most = [](uint32_t a, uint32_t b) __attribute__((always_inline)) { return a > b ? a : b; };
+    v = most(v, lane_moved<0x111>(v));
+    v = most(v, lane_moved<0x112>(v));
+    v = most(v, lane_moved<0x114>(v));
+    v = most(v, lane_moved<0x118>(v));
+    v = most(v, lane_moved<0x142, 0xa>(v));
+    return most(v, lane_moved<0x143, 0xc>(v));
+}
+
 struct Larger { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a > b ? a : b; } };
 struct Smaller { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a < b ? a : b; } };
 struct Sum { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a + b; } };
