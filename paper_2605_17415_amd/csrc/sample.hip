@@ -1,6 +1,6 @@
 // The next token of each row from its logits.  No row is sorted: what decides is always within a short list of tokens, whose ranks are counted.
 //   - k_sample_tops reads the logits once and leaves the largest one of every 4,096 tokens (a chunk) and of every 64 (a group).
-//   - Few ranks are kept (top_k up to 256): at least k tokens are not under the k-th largest group maximum, so the tokens not under it, a
+//   - Few ranks are kept (top_k up to 1,024): at least k tokens are not under the k-th largest group maximum, so the tokens not under it, a
 //     little more than k of them in as few groups, are the list (k_sample_rows).
 //   - Otherwise a second reading (k_sample_chunks) adds up the weights of every chunk, and where a rank is looked for by its number or its mass, of
 //     2,048 bins of logits.  k_sample_rows finds the bins in which the two ranks lie; a third reading (k_sample_bins) lists their tokens, and
@@ -34,7 +34,7 @@ constexpr int kMostTokens = 1 << 20;
 constexpr double kUnit = 4398046511104.0;        // 2^42
 
 constexpr int kChunk = 4096, kGroup = 64, kGroups = kChunk / kGroup;
-constexpr int kFewRanks = 256;                   // top_k that goes by the groups
+constexpr int kFewRanks = 1024;                  // top_k that goes by the groups
 constexpr int kList = 2048;                      // tokens of a list
 constexpr int kBins = 2048;
 constexpr int kSliceRows = 1024;                 // rows that share a workspace's places
@@ -476,10 +476,13 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
     const Weights weight(x.top, how.temperature, table);
     if (how.way == kAll) {
         uint64_t sum = 0;
+        // a logit whose weight is surely too small: the logarithm and its product are good to 2^-20 of themselves
+        const float under = how.least > 0.0 ? x.top + how.temperature * (1.000002f * logf((float)how.least)) - __builtin_fabsf(x.top) * 1e-6f : -INFINITY;
 #pragma unroll
         for (int j = 0; j < kEach; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                if (!__ballot(v[j][e] >= under)) continue;
                 const double w = weight(v[j][e]);
                 sum += w >= how.least ? Weights::whole(w) : 0;
             }
@@ -695,22 +698,45 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     }
     __syncthreads();
     const int chosen = (int)s.many;
-    __syncthreads();
-    if (threadIdx.x == 0) s.many = 0;
-    __syncthreads();
-    for (int u = threadIdx.x >> 6; u < chosen; u += kWaves) {
-        const int i = s.groups[u] * kGroup + lane;
-        const float v = i < a.vocabulary ? logit<T>(row, i) : -INFINITY;
-        const bool in = v > -INFINITY && bins(v) <= cut_bin;
-        const uint64_t which = __ballot(in);
-        uint32_t begin = 0;
-        if (lane == 0) begin = atomicAdd(&s.many, (uint32_t)__popcll(which));
-        const uint32_t at = __shfl(begin, 0) + (uint32_t)__popcll(which & ((1ull << lane) - 1));
-        if (in && at < kList) s.rank[at] = rank_of(v, i);
+    // their tokens, a group a wavefront at a time: f(token, logit, bin, whether it may be among the first k)
+    auto tokens = [&](auto&& f) __attribute__((always_inline)) {
+        for (int u = threadIdx.x >> 6; u < chosen; u += kWaves) {
+            const int i = s.groups[u] * kGroup + lane;
+            const float v = i < a.vocabulary ? logit<T>(row, i) : -INFINITY;
+            const int bin = v > -INFINITY ? bins(v) : 1024;
+            f(i, v, bin, bin <= cut_bin);
+        }
+    };
+    auto list = [&](int last_bin) __attribute__((always_inline)) {
+        __syncthreads();
+        if (threadIdx.x == 0) s.many = 0;
+        __syncthreads();
+        tokens([&](int i, float v, int bin, bool) __attribute__((always_inline)) {
+            const bool in = bin <= last_bin;
+            const uint64_t which = __ballot(in);
+            uint32_t begin = 0;
+            if (lane == 0 && which) begin = atomicAdd(&s.many, (uint32_t)__popcll(which));
+            const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)begin) + (uint32_t)__popcll(which & ((1ull << lane) - 1));
+            if (in && at < kList) s.rank[at] = rank_of(v, i);
+        });
+        __syncthreads();
+        return (int)s.many;
+    };
+    int n = list(cut_bin);
+    if (n > kList) {                               // large logits stand together: the bin of the k-th one, counted
+        __syncthreads();
+        s.counts[threadIdx.x] = 0;
+        if (threadIdx.x == 0) s.value[0] = 1023;
+        __syncthreads();
+        tokens([&](int, float, int bin, bool in) __attribute__((always_inline)) { if (in) atomicAdd(&s.counts[bin], 1u); });
+        __syncthreads();
+        uint64_t total;
+        const uint64_t here = s.counts[threadIdx.x], so_far = scan(here, s.sums, total);
+        if (so_far >= (uint64_t)how.k && so_far - here < (uint64_t)how.k) s.value[0] = threadIdx.x;
+        __syncthreads();
+        n = list((int)s.value[0]);
+        if (n > kList) return false;
     }
-    __syncthreads();
-    const int n = (int)s.many;
-    if (n > kList) return false;
     uint64_t rank[kHeld], amount[kHeld], place[kHeld], mixed = 0, sum = 0;
     double w[kHeld];
     const uint64_t any = s.rank[0];

@@ -291,7 +291,7 @@ def _digests(digests, pool, d):
     if digests.requires_grad:
         _no_gradient(digests, "digests")
     kind = torch.float16 if pool.dtype == torch.uint8 else pool.dtype
-    if digests.dtype != kind or tuple(digests.shape) != (pool.shape[0], pool.shape[1], 2, d) or not digests.is_contiguous():
+    if digests.dtype != kind or digests.shape != (*pool.shape[:2], 2, d) or not digests.is_contiguous():
         raise ValueError(f"digests must be a contiguous tensor of pages x heads x 2 x {d} in {kind}, got {tuple(digests.shape)} in {digests.dtype}")
     return digests.data_ptr()
 
@@ -300,7 +300,7 @@ def _floats(t, name, like, shape):
     _on_device(t, name, like)
     if t.requires_grad:
         _no_gradient(t, name)
-    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor of {tuple(shape)}, got {tuple(t.shape)} in {t.dtype}")
     return t.data_ptr()
 
@@ -363,7 +363,7 @@ def kv_select(scores, lengths, page, count, starts=None, first=1, last=1, out=No
 
 def _columns(t, name, like, shape):
     _on_device(t, name, like)
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of {tuple(shape)}, got {tuple(t.shape)} in {t.dtype}")
     return t.data_ptr()
 

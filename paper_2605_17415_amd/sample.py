@@ -49,13 +49,13 @@ def declared_sample_symbols():
 _pack_logits, _pack_sampling = kv._packer(_Logits), struct.Struct("@PPPPfiff").pack
 
 
-def _setting(v, name, like, dtype):
+def _setting(v, name, like, rows, dtype):
     """(pointer, value): an array with a value for each row, or one value for all."""
     if not isinstance(v, torch.Tensor):
         return 0, v
     kv._on_device(v, name, like)
-    if v.dtype != dtype or tuple(v.shape) != (like.shape[0],) or not v.is_contiguous():
-        raise ValueError(f"{name} must be a number or a contiguous {dtype} tensor of ({like.shape[0]},), got {tuple(v.shape)} in {v.dtype}")
+    if v.dtype != dtype or v.shape != (rows,) or not v.is_contiguous():
+        raise ValueError(f"{name} must be a number or a contiguous {dtype} tensor of ({rows},), got {tuple(v.shape)} in {v.dtype}")
     return v.data_ptr(), 0
 
 
@@ -68,18 +68,19 @@ def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out
     (float32; top_k int32).  logprobs (float32 [rows], optional) receives the logarithm of the token's probability among the kept
     ones.  A row without a finite or infinite logit above -inf gives -1."""
     kv._on_device(logits, "logits")
-    for t, name in ((logits, "logits"), (logprobs, "logprobs")):
-        if t is not None and t.requires_grad:
-            kv._no_gradient(t, name)
+    if logits.requires_grad:
+        kv._no_gradient(logits, "logits")
     kind = _TYPES.get(logits.dtype)
     if kind is None:
         raise TypeError(f"logits must be float32, float16 or bfloat16, got {logits.dtype}")
     if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1 and logits.numel()):
         raise ValueError(f"logits must be rows x vocabulary with neighbouring tokens, got {tuple(logits.shape)} with strides {logits.stride()}")
-    rows, where = logits.shape[0], kv._stream(stream, logits)
-    data = _pack_logits(logits.data_ptr(), logits.stride(0) if rows > 1 else logits.shape[1], rows, logits.shape[1], kind)
-    (t, t_all), (k, k_all), (p, p_all), (m, m_all) = (_setting(v, name, logits, dtype) for v, name, dtype in (
-        (temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)))
+    (rows, vocabulary), where = logits.shape, kv._stream(stream, logits)
+    data = _pack_logits(logits.data_ptr(), logits.stride(0) if rows > 1 else vocabulary, rows, vocabulary, kind)
+    t, t_all = _setting(temperature, "temperature", logits, rows, torch.float32)
+    k, k_all = _setting(top_k, "top_k", logits, rows, torch.int32)
+    p, p_all = _setting(top_p, "top_p", logits, rows, torch.float32)
+    m, m_all = _setting(min_p, "min_p", logits, rows, torch.float32)
     how, numbers = _pack_sampling(t, k, p, m, t_all, k_all, p_all, m_all), kv._floats(u, "u", logits, (rows,))
     if out is None:
         out = kv._blank(rows, torch.int32, logits, stream)

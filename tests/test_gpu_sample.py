@@ -178,3 +178,16 @@ def test_more_rows_than_share_a_workspace():
     u = np.float32(0.4) * np.ones(rows, np.float32)
     check(x, u, top_k=30)
     check(x, u, top_p=0.8)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("v", (9000, 140_000))
+def test_large_logits_that_stand_together(kind, v):
+    """A vocabulary in the order of its tokens' frequency: the first few groups hold the largest logits."""
+    g = torch.Generator().manual_seed(v)
+    x = torch.randn(4, v, generator=g) - 3 * torch.log1p(torch.arange(v) / 500.0)
+    x[1] = -torch.arange(v) * 1e-3
+    x[2, 3000:5000] += 30
+    x = x.to(TYPES[kind])
+    for how in (dict(top_k=50), dict(top_k=400, top_p=0.9), dict(top_k=1024), dict(top_k=1000, min_p=0.01), dict(top_k=1025), dict(top_p=0.9), dict(min_p=0.3), dict(min_p=1e-9)):
+        check(x, np.linspace(0.05, 0.95, 4), **how)
