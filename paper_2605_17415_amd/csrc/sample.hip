@@ -668,9 +668,8 @@ __device__ __forceinline__ void locate(const SampleArgs& a, int r, const Weights
 
 // Few ranks: false where the list would be too long.
 template <int T>
-__device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Settings& how, const RowTop& x, const Weights& weight, ListShared& s) {
-    const int groups = a.chunks * kGroups, lane = threadIdx.x & 63;
-    const float* tops = a.group_top + (int64_t)r * groups;
+__device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Settings& how, float top, const Weights& weight, const float* tops, int groups, ListShared& s) {
+    const int lane = threadIdx.x & 63;
     const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
     // the bin of the k-th largest group maximum
     float low = INFINITY;
@@ -678,7 +677,7 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     s.counts[threadIdx.x] = 0;
     if (threadIdx.x == 0) { s.many = 0; s.value[0] = 1023; }
     low = all_threads(low, s.sums, Smaller());
-    const Bins bins(x.top, low, INFINITY, 1024);
+    const Bins bins(top, low, INFINITY, 1024);
     for (int g = threadIdx.x; g < groups; g += kThreads) {
         const float t = tops[g];
         if (t > -INFINITY) atomicAdd(&s.counts[bins(t)], 1u);
@@ -700,11 +699,21 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     const int chosen = (int)s.many;
     // their tokens, a group a wavefront at a time: f(token, logit, bin, whether it may be among the first k)
     auto tokens = [&](auto&& f) __attribute__((always_inline)) {
-        for (int u = threadIdx.x >> 6; u < chosen; u += kWaves) {
-            const int i = s.groups[u] * kGroup + lane;
-            const float v = i < a.vocabulary ? logit<T>(row, i) : -INFINITY;
-            const int bin = v > -INFINITY ? bins(v) : 1024;
-            f(i, v, bin, bin <= cut_bin);
+        constexpr int kAhead = 4;
+        for (int u0 = threadIdx.x >> 6; u0 < chosen; u0 += kWaves * kAhead) {
+            float v[kAhead];
+            int i[kAhead];
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                const int u = u0 + e * kWaves;
+                i[e] = u < chosen ? s.groups[u] * kGroup + lane : a.vocabulary;
+                v[e] = logit<T>(row, i[e] < a.vocabulary ? i[e] : 0);
+            }
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                const int bin = i[e] < a.vocabulary && v[e] > -INFINITY ? bins(v[e]) : 1024;
+                f(i[e], v[e], bin, bin <= cut_bin);
+            }
         }
     };
     auto list = [&](int last_bin) __attribute__((always_inline)) {
@@ -767,10 +776,8 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
 }
 
 // What the bins tell: a thread two of them.
-__device__ __forceinline__ RowBins look_up(const SampleArgs& a, int r, const Settings& how, ListShared& s) {
-    const uint64_t* masses = a.bin_mass + (int64_t)r * kBins + 2 * threadIdx.x;
-    const uint32_t* counts = a.bin_count + (int64_t)r * kBins + 2 * threadIdx.x;
-    const uint64_t m0 = masses[0], m1 = masses[1], c0 = counts[0], c1 = counts[1];
+__device__ __forceinline__ RowBins look_up(const uint64_t* masses, const uint32_t* counts, const Settings& how, ListShared& s) {
+    const uint64_t m0 = masses[2 * threadIdx.x], m1 = masses[2 * threadIdx.x + 1], c0 = counts[2 * threadIdx.x], c1 = counts[2 * threadIdx.x + 1];
     uint64_t all, many;
     const uint64_t mass = scan(m0 + m1, s.sums, all) - m0 - m1;
     __syncthreads();
@@ -833,36 +840,21 @@ __global__ __launch_bounds__(kThreads) void k_sample_rows(SampleArgs a) {
     if (done) {
         fill_table(s.list.table);
         const Weights weight(x.top, how.temperature, s.list.table);
-        if (how.way == kFew) done = few_ranks<T>(a, r, how, x, weight, s.list);
+        if (how.way == kFew) done = few_ranks<T>(a, r, how, x.top, weight, a.group_top + (int64_t)r * a.chunks * kGroups, a.chunks * kGroups, s.list);
         else if (how.way == kAll) locate<T>(a, r, weight, how.least, 0, a.chunk_mass + (int64_t)r * a.chunks, s.list);
         else {
-            const RowBins f = look_up(a, r, how, s.list);
+            const RowBins f = look_up(a.bin_mass + (int64_t)r * kBins, a.bin_count + (int64_t)r * kBins, how, s.list);
             if (threadIdx.x == 0) a.found[r] = f;
         }
     }
     if (!done) whole_row<T>(a, r, how, s.whole);
 }
 
-// Ranks by bins: where exactly they end, and the token.
+// Ranks by bins: where exactly they end among the n listed tokens, and the token.  The masses of the chunks' tokens that are kept for certain stand in
+// s.mass.
 template <int T>
-__global__ __launch_bounds__(kThreads) void k_sample_cut(SampleArgs a) {
-    __shared__ union { ListShared list; Shared whole; } shared;
-    ListShared& s = shared.list;
-    const int r = blockIdx.x;
-    const Settings how(a, r);
-    if (how.way != kBinned) return;
-    const RowTop x = row_top<kWaves>(a, r);
-    if (!(__builtin_fabsf(x.top) < INFINITY)) return;       // done by k_sample_rows
-    const int n = (int)a.list_count[r];
-    if (n > kList) {
-        whole_row<T>(a, r, how, shared.whole);
-        return;
-    }
-    fill_table(s.table);
-    const Weights weight(x.top, how.temperature, s.table);
-    const Bins bins = row_bins(x, how);
-    const RowBins f = a.found[r];
-    const uint64_t* list = a.list + (int64_t)r * kList;
+__device__ __forceinline__ void cut_list(const SampleArgs& a, int r, const Settings& how, const Weights& weight, const Bins& bins, const RowBins& f, const uint64_t* list, int n,
+                                         ListShared& s) {
     const uint64_t any = n ? list[0] : 0;
     uint64_t rank[kHeld], mass[kHeld], amount[kHeld], mixed = 0, cut = 0;
     int bin[kHeld];
@@ -877,7 +869,6 @@ __global__ __launch_bounds__(kThreads) void k_sample_cut(SampleArgs a) {
         mass[e] = i < n ? Weights::whole(w[e]) : 0;
         mixed |= rank[e] ^ any;
     }
-    for (int c = threadIdx.x; c < a.chunks; c += kThreads) s.mass[c] = a.chunk_mass[(int64_t)r * a.chunks + c];
     mixed = all_threads(mixed, s.sums, Union());
     const int high = 63 - __builtin_clzll(mixed | 1);
     uint64_t in_k = 0;
@@ -903,17 +894,130 @@ __global__ __launch_bounds__(kThreads) void k_sample_cut(SampleArgs a) {
     locate<T>(a, r, weight, how.least, cut, s.mass, s);
 }
 
-// Rows of one chunk or less, and everything at once.
 template <int T>
-__global__ __launch_bounds__(kThreads) void k_sample_whole(SampleArgs a) {
-    __shared__ Shared s;
-    whole_row<T>(a, blockIdx.x, Settings(a, blockIdx.x), s);
+__global__ __launch_bounds__(kThreads) void k_sample_cut(SampleArgs a) {
+    __shared__ union { ListShared list; Shared whole; } s;
+    const int r = blockIdx.x;
+    const Settings how(a, r);
+    if (how.way != kBinned) return;
+    const RowTop x = row_top<kWaves>(a, r);
+    if (!(__builtin_fabsf(x.top) < INFINITY)) return;       // done by k_sample_rows
+    const int n = (int)a.list_count[r];
+    if (n > kList) {
+        whole_row<T>(a, r, how, s.whole);
+        return;
+    }
+    for (int c = threadIdx.x; c < a.chunks; c += kThreads) s.list.mass[c] = a.chunk_mass[(int64_t)r * a.chunks + c];
+    fill_table(s.list.table);
+    cut_list<T>(a, r, how, Weights(x.top, how.temperature, s.list.table), row_bins(x, how), a.found[r], a.list + (int64_t)r * kList, n, s.list);
+}
+
+// Rows of up to kOneRow tokens: the same by one workgroup a row, its numbers in LDS, in one launch.
+constexpr int kOneRow = 1 << 16;
+template <int T>
+__global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
+    struct Parts {
+        ListShared list;
+        uint64_t bin_mass[kBins];
+        uint32_t bin_count[kBins];
+        float group_top[kOneRow / kGroup];
+    };
+    __shared__ union { Parts part; Shared whole; } shared;
+    Parts& s = shared.part;
+    const int r = blockIdx.x, n = a.vocabulary, lane = threadIdx.x & 63;
+    const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
+    const Settings how(a, r);
+    RowTop x{-INFINITY, INFINITY};
+    int at = n;
+    for (int i0 = 0; i0 < n; i0 += kThreads * 8) {
+        const int i = i0 + threadIdx.x * 8;
+        float v[8], most;
+        logits_of<T, 8>(row, i, n, v);
+        most = v[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) most = fmaxf(most, v[e]);
+        if (how.way == kTop) {
+#pragma unroll
+            for (int e = 7; e >= 0; --e) at = v[e] == most && most > x.top ? i + e : at;
+        } else if (how.way == kFew) {
+            const float group = lanes8(most, Larger());
+            if ((lane & 7) == 0 && i < n) s.group_top[i / kGroup] = group;
+        } else if (how.way == kBinned) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x.low = v[e] > -INFINITY ? fminf(x.low, v[e]) : x.low;
+        }
+        x.top = fmaxf(x.top, most);
+    }
+    const float mine = x.top;
+    x.top = all_threads(x.top, s.list.sums, Larger());
+    if (x.top == -INFINITY || how.way == kTop) {
+        top_token(a, r, x.top, all_threads(mine == x.top ? at : n, s.list.sums, Smaller()));
+        return;
+    }
+    bool done = x.top < INFINITY;
+    if (done) {
+        fill_table(s.list.table);
+        const Weights weight(x.top, how.temperature, s.list.table);
+        if (how.way == kFew) {
+            done = few_ranks<T>(a, r, how, x.top, weight, s.group_top, (n + kGroup - 1) / kGroup, s.list);
+        } else {
+            const bool binned = how.way == kBinned;
+            x.low = all_threads(x.low, s.list.sums, Smaller());
+            const Bins bins = row_bins(x, how);
+            RowBins f{0, 0, 0, kBins, kBins, kBins, 0};
+            if (threadIdx.x < kOneRow / kChunk) s.list.mass[threadIdx.x] = 0;
+            if (threadIdx.x == 0) s.list.many = 0;
+            if (binned) {
+                for (int i = threadIdx.x; i < kBins; i += kThreads) { s.bin_mass[i] = 0; s.bin_count[i] = 0; }
+                __syncthreads();
+                for (int i = threadIdx.x * 4; i < n; i += kThreads * 4) {
+                    float v[4];
+                    logits_of<T, 4>(row, i, n, v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (!(v[e] > -INFINITY)) continue;
+                        const int bin = bins(v[e]);
+                        const uint64_t m = how.p < 1.f ? weight.mass(v[e]) : 0;
+                        if (m) atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin_mass[bin]), (unsigned long long)m);
+                        if (how.k) atomicAdd(&s.bin_count[bin], 1u);
+                    }
+                }
+                __syncthreads();
+                f = look_up(s.bin_mass, s.bin_count, how, s.list);
+            }
+            __syncthreads();
+            for (int i0 = 0; i0 < n; i0 += kThreads * 4) {           // a chunk
+                const int i = i0 + threadIdx.x * 4;
+                float v[4];
+                logits_of<T, 4>(row, i, n, v);
+                uint64_t sum = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int bin = !binned ? 0 : (v[e] > -INFINITY ? bins(v[e]) : kBins + 1);
+                    const double w = weight(v[e]);
+                    sum += bin < f.p0 && w >= how.least ? Weights::whole(w) : 0;
+                    if (bin >= f.p0 && (bin <= f.p1 || bin == f.bin_k)) {
+                        const uint32_t to = atomicAdd(&s.list.many, 1u);
+                        if (to < kList) s.list.rank[to] = rank_of(v[e], i + e);
+                    }
+                }
+                sum = lanes64(sum, Sum());
+                if (lane == 0 && sum) atomicAdd(reinterpret_cast<unsigned long long*>(&s.list.mass[i0 / kChunk]), (unsigned long long)sum);
+            }
+            __syncthreads();
+            const int many = (int)s.list.many;
+            done = many <= kList;
+            if (done && binned) cut_list<T>(a, r, how, weight, bins, f, s.list.rank, many, s.list);
+            else if (done) locate<T>(a, r, weight, how.least, 0, s.list.mass, s.list);
+        }
+    }
+    if (!done) whole_row<T>(a, r, how, shared.whole);
 }
 
 struct SampleWork { int64_t chunk_top, chunk_low, chunk_at, group_top, chunk_mass, bin_mass, bin_count, list, list_count, found, bytes; };
 SampleWork sample_work(int64_t rows, int32_t vocabulary) {
     SampleWork w{};
-    if (vocabulary <= kChunk) return w;
+    if (vocabulary <= kOneRow) return w;
     if (rows > kSliceRows) rows = kSliceRows;
     const int64_t chunks = (vocabulary + kChunk - 1) / kChunk;
     int64_t at = 0;
@@ -934,11 +1038,11 @@ SampleWork sample_work(int64_t rows, int32_t vocabulary) {
 
 template <int T>
 hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st) {
-    if (a.vocabulary <= kChunk) {
-        k_sample_whole<T><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
+    a.chunks = (a.vocabulary + kChunk - 1) / kChunk;
+    if (a.vocabulary <= kOneRow) {
+        k_sample_row<T><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
-    a.chunks = (a.vocabulary + kChunk - 1) / kChunk;
     a.chunk_top = reinterpret_cast<float*>(work + w.chunk_top);
     a.chunk_low = reinterpret_cast<float*>(work + w.chunk_low);
     a.group_top = reinterpret_cast<float*>(work + w.group_top);

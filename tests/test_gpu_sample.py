@@ -51,7 +51,7 @@ WAYS = [dict(), dict(temperature=0.0), dict(temperature=0.7, top_k=40), dict(top
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("v", (1, 2, 63, 1000, 1024, 1025, 5000, 32_001))
+@pytest.mark.parametrize("v", (1, 2, 63, 1000, 1024, 1025, 5000, 32_001, 65_536, 65_537))
 @pytest.mark.parametrize("way", range(len(WAYS)))
 def test_settings(kind, v, way):
     rows = 6
@@ -170,7 +170,7 @@ def test_long_lists(kind, v):
 
 
 def test_more_rows_than_share_a_workspace():
-    rows, v = 2500, 5000
+    rows, v = 1100, 66_000
     x = logits(12, rows, v, "bf16")
     r = np.random.default_rng(1)
     check(x, r.random(rows, np.float32), temperature=r.choice([0.0, 0.8, 1.0], rows), top_k=r.choice([0, 20, 600], rows), top_p=r.choice([0.9, 1.0], rows),

@@ -62,12 +62,12 @@ def test_the_rest(lib):
     assert lib.ivftq_sample_tokens(None, HERE, C.byref(how()), HERE, None, HERE, 1 << 40, None) == 1
     assert lib.ivftq_sample_tokens(C.byref(logits()), HERE, None, HERE, None, HERE, 1 << 40, None) == 1
     assert lib.ivftq_sample_workspace(C.byref(logits())) == 0
-    large = logits(vocabulary=50_000, row_stride=50_000)
+    large = logits(vocabulary=70_000, row_stride=70_000)
     need = lib.ivftq_sample_workspace(C.byref(large))
     assert need > 0 and need % 256 == 0
     assert call(lib, large, size=need - 1) == call(lib, large, work=None) == call(lib, large, work=C.c_void_p((1 << 20) + 16)) == 1
     # many rows are taken a slice at a time
-    assert lib.ivftq_sample_workspace(C.byref(logits(vocabulary=50_000, row_stride=50_000, rows=5000))) < 1 << 27
+    assert lib.ivftq_sample_workspace(C.byref(logits(vocabulary=70_000, row_stride=70_000, rows=5000))) < 1 << 27
 
 
 @pytest.fixture
