@@ -3,8 +3,9 @@
 //   - Few ranks are kept (top_k up to 1,024): at least k tokens are not under the k-th largest group maximum, so the tokens not under it, a
 //     little more than k of them in as few groups, are the list (k_sample_rows).
 //   - Otherwise a second reading (k_sample_chunks) adds up the weights of every chunk, and where a rank is looked for by its number or its mass, of
-//     2,048 bins of logits.  k_sample_rows finds the bins in which the two ranks lie; a third reading (k_sample_bins) lists their tokens, and
-//     k_sample_cut counts ranks among them.
+//     2,048 bins of logits.  A third reading (k_sample_bins) finds the bins in which the two ranks lie and lists their tokens, among which
+//     k_sample_rows counts ranks.
+//   - Rows of up to 65,536 tokens are one workgroup's (k_sample_row), all of it in one launch.
 //   - The token is looked for in the chunk in which the sum passes u times all of it.
 // Where a list would be too long (thousands of tokens within a bin) the row is worked through digit by digit of the logits' order by one
 // workgroup.
@@ -180,8 +181,8 @@ struct AnyWeights : Weights {
 // A share of a mass: the tokens that less than it comes before are those that less than this whole number does.
 __device__ __forceinline__ uint64_t share_of(float p, uint64_t mass) { return (uint64_t)__builtin_ceil((double)p * (double)mass); }
 
-// Sum over the threads up to this one; all: over all threads.  sums: kWaves numbers in LDS.
-template <class T>
+// Sum over the threads up to this one; all: over all threads.  sums: W numbers in LDS.
+template <int W = kWaves, class T>
 __device__ __forceinline__ T scan(T v, T* sums, T& all) {
     const T incl = lanes_upto(v);
     __syncthreads();
@@ -190,7 +191,7 @@ __device__ __forceinline__ T scan(T v, T* sums, T& all) {
     T before = 0;
     all = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) { before += w < (int)(threadIdx.x >> 6) ? sums[w] : 0; all += sums[w]; }
+    for (int w = 0; w < W; ++w) { before += w < (int)(threadIdx.x >> 6) ? sums[w] : 0; all += sums[w]; }
     return before + incl;
 }
 
@@ -514,11 +515,70 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
     }
 }
 
+// What the bins tell; by W wavefronts, each thread kBins / 64 W of them.  sums: W numbers, value: 4, in LDS.
+template <int W>
+__device__ __forceinline__ RowBins look_up(const uint64_t* masses, const uint32_t* counts, const Settings& how, uint64_t* sums, uint64_t* value) {
+    constexpr int kOwn = kBins / (64 * W);
+    uint64_t m[kOwn], mass = 0, count = 0, all, many;
+    uint32_t c[kOwn];
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        m[e] = masses[kOwn * threadIdx.x + e];
+        c[e] = counts[kOwn * threadIdx.x + e];
+        mass += m[e];
+        count += c[e];
+    }
+    mass = scan<W>(mass, sums, all) - mass;
+    __syncthreads();
+    count = scan<W>(count, sums, many) - count;
+    RowBins f{all, 0, all, kBins, kBins, kBins, 0};
+    uint64_t in_k = 0;
+    if (how.k && many > (uint64_t)how.k) {             // (otherwise every token above -infinity)
+        uint64_t before_mass = mass, before = count;
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e) {
+            if (before < (uint64_t)how.k && before + c[e] >= (uint64_t)how.k) {
+                value[0] = kOwn * threadIdx.x + e;
+                value[1] = before;
+                value[2] = before_mass;
+                value[3] = m[e];
+            }
+            before += c[e];
+            before_mass += m[e];
+        }
+        __syncthreads();
+        f.bin_k = (int)value[0];
+        f.count_k = (uint32_t)value[1];
+        f.before_k = value[2];
+        in_k = value[3];
+        f.p0 = f.bin_k;
+        f.p1 = f.bin_k;
+        __syncthreads();
+    }
+    if (how.p < 1.f) {                                 // the mass of the ranks that top_k leaves is before_k to before_k + in_k
+        const uint64_t low = share_of(how.p, f.before_k), high = share_of(how.p, f.before_k + in_k);
+        if (threadIdx.x == 0) { value[0] = 0; value[1] = 0; value[2] = f.bin_k < kBins ? f.bin_k : kBins - 1; }
+        __syncthreads();
+        uint64_t before = mass;
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e) {
+            if (before < low && before + m[e] >= low) { value[0] = kOwn * threadIdx.x + e; value[1] = before; }
+            if (before < high && before + m[e] >= high) value[2] = kOwn * threadIdx.x + e;
+            before += m[e];
+        }
+        __syncthreads();
+        f.p0 = (int)value[0];
+        f.before_p = value[1];
+        f.p1 = (int)value[2];
+    }
+    return f;
+}
+
 // The third reading: the masses of the chunks' tokens that are kept for certain, and the tokens whose ranks have to be counted.
 template <int T>
 __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
     __shared__ double table[64];
-    __shared__ uint64_t sums[4];
+    __shared__ uint64_t sums[4], value[4];
     __shared__ uint32_t many, begin;
     const int r = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, n = a.vocabulary;
     const Settings how(a, r);
@@ -533,7 +593,9 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
     fill_table(table);
     const Weights weight(x.top, how.temperature, table);
     const Bins bins = row_bins(x, how);
-    const RowBins f = a.found[r];
+    const RowBins f = look_up<4>(a.bin_mass + (int64_t)r * kBins, a.bin_count + (int64_t)r * kBins, how, sums, value);
+    if (chunk == 0 && threadIdx.x == 0) a.found[r] = f;
+    __syncthreads();
     uint64_t sum = 0;
     uint32_t open = 0;                                     // of the thread's tokens: those of the list, a bit each
 #pragma unroll
@@ -775,81 +837,6 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     return true;
 }
 
-// What the bins tell: a thread two of them.
-__device__ __forceinline__ RowBins look_up(const uint64_t* masses, const uint32_t* counts, const Settings& how, ListShared& s) {
-    const uint64_t m0 = masses[2 * threadIdx.x], m1 = masses[2 * threadIdx.x + 1], c0 = counts[2 * threadIdx.x], c1 = counts[2 * threadIdx.x + 1];
-    uint64_t all, many;
-    const uint64_t mass = scan(m0 + m1, s.sums, all) - m0 - m1;
-    __syncthreads();
-    const uint64_t count = scan(c0 + c1, s.sums, many) - c0 - c1;
-    RowBins f{all, 0, all, kBins, kBins, kBins, 0};
-    uint64_t in_k = 0;
-    if (how.k && many > (uint64_t)how.k) {             // (otherwise every token above -infinity)
-        const bool first = count < (uint64_t)how.k && count + c0 >= (uint64_t)how.k, second = count + c0 < (uint64_t)how.k && count + c0 + c1 >= (uint64_t)how.k;
-        if (first || second) {
-            s.value[0] = 2 * threadIdx.x + second;
-            s.value[1] = second ? count + c0 : count;
-            s.value[2] = second ? mass + m0 : mass;
-            s.value[3] = second ? m1 : m0;
-        }
-        __syncthreads();
-        f.bin_k = (int)s.value[0];
-        f.count_k = (uint32_t)s.value[1];
-        f.before_k = s.value[2];
-        in_k = s.value[3];
-        f.p0 = f.bin_k;
-        f.p1 = f.bin_k;
-        __syncthreads();
-    }
-    if (how.p < 1.f) {                                 // the mass of the ranks that top_k leaves is before_k to before_k + in_k
-        const uint64_t low = share_of(how.p, f.before_k), high = share_of(how.p, f.before_k + in_k);
-        if (threadIdx.x == 0) { s.value[0] = 0; s.value[1] = 0; s.value[2] = f.bin_k < kBins ? f.bin_k : kBins - 1; }
-        __syncthreads();
-        const uint64_t m[2] = {m0, m1};
-        uint64_t before = mass;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if (before < low && before + m[e] >= low) { s.value[0] = 2 * threadIdx.x + e; s.value[1] = before; }
-            if (before < high && before + m[e] >= high) s.value[2] = 2 * threadIdx.x + e;
-            before += m[e];
-        }
-        __syncthreads();
-        f.p0 = (int)s.value[0];
-        f.before_p = s.value[1];
-        f.p1 = (int)s.value[2];
-    }
-    return f;
-}
-
-// After the first two readings: rows by their largest logit, by few ranks and by all chunks are done, of the others the bins are found.
-template <int T>
-__global__ __launch_bounds__(kThreads) void k_sample_rows(SampleArgs a) {
-    __shared__ union { ListShared list; Shared whole; } s;
-    const int r = blockIdx.x;
-    const Settings how(a, r);
-    const RowTop x = row_top<kWaves>(a, r);
-    if (x.top == -INFINITY || how.way == kTop) {
-        int at = a.vocabulary;
-        if (how.way == kTop)
-            for (int c = threadIdx.x; c < a.chunks; c += kThreads)
-                if (a.chunk_top[(int64_t)r * a.chunks + c] == x.top) at = min(at, a.chunk_at[(int64_t)r * a.chunks + c]);
-        top_token(a, r, x.top, all_threads(at, s.list.sums, Smaller()));
-        return;
-    }
-    bool done = x.top < INFINITY;
-    if (done) {
-        fill_table(s.list.table);
-        const Weights weight(x.top, how.temperature, s.list.table);
-        if (how.way == kFew) done = few_ranks<T>(a, r, how, x.top, weight, a.group_top + (int64_t)r * a.chunks * kGroups, a.chunks * kGroups, s.list);
-        else if (how.way == kAll) locate<T>(a, r, weight, how.least, 0, a.chunk_mass + (int64_t)r * a.chunks, s.list);
-        else {
-            const RowBins f = look_up(a.bin_mass + (int64_t)r * kBins, a.bin_count + (int64_t)r * kBins, how, s.list);
-            if (threadIdx.x == 0) a.found[r] = f;
-        }
-    }
-    if (!done) whole_row<T>(a, r, how, s.whole);
-}
-
 // Ranks by bins: where exactly they end among the n listed tokens, and the token.  The masses of the chunks' tokens that are kept for certain stand in
 // s.mass.
 template <int T>
@@ -894,22 +881,40 @@ __device__ __forceinline__ void cut_list(const SampleArgs& a, int r, const Setti
     locate<T>(a, r, weight, how.least, cut, s.mass, s);
 }
 
+// After the readings: each row's token.
 template <int T>
-__global__ __launch_bounds__(kThreads) void k_sample_cut(SampleArgs a) {
+__global__ __launch_bounds__(kThreads) void k_sample_rows(SampleArgs a) {
     __shared__ union { ListShared list; Shared whole; } s;
     const int r = blockIdx.x;
     const Settings how(a, r);
-    if (how.way != kBinned) return;
     const RowTop x = row_top<kWaves>(a, r);
-    if (!(__builtin_fabsf(x.top) < INFINITY)) return;       // done by k_sample_rows
-    const int n = (int)a.list_count[r];
-    if (n > kList) {
-        whole_row<T>(a, r, how, s.whole);
+    if (x.top == -INFINITY || how.way == kTop) {
+        int at = a.vocabulary;
+        if (how.way == kTop)
+            for (int c = threadIdx.x; c < a.chunks; c += kThreads)
+                if (a.chunk_top[(int64_t)r * a.chunks + c] == x.top) at = min(at, a.chunk_at[(int64_t)r * a.chunks + c]);
+        top_token(a, r, x.top, all_threads(at, s.list.sums, Smaller()));
         return;
     }
-    for (int c = threadIdx.x; c < a.chunks; c += kThreads) s.list.mass[c] = a.chunk_mass[(int64_t)r * a.chunks + c];
-    fill_table(s.list.table);
-    cut_list<T>(a, r, how, Weights(x.top, how.temperature, s.list.table), row_bins(x, how), a.found[r], a.list + (int64_t)r * kList, n, s.list);
+    bool done = x.top < INFINITY;
+    if (done) {
+        const uint64_t* masses = a.chunk_mass + (int64_t)r * a.chunks;
+        fill_table(s.list.table);
+        const Weights weight(x.top, how.temperature, s.list.table);
+        if (how.way == kFew) {
+            done = few_ranks<T>(a, r, how, x.top, weight, a.group_top + (int64_t)r * a.chunks * kGroups, a.chunks * kGroups, s.list);
+        } else if (how.way == kAll) {
+            locate<T>(a, r, weight, how.least, 0, masses, s.list);
+        } else {
+            const int n = (int)a.list_count[r];
+            done = n <= kList;
+            if (done) {
+                for (int c = threadIdx.x; c < a.chunks; c += kThreads) s.list.mass[c] = masses[c];
+                cut_list<T>(a, r, how, weight, row_bins(x, how), a.found[r], a.list + (int64_t)r * kList, n, s.list);
+            }
+        }
+    }
+    if (!done) whole_row<T>(a, r, how, s.whole);
 }
 
 // Rows of up to kOneRow tokens: the same by one workgroup a row, its numbers in LDS, in one launch.
@@ -983,7 +988,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
                     }
                 }
                 __syncthreads();
-                f = look_up(s.bin_mass, s.bin_count, how, s.list);
+                f = look_up<kWaves>(s.bin_mass, s.bin_count, how, s.list.sums, s.list.value);
             }
             __syncthreads();
             for (int i0 = 0; i0 < n; i0 += kThreads * 4) {           // a chunk
@@ -1061,11 +1066,8 @@ hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st)
         const unsigned rows = (unsigned)(left < kSliceRows ? left : kSliceRows), wgs = rows * (unsigned)a.chunks;
         k_sample_tops<T><<<wgs, kChunkThreads, 0, st>>>(a);
         if (again) k_sample_chunks<T><<<wgs, kChunkThreads, 0, st>>>(a);
+        if (binned) k_sample_bins<T><<<wgs, kChunkThreads, 0, st>>>(a);
         k_sample_rows<T><<<rows, kThreads, 0, st>>>(a);
-        if (binned) {
-            k_sample_bins<T><<<wgs, kChunkThreads, 0, st>>>(a);
-            k_sample_cut<T><<<rows, kThreads, 0, st>>>(a);
-        }
         if (hipError_t e = hipGetLastError()) return e;
         a.logits += (int64_t)rows * a.row_stride * kSize<T>;
         a.u += rows;
