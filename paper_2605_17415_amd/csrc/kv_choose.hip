@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void k_kv_digest_row(KvView c, uint16_t* diges
 // wavefront's lanes are 64 / (D / 8) tokens of D / 8 pieces of eight coordinates.
 template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_digest(KvView c, uint16_t* digests) {
-    constexpr int kPieces = D / 8, kTokens = 64 / kPieces, kAhead = 4;
+    constexpr int kPieces = D / 8, kTokens = 64 / kPieces, kAhead = F == IVFTQ_KV_CODE4 ? 16 : 8;       // loads on their way: a page of 64 at once, half of one
     __shared__ float level[16];
     if constexpr (F == IVFTQ_KV_CODE4) level_table(c, level);
     const int lane = threadIdx.x & 63, token = lane / kPieces, j = lane % kPieces * 8;
@@ -150,14 +150,14 @@ __global__ __launch_bounds__(256) void k_kv_digest(KvView c, uint16_t* digests) 
                     }
                 }
                 // over the lanes of one piece
-                if constexpr ((kTokens & (kTokens - 1)) == 0 && kTokens * kPieces == 64) {
+                if constexpr (kTokens * kPieces == 64) {
+                    auto join = [](float v, auto op) __attribute__((always_inline)) {
+                        if constexpr (kPieces <= 8) v = op(v, lane_moved<0x128>(v));          // row_ror:8
+                        if constexpr (kPieces <= 16) v = lane_pair<false>(v, op);
+                        return lane_pair<true>(v, op);
+                    };
 #pragma unroll
-                    for (int o = kPieces; o < 64; o <<= 1)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            box.low[e] = fminf(box.low[e], __shfl_xor(box.low[e], o));
-                            box.high[e] = fmaxf(box.high[e], __shfl_xor(box.high[e], o));
-                        }
+                    for (int e = 0; e < 8; ++e) { box.low[e] = join(box.low[e], Smaller()); box.high[e] = join(box.high[e], Larger()); }
                 } else {
                     const Box own = box;
 #pragma unroll
