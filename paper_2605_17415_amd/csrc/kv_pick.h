@@ -531,17 +531,21 @@ __global__ __launch_bounds__(256, D <= 64 ? 4 : (D <= 128 ? 3 : 1)) void k_kv_pi
     }
 }
 
+struct NoRotation { __device__ __forceinline__ NoRotation(const float*, int) {} };
+
 // The parts of a unit put together, a workgroup a unit and column tile, a wavefront a row; codes: rotated back, each wavefront a block
 // of 32 coordinates.
 template <int F, int D>
 __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
-    constexpr int kPart = D / 4;
+    constexpr int kPart = D / 4, kBeside = D <= 64 ? 4 : (D <= 128 && D != 96 ? 2 : 1);
     __shared__ __align__(16) float row_sum[F == IVFTQ_KV_CODE4 ? 16 : 1][D + 4];
     const FewArgs& f = p.f;
     const KvAttend& a = f.a;
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, col0 = blockIdx.y * 16;
     const uint32_t wg = kv_workgroup();
+    // units are few here: the rotation is asked for before everything that it waits for
+    const std::conditional_t<F == IVFTQ_KV_CODE4, KvTurnRows<D, true>, NoRotation> rotation(c.rotation, wave < D / 32 ? wave : 0);
     const int h = (int)(wg % (uint32_t)c.heads), at = (int)(wg / (uint32_t)c.heads);
     if (at >= p.units) return;
     const PickUnit unit = pick_unit(p, at);
@@ -566,13 +570,20 @@ __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
         float l = u.x == -INFINITY ? u.y * 0.f : u.y * turn;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
+        // kBeside parts side by side, eight times as many on their way
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int j = lane < kPart ? lane * 4 : 0;
-#pragma unroll 4
-        for (int w = 0; w < p.splits; ++w) {
-            const float t = __shfl(turn, w);
-            const float4 x = *reinterpret_cast<const float4*>(f.part + (slot0 + w * 16) * D + j);
-            acc.x += x.x * t; acc.y += x.y * t; acc.z += x.z * t; acc.w += x.w * t;
+        const int beside = lane / kPart < kBeside ? lane / kPart : 0, j = lane % kPart * 4;
+#pragma unroll 8
+        for (int w = 0; w < p.splits; w += kBeside) {
+            const bool there = w + beside < p.splits;
+            const int part = there ? w + beside : w;
+            const float t = __shfl(turn, part);
+            const float4 x = *reinterpret_cast<const float4*>(f.part + (slot0 + part * 16) * D + j);
+            acc.x += there ? x.x * t : 0.f; acc.y += there ? x.y * t : 0.f; acc.z += there ? x.z * t : 0.f; acc.w += there ? x.w * t : 0.f;
+        }
+#pragma unroll
+        for (int o = kPart; o < kPart * kBeside; o <<= 1) {
+            acc.x += __shfl(acc.x, lane + o); acc.y += __shfl(acc.y, lane + o); acc.z += __shfl(acc.z, lane + o); acc.w += __shfl(acc.w, lane + o);
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
         acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
@@ -597,7 +608,7 @@ __global__ __launch_bounds__(512) void k_kv_picked_join(PickArgs p) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[k][e] = in ? row_sum[n][32 * k + 8 * g + e] : 0.f;
         const float norm = kv_unit_row<D>(x) * c.level_unit;
-        KvTurn<D, true>(c.rotation, wave)(x, y);
+        KvTurn<D, true>{rotation}(x, y);
         int row, head;
         place(in ? col0 + n : 0, row, head);
         if (in) kv_store_turned(a.out, row, head, wave, y, norm);
