@@ -102,7 +102,7 @@ PickWork pick_work(const ivftq_kv_cache& c, int64_t rows, int q_heads, int max_n
     return w;
 }
 
-ScoreWork score_work(int format, int d, int batch, int64_t rows, int q_heads, int kv_heads, bool one) {
+ScoreWork score_work(int format, int d, int64_t rows, int q_heads, int kv_heads, bool one) {
     ScoreWork w{};
     int64_t at = 0;
     auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
@@ -111,7 +111,7 @@ ScoreWork score_work(int format, int d, int batch, int64_t rows, int q_heads, in
         w.zn = room(rows * q_heads * 4);
     }
     if (!one) {
-        w.tiles = (int32_t)(rows / 16 + batch + 1);
+        w.tiles = (int32_t)((rows + 15) / 16);
         w.sides = room((int64_t)w.tiles * 16 * kv_heads * (format == IVFTQ_KV_BF16 ? 3 : 2) * 2 * d * 2);
         w.unit = room((int64_t)w.tiles * 16 * kv_heads * 4);
     }
@@ -422,7 +422,7 @@ int64_t ivftq_kv_score_workspace(const ivftq_kv_cache* cache, int64_t rows, int3
         refuse(IVFTQ_INVALID_ARG, "max_new = %d", max_new);
         return -1;
     }
-    return score_work(cache->format, cache->d, cache->batch, rows, q_heads, cache->heads, max_new == 1 || rows <= 1).bytes;
+    return score_work(cache->format, cache->d, rows, q_heads, cache->heads, max_new == 1 || rows <= 1).bytes;
 }
 ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts, int32_t max_new,
                             void* workspace, int64_t workspace_bytes, void* stream) {
@@ -431,9 +431,9 @@ ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q,
     if (!q->rows || !cache->batch) return IVFTQ_OK;
     if (!scores || !aligned(scores, 4)) return refuse(IVFTQ_INVALID_ARG, "scores is NULL or not 4-byte aligned");
     const KvAttend a = attend_of(*cache, *q, starts, max_new, workspace);
-    if ((int64_t)cache->batch * cache->heads * ((a.max_new + 15) / 16) > INT32_MAX)
+    if ((int64_t)cache->batch * cache->heads * ((a.max_new + 15) / 16 + 1) > INT32_MAX)
         return refuse(IVFTQ_UNSUPPORTED, "more than 2^31 workgroups: %d sequences of %d heads and up to %d rows", cache->batch, cache->heads, a.max_new);
-    if (ivftq_status e = check_work(workspace, workspace_bytes, score_work(cache->format, cache->d, cache->batch, q->rows, q->heads, cache->heads, a.max_new == 1).bytes)) return e;
+    if (ivftq_status e = check_work(workspace, workspace_bytes, score_work(cache->format, cache->d, q->rows, q->heads, cache->heads, a.max_new == 1).bytes)) return e;
     return done(launch_kv_score(a, digests, scores, cache->d, cache->format, static_cast<hipStream_t>(stream)), "ivftq_kv_score");
 }
 

@@ -23,8 +23,8 @@ struct ScoreArgs {
     const float* zn;                  // codes: the queries' norms
     uint16_t* sides;                  // [heads][tiles][parts][2 D / 32][64 lanes][8]: operands as they are read
     float* unit;                      // [heads][tiles][16] what the parts are multiplied by
-    int32_t tiles;                    // tiles of 16 rows, those of sequence b from score_tile on
-    int32_t row_tiles, each;          // row tiles of 16 a sequence, and a workgroup's
+    int32_t tiles;                    // tiles of 16 rows: those of row r in tile r / 16, whatever sequence it is of
+    int32_t row_tiles, each;          // tiles that a sequence's rows may lie in, and a workgroup's
 };
 template <int F> constexpr int kSideParts = F == IVFTQ_KV_BF16 ? 3 : 2;
 
@@ -113,11 +113,8 @@ __global__ __launch_bounds__(256) void k_kv_score_one(ScoreArgs f) {
     if (lane < kAll && mine < c.columns) f.scores[(row * c.heads + h) * c.columns + mine] = there ? score : -INFINITY;
 }
 
-// The first tile of a sequence: no two sequences' tiles meet, however long they are.
-__device__ __forceinline__ int score_tile(int first, int b) { return first / 16 + b; }
-
-// Sides of several rows: 32 lanes a (row, head) pair, of which D / 8 work.  (Rows that lie one after the other, 8 KB apart, meet in one
-// channel of the L2: read that way the products took four times as long.)
+// Sides of several rows: 32 lanes a (row, head) pair, of which D / 8 work.  (A row's operands one after the other, rows 8 KB apart,
+// meet in one channel of the L2: the products took 36 us of a chunk's scores that way, 18 so.)
 template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_sides(ScoreArgs f) {
     constexpr int kParts = kSideParts<F>;
@@ -139,12 +136,8 @@ __global__ __launch_bounds__(256) void k_kv_sides(ScoreArgs f) {
         by = most > 0.f && most < INFINITY ? ldexpf(1.f, e < -100 ? 114 : 14 - e) : 1.f;
     }
     if (pair >= pairs || piece >= D / 8) return;
-    const int row = (int)(pair / c.heads), h = (int)(pair % c.heads);
-    int first, count;
-    const int b = kv_sequence(c, row, first, count);
-    if (b < 0 || row - first >= f.a.max_new) return;
-    const int64_t tile = (int64_t)h * f.tiles + score_tile(first, b) + (row - first) / 16;
-    const int i = (row - first) % 16;
+    const int row = (int)(pair / c.heads), h = (int)(pair % c.heads), i = row % 16;
+    const int64_t tile = (int64_t)h * f.tiles + row / 16;
     if (piece == 0) f.unit[tile * 16 + i] = 1.f / by;
     uint16_t* to = f.sides + (tile * (kParts * 2 * D / 32) + j / 32) * 512 + (j % 32 / 8 * 16 + i) * 8;
 #pragma unroll
@@ -178,9 +171,10 @@ __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
     if (b >= c.batch) return;
     int first, count;
     kv_new_rows(c, b, first, count);
-    const int base = kv_length(c, b) - count;
+    const int base = kv_length(c, b) - count - first;                      // a row's position: base + row
     if (count > a.max_new) count = a.max_new;
-    if (16 * rt0 >= count) return;
+    const int end = first + count, tile0 = first / 16 + rt0, last = min(first / 16 + min(rt0 + f.each, f.row_tiles), (end + 15) / 16);
+    if (!count || tile0 >= last) return;
     const int col0 = ((int)blockIdx.y * 4 + wave) * 16 * kTiles;
     if (col0 >= c.columns) return;
     uint32_t known[kTiles];
@@ -199,22 +193,18 @@ __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) box[t][k] = *reinterpret_cast<const uintx4*>(p + 32 * k);
     }
-    int last = rt0 + f.each < f.row_tiles ? rt0 + f.each : f.row_tiles;
-    if (last > (count + 15) / 16) last = (count + 15) / 16;
     // A tile's operands are asked for while the tile before is worked on, part by part (left alone the compiler asks for one ahead and waits).
-    const int64_t tile0 = (int64_t)h * f.tiles + score_tile(first, b);
     uintx4 w[kParts][kSteps];
-    auto ask = [&](int part, int64_t tile) __attribute__((always_inline)) {
-        const uint16_t* p = f.sides + (tile * kParts + part) * (kSteps * 512) + lane * 8;
+    auto ask = [&](int part, int tile) __attribute__((always_inline)) {
+        const uint16_t* p = f.sides + (((int64_t)h * f.tiles + tile) * kParts + part) * (kSteps * 512) + lane * 8;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) w[part][k] = *reinterpret_cast<const uintx4*>(p + 512 * k);
     };
 #pragma unroll
-    for (int part = 0; part < kParts; ++part) ask(part, tile0 + rt0);
-    for (int rt = rt0; rt < last; ++rt) {
-        const int rows = count - 16 * rt < 16 ? count - 16 * rt : 16;
-        const int64_t next = tile0 + (rt + 1 < last ? rt + 1 : rt);
-        const float mine = f.unit[(tile0 + rt) * 16 + n];
+    for (int part = 0; part < kParts; ++part) ask(part, tile0);
+    for (int tile = tile0; tile < last; ++tile) {
+        const int next = tile + 1 < last ? tile + 1 : tile;
+        const float mine = f.unit[((int64_t)h * f.tiles + tile) * 16 + n];
         floatx4 acc[kTiles];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -228,17 +218,17 @@ __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
             ask(part, next);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // register r: row 4 g + r, page n: sixteen neighbouring scores a row (four a lane, of one row, were stored at a third of the speed:
-        // rows begin at any multiple of four bytes)
+        // register r: row 4 g + r, page n: sixteen neighbouring scores a row
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = 4 * g + r, reach = (base + 16 * rt + i) >> c.page_log2;          // a position under zero reaches column -1
-            const float unit = __shfl(mine, i);
-            float* out = f.scores + ((int64_t)(first + 16 * rt + i) * c.heads + h) * c.columns + col0 + n;
+            const int row = 16 * tile + 4 * g + r, reach = (base + row) >> c.page_log2;      // a position under zero reaches column -1
+            const float unit = __shfl(mine, 4 * g + r);
+            if (row < first || row >= end) continue;                       // of another sequence
+            float* out = f.scores + ((int64_t)row * c.heads + h) * c.columns + col0 + n;
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 const int col = col0 + 16 * t + n;
-                if (i < rows && col < c.columns) out[16 * t] = col <= reach && (known[t] >> n & 1) ? acc[t][r] * unit : -INFINITY;
+                if (col < c.columns) out[16 * t] = col <= reach && (known[t] >> n & 1) ? acc[t][r] * unit : -INFINITY;
             }
         }
     }
@@ -624,7 +614,7 @@ struct PickWork {
 };
 PickWork pick_work(const ivftq_kv_cache& c, int64_t rows, int q_heads, int max_new, int count);
 struct ScoreWork { int64_t z, zn, sides, unit, bytes; int32_t tiles; };
-ScoreWork score_work(int format, int d, int batch, int64_t rows, int q_heads, int kv_heads, bool one);
+ScoreWork score_work(int format, int d, int64_t rows, int q_heads, int kv_heads, bool one);
 
 // 16-row tiles that a workgroup rotates, and workgroups (as kv_attend_launch).
 template <int D>
@@ -637,11 +627,11 @@ void rotate_queries(const KvAttend& a, uint16_t* z, float* zn, hipStream_t st) {
 template <int F, int D>
 hipError_t kv_score_launch(const KvAttend& a, const void* digests, float* scores, hipStream_t st) {
     const bool one = a.max_new == 1;
-    const ScoreWork w = score_work(F, D, a.c.batch, a.q.rows, a.q.heads, a.c.heads, one);
+    const ScoreWork w = score_work(F, D, a.q.rows, a.q.heads, a.c.heads, one);
     uint16_t* z = reinterpret_cast<uint16_t*>(a.work + w.z);
     float* zn = reinterpret_cast<float*>(a.work + w.zn);
     if constexpr (F == IVFTQ_KV_CODE4) rotate_queries<D>(a, z, zn, st);
-    ScoreArgs f{a, static_cast<const uint16_t*>(digests), scores, z, zn, reinterpret_cast<uint16_t*>(a.work + w.sides), reinterpret_cast<float*>(a.work + w.unit), w.tiles, (a.max_new + 15) / 16, 1};
+    ScoreArgs f{a, static_cast<const uint16_t*>(digests), scores, z, zn, reinterpret_cast<uint16_t*>(a.work + w.sides), reinterpret_cast<float*>(a.work + w.unit), w.tiles, (a.max_new + 15) / 16 + 1, 1};
     const int64_t pairs = (int64_t)a.c.rows * a.c.heads;
     if (one) {
         constexpr int pages = 4 * (D <= 128 ? 32 : 16);

@@ -313,7 +313,7 @@ def _most_new(max_new, starts, rows):
 
 def _blank(shape, dtype, like, stream):
     """A tensor that is given back."""
-    return _result(_scratch(shape, dtype, like, stream), stream)
+    return like.new_empty(shape, dtype=dtype) if stream is None else _result(_scratch(shape, dtype, like, stream), stream)
 
 
 def kv_digest(pool, digests, table, lengths, starts=None, rotation=None, levels=None, stream=None, asked=None, granted=None):
@@ -336,7 +336,7 @@ def kv_score(q, digests, pool, table, lengths, starts=None, max_new=None, rotati
         out = _blank(shape, torch.float32, q, stream)
     result, first, max_new = _floats(out, "out", pool, shape), _starts(starts, table, pool), _most_new(max_new, starts, q.shape[0])
     lib = _library()
-    need = lib.ivftq_kv_score_workspace(cache, q.shape[0], q.shape[1], max_new)
+    need = 0 if max_new == 1 and pool.dtype != torch.uint8 else lib.ivftq_kv_score_workspace(cache, q.shape[0], q.shape[1], max_new)
     if need < 0:
         _check(1)
     work = _scratch(need, torch.uint8, q, stream) if need else None

@@ -124,7 +124,7 @@ def test_digests_of_no_numbers(form):
 
 @pytest.mark.parametrize("d,page", SIZES[:5])
 @pytest.mark.parametrize("form,kind", FORMS)
-@pytest.mark.parametrize("news", ([1, 1, 1, 1], [37, 5, 0, 1]))
+@pytest.mark.parametrize("news", ([1, 1, 1, 1], [37, 5, 0, 1], [3, 2, 9, 4]))
 def test_scores(form, kind, d, page, news):
     heads, group = (2, 3) if d < 192 else (1, 5)
     lens = [260, 5, 0, 70]
