@@ -229,6 +229,7 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void k_kv_select_held(KvSelec
     const int lane = threadIdx.x & 63, wave = kv_wave() % W, sub = kv_wave() / W;
     const int64_t unit = (int64_t)kv_workgroup() * kUnits + sub, last_unit = (int64_t)c.rows * c.heads - 1;
     const int64_t used = unit < last_unit ? unit : last_unit;                    // (past the end: the last one once more, for the barriers)
+    const int row = (int)((uint32_t)used / (uint32_t)c.heads);                    // rows times heads are under 2^31
     int turn = 0;
     // two numbers of every wavefront
     auto exchange = [&](uint32_t a, uint32_t b, uint32_t (&as)[W], uint32_t (&bs)[W]) __attribute__((always_inline)) {
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void k_kv_select_held(KvSelec
         for (int w = 0; w < W; ++w) { as[w] = shared[sub][turn][w][0]; bs[w] = shared[sub][turn][w][1]; }
         turn ^= 1;
     };
-    const int pos = kv_uniform(kv_position(c, used / c.heads));
+    const int pos = kv_uniform(kv_position(c, row));
     const int reach = pos < 0 ? 0 : (pos >> c.page_log2) + 1, n = reach < c.columns ? reach : c.columns;
     const float* scores = s.scores + used * c.columns;
     int32_t* out = s.chosen + used * s.count;
@@ -252,8 +253,9 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void k_kv_select_held(KvSelec
     }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-        const int col = 64 * (R * wave + j) + lane;
-        key[j] = order_of(score[j]) & (col >= s.first && col < n - s.last ? ~0u : 0u);
+        const int begin = 64 * (R * wave + j), col = begin + lane;
+        key[j] = order_of(score[j]);
+        if (begin < s.first || begin + 64 > n - s.last) key[j] &= col >= s.first && col < n - s.last ? ~0u : 0u;
         high = key[j] > high ? key[j] : high;
         low = key[j] - 1 < low - 1 ? key[j] : low;        // of those above zero
     }
@@ -266,6 +268,11 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void k_kv_select_held(KvSelec
     low = kv_uniform((int)low) + 1;
     auto not_under = [&](uint32_t t) __attribute__((always_inline)) {
         uint32_t count = 0;
+        if constexpr (W == 1) {                          // counted by the scalar unit: the vector unit is what bounds many wavefronts
+#pragma unroll
+            for (int j = 0; j < R; ++j) count += (uint32_t)__popcll(__ballot(key[j] >= t));
+            return (int)count;
+        }
 #pragma unroll
         for (int j = 0; j < R; ++j) count += key[j] >= t;
         exchange(lanes64(count, Sum()), 0, as, bs);
@@ -293,36 +300,45 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void k_kv_select_held(KvSelec
             if (count == want) break;
         }
     }
-    uint32_t better = 0, same = 0;
+    // what is above low, and of its equals the first `ties`, in order; the first columns before and the last ones behind
+    const uint64_t before = (1ull << lane) - 1;
+    const int head = s.first < n ? s.first : n;
+    int at = head, equal = 0, total = 0;
+    if constexpr (W > 1) {
+        uint32_t better = 0, same = 0;
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-        const int col = 64 * (R * wave + j) + lane;
-        better += key[j] > low || (col < n && (col < s.first || col >= n - s.last));
-        same += key[j] == low;
-    }
-    exchange(lanes64(better, Sum()), lanes64(same, Sum()), as, bs);
-    int at = 0, equal = 0, total_better = 0, total_same = 0;
+        for (int j = 0; j < R; ++j) { better += key[j] > low; same += key[j] == low; }
+        exchange(lanes64(better, Sum()), lanes64(same, Sum()), as, bs);
+        int total_same = 0;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        at += w < wave ? as[w] : 0;
-        equal += w < wave ? bs[w] : 0;
-        total_better += as[w];
-        total_same += bs[w];
+        for (int w = 0; w < W; ++w) {
+            at += w < wave ? as[w] : 0;
+            equal += w < wave ? bs[w] : 0;
+            total += as[w];
+            total_same += bs[w];
+        }
+        at += equal < ties ? equal : ties;
+        total += total_same < ties ? total_same : ties;
     }
     if (unit > last_unit) return;
-    at += equal < ties ? equal : ties;
-    const uint64_t before = (1ull << lane) - 1;
+    const bool all_equals = ties == 1 << 30;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-        const int col = 64 * (R * wave + j) + lane;
-        const uint64_t all_same = __ballot(key[j] == low);
-        const bool always = col < n && (col < s.first || col >= n - s.last), tie = key[j] == low && equal + __popcll(all_same & before) < ties;
-        const uint64_t all_in = __ballot(always || key[j] > low || tie);
-        if (all_in >> lane & 1) out[at + __popcll(all_in & before)] = col;
-        at += __popcll(all_in);
-        equal += __popcll(all_same);
+        uint64_t in = __ballot(key[j] >= low);
+        if (!in) continue;
+        if (!all_equals) {
+            const uint64_t same = __ballot(key[j] == low);
+            in = __ballot(key[j] > low || (key[j] == low && equal + __popcll(same & before) < ties));
+            equal += __popcll(same);
+        }
+        if (in >> lane & 1) out[at + __popcll(in & before)] = 64 * (R * wave + j) + lane;
+        at += __popcll(in);
     }
-    for (int i = total_better + (total_same < ties ? total_same : ties) + (int)(threadIdx.x % (64 * W)); i < s.count; i += 64 * W) out[i] = -1;
+    if constexpr (W == 1) total = at - head;
+    const int t = (int)(threadIdx.x % (64 * W)), tail = n > head ? (s.last < n - head ? s.last : n - head) : 0;
+    for (int i = t; i < head; i += 64 * W) out[i] = i;
+    for (int i = t; i < tail; i += 64 * W) out[head + total + i] = n - tail + i;
+    for (int i = head + total + tail + t; i < s.count; i += 64 * W) out[i] = -1;
 }
 
 // Longer rows, a workgroup a row and head: the order of the count-th highest score is found eight bits at a time by counting, then what is above it, and
