@@ -74,9 +74,11 @@ PickWork pick_work(const ivftq_kv_cache& c, int64_t rows, int q_heads, int max_n
     const int format = c.format, d = c.d, group = q_heads / c.heads;
     const int64_t all = rows * q_heads;
     w.col_tiles = (group + 15) / 16;
-    // Rows of a unit: their heads fill a product's columns, their columns' bits and their lists 16 KB and 4,096 places.
+    // Rows of a unit: their heads fill a product's columns, their columns' bits and their lists 16 KB and 4,096 places (a chunk of 794 rows, four
+    // heads a group: 94 us, two rows each 121, one 153).  Where the rows alone are too few for the chip each is worked on by itself (eight
+    // sequences of four new rows: 16 us, 23 together).
     w.words = (c.columns + 31) / 32;
-    w.tokens = group < 16 ? 16 / group : 1;
+    w.tokens = group < 16 && rows * c.heads >= 1024 ? 16 / group : 1;
     if (w.tokens > max_new) w.tokens = max_new;
     while (w.tokens > 1 && ((int64_t)w.tokens * w.words > 4096 || (int64_t)w.tokens * count > kMostPicks)) --w.tokens;
     if (w.tokens == 1) w.words = 0;
@@ -84,7 +86,8 @@ PickWork pick_work(const ivftq_kv_cache& c, int64_t rows, int q_heads, int max_n
     w.units = (int32_t)(w.tokens == 1 ? rows : rows / w.tokens + c.batch);
     // as many workgroups as the chip holds, but eight tiles for each, two for each of its wavefronts: the second kernel costs what those do
     const int64_t pairs = (int64_t)w.units * c.heads * w.col_tiles, most = (int64_t)(count < c.columns ? count : c.columns) * c.page / kFewTile / 8;
-    int64_t splits = pairs ? 256 * (d <= 64 ? 4 : (d <= 128 ? 3 : 1)) / pairs : 1;
+    const int64_t busy = (w.tokens == 1 ? rows : (rows / w.tokens > c.batch ? rows / w.tokens : c.batch)) * c.heads * w.col_tiles;
+    int64_t splits = busy ? 256 * (d <= 64 ? 4 : (d <= 128 ? 3 : 1)) / busy : 1;
     splits = splits < most ? splits : most;
     w.splits = (int)(splits < 1 ? 1 : (splits < 64 ? splits : 64));
     int64_t at = 0;

@@ -401,13 +401,14 @@ hipError_t launch_kv_digest(const KvView& c, void* digests, int d, int format, h
 }
 hipError_t launch_kv_select(const KvSelect& s, hipStream_t st) {
     const int64_t units = (int64_t)s.c.rows * s.c.heads;
-    // Many pairs: a wavefront each, with as many registers as its row is long (6,432 rows of 1,251: 24 us, four wavefronts each 37); few: four
-    // wavefronts (32 rows of 2,048: 8.6 us, one each 14.3, sixteen 11.6).
+    // Many pairs: a wavefront each, with as many registers as its row is long (6,352 pairs of 1,251 columns: 20.5 us, four wavefronts each 36;
+    // 1,024 of 516: 7.6 and 9.9); few, or rows so long that a single wavefront takes too long for them: four (32 of 2,048: 8.5 us, one each 12.9;
+    // 1,024 of 2,032: 11.4 and 16).
     const int n = s.c.columns, of_one = (n + 255) / 256, of_four = (n + 511) / 512;
     auto one = [&](auto r) { k_kv_select_held<decltype(r)::value, 1><<<kv_grid((units + 3) / 4, 256), 256, 0, st>>>(s); };
     auto four = [&](auto r) { k_kv_select_held<decltype(r)::value, 4><<<kv_grid(units, 256), 256, 0, st>>>(s); };
     if (n > 4096) k_kv_select<<<kv_grid(units, 256), 256, 0, st>>>(s);
-    else if (units >= 1024 && n <= 2048)
+    else if (n <= 2048 && units >= (n <= 1280 ? 1024 : 4096))
         switch (of_one) {
             case 1: one(std::integral_constant<int, 4>{}); break;
             case 2: one(std::integral_constant<int, 8>{}); break;

@@ -5,7 +5,7 @@
 //   - Otherwise a second reading (k_sample_chunks) adds up the weights of every chunk, and where a rank is looked for by its number or its mass, of
 //     2,048 bins of logits.  A third reading (k_sample_bins) finds the bins in which the two ranks lie and lists their tokens, among which
 //     k_sample_rows counts ranks.
-//   - Rows of up to 65,536 tokens are one workgroup's (k_sample_row), all of it in one launch.
+//   - Shorter rows are one workgroup's (k_sample_row), all of it in one launch.
 //   - The token is looked for in the chunk in which the sum passes u times all of it.
 // Where a list would be too long (thousands of tokens within a bin) the row is worked through digit by digit of the logits' order by one
 // workgroup.
@@ -39,6 +39,11 @@ constexpr int kFewRanks = 1024;                  // top_k that goes by the group
 constexpr int kList = 2048;                      // tokens of a list
 constexpr int kBins = 2048;
 constexpr int kSliceRows = 1024;                 // rows that share a workspace's places
+// Rows of up to 32,768 tokens, and of up to 65,536 where there are 256, are one workgroup's each, in one launch (32,000 tokens, 1 and 256 rows, top k
+// and top p: 14 and 25 us, 17 and 31 by chunks, which are three launches more; all tokens kept: 20 and 22, 15 and 26; 64,000 tokens, all kept:
+// 32 and 37 us, 15 and 39).
+constexpr int kOneRow = 1 << 16;
+inline bool one_row(int64_t rows, int32_t vocabulary) { return vocabulary <= kOneRow / 2 || (vocabulary <= kOneRow && rows >= 256); }
 
 // What a row's search by bins has found.
 struct RowBins {
@@ -118,9 +123,16 @@ __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t bits = __builtin_bit_cast(uint32_t, v);
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
-// A token's rank as a number: larger ones first.
-__device__ __forceinline__ uint64_t rank_of(float v, int i) { return (uint64_t)key_of(v) << 20 | (uint32_t)(kMostTokens - 1 - i); }
 __device__ __forceinline__ float of_key(uint32_t k) { return __builtin_bit_cast(float, k >> 31 ? k & 0x7fffffffu : ~k); }
+// A token's rank as a number, larger ones first: the key, without the bits that its type leaves alike, and the place from the end.
+template <int T> constexpr int kSpare = T == IVFTQ_LOGITS_F32 ? 0 : (T == IVFTQ_LOGITS_F16 ? 13 : 16);
+template <int T>
+__device__ __forceinline__ uint64_t rank_of(float v, int i) { return (uint64_t)(key_of(v) >> kSpare<T>) << 20 | (uint32_t)(kMostTokens - 1 - i); }
+template <int T>
+__device__ __forceinline__ float of_rank(uint64_t r) {
+    const uint32_t k = (uint32_t)(r >> 20) << kSpare<T>;
+    return of_key(k >> 31 ? k : k | ((1u << kSpare<T>) - 1));
+}
 
 // e^x for x <= 0 to about 2^-50: x = n ln 2 + r, |r| <= ln 2 / 2, the series of e^r up to r^12.
 __device__ __forceinline__ double exp64(double x) {
@@ -625,7 +637,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (open >> (8 * j + e) & 1) {
-                if (at < kList) a.list[(int64_t)r * kList + at] = rank_of(v[j][e], chunk * kChunk + (j * kChunkThreads + (int)threadIdx.x) * 8 + e);
+                if (at < kList) a.list[(int64_t)r * kList + at] = rank_of<T>(v[j][e], chunk * kChunk + (j * kChunkThreads + (int)threadIdx.x) * 8 + e);
                 ++at;
             }
 }
@@ -717,7 +729,7 @@ __device__ __forceinline__ void locate(const SampleArgs& a, int r, const Weights
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         w[e] = weight(v[e]);
-        one[e] = i + e < a.vocabulary && rank_of(v[e], i + e) >= cut && w[e] >= least ? Weights::whole(w[e]) : 0;
+        one[e] = i + e < a.vocabulary && rank_of<T>(v[e], i + e) >= cut && w[e] >= least ? Weights::whole(w[e]) : 0;
         sum += one[e];
     }
     uint64_t at = before + scan(sum, s.sums, whole) - sum;
@@ -788,7 +800,7 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
             uint32_t begin = 0;
             if (lane == 0 && which) begin = atomicAdd(&s.many, (uint32_t)__popcll(which));
             const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)begin) + (uint32_t)__popcll(which & ((1ull << lane) - 1));
-            if (in && at < kList) s.rank[at] = rank_of(v, i);
+            if (in && at < kList) s.rank[at] = rank_of<T>(v, i);
         });
         __syncthreads();
         return (int)s.many;
@@ -816,7 +828,7 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
         const int i = threadIdx.x + e * kThreads;
         rank[e] = i < n ? s.rank[i] : any;
         amount[e] = i < n;
-        w[e] = i < n ? weight(of_key((uint32_t)(rank[e] >> 20))) : 0.0;
+        w[e] = i < n ? weight(of_rank<T>(rank[e])) : 0.0;
         place[e] = rank[e] & (kMostTokens - 1);
         mixed |= rank[e] ^ any;
     }
@@ -830,7 +842,7 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     sum = 0;
 #pragma unroll
     for (int e = 0; e < kHeld; ++e) sum += amount[e] = rank[e] >= cut && w[e] >= how.least ? amount[e] : 0;
-    const uint64_t kept = all_threads(sum, s.sums, Sum()), found = find_rank(place, amount, 19, 0, target_of(a.u[r], kept) + 1, s);
+    const uint64_t kept = all_threads(sum, s.sums, Sum()), found = find_rank(place, amount, 31 - __builtin_clz((uint32_t)a.vocabulary | 1), 0, target_of(a.u[r], kept) + 1, s);
 #pragma unroll
     for (int e = 0; e < kHeld; ++e)
         if (amount[e] && place[e] == found) drawn(a, r, kMostTokens - 1 - (int)found, w[e], kept);
@@ -850,7 +862,7 @@ __device__ __forceinline__ void cut_list(const SampleArgs& a, int r, const Setti
     for (int e = 0; e < kHeld; ++e) {
         const int i = threadIdx.x + e * kThreads;
         rank[e] = i < n ? list[i] : any;
-        const float v = of_key((uint32_t)(rank[e] >> 20));
+        const float v = of_rank<T>(rank[e]);
         bin[e] = i < n ? bins(v) : kBins + 1;
         w[e] = i < n ? weight(v) : 0.0;
         mass[e] = i < n ? Weights::whole(w[e]) : 0;
@@ -917,8 +929,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_rows(SampleArgs a) {
     if (!done) whole_row<T>(a, r, how, s.whole);
 }
 
-// Rows of up to kOneRow tokens: the same by one workgroup a row, its numbers in LDS, in one launch.
-constexpr int kOneRow = 1 << 16;
+// The same by one workgroup a row, its numbers in LDS, in one launch.
 template <int T>
 __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
     struct Parts {
@@ -1003,7 +1014,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
                     sum += bin < f.p0 && w >= how.least ? Weights::whole(w) : 0;
                     if (bin >= f.p0 && (bin <= f.p1 || bin == f.bin_k)) {
                         const uint32_t to = atomicAdd(&s.list.many, 1u);
-                        if (to < kList) s.list.rank[to] = rank_of(v[e], i + e);
+                        if (to < kList) s.list.rank[to] = rank_of<T>(v[e], i + e);
                     }
                 }
                 sum = lanes64(sum, Sum());
@@ -1022,7 +1033,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
 struct SampleWork { int64_t chunk_top, chunk_low, chunk_at, group_top, chunk_mass, bin_mass, bin_count, list, list_count, found, bytes; };
 SampleWork sample_work(int64_t rows, int32_t vocabulary) {
     SampleWork w{};
-    if (vocabulary <= kOneRow) return w;
+    if (one_row(rows, vocabulary)) return w;
     if (rows > kSliceRows) rows = kSliceRows;
     const int64_t chunks = (vocabulary + kChunk - 1) / kChunk;
     int64_t at = 0;
@@ -1044,7 +1055,7 @@ SampleWork sample_work(int64_t rows, int32_t vocabulary) {
 template <int T>
 hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st) {
     a.chunks = (a.vocabulary + kChunk - 1) / kChunk;
-    if (a.vocabulary <= kOneRow) {
+    if (one_row(a.rows, a.vocabulary)) {
         k_sample_row<T><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }

@@ -51,7 +51,7 @@ WAYS = [dict(), dict(temperature=0.0), dict(temperature=0.7, top_k=40), dict(top
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("v", (1, 2, 63, 1000, 1024, 1025, 5000, 32_001, 65_536, 65_537))
+@pytest.mark.parametrize("v", (1, 2, 63, 1000, 1024, 1025, 5000, 32_001, 32_768, 32_769))
 @pytest.mark.parametrize("way", range(len(WAYS)))
 def test_settings(kind, v, way):
     rows = 6
@@ -191,3 +191,12 @@ def test_large_logits_that_stand_together(kind, v):
     x = x.to(TYPES[kind])
     for how in (dict(top_k=50), dict(top_k=400, top_p=0.9), dict(top_k=1024), dict(top_k=1000, min_p=0.01), dict(top_k=1025), dict(top_p=0.9), dict(min_p=0.3), dict(min_p=1e-9)):
         check(x, np.linspace(0.05, 0.95, 4), **how)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_many_rows_of_middling_vocabularies(kind):
+    """One workgroup a row, and several."""
+    for rows, v in ((255, 40_000), (256, 40_000), (260, 65_536)):
+        r = np.random.default_rng(rows)
+        check(logits(v, rows, v, kind), r.random(rows, np.float32), temperature=r.choice([0.0, 0.7, 1.2], rows), top_k=r.choice([0, 30, 1500], rows),
+              top_p=r.choice([0.5, 0.95, 1.0], rows), min_p=r.choice([0.0, 0.05], rows))
