@@ -119,7 +119,9 @@ int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int
  * token of a sequence as a new row its digests are made afresh.  Coordinates that are no number count for nothing. */
 ivftq_status ivftq_kv_digest(const ivftq_kv_cache* cache, void* digests, const int32_t* starts, void* stream);
 
-/* scores: rows x heads x columns floats; -infinity where a page holds no token that the row sees (behind its position, no page).
+/* scores: rows x heads x columns floats; -infinity where a page holds no token that the row sees (behind its position, no page).  A page with
+ * an infinite key coordinate has no number for a score (ivftq_kv_select then gives it only as one of the first or last) where no query of
+ * the group has a coordinate of the sign that meets it.
  * q, starts, max_new as in ivftq_kv_attend; rows that it gives no result keep their scores.  workspace: ivftq_kv_score_workspace
  * bytes (starts NULL: of max_new = 1), 256-byte aligned. */
 ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts,

