@@ -109,7 +109,8 @@ ScoreWork score_work(int format, int d, int64_t rows, int q_heads, int kv_heads,
     ScoreWork w{};
     int64_t at = 0;
     auto room = [&](int64_t bytes) { const int64_t p = at; at += round_up64(bytes, 256); return p; };
-    if (format == IVFTQ_KV_CODE4) {
+    w.z = -1;
+    if (format == IVFTQ_KV_CODE4 && (one || 16 % (q_heads / kv_heads))) {
         w.z = room(rows * q_heads * d * 4);
         w.zn = room(rows * q_heads * 4);
     }

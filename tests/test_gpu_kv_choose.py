@@ -145,7 +145,7 @@ def test_scores(form, kind, d, page, news):
 
 
 @pytest.mark.parametrize("form,kind", FORMS[:3])
-@pytest.mark.parametrize("group", (1, 2, 7, 16, 33))
+@pytest.mark.parametrize("group", (1, 2, 4, 7, 8, 16, 33))
 @pytest.mark.parametrize("most", (17, 1))
 def test_scores_of_strided_queries(form, kind, group, most):
     """Queries side by side with keys and values, a table with a stride, scores in a given place that rows past max_new keep."""
