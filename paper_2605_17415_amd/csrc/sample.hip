@@ -493,8 +493,9 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_chunks(SampleArgs a) {
     const Weights weight(x.top, how.temperature, table);
     if (how.way == kAll) {
         uint64_t sum = 0;
-        // a logit whose weight is surely too small: the logarithm and its product are good to 2^-20 of themselves
-        const float under = how.least > 0.0 ? x.top + how.temperature * (1.000002f * logf((float)how.least)) - __builtin_fabsf(x.top) * 1e-6f : -INFINITY;
+        // a logit whose weight is surely too small: the logarithm and its product are good to 2^-20 of themselves (and under zero, for infinite
+        // temperatures, whose weights are all 1)
+        const float under = how.least > 0.0 ? x.top + how.temperature * (1.000002f * logf((float)how.least) - 1e-6f) - __builtin_fabsf(x.top) * 1e-6f : -INFINITY;
 #pragma unroll
         for (int j = 0; j < kEach; ++j)
 #pragma unroll

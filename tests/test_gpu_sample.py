@@ -104,6 +104,17 @@ def test_no_numbers(kind):
             check(x, u, temperature=[float("inf")] * 9)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("v", (3000, 70_000))
+def test_temperatures_that_leave_all_weights_alike(kind, v):
+    x = logits(v, 4, v, kind)
+    x[1, torch.rand(v, generator=torch.Generator().manual_seed(9)) < 0.7] = -torch.inf
+    x[2, 3], x[3, 5] = torch.nan, torch.inf
+    for temperature in (float("inf"), 1e38, 1e30):
+        for how in (dict(), dict(min_p=0.5), dict(min_p=1.0), dict(min_p=1.0, top_k=2000), dict(min_p=1.0, top_p=0.5)):
+            check(x, [0.2, 0.99, 0.6, 0.4], temperature=temperature, **how)
+
+
 def test_settings_out_of_range_in_arrays():
     """They count as the end of the range that they lie behind, no number as no restriction, a temperature that is none as zero."""
     x = logits(4, 6, 4000, "f32")
