@@ -606,11 +606,13 @@ struct UnitRows {
         float sum = 0.f;
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) sum += square[s][n];
-        const float norm = sqrtf(sum), scale = norm > 0.f ? kSplitScale / norm : 0.f;
+        const float norm = sqrtf(sum), inv = norm > 0.f ? 1.f / norm : 0.f;
         halfx8 h, l;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float v = x[e] * scale;
+            // Rounded, and then by a power of two: of a single product the compiler makes h once from the rounded and once from the exact one, and
+            // where the rounded one lies between two halves (one in 8,192) l does not fit the h that is stored.
+            const float v = x[e] * inv * kSplitScale;
             h[e] = (_Float16)v;
             l[e] = (_Float16)(v - (float)h[e]);
         }

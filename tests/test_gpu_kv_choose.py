@@ -169,6 +169,28 @@ def test_scores_of_strided_queries(form, kind, group, most):
     assert np.array_equal(np.isneginf(got[rows]), np.isneginf(want[rows])) and (np.abs(got[fine] - want[fine]) <= bound[fine]).all()
 
 
+@pytest.mark.parametrize("kind", ("f16", "bf16"))
+@pytest.mark.parametrize("group", (1, 4, 16))
+@pytest.mark.parametrize("d", (64, 96, 128, 192, 256))
+def test_scores_over_codes_of_whole_groups(d, group, kind):
+    """Every head size where sides come straight from the queries: large, small and zero rows, more rows than a workgroup's, an odd number of heads."""
+    lens, news = [900, 77], [61, 14]
+    c = ref.Cache(d, "code4", 3, d, 32, lens, columns=40)
+    t, codec = c.device()
+    g = torch.Generator().manual_seed(d + group)
+    q = torch.randn(75, 3 * group, d, generator=g)
+    q[3] *= 1000.0
+    q[17, ::2] *= 2.0 ** -12
+    q[18], q[19, 0] = 0.0, 0.0
+    q = q.to(ref.TYPES[kind])
+    box = torch.randn(c.pages, 3, 2, d, generator=g).sort(dim=2).values.to(torch.float16)
+    got = _pkg().kv_score(q.to(DEV), box.to(DEV), t["pool"], t["table"], t["lengths"], starts=starts_of(news), max_new=61, **codec).double().cpu().numpy()
+    want, bound = pick.scores(c, q, box, news)
+    assert np.array_equal(np.isneginf(got), np.isneginf(want))
+    fine = np.isfinite(want)
+    assert (np.abs(got[fine] - want[fine]) <= bound[fine]).all()
+
+
 @pytest.mark.parametrize("form", ("f16", "code4"))
 def test_scores_bound_the_products(form):
     """What the scores are for: no key of the page has a larger product, summed over the group's heads."""
