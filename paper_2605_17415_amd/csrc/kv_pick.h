@@ -11,7 +11,7 @@
 // several workgroups share a unit's tiles, and a second kernel joins their parts.
 //
 // Measured: scores of four new rows over 42,000 (head, page) pairs of 128 coordinates in bfloat16 7.5 us, 22 MB of digests (2.9 TB/s); of 794 rows over
-// up to 641 pages of codes 42 us, 18 of them the products.  Attention of 32 rows, 8 heads, over 64 pages of 64 tokens each in
+// up to 641 pages of codes 36 us, 18 of them the products.  Attention of 32 rows, 8 heads, over 64 pages of 64 tokens each in
 // bfloat16: 95 us for 537 MB (5.7 TB/s); of 794 rows over 16 pages each: 94 us, 1.9 GB from the L2 (20 TB/s).
 #pragma once
 #include "kv_many.h"
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void k_kv_sides(ScoreArgs f) {
 }
 
 // Codes, where 16 rows of (row, query head) pairs are whole groups: sides made by the workgroup that rotates the queries, as k_kv_rotate_queries
-// does it, which leaves nothing in between (25,000 pairs of 128: 17 us and 9 otherwise).
+// does it, which leaves nothing in between (25,000 pairs of 128: 20 us; in two kernels 17 and 9).
 template <int D>
 __global__ __launch_bounds__(D * 2) void k_kv_rotate_sides(ScoreArgs f, int tiles) {
     __shared__ UnitRows<D> unit;
