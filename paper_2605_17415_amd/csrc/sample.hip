@@ -197,18 +197,20 @@ struct AnyWeights : Weights {
 // A share of a mass: the tokens that less than it comes before are those that less than this whole number does.
 __device__ __forceinline__ uint64_t share_of(float p, uint64_t mass) { return (uint64_t)__builtin_ceil((double)p * (double)mass); }
 
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
 // Sum over the threads up to this one; all: over all threads.  sums: W numbers in LDS.
-template <int W = kWaves, class T>
-__device__ __forceinline__ T scan(T v, T* sums, T& all) {
-    const T incl = lanes_upto(v);
+template <int W = kWaves>
+__device__ __forceinline__ uint64_t scan(uint64_t v, uint64_t* sums, uint64_t& all) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const uint64_t incl = lanes_upto(v);
     __syncthreads();
-    if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = incl;
+    if (lane == 63) sums[wave] = incl;
     __syncthreads();
-    T before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) { before += w < (int)(threadIdx.x >> 6) ? sums[w] : 0; all += sums[w]; }
-    return before + incl;
+    const uint64_t of = lane < W ? sums[lane] : 0, upto = lanes_upto(of);
+    all = lane_value(upto, W - 1);
+    return lane_value(upto - of, wave) + incl;
 }
 
 struct Shared {
@@ -337,7 +339,7 @@ __device__ void whole_row(const SampleArgs& a, int r, const Settings& how, Share
         __syncthreads();
         if (s.digit != 0xffffffffu) {
             const int i = (int)s.digit * kBlock + threadIdx.x;
-            const uint64_t before = s.above, is = i < n && key_of(logit<T>(row, i)) == cut;
+            const uint64_t before = s.above, is = i < n && key_of(logit<T>(row, i)) == cut ? 1 : 0;
             __syncthreads();
             const uint64_t place = before + scan(is, s.sums, all);
             if (is && place == ties) s.digit = (uint32_t)i;
@@ -650,32 +652,48 @@ __global__ __launch_bounds__(kChunkThreads) void k_sample_bins(SampleArgs a) {
 // ---- rows --------------------------------------------------------------------------------------------------------------
 
 struct ListShared {
-    uint64_t bins[1024], sums[kWaves], value[4];
+    // Bins of find_rank, their amounts and tokens: one of the two is in use, the other one cleared for the next step.  Before, few_ranks keeps in the
+    // second ones the numbers of the groups and what their bins count.
+    uint64_t bins[2][1024], sums[8][kWaves], value[4];
+    uint32_t tally[2][1024], many[3];
     uint64_t mass[kMostTokens / kChunk];           // of chunks
     uint64_t rank[kList];                          // the list's tokens
-    uint32_t counts[1024], many;
-    int groups[kList];
     double table[64];
+    __device__ __forceinline__ void clear() { bins[0][threadIdx.x] = 0; tally[0][threadIdx.x] = 0; }       // for the first find_rank, a barrier before it
 };
 
-// Over all threads.
+// Over all threads; at: a number a wavefront, not read since the last barrier.
 template <class T, class Op>
 __device__ __forceinline__ T all_threads(T v, uint64_t* sums, Op op) {
     T* at = reinterpret_cast<T*>(sums);
     v = lanes64(v, op);
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
     __syncthreads();
-    T all = at[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) all = op(all, at[w]);
-    return all;
+    const T v8 = lanes8(at[threadIdx.x & (kWaves - 1)], op);
+    return op(v8, lane_moved<0x140>(v8));
+}
+
+// The first of 1,024 bins up to which `want` is reached, the sums before it and up to it (the last bin where none does); the same for every
+// thread, with one barrier: each wavefront reads the sums of all and the bins of the one that has it.  `clear` runs before the barrier.
+struct FoundBin { int bin; uint64_t before, upto; };
+template <class T, class Clear>
+__device__ __forceinline__ FoundBin find_bin(const T* bins, uint64_t before, uint64_t want, uint64_t* sums, Clear clear) {
+    const int lane = threadIdx.x & 63;
+    const uint64_t incl = lanes_upto((uint64_t)bins[threadIdx.x]);
+    if (lane == 63) sums[threadIdx.x >> 6] = incl;
+    clear();
+    __syncthreads();
+    const uint64_t of_wave = lane < kWaves ? sums[lane] : 0, upto_wave = before + lanes_upto(of_wave), in_wave = __ballot(upto_wave >= want) & ((1ull << kWaves) - 1);
+    const int wave = in_wave ? __builtin_ctzll(in_wave) : kWaves - 1;
+    const uint64_t of = (uint64_t)bins[wave * 64 + lane], upto = lane_value(upto_wave - of_wave, wave) + lanes_upto(of), in = __ballot(upto >= want);
+    const int at = in ? __builtin_ctzll(in) : 63;
+    return {wave * 64 + at, lane_value(upto - of, at), lane_value(upto, at)};
 }
 
 // Of the tokens that have an amount, ordered by `by` (all different, the largest first), the one at which the sum reaches `want`: ten bits of `by`
-// at a time, from bit `high` on, until one token is left.  Each thread holds two.
+// at a time, from bit `high` on, until one token is left, two barriers each.  Each thread holds two.
 constexpr int kHeld = kList / kThreads;
-__device__ __forceinline__ uint64_t find_rank(const uint64_t (&by)[kHeld], const uint64_t (&amount)[kHeld], int high, uint64_t before, uint64_t want, ListShared& s) {
+__device__ __forceinline__ uint64_t find_rank(const uint64_t (&by)[kHeld], const uint64_t (&amount)[kHeld], int high, uint64_t before, uint64_t want, ListShared& s, int& turn) {
     uint32_t open = 0;
 #pragma unroll
     for (int e = 0; e < kHeld; ++e) open |= amount[e] ? 1u << e : 0;
@@ -683,31 +701,24 @@ __device__ __forceinline__ uint64_t find_rank(const uint64_t (&by)[kHeld], const
     while (true) {
         const int shift = past > 10 ? past - 10 : 0;
         const uint32_t mask = (1u << (past - shift)) - 1;
-        __syncthreads();
-        s.bins[threadIdx.x] = 0;
-        s.counts[threadIdx.x] = 0;
-        if (threadIdx.x == 0) { s.value[0] = 0; s.value[1] = before; s.value[2] = 1; }
-        __syncthreads();
+        uint64_t* bins = s.bins[turn];
+        uint32_t* tally = s.tally[turn];
+        turn ^= 1;
         uint32_t digit[kHeld];
 #pragma unroll
         for (int e = 0; e < kHeld; ++e) {
             digit[e] = mask - ((uint32_t)(by[e] >> shift) & mask);           // the largest first
             if (open >> e & 1) {
-                atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[digit[e]]), (unsigned long long)amount[e]);
-                atomicAdd(&s.counts[digit[e]], 1u);
+                atomicAdd(reinterpret_cast<unsigned long long*>(&bins[digit[e]]), (unsigned long long)amount[e]);
+                atomicAdd(&tally[digit[e]], 1u);
             }
         }
         __syncthreads();
-        uint64_t all;
-        const uint64_t mine = s.bins[threadIdx.x], upto = before + scan(mine, s.sums, all);
-        if (mine && upto >= want && upto - mine < want) { s.value[0] = threadIdx.x; s.value[1] = upto - mine; s.value[2] = s.counts[threadIdx.x]; }
-        __syncthreads();
-        const uint32_t found = (uint32_t)s.value[0];
-        before = s.value[1];
-        const bool last = s.value[2] <= 1 || shift == 0;
+        const FoundBin found = find_bin(bins, before, want, s.sums[7], [&]() __attribute__((always_inline)) { s.bins[turn][threadIdx.x] = 0; s.tally[turn][threadIdx.x] = 0; });
+        before = found.before;
 #pragma unroll
-        for (int e = 0; e < kHeld; ++e) open &= digit[e] == found ? ~0u : ~(1u << e);
-        if (last) break;
+        for (int e = 0; e < kHeld; ++e) open &= (int)digit[e] == found.bin ? ~0u : ~(1u << e);
+        if (tally[found.bin] <= 1 || shift == 0) break;
         past = shift;
     }
 #pragma unroll
@@ -720,24 +731,38 @@ __device__ __forceinline__ uint64_t find_rank(const uint64_t (&by)[kHeld], const
 // The token among those of rank `cut` and better, by the masses of the chunks (in `mass`, a number a chunk).
 template <int T>
 __device__ __forceinline__ void locate(const SampleArgs& a, int r, const Weights& weight, double least, uint64_t cut, const uint64_t* mass, ListShared& s) {
+    static_assert(kMostTokens / kChunk == 256, "a lane has four chunks");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     __syncthreads();
-    uint64_t all;
-    const uint64_t mine = (int)threadIdx.x < a.chunks ? mass[threadIdx.x] : 0, upto = scan(mine, s.sums, all), target = target_of(a.u[r], all);
-    if (upto > target && upto - mine <= target) { s.value[0] = threadIdx.x; s.value[1] = upto - mine; }
-    __syncthreads();
-    const int i = (int)s.value[0] * kChunk + (int)threadIdx.x * 4;
-    const uint64_t before = s.value[1];
+    // the chunk, by every wavefront
+    uint64_t m[4], own = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) own += m[e] = 4 * lane + e < a.chunks ? mass[4 * lane + e] : 0;
+    const uint64_t upto = lanes_upto(own), all = lane_value(upto, 63), target = target_of(a.u[r], all), in = __ballot(upto > target);
+    const int of = in ? __builtin_ctzll(in) : 63;
+    uint64_t before = lane_value(upto - own, of);
+    int chunk = 4 * of;
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+        const uint64_t past = before + lane_value(m[e], of);
+        if (chunk == 4 * of + e && past <= target) { before = past; ++chunk; }
+    }
+    const int i = chunk * kChunk + (int)threadIdx.x * 4;
     float v[4];
     logits_of<T, 4>(a.logits + (int64_t)r * a.row_stride * kSize<T>, i, a.vocabulary, v);
     double w[4];
-    uint64_t one[4], sum = 0, whole;
+    uint64_t one[4], sum = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         w[e] = weight(v[e]);
         one[e] = i + e < a.vocabulary && rank_of<T>(v[e], i + e) >= cut && w[e] >= least ? Weights::whole(w[e]) : 0;
         sum += one[e];
     }
-    uint64_t at = before + scan(sum, s.sums, whole) - sum;
+    const uint64_t incl = lanes_upto(sum);
+    if (lane == 63) s.sums[6][wave] = incl;
+    __syncthreads();
+    const uint64_t one_wave = lane < kWaves ? s.sums[6][lane] : 0;
+    uint64_t at = before + lane_value(lanes_upto(one_wave) - one_wave, wave) + incl - sum;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (at + one[e] > target && at <= target) drawn(a, r, i + e, w[e], all);
@@ -745,37 +770,84 @@ __device__ __forceinline__ void locate(const SampleArgs& a, int r, const Weights
     }
 }
 
+// Numbers over the lanes put in order, the largest first (a bitonic network: runs of 2, 4, .. 64 lanes, turn by turn rising and falling, are
+// joined by comparing lanes J apart).
+template <int J>
+__device__ __forceinline__ uint64_t ordered(uint64_t v, bool larger) {
+    if constexpr (J >= 16) {
+        uint32_t a, b, c, d;
+        lane_pair32<J == 32>((uint32_t)v, a, b);
+        lane_pair32<J == 32>((uint32_t)(v >> 32), c, d);
+        const uint64_t x = (uint64_t)c << 32 | a, y = (uint64_t)d << 32 | b;
+        return (x > y) == larger ? x : y;
+    } else {
+        uint64_t other;
+        if constexpr (J == 1) other = lane_moved<0xb1>(v);
+        else if constexpr (J == 2) other = lane_moved<0x4e>(v);
+        else if constexpr (J == 4) other = lane_moved<0x1b>(lane_moved<0x141>(v));      // the half row turned round, and its quads
+        else other = lane_moved<0x128>(v);
+        return (v > other) == larger ? v : other;
+    }
+}
+template <int K, int J>
+__device__ __forceinline__ uint64_t joined(uint64_t v) {
+    const int lane = threadIdx.x & 63;
+    v = ordered<J>(v, ((lane & J) == 0) == ((lane & K) == 0));
+    if constexpr (J > 1) v = joined<K, J / 2>(v);
+    return v;
+}
+__device__ __forceinline__ uint64_t in_order(uint64_t v) { return joined<64, 32>(joined<32, 16>(joined<16, 8>(joined<8, 4>(joined<4, 2>(joined<2, 1>(v)))))); }
+
+// Up to 64 listed tokens: by one wavefront, without a barrier, in the order of their ranks and then of their places.  (Sixteen wavefronts take about
+// 2,500 cycles a digit of find_rank, instructions of which each wavefront does its own; this takes as long as one or two.)
+template <int T>
+__device__ __forceinline__ void short_list(const SampleArgs& a, int r, const Settings& how, const Weights& weight, int n, const uint64_t* list) {
+    constexpr uint64_t kMass = (1ull << 43) - 1;          // a token's is 2^42 at most
+    const int lane = threadIdx.x & 63;
+    const uint64_t rank = in_order(lane < n ? list[lane] : 0);
+    const double w = weight(of_rank<T>(rank));
+    uint64_t mass = rank && lane < how.k ? Weights::whole(w) : 0;
+    if (how.p < 1.f) {
+        const uint64_t upto = lanes_upto(mass);
+        mass = upto - mass < share_of(how.p, lane_value(upto, 63)) ? mass : 0;
+    }
+    mass = w >= how.least ? mass : 0;
+    const uint64_t place = rank & (kMostTokens - 1), by_place = in_order(mass ? place << 43 | mass : 0), one = by_place & kMass, upto = lanes_upto(one);
+    const uint64_t all = lane_value(upto, 63), in = __ballot(upto > target_of(a.u[r], all));
+    const uint64_t found = lane_value(by_place, in ? __builtin_ctzll(in) : 63) >> 43;
+    if (mass && place == found) drawn(a, r, kMostTokens - 1 - (int)found, w, all);
+}
+
 // Few ranks: false where the list would be too long.
 template <int T>
 __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Settings& how, float top, const Weights& weight, const float* tops, int groups, ListShared& s) {
     const int lane = threadIdx.x & 63;
     const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
+    uint32_t* counts = s.tally[1];
+    int* of_groups = reinterpret_cast<int*>(s.bins[1]);
+    int turn = 0;
     // the bin of the k-th largest group maximum
     float low = INFINITY;
     for (int g = threadIdx.x; g < groups; g += kThreads) { const float t = tops[g]; low = t > -INFINITY ? fminf(low, t) : low; }
-    s.counts[threadIdx.x] = 0;
-    if (threadIdx.x == 0) { s.many = 0; s.value[0] = 1023; }
-    low = all_threads(low, s.sums, Smaller());
+    counts[threadIdx.x] = 0;
+    s.clear();
+    if (threadIdx.x < 3) s.many[threadIdx.x] = 0;
+    low = all_threads(low, s.sums[0], Smaller());
     const Bins bins(top, low, INFINITY, 1024);
     for (int g = threadIdx.x; g < groups; g += kThreads) {
         const float t = tops[g];
-        if (t > -INFINITY) atomicAdd(&s.counts[bins(t)], 1u);
+        if (t > -INFINITY) atomicAdd(&counts[bins(t)], 1u);
     }
     __syncthreads();
-    uint64_t all;
-    const uint64_t mine = s.counts[threadIdx.x], upto = scan(mine, s.sums, all);
-    if (upto >= (uint64_t)how.k && upto - mine < (uint64_t)how.k) { s.value[0] = threadIdx.x; s.value[1] = upto; }
-    if (threadIdx.x == 1023 && upto < (uint64_t)how.k) s.value[1] = upto;
-    __syncthreads();
-    const int cut_bin = (int)s.value[0];
-    if (s.value[1] > (uint64_t)kList) return false;
-    __syncthreads();
+    const FoundBin of_k = find_bin(counts, 0, (uint64_t)how.k, s.sums[1], []() {});
+    const int cut_bin = of_k.bin;
+    if (of_k.upto > (uint64_t)kList) return false;
     for (int g = threadIdx.x; g < groups; g += kThreads) {
         const float t = tops[g];
-        if (t > -INFINITY && bins(t) <= cut_bin) s.groups[atomicAdd(&s.many, 1u)] = g;
+        if (t > -INFINITY && bins(t) <= cut_bin) of_groups[atomicAdd(&s.many[0], 1u)] = g;
     }
     __syncthreads();
-    const int chosen = (int)s.many;
+    const int chosen = (int)s.many[0];
     // their tokens, a group a wavefront at a time: f(token, logit, bin, whether it may be among the first k)
     auto tokens = [&](auto&& f) __attribute__((always_inline)) {
         constexpr int kAhead = 4;
@@ -785,7 +857,7 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) {
                 const int u = u0 + e * kWaves;
-                i[e] = u < chosen ? s.groups[u] * kGroup + lane : a.vocabulary;
+                i[e] = u < chosen ? of_groups[u] * kGroup + lane : a.vocabulary;
                 v[e] = logit<T>(row, i[e] < a.vocabulary ? i[e] : 0);
             }
 #pragma unroll
@@ -795,35 +867,30 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
             }
         }
     };
-    auto list = [&](int last_bin) __attribute__((always_inline)) {
-        __syncthreads();
-        if (threadIdx.x == 0) s.many = 0;
-        __syncthreads();
+    auto list = [&](int last_bin, uint32_t& many) __attribute__((always_inline)) {
         tokens([&](int i, float v, int bin, bool) __attribute__((always_inline)) {
             const bool in = bin <= last_bin;
             const uint64_t which = __ballot(in);
             uint32_t begin = 0;
-            if (lane == 0 && which) begin = atomicAdd(&s.many, (uint32_t)__popcll(which));
+            if (lane == 0 && which) begin = atomicAdd(&many, (uint32_t)__popcll(which));
             const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)begin) + (uint32_t)__popcll(which & ((1ull << lane) - 1));
             if (in && at < kList) s.rank[at] = rank_of<T>(v, i);
         });
         __syncthreads();
-        return (int)s.many;
+        return (int)many;
     };
-    int n = list(cut_bin);
+    int n = list(cut_bin, s.many[1]);
     if (n > kList) {                               // large logits stand together: the bin of the k-th one, counted
+        counts[threadIdx.x] = 0;
         __syncthreads();
-        s.counts[threadIdx.x] = 0;
-        if (threadIdx.x == 0) s.value[0] = 1023;
+        tokens([&](int, float, int bin, bool in) __attribute__((always_inline)) { if (in) atomicAdd(&counts[bin], 1u); });
         __syncthreads();
-        tokens([&](int, float, int bin, bool in) __attribute__((always_inline)) { if (in) atomicAdd(&s.counts[bin], 1u); });
-        __syncthreads();
-        uint64_t total;
-        const uint64_t here = s.counts[threadIdx.x], so_far = scan(here, s.sums, total);
-        if (so_far >= (uint64_t)how.k && so_far - here < (uint64_t)how.k) s.value[0] = threadIdx.x;
-        __syncthreads();
-        n = list((int)s.value[0]);
+        n = list(find_bin(counts, 0, (uint64_t)how.k, s.sums[2], []() {}).bin, s.many[2]);
         if (n > kList) return false;
+    }
+    if (n <= 64) {
+        if (threadIdx.x < 64) short_list<T>(a, r, how, weight, n, s.rank);
+        return true;
     }
     uint64_t rank[kHeld], amount[kHeld], place[kHeld], mixed = 0, sum = 0;
     double w[kHeld];
@@ -837,17 +904,17 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
         place[e] = rank[e] & (kMostTokens - 1);
         mixed |= rank[e] ^ any;
     }
-    mixed = all_threads(mixed, s.sums, Union());
+    mixed = all_threads(mixed, s.sums[3], Union());
     const int high = 63 - __builtin_clzll(mixed | 1);
-    uint64_t cut = n > how.k ? find_rank(rank, amount, high, 0, (uint64_t)how.k, s) : 0;
+    uint64_t cut = n > how.k ? find_rank(rank, amount, high, 0, (uint64_t)how.k, s, turn) : 0;
 #pragma unroll
     for (int e = 0; e < kHeld; ++e) sum += amount[e] = amount[e] && rank[e] >= cut ? Weights::whole(w[e]) : 0;
-    if (how.p < 1.f) cut = find_rank(rank, amount, high, 0, share_of(how.p, all_threads(sum, s.sums, Sum())), s);
+    if (how.p < 1.f) cut = find_rank(rank, amount, high, 0, share_of(how.p, all_threads(sum, s.sums[4], Sum())), s, turn);
     // of what is kept, in the order of the tokens, the first up to which the mass passes the target
     sum = 0;
 #pragma unroll
     for (int e = 0; e < kHeld; ++e) sum += amount[e] = rank[e] >= cut && w[e] >= how.least ? amount[e] : 0;
-    const uint64_t kept = all_threads(sum, s.sums, Sum()), found = find_rank(place, amount, 31 - __builtin_clz((uint32_t)a.vocabulary | 1), 0, target_of(a.u[r], kept) + 1, s);
+    const uint64_t kept = all_threads(sum, s.sums[5], Sum()), found = find_rank(place, amount, 31 - __builtin_clz((uint32_t)a.vocabulary | 1), 0, target_of(a.u[r], kept) + 1, s, turn);
 #pragma unroll
     for (int e = 0; e < kHeld; ++e)
         if (amount[e] && place[e] == found) drawn(a, r, kMostTokens - 1 - (int)found, w[e], kept);
@@ -861,8 +928,9 @@ __device__ __forceinline__ void cut_list(const SampleArgs& a, int r, const Setti
                                          ListShared& s) {
     const uint64_t any = n ? list[0] : 0;
     uint64_t rank[kHeld], mass[kHeld], amount[kHeld], mixed = 0, cut = 0;
-    int bin[kHeld];
+    int bin[kHeld], turn = 0;
     double w[kHeld];
+    s.clear();
 #pragma unroll
     for (int e = 0; e < kHeld; ++e) {
         const int i = threadIdx.x + e * kThreads;
@@ -873,21 +941,21 @@ __device__ __forceinline__ void cut_list(const SampleArgs& a, int r, const Setti
         mass[e] = i < n ? Weights::whole(w[e]) : 0;
         mixed |= rank[e] ^ any;
     }
-    mixed = all_threads(mixed, s.sums, Union());
+    mixed = all_threads(mixed, s.sums[3], Union());
     const int high = 63 - __builtin_clzll(mixed | 1);
     uint64_t in_k = 0;
     if (f.bin_k < kBins) {
 #pragma unroll
         for (int e = 0; e < kHeld; ++e) amount[e] = bin[e] == f.bin_k;
-        cut = find_rank(rank, amount, high, f.count_k, (uint64_t)how.k, s);
+        cut = find_rank(rank, amount, high, f.count_k, (uint64_t)how.k, s, turn);
 #pragma unroll
         for (int e = 0; e < kHeld; ++e) in_k += bin[e] == f.bin_k && rank[e] >= cut ? mass[e] : 0;
     }
     if (how.p < 1.f) {
-        const uint64_t all = f.bin_k < kBins ? f.before_k + all_threads(in_k, s.sums, Sum()) : f.total;
+        const uint64_t all = f.bin_k < kBins ? f.before_k + all_threads(in_k, s.sums[4], Sum()) : f.total;
 #pragma unroll
         for (int e = 0; e < kHeld; ++e) amount[e] = bin[e] >= f.p0 && bin[e] <= f.p1 && rank[e] >= cut ? mass[e] : 0;
-        cut = find_rank(rank, amount, high, f.before_p, share_of(how.p, all), s);
+        cut = find_rank(rank, amount, high, f.before_p, share_of(how.p, all), s, turn);
     }
 #pragma unroll
     for (int e = 0; e < kHeld; ++e)
@@ -910,7 +978,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_rows(SampleArgs a) {
         if (how.way == kTop)
             for (int c = threadIdx.x; c < a.chunks; c += kThreads)
                 if (a.chunk_top[(int64_t)r * a.chunks + c] == x.top) at = min(at, a.chunk_at[(int64_t)r * a.chunks + c]);
-        top_token(a, r, x.top, all_threads(at, s.list.sums, Smaller()));
+        top_token(a, r, x.top, all_threads(at, s.list.sums[0], Smaller()));
         return;
     }
     bool done = x.top < INFINITY;
@@ -970,9 +1038,9 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
         x.top = fmaxf(x.top, most);
     }
     const float mine = x.top;
-    x.top = all_threads(x.top, s.list.sums, Larger());
+    x.top = all_threads(x.top, s.list.sums[6], Larger());
     if (x.top == -INFINITY || how.way == kTop) {
-        top_token(a, r, x.top, all_threads(mine == x.top ? at : n, s.list.sums, Smaller()));
+        top_token(a, r, x.top, all_threads(mine == x.top ? at : n, s.list.sums[0], Smaller()));
         return;
     }
     bool done = x.top < INFINITY;
@@ -983,11 +1051,11 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
             done = few_ranks<T>(a, r, how, x.top, weight, s.group_top, (n + kGroup - 1) / kGroup, s.list);
         } else {
             const bool binned = how.way == kBinned;
-            x.low = all_threads(x.low, s.list.sums, Smaller());
+            x.low = all_threads(x.low, s.list.sums[0], Smaller());
             const Bins bins = row_bins(x, how);
             RowBins f{0, 0, 0, kBins, kBins, kBins, 0};
             if (threadIdx.x < kOneRow / kChunk) s.list.mass[threadIdx.x] = 0;
-            if (threadIdx.x == 0) s.list.many = 0;
+            if (threadIdx.x == 0) s.list.many[0] = 0;
             if (binned) {
                 for (int i = threadIdx.x; i < kBins; i += kThreads) { s.bin_mass[i] = 0; s.bin_count[i] = 0; }
                 __syncthreads();
@@ -1004,7 +1072,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
                     }
                 }
                 __syncthreads();
-                f = look_up<kWaves>(s.bin_mass, s.bin_count, how, s.list.sums, s.list.value);
+                f = look_up<kWaves>(s.bin_mass, s.bin_count, how, s.list.sums[1], s.list.value);
             }
             __syncthreads();
             for (int i0 = 0; i0 < n; i0 += kThreads * 4) {           // a chunk
@@ -1018,7 +1086,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
                     const double w = weight(v[e]);
                     sum += bin < f.p0 && w >= how.least ? Weights::whole(w) : 0;
                     if (bin >= f.p0 && (bin <= f.p1 || bin == f.bin_k)) {
-                        const uint32_t to = atomicAdd(&s.list.many, 1u);
+                        const uint32_t to = atomicAdd(&s.list.many[0], 1u);
                         if (to < kList) s.list.rank[to] = rank_of<T>(v[e], i + e);
                     }
                 }
@@ -1026,7 +1094,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
                 if (lane == 0 && sum) atomicAdd(reinterpret_cast<unsigned long long*>(&s.list.mass[i0 / kChunk]), (unsigned long long)sum);
             }
             __syncthreads();
-            const int many = (int)s.list.many;
+            const int many = (int)s.list.many[0];
             done = many <= kList;
             if (done && binned) cut_list<T>(a, r, how, weight, bins, f, s.list.rank, many, s.list);
             else if (done) locate<T>(a, r, weight, how.least, 0, s.list.mass, s.list);
