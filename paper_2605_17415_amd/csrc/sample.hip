@@ -469,8 +469,9 @@ struct Bins {
         by = wide > 0.f ? (float)bins / wide : 0.f;
         if (!(by < 1e30f)) by = 1e30f;
     }
+    __device__ __forceinline__ float scaled(float v) const { return (top - v) * by; }
     __device__ __forceinline__ int operator()(float v) const {      // v above -infinity
-        const float x = (top - v) * by;
+        const float x = scaled(v);
         return x < (float)last ? (int)x : last;
     }
 };
@@ -821,7 +822,6 @@ __device__ __forceinline__ void short_list(const SampleArgs& a, int r, const Set
 // Few ranks: false where the list would be too long.
 template <int T>
 __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Settings& how, float top, const Weights& weight, const float* tops, int groups, ListShared& s) {
-    const int lane = threadIdx.x & 63;
     const char* row = a.logits + (int64_t)r * a.row_stride * kSize<T>;
     uint32_t* counts = s.tally[1];
     int* of_groups = reinterpret_cast<int*>(s.bins[1]);
@@ -848,33 +848,38 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     }
     __syncthreads();
     const int chosen = (int)s.many[0];
-    // their tokens, a group a wavefront at a time: f(token, logit, bin, whether it may be among the first k)
-    auto tokens = [&](auto&& f) __attribute__((always_inline)) {
-        constexpr int kAhead = 4;
-        for (int u0 = threadIdx.x >> 6; u0 < chosen; u0 += kWaves * kAhead) {
-            float v[kAhead];
+    // their tokens, eight a thread and two such pieces on their way: f(token, logit) for those in the bins up to last_bin.  Few of them are, and all
+    // sixteen wavefronts' instructions count: what is not needed for the others is done for those alone (their bins and ranks for all: 15,000 cycles
+    // for 411 groups; a group a wavefront: 22,000).
+    auto tokens = [&](int last_bin, auto&& f) __attribute__((always_inline)) {
+        constexpr int kAhead = 2, kPieces = kGroup / 8;
+        const bool every = last_bin >= bins.last;
+        const float past = (float)(last_bin + 1);          // of bins.scaled
+        for (int u0 = threadIdx.x / kPieces; u0 < chosen; u0 += kThreads / kPieces * kAhead) {
+            float v[kAhead][8];
             int i[kAhead];
 #pragma unroll
-            for (int e = 0; e < kAhead; ++e) {
-                const int u = u0 + e * kWaves;
-                i[e] = u < chosen ? of_groups[u] * kGroup + lane : a.vocabulary;
-                v[e] = logit<T>(row, i[e] < a.vocabulary ? i[e] : 0);
+            for (int j = 0; j < kAhead; ++j) {
+                const int u = u0 + j * (kThreads / kPieces);
+                i[j] = u < chosen ? of_groups[u] * kGroup + (int)threadIdx.x % kPieces * 8 : a.vocabulary;
+                logits_of<T, 8>(row, i[j], a.vocabulary, v[j]);
             }
 #pragma unroll
-            for (int e = 0; e < kAhead; ++e) {
-                const int bin = i[e] < a.vocabulary && v[e] > -INFINITY ? bins(v[e]) : 1024;
-                f(i[e], v[e], bin, bin <= cut_bin);
+            for (int j = 0; j < kAhead; ++j) {
+                uint32_t in = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) in |= (every ? v[j][e] > -INFINITY : bins.scaled(v[j][e]) < past) ? 1u << e : 0;
+                for (; in; in &= in - 1) {
+                    const int at = i[j] + __builtin_ctz(in);
+                    f(at, logit<T>(row, at));
+                }
             }
         }
     };
     auto list = [&](int last_bin, uint32_t& many) __attribute__((always_inline)) {
-        tokens([&](int i, float v, int bin, bool) __attribute__((always_inline)) {
-            const bool in = bin <= last_bin;
-            const uint64_t which = __ballot(in);
-            uint32_t begin = 0;
-            if (lane == 0 && which) begin = atomicAdd(&many, (uint32_t)__popcll(which));
-            const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)begin) + (uint32_t)__popcll(which & ((1ull << lane) - 1));
-            if (in && at < kList) s.rank[at] = rank_of<T>(v, i);
+        tokens(last_bin, [&](int i, float v) __attribute__((always_inline)) {
+            const uint32_t at = atomicAdd(&many, 1u);
+            if (at < kList) s.rank[at] = rank_of<T>(v, i);
         });
         __syncthreads();
         return (int)many;
@@ -883,7 +888,7 @@ __device__ __forceinline__ bool few_ranks(const SampleArgs& a, int r, const Sett
     if (n > kList) {                               // large logits stand together: the bin of the k-th one, counted
         counts[threadIdx.x] = 0;
         __syncthreads();
-        tokens([&](int, float, int bin, bool in) __attribute__((always_inline)) { if (in) atomicAdd(&counts[bin], 1u); });
+        tokens(cut_bin, [&](int, float v) __attribute__((always_inline)) { atomicAdd(&counts[bins(v)], 1u); });
         __syncthreads();
         n = list(find_bin(counts, 0, (uint64_t)how.k, s.sums[2], []() {}).bin, s.many[2]);
         if (n > kList) return false;
