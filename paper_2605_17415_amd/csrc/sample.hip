@@ -13,9 +13,9 @@
 // Weights are whole numbers of 2^-42, so that partial sums of any split and order agree to the last bit, and e^x is computed in 64 bits:
 // a float32 weight is off by 2^-23, which over a hundred thousand tokens moves the drawn one in some of every thousand rows.
 //
-// Measured: 200 rows of 128,000 logits in bfloat16 with settings of all kinds 69 us, the first reading 11 (4.6 TB/s), the second and third 21 and 15,
-// of which the weights of half the rows (14 operations in 64 bits each) take most, the rows 25 (barriers of sixteen wavefronts: about eight a
-// digit of ten bits, two or three digits a rank, up to three ranks).  One row of 32,000 with top k and top p: 13 us.
+// Measured: 200 rows of 128,000 logits in bfloat16 with settings of all kinds 66 us, the first reading 11 (4.6 TB/s), the second and third 21 and 16,
+// of which the weights of half the rows (14 operations in 64 bits each) take a third, the rows 18 (16 us those of 400 ranks: sixteen wavefronts'
+// instructions, some 2,500 cycles a digit of ten bits).  One row of 32,000 with top k and top p: 9.2 us.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -43,11 +43,12 @@ constexpr int kFewRanks = 1024;                  // top_k that goes by the group
 constexpr int kList = 2048;                      // tokens of a list
 constexpr int kBins = 2048;
 constexpr int kSliceRows = 1024;                 // rows that share a workspace's places
-// Rows of up to 32,768 tokens, and of up to 65,536 where there are 256, are one workgroup's each, in one launch (32,000 tokens, 1 and 256 rows, top k
-// and top p: 14 and 25 us, 17 and 31 by chunks, which are three launches more; all tokens kept: 20 and 22, 15 and 26; 64,000 tokens, all kept:
-// 32 and 37 us, 15 and 39).
+// Rows that are one workgroup's each, in one launch: of up to 65,536 tokens where there are 256 (64,000: 17 us with top k and top p, 68 with top p alone, 40
+// with all tokens; by chunks 20, 109 and 41).  Fewer: up to 32,768 (one row of 32,000 with top k and top p: 9.3 us, 10.4 by chunks, which are three
+// launches more), but where it is known that every row needs all of its weights up to 16,384 (top p alone 23 and 24, all tokens 12 and
+// 12; of 32,000 34 and 24, 17 and 12).
 constexpr int kOneRow = 1 << 16;
-inline bool one_row(int64_t rows, int32_t vocabulary) { return vocabulary <= kOneRow / 2 || (vocabulary <= kOneRow && rows >= 256); }
+inline bool one_row(int64_t rows, int32_t vocabulary, bool weights) { return vocabulary <= (rows >= 256 ? kOneRow : (weights ? kOneRow / 4 : kOneRow / 2)); }
 
 // What a row's search by bins has found.
 struct RowBins {
@@ -1111,7 +1112,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
 struct SampleWork { int64_t chunk_top, chunk_low, chunk_at, group_top, chunk_mass, bin_mass, bin_count, list, list_count, found, bytes; };
 SampleWork sample_work(int64_t rows, int32_t vocabulary) {
     SampleWork w{};
-    if (one_row(rows, vocabulary)) return w;
+    if (one_row(rows, vocabulary, true)) return w;
     if (rows > kSliceRows) rows = kSliceRows;
     const int64_t chunks = (vocabulary + kChunk - 1) / kChunk;
     int64_t at = 0;
@@ -1133,7 +1134,11 @@ SampleWork sample_work(int64_t rows, int32_t vocabulary) {
 template <int T>
 hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st) {
     a.chunks = (a.vocabulary + kChunk - 1) / kChunk;
-    if (one_row(a.rows, a.vocabulary)) {
+    // what the settings of all rows rule out is not launched
+    const bool k = a.how.top_k || (a.how.top_k_all > 1 && a.how.top_k_all < a.vocabulary), few = !a.how.top_k && k && a.how.top_k_all <= kFewRanks;
+    const bool top = (!a.how.temperature && a.how.temperature_all == 0.f) || (!a.how.top_k && a.how.top_k_all == 1) || (!a.how.top_p && a.how.top_p_all == 0.f);
+    const bool again = !top && !few, binned = again && (k || a.how.top_p || a.how.top_p_all < 1.f);
+    if (one_row(a.rows, a.vocabulary, again && !a.how.top_k && !a.how.temperature)) {
         k_sample_row<T><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
@@ -1147,10 +1152,6 @@ hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st)
     a.list = reinterpret_cast<uint64_t*>(work + w.list);
     a.list_count = reinterpret_cast<uint32_t*>(work + w.list_count);
     a.found = reinterpret_cast<RowBins*>(work + w.found);
-    // what the settings of all rows rule out is not launched
-    const bool k = a.how.top_k || (a.how.top_k_all > 1 && a.how.top_k_all < a.vocabulary), few = !a.how.top_k && k && a.how.top_k_all <= kFewRanks;
-    const bool top = (!a.how.temperature && a.how.temperature_all == 0.f) || (!a.how.top_k && a.how.top_k_all == 1) || (!a.how.top_p && a.how.top_p_all == 0.f);
-    const bool again = !top && !few, binned = again && (k || a.how.top_p || a.how.top_p_all < 1.f);
     for (int64_t left = a.rows; left > 0; left -= kSliceRows) {
         const unsigned rows = (unsigned)(left < kSliceRows ? left : kSliceRows), wgs = rows * (unsigned)a.chunks;
         k_sample_tops<T><<<wgs, kChunkThreads, 0, st>>>(a);
