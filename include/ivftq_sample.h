@@ -53,8 +53,8 @@ typedef struct ivftq_sampling {
  * its content does not matter. */
 ivftq_status ivftq_sample_tokens(const ivftq_logits* logits, const float* u, const ivftq_sampling* how, int32_t* tokens, float* logprobs,
                                  void* workspace, int64_t workspace_bytes, void* stream);
-/* -1 for logits that ivftq_sample_tokens refuses. */
-int64_t ivftq_sample_workspace(const ivftq_logits* logits);
+/* -1 for logits that ivftq_sample_tokens refuses.  how NULL: enough for any. */
+int64_t ivftq_sample_workspace(const ivftq_logits* logits, const ivftq_sampling* how);
 
 #ifdef __cplusplus
 }

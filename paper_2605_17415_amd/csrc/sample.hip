@@ -1109,10 +1109,24 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a) {
     if (!done) whole_row<T>(a, r, how, shared.whole);
 }
 
+// What the settings of all rows tell: nothing without settings.
+struct Needs {
+    bool again, binned;                          // the second and the third reading are not ruled out
+    bool weights;                                // every row needs all of its weights
+    Needs(const ivftq_sampling* how, int32_t vocabulary) {
+        if (!how) { again = binned = weights = true; return; }
+        const bool k = how->top_k || (how->top_k_all > 1 && how->top_k_all < vocabulary), few = !how->top_k && k && how->top_k_all <= kFewRanks;
+        const bool top = (!how->temperature && how->temperature_all == 0.f) || (!how->top_k && how->top_k_all == 1) || (!how->top_p && how->top_p_all == 0.f);
+        again = !top && !few;
+        binned = again && (k || how->top_p || how->top_p_all < 1.f);
+        weights = again && !how->top_k && !how->temperature;
+    }
+};
+
 struct SampleWork { int64_t chunk_top, chunk_low, chunk_at, group_top, chunk_mass, bin_mass, bin_count, list, list_count, found, bytes; };
-SampleWork sample_work(int64_t rows, int32_t vocabulary) {
+SampleWork sample_work(int64_t rows, int32_t vocabulary, const Needs& needs) {
     SampleWork w{};
-    if (one_row(rows, vocabulary, true)) return w;
+    if (one_row(rows, vocabulary, needs.weights)) return w;
     if (rows > kSliceRows) rows = kSliceRows;
     const int64_t chunks = (vocabulary + kChunk - 1) / kChunk;
     int64_t at = 0;
@@ -1134,11 +1148,8 @@ SampleWork sample_work(int64_t rows, int32_t vocabulary) {
 template <int T>
 hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st) {
     a.chunks = (a.vocabulary + kChunk - 1) / kChunk;
-    // what the settings of all rows rule out is not launched
-    const bool k = a.how.top_k || (a.how.top_k_all > 1 && a.how.top_k_all < a.vocabulary), few = !a.how.top_k && k && a.how.top_k_all <= kFewRanks;
-    const bool top = (!a.how.temperature && a.how.temperature_all == 0.f) || (!a.how.top_k && a.how.top_k_all == 1) || (!a.how.top_p && a.how.top_p_all == 0.f);
-    const bool again = !top && !few, binned = again && (k || a.how.top_p || a.how.top_p_all < 1.f);
-    if (one_row(a.rows, a.vocabulary, again && !a.how.top_k && !a.how.temperature)) {
+    const Needs needs(&a.how, a.vocabulary);     // what it rules out is not launched
+    if (one_row(a.rows, a.vocabulary, needs.weights)) {
         k_sample_row<T><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
@@ -1155,8 +1166,8 @@ hipError_t sample(SampleArgs a, const SampleWork& w, char* work, hipStream_t st)
     for (int64_t left = a.rows; left > 0; left -= kSliceRows) {
         const unsigned rows = (unsigned)(left < kSliceRows ? left : kSliceRows), wgs = rows * (unsigned)a.chunks;
         k_sample_tops<T><<<wgs, kChunkThreads, 0, st>>>(a);
-        if (again) k_sample_chunks<T><<<wgs, kChunkThreads, 0, st>>>(a);
-        if (binned) k_sample_bins<T><<<wgs, kChunkThreads, 0, st>>>(a);
+        if (needs.again) k_sample_chunks<T><<<wgs, kChunkThreads, 0, st>>>(a);
+        if (needs.binned) k_sample_bins<T><<<wgs, kChunkThreads, 0, st>>>(a);
         k_sample_rows<T><<<rows, kThreads, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
         a.logits += (int64_t)rows * a.row_stride * kSize<T>;
@@ -1199,7 +1210,9 @@ using namespace ivftq;
 
 extern "C" {
 
-int64_t ivftq_sample_workspace(const ivftq_logits* logits) { return check_logits(logits) ? -1 : sample_work(logits->rows, logits->vocabulary).bytes; }
+int64_t ivftq_sample_workspace(const ivftq_logits* logits, const ivftq_sampling* how) {
+    return check_logits(logits) ? -1 : sample_work(logits->rows, logits->vocabulary, Needs(how, logits->vocabulary)).bytes;
+}
 
 ivftq_status ivftq_sample_tokens(const ivftq_logits* logits, const float* u, const ivftq_sampling* how, int32_t* tokens, float* logprobs, void* workspace,
                                  int64_t workspace_bytes, void* stream) {
@@ -1214,7 +1227,7 @@ ivftq_status ivftq_sample_tokens(const ivftq_logits* logits, const float* u, con
     if (!aligned(u, 4) || !aligned(tokens, 4) || !aligned(logprobs, 4) || !aligned(how->temperature, 4) || !aligned(how->top_k, 4) || !aligned(how->top_p, 4) ||
         !aligned(how->min_p, 4))
         return refuse(IVFTQ_INVALID_ARG, "u, tokens, logprobs and the arrays of settings are 4-byte aligned");
-    const SampleWork w = sample_work(logits->rows, logits->vocabulary);
+    const SampleWork w = sample_work(logits->rows, logits->vocabulary, Needs(how, logits->vocabulary));
     if (w.bytes && (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)))
         return refuse(IVFTQ_INVALID_ARG, "workspace of %lld bytes where %lld are needed, 256-byte aligned", (long long)workspace_bytes, (long long)w.bytes);
     SampleArgs a{};

@@ -24,7 +24,7 @@ class _Sampling(C.Structure):
 _P = C.c_void_p
 _SIGNATURES = {
     "ivftq_sample_tokens": (C.c_int, [_P, _P, _P, _P, _P, _P, C.c_int64, _P]),
-    "ivftq_sample_workspace": (C.c_int64, [_P]),
+    "ivftq_sample_workspace": (C.c_int64, [_P, _P]),
 }
 
 _lib = None
@@ -86,7 +86,7 @@ def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out
         out = kv._blank(rows, torch.int32, logits, stream)
     result, logs = kv._ints(out, "out", logits, rows), None if logprobs is None else kv._floats(logprobs, "logprobs", logits, (rows,))
     lib = _library()
-    need = lib.ivftq_sample_workspace(data)
+    need = lib.ivftq_sample_workspace(data, how)
     if need < 0:
         _check(1)
     work = kv._scratch(need, torch.uint8, logits, stream) if need else None

@@ -46,7 +46,7 @@ def test_every_declared_symbol_is_exported_and_bound(lib):
                                            (dict(data=C.c_void_p((1 << 20) + 1)), 1), (dict(data=ODD, type=2), 1)])
 def test_logits_that_are_refused(lib, change, status):
     assert call(lib, logits(**change)) == status
-    assert lib.ivftq_sample_workspace(C.byref(logits(**change))) == -1
+    assert lib.ivftq_sample_workspace(C.byref(logits(**change)), None) == -1
 
 
 @pytest.mark.parametrize("change", [dict(temperature_all=-0.5), dict(temperature_all=float("nan")), dict(top_k_all=-1), dict(top_p_all=-0.1), dict(top_p_all=1.5),
@@ -61,13 +61,20 @@ def test_the_rest(lib):
     assert call(lib, logits(rows=0, data=None), u=None, tokens=None) == 0
     assert lib.ivftq_sample_tokens(None, HERE, C.byref(how()), HERE, None, HERE, 1 << 40, None) == 1
     assert lib.ivftq_sample_tokens(C.byref(logits()), HERE, None, HERE, None, HERE, 1 << 40, None) == 1
-    assert lib.ivftq_sample_workspace(C.byref(logits())) == 0
+    assert lib.ivftq_sample_workspace(C.byref(logits()), None) == 0
     large = logits(vocabulary=70_000, row_stride=70_000)
-    need = lib.ivftq_sample_workspace(C.byref(large))
+    need = lib.ivftq_sample_workspace(C.byref(large), None)
     assert need > 0 and need % 256 == 0
     assert call(lib, large, size=need - 1) == call(lib, large, work=None) == call(lib, large, work=C.c_void_p((1 << 20) + 16)) == 1
     # many rows are taken a slice at a time
-    assert lib.ivftq_sample_workspace(C.byref(logits(vocabulary=70_000, row_stride=70_000, rows=5000))) < 1 << 27
+    assert lib.ivftq_sample_workspace(C.byref(logits(vocabulary=70_000, row_stride=70_000, rows=5000)), None) < 1 << 27
+    # what any settings need is enough for each
+    for v in (1000, 20_000, 40_000, 70_000):
+        for rows in (1, 255, 256):
+            x = logits(vocabulary=v, row_stride=v, rows=rows)
+            most = lib.ivftq_sample_workspace(C.byref(x), None)
+            assert all(0 <= lib.ivftq_sample_workspace(C.byref(x), C.byref(how(**s))) <= most
+                       for s in (dict(), dict(top_k=HERE), dict(temperature=HERE), dict(top_k_all=50), dict(top_k_all=5000), dict(top_p_all=0.5), dict(temperature_all=0.0)))
 
 
 @pytest.fixture
