@@ -180,6 +180,22 @@ def test_long_lists(kind, v):
         check(x, u, **how)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("v", (64, 65, 3000, 20_000, 100_000))
+def test_lists_of_a_wavefront(kind, v):
+    """As many ranks as one wavefront has lanes, one less and one more; equal logits at the last one; fewer tokens than ranks."""
+    x = logits(v, 5, v, kind)
+    x[1] = torch.randn(v, generator=torch.Generator().manual_seed(v)).to(x.dtype).round(decimals=1)
+    x[2] = (torch.arange(v, 0, -1) * 0.125).to(x.dtype)
+    x[3, torch.arange(v) % 997 != 5] = -torch.inf
+    x[4, ::2] = x[4, 1]
+    u = np.float32([0.0, 0.3, 0.999, 0.6, 1 - 2.0 ** -24])
+    for k in (2, 3, 62, 63, 64, 65, 66):
+        for how in (dict(), dict(top_p=0.9), dict(top_p=0.5, temperature=3.0), dict(min_p=0.3), dict(temperature=1e-3), dict(temperature=50.0, top_p=0.99, min_p=0.5)):
+            check(x, u, top_k=k, **how)
+            check(x, u, top_k=[k] * 5, **how)
+
+
 def test_more_rows_than_share_a_workspace():
     rows, v = 1100, 66_000
     x = logits(12, rows, v, "bf16")
