@@ -120,8 +120,7 @@ int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int
 ivftq_status ivftq_kv_digest(const ivftq_kv_cache* cache, void* digests, const int32_t* starts, void* stream);
 
 /* scores: rows x heads x columns floats; -infinity where a page holds no token that the row sees (behind its position, no page).  A page with
- * an infinite key coordinate has no number for a score (ivftq_kv_select then gives it only as one of the first or last) where no query of
- * the group has a coordinate of the sign that meets it.
+ * an infinite key coordinate has the score +infinity, and so has one whose sum float32 has no number for: nothing bounds its products.
  * q, starts, max_new as in ivftq_kv_attend; rows that it gives no result keep their scores.  workspace: ivftq_kv_score_workspace
  * bytes (starts NULL: of max_new = 1), 256-byte aligned. */
 ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts,

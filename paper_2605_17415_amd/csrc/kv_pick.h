@@ -38,6 +38,22 @@ __device__ __forceinline__ uintx4 kv_in_order(uintx4 w) {
                   __builtin_amdgcn_perm(w[3], w[1], 0x05040100u), __builtin_amdgcn_perm(w[3], w[1], 0x07060302u)};
 }
 
+// Digests whose ends are not all finite.  A coordinate that is no number in every key has an empty interval, +infinity to -infinity, and counts for
+// nothing: it is read as 0 to 0.  One end alone tells: a lowest value of +infinity, or a highest one of -infinity, stands otherwise only where every key has
+// that infinity, and then the other end keeps it.  What is left of infinities makes a sum infinite or, times a query's zero or a part that is zero, no number.
+template <bool BF>
+__device__ __forceinline__ uintx4 kv_interval(uintx4 w, bool high) {
+    const uint32_t none = (BF ? 0x7f80u : 0x7c00u) | (high ? 0x8000u : 0u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t a = w[e] & 0xffffu, b = w[e] >> 16;
+        w[e] = (a == none ? 0u : a) | (b == none ? 0u : b) << 16;
+    }
+    return w;
+}
+// Nothing bounds the products of such a page: no number stands for the largest score, in one row's kernel as in that of several.
+__device__ __forceinline__ float kv_score_of(float sum) { return sum == sum ? sum : INFINITY; }
+
 // Eight coordinates from j on of the sides of a row and head: sums of the negative ones, and of the others.
 template <int F, int D>
 __device__ __forceinline__ void score_sides(const ScoreArgs& f, int64_t row, int h, int j, float (&low)[8], float (&high)[8]) {
@@ -69,6 +85,7 @@ template <int F, int D>
 __global__ __launch_bounds__(256) void k_kv_score_one(ScoreArgs f) {
     constexpr int kPieces = D / 4, kLanes = kPieces <= 16 ? 16 : (kPieces <= 32 ? 32 : 64), kPages = 64 / kLanes, kLoads = 32 / kPages < 16 ? 32 / kPages : 16;
     constexpr int kAll = kPages * kLoads;                                 // pages of a wavefront
+    constexpr bool bf = F == IVFTQ_KV_BF16;
     const KvAttend& a = f.a;
     const KvView& c = a.c;
     const int wave = kv_wave(), lane = threadIdx.x & 63, piece = lane % kLanes, sub = lane / kLanes;
@@ -96,25 +113,33 @@ __global__ __launch_bounds__(256) void k_kv_score_one(ScoreArgs f) {
         score_sides<F, D>(f, row, h, j, low, high);
 #pragma unroll
         for (int e = 0; e < 8; ++e) side[e] = piece * 8 < D ? low[e] : (piece < kPieces ? high[e] : 0.f);
+        auto add_up = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            float v = 0.f;
+            for (int i = 0; i < kLoads; ++i) {
+                float v = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v = __builtin_fmaf(kv_to_float<F == IVFTQ_KV_BF16>(e & 1 ? w[i][e >> 1] >> 16 : w[i][e >> 1] & 0xffff), side[e], v);
-            if (kLanes > kPieces) v = piece < kPieces ? v : 0.f;
-            v = lanes8(v, Sum());
-            v += lane_moved<0x140>(v);
-            if (kLanes >= 32) v = lane_pair<false>(v, Sum());
-            if (kLanes == 64) v = lane_pair<true>(v, Sum());
-            // the lanes that write the pages of this load
+                for (int e = 0; e < 8; ++e) v = __builtin_fmaf(kv_to_float<bf>(e & 1 ? w[i][e >> 1] >> 16 : w[i][e >> 1] & 0xffff), side[e], v);
+                if (kLanes > kPieces) v = piece < kPieces ? v : 0.f;
+                v = lanes8(v, Sum());
+                v += lane_moved<0x140>(v);
+                if (kLanes >= 32) v = lane_pair<false>(v, Sum());
+                if (kLanes == 64) v = lane_pair<true>(v, Sum());
+                // the lanes that write the pages of this load
 #pragma unroll
-            for (int u = 0; u < kPages; ++u) {
-                const float of = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), u * kLanes));
-                score = lane == i * kPages + u ? of : score;
+                for (int u = 0; u < kPages; ++u) {
+                    const float of = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), u * kLanes));
+                    score = lane == i * kPages + u ? of : score;
+                }
             }
+        };
+        add_up();
+        if (__ballot(there && !(__builtin_fabsf(score) < INFINITY))) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) w[i] = kv_interval<bf>(w[i], piece * 8 >= D);
+            add_up();
         }
     }
-    if (lane < kAll && mine < c.columns) f.scores[(row * c.heads + h) * c.columns + mine] = there ? score : -INFINITY;
+    if (lane < kAll && mine < c.columns) f.scores[(row * c.heads + h) * c.columns + mine] = there ? kv_score_of(score) : -INFINITY;
 }
 
 // Sides of several rows: 32 lanes a (row, head) pair, of which D / 8 work.  (A row's operands one after the other, rows 8 KB apart,
@@ -267,6 +292,12 @@ __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
     };
 #pragma unroll
     for (int part = 0; part < kParts; ++part) ask(part, tile0);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+        if (__ballot(kv_any_not_finite<F == IVFTQ_KV_BF16>(box[t]))) {
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) box[t][k] = kv_interval<F == IVFTQ_KV_BF16>(box[t][k], k >= kSteps / 2);
+        }
     for (int tile = tile0; tile < last; ++tile) {
         const int next = tile + 1 < last ? tile + 1 : tile;
         const float mine = f.unit[((int64_t)h * f.tiles + tile) * 16 + n];
@@ -293,7 +324,7 @@ __global__ __launch_bounds__(256) void k_kv_score(ScoreArgs f) {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 const int col = col0 + 16 * t + n;
-                if (col < c.columns) out[16 * t] = col <= reach && (known[t] >> n & 1) ? acc[t][r] * unit : -INFINITY;
+                if (col < c.columns) out[16 * t] = col <= reach && (known[t] >> n & 1) ? kv_score_of(acc[t][r] * unit) : -INFINITY;
             }
         }
     }

@@ -1,0 +1,94 @@
+"""Scores of pages whose digests are not all finite numbers: one rule for one new row and for several, so that a decoding step and a chunk over
+the same cache choose the same pages."""
+import numpy as np
+import pytest
+
+import kv_pick_reference as pick
+import kv_reference as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+FORMS = [("f16", "f16"), ("bf16", "bf16"), ("code4", "bf16"), ("code4", "f16")]
+PAGE, COLUMNS = 16, 12
+INF = np.inf
+
+
+def _pkg():
+    import paper_2605_17415_amd as pkg
+    return pkg
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def planted(form, d, heads):
+    """(cache, columns whose score is infinite): a sequence of twelve full pages of which six have such keys in head 0."""
+    c = ref.Cache(d, form, heads, d, PAGE, [PAGE * COLUMNS])
+    at = [int(p) for p in c.table[0]]
+    if form == "code4":                                      # by the norms: a row's coordinates are all infinite, or no numbers
+        n = c.norms[0]
+        n[at[1], 0, 5] = INF
+        n[at[3], 0, :] = INF
+        n[at[5], 0, :] = np.nan                              # the page has no number at all
+        n[at[7], 0, 2:9] = np.nan
+        n[at[9], 0, 0], n[at[9], 0, 1] = np.nan, INF
+        return c, [1, 3, 9]
+    k = c.rows16[0]
+    k[at[1], 0, 5, 3] = INF                                  # one token
+    k[at[2], 0, 6, d - 2] = -INF
+    k[at[3], 0, :, 17], k[at[4], 0, :, 40] = INF, -INF       # every token
+    k[at[5], 0, :, 9] = np.nan                               # no token has a number there
+    k[at[6], 0, :, :] = np.nan
+    k[at[7], 0, 3, 7] = np.nan
+    k[at[8], 0, 2, 11], k[at[8], 0, 9, 11], k[at[8], 0, 4, 30] = INF, -INF, -INF
+    return c, [1, 2, 3, 4, 8]
+
+
+def score_both(c, q, starts=None):
+    """Scores of the last row alone, and of all rows."""
+    t, codec = c.device()
+    kind = torch.float16 if c.form == "code4" else ref.TYPES[c.form]
+    box = torch.full((c.pages, c.heads, 2, c.d), 7.0, dtype=kind, device=DEV)
+    _pkg().kv_digest(t["pool"], box, t["table"], t["lengths"], starts=ints([0, c.lens[0]]), **codec)
+    rows = q.shape[0]
+    one = _pkg().kv_score(q[-1:].contiguous().to(DEV), box, t["pool"], t["table"], t["lengths"], **codec)
+    all_ = _pkg().kv_score(q.to(DEV), box, t["pool"], t["table"], t["lengths"], starts=ints([0, rows]), max_new=rows, **codec)
+    return box.cpu(), one, all_, t
+
+
+def finite_box(box):
+    """Digests as scores take them: an interval that has no number is 0 to 0; infinite ends, whose pages are looked at apart, are 0 here."""
+    box = box.double().clone()
+    return torch.where(box.isinf(), 0.0, box)
+
+
+@pytest.mark.parametrize("d", (64, 96, 128, 192, 256))
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("group", (1, 3, 4, 16))
+def test_infinite_keys_and_keys_that_are_no_numbers(form, kind, d, group):
+    heads = 2
+    c, high = planted(form, d, heads)
+    g = torch.Generator().manual_seed(d + group)
+    q = torch.randn(5, heads * group, d, generator=g)
+    q[1, :group, [3, 17, 9]] = 0.0                           # nothing meets the coordinate
+    q[2, :group] = q[2, :group].abs()                        # one side alone
+    q[3, :group] = -q[3, :group].abs()
+    q[4, :group, 11] = 0.0
+    q = q.to(ref.TYPES[kind])
+    print(f"scores {form} {kind} d={d} group={group}", flush=True)
+    box, one, all_, t = score_both(c, q)
+    want, bound = pick.scores(c, q, finite_box(box), [5])
+    want[:, 0, high] = INF
+    bound[:, 0, high] = 0.0
+    for got, rows in ((one, [4]), (all_, range(5))):
+        got, want_, bound_ = got.double().cpu().numpy(), want[list(rows)], bound[list(rows)]
+        assert np.array_equal(np.isposinf(got), np.isposinf(want_)) and np.array_equal(np.isneginf(got), np.isneginf(want_))
+        fine = np.isfinite(want_)
+        assert np.isfinite(got[fine]).all() and (np.abs(got[fine] - want_[fine]) <= bound_[fine]).all()
+    a = _pkg().kv_select(one, t["lengths"], PAGE, 7).cpu().numpy()
+    b = _pkg().kv_select(all_, t["lengths"], PAGE, 7, starts=ints([0, 5])).cpu().numpy()
+    for chosen in (a[0, 0], b[4, 0]):
+        assert set(high) <= set(chosen.tolist())             # none of their keys is passed over
+    assert np.array_equal(a[0, 0], b[4, 0])
