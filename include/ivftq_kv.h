@@ -121,6 +121,7 @@ ivftq_status ivftq_kv_digest(const ivftq_kv_cache* cache, void* digests, const i
 
 /* scores: rows x heads x columns floats; -infinity where a page holds no token that the row sees (behind its position, no page).  A page with
  * an infinite key coordinate has the score +infinity, and so has one whose sum float32 has no number for: nothing bounds its products.
+ * A query's coordinate that is no finite number counts for nothing (codes: the whole query, and one whose length float32 does not hold).
  * q, starts, max_new as in ivftq_kv_attend; rows that it gives no result keep their scores.  workspace: ivftq_kv_score_workspace
  * bytes (starts NULL: of max_new = 1), 256-byte aligned. */
 ivftq_status ivftq_kv_score(const ivftq_kv_cache* cache, const ivftq_kv_rows* q, const void* digests, float* scores, const int32_t* starts,

@@ -54,13 +54,17 @@ __device__ __forceinline__ uintx4 kv_interval(uintx4 w, bool high) {
 // Nothing bounds the products of such a page: no number stands for the largest score, in one row's kernel as in that of several.
 __device__ __forceinline__ float kv_score_of(float sum) { return sum == sum ? sum : INFINITY; }
 
+// A query's coordinate that is no finite number counts for nothing: it would leave a row without scores to choose by (codes: the rotation makes all of the
+// query's coordinates none).
+__device__ __forceinline__ float kv_finite(float v) { return __builtin_fabsf(v) < INFINITY ? v : 0.f; }
+
 // Eight coordinates from j on of the sides of a row and head: sums of the negative ones, and of the others.
 template <int F, int D>
 __device__ __forceinline__ void score_sides(const ScoreArgs& f, int64_t row, int h, int j, float (&low)[8], float (&high)[8]) {
     const KvAttend& a = f.a;
 #pragma unroll
     for (int e = 0; e < 8; ++e) low[e] = high[e] = 0.f;
-    auto add = [&](int e, float v) __attribute__((always_inline)) { low[e] += fminf(v, 0.f); high[e] += fmaxf(v, 0.f); };
+    auto add = [&](int e, float v) __attribute__((always_inline)) { v = kv_finite(v); low[e] += fminf(v, 0.f); high[e] += fmaxf(v, 0.f); };
 #pragma unroll 4
     for (int i = 0; i < a.group; ++i) {
         const int64_t head = (int64_t)h * a.group + i;
@@ -218,14 +222,15 @@ __global__ __launch_bounds__(D * 2) void k_kv_rotate_sides(ScoreArgs f, int tile
         const float norm = unit.bring(x);
         turn(unit, y);
         // no coordinate of the sums is larger than the norms' sum: that goes to 2^14
-        const float most = over_group(norm);
+        const float most = over_group(kv_finite(norm));
         const int exponent = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
         const float by = most > 0.f && most < INFINITY ? ldexpf(1.f, exponent < -100 ? 113 : 13 - exponent) : 1.f;
         float low[8], high[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            low[e] = over_group(fminf(y[e] * norm, 0.f)) * by;
-            high[e] = over_group(fmaxf(y[e] * norm, 0.f)) * by;
+            const float v = kv_finite(y[e] * norm);
+            low[e] = over_group(fminf(v, 0.f)) * by;
+            high[e] = over_group(fmaxf(v, 0.f)) * by;
         }
         if (!in || n % group) continue;
         const int64_t place = (head / group) * f.tiles + row / 16;

@@ -92,3 +92,26 @@ def test_infinite_keys_and_keys_that_are_no_numbers(form, kind, d, group):
     for chosen in (a[0, 0], b[4, 0]):
         assert set(high) <= set(chosen.tolist())             # none of their keys is passed over
     assert np.array_equal(a[0, 0], b[4, 0])
+
+
+@pytest.mark.parametrize("d", (64, 128, 192))
+@pytest.mark.parametrize("form,kind", FORMS)
+@pytest.mark.parametrize("group", (1, 3, 8))
+def test_queries_that_are_no_finite_numbers(form, kind, d, group):
+    """They count for nothing: a coordinate as if it were zero; over codes, where the rotation mixes them, the whole query."""
+    heads = 2
+    c = ref.Cache(d, form, heads, d, PAGE, [PAGE * COLUMNS])
+    q = torch.randn(5, heads * group, d, generator=torch.Generator().manual_seed(d + group)).to(ref.TYPES[kind])
+    bad = [(0, 0, 5, np.nan), (1, 0, 7, INF), (1, group, d - 1, -INF), (2, group - 1, 0, np.nan), (4, 0, 3, INF), (4, heads * group - 1, 9, -INF), (4, 0, 8, np.nan)]
+    clean = q.clone()
+    for r, h, j, v in bad:
+        q[r, h, j] = v
+        clean[r, h, (slice(None) if form == "code4" else j)] = 0.0
+    q[3], clean[3] = np.nan, 0.0                             # nothing of the row is a number
+    print(f"queries {form} {kind} d={d} group={group}", flush=True)
+    box, one, all_, _ = score_both(c, q)
+    _, one_clean, all_clean, _ = score_both(c, clean)
+    assert torch.equal(one, one_clean) and torch.equal(all_, all_clean)
+    want, bound = pick.scores(c, clean, box, [5])
+    for got, rows in ((one, [4]), (all_, range(5))):
+        assert (np.abs(got.double().cpu().numpy() - want[list(rows)]) <= bound[list(rows)]).all()
