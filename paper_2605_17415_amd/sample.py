@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import numbers
 import struct
 
 import torch
@@ -59,6 +60,17 @@ def _setting(v, name, like, rows, dtype):
     return v.data_ptr(), 0
 
 
+def _settings(*values):
+    """The library's structure; values: pointers, then the numbers for all rows in its order."""
+    try:
+        return _pack_sampling(*values)
+    except (struct.error, TypeError, OverflowError):
+        for name, v, kind in zip(("temperature", "top_k", "top_p", "min_p"), values[4:], (numbers.Real, numbers.Integral, numbers.Real, numbers.Real)):
+            if not isinstance(v, kind):
+                raise TypeError(f"{name} must be a {'whole ' if kind is numbers.Integral else ''}number, or a tensor with a value for each row, got {v!r}") from None
+        raise ValueError("temperature = {!r}, top_k = {!r}, top_p = {!r}, min_p = {!r}: one does not fit 32 bits".format(*values[4:])) from None
+
+
 def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, logprobs=None, stream=None):
     """Tokens, int32 [rows], of logits [rows, vocabulary] in float32, float16 or bfloat16; u: float32 [rows] from [0, 1).
 
@@ -81,7 +93,7 @@ def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out
     k, k_all = _setting(top_k, "top_k", logits, rows, torch.int32)
     p, p_all = _setting(top_p, "top_p", logits, rows, torch.float32)
     m, m_all = _setting(min_p, "min_p", logits, rows, torch.float32)
-    how, numbers = _pack_sampling(t, k, p, m, t_all, k_all, p_all, m_all), kv._floats(u, "u", logits, (rows,))
+    how, draws = _settings(t, k, p, m, t_all, k_all, p_all, m_all), kv._floats(u, "u", logits, (rows,))
     if out is None:
         out = kv._blank(rows, torch.int32, logits, stream)
     result, logs = kv._ints(out, "out", logits, rows), None if logprobs is None else kv._floats(logprobs, "logprobs", logits, (rows,))
@@ -90,5 +102,5 @@ def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out
     if need < 0:
         _check(1)
     work = kv._scratch(need, torch.uint8, logits, stream) if need else None
-    kv._run(lib.ivftq_sample_tokens, logits, data, numbers, how, result, logs, None if work is None else work.data_ptr(), need, where)
+    kv._run(lib.ivftq_sample_tokens, logits, data, draws, how, result, logs, None if work is None else work.data_ptr(), need, where)
     return out
