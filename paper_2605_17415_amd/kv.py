@@ -28,6 +28,7 @@ from .binding import _check, ivftq_build_codebook, ivftq_haar_rotation, load_lib
 
 F16, BF16, CODE4 = range(3)
 HEAD_SIZES = (64, 96, 128, 192, 256)
+MOST_PICKS = 4096           # pages that a row and key-value head can be given
 _TYPES = {torch.float16: F16, torch.bfloat16: BF16}
 
 
@@ -320,6 +321,7 @@ def kv_digest(pool, digests, table, lengths, starts=None, rotation=None, levels=
     """Digests of the pages that hold the new rows, after kv_append has written them (and with its starts, asked and granted): a page that
     begins with a new row gets the digest of its new rows, one that goes on has them added.  With all of a sequence's tokens between
     its starts its digests are made afresh."""
+    _on_device(digests, "digests")
     d = digests.shape[-1]
     where = _digests(digests, pool, d)
     _run(_library().ivftq_kv_digest, pool, _cache(pool, table, lengths, d, rotation, levels, asked, granted), where, _starts(starts, table, pool), _stream(stream, pool))
@@ -353,7 +355,10 @@ def kv_select(scores, lengths, page, count, starts=None, first=1, last=1, out=No
         raise ValueError(f"scores must be rows x heads x columns, got {tuple(scores.shape)}")
     rows, heads, columns = scores.shape
     data, where = _floats(scores, "scores", scores, scores.shape), _stream(stream, scores)
+    _on_device(lengths, "lengths", scores)
     lens, batch = _ints(lengths, "lengths", scores), lengths.shape[0]
+    if not 1 <= count <= MOST_PICKS:
+        raise ValueError(f"count = {count}: 1 to {MOST_PICKS}")
     if out is None:
         out = _blank((rows, heads, count), torch.int32, scores, stream)
     _run(_library().ivftq_kv_select, scores, data, lens, None if starts is None else _ints(starts, "starts", scores, batch + 1), rows, batch, heads, columns, page, count,
@@ -374,6 +379,7 @@ def kv_attend_pages(q, pool, table, lengths, chosen, starts=None, max_new=None, 
     lib = _library()
     d = q.shape[-1]
     cache, rows, where = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d), _stream(stream, pool)
+    _on_device(chosen, "chosen", pool)
     if chosen.dim() != 3:
         raise ValueError(f"chosen must be rows x heads x count, got {tuple(chosen.shape)}")
     count = chosen.shape[2]
