@@ -791,9 +791,8 @@ hipError_t kv_picked_launch(const KvAttend& a, const PickWork& w, const int32_t*
         k_kv_picked_join<F, D><<<kv_grid(units, 512, (unsigned)w.col_tiles), 512, 0, st>>>(p);
     } else if constexpr (codes) {
         const ManyArgs f{a, z, zn, whole, nullptr, nullptr, nullptr, 0, 0};
-        const int64_t all = (int64_t)a.q.rows * a.q.heads, fill = all / (16 * 768);
-        const int tiles = fill < 1 ? 1 : (fill < kTurnTiles ? (int)fill : kTurnTiles);
-        k_kv_rotate_back<D, false><<<(unsigned)((all + 16 * tiles - 1) / (16 * tiles)), D * 2, 0, st>>>(f, tiles);
+        const TurnGrid turn((int64_t)a.q.rows * a.q.heads);
+        k_kv_rotate_back<D, false><<<turn.wgs, D * 2, 0, st>>>(f, turn.tiles);
     }
     return hipGetLastError();
 }
