@@ -109,7 +109,8 @@ int64_t ivftq_kv_attend_workspace(const ivftq_kv_cache* cache, int64_t rows, int
  *     low[j] = min_t k_t[j]     high[j] = max_t k_t[j]     (codes: of the rotated keys, norm * level)
  * and a row's queries with it the products that they can have with any key of the page,
  *     score = sum_g sum_j max(q_g[j] low[j], q_g[j] high[j])  >=  sum_g max_t <q_g, k_t>     (g: the key-value head's query heads).
- * Each row and key-value head attends to the pages of the highest scores.  A step of a model: ivftq_kv_append, ivftq_kv_digest,
+ * In 16 bits the digest is exact.  Over codes its ends are norm * level rounded to the nearest float16: the bounds hold to half a float16 step, 2^-11
+ * of an end, of each coordinate.  Each row and key-value head attends to the pages of the highest scores.  A step of a model: ivftq_kv_append, ivftq_kv_digest,
  * ivftq_kv_score, ivftq_kv_select, ivftq_kv_attend_pages.
  * digests: for each page, one after the other, heads x (low[d], high[d]) in the cache's type (codes: float16), 16-byte aligned; an
  * array like a pool, whose pages ivftq_kv_fork_pools and ivftq_kv_compact_pools move with the pool's. */

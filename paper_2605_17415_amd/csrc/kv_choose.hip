@@ -8,9 +8,11 @@ namespace ivftq {
 namespace {
 
 // ---- digests ---------------------------------------------------------------------------------------------------------
-// The smallest and the largest value of each key coordinate: comparisons only, so a digest is exact and the order of its tokens does not
-// matter.  Prompts of 45,000 tokens, 8 heads of 128 in codes: 16 us for 27 MB; a wavefront has one page of one head, three dependent loads and five
-// vector instructions a code.  One row a sequence: 3 us, its chain of loads.
+// The smallest and the largest value of each key coordinate: comparisons only, so the order of its tokens does not matter and a digest in 16 bits
+// is exact.  Over codes the ends are rounded to float16, to the nearest as all that is stored (once more, where a page goes on, changes nothing): an end may
+// lie half a step, 2^-11 of it, inside the keys' range, and a score that much under a bound; scores only put pages in order.
+// Prompts of 45,000 tokens, 8 heads of 128 in codes: 16 us for 27 MB; a wavefront has one page of one head, three dependent loads and five vector
+// instructions a code.  One row a sequence: 3 us, its chain of loads.
 
 // Pages of a sequence that hold new rows.
 struct NewPages { int lo, end, col0, count; };          // positions of the new rows, first column, number of pages

@@ -115,3 +115,30 @@ def test_queries_that_are_no_finite_numbers(form, kind, d, group):
     want, bound = pick.scores(c, clean, box, [5])
     for got, rows in ((one, [4]), (all_, range(5))):
         assert (np.abs(got.double().cpu().numpy() - want[list(rows)]) <= bound[list(rows)]).all()
+
+
+@pytest.mark.parametrize("d", (64, 128, 256))
+@pytest.mark.parametrize("form,kind", FORMS)
+def test_scores_bound_the_products(form, kind, d):
+    """No key of a page has larger products, summed over the group's heads, than its score: in 16 bits to the float32 sums, over codes to half a
+    float16 step of every coordinate of the digest besides."""
+    heads, group = 2, 3
+    c = ref.Cache(d, form, heads, d, PAGE, [PAGE * COLUMNS])
+    q = torch.randn(5, heads * group, d, generator=torch.Generator().manual_seed(d)).to(ref.TYPES[kind])
+    print(f"bounds {form} {kind} d={d}", flush=True)
+    box, one, all_, _ = score_both(c, q)
+    _, off = pick.scores(c, q, box, [5])
+    size = box.double().abs().amax(2).numpy()                # [pages, heads, d]
+    for h in range(heads):
+        k = c.rotated(0, 0, h, c.lens[0]).reshape(COLUMNS, PAGE, d)
+        for r in range(5):
+            z = q[r, h * group: (h + 1) * group].double().numpy()
+            if form == "code4":
+                z = z @ c.rotation.astype(np.float64).T
+            most = np.einsum("gd,ctd->gct", z, k).max(2).sum(0)
+            seen = (PAGE * COLUMNS - 5 + r) // PAGE + 1
+            # a digest is norm * level in float32 (2^-24) rounded to float16 (2^-11, under 2^-14 2^-25)
+            step = np.abs(z).sum(0) @ ((2.0 ** -11 + 2.0 ** -23) * size[c.table[0], h] + 2.0 ** -25).T if form == "code4" else 0.0
+            # (the last column's page is whole in its digest, but a row sees a part of it: its score bounds that too)
+            for got in (all_[r, h],) + ((one[0, h],) if r == 4 else ()):
+                assert (got.double().cpu().numpy()[:seen] >= (most - off[r, h] - step)[:seen]).all()
