@@ -35,6 +35,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // bits down to 2^-26 of the largest one, which counts where the heaviest token (a first token that most heads look at) has next to no
 // value and the result is made of the others; bfloat16 has range enough.  Codes: weights meet the values' norms before they are rounded,
 // so what is compared is the score plus the norm's exponent.
+// That rounding (float16 2^-11, bfloat16 2^-8 of a weight) is as large as the result's own, and the sum that divides is that of the weights as they were: results
+// in bfloat16 are off by 0.0023 of their size where operations in 32 bits with one rounding at the end are by 0.0017, in float16 by 0.00027 and 0.0002.
+// A second part of the weights would double the second product.
 template <int F> constexpr float kWeightLift = F == IVFTQ_KV_BF16 ? 0.f : 12.f;
 template <int F> constexpr float kWeightRoom = F == IVFTQ_KV_BF16 ? 8.f : 15.f;
 

@@ -10,9 +10,10 @@
 // workgroup's wavefronts take every fourth tile of 32 tokens of those; a row that has not chosen a page has it masked.  Where the units are few
 // several workgroups share a unit's tiles, and a second kernel joins their parts.
 //
-// Measured: scores of four new rows over 42,000 (head, page) pairs of 128 coordinates in bfloat16 7.5 us, 22 MB of digests (2.9 TB/s); of 794 rows over
-// up to 641 pages of codes 36 us, 18 of them the products.  Attention of 32 rows, 8 heads, over 64 pages of 64 tokens each in
-// bfloat16: 95 us for 537 MB (5.7 TB/s); of 794 rows over 16 pages each: 94 us, 1.9 GB from the L2 (20 TB/s).
+// Measured (kernels traced, medians): scores of four new rows over 42,000 (head, page) pairs of 128 coordinates in bfloat16 10.7 us (least 7.8) for 22 MB of
+// digests, over codes 12.6 behind a rotation of 6.1; of 794 rows over up to 641 pages of codes 39 us (passes among others 36.6), 19 of them the products.
+// Attention of 32 rows, 8 heads, over 64 pages of 64 tokens each in bfloat16: 96 us for 537 MB (5.6 TB/s); of 794 rows over 16 pages each: 104 us, and 93
+// where passes follow one another, 1.9 GB from the L2 (20 TB/s).
 #pragma once
 #include "kv_many.h"
 #include "wave_ops.h"

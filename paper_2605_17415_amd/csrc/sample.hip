@@ -8,13 +8,16 @@
 //   - Shorter rows are one workgroup's (k_sample_row), all of it in one launch.
 //   - The token is looked for in the chunk in which the sum passes u times all of it.
 // Where a list would be too long (thousands of tokens within a bin) the row is worked through digit by digit of the logits' order by one
-// workgroup.
+// workgroup.  For top_k up to 1,024 one group of 64 tokens that holds nothing but a finite value far under the others (a padded or masked vocabulary's lowest
+// number, -1e9) is enough: the bins reach down to it, and all other logits fall into the first.  200 rows of 128,000 with top k and top p: 21 us, 791 with the
+// last 256 tokens masked so; masked by -infinity 21.  (With the other ways the bins reach down 32 temperatures, whatever the lowest
+// logit is; the last one is open, so that a top_k over 1,024 whose last rank lies beyond lists all that is there.)
 //
 // Weights are whole numbers of 2^-42, so that partial sums of any split and order agree to the last bit, and e^x is computed in 64 bits:
 // a float32 weight is off by 2^-23, which over a hundred thousand tokens moves the drawn one in some of every thousand rows.
 //
-// Measured: 200 rows of 128,000 logits in bfloat16 with settings of all kinds 66 us, the first reading 11 (4.6 TB/s), the second and third 21 and 16,
-// of which the weights of half the rows (14 operations in 64 bits each) take a third, the rows 18 (16 us those of 400 ranks: sixteen wavefronts'
+// Measured: 200 rows of 128,000 logits in bfloat16 with settings of all kinds 67 us, the first reading 11 (4.6 TB/s), the second and third 22 and 17,
+// of which the weights of half the rows (14 operations in 64 bits each) take a third, the rows 19 (16 us those of 400 ranks: sixteen wavefronts'
 // instructions, some 2,500 cycles a digit of ten bits).  One row of 32,000 with top k and top p: 9.2 us.
 #include <hip/hip_runtime.h>
 

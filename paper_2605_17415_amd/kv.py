@@ -329,8 +329,9 @@ def kv_digest(pool, digests, table, lengths, starts=None, rotation=None, levels=
 
 def kv_score(q, digests, pool, table, lengths, starts=None, max_new=None, rotation=None, levels=None, out=None, stream=None):
     """Scores of every page for the new rows q [rows, query heads, d]: float32 [rows, heads, columns], for each key-value head the most that
-    the products of its query heads with a key of the page can add up to (-inf: the row sees nothing of it).  max_new and rows past it as
-    in kv_attend."""
+    the products of its query heads with a key of the page can add up to (-inf: the row sees nothing of it; inf: one of the page's keys is
+    infinite).  What is no number in every key counts for nothing, and so does a query's coordinate that is no finite number.  max_new and rows
+    past it as in kv_attend."""
     d = q.shape[-1]
     cache, rows, where = _cache(pool, table, lengths, d, rotation, levels), _rows(q, "q", pool, d), _stream(stream, pool)
     box, shape = _digests(digests, pool, d), (q.shape[0], pool.shape[1], table.shape[1])
